@@ -22,32 +22,32 @@ def listed():
     return [
         # --- layer norm -------------------------------------------------------------------------
         # one token of a model that is answering: nothing but latency
-        dict(name="norm forward, one token", op="norm", step="forward", n=1, d=4096, type="bf16", params="bf16"),
+        dict(name="norm_forward_one_token", op="norm", step="forward", n=1, d=4096, type="bf16", params="bf16"),
         # an odd width, binary32: no row but the first starts on a 16-byte boundary
-        dict(name="norm forward, odd width", op="norm", step="forward", n=1500, d=1001, type="f32", params="f32"),
+        dict(name="norm_forward_odd_width", op="norm", step="forward", n=1500, d=1001, type="f32", params="f32"),
         # a training batch's tokens through one norm
-        dict(name="norm forward, batch", op="norm", step="forward", n=16384, d=4096, type="bf16", params="bf16"),
+        dict(name="norm_forward_batch", op="norm", step="forward", n=16384, d=4096, type="bf16", params="bf16"),
         # a small model's batch in half precision with binary32 parameters
-        dict(name="norm backward, half", op="norm", step="backward", n=2048, d=1000, type="f16", params="f32"),
+        dict(name="norm_backward_half", op="norm", step="backward", n=2048, d=1000, type="f16", params="f32"),
         # a wide model's batch: the weight's gradient sums 16384 rows
-        dict(name="norm backward, batch", op="norm", step="backward", n=16384, d=8192, type="bf16", params="bf16"),
+        dict(name="norm_backward_batch", op="norm", step="backward", n=16384, d=8192, type="bf16", params="bf16"),
         # --- cross entropy over the vocabulary ---------------------------------------------------
         # scoring the end of one short answer with a small head
-        dict(name="loss forward, few tokens", op="loss", step="forward", n=5, v=1000, d=256, type="bf16", ignored=0.0),
+        dict(name="loss_forward_few_tokens", op="loss", step="forward", n=5, v=1000, d=256, type="bf16", ignored=0.0),
         # evaluation: the loss of a batch, no gradient
-        dict(name="loss forward, batch", op="loss", step="forward", n=2048, v=32000, d=2048, type="f16", ignored=0.0),
+        dict(name="loss_forward_batch", op="loss", step="forward", n=2048, v=32000, d=2048, type="f16", ignored=0.0),
         # a training step whose tokens, vocabulary and width fit no tile, with padding tokens
-        dict(name="loss step, ragged", op="loss", step="train", n=1023, v=50001, d=1000, type="bf16", ignored=0.1),
+        dict(name="loss_step_ragged", op="loss", step="train", n=1023, v=50001, d=1000, type="bf16", ignored=0.1),
         # a training step of a large head
-        dict(name="loss step, large", op="loss", step="train", n=8192, v=128000, d=4096, type="bf16", ignored=0.02),
+        dict(name="loss_step_large", op="loss", step="train", n=8192, v=128000, d=4096, type="bf16", ignored=0.02),
         # --- distillation from a teacher's top logits -------------------------------------------
         # how far a student is from its teacher, on a short text; some tokens have fewer entries
-        dict(name="distill forward, ragged", op="distill", step="forward", n=333, v=10007, d=776, k=20, type="f16",
+        dict(name="distill_forward_ragged", op="distill", step="forward", n=333, v=10007, d=776, k=20, type="f16",
              ignored=0.1),
         # a training step of a tiny student
-        dict(name="distill step, small", op="distill", step="train", n=64, v=8000, d=512, k=8, type="f16", ignored=0.0),
+        dict(name="distill_step_small", op="distill", step="train", n=64, v=8000, d=512, k=8, type="f16", ignored=0.0),
         # a training step of an ordinary student
-        dict(name="distill step, batch", op="distill", step="train", n=2048, v=32000, d=2048, k=64, type="bf16",
+        dict(name="distill_step_batch", op="distill", step="train", n=2048, v=32000, d=2048, k=64, type="bf16",
              ignored=0.05),
     ]
 
