@@ -51,7 +51,9 @@ extern "C" {
 
 typedef struct rsdgc_plan rsdgc_plan; /* opaque, library-owned */
 
-typedef enum { RSDGC_F32 = 0, RSDGC_BF16 = 1 } rsdgc_dtype;
+/* RSDGC_F16 (IEEE binary16) is a type of the language-model operators below; gradient arenas are
+ * binary32 or bfloat16. */
+typedef enum { RSDGC_F32 = 0, RSDGC_BF16 = 1, RSDGC_F16 = 2 } rsdgc_dtype;
 
 typedef enum {
     RSDGC_OK = 0,
@@ -333,6 +335,114 @@ int rsdgc_decompress_assign(rsdgc_plan *plan, int32_t n_workers, const int32_t *
  */
 int rsdgc_payload_to_coo(rsdgc_plan *plan, const int32_t *idx_dev, const int32_t *counts_dev,
                          int64_t *coo_index_dev, int64_t coo_capacity, void *stream);
+
+/* =========================================================================================
+ * Operators of a language model's last layers, whose weight gradients the compression takes in:
+ * a layer norm, the product with the vocabulary matrix with its loss, distillation.  (The paper
+ * trains image classifiers; these have no counterpart in it.)  They need no plan.  A weight's
+ * gradient may be written straight into a layer of a gradient arena (same type, elem_offset_l).
+ *
+ * All calls work on the current device, are enqueued on `stream`, allocate nothing, keep nothing
+ * from call to call and may be captured into a graph.  Matrices are row-major with a row stride in
+ * elements (>= the width); 16-byte alignment of rows is used where it is there and never required
+ * unless a call says so.  Where nothing else is said an optional pointer may be NULL.  Sums,
+ * statistics and losses are binary32; an output of fewer bits is rounded once, to nearest even.
+ * Results are the same bits from call to call.  Outputs must not overlap inputs or one another.
+ * ========================================================================================= */
+
+/*
+ * Layer norm of n_rows rows of `width` values:
+ *   mean = sum x / width,  rstd = (sum (x - mean)^2 / width + eps)^(-1/2),
+ *   y = (x - mean) * rstd * weight + bias.
+ * x, y: `dtype`; weight, bias (both optional: 1 and 0): param_dtype, which is `dtype` or binary32.
+ * mean_dev, rstd_dev: optional, binary32, what the backward pass takes.  n_rows = 0 does nothing.
+ * Errors: INVALID (a needed pointer NULL, stride < width, width < 1, eps negative or NaN, types),
+ * ALIGNMENT (a pointer that is not a multiple of its element size), CAPACITY (n_rows >= 2^31,
+ * width > 2^24), CUDA.
+ */
+int rsdgc_layer_norm_forward(const void *x_dev, int64_t x_stride, const void *weight_dev, const void *bias_dev,
+                             void *y_dev, int64_t y_stride, float *mean_dev, float *rstd_dev, int64_t n_rows,
+                             int64_t width, int32_t dtype, int32_t param_dtype, float eps, void *stream);
+
+/*
+ * Its gradient for a given dy, with g = dy * weight and xhat = (x - mean) * rstd:
+ *   dx = rstd * (g - mean(g) - xhat * mean(g * xhat)),
+ *   dweight = sum over rows of dy * xhat,  dbias = sum over rows of dy.
+ * dx_dev, dweight_dev, dbias_dev: each optional, one at least; dweight and dbias are `width` values of
+ * grad_dtype (any of the three types) and are overwritten, with zeros when n_rows = 0.
+ * workspace_dev: rsdgc_layer_norm_workspace_bytes() bytes, 16-byte aligned, needed for dweight or dbias.
+ * Errors: as above.
+ */
+int64_t rsdgc_layer_norm_workspace_bytes(int64_t n_rows, int64_t width);
+int rsdgc_layer_norm_backward(const void *dy_dev, int64_t dy_stride, const void *x_dev, int64_t x_stride,
+                              const void *weight_dev, const float *mean_dev, const float *rstd_dev, void *dx_dev,
+                              int64_t dx_stride, void *dweight_dev, void *dbias_dev, int32_t grad_dtype,
+                              int64_t n_rows, int64_t width, int32_t dtype, int32_t param_dtype,
+                              void *workspace_dev, void *stream);
+
+/*
+ * The vocabulary head with its loss: logits z = hidden weight^T (n_tokens x vocab), never stored.
+ *   lse[n] = log sum_v exp(z[n][v]),  loss[n] = lse[n] - z[n][labels[n]].
+ * hidden (n_tokens x width) and weight (vocab x width): `dtype`, bfloat16 or binary16; 16-byte aligned,
+ * strides multiples of 8 (any width).  labels: int64; a negative label means "no loss here" (loss 0, no
+ * gradient), one >= vocab gives a NaN loss and no gradient.  loss, lse: binary32; lse is what the
+ * backward pass takes and may be NULL.  workspace_dev: rsdgc_head_workspace_bytes() bytes with
+ * n_targets = 1, 256-byte aligned; nothing in it has to survive between calls.
+ * Errors: INVALID (a needed pointer NULL, stride < width, sizes < 1, types), ALIGNMENT,
+ * CAPACITY (n_tokens > 2^24, vocab > 2^28, width > 2^20, n_targets > 1024), CUDA.
+ */
+int64_t rsdgc_head_workspace_bytes(int64_t n_tokens, int64_t vocab, int64_t width, int64_t n_targets);
+int rsdgc_head_loss_forward(const void *hidden_dev, int64_t hidden_stride, const void *weight_dev,
+                            int64_t weight_stride, const int64_t *labels_dev, float *loss_dev, float *lse_dev,
+                            int64_t n_tokens, int64_t vocab, int64_t width, int32_t dtype, void *workspace_dev,
+                            void *stream);
+
+/*
+ * Its gradient for a given d(sum)/d(loss[n]) = grad_loss[n] (binary32):
+ *   dz[n][v] = grad_loss[n] * (exp(z[n][v] - lse[n]) - [v == labels[n]]),
+ *   dhidden = dz weight,  dweight = dz^T hidden.
+ * The logits are computed again, a piece of the vocabulary at a time.  dz is rounded to `dtype` as the two
+ * products' operand (binary16: scaled by a power of two first); the products add up in binary32.
+ * dhidden: `dtype`; dweight: dweight_dtype, which is `dtype` or binary32 (then still with dz's rounding in
+ * it); both are overwritten; any stride >= width.  n_tokens = 0 sets dweight to zero.  A row of hidden that
+ * is not finite makes dweight NaN even where its label is negative (0 * NaN), as the formula does.
+ * Errors: as above.
+ */
+int rsdgc_head_loss_backward(const void *hidden_dev, int64_t hidden_stride, const void *weight_dev,
+                             int64_t weight_stride, const int64_t *labels_dev, const float *lse_dev,
+                             const float *grad_loss_dev, void *dhidden_dev, int64_t dhidden_stride,
+                             void *dweight_dev, int64_t dweight_stride, int32_t dweight_dtype, int64_t n_tokens,
+                             int64_t vocab, int64_t width, int32_t dtype, void *workspace_dev, void *stream);
+
+/*
+ * The same head trained towards a teacher's n_targets top logits per token, at temperature T > 0:
+ *   q[n] = softmax over the given entries of top_logit[n] / T,
+ *   lse[n] = log sum_v exp(z[n][v] / T),
+ *   loss[n] = T^2 * sum_j q[n][j] * (log q[n][j] - (z[n][top_index[n][j]] / T - lse[n])),
+ *   dz[n][v] = grad_loss[n] * T * (exp(z[n][v] / T - lse[n]) - sum over j with top_index[n][j] == v of q[n][j]).
+ * top_index: int64, in any order, entries may repeat; a negative index leaves the entry out; a token whose
+ * entries are all left out, or all -inf, has loss 0 and no gradient; an index >= vocab gives a NaN loss
+ * and no gradient.  top_logit: top_dtype, any of the three types.  Both n_tokens x n_targets with row
+ * strides >= n_targets.  workspace_dev: as above, for this n_targets.  Errors: as above.
+ */
+int rsdgc_head_distill_forward(const void *hidden_dev, int64_t hidden_stride, const void *weight_dev,
+                               int64_t weight_stride, const int64_t *top_index_dev, int64_t top_index_stride,
+                               const void *top_logit_dev, int64_t top_logit_stride, int32_t top_dtype,
+                               int64_t n_targets, float temperature, float *loss_dev, float *lse_dev,
+                               int64_t n_tokens, int64_t vocab, int64_t width, int32_t dtype, void *workspace_dev,
+                               void *stream);
+int rsdgc_head_distill_backward(const void *hidden_dev, int64_t hidden_stride, const void *weight_dev,
+                                int64_t weight_stride, const int64_t *top_index_dev, int64_t top_index_stride,
+                                const void *top_logit_dev, int64_t top_logit_stride, int32_t top_dtype,
+                                int64_t n_targets, float temperature, const float *lse_dev,
+                                const float *grad_loss_dev, void *dhidden_dev, int64_t dhidden_stride,
+                                void *dweight_dev, int64_t dweight_stride, int32_t dweight_dtype, int64_t n_tokens,
+                                int64_t vocab, int64_t width, int32_t dtype, void *workspace_dev, void *stream);
+
+/* Waits for the stream, copies the status bits that the operators above have raised on the current
+ * device since the last call to *flags_host (RSDGC_STATUS_TIMEOUT: a bounded on-chip wait gave up,
+ * results are invalid) and clears them. */
+int rsdgc_operator_status(void *stream, uint32_t *flags_host);
 
 /* Waits for the stream, copies the device status word to *out_host and clears it. */
 int rsdgc_get_status(rsdgc_plan *plan, void *stream, rsdgc_status *out_host);

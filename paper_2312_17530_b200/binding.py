@@ -14,7 +14,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 # RSDGC_LIBRARY selects another build of the same library (e.g. the bounds-checked one)
 LIB_PATH = os.environ.get("RSDGC_LIBRARY") or os.path.join(_HERE, "librsdgc_b200.so")
 
-RSDGC_F32, RSDGC_BF16 = 0, 1
+RSDGC_F32, RSDGC_BF16, RSDGC_F16 = 0, 1, 2
 KEEP_AT_LEAST_ONE = 1
 NO_BULK_COPY = 2
 MOMENTUM = 4
@@ -30,7 +30,10 @@ EXPORTS = [
     "rsdgc_strerror", "rsdgc_last_cuda_error", "rsdgc_profile_enable", "rsdgc_profile_read",
     "rsdgc_update_ratios_noalloc", "rsdgc_compress_momentum", "rsdgc_plan_reserve_workers",
     "rsdgc_compress_workers", "rsdgc_decompress_assign", "rsdgc_payload_to_coo", "rsdgc_compress_workers_host",
-    "rsdgc_selftest_bounded_wait", "rsdgc_plan_tail_slices",
+    "rsdgc_selftest_bounded_wait", "rsdgc_plan_tail_slices", "rsdgc_operator_status",
+    "rsdgc_layer_norm_workspace_bytes", "rsdgc_layer_norm_forward", "rsdgc_layer_norm_backward",
+    "rsdgc_head_workspace_bytes", "rsdgc_head_loss_forward", "rsdgc_head_loss_backward", "rsdgc_head_distill_forward",
+    "rsdgc_head_distill_backward",
 ]
 NOALLOC_MAX_LAYERS = 64
 N_COMPRESS_KERNELS = 5
@@ -108,6 +111,21 @@ def lib():
         L.rsdgc_selftest_bounded_wait.argtypes = [vp, i32, vp]
         L.rsdgc_plan_tail_slices.argtypes = [vp, vp, i64, vp]
         L.rsdgc_plan_tail_slices.restype = i64
+        L.rsdgc_operator_status.argtypes = [vp, C.POINTER(u32)]
+        L.rsdgc_layer_norm_workspace_bytes.argtypes = [i64, i64]
+        L.rsdgc_layer_norm_workspace_bytes.restype = i64
+        L.rsdgc_layer_norm_forward.argtypes = [vp, i64, vp, vp, vp, i64, vp, vp, i64, i64, i32, i32, f32, vp]
+        L.rsdgc_layer_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, i32, i64, i64, i32, i32,
+                                                vp, vp]
+        L.rsdgc_head_workspace_bytes.argtypes = [i64, i64, i64, i64]
+        L.rsdgc_head_workspace_bytes.restype = i64
+        L.rsdgc_head_loss_forward.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, i64, i64, i32, vp, vp]
+        L.rsdgc_head_loss_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, i32, i64, i64, i64, i32, vp,
+                                               vp]
+        L.rsdgc_head_distill_forward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i32, i64, f32, vp, vp, i64, i64, i64,
+                                                 i32, vp, vp]
+        L.rsdgc_head_distill_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i32, i64, f32, vp, vp, vp, i64, vp,
+                                                  i64, i32, i64, i64, i64, i32, vp, vp]
         L.rsdgc_launch_count.argtypes = []
         L.rsdgc_launch_count.restype = i64
         L.rsdgc_strerror.argtypes = [C.c_int]
@@ -319,6 +337,227 @@ def update_ratios_noalloc(weights, layer_offsets: Sequence[int], layer_sizes: Se
     sizes = (C.c_int64 * max(1, n))(*[int(x) for x in layer_sizes])
     _check(lib().rsdgc_update_ratios_noalloc(_ptr(weights), offs, sizes, n, global_keep, _ptr(ratios), _stream()),
            "rsdgc_update_ratios_noalloc")
+
+
+# ---- language-model operators (no plan; torch tensors on the current device) ---------------------
+_DTYPES = None
+
+
+def _dtype_code(t) -> int:
+    """rsdgc_dtype of a tensor; raises for a type the operators do not take."""
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+
+        _DTYPES = {torch.float32: RSDGC_F32, torch.bfloat16: RSDGC_BF16, torch.float16: RSDGC_F16}
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError("type %s is not taken: float32, bfloat16 or float16" % t.dtype)
+    return code
+
+
+def _on_device(*tensors) -> None:
+    """The library sees plain pointers: every tensor given has to be on the current device."""
+    import torch
+
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("a tensor is not on the current CUDA device (%d)" % dev)
+
+
+def _rows(t, n: int, d: int, what: str) -> int:
+    """Row stride of an n x d matrix whose rows are contiguous."""
+    if t.dim() != 2 or t.size(0) != n or t.size(1) != d:
+        raise ValueError("%s: a %d x %d matrix is wanted, got %s" % (what, n, d, tuple(t.shape)))
+    if d > 1 and t.stride(1) != 1:
+        raise ValueError("%s: rows have to be contiguous" % what)
+    return t.stride(0) if n > 1 else d
+
+
+def _vector(t, n: int, dtype, what: str) -> None:
+    """None, or n contiguous values (of `dtype`, where one is given)."""
+    if t is None:
+        return
+    if t.dim() != 1 or t.size(0) != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError("%s: %d contiguous values are wanted, got %s" % (what, n, tuple(t.shape)))
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError("%s: %s is wanted, got %s" % (what, dtype, t.dtype))
+
+
+def layer_norm_workspace_bytes(n_rows: int, width: int) -> int:
+    """Bytes of workspace layer_norm_backward() needs for a weight's or bias's gradient."""
+    return _size(lib().rsdgc_layer_norm_workspace_bytes(n_rows, width), "rsdgc_layer_norm_workspace_bytes")
+
+
+def _size(n: int, what: str) -> int:
+    if n < 0:
+        _check(n, what)
+    return n
+
+
+def layer_norm_forward(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5) -> None:
+    """``y`` = layer norm of the rows of ``x`` (float32, bfloat16 or float16), times ``weight`` plus ``bias``
+    (each may be None; ``x``'s type or float32).  ``mean``, ``rstd``: float32, one per row, for the backward pass."""
+    import torch
+
+    n, d = x.shape
+    _on_device(x, weight, bias, y, mean, rstd)
+    xs, ys = _rows(x, n, d, "x"), _rows(y, n, d, "y")
+    if y.dtype != x.dtype:
+        raise ValueError("y: %s is wanted, got %s" % (x.dtype, y.dtype))
+    params = weight if weight is not None else bias
+    ptype = x.dtype if params is None else params.dtype
+    _vector(weight, d, ptype, "weight")
+    _vector(bias, d, ptype, "bias")
+    _vector(mean, n, torch.float32, "mean")
+    _vector(rstd, n, torch.float32, "rstd")
+    code = _dtype_code(x)
+    _check(lib().rsdgc_layer_norm_forward(_ptr(x), xs, _ptr(weight), _ptr(bias), _ptr(y), ys, _ptr(mean), _ptr(rstd),
+                                          n, d, code, code if params is None else _dtype_code(params), eps, _stream()),
+           "rsdgc_layer_norm_forward")
+
+
+def layer_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None, workspace=None) -> None:
+    """Gradients of layer_norm_forward() for ``dy``: ``dx`` like ``x``; ``dweight``, ``dbias`` (one value per column,
+    any of the three types, e.g. a layer of a gradient arena).  Each may be None.  ``workspace``:
+    layer_norm_workspace_bytes() bytes, needed for ``dweight`` or ``dbias``."""
+    import torch
+
+    n, d = x.shape
+    _on_device(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
+    xs, gs = _rows(x, n, d, "x"), _rows(dy, n, d, "dy")
+    ds = d if dx is None else _rows(dx, n, d, "dx")
+    for t, what in ((dy, "dy"), (dx, "dx")):
+        if t is not None and t.dtype != x.dtype:
+            raise ValueError("%s: %s is wanted, got %s" % (what, x.dtype, t.dtype))
+    _vector(weight, d, None, "weight")
+    _vector(mean, n, torch.float32, "mean")
+    _vector(rstd, n, torch.float32, "rstd")
+    grads = dweight if dweight is not None else dbias
+    _vector(dweight, d, None, "dweight")
+    _vector(dbias, d, None if grads is None else grads.dtype, "dbias")
+    if grads is not None and (workspace is None or
+                              workspace.numel() * workspace.element_size() < layer_norm_workspace_bytes(n, d)):
+        raise ValueError("workspace: %d bytes are wanted" % layer_norm_workspace_bytes(n, d))
+    code = _dtype_code(x)
+    _check(lib().rsdgc_layer_norm_backward(_ptr(dy), gs, _ptr(x), xs, _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dx), ds,
+                                           _ptr(dweight), _ptr(dbias),
+                                           RSDGC_F32 if grads is None else _dtype_code(grads), n, d, code,
+                                           code if weight is None else _dtype_code(weight), _ptr(workspace), _stream()),
+           "rsdgc_layer_norm_backward")
+
+
+def head_workspace_bytes(n_tokens: int, vocab: int, width: int, n_targets: int = 1) -> int:
+    """Bytes of workspace (256-byte aligned) that the calls on a vocabulary head need; ``n_targets``: entries of the
+    teacher per token (1 for labels)."""
+    return _size(lib().rsdgc_head_workspace_bytes(n_tokens, vocab, width, n_targets), "rsdgc_head_workspace_bytes")
+
+
+def _head_args(hidden, weight, workspace, n_targets: int, *others):
+    """(n, v, d, hidden stride, weight stride, type) of a vocabulary head, after the checks all its calls share."""
+    if hidden.dim() != 2 or weight.dim() != 2:
+        raise ValueError("hidden and weight have to be matrices")
+    n, d = hidden.shape
+    v = weight.size(0)
+    _on_device(hidden, weight, workspace, *others)
+    if weight.dtype != hidden.dtype:
+        raise ValueError("weight: %s is wanted, got %s" % (hidden.dtype, weight.dtype))
+    hs, ws = _rows(hidden, n, d, "hidden"), _rows(weight, v, d, "weight")
+    # the stride of a single row is free
+    hs, ws = hs if n > 1 else (d + 7) // 8 * 8, ws if v > 1 else (d + 7) // 8 * 8
+    size = head_workspace_bytes(n, v, d, n_targets)
+    if workspace.numel() * workspace.element_size() < size:
+        raise ValueError("workspace: %d bytes are wanted" % size)
+    return n, v, d, hs, ws, _dtype_code(hidden)
+
+
+def _head_grad_args(hidden, weight, lse, grad_loss, dhidden, dweight):
+    import torch
+
+    n, d = hidden.shape
+    _vector(lse, n, torch.float32, "lse")
+    _vector(grad_loss, n, torch.float32, "grad_loss")
+    if dhidden.dtype != hidden.dtype:
+        raise ValueError("dhidden: %s is wanted, got %s" % (hidden.dtype, dhidden.dtype))
+    return _rows(dhidden, n, d, "dhidden"), _rows(dweight, weight.size(0), d, "dweight"), _dtype_code(dweight)
+
+
+def _labels(labels, n: int) -> None:
+    import torch
+
+    if labels is None:
+        raise ValueError("labels are wanted")
+    _vector(labels, n, torch.int64, "labels")
+
+
+def head_loss_forward(hidden, weight, labels, loss, lse, workspace) -> None:
+    """``loss`` = cross entropy of the logits ``hidden`` @ ``weight``.T with ``labels`` (int64; negative: no loss), ``lse``
+    = their log-sum-exp (None where no backward pass follows), both float32, without storing the logits.  bfloat16 or
+    float16, rows 16-byte aligned."""
+    import torch
+
+    n, v, d, hs, ws, code = _head_args(hidden, weight, workspace, 1, labels, loss, lse)
+    _labels(labels, n)
+    _vector(loss, n, torch.float32, "loss")
+    _vector(lse, n, torch.float32, "lse")
+    _check(lib().rsdgc_head_loss_forward(_ptr(hidden), hs, _ptr(weight), ws, _ptr(labels), _ptr(loss), _ptr(lse), n, v, d,
+                                         code, _ptr(workspace), _stream()), "rsdgc_head_loss_forward")
+
+
+def head_loss_backward(hidden, weight, labels, lse, grad_loss, dhidden, dweight, workspace) -> None:
+    """Gradients of head_loss_forward() for ``grad_loss`` (float32, one per token): ``dhidden`` like ``hidden``, ``dweight``
+    vocab x width in ``weight``'s type or float32, e.g. a layer of a gradient arena."""
+    n, v, d, hs, ws, code = _head_args(hidden, weight, workspace, 1, labels, lse, grad_loss, dhidden, dweight)
+    _labels(labels, n)
+    dhs, dws, dwt = _head_grad_args(hidden, weight, lse, grad_loss, dhidden, dweight)
+    _check(lib().rsdgc_head_loss_backward(_ptr(hidden), hs, _ptr(weight), ws, _ptr(labels), _ptr(lse), _ptr(grad_loss),
+                                          _ptr(dhidden), dhs, _ptr(dweight), dws, dwt, n, v, d, code, _ptr(workspace),
+                                          _stream()), "rsdgc_head_loss_backward")
+
+
+def _top_args(top_index, top_logit, n: int):
+    import torch
+
+    if top_index.dim() != 2 or top_index.dtype != torch.int64:
+        raise ValueError("top_index: an int64 matrix is wanted")
+    k = top_index.size(1)
+    i, l = _rows(top_index, n, k, "top_index"), _rows(top_logit, n, k, "top_logit")
+    return k, i, l, _dtype_code(top_logit)
+
+
+def head_distill_forward(hidden, weight, top_index, top_logit, temperature: float, loss, lse, workspace) -> None:
+    """``loss`` = T^2 KL(teacher || student) per token, the teacher being the softmax of its top logits ``top_logit`` at
+    the vocabulary entries ``top_index`` (int64, negative: entry left out) and the student that of ``hidden`` @
+    ``weight``.T, both at temperature T; ``lse`` = log-sum-exp of the student's logits / T."""
+    import torch
+
+    k, istride, lstride, tcode = _top_args(top_index, top_logit, hidden.size(0))
+    n, v, d, hs, ws, code = _head_args(hidden, weight, workspace, k, top_index, top_logit, loss, lse)
+    _vector(loss, n, torch.float32, "loss")
+    _vector(lse, n, torch.float32, "lse")
+    _check(lib().rsdgc_head_distill_forward(_ptr(hidden), hs, _ptr(weight), ws, _ptr(top_index), istride, _ptr(top_logit),
+                                            lstride, tcode, k, temperature, _ptr(loss), _ptr(lse), n, v, d, code,
+                                            _ptr(workspace), _stream()), "rsdgc_head_distill_forward")
+
+
+def head_distill_backward(hidden, weight, top_index, top_logit, temperature: float, lse, grad_loss, dhidden, dweight,
+                          workspace) -> None:
+    """Gradients of head_distill_forward(), as head_loss_backward() gives them."""
+    k, istride, lstride, tcode = _top_args(top_index, top_logit, hidden.size(0))
+    n, v, d, hs, ws, code = _head_args(hidden, weight, workspace, k, top_index, top_logit, lse, grad_loss, dhidden, dweight)
+    dhs, dws, dwt = _head_grad_args(hidden, weight, lse, grad_loss, dhidden, dweight)
+    _check(lib().rsdgc_head_distill_backward(_ptr(hidden), hs, _ptr(weight), ws, _ptr(top_index), istride, _ptr(top_logit),
+                                             lstride, tcode, k, temperature, _ptr(lse), _ptr(grad_loss), _ptr(dhidden), dhs,
+                                             _ptr(dweight), dws, dwt, n, v, d, code, _ptr(workspace), _stream()),
+           "rsdgc_head_distill_backward")
+
+
+def operator_status() -> int:
+    """Status bits raised by the operators since the last call (waits for the current stream, clears them)."""
+    flags = C.c_uint32()
+    _check(lib().rsdgc_operator_status(_stream(), C.byref(flags)), "rsdgc_operator_status")
+    return flags.value
 
 
 def launch_count() -> int:

@@ -1,0 +1,1077 @@
+// The vocabulary head: softmax cross entropy and distillation from a teacher's top logits, forward and
+// backward, straight from the hidden states and the vocabulary matrix, without keeping the logits.
+//
+//   z = h W^T (n x V),  c = 1 / T,  lse_n = log sum_v exp(c z_nv)
+//   labels:    loss_n = lse_n - z_{n, y_n}                                             (T = 1)
+//   top logits: q = softmax of the k given logits / T, loss_n = T^2 sum_j q_j (log q_j - (c z_{n, i_j} - lse_n))
+//   gradient:  dz_nv = g_n T (softmax(c z)_nv - target_nv),  dh = dz W,  dW = dz^T h
+//
+// Both losses are the same computation: a target distribution with k entries per row.  Three matrix products
+// carry it, all by one persistent kernel (k_head) that differs only in what it does with a finished tile:
+//   forward   z tile -> per row and 128 columns the maximum and the sum of exponentials, and z at the targets
+//   backward  z tile again (recomputed) -> dz of one piece of the vocabulary, 16 bits, in the workspace
+//             dz W_piece -> added to dh;  dz^T h -> the piece's rows of dW
+// A piece is as wide as keeps dz in the L2 cache between its writer and its two readers.
+//
+// The tile kernel: pairs of CTAs (cluster of 2) compute 256 x 256 tiles with tcgen05.mma.cta_group::2, K in steps
+// of 64; each CTA loads its 128 rows of either operand by TMA (128-byte swizzle) through a ring of kStages
+// stages, the accumulators of two tiles alternate in the 512 TMEM columns, so that eight warps empty one while
+// the other is filled.  Operands whose contraction index is not the contiguous one (W in dz W, both in dz^T h)
+// are read as they lie in memory: the MMA takes them as MN-major.
+#include <cuda.h>
+
+#include <climits>
+#include <cmath>
+#include <cstring>
+#include <mutex>
+#include <type_traits>
+
+#include "device_utils.cuh"
+#include "operators_internal.cuh"
+
+namespace rsdgc {
+
+constexpr int kTile = 256;          // rows and columns of a pair's tile
+constexpr int kHalf = 128;          // rows of either operand that one CTA holds
+constexpr int kStepK = 64;          // contraction step: 64 x 2 bytes = the 128-byte swizzle span
+constexpr int kBoxBytes = 64 * kStepK * 2;
+constexpr int kOperandBytes = 2 * kBoxBytes;
+constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kStages = 6;
+constexpr int kEpilogueWarps = 8;
+constexpr int kHeadThreads = 128 + 32 * kEpilogueWarps;  // producer, MMA, two idle warps, epilogue
+constexpr int kHeadSmem = kStages * kStageBytes + 1024;
+constexpr unsigned kHeadSpin = 1u << 20;  // polls of a wait before it gives up
+constexpr int kMaxTargets = 1024;
+constexpr int kNoTarget = INT_MAX;
+
+enum { kModeForward = 0, kModeLogitGrad = 1, kModeProducts = 2 };
+
+// One matrix product C (m x n) = A B^T over k: tensor maps with boxes of 64 x 64 elements.
+struct __align__(64) HeadJob {
+    CUtensorMap a, b;
+    int a_mn, b_mn;          // the operand lies with its rows (not k) contiguous
+    int m_tiles, n_tiles, k_steps, band;
+};
+
+struct HeadParams {
+    HeadJob job[2];
+    int n_jobs;
+    int n;                   // tokens
+    int vocab;               // columns of this launch (the vocabulary, or the piece)
+    long long v0;            // first of them
+    long long vocab_total;
+    float c2;                // log2(e) / T
+    // targets: labels (k == 0), or k sorted entries per row
+    const long long *labels;
+    const int *target_index;
+    const float *target_q;
+    int k;
+    // forward
+    float2 *partial;         // [2 * n_tiles][n]: (maximum in log2 units, sum)
+    float *target_z;         // [n][max(k, 1)]
+    // dz
+    const float *lse, *grad, *entropy, *scale;
+    float temperature;
+    void *dz;
+    long long dz_pitch;
+    // products
+    float *dh_sum;
+    long long dh_sum_pitch;
+    void *dh;
+    long long dh_stride;
+    void *dw;
+    long long dw_stride;
+    int width;
+    int first, last;         // piece
+    unsigned int *status;
+};
+
+// ---- PTX ----------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t leader_addr(uint32_t a)  // the same variable in the pair's first CTA
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(a));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void barrier_arrive_leader(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
+        "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void mma_f16(uint32_t tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void mma_commit_both(uint32_t bar)  // arrives on both CTAs' barrier when the MMAs so far are done
+{
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+        "h"((uint16_t)3)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,"
+        "%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+// The loaded registers pass through the wait, so that nothing reads them before it.
+__device__ __forceinline__ void tmem_wait_load(uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+                   "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+                   "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
+}
+__device__ __forceinline__ float exp2_approx(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Shared-memory descriptor of an operand stage, 128-byte swizzle.  K-major: rows of 128 bytes, groups of 8 rows
+// 1024 bytes apart.  MN-major: per k a run of 64 elements (128 bytes), groups of 8 k 1024 bytes apart, the next
+// 64 elements of the row index one box further.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, int mn)
+{
+    const uint64_t lead = mn ? (uint64_t)(kBoxBytes >> 4) : 1u;
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | (lead << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+struct TilePos {
+    int job, m, n;
+};
+// Tiles of a job in bands of `band` tile rows, a band column by column: what runs at a time shares its operands in L2.
+__device__ __forceinline__ TilePos tile_pos(const HeadParams &p, int t)
+{
+    TilePos r;
+    r.job = 0;
+    const int t0 = p.job[0].m_tiles * p.job[0].n_tiles;
+    if (p.n_jobs > 1 && t >= t0) {
+        r.job = 1;
+        t -= t0;
+    }
+    const HeadJob &j = p.job[r.job];
+    const int per = j.band * j.n_tiles, b = t / per, i = t - b * per, rows = min(j.band, j.m_tiles - b * j.band);
+    r.n = i / rows;
+    r.m = b * j.band + i - r.n * rows;
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float a, float b);
+template <>
+__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__half>(float a, float b)
+{
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// 32 consecutive values of a row, rounded to Q; `count` of them exist.  16-byte stores where the row allows.
+template <typename Q>
+__device__ __forceinline__ void store_row32(Q *dst, const float (&v)[32], int count, bool vec)
+{
+    if (vec && count >= 32) {
+        if constexpr (sizeof(Q) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                reinterpret_cast<float4 *>(dst)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                reinterpret_cast<uint4 *>(dst)[i] =
+                    make_uint4(pack2<Q>(v[8 * i], v[8 * i + 1]), pack2<Q>(v[8 * i + 2], v[8 * i + 3]),
+                               pack2<Q>(v[8 * i + 4], v[8 * i + 5]), pack2<Q>(v[8 * i + 6], v[8 * i + 7]));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (i < count) dst[i] = from_f32<Q>(v[i]);
+    }
+}
+
+__device__ __forceinline__ float pick32(const float (&z)[32], int i)
+{
+    float v = z[0];
+#pragma unroll
+    for (int j = 1; j < 32; ++j) v = i == j ? z[j] : v;
+    return v;
+}
+__device__ __forceinline__ void subtract32(float (&z)[32], int i, float x)
+{
+#pragma unroll
+    for (int j = 0; j < 32; ++j) z[j] -= i == j ? x : 0.0f;
+}
+
+// A row's targets inside the columns that a thread walks, in ascending order.
+struct Targets {
+    const int *index;
+    int j, k, next;
+    __device__ __forceinline__ void start(const HeadParams &p, int row, long long col, bool live)
+    {
+        j = 0;
+        k = p.k;
+        next = kNoTarget;
+        index = p.target_index + (long long)row * k;
+        if (!live) return;
+        int lo = 0, hi = k;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (index[mid] < col) lo = mid + 1; else hi = mid;
+        }
+        j = lo;
+        if (j < k) next = index[j];
+    }
+    __device__ __forceinline__ void advance() { next = ++j < k ? index[j] : kNoTarget; }
+};
+
+// T: type of the operands (bfloat16 or binary16).  Q: type of dW.
+template <int MODE, typename T, typename Q>
+__global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant__ HeadParams p)
+{
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) unsigned long long full[kStages], empty[kStages], acc_full[2], acc_empty[2], drain;
+    __shared__ uint32_t tmem_base;
+    __shared__ volatile int dead;
+
+    const uint32_t ring = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+    int tiles = p.job[0].m_tiles * p.job[0].n_tiles;
+    if (p.n_jobs > 1) tiles += p.job[1].m_tiles * p.job[1].n_tiles;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            barrier_init(smem_addr(&full[i]), 1);
+            barrier_init(smem_addr(&empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            barrier_init(smem_addr(&acc_full[i]), 1);
+            barrier_init(smem_addr(&acc_empty[i]), 2 * kEpilogueWarps);
+        }
+        barrier_init(smem_addr(&drain), 1);
+        dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&tmem_base))
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    tmem_fence_before();
+    __syncthreads();
+    cluster_sync_all();  // the peer's barriers exist before anything arrives on them
+    tmem_fence_after();
+    grid_dependency_wait();
+    grid_dependency_launch_next();
+
+    // Bounded: a wait that gives up marks the CTA dead, raises the status bit, and every role leaves its loop.
+    auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+        for (unsigned i = 0; i < kHeadSpin; ++i) {
+            if (barrier_try(bar, parity)) return true;
+            if (dead) return false;
+        }
+        dead = 1;
+        atomicOr(p.status, RSDGC_STATUS_TIMEOUT);
+        return false;
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {  // ---- producer, in both CTAs; all bytes count on the first CTA's barriers
+            int stage = 0, it = 0;
+            uint32_t parity = 0;
+            bool ok = true;
+            for (int t = pair; t < tiles && ok; t += pairs) {
+                const TilePos tp = tile_pos(p, t);
+                const HeadJob &j = p.job[tp.job];
+                const int ra = tp.m * kTile + (int)rank * kHalf, rb = tp.n * kTile + (int)rank * kHalf;
+                for (int k = 0; k < j.k_steps; ++k) {
+                    if (!wait(smem_addr(&empty[stage]), parity ^ 1u)) {
+                        ok = false;
+                        break;
+                    }
+                    if (rank == 0) barrier_expect(smem_addr(&full[stage]), 2 * kStageBytes);
+                    const uint32_t bar = leader_addr(smem_addr(&full[stage])), dst = ring + stage * kStageBytes;
+                    const int kc = k * kStepK;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        load_box(dst + i * kBoxBytes, &j.a, j.a_mn ? ra + 64 * i : kc, j.a_mn ? kc : ra + 64 * i, bar);
+                        load_box(dst + kOperandBytes + i * kBoxBytes, &j.b, j.b_mn ? rb + 64 * i : kc,
+                                 j.b_mn ? kc : rb + 64 * i, bar);
+                    }
+                    ++it;
+                    if (++stage == kStages) {
+                        stage = 0;
+                        parity ^= 1u;
+                    }
+                }
+            }
+            // the last commits arrive on this CTA's barriers: it must not leave before they have
+            for (int i = 0; i < kStages && ok; ++i) {
+                ok = wait(smem_addr(&empty[stage]), parity ^ 1u);
+                if (++stage == kStages) {
+                    stage = 0;
+                    parity ^= 1u;
+                }
+            }
+            if (!ok && rank == 0)  // what is still in flight lands in this pair's shared memory: wait for it (bounded)
+                for (int i = it < kStages ? 0 : it - kStages; i < it; ++i) {
+                    const uint32_t bar = smem_addr(&full[i % kStages]), ph = (uint32_t)(i / kStages) & 1u;
+                    for (unsigned n = 0; n < kHeadSpin && !barrier_try(bar, ph); ++n) {}
+                }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {  // ---- MMA, the pair's first CTA
+            int stage = 0;
+            uint32_t parity = 0;
+            int local = 0;
+            bool ok = true;
+            constexpr uint32_t type = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+            for (int t = pair; t < tiles && ok; t += pairs, ++local) {
+                const TilePos tp = tile_pos(p, t);
+                const HeadJob &j = p.job[tp.job];
+                const int acc = local & 1;
+                const uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)j.a_mn << 15) |
+                                       ((uint32_t)j.b_mn << 16) | ((uint32_t)(kTile >> 3) << 17) |
+                                       ((uint32_t)(kTile >> 4) << 24);
+                const uint32_t da = j.a_mn ? 2048 >> 4 : 32 >> 4, db = j.b_mn ? 2048 >> 4 : 32 >> 4;
+                if (!wait(smem_addr(&acc_empty[acc]), (uint32_t)((local >> 1) & 1) ^ 1u)) {
+                    ok = false;
+                    break;
+                }
+                tmem_fence_after();
+                const uint32_t d = tmem_base + (uint32_t)acc * kTile;
+                for (int k = 0; k < j.k_steps; ++k) {
+                    if (!wait(smem_addr(&full[stage]), parity)) {
+                        ok = false;
+                        break;
+                    }
+                    tmem_fence_after();
+                    const uint32_t a0 = ring + stage * kStageBytes;
+                    const uint64_t a = operand_desc(a0, j.a_mn), b = operand_desc(a0 + kOperandBytes, j.b_mn);
+#pragma unroll
+                    for (int i = 0; i < kStepK / 16; ++i) mma_f16(d, a + i * da, b + i * db, idesc, (uint32_t)(k | i));
+                    mma_commit_both(smem_addr(&empty[stage]));
+                    if (++stage == kStages) {
+                        stage = 0;
+                        parity ^= 1u;
+                    }
+                }
+                if (ok) mma_commit_both(smem_addr(&acc_full[acc]));
+            }
+            if (!ok) {  // the MMAs issued so far still read shared memory and write TMEM: let them end (bounded)
+                mma_commit_both(smem_addr(&drain));
+                for (unsigned n = 0; n < kHeadSpin && !barrier_try(smem_addr(&drain), 0); ++n) {}
+            }
+        }
+    } else if (warp >= 4) {  // ---- epilogue: a thread owns one row and half of the tile's columns
+        const int quad = warp & 3, half = (warp - 4) >> 2;
+        const float c2 = p.c2;
+        int local = 0;
+        for (int t = pair; t < tiles; t += pairs, ++local) {
+            const TilePos tp = tile_pos(p, t);
+            const int acc = local & 1;
+            const int row = tp.m * kTile + (int)rank * kHalf + quad * 32 + lane;
+            const int col0 = tp.n * kTile + half * kHalf;
+            const uint32_t src = tmem_base + (uint32_t)acc * kTile + half * kHalf + ((uint32_t)(quad * 32) << 16);
+            // what a row needs, loaded before the tile is ready
+            [[maybe_unused]] Targets tg;
+            [[maybe_unused]] long long label = -1;
+            [[maybe_unused]] float gs = 0.0f, l2 = 0.0f;
+            if constexpr (MODE != kModeProducts) {
+                const bool live = row < p.n;
+                if (p.k)
+                    tg.start(p, row, p.v0 + col0, live);
+                else
+                    label = live ? p.labels[row] - p.v0 - col0 : -1;
+                if constexpr (MODE == kModeLogitGrad) {
+                    if (live) {
+                        const bool wanted = p.k ? p.entropy[row] < INFINITY : p.labels[row] >= 0 && p.labels[row] < p.vocab_total;
+                        gs = wanted ? p.grad[row] * p.temperature * (p.scale ? p.scale[0] : 1.0f) : 0.0f;
+                        l2 = p.lse[row] * 1.4426950408889634f;
+                    }
+                }
+            }
+            if (!__all_sync(0xFFFFFFFFu, wait(smem_addr(&acc_full[acc]), (uint32_t)((local >> 1) & 1)))) break;
+            tmem_fence_after();
+            [[maybe_unused]] float m = -INFINITY, s = 0.0f;
+            uint32_t raw[2][32];
+            tmem_load32(src, raw[0]);
+#pragma unroll
+            for (int ch = 0; ch < kHalf / 32; ++ch) {
+                tmem_wait_load(raw[ch & 1]);
+                if (ch + 1 < kHalf / 32) {
+                    tmem_load32(src + 32 * (ch + 1), raw[(ch + 1) & 1]);
+                } else {  // the accumulator is read: the next but one tile may overwrite it
+                    tmem_fence_before();
+                    __syncwarp();
+                    if (lane == 0) barrier_arrive_leader(smem_addr(&acc_empty[acc]));
+                }
+                float z[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(raw[ch & 1][i]);
+                const int col = col0 + 32 * ch;
+                if constexpr (MODE == kModeForward) {
+                    if (p.k) {
+                        while (tg.next < p.v0 + col + 32) {
+                            p.target_z[(long long)row * p.k + tg.j] = pick32(z, tg.next - (int)p.v0 - col);
+                            tg.advance();
+                        }
+                    } else if (label >= 32 * ch && label < 32 * ch + 32) {
+                        p.target_z[row] = pick32(z, (int)label - 32 * ch);
+                    }
+                    if (col + 32 > p.vocab) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (col + i >= p.vocab) z[i] = -INFINITY;
+                    }
+                    float top = z[0];
+#pragma unroll
+                    for (int i = 1; i < 32; ++i) top = fmaxf(top, z[i]);
+                    const float now = fmaxf(m, top * c2);
+                    const float ref = now == -INFINITY ? 0.0f : now;
+                    float add = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) add += exp2_approx(fmaf(z[i], c2, -ref));
+                    s = fmaf(s, exp2_approx(m - ref), add);
+                    m = now;
+                } else if constexpr (MODE == kModeLogitGrad) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) z[i] = gs * exp2_approx(fmaf(z[i], c2, -l2));
+                    if (p.k) {
+                        while (tg.next < p.v0 + col + 32) {
+                            subtract32(z, tg.next - (int)p.v0 - col, gs * p.target_q[(long long)row * p.k + tg.j]);
+                            tg.advance();
+                        }
+                    } else if (label >= 32 * ch && label < 32 * ch + 32) {
+                        subtract32(z, (int)label - 32 * ch, gs);
+                    }
+                    if (col + 32 > p.vocab || gs == 0.0f) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (col + i >= p.vocab || gs == 0.0f) z[i] = 0.0f;
+                    }
+                    // dz in 16 bits, as both products' operand: their sums run over it in binary32
+                    if (row < p.n) store_row32<T>((T *)p.dz + (long long)row * p.dz_pitch + col, z, 32, true);
+                } else {
+                    const float back = p.scale ? p.scale[1] : 1.0f;
+                    if (tp.job == 0) {
+                        if (row < p.n && col < p.width) {
+                            float *sum = p.dh_sum + (long long)row * p.dh_sum_pitch + col;
+                            const int count = min(32, p.width - col);
+                            if (!p.first) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    if (4 * i < count) {  // the pitch is a multiple of 4
+                                        const float4 o = reinterpret_cast<const float4 *>(sum)[i];
+                                        z[4 * i] += o.x;
+                                        z[4 * i + 1] += o.y;
+                                        z[4 * i + 2] += o.z;
+                                        z[4 * i + 3] += o.w;
+                                    }
+                                }
+                            }
+                            if (p.last) {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) z[i] *= back;
+                                T *dst = (T *)p.dh + (long long)row * p.dh_stride + col;
+                                store_row32<T>(dst, z, count, ((uintptr_t)dst & 15) == 0);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i)
+                                    if (4 * i < count)
+                                        reinterpret_cast<float4 *>(sum)[i] =
+                                            make_float4(z[4 * i], z[4 * i + 1], z[4 * i + 2], z[4 * i + 3]);
+                            }
+                        }
+                    } else if (row < p.vocab && col < p.width) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) z[i] *= back;
+                        Q *dst = (Q *)p.dw + (p.v0 + row) * p.dw_stride + col;
+                        store_row32<Q>(dst, z, min(32, p.width - col), ((uintptr_t)dst & 15) == 0);
+                    }
+                }
+            }
+            if constexpr (MODE == kModeForward)
+                if (row < p.n) p.partial[(long long)(2 * tp.n + half) * p.n + row] = make_float2(m, s);
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    cluster_sync_all();  // the peer may still signal this CTA's barriers, and its MMAs read this CTA's memory
+    if (warp == 2)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem_base));
+}
+
+// ---- the small kernels around the tiles -----------------------------------------------------------
+
+// Top logits -> per row the sorted vocabulary indices with their probabilities q (binary32 softmax of the k
+// logits / T) and sum q log q.  Entries with a negative index are left out; a row without entries gets +inf
+// (no loss), one with an index beyond the vocabulary NaN (its loss is NaN, it has no gradient).  A warp per row;
+// places are found by counting smaller entries, k^2 / 32 steps, k <= kMaxTargets.
+constexpr int kPrepWarps = 4;
+template <typename L>
+__global__ void __launch_bounds__(32 * kPrepWarps)
+k_head_targets(const long long *__restrict__ index, long long is, const L *__restrict__ logit, long long ls, int n, int k,
+               long long vocab, float inv_t, int *__restrict__ out_index, float *__restrict__ out_q,
+               float *__restrict__ entropy)
+{
+    __shared__ int sidx[kPrepWarps][kMaxTargets];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x * kPrepWarps + warp;
+    grid_dependency_wait();
+    grid_dependency_launch_next();
+    if (row >= n) return;
+    int *const mine = sidx[warp];
+    bool bad = false;
+    float top = -INFINITY;
+    for (int j = lane; j < k; j += 32) {
+        const long long i = index[row * is + j];
+        const bool in = i >= 0 && i < vocab;
+        bad |= i >= vocab;
+        mine[j] = in ? (int)i : kNoTarget;
+        if (in) {
+            const float u = to_f32(logit[row * ls + j]) * inv_t;
+            top = u > top || u != u ? u : top;
+        }
+    }
+    bad = __any_sync(0xFFFFFFFFu, bad);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+        const float o = __shfl_xor_sync(0xFFFFFFFFu, top, d);
+        top = o > top || o != o ? o : top;
+    }
+    __syncwarp();
+    if (bad || top == -INFINITY) {  // nothing to aim at
+        for (int j = lane; j < k; j += 32) out_index[(long long)row * k + j] = kNoTarget;
+        if (lane == 0) entropy[row] = bad ? NAN : INFINITY;
+        return;
+    }
+    float sum = 0.0f;
+    for (int j = lane; j < k; j += 32)
+        if (mine[j] != kNoTarget) sum += expf(to_f32(logit[row * ls + j]) * inv_t - top);
+    sum = warp_sum(sum);
+    const float log_sum = logf(sum), inv = 1.0f / sum;
+    float ent = 0.0f;
+    for (int j = lane; j < k; j += 32) {
+        const int i = mine[j];
+        int place = 0;
+        for (int o = 0; o < k; ++o) {
+            const int x = mine[o];
+            place += x < i || (x == i && o < j);
+        }
+        float q = 0.0f;
+        if (i != kNoTarget) {
+            const float u = to_f32(logit[row * ls + j]) * inv_t - top;
+            q = expf(u) * inv;
+            if (!(q == 0.0f)) ent = fmaf(q, u - log_sum, ent);
+        }
+        out_index[(long long)row * k + place] = i;
+        out_q[(long long)row * k + place] = q;
+    }
+    ent = warp_sum(ent);
+    if (lane == 0) entropy[row] = ent;
+}
+
+// Binary16 operands of the gradients' products: dz is scaled by a power of two that brings the largest
+// |grad| T to [2^13, 2^14), so that probabilities down to 2^-27 stay normal numbers; scale[1] takes it back.
+__global__ void __launch_bounds__(1024)
+k_head_scale(const float *__restrict__ grad, const long long *__restrict__ labels, const float *__restrict__ entropy, int n,
+             long long vocab, float temperature, float *__restrict__ scale)
+{
+    __shared__ float part[32];
+    grid_dependency_wait();
+    grid_dependency_launch_next();
+    float top = 0.0f;
+    for (int i = threadIdx.x; i < n; i += 1024) {
+        const bool wanted = labels ? labels[i] >= 0 && labels[i] < vocab : entropy[i] < INFINITY;
+        if (wanted) top = fmaxf(top, fabsf(grad[i]));
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 32; ++i) top = fmaxf(top, part[i]);
+        top *= temperature;
+        int e = 0;
+        if (top > 0.0f && top < INFINITY) frexpf(top, &e);  // top = f 2^e, f in [1/2, 1)
+        e = max(-100, min(100, 14 - e));
+        scale[0] = ldexpf(1.0f, e);
+        scale[1] = ldexpf(1.0f, -e);
+    }
+}
+
+// Joins a row's partial maxima and sums (two per tile column) to its log-sum-exp, and forms the loss.  32 rows
+// per CTA, the partials of a row dealt to eight warps.
+__global__ void __launch_bounds__(256)
+k_head_join(const float2 *__restrict__ partial, int parts, int n, const long long *__restrict__ labels, long long vocab,
+            const int *__restrict__ target_index, const float *__restrict__ target_q, const float *__restrict__ target_z,
+            const float *__restrict__ entropy, int k, float inv_t, float *__restrict__ loss, float *__restrict__ lse)
+{
+    __shared__ float sm[8][33], ss[8][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int row0 = blockIdx.x * 32;
+    grid_dependency_wait();
+    grid_dependency_launch_next();
+    float m = -INFINITY, s = 0.0f;
+    auto join = [&](float om, float os) {
+        const float now = fmaxf(m, om), ref = now == -INFINITY ? 0.0f : now;
+        s = s * exp2_approx(m - ref) + os * exp2_approx(om - ref);
+        m = now;
+    };
+    if (row0 + lane < n)
+        for (int i = warp; i < parts; i += 8) {
+            const float2 v = partial[(long long)i * n + row0 + lane];
+            join(v.x, v.y);
+        }
+    sm[warp][lane] = m;
+    ss[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0) {
+        for (int w = 1; w < 8; ++w) join(sm[w][lane], ss[w][lane]);
+        const float l = (m + log2f(s)) * 0.6931471805599453f;
+        sm[0][lane] = l;
+        if (row0 + lane < n) {
+            if (lse) lse[row0 + lane] = l;
+            if (!k) {
+                const long long y = labels[row0 + lane];
+                loss[row0 + lane] = y < 0 ? 0.0f : y >= vocab ? NAN : l - target_z[row0 + lane];
+            }
+        }
+    }
+    if (!k) return;
+    __syncthreads();
+    for (int r = warp; r < 32; r += 8) {
+        const int row = row0 + r;
+        if (row >= n) break;
+        float cross = 0.0f;
+        for (int j = lane; j < k; j += 32) {
+            const long long at = (long long)row * k + j;
+            if (target_index[at] != kNoTarget) {
+                const float q = target_q[at];
+                if (!(q == 0.0f)) cross = fmaf(q, sm[0][r] - target_z[at] * inv_t, cross);
+            }
+        }
+        cross = warp_sum(cross);
+        if (lane == 0) {
+            const float e = entropy[row];
+            loss[row] = e == INFINITY ? 0.0f : (e + cross) / (inv_t * inv_t);
+        }
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+namespace {
+
+typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                             const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encode_fn()
+{
+    static EncodeFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) == cudaSuccess &&
+            r == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeFn>(p);
+        else
+            (void)cudaGetLastError();
+    });
+    return fn;
+}
+
+// rows x cols values of 16 bits, boxes of 64 x 64; what lies outside reads as zero
+cudaError_t encode(CUtensorMap *map, int dtype, const void *base, long long rows, long long cols, long long stride)
+{
+    EncodeFn fn = encode_fn();
+    if (!fn) return cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)stride * 2};
+    const cuuint32_t box[2] = {64, 64}, one[2] = {1, 1};
+    const CUresult r = fn(map, dtype == RSDGC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                          const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
+inline int tiles_of(int64_t a) { return (int)((a + kTile - 1) / kTile); }
+
+// A piece of the vocabulary: dz (n x piece, 16 bits) of at most kPieceBytes, so that it is still in L2 when the
+// two products read it; never under kPieceMin columns, because every piece adds to dh once.
+constexpr int64_t kPieceBytes = 64ll << 20;
+constexpr int64_t kPieceMin = 2048;
+
+struct HeadLayout {
+    int64_t piece, pieces;
+    int64_t partial, target_z, index, q, entropy, scale, dz, dh_sum, bytes;
+    int64_t dh_pitch;
+};
+
+HeadLayout head_layout(int64_t n, int64_t v, int64_t d, int64_t k)
+{
+    HeadLayout L{};
+    int64_t most = kPieceBytes / (2 * (n > 0 ? n : 1)) / kTile * kTile;
+    if (most < kPieceMin) most = kPieceMin;
+    L.pieces = (v + most - 1) / most;
+    L.piece = up((v + L.pieces - 1) / L.pieces, kTile);
+    L.pieces = (v + L.piece - 1) / L.piece;
+    L.dh_pitch = up(d, 4);
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t p = at;
+        at = up(at + bytes, 256);
+        return p;
+    };
+    L.target_z = take(4 * n * k);
+    L.index = take(4 * n * k);
+    L.q = take(4 * n * k);
+    L.entropy = take(4 * n);
+    L.scale = take(8);
+    const int64_t shared = at;  // the forward pass's partials and the backward pass's dz share the rest
+    L.partial = take(8 * n * 2 * tiles_of(v));
+    L.bytes = at;
+    at = shared;
+    L.dz = take(2 * n * L.piece);
+    L.dh_sum = take(L.pieces > 1 ? 4 * n * L.dh_pitch : 0);
+    if (at > L.bytes) L.bytes = at;
+    return L;
+}
+
+int head_check(int64_t n, int64_t v, int64_t d, int64_t k)
+{
+    if (n < 0 || v < 1 || d < 1 || k < 1) return RSDGC_ERR_INVALID;
+    if (n > (1 << 24) || v > (1 << 28) || d > (1 << 20) || k > kMaxTargets || n * k > INT_MAX) return RSDGC_ERR_CAPACITY;
+    return RSDGC_OK;
+}
+
+struct HeadCall {
+    const void *hidden, *weight;
+    int64_t hs, ws;
+    const long long *labels;      // or
+    const long long *top_index;
+    const void *top_logit;
+    int64_t is, ls;
+    int32_t top_dtype;
+    int64_t k;                    // 0: labels
+    float temperature;
+    int64_t n, v, d;
+    int32_t dtype;
+    unsigned char *workspace;
+    cudaStream_t s;
+};
+
+int call_check(const HeadCall &c)
+{
+    int rc = head_check(c.n, c.v, c.d, c.k ? c.k : 1);
+    if (rc) return rc;
+    if (c.dtype != RSDGC_BF16 && c.dtype != RSDGC_F16) return RSDGC_ERR_INVALID;
+    if (!(c.temperature > 0.0f) || !(c.temperature < INFINITY)) return RSDGC_ERR_INVALID;
+    if (!c.weight || c.ws < c.d) return RSDGC_ERR_INVALID;
+    if (c.k && !known_dtype(c.top_dtype)) return RSDGC_ERR_INVALID;
+    if (c.n > 0) {
+        if (!c.hidden || c.hs < c.d || !c.workspace) return RSDGC_ERR_INVALID;
+        if (c.k ? !c.top_index || !c.top_logit || c.is < c.k || c.ls < c.k : !c.labels) return RSDGC_ERR_INVALID;
+        if (!pointer_aligned(c.hidden, 16) || (c.hs & 7) || !pointer_aligned(c.workspace, 256) ||
+            !pointer_aligned(c.labels, 8) || !pointer_aligned(c.top_index, 8) ||
+            (c.k && !pointer_aligned(c.top_logit, dtype_bytes(c.top_dtype))))
+            return RSDGC_ERR_ALIGNMENT;
+    }
+    if (!pointer_aligned(c.weight, 16) || (c.ws & 7)) return RSDGC_ERR_ALIGNMENT;
+    return RSDGC_OK;
+}
+
+template <int MODE, typename T, typename Q>
+cudaError_t launch_tiles(const HeadParams &p, cudaStream_t s)
+{
+    static std::once_flag once[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    static cudaError_t attr[64];
+    std::call_once(once[dev & 63], [&] {
+        attr[dev & 63] = cudaFuncSetAttribute(k_head<MODE, T, Q>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem);
+    });
+    if (attr[dev & 63] != cudaSuccess) return attr[dev & 63];
+    long long tiles = 0;
+    for (int i = 0; i < p.n_jobs; ++i) tiles += (long long)p.job[i].m_tiles * p.job[i].n_tiles;
+    if (tiles > INT_MAX) return cudaErrorInvalidValue;
+    const int most = current_device_sms() / 2;
+    const unsigned pairs = (unsigned)(tiles < most ? tiles : most);
+    return launch_chained(k_head<MODE, T, Q>, 2 * pairs, kHeadThreads, kHeadSmem, s, 2, p);
+}
+
+constexpr int kBand = 16;
+cudaError_t set_job(HeadJob &j, int dtype, const void *a, bool a_mn, long long ar, long long ac, long long as, const void *b,
+                    bool b_mn, long long br, long long bc, long long bs, long long m, long long n, long long k)
+{
+    j.a_mn = a_mn;
+    j.b_mn = b_mn;
+    j.m_tiles = tiles_of(m);
+    j.n_tiles = tiles_of(n);
+    j.k_steps = (int)((k + kStepK - 1) / kStepK);
+    j.band = j.m_tiles < kBand ? j.m_tiles : kBand;
+    const cudaError_t e = encode(&j.a, dtype, a, ar, ac, as);
+    return e == cudaSuccess ? encode(&j.b, dtype, b, br, bc, bs) : e;
+}
+
+cudaError_t targets(const HeadCall &c, const HeadLayout &L)
+{
+    if (!c.k) return cudaSuccess;
+    const unsigned grid = (unsigned)((c.n + kPrepWarps - 1) / kPrepWarps);
+    int *oi = (int *)(c.workspace + L.index);
+    float *oq = (float *)(c.workspace + L.q), *oe = (float *)(c.workspace + L.entropy);
+    const float inv_t = 1.0f / c.temperature;
+    auto go = [&](auto t) {
+        typedef decltype(t) T;
+        return launch_chained(k_head_targets<T>, grid, 32 * kPrepWarps, 0, c.s, 1, c.top_index, (long long)c.is,
+                              (const T *)c.top_logit, (long long)c.ls, (int)c.n, (int)c.k, (long long)c.v, inv_t, oi, oq, oe);
+    };
+    return c.top_dtype == RSDGC_F32 ? go(float{}) : c.top_dtype == RSDGC_BF16 ? go(__nv_bfloat16{}) : go(__half{});
+}
+
+void common_params(HeadParams &p, const HeadCall &c, const HeadLayout &L)
+{
+    p.n = (int)c.n;
+    p.vocab_total = c.v;
+    p.c2 = 1.4426950408889634f / c.temperature;
+    p.labels = c.labels;
+    p.k = (int)c.k;
+    p.target_index = (const int *)(c.workspace + L.index);
+    p.target_q = (const float *)(c.workspace + L.q);
+    p.entropy = (const float *)(c.workspace + L.entropy);
+    p.temperature = c.temperature;
+}
+
+int head_forward(const HeadCall &c, float *loss, float *lse)
+{
+    int rc = call_check(c);
+    if (rc) return rc;
+    if (c.n == 0) return RSDGC_OK;
+    if (!loss) return RSDGC_ERR_INVALID;
+    if (!pointer_aligned(loss, 4) || !pointer_aligned(lse, 4)) return RSDGC_ERR_ALIGNMENT;
+    const HeadLayout L = head_layout(c.n, c.v, c.d, c.k ? c.k : 1);
+    HeadParams p;
+    std::memset(&p, 0, sizeof p);
+    cudaError_t e = operator_status_ptr(&p.status);
+    common_params(p, c, L);
+    p.n_jobs = 1;
+    p.vocab = (int)c.v;
+    p.partial = (float2 *)(c.workspace + L.partial);
+    p.target_z = (float *)(c.workspace + L.target_z);
+    if (e == cudaSuccess)
+        e = set_job(p.job[0], c.dtype, c.hidden, false, c.n, c.d, c.hs, c.weight, false, c.v, c.d, c.ws, c.n, c.v, c.d);
+    if (e == cudaSuccess) e = targets(c, L);
+    if (e == cudaSuccess)
+        e = c.dtype == RSDGC_BF16 ? launch_tiles<kModeForward, __nv_bfloat16, __nv_bfloat16>(p, c.s)
+                                  : launch_tiles<kModeForward, __half, __half>(p, c.s);
+    if (e == cudaSuccess)
+        e = launch_chained(k_head_join, (unsigned)((c.n + 31) / 32), 256, 0, c.s, 1, (const float2 *)p.partial,
+                           2 * p.job[0].n_tiles, (int)c.n, c.labels, (long long)c.v, p.target_index, p.target_q,
+                           (const float *)p.target_z, p.entropy, (int)c.k, 1.0f / c.temperature, loss, lse);
+    return operator_result(e);
+}
+
+template <typename T, typename Q>
+cudaError_t backward_pieces(const HeadCall &c, const HeadLayout &L, HeadParams &p)
+{
+    for (int64_t i = 0; i < L.pieces; ++i) {
+        const int64_t v0 = i * L.piece, width = c.v - v0 < L.piece ? c.v - v0 : L.piece;
+        const void *w = (const unsigned char *)c.weight + v0 * c.ws * 2;
+        p.v0 = v0;
+        p.vocab = (int)width;
+        p.first = i == 0;
+        p.last = i + 1 == L.pieces;
+        p.n_jobs = 1;
+        cudaError_t e = set_job(p.job[0], c.dtype, c.hidden, false, c.n, c.d, c.hs, w, false, width, c.d, c.ws, c.n, width, c.d);
+        if (e == cudaSuccess) e = launch_tiles<kModeLogitGrad, T, T>(p, c.s);
+        if (e != cudaSuccess) return e;
+        // the tile kernel filled whole tiles of dz with zeros beyond the vocabulary, so k runs over whole steps
+        p.n_jobs = 2;
+        e = set_job(p.job[0], c.dtype, p.dz, false, c.n, L.piece, L.piece, w, true, width, c.d, c.ws, c.n, c.d, width);
+        if (e == cudaSuccess)
+            e = set_job(p.job[1], c.dtype, p.dz, true, c.n, L.piece, L.piece, c.hidden, true, c.n, c.d, c.hs, width, c.d, c.n);
+        if (e == cudaSuccess) e = launch_tiles<kModeProducts, T, Q>(p, c.s);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+int head_backward(const HeadCall &c, const float *lse, const float *grad, void *dh, int64_t dh_stride, void *dw,
+                  int64_t dw_stride, int32_t dw_dtype)
+{
+    int rc = call_check(c);
+    if (rc) return rc;
+    if (!dw || dw_stride < c.d || (dw_dtype != c.dtype && dw_dtype != RSDGC_F32)) return RSDGC_ERR_INVALID;
+    if (!pointer_aligned(dw, dtype_bytes(dw_dtype))) return RSDGC_ERR_ALIGNMENT;
+    cudaError_t e = cudaSuccess;
+    if (c.n == 0) {  // sums over nothing
+        const size_t b = (size_t)dtype_bytes(dw_dtype);
+        e = cudaMemset2DAsync(dw, (size_t)dw_stride * b, 0, (size_t)c.d * b, (size_t)c.v, c.s);
+        return operator_result(e);
+    }
+    if (!lse || !grad || !dh || dh_stride < c.d) return RSDGC_ERR_INVALID;
+    if (!pointer_aligned(lse, 4) || !pointer_aligned(grad, 4) || !pointer_aligned(dh, 2)) return RSDGC_ERR_ALIGNMENT;
+    const HeadLayout L = head_layout(c.n, c.v, c.d, c.k ? c.k : 1);
+    HeadParams p;
+    std::memset(&p, 0, sizeof p);
+    e = operator_status_ptr(&p.status);
+    common_params(p, c, L);
+    p.lse = lse;
+    p.grad = grad;
+    p.dz = c.workspace + L.dz;
+    p.dz_pitch = L.piece;
+    p.dh_sum = (float *)(c.workspace + L.dh_sum);
+    p.dh_sum_pitch = L.dh_pitch;
+    p.dh = dh;
+    p.dh_stride = dh_stride;
+    p.dw = dw;
+    p.dw_stride = dw_stride;
+    p.width = (int)c.d;
+    if (e == cudaSuccess) e = targets(c, L);
+    if (e == cudaSuccess && c.dtype == RSDGC_F16) {
+        p.scale = (const float *)(c.workspace + L.scale);
+        e = launch_chained(k_head_scale, 1, 1024, 0, c.s, 1, grad, c.labels, p.entropy, (int)c.n, (long long)c.v,
+                           c.temperature, (float *)(c.workspace + L.scale));
+    }
+    if (e == cudaSuccess) {
+        if (c.dtype == RSDGC_BF16)
+            e = dw_dtype == RSDGC_F32 ? backward_pieces<__nv_bfloat16, float>(c, L, p)
+                                      : backward_pieces<__nv_bfloat16, __nv_bfloat16>(c, L, p);
+        else
+            e = dw_dtype == RSDGC_F32 ? backward_pieces<__half, float>(c, L, p) : backward_pieces<__half, __half>(c, L, p);
+    }
+    return operator_result(e);
+}
+
+}  // namespace
+}  // namespace rsdgc
+
+using namespace rsdgc;
+
+extern "C" int64_t rsdgc_head_workspace_bytes(int64_t n_tokens, int64_t vocab, int64_t width, int64_t n_targets)
+{
+    const int rc = head_check(n_tokens, vocab, width, n_targets);
+    return rc ? rc : head_layout(n_tokens, vocab, width, n_targets).bytes;
+}
+
+extern "C" int rsdgc_head_loss_forward(const void *hidden_dev, int64_t hidden_stride, const void *weight_dev,
+                                       int64_t weight_stride, const int64_t *labels_dev, float *loss_dev, float *lse_dev,
+                                       int64_t n_tokens, int64_t vocab, int64_t width, int32_t dtype, void *workspace_dev,
+                                       void *stream)
+{
+    OperatorRange range("rsdgc_head_loss_forward");
+    const HeadCall c = {hidden_dev, weight_dev, hidden_stride, weight_stride, (const long long *)labels_dev, nullptr, nullptr,
+                        0, 0, 0, 0, 1.0f, n_tokens, vocab, width, dtype, (unsigned char *)workspace_dev, (cudaStream_t)stream};
+    return head_forward(c, loss_dev, lse_dev);
+}
+
+extern "C" int rsdgc_head_loss_backward(const void *hidden_dev, int64_t hidden_stride, const void *weight_dev,
+                                        int64_t weight_stride, const int64_t *labels_dev, const float *lse_dev,
+                                        const float *grad_loss_dev, void *dhidden_dev, int64_t dhidden_stride,
+                                        void *dweight_dev, int64_t dweight_stride, int32_t dweight_dtype, int64_t n_tokens,
+                                        int64_t vocab, int64_t width, int32_t dtype, void *workspace_dev, void *stream)
+{
+    OperatorRange range("rsdgc_head_loss_backward");
+    const HeadCall c = {hidden_dev, weight_dev, hidden_stride, weight_stride, (const long long *)labels_dev, nullptr, nullptr,
+                        0, 0, 0, 0, 1.0f, n_tokens, vocab, width, dtype, (unsigned char *)workspace_dev, (cudaStream_t)stream};
+    return head_backward(c, lse_dev, grad_loss_dev, dhidden_dev, dhidden_stride, dweight_dev, dweight_stride, dweight_dtype);
+}
+
+extern "C" int rsdgc_head_distill_forward(const void *hidden_dev, int64_t hidden_stride, const void *weight_dev,
+                                          int64_t weight_stride, const int64_t *top_index_dev, int64_t top_index_stride,
+                                          const void *top_logit_dev, int64_t top_logit_stride, int32_t top_dtype,
+                                          int64_t n_targets, float temperature, float *loss_dev, float *lse_dev,
+                                          int64_t n_tokens, int64_t vocab, int64_t width, int32_t dtype,
+                                          void *workspace_dev, void *stream)
+{
+    if (n_targets < 1) return RSDGC_ERR_INVALID;
+    OperatorRange range("rsdgc_head_distill_forward");
+    const HeadCall c = {hidden_dev, weight_dev, hidden_stride, weight_stride, nullptr, (const long long *)top_index_dev,
+                        top_logit_dev, top_index_stride, top_logit_stride, top_dtype, n_targets, temperature, n_tokens, vocab,
+                        width, dtype, (unsigned char *)workspace_dev, (cudaStream_t)stream};
+    return head_forward(c, loss_dev, lse_dev);
+}
+
+extern "C" int rsdgc_head_distill_backward(const void *hidden_dev, int64_t hidden_stride, const void *weight_dev,
+                                           int64_t weight_stride, const int64_t *top_index_dev, int64_t top_index_stride,
+                                           const void *top_logit_dev, int64_t top_logit_stride, int32_t top_dtype,
+                                           int64_t n_targets, float temperature, const float *lse_dev,
+                                           const float *grad_loss_dev, void *dhidden_dev, int64_t dhidden_stride,
+                                           void *dweight_dev, int64_t dweight_stride, int32_t dweight_dtype,
+                                           int64_t n_tokens, int64_t vocab, int64_t width, int32_t dtype,
+                                           void *workspace_dev, void *stream)
+{
+    if (n_targets < 1) return RSDGC_ERR_INVALID;
+    OperatorRange range("rsdgc_head_distill_backward");
+    const HeadCall c = {hidden_dev, weight_dev, hidden_stride, weight_stride, nullptr, (const long long *)top_index_dev,
+                        top_logit_dev, top_index_stride, top_logit_stride, top_dtype, n_targets, temperature, n_tokens, vocab,
+                        width, dtype, (unsigned char *)workspace_dev, (cudaStream_t)stream};
+    return head_backward(c, lse_dev, grad_loss_dev, dhidden_dev, dhidden_stride, dweight_dev, dweight_stride, dweight_dtype);
+}

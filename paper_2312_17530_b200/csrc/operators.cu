@@ -1,0 +1,84 @@
+// What the language-model operators share on the host: the per-device status word, NVTX ranges, results.
+#include <mutex>
+
+#include "operators_internal.cuh"
+
+#ifdef RSDGC_NVTX
+#include <nvtx3/nvToolsExt.h>
+#endif
+
+namespace rsdgc {
+
+namespace {
+constexpr int kMaxDevices = 64;
+__device__ unsigned int g_operator_status;
+}  // namespace
+
+cudaError_t operator_status_ptr(unsigned int **out)
+{
+    static std::mutex mu;
+    static void *ptrs[kMaxDevices] = {};
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    std::lock_guard<std::mutex> lock(mu);
+    if (!ptrs[dev]) {
+        void *p = nullptr;
+        e = cudaGetSymbolAddress(&p, g_operator_status);
+        if (e != cudaSuccess) return e;
+        ptrs[dev] = p;
+    }
+    *out = static_cast<unsigned int *>(ptrs[dev]);
+    return cudaSuccess;
+}
+
+int current_device_sms()
+{
+    static std::mutex mu;
+    static int sms[kMaxDevices] = {};
+    int dev = -1;
+    // without a device the sizes of a B200 are assumed, so that workspaces can be sized on the host
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) {
+        (void)cudaGetLastError();
+        return 148;
+    }
+    std::lock_guard<std::mutex> lock(mu);
+    if (!sms[dev] && cudaDeviceGetAttribute(&sms[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 148;
+    }
+    return sms[dev];
+}
+
+#ifdef RSDGC_NVTX
+OperatorRange::OperatorRange(const char *name) { nvtxRangePushA(name); }
+OperatorRange::~OperatorRange() { nvtxRangePop(); }
+#else
+OperatorRange::OperatorRange(const char *) {}
+OperatorRange::~OperatorRange() {}
+#endif
+
+int operator_result(cudaError_t e)
+{
+    if (e == cudaSuccess) return RSDGC_OK;
+    (void)cudaGetLastError();
+    set_last_cuda_error((int)e);
+    return RSDGC_ERR_CUDA;
+}
+
+}  // namespace rsdgc
+
+using namespace rsdgc;
+
+extern "C" int rsdgc_operator_status(void *stream, uint32_t *flags_host)
+{
+    if (!flags_host) return RSDGC_ERR_INVALID;
+    unsigned int *p = nullptr;
+    cudaStream_t s = (cudaStream_t)stream;
+    cudaError_t e = operator_status_ptr(&p);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(flags_host, p, sizeof(unsigned int), cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaMemsetAsync(p, 0, sizeof(unsigned int), s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    return operator_result(e);
+}

@@ -1,0 +1,79 @@
+// Declarations shared by the language-model operators (layer norm, vocabulary head): element types,
+// launch helpers and the device status word that calls without a plan report into.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "rsdgc_internal.cuh"
+
+namespace rsdgc {
+
+inline bool known_dtype(int t) { return t == RSDGC_F32 || t == RSDGC_BF16 || t == RSDGC_F16; }
+inline int dtype_bytes(int t) { return t == RSDGC_F32 ? 4 : 2; }
+inline bool pointer_aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// ---- element access: every type is widened to binary32 exactly, narrowed by one rounding (to nearest even)
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+
+__device__ __forceinline__ float warp_sum(float x)
+{
+#pragma unroll
+    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
+    return x;
+}
+
+// The status word of calls that take no plan: one per device, raised by the kernels, read and cleared by
+// rsdgc_operator_status().  *out is its device address on the current device.
+cudaError_t operator_status_ptr(unsigned int **out);
+
+// Multiprocessors of the current device, asked once per device.
+int current_device_sms();
+
+// NVTX range around an entry point (nothing without RSDGC_NVTX).
+struct OperatorRange {
+    explicit OperatorRange(const char *name);
+    ~OperatorRange();
+};
+// The entry point's return value for the launches' outcome.
+int operator_result(cudaError_t e);
+
+// Launches `kernel` so that its prologue may overlap the end of the previous kernel in the stream; the kernel
+// calls grid_dependency_wait() before it touches anything another kernel writes.
+template <typename... Params, typename... Args>
+inline cudaError_t launch_chained(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
+                                  int cluster, Args... args)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    int n = 0;
+    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n++].val.programmaticStreamSerializationAllowed = 1;
+    if (cluster > 1) {
+        at[n].id = cudaLaunchAttributeClusterDimension;
+        at[n].val.clusterDim.x = (unsigned)cluster;
+        at[n].val.clusterDim.y = 1;
+        at[n++].val.clusterDim.z = 1;
+    }
+    cfg.attrs = at;
+    cfg.numAttrs = (unsigned)n;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+    if (e == cudaSuccess) count_launch(1);
+    return e;
+}
+
+}  // namespace rsdgc
