@@ -25,41 +25,48 @@
 #include <cstring>
 #include <mutex>
 #include <type_traits>
+#include <utility>
 
 #include "device_utils.cuh"
 #include "operators_internal.cuh"
 
 namespace rsdgc {
 
-constexpr int kTile = 256;          // rows and columns of a pair's tile
-constexpr int kHalf = 128;          // rows of either operand that one CTA holds
+constexpr int kTile = 256;          // rows of a pair's tile, and columns of one accumulator
+constexpr int kHalf = 128;          // rows of an operand block that one CTA holds
 constexpr int kStepK = 64;          // contraction step: 64 x 2 bytes = the 128-byte swizzle span
 constexpr int kBoxBytes = 64 * kStepK * 2;
-constexpr int kOperandBytes = 2 * kBoxBytes;
-constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kStages = 6;
+constexpr int kBlockBytes = 2 * kBoxBytes;
+constexpr int kStageBytes = 3 * kBlockBytes;             // one block of A, one or two of B
+constexpr int kStages = 4;
 constexpr int kEpilogueWarps = 8;
 constexpr int kHeadThreads = 128 + 32 * kEpilogueWarps;  // producer, MMA, two idle warps, epilogue
 constexpr int kHeadSmem = kStages * kStageBytes + 1024;
-constexpr unsigned kHeadSpin = 1u << 20;  // polls of a wait before it gives up
+constexpr int kSlots = 4;                                // tiles announced ahead
+constexpr unsigned kHeadSpin = 1u << 20;                 // polls of a wait before it gives up
 constexpr int kMaxTargets = 1024;
 constexpr int kNoTarget = INT_MAX;
+constexpr int kMaxJobs = 3;
 
-enum { kModeForward = 0, kModeLogitGrad = 1, kModeProducts = 2 };
+enum { kForward = 0, kLogitGrad = 1, kHiddenGrad = 2, kWeightGrad = 3 };
 
-// One matrix product C (m x n) = A B^T over k: tensor maps with boxes of 64 x 64 elements.
+// One matrix product C (m x n) = A B^T over k: tensor maps with boxes of 64 x 64 elements, and what becomes of C.
 struct __align__(64) HeadJob {
     CUtensorMap a, b;
     int a_mn, b_mn;          // the operand lies with its rows (not k) contiguous
     int m_tiles, n_tiles, k_steps, band;
+    int halves;              // accumulators of a tile: 256 x 256 or 256 x 512
+    int kind;
+    int vocab;               // entries of the vocabulary this job is about (all, or a piece's)
+    long long v0;            // first of them
+    void *dz;                // the piece's buffer
+    int first, last;         // piece
 };
 
 struct HeadParams {
-    HeadJob job[2];
-    int n_jobs;
+    HeadJob job[kMaxJobs];
+    int n_jobs, tiles;
     int n;                   // tokens
-    int vocab;               // columns of this launch (the vocabulary, or the piece)
-    long long v0;            // first of them
     long long vocab_total;
     float c2;                // log2(e) / T
     // targets: labels (k == 0), or k sorted entries per row
@@ -68,14 +75,13 @@ struct HeadParams {
     const float *target_q;
     int k;
     // forward
-    float2 *partial;         // [2 * n_tiles][n]: (maximum in log2 units, sum)
+    float2 *partial;         // [2 * columns / 256][n]: (maximum in log2 units, sum)
+    int parts;
     float *target_z;         // [n][max(k, 1)]
-    // dz
+    // gradients
     const float *lse, *grad, *entropy, *scale;
     float temperature;
-    void *dz;
     long long dz_pitch;
-    // products
     float *dh_sum;
     long long dh_sum_pitch;
     void *dh;
@@ -83,7 +89,7 @@ struct HeadParams {
     void *dw;
     long long dw_stride;
     int width;
-    int first, last;         // piece
+    int *next_tile;          // counter of tiles handed out beyond the first round; NULL: fixed rounds
     unsigned int *status;
 };
 
@@ -95,12 +101,13 @@ __device__ __forceinline__ uint32_t cluster_rank()
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ uint32_t leader_addr(uint32_t a)  // the same variable in the pair's first CTA
+__device__ __forceinline__ uint32_t addr_in(uint32_t a, uint32_t rank)  // the same variable in a CTA of the pair
 {
     uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(a));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
     return r;
 }
+__device__ __forceinline__ uint32_t leader_addr(uint32_t a) { return addr_in(a, 0); }
 __device__ __forceinline__ void cluster_sync_all()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -121,13 +128,42 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
         : "memory");
     return ok != 0;
 }
+__device__ __forceinline__ bool barrier_test(uint32_t bar, uint32_t parity)  // without waiting
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool barrier_try_cluster(uint32_t bar, uint32_t parity)  // sees what the peer wrote before arriving
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void barrier_arrive_leader(uint32_t bar)
+__device__ __forceinline__ void barrier_arrive_in(uint32_t bar, uint32_t rank)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_addr(bar)) : "memory");
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr_in(bar, rank)) : "memory");
+}
+__device__ __forceinline__ void barrier_arrive_leader(uint32_t bar) { barrier_arrive_in(bar, 0); }
+__device__ __forceinline__ void store_in(uint32_t addr, int value, uint32_t rank)
+{
+    asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(addr_in(addr, rank)), "r"(value) : "memory");
 }
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
 {
@@ -176,6 +212,17 @@ __device__ __forceinline__ void tmem_wait_load(uint32_t (&r)[32])
                    "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
                    "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
 }
+// One thread of the converged warp, the same one each time; its branch is known to be taken by a single thread.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t is;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xFFFFFFFF;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(is));
+    return is != 0;
+}
 __device__ __forceinline__ float exp2_approx(float x)
 {
     float y;
@@ -200,10 +247,11 @@ __device__ __forceinline__ TilePos tile_pos(const HeadParams &p, int t)
 {
     TilePos r;
     r.job = 0;
-    const int t0 = p.job[0].m_tiles * p.job[0].n_tiles;
-    if (p.n_jobs > 1 && t >= t0) {
-        r.job = 1;
-        t -= t0;
+    int own = p.job[0].m_tiles * p.job[0].n_tiles;
+    while (r.job + 1 < p.n_jobs && t >= own) {
+        t -= own;
+        ++r.job;
+        own = p.job[r.job].m_tiles * p.job[r.job].n_tiles;
     }
     const HeadJob &j = p.job[r.job];
     const int per = j.band * j.n_tiles, b = t / per, i = t - b * per, rows = min(j.band, j.m_tiles - b * j.band);
@@ -285,12 +333,14 @@ struct Targets {
     __device__ __forceinline__ void advance() { next = ++j < k ? index[j] : kNoTarget; }
 };
 
-// T: type of the operands (bfloat16 or binary16).  Q: type of dW.
-template <int MODE, typename T, typename Q>
+// T: type of the operands (bfloat16 or binary16).  Q: type of dW.  BACK: the launch's jobs are gradients.
+template <bool BACK, typename T, typename Q>
 __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant__ HeadParams p)
 {
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long full[kStages], empty[kStages], acc_full[2], acc_empty[2], drain;
+    __shared__ __align__(8) unsigned long long slot_full[kSlots], slot_empty[kSlots];
+    __shared__ int slot_tile[kSlots];
     __shared__ uint32_t tmem_base;
     __shared__ volatile int dead;
 
@@ -298,9 +348,6 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-
-    int tiles = p.job[0].m_tiles * p.job[0].n_tiles;
-    if (p.n_jobs > 1) tiles += p.job[1].m_tiles * p.job[1].n_tiles;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
@@ -310,6 +357,10 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
         for (int i = 0; i < 2; ++i) {
             barrier_init(smem_addr(&acc_full[i]), 1);
             barrier_init(smem_addr(&acc_empty[i]), 2 * kEpilogueWarps);
+        }
+        for (int i = 0; i < kSlots; ++i) {
+            barrier_init(smem_addr(&slot_full[i]), 1);
+            barrier_init(smem_addr(&slot_empty[i]), 2 * (1 + kEpilogueWarps));
         }
         barrier_init(smem_addr(&drain), 1);
         dead = 0;
@@ -326,16 +377,30 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
     tmem_fence_after();
     grid_dependency_wait();
     grid_dependency_launch_next();
+    asm volatile("fence.proxy.async.global;" ::: "memory");  // dz was written by ordinary stores, TMA reads it
 
     // Bounded: a wait that gives up marks the CTA dead, raises the status bit, and every role leaves its loop.
+    auto give_up = [&]() -> bool {
+        dead = 1;
+        atomicOr(p.status, RSDGC_STATUS_TIMEOUT);
+        return false;
+    };
     auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
         for (unsigned i = 0; i < kHeadSpin; ++i) {
             if (barrier_try(bar, parity)) return true;
             if (dead) return false;
         }
-        dead = 1;
-        atomicOr(p.status, RSDGC_STATUS_TIMEOUT);
-        return false;
+        return give_up();
+    };
+    // The pair's next tile, announced by the first CTA's producer `i` tiles after the first; -1 after a wait that gave up.
+    auto next_tile = [&](int i) -> int {
+        const uint32_t bar = smem_addr(&slot_full[i % kSlots]), parity = (uint32_t)(i / kSlots) & 1u;
+        for (unsigned n = 0; n < kHeadSpin; ++n) {
+            if (barrier_try_cluster(bar, parity)) return *(volatile int *)&slot_tile[i % kSlots];
+            if (dead) return -1;
+        }
+        give_up();
+        return -1;
     };
 
     if (warp == 0) {
@@ -343,29 +408,57 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
             int stage = 0, it = 0;
             uint32_t parity = 0;
             bool ok = true;
-            for (int t = pair; t < tiles && ok; t += pairs) {
+            for (int t = pair, i = 0; t < p.tiles; ++i) {
+                int after = 0;
+                if (rank == 0) {  // fetch and announce the tile after this one
+                    after = p.next_tile ? pairs + atomicAdd(p.next_tile, 1) : t + pairs;
+                    if (!wait(smem_addr(&slot_empty[i % kSlots]), ((uint32_t)(i / kSlots) & 1u) ^ 1u)) {
+                        ok = false;
+                        break;
+                    }
+                    for (uint32_t r = 0; r < 2; ++r) {
+                        store_in(smem_addr(&slot_tile[i % kSlots]), after, r);
+                        barrier_arrive_in(smem_addr(&slot_full[i % kSlots]), r);
+                    }
+                }
                 const TilePos tp = tile_pos(p, t);
                 const HeadJob &j = p.job[tp.job];
-                const int ra = tp.m * kTile + (int)rank * kHalf, rb = tp.n * kTile + (int)rank * kHalf;
+                const int halves = j.halves;
+                const int ra = tp.m * kTile + (int)rank * kHalf, rb = tp.n * halves * kTile + (int)rank * kHalf;
                 for (int k = 0; k < j.k_steps; ++k) {
                     if (!wait(smem_addr(&empty[stage]), parity ^ 1u)) {
                         ok = false;
                         break;
                     }
-                    if (rank == 0) barrier_expect(smem_addr(&full[stage]), 2 * kStageBytes);
+                    if (rank == 0) barrier_expect(smem_addr(&full[stage]), 2 * (1 + halves) * kBlockBytes);
                     const uint32_t bar = leader_addr(smem_addr(&full[stage])), dst = ring + stage * kStageBytes;
                     const int kc = k * kStepK;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
+                    for (int i = 0; i < 2; ++i)
                         load_box(dst + i * kBoxBytes, &j.a, j.a_mn ? ra + 64 * i : kc, j.a_mn ? kc : ra + 64 * i, bar);
-                        load_box(dst + kOperandBytes + i * kBoxBytes, &j.b, j.b_mn ? rb + 64 * i : kc,
-                                 j.b_mn ? kc : rb + 64 * i, bar);
+                    for (int h = 0; h < halves; ++h) {
+                        const int r = rb + h * kTile;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            load_box(dst + (1 + h) * kBlockBytes + i * kBoxBytes, &j.b, j.b_mn ? r + 64 * i : kc,
+                                     j.b_mn ? kc : r + 64 * i, bar);
                     }
                     ++it;
                     if (++stage == kStages) {
                         stage = 0;
                         parity ^= 1u;
                     }
+                }
+                if (!ok) break;
+                if (rank == 0) {
+                    t = after;
+                } else {
+                    t = next_tile(i);
+                    if (t < 0) {
+                        ok = false;
+                        break;
+                    }
+                    barrier_arrive_leader(smem_addr(&slot_empty[i % kSlots]));
                 }
             }
             // the last commits arrive on this CTA's barriers: it must not leave before they have
@@ -383,179 +476,227 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {  // ---- MMA, the pair's first CTA
-            int stage = 0;
+        if (rank == 0) {  // ---- MMA, the pair's first CTA: the warp walks together, one thread issues
+            int stage = 0, sub = 0;    // sub: accumulators used so far; they alternate
             uint32_t parity = 0;
-            int local = 0;
             bool ok = true;
-            constexpr uint32_t type = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
-            for (int t = pair; t < tiles && ok; t += pairs, ++local) {
+            constexpr uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+            auto wait_warp = [&](uint32_t bar, uint32_t ph) -> bool { return __all_sync(0xFFFFFFFFu, wait(bar, ph)); };
+            for (int t = pair, i = 0; t < p.tiles; ++i) {
                 const TilePos tp = tile_pos(p, t);
                 const HeadJob &j = p.job[tp.job];
-                const int acc = local & 1;
-                const uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)j.a_mn << 15) |
-                                       ((uint32_t)j.b_mn << 16) | ((uint32_t)(kTile >> 3) << 17) |
+                const int a_mn = j.a_mn, b_mn = j.b_mn, steps = j.k_steps, halves = j.halves;
+                const uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)a_mn << 15) |
+                                       ((uint32_t)b_mn << 16) | ((uint32_t)(kTile >> 3) << 17) |
                                        ((uint32_t)(kTile >> 4) << 24);
-                const uint32_t da = j.a_mn ? 2048 >> 4 : 32 >> 4, db = j.b_mn ? 2048 >> 4 : 32 >> 4;
-                if (!wait(smem_addr(&acc_empty[acc]), (uint32_t)((local >> 1) & 1) ^ 1u)) {
-                    ok = false;
-                    break;
-                }
-                tmem_fence_after();
-                const uint32_t d = tmem_base + (uint32_t)acc * kTile;
-                for (int k = 0; k < j.k_steps; ++k) {
-                    if (!wait(smem_addr(&full[stage]), parity)) {
-                        ok = false;
-                        break;
-                    }
-                    tmem_fence_after();
-                    const uint32_t a0 = ring + stage * kStageBytes;
-                    const uint64_t a = operand_desc(a0, j.a_mn), b = operand_desc(a0 + kOperandBytes, j.b_mn);
+                const uint32_t da = a_mn ? 2048 >> 4 : 32 >> 4, db = b_mn ? 2048 >> 4 : 32 >> 4;
+                const uint64_t a_base = operand_desc(ring, a_mn), b_base = operand_desc(ring + kBlockBytes, b_mn);
+                auto issue = [&](int st, int h, int acc, int k) {
+                    const uint64_t a = a_base + (uint32_t)(st * (kStageBytes >> 4));
+                    const uint64_t b = b_base + (uint32_t)(st * (kStageBytes >> 4) + h * (kBlockBytes >> 4));
 #pragma unroll
-                    for (int i = 0; i < kStepK / 16; ++i) mma_f16(d, a + i * da, b + i * db, idesc, (uint32_t)(k | i));
-                    mma_commit_both(smem_addr(&empty[stage]));
+                    for (int i = 0; i < kStepK / 16; ++i)
+                        mma_f16(tmem_base + (uint32_t)acc * kTile, a + i * da, b + i * db, idesc, (uint32_t)(k | i));
+                };
+                const int acc0 = sub & 1, acc1 = acc0 ^ 1;
+                const uint32_t parity0 = (uint32_t)((sub >> 1) & 1) ^ 1u, parity1 = (uint32_t)(((sub + 1) >> 1) & 1) ^ 1u;
+                ok = wait_warp(smem_addr(&acc_empty[acc0]), parity0);
+                if (!ok) break;
+                tmem_fence_after();
+                // With two accumulators the second may still be read when the first is free: its products follow
+                // as soon as it is, at the latest when the ring is full of stages that wait for it.
+                bool second = halves == 1;
+                int behind = 0, tail = stage, kb = 0;
+                for (int k = 0; k < steps; ++k) {
+                    ok = wait_warp(smem_addr(&full[stage]), parity);
+                    if (!ok) break;
+                    if (elect_one()) {
+                        issue(stage, 0, acc0, k);
+                        if (k + 1 == steps) mma_commit_both(smem_addr(&acc_full[acc0]));
+                    }
+                    __syncwarp();
+                    ++behind;
+                    if (!second) {
+                        if (behind == kStages || k + 1 == steps) {
+                            ok = wait_warp(smem_addr(&acc_empty[acc1]), parity1);
+                            if (!ok) break;
+                            second = true;
+                        } else {
+                            second = __all_sync(0xFFFFFFFFu, barrier_test(smem_addr(&acc_empty[acc1]), parity1));
+                        }
+                        if (second) tmem_fence_after();
+                    }
+                    for (; second && behind; --behind, ++kb) {
+                        if (elect_one()) {
+                            if (halves == 2) issue(tail, 1, acc1, kb);
+                            mma_commit_both(smem_addr(&empty[tail]));
+                        }
+                        __syncwarp();
+                        if (++tail == kStages) tail = 0;
+                    }
                     if (++stage == kStages) {
                         stage = 0;
                         parity ^= 1u;
                     }
                 }
-                if (ok) mma_commit_both(smem_addr(&acc_full[acc]));
+                if (!ok) break;
+                if (halves == 2 && elect_one()) mma_commit_both(smem_addr(&acc_full[acc1]));
+                __syncwarp();
+                sub += halves;
+                t = next_tile(i);
+                ok = __all_sync(0xFFFFFFFFu, t >= 0);
+                if (!ok) break;
+                if (elect_one()) barrier_arrive_leader(smem_addr(&slot_empty[i % kSlots]));
+                __syncwarp();
             }
             if (!ok) {  // the MMAs issued so far still read shared memory and write TMEM: let them end (bounded)
-                mma_commit_both(smem_addr(&drain));
+                if (elect_one()) mma_commit_both(smem_addr(&drain));
+                __syncwarp();
                 for (unsigned n = 0; n < kHeadSpin && !barrier_try(smem_addr(&drain), 0); ++n) {}
             }
         }
-    } else if (warp >= 4) {  // ---- epilogue: a thread owns one row and half of the tile's columns
+    } else if (warp >= 4) {  // ---- epilogue: a thread owns one row and half of an accumulator's columns
         const int quad = warp & 3, half = (warp - 4) >> 2;
         const float c2 = p.c2;
-        int local = 0;
-        for (int t = pair; t < tiles; t += pairs, ++local) {
+        int sub = 0;
+        bool ok = true;
+        for (int t = pair, i = 0; t < p.tiles; ++i) {
             const TilePos tp = tile_pos(p, t);
-            const int acc = local & 1;
+            const HeadJob &j = p.job[tp.job];
             const int row = tp.m * kTile + (int)rank * kHalf + quad * 32 + lane;
-            const int col0 = tp.n * kTile + half * kHalf;
-            const uint32_t src = tmem_base + (uint32_t)acc * kTile + half * kHalf + ((uint32_t)(quad * 32) << 16);
-            // what a row needs, loaded before the tile is ready
-            [[maybe_unused]] Targets tg;
-            [[maybe_unused]] long long label = -1;
             [[maybe_unused]] float gs = 0.0f, l2 = 0.0f;
-            if constexpr (MODE != kModeProducts) {
-                const bool live = row < p.n;
-                if (p.k)
-                    tg.start(p, row, p.v0 + col0, live);
-                else
-                    label = live ? p.labels[row] - p.v0 - col0 : -1;
-                if constexpr (MODE == kModeLogitGrad) {
-                    if (live) {
-                        const bool wanted = p.k ? p.entropy[row] < INFINITY : p.labels[row] >= 0 && p.labels[row] < p.vocab_total;
-                        gs = wanted ? p.grad[row] * p.temperature * (p.scale ? p.scale[0] : 1.0f) : 0.0f;
-                        l2 = p.lse[row] * 1.4426950408889634f;
-                    }
+            const bool live = row < p.n;
+            if constexpr (BACK) {
+                if (j.kind == kLogitGrad && live) {
+                    const bool wanted = p.k ? p.entropy[row] < INFINITY : p.labels[row] >= 0 && p.labels[row] < p.vocab_total;
+                    gs = wanted ? p.grad[row] * p.temperature * (p.scale ? p.scale[0] : 1.0f) : 0.0f;
+                    l2 = p.lse[row] * 1.4426950408889634f;
                 }
             }
-            if (!__all_sync(0xFFFFFFFFu, wait(smem_addr(&acc_full[acc]), (uint32_t)((local >> 1) & 1)))) break;
-            tmem_fence_after();
-            [[maybe_unused]] float m = -INFINITY, s = 0.0f;
-            uint32_t raw[2][32];
-            tmem_load32(src, raw[0]);
-#pragma unroll
-            for (int ch = 0; ch < kHalf / 32; ++ch) {
-                tmem_wait_load(raw[ch & 1]);
-                if (ch + 1 < kHalf / 32) {
-                    tmem_load32(src + 32 * (ch + 1), raw[(ch + 1) & 1]);
-                } else {  // the accumulator is read: the next but one tile may overwrite it
-                    tmem_fence_before();
-                    __syncwarp();
-                    if (lane == 0) barrier_arrive_leader(smem_addr(&acc_empty[acc]));
+            for (int h = 0; h < j.halves; ++h, ++sub) {
+                const int acc = sub & 1;
+                const int col0 = (tp.n * j.halves + h) * kTile + half * kHalf;
+                const uint32_t src = tmem_base + (uint32_t)acc * kTile + half * kHalf + ((uint32_t)(quad * 32) << 16);
+                // what a row needs, loaded before the tile is ready
+                [[maybe_unused]] Targets tg;
+                [[maybe_unused]] long long label = -1;
+                if (!BACK || j.kind == kLogitGrad) {
+                    if (p.k)
+                        tg.start(p, row, j.v0 + col0, live);
+                    else
+                        label = live ? p.labels[row] - j.v0 - col0 : -1;
                 }
-                float z[32];
+                ok = __all_sync(0xFFFFFFFFu, wait(smem_addr(&acc_full[acc]), (uint32_t)((sub >> 1) & 1)));
+                if (!ok) break;
+                tmem_fence_after();
+                [[maybe_unused]] float m = -INFINITY, s = 0.0f;
+                uint32_t raw[2][32];
+                tmem_load32(src, raw[0]);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(raw[ch & 1][i]);
-                const int col = col0 + 32 * ch;
-                if constexpr (MODE == kModeForward) {
-                    if (p.k) {
-                        while (tg.next < p.v0 + col + 32) {
-                            p.target_z[(long long)row * p.k + tg.j] = pick32(z, tg.next - (int)p.v0 - col);
-                            tg.advance();
+                for (int ch = 0; ch < kHalf / 32; ++ch) {
+                    tmem_wait_load(raw[ch & 1]);
+                    if (ch + 1 < kHalf / 32) {
+                        tmem_load32(src + 32 * (ch + 1), raw[(ch + 1) & 1]);
+                    } else {  // the accumulator is read: the tile after the next may overwrite it
+                        tmem_fence_before();
+                        __syncwarp();
+                        if (lane == 0) barrier_arrive_leader(smem_addr(&acc_empty[acc]));
+                    }
+                    float z[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(raw[ch & 1][i]);
+                    const int col = col0 + 32 * ch;
+                    if constexpr (!BACK) {
+                        if (p.k) {
+                            while (tg.next < col + 32) {
+                                p.target_z[(long long)row * p.k + tg.j] = pick32(z, tg.next - col);
+                                tg.advance();
+                            }
+                        } else if (label >= 32 * ch && label < 32 * ch + 32) {
+                            p.target_z[row] = pick32(z, (int)label - 32 * ch);
                         }
-                    } else if (label >= 32 * ch && label < 32 * ch + 32) {
-                        p.target_z[row] = pick32(z, (int)label - 32 * ch);
-                    }
-                    if (col + 32 > p.vocab) {
+                        if (col + 32 > j.vocab) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (col + i >= p.vocab) z[i] = -INFINITY;
-                    }
-                    float top = z[0];
-#pragma unroll
-                    for (int i = 1; i < 32; ++i) top = fmaxf(top, z[i]);
-                    const float now = fmaxf(m, top * c2);
-                    const float ref = now == -INFINITY ? 0.0f : now;
-                    float add = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) add += exp2_approx(fmaf(z[i], c2, -ref));
-                    s = fmaf(s, exp2_approx(m - ref), add);
-                    m = now;
-                } else if constexpr (MODE == kModeLogitGrad) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) z[i] = gs * exp2_approx(fmaf(z[i], c2, -l2));
-                    if (p.k) {
-                        while (tg.next < p.v0 + col + 32) {
-                            subtract32(z, tg.next - (int)p.v0 - col, gs * p.target_q[(long long)row * p.k + tg.j]);
-                            tg.advance();
+                            for (int i = 0; i < 32; ++i)
+                                if (col + i >= j.vocab) z[i] = -INFINITY;
                         }
-                    } else if (label >= 32 * ch && label < 32 * ch + 32) {
-                        subtract32(z, (int)label - 32 * ch, gs);
-                    }
-                    if (col + 32 > p.vocab || gs == 0.0f) {
+                        float top = z[0];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (col + i >= p.vocab || gs == 0.0f) z[i] = 0.0f;
-                    }
-                    // dz in 16 bits, as both products' operand: their sums run over it in binary32
-                    if (row < p.n) store_row32<T>((T *)p.dz + (long long)row * p.dz_pitch + col, z, 32, true);
-                } else {
-                    const float back = p.scale ? p.scale[1] : 1.0f;
-                    if (tp.job == 0) {
-                        if (row < p.n && col < p.width) {
-                            float *sum = p.dh_sum + (long long)row * p.dh_sum_pitch + col;
-                            const int count = min(32, p.width - col);
-                            if (!p.first) {
+                        for (int i = 1; i < 32; ++i) top = fmaxf(top, z[i]);
+                        const float now = fmaxf(m, top * c2);
+                        const float ref = now == -INFINITY ? 0.0f : now;
+                        float add = 0.0f;
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) {
-                                    if (4 * i < count) {  // the pitch is a multiple of 4
-                                        const float4 o = reinterpret_cast<const float4 *>(sum)[i];
-                                        z[4 * i] += o.x;
-                                        z[4 * i + 1] += o.y;
-                                        z[4 * i + 2] += o.z;
-                                        z[4 * i + 3] += o.w;
+                        for (int i = 0; i < 32; ++i) add += exp2_approx(fmaf(z[i], c2, -ref));
+                        s = fmaf(s, exp2_approx(m - ref), add);
+                        m = now;
+                    } else if (j.kind == kLogitGrad) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) z[i] = gs * exp2_approx(fmaf(z[i], c2, -l2));
+                        if (p.k) {
+                            while (tg.next < j.v0 + col + 32) {
+                                subtract32(z, tg.next - (int)j.v0 - col, gs * p.target_q[(long long)row * p.k + tg.j]);
+                                tg.advance();
+                            }
+                        } else if (label >= 32 * ch && label < 32 * ch + 32) {
+                            subtract32(z, (int)label - 32 * ch, gs);
+                        }
+                        if (col + 32 > j.vocab || gs == 0.0f) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (col + i >= j.vocab || gs == 0.0f) z[i] = 0.0f;
+                        }
+                        // dz in 16 bits, as both products' operand: their sums run over it in binary32
+                        if (live && col < p.dz_pitch) store_row32<T>((T *)j.dz + (long long)row * p.dz_pitch + col, z, 32, true);
+                    } else {
+                        const float back = p.scale ? p.scale[1] : 1.0f;
+                        const int count = min(32, p.width - col);
+                        if (j.kind == kHiddenGrad) {
+                            if (live && count > 0) {
+                                float *sum = p.dh_sum + (long long)row * p.dh_sum_pitch + col;
+                                if (!j.first) {
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) {
+                                        if (4 * i < count) {  // the pitch is a multiple of 4
+                                            const float4 o = reinterpret_cast<const float4 *>(sum)[i];
+                                            z[4 * i] += o.x;
+                                            z[4 * i + 1] += o.y;
+                                            z[4 * i + 2] += o.z;
+                                            z[4 * i + 3] += o.w;
+                                        }
                                     }
                                 }
-                            }
-                            if (p.last) {
+                                if (j.last) {
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) z[i] *= back;
-                                T *dst = (T *)p.dh + (long long)row * p.dh_stride + col;
-                                store_row32<T>(dst, z, count, ((uintptr_t)dst & 15) == 0);
-                            } else {
+                                    for (int i = 0; i < 32; ++i) z[i] *= back;
+                                    T *dst = (T *)p.dh + (long long)row * p.dh_stride + col;
+                                    store_row32<T>(dst, z, count, ((uintptr_t)dst & 15) == 0);
+                                } else {
 #pragma unroll
-                                for (int i = 0; i < 8; ++i)
-                                    if (4 * i < count)
-                                        reinterpret_cast<float4 *>(sum)[i] =
-                                            make_float4(z[4 * i], z[4 * i + 1], z[4 * i + 2], z[4 * i + 3]);
+                                    for (int i = 0; i < 8; ++i)
+                                        if (4 * i < count)
+                                            reinterpret_cast<float4 *>(sum)[i] =
+                                                make_float4(z[4 * i], z[4 * i + 1], z[4 * i + 2], z[4 * i + 3]);
+                                }
                             }
+                        } else if (row < j.vocab && count > 0) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) z[i] *= back;
+                            Q *dst = (Q *)p.dw + (j.v0 + row) * p.dw_stride + col;
+                            store_row32<Q>(dst, z, count, ((uintptr_t)dst & 15) == 0);
                         }
-                    } else if (row < p.vocab && col < p.width) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) z[i] *= back;
-                        Q *dst = (Q *)p.dw + (p.v0 + row) * p.dw_stride + col;
-                        store_row32<Q>(dst, z, min(32, p.width - col), ((uintptr_t)dst & 15) == 0);
                     }
                 }
+                if constexpr (!BACK) {
+                    const int part = col0 / kHalf;
+                    if (live && part < p.parts) p.partial[(long long)part * p.n + row] = make_float2(m, s);
+                }
             }
-            if constexpr (MODE == kModeForward)
-                if (row < p.n) p.partial[(long long)(2 * tp.n + half) * p.n + row] = make_float2(m, s);
+            if (!ok) break;
+            t = next_tile(i);
+            ok = __all_sync(0xFFFFFFFFu, t >= 0);
+            if (!ok) break;
+            if (lane == 0) barrier_arrive_leader(smem_addr(&slot_empty[i % kSlots]));
         }
     }
     __syncwarp();
@@ -663,16 +804,18 @@ k_head_scale(const float *__restrict__ grad, const long long *__restrict__ label
     }
 }
 
-// Joins a row's partial maxima and sums (two per tile column) to its log-sum-exp, and forms the loss.  32 rows
-// per CTA, the partials of a row dealt to eight warps.
+// Joins a row's partial maxima and sums (one per 128 columns) to its log-sum-exp, and forms the loss.  Eight rows
+// per CTA; the partials of a row are dealt to 32 threads, four loads at a time.
+constexpr int kJoinRows = 8;
 __global__ void __launch_bounds__(256)
 k_head_join(const float2 *__restrict__ partial, int parts, int n, const long long *__restrict__ labels, long long vocab,
             const int *__restrict__ target_index, const float *__restrict__ target_q, const float *__restrict__ target_z,
-            const float *__restrict__ entropy, int k, float inv_t, float *__restrict__ loss, float *__restrict__ lse)
+            const float *__restrict__ entropy, int k, float inv_t, float z_scale, float *__restrict__ loss,
+            float *__restrict__ lse)
 {
-    __shared__ float sm[8][33], ss[8][33];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int row0 = blockIdx.x * 32;
+    __shared__ float sm[8][kJoinRows], ss[8][kJoinRows], row_lse[kJoinRows];
+    const int r = threadIdx.x % kJoinRows, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int row0 = blockIdx.x * kJoinRows;
     grid_dependency_wait();
     grid_dependency_launch_next();
     float m = -INFINITY, s = 0.0f;
@@ -681,44 +824,54 @@ k_head_join(const float2 *__restrict__ partial, int parts, int n, const long lon
         s = s * exp2_approx(m - ref) + os * exp2_approx(om - ref);
         m = now;
     };
-    if (row0 + lane < n)
-        for (int i = warp; i < parts; i += 8) {
-            const float2 v = partial[(long long)i * n + row0 + lane];
-            join(v.x, v.y);
+    if (row0 + r < n) {
+        const float2 *src = partial + row0 + r;
+        for (int i = threadIdx.x / kJoinRows; i < parts; i += 128) {
+            float2 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                v[u] = i + 32 * u < parts ? src[(long long)(i + 32 * u) * n] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) join(v[u].x, v[u].y);
         }
-    sm[warp][lane] = m;
-    ss[warp][lane] = s;
+    }
+#pragma unroll
+    for (int d = kJoinRows; d < 32; d <<= 1) {
+        const float om = __shfl_xor_sync(0xFFFFFFFFu, m, d), os = __shfl_xor_sync(0xFFFFFFFFu, s, d);
+        join(om, os);
+    }
+    if (lane < kJoinRows) {
+        sm[warp][lane] = m;
+        ss[warp][lane] = s;
+    }
     __syncthreads();
-    if (warp == 0) {
-        for (int w = 1; w < 8; ++w) join(sm[w][lane], ss[w][lane]);
+    if (threadIdx.x < kJoinRows && row0 + r < n) {
+        for (int w = 0; w < 8; ++w)
+            if (w != 0) join(sm[w][r], ss[w][r]);
         const float l = (m + log2f(s)) * 0.6931471805599453f;
-        sm[0][lane] = l;
-        if (row0 + lane < n) {
-            if (lse) lse[row0 + lane] = l;
-            if (!k) {
-                const long long y = labels[row0 + lane];
-                loss[row0 + lane] = y < 0 ? 0.0f : y >= vocab ? NAN : l - target_z[row0 + lane];
-            }
+        row_lse[r] = l;
+        if (lse) lse[row0 + r] = l;
+        if (!k) {
+            const long long y = labels[row0 + r];
+            loss[row0 + r] = y < 0 ? 0.0f : y >= vocab ? NAN : l - target_z[row0 + r] * z_scale;
         }
     }
     if (!k) return;
     __syncthreads();
-    for (int r = warp; r < 32; r += 8) {
-        const int row = row0 + r;
-        if (row >= n) break;
-        float cross = 0.0f;
-        for (int j = lane; j < k; j += 32) {
-            const long long at = (long long)row * k + j;
-            if (target_index[at] != kNoTarget) {
-                const float q = target_q[at];
-                if (!(q == 0.0f)) cross = fmaf(q, sm[0][r] - target_z[at] * inv_t, cross);
-            }
+    const int row = row0 + warp;
+    if (row >= n) return;
+    float cross = 0.0f;
+    for (int j = lane; j < k; j += 32) {
+        const long long at = (long long)row * k + j;
+        if (target_index[at] != kNoTarget) {
+            const float q = target_q[at];
+            if (!(q == 0.0f)) cross = fmaf(q, row_lse[warp] - target_z[at] * z_scale, cross);
         }
-        cross = warp_sum(cross);
-        if (lane == 0) {
-            const float e = entropy[row];
-            loss[row] = e == INFINITY ? 0.0f : (e + cross) / (inv_t * inv_t);
-        }
+    }
+    cross = warp_sum(cross);
+    if (lane == 0) {
+        const float e = entropy[row];
+        loss[row] = e == INFINITY ? 0.0f : (e + cross) / (inv_t * inv_t);
     }
 }
 
@@ -763,14 +916,14 @@ cudaError_t encode(CUtensorMap *map, int dtype, const void *base, long long rows
 inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 inline int tiles_of(int64_t a) { return (int)((a + kTile - 1) / kTile); }
 
-// A piece of the vocabulary: dz (n x piece, 16 bits) of at most kPieceBytes, so that it is still in L2 when the
-// two products read it; never under kPieceMin columns, because every piece adds to dh once.
+// A piece of the vocabulary: dz (n x piece, 16 bits) of about kPieceBytes, twice (one is written while the other
+// is read); never under kPieceMin columns, because every piece adds to dh once.
 constexpr int64_t kPieceBytes = 64ll << 20;
 constexpr int64_t kPieceMin = 2048;
 
 struct HeadLayout {
     int64_t piece, pieces;
-    int64_t partial, target_z, index, q, entropy, scale, dz, dh_sum, bytes;
+    int64_t partial, target_z, index, q, entropy, scale, counter, dz[2], dh_sum, bytes;
     int64_t dh_pitch;
 };
 
@@ -794,11 +947,13 @@ HeadLayout head_layout(int64_t n, int64_t v, int64_t d, int64_t k)
     L.q = take(4 * n * k);
     L.entropy = take(4 * n);
     L.scale = take(8);
+    L.counter = take(4 * (L.pieces + 1));
     const int64_t shared = at;  // the forward pass's partials and the backward pass's dz share the rest
     L.partial = take(8 * n * 2 * tiles_of(v));
     L.bytes = at;
     at = shared;
-    L.dz = take(2 * n * L.piece);
+    L.dz[0] = take(2 * n * L.piece);
+    L.dz[1] = take(L.pieces > 1 ? 2 * n * L.piece : 0);
     L.dh_sum = take(L.pieces > 1 ? 4 * n * L.dh_pitch : 0);
     if (at > L.bytes) L.bytes = at;
     return L;
@@ -847,35 +1002,69 @@ int call_check(const HeadCall &c)
     return RSDGC_OK;
 }
 
-template <int MODE, typename T, typename Q>
-cudaError_t launch_tiles(const HeadParams &p, cudaStream_t s)
+// Clusters of two that the device holds at a time; 0 and an error in *e if the kernel cannot run.
+template <bool BACK, typename T, typename Q>
+int head_pairs(cudaError_t *e)
 {
-    static std::once_flag once[64];
+    static std::mutex mu;
+    static int most[64];
     int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    static cudaError_t attr[64];
-    std::call_once(once[dev & 63], [&] {
-        attr[dev & 63] = cudaFuncSetAttribute(k_head<MODE, T, Q>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem);
-    });
-    if (attr[dev & 63] != cudaSuccess) return attr[dev & 63];
-    long long tiles = 0;
-    for (int i = 0; i < p.n_jobs; ++i) tiles += (long long)p.job[i].m_tiles * p.job[i].n_tiles;
-    if (tiles > INT_MAX) return cudaErrorInvalidValue;
-    const int most = current_device_sms() / 2;
-    const unsigned pairs = (unsigned)(tiles < most ? tiles : most);
-    return launch_chained(k_head<MODE, T, Q>, 2 * pairs, kHeadThreads, kHeadSmem, s, 2, p);
+    *e = cudaGetDevice(&dev);
+    if (*e != cudaSuccess) return 0;
+    std::lock_guard<std::mutex> lock(mu);
+    int &m = most[dev & 63];
+    if (m) return m;
+    *e = cudaFuncSetAttribute(k_head<BACK, T, Q>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem);
+    if (*e != cudaSuccess) return 0;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = (unsigned)current_device_sms();
+    cfg.blockDim = kHeadThreads;
+    cfg.dynamicSmemBytes = kHeadSmem;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = 2;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    int n = 0;
+    *e = cudaOccupancyMaxActiveClusters(&n, k_head<BACK, T, Q>, &cfg);
+    if (*e == cudaSuccess && n < 1) *e = cudaErrorLaunchOutOfResources;
+    if (*e != cudaSuccess) return 0;
+    return m = n;
 }
 
-constexpr int kBand = 16;
-cudaError_t set_job(HeadJob &j, int dtype, const void *a, bool a_mn, long long ar, long long ac, long long as, const void *b,
-                    bool b_mn, long long br, long long bc, long long bs, long long m, long long n, long long k)
+template <bool BACK, typename T, typename Q>
+cudaError_t launch_tiles(HeadParams &p, int *counter, cudaStream_t s)
 {
+    cudaError_t e = cudaSuccess;
+    const int most = head_pairs<BACK, T, Q>(&e);
+    if (e != cudaSuccess) return e;
+    long long tiles = 0;
+    for (int i = 0; i < p.n_jobs; ++i) tiles += (long long)p.job[i].m_tiles * p.job[i].n_tiles;
+    if (tiles > INT_MAX / 2) return cudaErrorInvalidValue;
+    p.tiles = (int)tiles;
+    p.next_tile = counter;
+    const unsigned pairs = (unsigned)(tiles < most ? tiles : most);
+    return launch_chained(k_head<BACK, T, Q>, 2 * pairs, kHeadThreads, kHeadSmem, s, 2, p);
+}
+
+constexpr double kTruncationBf16 = 0.26, kTruncationF16 = 0.29;
+constexpr int kBand = 16;
+// Two accumulators per tile (256 x 512): every operand block brought in serves more products, 48 instead of 64 bytes
+// per cycle and SM at the full MMA rate; but the first accumulator is then idle while it is emptied.
+constexpr int kTwoHalvesFrom = 16;  // contraction steps
+
+cudaError_t set_job(HeadJob &j, int kind, int dtype, const void *a, bool a_mn, long long ar, long long ac, long long as,
+                    const void *b, bool b_mn, long long br, long long bc, long long bs, long long m, long long n, long long k)
+{
+    std::memset(&j, 0, sizeof j);
+    j.kind = kind;
     j.a_mn = a_mn;
     j.b_mn = b_mn;
-    j.m_tiles = tiles_of(m);
-    j.n_tiles = tiles_of(n);
     j.k_steps = (int)((k + kStepK - 1) / kStepK);
+    j.halves = j.k_steps >= kTwoHalvesFrom && n > kTile ? 2 : 1;
+    j.m_tiles = tiles_of(m);
+    j.n_tiles = (tiles_of(n) + j.halves - 1) / j.halves;
     j.band = j.m_tiles < kBand ? j.m_tiles : kBand;
     const cudaError_t e = encode(&j.a, dtype, a, ar, ac, as);
     return e == cudaSuccess ? encode(&j.b, dtype, b, br, bc, bs) : e;
@@ -900,7 +1089,11 @@ void common_params(HeadParams &p, const HeadCall &c, const HeadLayout &L)
 {
     p.n = (int)c.n;
     p.vocab_total = c.v;
-    p.c2 = 1.4426950408889634f / c.temperature;
+    // The tensor core truncates its running sum: a step of 16 terms takes about kTruncation * 2^-24 of the final value
+    // off it (measured on sums of 512 to 8192 terms; 4.2e-6 of z at 4096 before, 1.1e-6 after).  The exponent's factor
+    // puts the mean of that back.
+    const double steps = (double)((c.d + 15) / 16), lost = c.dtype == RSDGC_BF16 ? kTruncationBf16 : kTruncationF16;
+    p.c2 = (float)(1.4426950408889634 / c.temperature * (1.0 + lost * steps * 0x1p-24));
     p.labels = c.labels;
     p.k = (int)c.k;
     p.target_index = (const int *)(c.workspace + L.index);
@@ -922,42 +1115,66 @@ int head_forward(const HeadCall &c, float *loss, float *lse)
     cudaError_t e = operator_status_ptr(&p.status);
     common_params(p, c, L);
     p.n_jobs = 1;
-    p.vocab = (int)c.v;
+    p.parts = 2 * tiles_of(c.v);
     p.partial = (float2 *)(c.workspace + L.partial);
     p.target_z = (float *)(c.workspace + L.target_z);
     if (e == cudaSuccess)
-        e = set_job(p.job[0], c.dtype, c.hidden, false, c.n, c.d, c.hs, c.weight, false, c.v, c.d, c.ws, c.n, c.v, c.d);
+        e = set_job(p.job[0], kForward, c.dtype, c.hidden, false, c.n, c.d, c.hs, c.weight, false, c.v, c.d, c.ws, c.n, c.v,
+                    c.d);
+    p.job[0].vocab = (int)c.v;
     if (e == cudaSuccess) e = targets(c, L);
     if (e == cudaSuccess)
-        e = c.dtype == RSDGC_BF16 ? launch_tiles<kModeForward, __nv_bfloat16, __nv_bfloat16>(p, c.s)
-                                  : launch_tiles<kModeForward, __half, __half>(p, c.s);
+        e = c.dtype == RSDGC_BF16 ? launch_tiles<false, __nv_bfloat16, __nv_bfloat16>(p, nullptr, c.s)
+                                  : launch_tiles<false, __half, __half>(p, nullptr, c.s);
     if (e == cudaSuccess)
-        e = launch_chained(k_head_join, (unsigned)((c.n + 31) / 32), 256, 0, c.s, 1, (const float2 *)p.partial,
-                           2 * p.job[0].n_tiles, (int)c.n, c.labels, (long long)c.v, p.target_index, p.target_q,
-                           (const float *)p.target_z, p.entropy, (int)c.k, 1.0f / c.temperature, loss, lse);
+        e = launch_chained(k_head_join, (unsigned)((c.n + kJoinRows - 1) / kJoinRows), 256, 0, c.s, 1, (const float2 *)p.partial,
+                           p.parts, (int)c.n, c.labels, (long long)c.v, p.target_index, p.target_q,
+                           (const float *)p.target_z, p.entropy, (int)c.k, 1.0f / c.temperature, p.c2 * 0.6931471805599453f, loss, lse);
     return operator_result(e);
 }
 
+// Launch i computes piece i's dz and, from the piece before it, dh and dW: three products whose tiles share a queue,
+// longest contraction first, so that the multiprocessors end together.
 template <typename T, typename Q>
 cudaError_t backward_pieces(const HeadCall &c, const HeadLayout &L, HeadParams &p)
 {
-    for (int64_t i = 0; i < L.pieces; ++i) {
-        const int64_t v0 = i * L.piece, width = c.v - v0 < L.piece ? c.v - v0 : L.piece;
-        const void *w = (const unsigned char *)c.weight + v0 * c.ws * 2;
-        p.v0 = v0;
-        p.vocab = (int)width;
-        p.first = i == 0;
-        p.last = i + 1 == L.pieces;
-        p.n_jobs = 1;
-        cudaError_t e = set_job(p.job[0], c.dtype, c.hidden, false, c.n, c.d, c.hs, w, false, width, c.d, c.ws, c.n, width, c.d);
-        if (e == cudaSuccess) e = launch_tiles<kModeLogitGrad, T, T>(p, c.s);
+    for (int64_t i = 0; i <= L.pieces; ++i) {
+        cudaError_t e = cudaSuccess;
+        p.n_jobs = 0;
+        auto piece = [&](HeadJob &j, int64_t at) {
+            j.v0 = at * L.piece;
+            j.vocab = (int)(c.v - j.v0 < L.piece ? c.v - j.v0 : L.piece);
+            j.dz = c.workspace + L.dz[at & 1];
+            j.first = at == 0;
+            j.last = at + 1 == L.pieces;
+        };
+        auto rows = [&](int64_t at) { return c.v - at * L.piece < L.piece ? c.v - at * L.piece : L.piece; };
+        auto weight = [&](int64_t at) { return (const unsigned char *)c.weight + at * L.piece * c.ws * 2; };
+        if (i < L.pieces) {
+            HeadJob &j = p.job[p.n_jobs++];
+            e = set_job(j, kLogitGrad, c.dtype, c.hidden, false, c.n, c.d, c.hs, weight(i), false, rows(i), c.d, c.ws, c.n,
+                        rows(i), c.d);
+            piece(j, i);
+        }
+        if (i > 0 && e == cudaSuccess) {
+            const int64_t at = i - 1, v = rows(at);
+            const void *dz = c.workspace + L.dz[at & 1];
+            // the tiles of dz are whole: zeros beyond the vocabulary, so the contraction may run over whole steps
+            HeadJob &j = p.job[p.n_jobs++];
+            e = set_job(j, kHiddenGrad, c.dtype, dz, false, c.n, L.piece, L.piece, weight(at), true, v, c.d, c.ws, c.n, c.d, v);
+            piece(j, at);
+            if (e == cudaSuccess) {
+                HeadJob &w = p.job[p.n_jobs++];
+                e = set_job(w, kWeightGrad, c.dtype, dz, true, c.n, L.piece, L.piece, c.hidden, true, c.n, c.d, c.hs, v, c.d, c.n);
+                piece(w, at);
+            }
+        }
         if (e != cudaSuccess) return e;
-        // the tile kernel filled whole tiles of dz with zeros beyond the vocabulary, so k runs over whole steps
-        p.n_jobs = 2;
-        e = set_job(p.job[0], c.dtype, p.dz, false, c.n, L.piece, L.piece, w, true, width, c.d, c.ws, c.n, c.d, width);
-        if (e == cudaSuccess)
-            e = set_job(p.job[1], c.dtype, p.dz, true, c.n, L.piece, L.piece, c.hidden, true, c.n, c.d, c.hs, width, c.d, c.n);
-        if (e == cudaSuccess) e = launch_tiles<kModeProducts, T, Q>(p, c.s);
+        auto length = [](const HeadJob &j) { return j.k_steps * j.halves; };
+        for (int a = 0; a < p.n_jobs; ++a)
+            for (int b = a + 1; b < p.n_jobs; ++b)
+                if (length(p.job[b]) > length(p.job[a])) std::swap(p.job[a], p.job[b]);
+        e = launch_tiles<true, T, Q>(p, (int *)(c.workspace + L.counter) + i, c.s);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
@@ -985,7 +1202,6 @@ int head_backward(const HeadCall &c, const float *lse, const float *grad, void *
     common_params(p, c, L);
     p.lse = lse;
     p.grad = grad;
-    p.dz = c.workspace + L.dz;
     p.dz_pitch = L.piece;
     p.dh_sum = (float *)(c.workspace + L.dh_sum);
     p.dh_sum_pitch = L.dh_pitch;
@@ -994,6 +1210,7 @@ int head_backward(const HeadCall &c, const float *lse, const float *grad, void *
     p.dw = dw;
     p.dw_stride = dw_stride;
     p.width = (int)c.d;
+    if (e == cudaSuccess) e = cudaMemsetAsync(c.workspace + L.counter, 0, 4 * (size_t)(L.pieces + 1), c.s);
     if (e == cudaSuccess) e = targets(c, L);
     if (e == cudaSuccess && c.dtype == RSDGC_F16) {
         p.scale = (const float *)(c.workspace + L.scale);
