@@ -37,11 +37,12 @@ constexpr int kHalf = 128;          // rows of an operand block that one CTA hol
 constexpr int kStepK = 64;          // contraction step: 64 x 2 bytes = the 128-byte swizzle span
 constexpr int kBoxBytes = 64 * kStepK * 2;
 constexpr int kBlockBytes = 2 * kBoxBytes;
-constexpr int kStageBytes = 3 * kBlockBytes;             // one block of A, one or two of B
-constexpr int kStages = 4;
+constexpr int kRingBlocks = 12;     // of A and B blocks: 4 stages of 1 + 2 blocks, or 6 stages of 1 + 1
+constexpr int kMaxStages = kRingBlocks / 2;
 constexpr int kEpilogueWarps = 8;
 constexpr int kHeadThreads = 128 + 32 * kEpilogueWarps;  // producer, MMA, two idle warps, epilogue
-constexpr int kHeadSmem = kStages * kStageBytes + 1024;
+constexpr int kStagingBytes = 4096;  // per epilogue warp: 32 rows of 128 bytes on their way out
+constexpr int kHeadSmem = kRingBlocks * kBlockBytes + kEpilogueWarps * kStagingBytes + 1024;
 constexpr int kSlots = 4;                                // tiles announced ahead
 constexpr unsigned kHeadSpin = 1u << 20;                 // polls of a wait before it gives up
 constexpr int kMaxTargets = 1024;
@@ -51,21 +52,25 @@ constexpr int kMaxJobs = 3;
 enum { kForward = 0, kLogitGrad = 1, kHiddenGrad = 2, kWeightGrad = 3 };
 
 // One matrix product C (m x n) = A B^T over k: tensor maps with boxes of 64 x 64 elements, and what becomes of C.
+enum { kOut16 = 0, kOutF32 = 1, kOutAddF32 = 2 };
+
 struct __align__(64) HeadJob {
-    CUtensorMap a, b;
+    CUtensorMap a, b, out;   // out: boxes of 32 rows x 128 bytes
     int a_mn, b_mn;          // the operand lies with its rows (not k) contiguous
     int m_tiles, n_tiles, k_steps, band;
     int halves;              // accumulators of a tile: 256 x 256 or 256 x 512
+    int splits, split_steps; // parts of the contraction, each a tile of its own
     int kind;
     int vocab;               // entries of the vocabulary this job is about (all, or a piece's)
     long long v0;            // first of them
-    void *dz;                // the piece's buffer
-    int first, last;         // piece
+    void *out_ptr;           // C is written through `out`, or, where its rows are not 16-byte aligned, by plain stores
+    long long out_stride;
+    int out_rows, out_cols, out_mode, out_plain;
 };
 
 struct HeadParams {
     HeadJob job[kMaxJobs];
-    int n_jobs, tiles;
+    int n_jobs, tiles, stages;
     int n;                   // tokens
     long long vocab_total;
     float c2;                // log2(e) / T
@@ -81,15 +86,9 @@ struct HeadParams {
     // gradients
     const float *lse, *grad, *entropy, *scale;
     float temperature;
-    long long dz_pitch;
-    float *dh_sum;
-    long long dh_sum_pitch;
-    void *dh;
-    long long dh_stride;
-    void *dw;
-    long long dw_stride;
-    int width;
     int *next_tile;          // counter of tiles handed out beyond the first round; NULL: fixed rounds
+    int *clear;              // counters of the launches after this one
+    int n_clear;
     unsigned int *status;
 };
 
@@ -240,20 +239,25 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, int mn)
 }
 
 struct TilePos {
-    int job, m, n;
+    int job, m, n, split, k0, steps;
 };
-// Tiles of a job in bands of `band` tile rows, a band column by column: what runs at a time shares its operands in L2.
+// Tiles of a job, part by part of the contraction, in bands of `band` tile rows, a band column by column: what runs
+// at a time shares its operands in L2.
 __device__ __forceinline__ TilePos tile_pos(const HeadParams &p, int t)
 {
     TilePos r;
     r.job = 0;
-    int own = p.job[0].m_tiles * p.job[0].n_tiles;
-    while (r.job + 1 < p.n_jobs && t >= own) {
-        t -= own;
+    int area = p.job[0].m_tiles * p.job[0].n_tiles;
+    while (r.job + 1 < p.n_jobs && t >= area * p.job[r.job].splits) {
+        t -= area * p.job[r.job].splits;
         ++r.job;
-        own = p.job[r.job].m_tiles * p.job[r.job].n_tiles;
+        area = p.job[r.job].m_tiles * p.job[r.job].n_tiles;
     }
     const HeadJob &j = p.job[r.job];
+    r.split = t / area;
+    t -= r.split * area;
+    r.k0 = r.split * j.split_steps;
+    r.steps = min(j.split_steps, j.k_steps - r.k0);
     const int per = j.band * j.n_tiles, b = t / per, i = t - b * per, rows = min(j.band, j.m_tiles - b * j.band);
     r.n = i / rows;
     r.m = b * j.band + i - r.n * rows;
@@ -275,27 +279,21 @@ __device__ __forceinline__ uint32_t pack2<__half>(float a, float b)
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-// 32 consecutive values of a row, rounded to Q; `count` of them exist.  16-byte stores where the row allows.
-template <typename Q>
-__device__ __forceinline__ void store_row32(Q *dst, const float (&v)[32], int count, bool vec)
+__device__ __forceinline__ void store_shared16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
-    if (vec && count >= 32) {
-        if constexpr (sizeof(Q) == 4) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                reinterpret_cast<float4 *>(dst)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                reinterpret_cast<uint4 *>(dst)[i] =
-                    make_uint4(pack2<Q>(v[8 * i], v[8 * i + 1]), pack2<Q>(v[8 * i + 2], v[8 * i + 3]),
-                               pack2<Q>(v[8 * i + 4], v[8 * i + 5]), pack2<Q>(v[8 * i + 6], v[8 * i + 7]));
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i < count) dst[i] = from_f32<Q>(v[i]);
-    }
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void store_box(const CUtensorMap *map, int x, int y, int z, uint32_t src)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x),
+                 "r"(y), "r"(z), "r"(src)
+                 : "memory");
+}
+__device__ __forceinline__ void add_box(const CUtensorMap *map, int x, int y, int z, uint32_t src)
+{
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map),
+                 "r"(x), "r"(y), "r"(z), "r"(src)
+                 : "memory");
 }
 
 __device__ __forceinline__ float pick32(const float (&z)[32], int i)
@@ -311,11 +309,11 @@ __device__ __forceinline__ void subtract32(float (&z)[32], int i, float x)
     for (int j = 0; j < 32; ++j) z[j] -= i == j ? x : 0.0f;
 }
 
-// A row's targets inside the columns that a thread walks, in ascending order.
+// A row's targets from a column on, in ascending order.
 struct Targets {
     const int *index;
     int j, k, next;
-    __device__ __forceinline__ void start(const HeadParams &p, int row, long long col, bool live)
+    __device__ __forceinline__ void start(const HeadParams &p, int row, int col, bool live)
     {
         j = 0;
         k = p.k;
@@ -331,14 +329,86 @@ struct Targets {
         if (j < k) next = index[j];
     }
     __device__ __forceinline__ void advance() { next = ++j < k ? index[j] : kNoTarget; }
+    __device__ __forceinline__ void skip_to(int col)
+    {
+        while (next < col) advance();
+    }
 };
 
-// T: type of the operands (bfloat16 or binary16).  Q: type of dW.  BACK: the launch's jobs are gradients.
-template <bool BACK, typename T, typename Q>
+// A warp's 32 rows x 128 bytes on their way to global memory: staged in shared memory in the 128-byte swizzle (the
+// 16-byte piece c of row r lies at c ^ (r & 7), so neither side meets a bank conflict), then one bulk store per box.
+// Stores straight from the rows' registers take 1.6 cycles per 16 bytes of a row, 6700 cycles per 128 x 256 accumulator.
+template <typename T>
+struct RowsOut {
+    uint32_t buf;
+    int lane;
+    // 32 columns as part `part` (0, 1) of a 64-column box of 16-bit values
+    __device__ __forceinline__ void put16(int part, const float (&z)[32]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            store_shared16(buf + lane * 128 + (((part * 4 + i) ^ (lane & 7)) << 4), pack2<T>(z[8 * i], z[8 * i + 1]),
+                           pack2<T>(z[8 * i + 2], z[8 * i + 3]), pack2<T>(z[8 * i + 4], z[8 * i + 5]),
+                           pack2<T>(z[8 * i + 6], z[8 * i + 7]));
+    }
+    __device__ __forceinline__ void put32(const float (&z)[32]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            store_shared16(buf + lane * 128 + ((i ^ (lane & 7)) << 4), __float_as_uint(z[4 * i]), __float_as_uint(z[4 * i + 1]),
+                           __float_as_uint(z[4 * i + 2]), __float_as_uint(z[4 * i + 3]));
+    }
+    __device__ __forceinline__ void wait_free() const  // the last box has left the buffer
+    {
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+    }
+    // row0, col: of the box in C; count: columns of a box
+    __device__ __forceinline__ void flush(const HeadJob &j, int row0, int col, int split) const
+    {
+        if (!j.out_plain) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0 && row0 < j.out_rows && col < j.out_cols) {
+                if (j.out_mode == kOutAddF32)
+                    add_box(&j.out, col, row0, split, buf);
+                else
+                    store_box(&j.out, col, row0, split, buf);
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+            return;
+        }
+        __syncwarp();
+        const int rows = min(32, j.out_rows - row0);
+        for (int r = 0; r < rows; ++r) {
+            if (j.out_mode == kOut16) {
+                uint16_t *dst = (uint16_t *)j.out_ptr + (long long)(row0 + r) * j.out_stride + col;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int c = lane + 32 * h;
+                    uint16_t v;
+                    asm volatile("ld.shared.u16 %0, [%1];"
+                                 : "=h"(v)
+                                 : "r"(buf + r * 128 + (((c >> 3) ^ (r & 7)) << 4) + (c & 7) * 2));
+                    if (col + c < j.out_cols) dst[c] = v;
+                }
+            } else {
+                float v;
+                asm volatile("ld.shared.f32 %0, [%1];"
+                             : "=f"(v)
+                             : "r"(buf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4));
+                if (col + lane < j.out_cols) ((float *)j.out_ptr)[(long long)(row0 + r) * j.out_stride + col + lane] = v;
+            }
+        }
+    }
+};
+
+// T: type of the operands (bfloat16 or binary16).  BACK: the launch's jobs are gradients.
+template <bool BACK, typename T>
 __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant__ HeadParams p)
 {
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) unsigned long long full[kStages], empty[kStages], acc_full[2], acc_empty[2], drain;
+    __shared__ __align__(8) unsigned long long full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
     __shared__ __align__(8) unsigned long long slot_full[kSlots], slot_empty[kSlots];
     __shared__ int slot_tile[kSlots];
     __shared__ uint32_t tmem_base;
@@ -348,9 +418,10 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int stages = p.stages, stage_bytes = kRingBlocks / stages * kBlockBytes;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) {
+        for (int i = 0; i < kMaxStages; ++i) {
             barrier_init(smem_addr(&full[i]), 1);
             barrier_init(smem_addr(&empty[i]), 1);
         }
@@ -366,6 +437,11 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
         dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == 3 && lane < 3 * p.n_jobs) {
+        const HeadJob &j = p.job[lane / 3];
+        const CUtensorMap *map = lane % 3 == 0 ? &j.a : lane % 3 == 1 ? &j.b : &j.out;
+        if (lane % 3 < 2 || (BACK && !j.out_plain)) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+    }
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&tmem_base))
                      : "memory");
@@ -377,6 +453,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
     tmem_fence_after();
     grid_dependency_wait();
     grid_dependency_launch_next();
+    if (BACK && blockIdx.x == 0)
+        for (int i = threadIdx.x; i < p.n_clear; i += kHeadThreads) p.clear[i] = 0;
     asm volatile("fence.proxy.async.global;" ::: "memory");  // dz was written by ordinary stores, TMA reads it
 
     // Bounded: a wait that gives up marks the CTA dead, raises the status bit, and every role leaves its loop.
@@ -409,30 +487,20 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
             uint32_t parity = 0;
             bool ok = true;
             for (int t = pair, i = 0; t < p.tiles; ++i) {
-                int after = 0;
-                if (rank == 0) {  // fetch and announce the tile after this one
-                    after = p.next_tile ? pairs + atomicAdd(p.next_tile, 1) : t + pairs;
-                    if (!wait(smem_addr(&slot_empty[i % kSlots]), ((uint32_t)(i / kSlots) & 1u) ^ 1u)) {
-                        ok = false;
-                        break;
-                    }
-                    for (uint32_t r = 0; r < 2; ++r) {
-                        store_in(smem_addr(&slot_tile[i % kSlots]), after, r);
-                        barrier_arrive_in(smem_addr(&slot_full[i % kSlots]), r);
-                    }
-                }
+                // the tile after this one: asked for here, announced behind this one's loads
+                const int after = rank != 0 ? 0 : p.next_tile ? pairs + atomicAdd(p.next_tile, 1) : t + pairs;
                 const TilePos tp = tile_pos(p, t);
                 const HeadJob &j = p.job[tp.job];
                 const int halves = j.halves;
                 const int ra = tp.m * kTile + (int)rank * kHalf, rb = tp.n * halves * kTile + (int)rank * kHalf;
-                for (int k = 0; k < j.k_steps; ++k) {
+                for (int k = 0; k < tp.steps; ++k) {
                     if (!wait(smem_addr(&empty[stage]), parity ^ 1u)) {
                         ok = false;
                         break;
                     }
                     if (rank == 0) barrier_expect(smem_addr(&full[stage]), 2 * (1 + halves) * kBlockBytes);
-                    const uint32_t bar = leader_addr(smem_addr(&full[stage])), dst = ring + stage * kStageBytes;
-                    const int kc = k * kStepK;
+                    const uint32_t bar = leader_addr(smem_addr(&full[stage])), dst = ring + stage * stage_bytes;
+                    const int kc = (tp.k0 + k) * kStepK;
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
                         load_box(dst + i * kBoxBytes, &j.a, j.a_mn ? ra + 64 * i : kc, j.a_mn ? kc : ra + 64 * i, bar);
@@ -444,13 +512,21 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                                      j.b_mn ? kc : r + 64 * i, bar);
                     }
                     ++it;
-                    if (++stage == kStages) {
+                    if (++stage == stages) {
                         stage = 0;
                         parity ^= 1u;
                     }
                 }
                 if (!ok) break;
                 if (rank == 0) {
+                    if (!wait(smem_addr(&slot_empty[i % kSlots]), ((uint32_t)(i / kSlots) & 1u) ^ 1u)) {
+                        ok = false;
+                        break;
+                    }
+                    for (uint32_t r = 0; r < 2; ++r) {
+                        store_in(smem_addr(&slot_tile[i % kSlots]), after, r);
+                        barrier_arrive_in(smem_addr(&slot_full[i % kSlots]), r);
+                    }
                     t = after;
                 } else {
                     t = next_tile(i);
@@ -462,16 +538,16 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 }
             }
             // the last commits arrive on this CTA's barriers: it must not leave before they have
-            for (int i = 0; i < kStages && ok; ++i) {
+            for (int i = 0; i < stages && ok; ++i) {
                 ok = wait(smem_addr(&empty[stage]), parity ^ 1u);
-                if (++stage == kStages) {
+                if (++stage == stages) {
                     stage = 0;
                     parity ^= 1u;
                 }
             }
             if (!ok && rank == 0)  // what is still in flight lands in this pair's shared memory: wait for it (bounded)
-                for (int i = it < kStages ? 0 : it - kStages; i < it; ++i) {
-                    const uint32_t bar = smem_addr(&full[i % kStages]), ph = (uint32_t)(i / kStages) & 1u;
+                for (int i = it < stages ? 0 : it - stages; i < it; ++i) {
+                    const uint32_t bar = smem_addr(&full[i % stages]), ph = (uint32_t)(i / stages) & 1u;
                     for (unsigned n = 0; n < kHeadSpin && !barrier_try(bar, ph); ++n) {}
                 }
         }
@@ -485,15 +561,15 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
             for (int t = pair, i = 0; t < p.tiles; ++i) {
                 const TilePos tp = tile_pos(p, t);
                 const HeadJob &j = p.job[tp.job];
-                const int a_mn = j.a_mn, b_mn = j.b_mn, steps = j.k_steps, halves = j.halves;
+                const int a_mn = j.a_mn, b_mn = j.b_mn, steps = tp.steps, halves = j.halves;
                 const uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)a_mn << 15) |
                                        ((uint32_t)b_mn << 16) | ((uint32_t)(kTile >> 3) << 17) |
                                        ((uint32_t)(kTile >> 4) << 24);
                 const uint32_t da = a_mn ? 2048 >> 4 : 32 >> 4, db = b_mn ? 2048 >> 4 : 32 >> 4;
                 const uint64_t a_base = operand_desc(ring, a_mn), b_base = operand_desc(ring + kBlockBytes, b_mn);
                 auto issue = [&](int st, int h, int acc, int k) {
-                    const uint64_t a = a_base + (uint32_t)(st * (kStageBytes >> 4));
-                    const uint64_t b = b_base + (uint32_t)(st * (kStageBytes >> 4) + h * (kBlockBytes >> 4));
+                    const uint64_t a = a_base + (uint32_t)(st * (stage_bytes >> 4));
+                    const uint64_t b = b_base + (uint32_t)(st * (stage_bytes >> 4) + h * (kBlockBytes >> 4));
 #pragma unroll
                     for (int i = 0; i < kStepK / 16; ++i)
                         mma_f16(tmem_base + (uint32_t)acc * kTile, a + i * da, b + i * db, idesc, (uint32_t)(k | i));
@@ -517,7 +593,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                     __syncwarp();
                     ++behind;
                     if (!second) {
-                        if (behind == kStages || k + 1 == steps) {
+                        if (behind == stages || k + 1 == steps) {
                             ok = wait_warp(smem_addr(&acc_empty[acc1]), parity1);
                             if (!ok) break;
                             second = true;
@@ -532,9 +608,9 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                             mma_commit_both(smem_addr(&empty[tail]));
                         }
                         __syncwarp();
-                        if (++tail == kStages) tail = 0;
+                        if (++tail == stages) tail = 0;
                     }
-                    if (++stage == kStages) {
+                    if (++stage == stages) {
                         stage = 0;
                         parity ^= 1u;
                     }
@@ -558,34 +634,37 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
     } else if (warp >= 4) {  // ---- epilogue: a thread owns one row and half of an accumulator's columns
         const int quad = warp & 3, half = (warp - 4) >> 2;
         const float c2 = p.c2;
+        const RowsOut<T> out = {ring + kRingBlocks * kBlockBytes + (warp - 4) * kStagingBytes, lane};
         int sub = 0;
         bool ok = true;
         for (int t = pair, i = 0; t < p.tiles; ++i) {
             const TilePos tp = tile_pos(p, t);
             const HeadJob &j = p.job[tp.job];
-            const int row = tp.m * kTile + (int)rank * kHalf + quad * 32 + lane;
+            const int row0 = tp.m * kTile + (int)rank * kHalf + quad * 32, row = row0 + lane;
+            const bool live = row < p.n, logits = !BACK || j.kind == kLogitGrad;
+            // what a row needs, loaded before the tile is ready
             [[maybe_unused]] float gs = 0.0f, l2 = 0.0f;
-            const bool live = row < p.n;
-            if constexpr (BACK) {
-                if (j.kind == kLogitGrad && live) {
-                    const bool wanted = p.k ? p.entropy[row] < INFINITY : p.labels[row] >= 0 && p.labels[row] < p.vocab_total;
+            [[maybe_unused]] Targets tg;
+            [[maybe_unused]] int label = INT_MAX;   // relative to the job's first column
+            const int v0 = (int)j.v0;
+            if (logits) {
+                const long long y = live && !p.k ? p.labels[row] : -1;
+                if (p.k)
+                    tg.start(p, row, v0 + tp.n * j.halves * kTile + half * kHalf, live);
+                else if (y >= j.v0 && y < j.v0 + j.vocab)
+                    label = (int)(y - j.v0);
+                if (BACK && live) {
+                    const bool wanted = p.k ? p.entropy[row] < INFINITY : y >= 0 && y < p.vocab_total;
                     gs = wanted ? p.grad[row] * p.temperature * (p.scale ? p.scale[0] : 1.0f) : 0.0f;
                     l2 = p.lse[row] * 1.4426950408889634f;
                 }
             }
+            const float back = BACK && !logits && p.scale ? p.scale[1] : 1.0f;
             for (int h = 0; h < j.halves; ++h, ++sub) {
                 const int acc = sub & 1;
                 const int col0 = (tp.n * j.halves + h) * kTile + half * kHalf;
                 const uint32_t src = tmem_base + (uint32_t)acc * kTile + half * kHalf + ((uint32_t)(quad * 32) << 16);
-                // what a row needs, loaded before the tile is ready
-                [[maybe_unused]] Targets tg;
-                [[maybe_unused]] long long label = -1;
-                if (!BACK || j.kind == kLogitGrad) {
-                    if (p.k)
-                        tg.start(p, row, j.v0 + col0, live);
-                    else
-                        label = live ? p.labels[row] - j.v0 - col0 : -1;
-                }
+                if (logits && p.k) tg.skip_to(v0 + col0);
                 ok = __all_sync(0xFFFFFFFFu, wait(smem_addr(&acc_full[acc]), (uint32_t)((sub >> 1) & 1)));
                 if (!ok) break;
                 tmem_fence_after();
@@ -612,78 +691,56 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                                 p.target_z[(long long)row * p.k + tg.j] = pick32(z, tg.next - col);
                                 tg.advance();
                             }
-                        } else if (label >= 32 * ch && label < 32 * ch + 32) {
-                            p.target_z[row] = pick32(z, (int)label - 32 * ch);
+                        } else if (label >= col && label < col + 32) {
+                            p.target_z[row] = pick32(z, label - col);
                         }
                         if (col + 32 > j.vocab) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
                                 if (col + i >= j.vocab) z[i] = -INFINITY;
                         }
-                        float top = z[0];
+                        // four chains each, so that their latencies overlap
+                        float top[4], add[4];
 #pragma unroll
-                        for (int i = 1; i < 32; ++i) top = fmaxf(top, z[i]);
-                        const float now = fmaxf(m, top * c2);
+                        for (int i = 0; i < 4; ++i) top[i] = fmaxf(z[i], z[i + 4]), add[i] = 0.0f;
+#pragma unroll
+                        for (int i = 8; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], z[i]);
+                        const float now = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c2);
                         const float ref = now == -INFINITY ? 0.0f : now;
-                        float add = 0.0f;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) add += exp2_approx(fmaf(z[i], c2, -ref));
-                        s = fmaf(s, exp2_approx(m - ref), add);
+                        for (int i = 0; i < 32; ++i) add[i & 3] += exp2_approx(fmaf(z[i], c2, -ref));
+                        s = fmaf(s, exp2_approx(m - ref), (add[0] + add[1]) + (add[2] + add[3]));
                         m = now;
-                    } else if (j.kind == kLogitGrad) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) z[i] = gs * exp2_approx(fmaf(z[i], c2, -l2));
-                        if (p.k) {
-                            while (tg.next < j.v0 + col + 32) {
-                                subtract32(z, tg.next - (int)j.v0 - col, gs * p.target_q[(long long)row * p.k + tg.j]);
-                                tg.advance();
-                            }
-                        } else if (label >= 32 * ch && label < 32 * ch + 32) {
-                            subtract32(z, (int)label - 32 * ch, gs);
-                        }
-                        if (col + 32 > j.vocab || gs == 0.0f) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (col + i >= j.vocab || gs == 0.0f) z[i] = 0.0f;
-                        }
-                        // dz in 16 bits, as both products' operand: their sums run over it in binary32
-                        if (live && col < p.dz_pitch) store_row32<T>((T *)j.dz + (long long)row * p.dz_pitch + col, z, 32, true);
                     } else {
-                        const float back = p.scale ? p.scale[1] : 1.0f;
-                        const int count = min(32, p.width - col);
-                        if (j.kind == kHiddenGrad) {
-                            if (live && count > 0) {
-                                float *sum = p.dh_sum + (long long)row * p.dh_sum_pitch + col;
-                                if (!j.first) {
+                        if (logits) {
 #pragma unroll
-                                    for (int i = 0; i < 8; ++i) {
-                                        if (4 * i < count) {  // the pitch is a multiple of 4
-                                            const float4 o = reinterpret_cast<const float4 *>(sum)[i];
-                                            z[4 * i] += o.x;
-                                            z[4 * i + 1] += o.y;
-                                            z[4 * i + 2] += o.z;
-                                            z[4 * i + 3] += o.w;
-                                        }
-                                    }
+                            for (int i = 0; i < 32; ++i) z[i] = gs * exp2_approx(fmaf(z[i], c2, -l2));
+                            if (p.k) {
+                                while (tg.next < v0 + col + 32) {
+                                    subtract32(z, tg.next - v0 - col, gs * p.target_q[(long long)row * p.k + tg.j]);
+                                    tg.advance();
                                 }
-                                if (j.last) {
-#pragma unroll
-                                    for (int i = 0; i < 32; ++i) z[i] *= back;
-                                    T *dst = (T *)p.dh + (long long)row * p.dh_stride + col;
-                                    store_row32<T>(dst, z, count, ((uintptr_t)dst & 15) == 0);
-                                } else {
-#pragma unroll
-                                    for (int i = 0; i < 8; ++i)
-                                        if (4 * i < count)
-                                            reinterpret_cast<float4 *>(sum)[i] =
-                                                make_float4(z[4 * i], z[4 * i + 1], z[4 * i + 2], z[4 * i + 3]);
-                                }
+                            } else if (label >= col && label < col + 32) {
+                                subtract32(z, label - col, gs);
                             }
-                        } else if (row < j.vocab && count > 0) {
+                            if (col + 32 > j.vocab || gs == 0.0f) {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    if (col + i >= j.vocab || gs == 0.0f) z[i] = 0.0f;
+                            }
+                        } else if (back != 1.0f) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i) z[i] *= back;
-                            Q *dst = (Q *)p.dw + (j.v0 + row) * p.dw_stride + col;
-                            store_row32<Q>(dst, z, count, ((uintptr_t)dst & 15) == 0);
+                        }
+                        // dz leaves in 16 bits, as both products' operand: their sums run over it in binary32
+                        if (j.out_mode == kOut16) {
+                            if (!(ch & 1)) out.wait_free();
+                            out.put16(ch & 1, z);
+                            if (ch & 1) out.flush(j, row0, col - 32, tp.split);
+                        } else {
+                            out.wait_free();
+                            out.put32(z);
+                            out.flush(j, row0, col, tp.split);
                         }
                     }
                 }
@@ -698,6 +755,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
             if (!ok) break;
             if (lane == 0) barrier_arrive_leader(smem_addr(&slot_empty[i % kSlots]));
         }
+        if (BACK && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     __syncthreads();
@@ -875,6 +933,38 @@ k_head_join(const float2 *__restrict__ partial, int parts, int n, const long lon
     }
 }
 
+// dh = the sum of its parts, in order, rounded once: a thread per four columns.
+template <typename T>
+__global__ void __launch_bounds__(256)
+k_head_hidden_sum(const float *__restrict__ sum, long long pitch, int parts, int n, int d, T *__restrict__ dh,
+                  long long stride)
+{
+    grid_dependency_wait();
+    grid_dependency_launch_next();
+    const int row = blockIdx.y, col = 4 * (blockIdx.x * 256 + threadIdx.x);
+    if (col >= d) return;
+    const float *src = sum + (long long)row * pitch + col;
+    const long long slab = (long long)n * pitch;
+    float4 t = *reinterpret_cast<const float4 *>(src);
+#pragma unroll 4
+    for (int i = 1; i < parts; ++i) {
+        const float4 o = *reinterpret_cast<const float4 *>(src + i * slab);
+        t.x += o.x;
+        t.y += o.y;
+        t.z += o.z;
+        t.w += o.w;
+    }
+    T *dst = dh + (long long)row * stride + col;
+    const float v[4] = {t.x, t.y, t.z, t.w};
+    if (col + 4 <= d && ((uintptr_t)dst & 7) == 0) {
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (col + i < d) dst[i] = from_f32<T>(v[i]);
+    }
+}
+
 // ---- host ---------------------------------------------------------------------------------------
 namespace {
 
@@ -913,16 +1003,49 @@ cudaError_t encode(CUtensorMap *map, int dtype, const void *base, long long rows
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+// C of a job: parts x rows x cols values of `elem` bytes in boxes of 32 rows x 128 bytes; falls back to plain stores
+// where rows do not start on 16-byte boundaries
+cudaError_t set_output(HeadJob &j, int mode, int dtype, void *base, long long rows, long long cols, long long stride,
+                       long long parts = 1)
+{
+    const int elem = mode == kOut16 ? 2 : 4;
+    j.out_mode = mode;
+    j.out_ptr = base;
+    j.out_stride = stride;
+    j.out_rows = (int)rows;
+    j.out_cols = (int)cols;
+    j.out_plain = !pointer_aligned(base, 16) || (stride * elem) % 16 != 0;
+    if (j.out_plain) return parts == 1 && mode != kOutAddF32 ? cudaSuccess : cudaErrorInvalidValue;
+    EncodeFn fn = encode_fn();
+    if (!fn) return cudaErrorNotSupported;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
+    const cuuint64_t strides[2] = {(cuuint64_t)stride * elem, (cuuint64_t)stride * elem * rows};
+    const cuuint32_t box[3] = {(cuuint32_t)(128 / elem), 32, 1}, one[3] = {1, 1, 1};
+    const CUresult r = fn(&j.out, mode != kOut16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                  : dtype == RSDGC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                        : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                          3, base, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 inline int tiles_of(int64_t a) { return (int)((a + kTile - 1) / kTile); }
 
-// A piece of the vocabulary: dz (n x piece, 16 bits) of about kPieceBytes, twice (one is written while the other
-// is read); never under kPieceMin columns, because every piece adds to dh once.
-constexpr int64_t kPieceBytes = 64ll << 20;
+// A piece of the vocabulary: dz (n x piece, 16 bits) of at most kPieceBytes, in two buffers (one is written while the
+// other is read); never under kPieceMin columns, because every piece adds to dh once.  A launch ends on its longest
+// tiles, so few large pieces are better than what L2 would hold: 8192 x 128000 x 4096 takes 22.2 / 20.7 / 20.1 / 19.9 ms
+// with pieces of 64 / 128 / 256 / 512 MB.
+constexpr int64_t kPieceBytes = 256ll << 20;
 constexpr int64_t kPieceMin = 2048;
+// With few tokens dh has few tiles, each with a contraction over the whole piece: it is cut into parts that are added
+// up at the end, in order, so that about kSplitTiles tiles share a launch with dW's, none longer than the launch's fair
+// share.  More parts cost more in sums than they balance (1023 x 50001 x 1000: 369 us with 5 parts, 392 with 10, 417
+// with 19, 660 with one).
+constexpr int64_t kSplitTiles = 37, kSplitSteps = 8;
 
 struct HeadLayout {
-    int64_t piece, pieces;
+    int64_t piece, pieces, splits;
     int64_t partial, target_z, index, q, entropy, scale, counter, dz[2], dh_sum, bytes;
     int64_t dh_pitch;
 };
@@ -936,6 +1059,10 @@ HeadLayout head_layout(int64_t n, int64_t v, int64_t d, int64_t k)
     L.piece = up((v + L.pieces - 1) / L.pieces, kTile);
     L.pieces = (v + L.piece - 1) / L.piece;
     L.dh_pitch = up(d, 4);
+    const int64_t area = tiles_of(n) * ((tiles_of(d) + 1) / 2), steps = L.piece / kStepK;
+    L.splits = area > 0 ? (kSplitTiles + area - 1) / area : 1;
+    if (L.splits > steps / kSplitSteps) L.splits = steps / kSplitSteps;
+    if (L.splits < 1) L.splits = 1;
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t p = at;
@@ -947,14 +1074,14 @@ HeadLayout head_layout(int64_t n, int64_t v, int64_t d, int64_t k)
     L.q = take(4 * n * k);
     L.entropy = take(4 * n);
     L.scale = take(8);
-    L.counter = take(4 * (L.pieces + 1));
+    L.counter = take(4 * L.pieces);
     const int64_t shared = at;  // the forward pass's partials and the backward pass's dz share the rest
     L.partial = take(8 * n * 2 * tiles_of(v));
     L.bytes = at;
     at = shared;
     L.dz[0] = take(2 * n * L.piece);
     L.dz[1] = take(L.pieces > 1 ? 2 * n * L.piece : 0);
-    L.dh_sum = take(L.pieces > 1 ? 4 * n * L.dh_pitch : 0);
+    L.dh_sum = take(L.pieces > 1 || L.splits > 1 ? 4 * n * L.dh_pitch * L.splits : 0);
     if (at > L.bytes) L.bytes = at;
     return L;
 }
@@ -1003,7 +1130,7 @@ int call_check(const HeadCall &c)
 }
 
 // Clusters of two that the device holds at a time; 0 and an error in *e if the kernel cannot run.
-template <bool BACK, typename T, typename Q>
+template <bool BACK, typename T>
 int head_pairs(cudaError_t *e)
 {
     static std::mutex mu;
@@ -1014,7 +1141,7 @@ int head_pairs(cudaError_t *e)
     std::lock_guard<std::mutex> lock(mu);
     int &m = most[dev & 63];
     if (m) return m;
-    *e = cudaFuncSetAttribute(k_head<BACK, T, Q>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem);
+    *e = cudaFuncSetAttribute(k_head<BACK, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem);
     if (*e != cudaSuccess) return 0;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = (unsigned)current_device_sms();
@@ -1027,32 +1154,38 @@ int head_pairs(cudaError_t *e)
     cfg.attrs = &at;
     cfg.numAttrs = 1;
     int n = 0;
-    *e = cudaOccupancyMaxActiveClusters(&n, k_head<BACK, T, Q>, &cfg);
+    *e = cudaOccupancyMaxActiveClusters(&n, k_head<BACK, T>, &cfg);
     if (*e == cudaSuccess && n < 1) *e = cudaErrorLaunchOutOfResources;
     if (*e != cudaSuccess) return 0;
     return m = n;
 }
 
-template <bool BACK, typename T, typename Q>
+template <bool BACK, typename T>
 cudaError_t launch_tiles(HeadParams &p, int *counter, cudaStream_t s)
 {
     cudaError_t e = cudaSuccess;
-    const int most = head_pairs<BACK, T, Q>(&e);
+    const int most = head_pairs<BACK, T>(&e);
     if (e != cudaSuccess) return e;
     long long tiles = 0;
-    for (int i = 0; i < p.n_jobs; ++i) tiles += (long long)p.job[i].m_tiles * p.job[i].n_tiles;
+    int halves = 1;
+    for (int i = 0; i < p.n_jobs; ++i) {
+        tiles += (long long)p.job[i].m_tiles * p.job[i].n_tiles * p.job[i].splits;
+        if (p.job[i].halves > halves) halves = p.job[i].halves;
+    }
+    p.stages = kRingBlocks / (1 + halves);
     if (tiles > INT_MAX / 2) return cudaErrorInvalidValue;
     p.tiles = (int)tiles;
     p.next_tile = counter;
     const unsigned pairs = (unsigned)(tiles < most ? tiles : most);
-    return launch_chained(k_head<BACK, T, Q>, 2 * pairs, kHeadThreads, kHeadSmem, s, 2, p);
+    return launch_chained(k_head<BACK, T>, 2 * pairs, kHeadThreads, kHeadSmem, s, 2, p);
 }
 
 constexpr double kTruncationBf16 = 0.26, kTruncationF16 = 0.29;
 constexpr int kBand = 16;
-// Two accumulators per tile (256 x 512): every operand block brought in serves more products, 48 instead of 64 bytes
-// per cycle and SM at the full MMA rate; but the first accumulator is then idle while it is emptied.
-constexpr int kTwoHalvesFrom = 16;  // contraction steps
+// Two accumulators per tile (256 x 512) wherever there are columns for them: every operand block brought in serves
+// more products, 48 instead of 64 bytes per cycle and SM at the full MMA rate, and the ring holds twice the work.
+// (Forward 2048 x 32000 x 2048: 219 us against 286; 333 x 10007 x 776: 20 against 24; 64 x 32000 x 4096: 64 against 82.)
+constexpr int kTwoHalvesFrom = kTile + 1;  // columns
 
 cudaError_t set_job(HeadJob &j, int kind, int dtype, const void *a, bool a_mn, long long ar, long long ac, long long as,
                     const void *b, bool b_mn, long long br, long long bc, long long bs, long long m, long long n, long long k)
@@ -1062,10 +1195,12 @@ cudaError_t set_job(HeadJob &j, int kind, int dtype, const void *a, bool a_mn, l
     j.a_mn = a_mn;
     j.b_mn = b_mn;
     j.k_steps = (int)((k + kStepK - 1) / kStepK);
-    j.halves = j.k_steps >= kTwoHalvesFrom && n > kTile ? 2 : 1;
     j.m_tiles = tiles_of(m);
+    j.halves = n >= kTwoHalvesFrom ? 2 : 1;
     j.n_tiles = (tiles_of(n) + j.halves - 1) / j.halves;
     j.band = j.m_tiles < kBand ? j.m_tiles : kBand;
+    j.splits = 1;
+    j.split_steps = j.k_steps;
     const cudaError_t e = encode(&j.a, dtype, a, ar, ac, as);
     return e == cudaSuccess ? encode(&j.b, dtype, b, br, bc, bs) : e;
 }
@@ -1124,8 +1259,8 @@ int head_forward(const HeadCall &c, float *loss, float *lse)
     p.job[0].vocab = (int)c.v;
     if (e == cudaSuccess) e = targets(c, L);
     if (e == cudaSuccess)
-        e = c.dtype == RSDGC_BF16 ? launch_tiles<false, __nv_bfloat16, __nv_bfloat16>(p, nullptr, c.s)
-                                  : launch_tiles<false, __half, __half>(p, nullptr, c.s);
+        e = c.dtype == RSDGC_BF16 ? launch_tiles<false, __nv_bfloat16>(p, nullptr, c.s)
+                                  : launch_tiles<false, __half>(p, nullptr, c.s);
     if (e == cudaSuccess)
         e = launch_chained(k_head_join, (unsigned)((c.n + kJoinRows - 1) / kJoinRows), 256, 0, c.s, 1, (const float2 *)p.partial,
                            p.parts, (int)c.n, c.labels, (long long)c.v, p.target_index, p.target_q,
@@ -1133,51 +1268,77 @@ int head_forward(const HeadCall &c, float *loss, float *lse)
     return operator_result(e);
 }
 
+struct HeadGrads {
+    void *dh, *dw;
+    long long dh_stride, dw_stride;
+    int dw_dtype;
+};
+
 // Launch i computes piece i's dz and, from the piece before it, dh and dW: three products whose tiles share a queue,
-// longest contraction first, so that the multiprocessors end together.
-template <typename T, typename Q>
-cudaError_t backward_pieces(const HeadCall &c, const HeadLayout &L, HeadParams &p)
+// longest contraction first, so that the multiprocessors end together.  dh goes to binary32 sums unless one piece in one
+// part is all there is: stored by the first piece, added to by the others (one bulk reduction per element and launch).
+template <typename T>
+cudaError_t backward_pieces(const HeadCall &c, const HeadLayout &L, HeadParams &p, const HeadGrads &g)
 {
+    int parts = 1;
+    float *sum = (float *)(c.workspace + L.dh_sum);
+    int *counter = (int *)(c.workspace + L.counter);
     for (int64_t i = 0; i <= L.pieces; ++i) {
         cudaError_t e = cudaSuccess;
         p.n_jobs = 0;
-        auto piece = [&](HeadJob &j, int64_t at) {
-            j.v0 = at * L.piece;
-            j.vocab = (int)(c.v - j.v0 < L.piece ? c.v - j.v0 : L.piece);
-            j.dz = c.workspace + L.dz[at & 1];
-            j.first = at == 0;
-            j.last = at + 1 == L.pieces;
-        };
         auto rows = [&](int64_t at) { return c.v - at * L.piece < L.piece ? c.v - at * L.piece : L.piece; };
         auto weight = [&](int64_t at) { return (const unsigned char *)c.weight + at * L.piece * c.ws * 2; };
+        auto buffer = [&](int64_t at) { return c.workspace + L.dz[at & 1]; };
         if (i < L.pieces) {
             HeadJob &j = p.job[p.n_jobs++];
             e = set_job(j, kLogitGrad, c.dtype, c.hidden, false, c.n, c.d, c.hs, weight(i), false, rows(i), c.d, c.ws, c.n,
                         rows(i), c.d);
-            piece(j, i);
+            j.v0 = i * L.piece;
+            j.vocab = (int)rows(i);
+            if (e == cudaSuccess) e = set_output(j, kOut16, c.dtype, buffer(i), c.n, L.piece, L.piece);
         }
         if (i > 0 && e == cudaSuccess) {
             const int64_t at = i - 1, v = rows(at);
-            const void *dz = c.workspace + L.dz[at & 1];
+            const void *dz = buffer(at);
             // the tiles of dz are whole: zeros beyond the vocabulary, so the contraction may run over whole steps
             HeadJob &j = p.job[p.n_jobs++];
             e = set_job(j, kHiddenGrad, c.dtype, dz, false, c.n, L.piece, L.piece, weight(at), true, v, c.d, c.ws, c.n, c.d, v);
-            piece(j, at);
+            j.split_steps = (j.k_steps + (int)L.splits - 1) / (int)L.splits;
+            j.splits = (j.k_steps + j.split_steps - 1) / j.split_steps;
+            if (at == 0) parts = j.splits;  // the other pieces are no longer: they have no more parts
+            if (e == cudaSuccess)
+                e = L.pieces == 1 && parts == 1
+                        ? set_output(j, kOut16, c.dtype, g.dh, c.n, c.d, g.dh_stride)
+                        : set_output(j, at == 0 ? kOutF32 : kOutAddF32, c.dtype, sum, c.n, c.d, L.dh_pitch, parts);
             if (e == cudaSuccess) {
                 HeadJob &w = p.job[p.n_jobs++];
                 e = set_job(w, kWeightGrad, c.dtype, dz, true, c.n, L.piece, L.piece, c.hidden, true, c.n, c.d, c.hs, v, c.d, c.n);
-                piece(w, at);
+                const bool wide = g.dw_dtype == RSDGC_F32;
+                if (e == cudaSuccess)
+                    e = set_output(w, wide ? kOutF32 : kOut16, c.dtype,
+                                   (unsigned char *)g.dw + at * L.piece * g.dw_stride * (wide ? 4 : 2), v, c.d, g.dw_stride);
             }
         }
         if (e != cudaSuccess) return e;
-        auto length = [](const HeadJob &j) { return j.k_steps * j.halves; };
+        auto length = [](const HeadJob &j) { return j.split_steps * j.halves; };
         for (int a = 0; a < p.n_jobs; ++a)
             for (int b = a + 1; b < p.n_jobs; ++b)
                 if (length(p.job[b]) > length(p.job[a])) std::swap(p.job[a], p.job[b]);
-        e = launch_tiles<true, T, Q>(p, (int *)(c.workspace + L.counter) + i, c.s);
+        // the first launch has tiles of one length and deals them out in rounds; it clears the others' counters
+        p.clear = counter;
+        p.n_clear = i == 0 ? (int)L.pieces : 0;
+        e = launch_tiles<true, T>(p, i == 0 ? nullptr : counter + i - 1, c.s);
         if (e != cudaSuccess) return e;
     }
-    return cudaSuccess;
+    if (L.pieces == 1 && parts == 1) return cudaSuccess;
+    const unsigned wide = (unsigned)((c.d + 1023) / 1024);
+    cudaError_t e = cudaSuccess;
+    for (int64_t row = 0; row < c.n && e == cudaSuccess; row += 32768) {  // rows of a grid
+        const unsigned rows = (unsigned)(c.n - row < 32768 ? c.n - row : 32768);
+        e = launch_chained(k_head_hidden_sum<T>, dim3(wide, rows), 256, 0, c.s, 1, (const float *)sum + row * L.dh_pitch,
+                           (long long)L.dh_pitch, parts, (int)c.n, (int)c.d, (T *)g.dh + row * g.dh_stride, g.dh_stride);
+    }
+    return e;
 }
 
 int head_backward(const HeadCall &c, const float *lse, const float *grad, void *dh, int64_t dh_stride, void *dw,
@@ -1202,15 +1363,6 @@ int head_backward(const HeadCall &c, const float *lse, const float *grad, void *
     common_params(p, c, L);
     p.lse = lse;
     p.grad = grad;
-    p.dz_pitch = L.piece;
-    p.dh_sum = (float *)(c.workspace + L.dh_sum);
-    p.dh_sum_pitch = L.dh_pitch;
-    p.dh = dh;
-    p.dh_stride = dh_stride;
-    p.dw = dw;
-    p.dw_stride = dw_stride;
-    p.width = (int)c.d;
-    if (e == cudaSuccess) e = cudaMemsetAsync(c.workspace + L.counter, 0, 4 * (size_t)(L.pieces + 1), c.s);
     if (e == cudaSuccess) e = targets(c, L);
     if (e == cudaSuccess && c.dtype == RSDGC_F16) {
         p.scale = (const float *)(c.workspace + L.scale);
@@ -1218,11 +1370,8 @@ int head_backward(const HeadCall &c, const float *lse, const float *grad, void *
                            c.temperature, (float *)(c.workspace + L.scale));
     }
     if (e == cudaSuccess) {
-        if (c.dtype == RSDGC_BF16)
-            e = dw_dtype == RSDGC_F32 ? backward_pieces<__nv_bfloat16, float>(c, L, p)
-                                      : backward_pieces<__nv_bfloat16, __nv_bfloat16>(c, L, p);
-        else
-            e = dw_dtype == RSDGC_F32 ? backward_pieces<__half, float>(c, L, p) : backward_pieces<__half, __half>(c, L, p);
+        const HeadGrads g = {dh, dw, dh_stride, dw_stride, dw_dtype};
+        e = c.dtype == RSDGC_BF16 ? backward_pieces<__nv_bfloat16>(c, L, p, g) : backward_pieces<__half>(c, L, p, g);
     }
     return operator_result(e);
 }
