@@ -159,7 +159,11 @@ __device__ __forceinline__ void barrier_arrive_in(uint32_t bar, uint32_t rank)
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr_in(bar, rank)) : "memory");
 }
-__device__ __forceinline__ void barrier_arrive_leader(uint32_t bar) { barrier_arrive_in(bar, 0); }
+// An arrival that publishes no memory: what it orders are TMEM reads (by their own fence) and values already used.
+__device__ __forceinline__ void barrier_arrive_leader(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_addr(bar)) : "memory");
+}
 __device__ __forceinline__ void store_in(uint32_t addr, int value, uint32_t rank)
 {
     asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(addr_in(addr, rank)), "r"(value) : "memory");
@@ -203,13 +207,59 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32])
         : "r"(addr));
 }
 // The loaded registers pass through the wait, so that nothing reads them before it.
-__device__ __forceinline__ void tmem_wait_load(uint32_t (&r)[32])
+__device__ __forceinline__ void tie32(uint32_t (&r)[32])
 {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
+    asm volatile(""
                  : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
                    "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
                    "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
                    "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
+}
+// 128 columns of the warp's 32 rows
+__device__ __forceinline__ void tmem_load128(uint32_t addr, uint32_t (&r)[4][32])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) tmem_load32(addr + 32 * i, r[i]);
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) tie32(r[i]);
+}
+// Two binary32 operations per instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\t"
+        "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 // One thread of the converged warp, the same one each time; its branch is known to be taken by a single thread.
 __device__ __forceinline__ bool elect_one()
@@ -296,12 +346,12 @@ __device__ __forceinline__ void add_box(const CUtensorMap *map, int x, int y, in
                  : "memory");
 }
 
-__device__ __forceinline__ float pick32(const float (&z)[32], int i)
+__device__ __forceinline__ float pick32(const uint32_t (&z)[32], int i)
 {
-    float v = z[0];
+    uint32_t v = z[0];
 #pragma unroll
     for (int j = 1; j < 32; ++j) v = i == j ? z[j] : v;
-    return v;
+    return __uint_as_float(v);
 }
 __device__ __forceinline__ void subtract32(float (&z)[32], int i, float x)
 {
@@ -481,8 +531,10 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
         return -1;
     };
 
-    if (warp == 0) {
-        if (lane == 0) {  // ---- producer, in both CTAs; all bytes count on the first CTA's barriers
+    // registers: 168 per thread at launch, 384 * 168 = 128 * 72 + 256 * 216
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == 0 && lane == 0) {  // ---- producer, in both CTAs; all bytes count on the first CTA's barriers
             int stage = 0, it = 0;
             uint32_t parity = 0;
             bool ok = true;
@@ -551,8 +603,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                     for (unsigned n = 0; n < kHeadSpin && !barrier_try(bar, ph); ++n) {}
                 }
         }
-    } else if (warp == 1) {
-        if (rank == 0) {  // ---- MMA, the pair's first CTA: the warp walks together, one thread issues
+        if (warp == 1 && rank == 0) {  // ---- MMA, the pair's first CTA: the warp walks together, one thread issues
             int stage = 0, sub = 0;    // sub: accumulators used so far; they alternate
             uint32_t parity = 0;
             bool ok = true;
@@ -631,7 +682,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 for (unsigned n = 0; n < kHeadSpin && !barrier_try(smem_addr(&drain), 0); ++n) {}
             }
         }
-    } else if (warp >= 4) {  // ---- epilogue: a thread owns one row and half of an accumulator's columns
+    } else {  // ---- epilogue: a thread owns one row and half of an accumulator's columns
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int quad = warp & 3, half = (warp - 4) >> 2;
         const float c2 = p.c2;
         const RowsOut<T> out = {ring + kRingBlocks * kBlockBytes + (warp - 4) * kStagingBytes, lane};
@@ -668,53 +720,78 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 ok = __all_sync(0xFFFFFFFFu, wait(smem_addr(&acc_full[acc]), (uint32_t)((sub >> 1) & 1)));
                 if (!ok) break;
                 tmem_fence_after();
-                [[maybe_unused]] float m = -INFINITY, s = 0.0f;
-                uint32_t raw[2][32];
-                tmem_load32(src, raw[0]);
+                // The accumulator goes to registers at once and is free for the tile after the next: what follows
+                // does not hold up the MMAs.
+                uint32_t raw[4][32];
+                tmem_load128(src, raw);
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive_leader(smem_addr(&acc_empty[acc]));
+                const bool ragged = logits && col0 + kHalf > j.vocab;
+                if constexpr (!BACK) {
 #pragma unroll
-                for (int ch = 0; ch < kHalf / 32; ++ch) {
-                    tmem_wait_load(raw[ch & 1]);
-                    if (ch + 1 < kHalf / 32) {
-                        tmem_load32(src + 32 * (ch + 1), raw[(ch + 1) & 1]);
-                    } else {  // the accumulator is read: the tile after the next may overwrite it
-                        tmem_fence_before();
-                        __syncwarp();
-                        if (lane == 0) barrier_arrive_leader(smem_addr(&acc_empty[acc]));
-                    }
-                    float z[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(raw[ch & 1][i]);
-                    const int col = col0 + 32 * ch;
-                    if constexpr (!BACK) {
+                    for (int ch = 0; ch < 4; ++ch) {
+                        const int col = col0 + 32 * ch;
                         if (p.k) {
                             while (tg.next < col + 32) {
-                                p.target_z[(long long)row * p.k + tg.j] = pick32(z, tg.next - col);
+                                p.target_z[(long long)row * p.k + tg.j] = pick32(raw[ch], tg.next - col);
                                 tg.advance();
                             }
                         } else if (label >= col && label < col + 32) {
-                            p.target_z[row] = pick32(z, label - col);
+                            p.target_z[row] = pick32(raw[ch], label - col);
                         }
-                        if (col + 32 > j.vocab) {
+                        if (ragged) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
-                                if (col + i >= j.vocab) z[i] = -INFINITY;
+                                if (col + i >= j.vocab) raw[ch][i] = 0xFF800000u;  // -inf
                         }
-                        // four chains each, so that their latencies overlap
-                        float top[4], add[4];
+                    }
+                    // independent chains, so that their latencies overlap
+                    float top[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) top[i] = fmaxf(z[i], z[i + 4]), add[i] = 0.0f;
+                    for (int c = 0; c < 4; ++c) {
+                        top[c] = __uint_as_float(raw[c][0]);
 #pragma unroll
-                        for (int i = 8; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], z[i]);
-                        const float now = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c2);
-                        const float ref = now == -INFINITY ? 0.0f : now;
+                        for (int i = 1; i < 31; i += 2)
+                            top[c] = max3(top[c], __uint_as_float(raw[c][i]), __uint_as_float(raw[c][i + 1]));
+                        top[c] = fmaxf(top[c], __uint_as_float(raw[c][31]));
+                    }
+                    const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c2;
+                    const float ref = m == -INFINITY ? 0.0f : m;
+                    const float2 cc = make_float2(c2, c2), rr = make_float2(-ref, -ref);
+                    float2 add[4];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) add[i & 3] += exp2_approx(fmaf(z[i], c2, -ref));
-                        s = fmaf(s, exp2_approx(m - ref), (add[0] + add[1]) + (add[2] + add[3]));
-                        m = now;
-                    } else {
+                    for (int c = 0; c < 4; ++c) add[c] = make_float2(0.0f, 0.0f);
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const float2 x =
+                                fma2(make_float2(__uint_as_float(raw[c][i]), __uint_as_float(raw[c][i + 1])), cc, rr);
+                            add[c] = add2(add[c], make_float2(exp2_approx(x.x), exp2_approx(x.y)));
+                        }
+                    const float2 sum = add2(add2(add[0], add[1]), add2(add[2], add[3]));
+                    const int part = col0 / kHalf;
+                    if (live && part < p.parts) p.partial[(long long)part * p.n + row] = make_float2(m, sum.x + sum.y);
+                } else {
+                    const float2 cc = make_float2(c2, c2), ll = make_float2(-l2, -l2);
+                    const float2 factor = logits ? make_float2(gs, gs) : make_float2(back, back);
+#pragma unroll
+                    for (int ch = 0; ch < 4; ++ch) {
+                        const int col = col0 + 32 * ch;
+                        float z[32];
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            float2 x = make_float2(__uint_as_float(raw[ch][i]), __uint_as_float(raw[ch][i + 1]));
+                            if (logits) {
+                                x = fma2(x, cc, ll);
+                                x = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+                            }
+                            x = mul2(x, factor);
+                            z[i] = x.x;
+                            z[i + 1] = x.y;
+                        }
                         if (logits) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) z[i] = gs * exp2_approx(fmaf(z[i], c2, -l2));
                             if (p.k) {
                                 while (tg.next < v0 + col + 32) {
                                     subtract32(z, tg.next - v0 - col, gs * p.target_q[(long long)row * p.k + tg.j]);
@@ -723,14 +800,11 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                             } else if (label >= col && label < col + 32) {
                                 subtract32(z, label - col, gs);
                             }
-                            if (col + 32 > j.vocab || gs == 0.0f) {
+                            if (ragged || gs == 0.0f) {
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
                                     if (col + i >= j.vocab || gs == 0.0f) z[i] = 0.0f;
                             }
-                        } else if (back != 1.0f) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) z[i] *= back;
                         }
                         // dz leaves in 16 bits, as both products' operand: their sums run over it in binary32
                         if (j.out_mode == kOut16) {
@@ -743,10 +817,6 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                             out.flush(j, row0, col, tp.split);
                         }
                     }
-                }
-                if constexpr (!BACK) {
-                    const int part = col0 / kHalf;
-                    if (live && part < p.parts) p.partial[(long long)part * p.n + row] = make_float2(m, s);
                 }
             }
             if (!ok) break;
@@ -1142,6 +1212,10 @@ int head_pairs(cudaError_t *e)
     int &m = most[dev & 63];
     if (m) return m;
     *e = cudaFuncSetAttribute(k_head<BACK, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem);
+    if (*e != cudaSuccess) return 0;
+    cudaFuncAttributes attr{};
+    *e = cudaFuncGetAttributes(&attr, k_head<BACK, T>);
+    if (*e == cudaSuccess && attr.numRegs != 168) *e = cudaErrorLaunchOutOfResources;  // the kernel's register split relies on it
     if (*e != cudaSuccess) return 0;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = (unsigned)current_device_sms();
