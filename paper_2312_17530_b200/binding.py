@@ -148,10 +148,32 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _stream() -> int:
-    import torch
+class _Torch:
+    """What the calls need of torch, looked up once (importing this module does not import torch)."""
 
-    return torch.cuda.current_stream().cuda_stream
+    def __init__(self):
+        import torch
+
+        self.f32, self.i64 = torch.float32, torch.int64
+        self.codes = {torch.float32: RSDGC_F32, torch.bfloat16: RSDGC_BF16, torch.float16: RSDGC_F16}
+        self.device = torch.cuda.current_device
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # the handle without a Stream object around it
+        self.stream = raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
+_torch = None
+
+
+def _tt() -> _Torch:
+    global _torch
+    if _torch is None:
+        _torch = _Torch()
+    return _torch
+
+
+def _stream() -> int:
+    t = _torch or _tt()
+    return t.stream(t.device())
 
 
 class Plan:
@@ -340,49 +362,49 @@ def update_ratios_noalloc(weights, layer_offsets: Sequence[int], layer_sizes: Se
 
 
 # ---- language-model operators (no plan; torch tensors on the current device) ---------------------
-_DTYPES = None
-
-
 def _dtype_code(t) -> int:
     """rsdgc_dtype of a tensor; raises for a type the operators do not take."""
-    global _DTYPES
-    if _DTYPES is None:
-        import torch
-
-        _DTYPES = {torch.float32: RSDGC_F32, torch.bfloat16: RSDGC_BF16, torch.float16: RSDGC_F16}
-    code = _DTYPES.get(t.dtype)
+    code = (_torch or _tt()).codes.get(t.dtype)
     if code is None:
         raise ValueError("type %s is not taken: float32, bfloat16 or float16" % t.dtype)
     return code
 
 
-def _on_device(*tensors) -> None:
-    """The library sees plain pointers: every tensor given has to be on the current device."""
-    import torch
-
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
+def _on_device(*tensors) -> int:
+    """The stream to work on.  The library sees plain pointers: every tensor given has to be on the current device."""
+    t = _torch or _tt()
+    dev = t.device()
+    for x in tensors:
+        if x is not None and x.get_device() != dev:
             raise ValueError("a tensor is not on the current CUDA device (%d)" % dev)
+    return t.stream(dev)
 
 
 def _rows(t, n: int, d: int, what: str) -> int:
     """Row stride of an n x d matrix whose rows are contiguous."""
     if t.dim() != 2 or t.size(0) != n or t.size(1) != d:
         raise ValueError("%s: a %d x %d matrix is wanted, got %s" % (what, n, d, tuple(t.shape)))
-    if d > 1 and t.stride(1) != 1:
+    row, col = t.stride()
+    if col != 1 and d > 1:
         raise ValueError("%s: rows have to be contiguous" % what)
-    return t.stride(0) if n > 1 else d
+    return row if n > 1 else d
 
 
-def _vector(t, n: int, dtype, what: str) -> None:
-    """None, or n contiguous values (of `dtype`, where one is given)."""
+def _vector(t, n: int, dtype, what: str) -> Optional[int]:
+    """Address of n contiguous values (of `dtype`, where one is given), or None."""
     if t is None:
-        return
+        return None
     if t.dim() != 1 or t.size(0) != n or (n > 1 and t.stride(0) != 1):
         raise ValueError("%s: %d contiguous values are wanted, got %s" % (what, n, tuple(t.shape)))
     if dtype is not None and t.dtype != dtype:
         raise ValueError("%s: %s is wanted, got %s" % (what, dtype, t.dtype))
+    return t.data_ptr()
+
+
+def _holds(workspace, size: int) -> int:
+    if workspace is None or workspace.nbytes < size:
+        raise ValueError("workspace: %d bytes are wanted" % size)
+    return workspace.data_ptr()
 
 
 def layer_norm_workspace_bytes(n_rows: int, width: int) -> int:
@@ -399,53 +421,41 @@ def _size(n: int, what: str) -> int:
 def layer_norm_forward(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5) -> None:
     """``y`` = layer norm of the rows of ``x`` (float32, bfloat16 or float16), times ``weight`` plus ``bias``
     (each may be None; ``x``'s type or float32).  ``mean``, ``rstd``: float32, one per row, for the backward pass."""
-    import torch
-
     n, d = x.shape
-    _on_device(x, weight, bias, y, mean, rstd)
+    stream = _on_device(x, weight, bias, y, mean, rstd)
     xs, ys = _rows(x, n, d, "x"), _rows(y, n, d, "y")
     if y.dtype != x.dtype:
         raise ValueError("y: %s is wanted, got %s" % (x.dtype, y.dtype))
-    params = weight if weight is not None else bias
-    ptype = x.dtype if params is None else params.dtype
-    _vector(weight, d, ptype, "weight")
-    _vector(bias, d, ptype, "bias")
-    _vector(mean, n, torch.float32, "mean")
-    _vector(rstd, n, torch.float32, "rstd")
-    code = _dtype_code(x)
-    _check(lib().rsdgc_layer_norm_forward(_ptr(x), xs, _ptr(weight), _ptr(bias), _ptr(y), ys, _ptr(mean), _ptr(rstd),
-                                          n, d, code, code if params is None else _dtype_code(params), eps, _stream()),
-           "rsdgc_layer_norm_forward")
+    params = x if weight is None and bias is None else bias if weight is None else weight
+    f32 = _torch.f32
+    code = lib().rsdgc_layer_norm_forward(
+        x.data_ptr(), xs, _vector(weight, d, params.dtype, "weight"), _vector(bias, d, params.dtype, "bias"), y.data_ptr(),
+        ys, _vector(mean, n, f32, "mean"), _vector(rstd, n, f32, "rstd"), n, d, _dtype_code(x), _dtype_code(params), eps,
+        stream)
+    if code:
+        _check(code, "rsdgc_layer_norm_forward")
 
 
 def layer_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None, workspace=None) -> None:
     """Gradients of layer_norm_forward() for ``dy``: ``dx`` like ``x``; ``dweight``, ``dbias`` (one value per column,
     any of the three types, e.g. a layer of a gradient arena).  Each may be None.  ``workspace``:
     layer_norm_workspace_bytes() bytes, needed for ``dweight`` or ``dbias``."""
-    import torch
-
     n, d = x.shape
-    _on_device(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
+    stream = _on_device(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
     xs, gs = _rows(x, n, d, "x"), _rows(dy, n, d, "dy")
     ds = d if dx is None else _rows(dx, n, d, "dx")
-    for t, what in ((dy, "dy"), (dx, "dx")):
-        if t is not None and t.dtype != x.dtype:
-            raise ValueError("%s: %s is wanted, got %s" % (what, x.dtype, t.dtype))
-    _vector(weight, d, None, "weight")
-    _vector(mean, n, torch.float32, "mean")
-    _vector(rstd, n, torch.float32, "rstd")
-    grads = dweight if dweight is not None else dbias
-    _vector(dweight, d, None, "dweight")
-    _vector(dbias, d, None if grads is None else grads.dtype, "dbias")
-    if grads is not None and (workspace is None or
-                              workspace.numel() * workspace.element_size() < layer_norm_workspace_bytes(n, d)):
-        raise ValueError("workspace: %d bytes are wanted" % layer_norm_workspace_bytes(n, d))
-    code = _dtype_code(x)
-    _check(lib().rsdgc_layer_norm_backward(_ptr(dy), gs, _ptr(x), xs, _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dx), ds,
-                                           _ptr(dweight), _ptr(dbias),
-                                           RSDGC_F32 if grads is None else _dtype_code(grads), n, d, code,
-                                           code if weight is None else _dtype_code(weight), _ptr(workspace), _stream()),
-           "rsdgc_layer_norm_backward")
+    if dy.dtype != x.dtype or (dx is not None and dx.dtype != x.dtype):
+        raise ValueError("dy and dx: %s is wanted" % x.dtype)
+    grads = dbias if dweight is None else dweight
+    f32 = _torch.f32
+    code = lib().rsdgc_layer_norm_backward(
+        dy.data_ptr(), gs, x.data_ptr(), xs, _vector(weight, d, None, "weight"), _vector(mean, n, f32, "mean"),
+        _vector(rstd, n, f32, "rstd"), _ptr(dx), ds, _vector(dweight, d, None, "dweight"),
+        _vector(dbias, d, None if grads is None else grads.dtype, "dbias"), RSDGC_F32 if grads is None else _dtype_code(grads),
+        n, d, _dtype_code(x), _dtype_code(x if weight is None else weight),
+        None if grads is None else _holds(workspace, layer_norm_workspace_bytes(n, d)), stream)
+    if code:
+        _check(code, "rsdgc_layer_norm_backward")
 
 
 def head_workspace_bytes(n_tokens: int, vocab: int, width: int, n_targets: int = 1) -> int:
@@ -454,103 +464,109 @@ def head_workspace_bytes(n_tokens: int, vocab: int, width: int, n_targets: int =
     return _size(lib().rsdgc_head_workspace_bytes(n_tokens, vocab, width, n_targets), "rsdgc_head_workspace_bytes")
 
 
-def _head_args(hidden, weight, workspace, n_targets: int, *others):
-    """(n, v, d, hidden stride, weight stride, type) of a vocabulary head, after the checks all its calls share."""
-    if hidden.dim() != 2 or weight.dim() != 2:
-        raise ValueError("hidden and weight have to be matrices")
+def _head_args(hidden, weight, workspace, n_targets: int):
+    """(n, v, d, hidden stride, weight stride, type, workspace's address) of a vocabulary head, after the checks that all
+    its calls share."""
     n, d = hidden.shape
     v = weight.size(0)
-    _on_device(hidden, weight, workspace, *others)
     if weight.dtype != hidden.dtype:
         raise ValueError("weight: %s is wanted, got %s" % (hidden.dtype, weight.dtype))
     hs, ws = _rows(hidden, n, d, "hidden"), _rows(weight, v, d, "weight")
     # the stride of a single row is free
     hs, ws = hs if n > 1 else (d + 7) // 8 * 8, ws if v > 1 else (d + 7) // 8 * 8
-    size = head_workspace_bytes(n, v, d, n_targets)
-    if workspace.numel() * workspace.element_size() < size:
-        raise ValueError("workspace: %d bytes are wanted" % size)
-    return n, v, d, hs, ws, _dtype_code(hidden)
+    return n, v, d, hs, ws, _dtype_code(hidden), _holds(workspace, head_workspace_bytes(n, v, d, n_targets))
 
 
-def _head_grad_args(hidden, weight, lse, grad_loss, dhidden, dweight):
-    import torch
-
-    n, d = hidden.shape
-    _vector(lse, n, torch.float32, "lse")
-    _vector(grad_loss, n, torch.float32, "grad_loss")
+def _head_grads(hidden, weight, dhidden, dweight):
+    """(dhidden's stride, dweight's stride, dweight's type)"""
     if dhidden.dtype != hidden.dtype:
         raise ValueError("dhidden: %s is wanted, got %s" % (hidden.dtype, dhidden.dtype))
-    return _rows(dhidden, n, d, "dhidden"), _rows(dweight, weight.size(0), d, "dweight"), _dtype_code(dweight)
+    d = hidden.size(1)
+    return _rows(dhidden, hidden.size(0), d, "dhidden"), _rows(dweight, weight.size(0), d, "dweight"), _dtype_code(dweight)
 
 
-def _labels(labels, n: int) -> None:
-    import torch
-
-    if labels is None:
-        raise ValueError("labels are wanted")
-    _vector(labels, n, torch.int64, "labels")
+def _matrix(t, what: str) -> None:
+    if t.dim() != 2:
+        raise ValueError("%s: a matrix is wanted" % what)
 
 
 def head_loss_forward(hidden, weight, labels, loss, lse, workspace) -> None:
     """``loss`` = cross entropy of the logits ``hidden`` @ ``weight``.T with ``labels`` (int64; negative: no loss), ``lse``
     = their log-sum-exp (None where no backward pass follows), both float32, without storing the logits.  bfloat16 or
     float16, rows 16-byte aligned."""
-    import torch
-
-    n, v, d, hs, ws, code = _head_args(hidden, weight, workspace, 1, labels, loss, lse)
-    _labels(labels, n)
-    _vector(loss, n, torch.float32, "loss")
-    _vector(lse, n, torch.float32, "lse")
-    _check(lib().rsdgc_head_loss_forward(_ptr(hidden), hs, _ptr(weight), ws, _ptr(labels), _ptr(loss), _ptr(lse), n, v, d,
-                                         code, _ptr(workspace), _stream()), "rsdgc_head_loss_forward")
+    _matrix(hidden, "hidden")
+    stream = _on_device(hidden, weight, workspace, labels, loss, lse)
+    n, v, d, hs, ws, code, space = _head_args(hidden, weight, workspace, 1)
+    f32 = _torch.f32
+    if labels is None:
+        raise ValueError("labels are wanted")
+    code = lib().rsdgc_head_loss_forward(hidden.data_ptr(), hs, weight.data_ptr(), ws,
+                                         _vector(labels, n, _torch.i64, "labels"), _vector(loss, n, f32, "loss"),
+                                         _vector(lse, n, f32, "lse"), n, v, d, code, space, stream)
+    if code:
+        _check(code, "rsdgc_head_loss_forward")
 
 
 def head_loss_backward(hidden, weight, labels, lse, grad_loss, dhidden, dweight, workspace) -> None:
     """Gradients of head_loss_forward() for ``grad_loss`` (float32, one per token): ``dhidden`` like ``hidden``, ``dweight``
     vocab x width in ``weight``'s type or float32, e.g. a layer of a gradient arena."""
-    n, v, d, hs, ws, code = _head_args(hidden, weight, workspace, 1, labels, lse, grad_loss, dhidden, dweight)
-    _labels(labels, n)
-    dhs, dws, dwt = _head_grad_args(hidden, weight, lse, grad_loss, dhidden, dweight)
-    _check(lib().rsdgc_head_loss_backward(_ptr(hidden), hs, _ptr(weight), ws, _ptr(labels), _ptr(lse), _ptr(grad_loss),
-                                          _ptr(dhidden), dhs, _ptr(dweight), dws, dwt, n, v, d, code, _ptr(workspace),
-                                          _stream()), "rsdgc_head_loss_backward")
+    _matrix(hidden, "hidden")
+    stream = _on_device(hidden, weight, workspace, labels, lse, grad_loss, dhidden, dweight)
+    n, v, d, hs, ws, code, space = _head_args(hidden, weight, workspace, 1)
+    dhs, dws, dwt = _head_grads(hidden, weight, dhidden, dweight)
+    f32 = _torch.f32
+    if labels is None:
+        raise ValueError("labels are wanted")
+    code = lib().rsdgc_head_loss_backward(hidden.data_ptr(), hs, weight.data_ptr(), ws,
+                                          _vector(labels, n, _torch.i64, "labels"), _vector(lse, n, f32, "lse"),
+                                          _vector(grad_loss, n, f32, "grad_loss"), dhidden.data_ptr(), dhs,
+                                          dweight.data_ptr(), dws, dwt, n, v, d, code, space, stream)
+    if code:
+        _check(code, "rsdgc_head_loss_backward")
 
 
 def _top_args(top_index, top_logit, n: int):
-    import torch
-
-    if top_index.dim() != 2 or top_index.dtype != torch.int64:
-        raise ValueError("top_index: an int64 matrix is wanted")
+    """(entries per token, strides of the two, type of the logits)"""
+    _matrix(top_index, "top_index")
+    if top_index.dtype != _tt().i64:
+        raise ValueError("top_index: int64 is wanted, got %s" % top_index.dtype)
     k = top_index.size(1)
-    i, l = _rows(top_index, n, k, "top_index"), _rows(top_logit, n, k, "top_logit")
-    return k, i, l, _dtype_code(top_logit)
+    return k, _rows(top_index, n, k, "top_index"), _rows(top_logit, n, k, "top_logit"), _dtype_code(top_logit)
 
 
 def head_distill_forward(hidden, weight, top_index, top_logit, temperature: float, loss, lse, workspace) -> None:
     """``loss`` = T^2 KL(teacher || student) per token, the teacher being the softmax of its top logits ``top_logit`` at
     the vocabulary entries ``top_index`` (int64, negative: entry left out) and the student that of ``hidden`` @
     ``weight``.T, both at temperature T; ``lse`` = log-sum-exp of the student's logits / T."""
-    import torch
-
+    _matrix(hidden, "hidden")
+    stream = _on_device(hidden, weight, workspace, top_index, top_logit, loss, lse)
     k, istride, lstride, tcode = _top_args(top_index, top_logit, hidden.size(0))
-    n, v, d, hs, ws, code = _head_args(hidden, weight, workspace, k, top_index, top_logit, loss, lse)
-    _vector(loss, n, torch.float32, "loss")
-    _vector(lse, n, torch.float32, "lse")
-    _check(lib().rsdgc_head_distill_forward(_ptr(hidden), hs, _ptr(weight), ws, _ptr(top_index), istride, _ptr(top_logit),
-                                            lstride, tcode, k, temperature, _ptr(loss), _ptr(lse), n, v, d, code,
-                                            _ptr(workspace), _stream()), "rsdgc_head_distill_forward")
+    n, v, d, hs, ws, code, space = _head_args(hidden, weight, workspace, k)
+    f32 = _torch.f32
+    code = lib().rsdgc_head_distill_forward(hidden.data_ptr(), hs, weight.data_ptr(), ws, top_index.data_ptr(), istride,
+                                            top_logit.data_ptr(), lstride, tcode, k, temperature,
+                                            _vector(loss, n, f32, "loss"), _vector(lse, n, f32, "lse"), n, v, d, code, space,
+                                            stream)
+    if code:
+        _check(code, "rsdgc_head_distill_forward")
 
 
 def head_distill_backward(hidden, weight, top_index, top_logit, temperature: float, lse, grad_loss, dhidden, dweight,
                           workspace) -> None:
     """Gradients of head_distill_forward(), as head_loss_backward() gives them."""
+    _matrix(hidden, "hidden")
+    stream = _on_device(hidden, weight, workspace, top_index, top_logit, lse, grad_loss, dhidden, dweight)
     k, istride, lstride, tcode = _top_args(top_index, top_logit, hidden.size(0))
-    n, v, d, hs, ws, code = _head_args(hidden, weight, workspace, k, top_index, top_logit, lse, grad_loss, dhidden, dweight)
-    dhs, dws, dwt = _head_grad_args(hidden, weight, lse, grad_loss, dhidden, dweight)
-    _check(lib().rsdgc_head_distill_backward(_ptr(hidden), hs, _ptr(weight), ws, _ptr(top_index), istride, _ptr(top_logit),
-                                             lstride, tcode, k, temperature, _ptr(lse), _ptr(grad_loss), _ptr(dhidden), dhs,
-                                             _ptr(dweight), dws, dwt, n, v, d, code, _ptr(workspace), _stream()),
-           "rsdgc_head_distill_backward")
+    n, v, d, hs, ws, code, space = _head_args(hidden, weight, workspace, k)
+    dhs, dws, dwt = _head_grads(hidden, weight, dhidden, dweight)
+    f32 = _torch.f32
+    code = lib().rsdgc_head_distill_backward(hidden.data_ptr(), hs, weight.data_ptr(), ws, top_index.data_ptr(), istride,
+                                             top_logit.data_ptr(), lstride, tcode, k, temperature,
+                                             _vector(lse, n, f32, "lse"), _vector(grad_loss, n, f32, "grad_loss"),
+                                             dhidden.data_ptr(), dhs, dweight.data_ptr(), dws, dwt, n, v, d, code, space,
+                                             stream)
+    if code:
+        _check(code, "rsdgc_head_distill_backward")
 
 
 def operator_status() -> int:
