@@ -207,22 +207,13 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32])
         : "r"(addr));
 }
 // The loaded registers pass through the wait, so that nothing reads them before it.
-__device__ __forceinline__ void tie32(uint32_t (&r)[32])
+__device__ __forceinline__ void tmem_wait_load(uint32_t (&r)[32])
 {
-    asm volatile(""
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
                    "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
                    "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
                    "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
-}
-// 128 columns of the warp's 32 rows
-__device__ __forceinline__ void tmem_load128(uint32_t addr, uint32_t (&r)[4][32])
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) tmem_load32(addr + 32 * i, r[i]);
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 4; ++i) tie32(r[i]);
 }
 // Two binary32 operations per instruction.
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
@@ -470,21 +461,20 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const int stages = p.stages, stage_bytes = kRingBlocks / stages * kBlockBytes;
 
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < kMaxStages; ++i) {
-            barrier_init(smem_addr(&full[i]), 1);
-            barrier_init(smem_addr(&empty[i]), 1);
+    if (warp == 0) {  // a lane per barrier
+        if (lane < kMaxStages) {
+            barrier_init(smem_addr(&full[lane]), 1);
+            barrier_init(smem_addr(&empty[lane]), 1);
+        } else if (lane < kMaxStages + 2) {
+            barrier_init(smem_addr(&acc_full[lane - kMaxStages]), 1);
+            barrier_init(smem_addr(&acc_empty[lane - kMaxStages]), 2 * kEpilogueWarps);
+        } else if (lane < kMaxStages + 2 + kSlots) {
+            barrier_init(smem_addr(&slot_full[lane - kMaxStages - 2]), 1);
+            barrier_init(smem_addr(&slot_empty[lane - kMaxStages - 2]), 2 * (1 + kEpilogueWarps));
+        } else if (lane == 31) {
+            barrier_init(smem_addr(&drain), 1);
+            dead = 0;
         }
-        for (int i = 0; i < 2; ++i) {
-            barrier_init(smem_addr(&acc_full[i]), 1);
-            barrier_init(smem_addr(&acc_empty[i]), 2 * kEpilogueWarps);
-        }
-        for (int i = 0; i < kSlots; ++i) {
-            barrier_init(smem_addr(&slot_full[i]), 1);
-            barrier_init(smem_addr(&slot_empty[i]), 2 * (1 + kEpilogueWarps));
-        }
-        barrier_init(smem_addr(&drain), 1);
-        dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 3 && lane < 3 * p.n_jobs) {
@@ -501,11 +491,11 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
     __syncthreads();
     cluster_sync_all();  // the peer's barriers exist before anything arrives on them
     tmem_fence_after();
-    grid_dependency_wait();
-    grid_dependency_launch_next();
-    if (BACK && blockIdx.x == 0)
-        for (int i = threadIdx.x; i < p.n_clear; i += kHeadThreads) p.clear[i] = 0;
-    asm volatile("fence.proxy.async.global;" ::: "memory");  // dz was written by ordinary stores, TMA reads it
+    // what earlier kernels of the stream wrote may be touched from here on (each role calls it when it is set up)
+    auto start = [&]() {
+        grid_dependency_wait();
+        grid_dependency_launch_next();
+    };
 
     // Bounded: a wait that gives up marks the CTA dead, raises the status bit, and every role leaves its loop.
     auto give_up = [&]() -> bool {
@@ -531,17 +521,18 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
         return -1;
     };
 
-    // registers: 168 per thread at launch, 384 * 168 = 128 * 72 + 256 * 216
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == 0 && lane == 0) {  // ---- producer, in both CTAs; all bytes count on the first CTA's barriers
             int stage = 0, it = 0;
             uint32_t parity = 0;
             bool ok = true;
+            TilePos tp = tile_pos(p, pair);
+            start();
+            asm volatile("fence.proxy.async.global;" ::: "memory");  // TMA reads what ordinary stores wrote
             for (int t = pair, i = 0; t < p.tiles; ++i) {
                 // the tile after this one: asked for here, announced behind this one's loads
                 const int after = rank != 0 ? 0 : p.next_tile ? pairs + atomicAdd(p.next_tile, 1) : t + pairs;
-                const TilePos tp = tile_pos(p, t);
+                if (i) tp = tile_pos(p, t);
                 const HeadJob &j = p.job[tp.job];
                 const int halves = j.halves;
                 const int ra = tp.m * kTile + (int)rank * kHalf, rb = tp.n * halves * kTile + (int)rank * kHalf;
@@ -683,14 +674,17 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
             }
         }
     } else {  // ---- epilogue: a thread owns one row and half of an accumulator's columns
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int quad = warp & 3, half = (warp - 4) >> 2;
         const float c2 = p.c2;
         const RowsOut<T> out = {ring + kRingBlocks * kBlockBytes + (warp - 4) * kStagingBytes, lane};
         int sub = 0;
         bool ok = true;
+        TilePos tp = tile_pos(p, pair);
+        start();
+        if (BACK && blockIdx.x == 0)
+            for (int i = threadIdx.x - 128; i < p.n_clear; i += 32 * kEpilogueWarps) p.clear[i] = 0;
         for (int t = pair, i = 0; t < p.tiles; ++i) {
-            const TilePos tp = tile_pos(p, t);
+            if (i) tp = tile_pos(p, t);
             const HeadJob &j = p.job[tp.job];
             const int row0 = tp.m * kTile + (int)rank * kHalf + quad * 32, row = row0 + lane;
             const bool live = row < p.n, logits = !BACK || j.kind == kLogitGrad;
@@ -720,78 +714,66 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 ok = __all_sync(0xFFFFFFFFu, wait(smem_addr(&acc_full[acc]), (uint32_t)((sub >> 1) & 1)));
                 if (!ok) break;
                 tmem_fence_after();
-                // The accumulator goes to registers at once and is free for the tile after the next: what follows
-                // does not hold up the MMAs.
-                uint32_t raw[4][32];
-                tmem_load128(src, raw);
-                tmem_fence_before();
-                __syncwarp();
-                if (lane == 0) barrier_arrive_leader(smem_addr(&acc_empty[acc]));
-                const bool ragged = logits && col0 + kHalf > j.vocab;
-                if constexpr (!BACK) {
-#pragma unroll
-                    for (int ch = 0; ch < 4; ++ch) {
-                        const int col = col0 + 32 * ch;
+                [[maybe_unused]] float m = -INFINITY, s = 0.0f;
+                // A loop of 32 columns that stays rolled: unrolled over the 128 columns the code outgrows the
+                // instruction cache and fetching it takes longer (5000 cycles per accumulator) than running it.
+#pragma unroll 1
+                for (int ch = 0; ch < kHalf / 32; ++ch) {
+                    const int col = col0 + 32 * ch;
+                    uint32_t raw[32];
+                    tmem_load32(src + 32 * ch, raw);
+                    tmem_wait_load(raw);
+                    if (ch + 1 == kHalf / 32) {  // the accumulator is read: the tile after the next may overwrite it
+                        tmem_fence_before();
+                        __syncwarp();
+                        if (lane == 0) barrier_arrive_leader(smem_addr(&acc_empty[acc]));
+                    }
+                    if constexpr (!BACK) {
                         if (p.k) {
                             while (tg.next < col + 32) {
-                                p.target_z[(long long)row * p.k + tg.j] = pick32(raw[ch], tg.next - col);
+                                p.target_z[(long long)row * p.k + tg.j] = pick32(raw, tg.next - col);
                                 tg.advance();
                             }
                         } else if (label >= col && label < col + 32) {
-                            p.target_z[row] = pick32(raw[ch], label - col);
+                            p.target_z[row] = pick32(raw, label - col);
                         }
-                        if (ragged) {
+                        if (col + 32 > j.vocab) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
-                                if (col + i >= j.vocab) raw[ch][i] = 0xFF800000u;  // -inf
+                                if (col + i >= j.vocab) raw[i] = 0xFF800000u;  // -inf
                         }
-                    }
-                    // independent chains, so that their latencies overlap
-                    float top[4];
+                        // two and four chains, so that their latencies overlap
+                        float top[2] = {__uint_as_float(raw[0]), __uint_as_float(raw[1])};
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        top[c] = __uint_as_float(raw[c][0]);
-#pragma unroll
-                        for (int i = 1; i < 31; i += 2)
-                            top[c] = max3(top[c], __uint_as_float(raw[c][i]), __uint_as_float(raw[c][i + 1]));
-                        top[c] = fmaxf(top[c], __uint_as_float(raw[c][31]));
-                    }
-                    const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c2;
-                    const float ref = m == -INFINITY ? 0.0f : m;
-                    const float2 cc = make_float2(c2, c2), rr = make_float2(-ref, -ref);
-                    float2 add[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) add[c] = make_float2(0.0f, 0.0f);
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const float2 x =
-                                fma2(make_float2(__uint_as_float(raw[c][i]), __uint_as_float(raw[c][i + 1])), cc, rr);
-                            add[c] = add2(add[c], make_float2(exp2_approx(x.x), exp2_approx(x.y)));
+                        for (int i = 2; i < 30; i += 4) {
+                            top[0] = max3(top[0], __uint_as_float(raw[i]), __uint_as_float(raw[i + 1]));
+                            top[1] = max3(top[1], __uint_as_float(raw[i + 2]), __uint_as_float(raw[i + 3]));
                         }
-                    const float2 sum = add2(add2(add[0], add[1]), add2(add[2], add[3]));
-                    const int part = col0 / kHalf;
-                    if (live && part < p.parts) p.partial[(long long)part * p.n + row] = make_float2(m, sum.x + sum.y);
-                } else {
-                    const float2 cc = make_float2(c2, c2), ll = make_float2(-l2, -l2);
-                    const float2 factor = logits ? make_float2(gs, gs) : make_float2(back, back);
-#pragma unroll
-                    for (int ch = 0; ch < 4; ++ch) {
-                        const int col = col0 + 32 * ch;
-                        float z[32];
+                        top[0] = max3(top[0], __uint_as_float(raw[30]), __uint_as_float(raw[31]));
+                        const float now = max3(m, top[0] * c2, top[1] * c2);
+                        const float ref = now == -INFINITY ? 0.0f : now;
+                        const float2 cc = make_float2(c2, c2), rr = make_float2(-ref, -ref);
+                        float2 add[4];
 #pragma unroll
                         for (int i = 0; i < 32; i += 2) {
-                            float2 x = make_float2(__uint_as_float(raw[ch][i]), __uint_as_float(raw[ch][i + 1]));
-                            if (logits) {
-                                x = fma2(x, cc, ll);
-                                x = make_float2(exp2_approx(x.x), exp2_approx(x.y));
-                            }
-                            x = mul2(x, factor);
-                            z[i] = x.x;
-                            z[i + 1] = x.y;
+                            const float2 x = fma2(make_float2(__uint_as_float(raw[i]), __uint_as_float(raw[i + 1])), cc, rr);
+                            const float2 y = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+                            add[(i >> 1) & 3] = i < 8 ? y : add2(add[(i >> 1) & 3], y);
                         }
+                        const float2 sum = add2(add2(add[0], add[1]), add2(add[2], add[3]));
+                        s = fmaf(s, exp2_approx(m - ref), sum.x + sum.y);
+                        m = now;
+                    } else {
+                        float z[32];
                         if (logits) {
+                            const float2 cc = make_float2(c2, c2), ll = make_float2(-l2, -l2), gg = make_float2(gs, gs);
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                const float2 x = fma2(make_float2(__uint_as_float(raw[i]), __uint_as_float(raw[i + 1])), cc, ll);
+                                const float2 y = mul2(make_float2(exp2_approx(x.x), exp2_approx(x.y)), gg);
+                                z[i] = y.x;
+                                z[i + 1] = y.y;
+                            }
                             if (p.k) {
                                 while (tg.next < v0 + col + 32) {
                                     subtract32(z, tg.next - v0 - col, gs * p.target_q[(long long)row * p.k + tg.j]);
@@ -800,23 +782,28 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                             } else if (label >= col && label < col + 32) {
                                 subtract32(z, label - col, gs);
                             }
-                            if (ragged || gs == 0.0f) {
+                            if (col + 32 > j.vocab || gs == 0.0f) {
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
                                     if (col + i >= j.vocab || gs == 0.0f) z[i] = 0.0f;
                             }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(raw[i]) * back;
                         }
                         // dz leaves in 16 bits, as both products' operand: their sums run over it in binary32
-                        if (j.out_mode == kOut16) {
-                            if (!(ch & 1)) out.wait_free();
-                            out.put16(ch & 1, z);
-                            if (ch & 1) out.flush(j, row0, col - 32, tp.split);
-                        } else {
-                            out.wait_free();
+                        const bool wide = j.out_mode != kOut16;
+                        if (wide || !(ch & 1)) out.wait_free();
+                        if (wide)
                             out.put32(z);
-                            out.flush(j, row0, col, tp.split);
-                        }
+                        else
+                            out.put16(ch & 1, z);
+                        if (wide || (ch & 1)) out.flush(j, row0, wide ? col : col - 32, tp.split);
                     }
+                }
+                if constexpr (!BACK) {
+                    const int part = col0 / kHalf;
+                    if (live && part < p.parts) p.partial[(long long)part * p.n + row] = make_float2(m, s);
                 }
             }
             if (!ok) break;
@@ -1213,10 +1200,6 @@ int head_pairs(cudaError_t *e)
     if (m) return m;
     *e = cudaFuncSetAttribute(k_head<BACK, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem);
     if (*e != cudaSuccess) return 0;
-    cudaFuncAttributes attr{};
-    *e = cudaFuncGetAttributes(&attr, k_head<BACK, T>);
-    if (*e == cudaSuccess && attr.numRegs != 168) *e = cudaErrorLaunchOutOfResources;  // the kernel's register split relies on it
-    if (*e != cudaSuccess) return 0;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = (unsigned)current_device_sms();
     cfg.blockDim = kHeadThreads;
@@ -1256,10 +1239,14 @@ cudaError_t launch_tiles(HeadParams &p, int *counter, cudaStream_t s)
 
 constexpr double kTruncationBf16 = 0.26, kTruncationF16 = 0.29;
 constexpr int kBand = 16;
-// Two accumulators per tile (256 x 512) wherever there are columns for them: every operand block brought in serves
+// Two accumulators per tile (256 x 512) unless all 256 x 256 tiles run at a time: every operand block brought in serves
 // more products, 48 instead of 64 bytes per cycle and SM at the full MMA rate, and the ring holds twice the work.
-// (Forward 2048 x 32000 x 2048: 219 us against 286; 333 x 10007 x 776: 20 against 24; 64 x 32000 x 4096: 64 against 82.)
-constexpr int kTwoHalvesFrom = kTile + 1;  // columns
+// (Forward 2048 x 32000 x 2048: 219 us against 286; 333 x 10007 x 776, 80 tiles: 20 against 24; 64 x 32000 x 4096: 64
+// against 82.  One accumulator for 64 x 8000 x 512, 32 tiles: see the head's notes on short launches.)
+bool two_accumulators(int64_t m, int64_t n)
+{
+    return n > kTile && (int64_t)tiles_of(m) * tiles_of(n) > current_device_sms() / 2;
+}
 
 cudaError_t set_job(HeadJob &j, int kind, int dtype, const void *a, bool a_mn, long long ar, long long ac, long long as,
                     const void *b, bool b_mn, long long br, long long bc, long long bs, long long m, long long n, long long k)
@@ -1270,7 +1257,7 @@ cudaError_t set_job(HeadJob &j, int kind, int dtype, const void *a, bool a_mn, l
     j.b_mn = b_mn;
     j.k_steps = (int)((k + kStepK - 1) / kStepK);
     j.m_tiles = tiles_of(m);
-    j.halves = n >= kTwoHalvesFrom ? 2 : 1;
+    j.halves = two_accumulators(m, n) ? 2 : 1;
     j.n_tiles = (tiles_of(n) + j.halves - 1) / j.halves;
     j.band = j.m_tiles < kBand ? j.m_tiles : kBand;
     j.splits = 1;
