@@ -93,7 +93,6 @@ struct HeadParams {
 };
 
 // ---- PTX ----------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ uint32_t cluster_rank()
 {
     uint32_t r;
@@ -110,22 +109,6 @@ __device__ __forceinline__ uint32_t leader_addr(uint32_t a) { return addr_in(a, 
 __device__ __forceinline__ void cluster_sync_all()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
 }
 __device__ __forceinline__ bool barrier_test(uint32_t bar, uint32_t parity)  // without waiting
 {
@@ -150,10 +133,6 @@ __device__ __forceinline__ bool barrier_try_cluster(uint32_t bar, uint32_t parit
         : "r"(bar), "r"(parity)
         : "memory");
     return ok != 0;
-}
-__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void barrier_arrive_in(uint32_t bar, uint32_t rank)
 {
