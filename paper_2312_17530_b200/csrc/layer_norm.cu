@@ -13,9 +13,9 @@
 
 namespace rsdgc {
 
-constexpr int kNormVecs = 4;          // 16-byte vectors of a row that a thread holds
-constexpr int kNormVecsWarp = 16;     // ... where rows are many and a warp takes one
-constexpr int kNormScalars = 16;      // elements it holds where rows are not 16-byte aligned
+constexpr int kNormVecs = 2;          // 16-byte packs of a row that a lane holds where a warp takes the row
+constexpr int kNormScalars = 16;      // elements a thread holds where rows are not 16-byte aligned
+constexpr int kNormRingThreads = 512;
 constexpr int kNormMaxThreads = 1024;
 constexpr int kNormBackThreads = 512; // backward: 128 registers for the columns' sums and the rows' operands
 constexpr int kBackWarps = 8;         // warps of a CTA whose rows take one warp each, backward
@@ -44,6 +44,70 @@ __device__ __forceinline__ void load_param(const P *p, long long i, float *out)
     for (int j = 0; j < VEC; ++j) out[j] = to_f32(k.v[j]);
 }
 
+// A 16-byte pack as pairs of binary32 values: the arithmetic runs two values per instruction (f32x2), which matters
+// because rows of 16-bit values are bound by the issue rate, not by memory, at one instruction per value and step.
+template <typename T>
+struct Pairs {
+    static constexpr int N = 8 / (int)sizeof(T);  // pairs of a pack
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const T *p)
+    {
+        const uint4 v = *reinterpret_cast<const uint4 *>(p);
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    }
+    __device__ __forceinline__ void store(T *p) const { *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]); }
+    __device__ __forceinline__ float2 get(int i) const;
+    __device__ __forceinline__ void set(int i, float2 v);
+};
+template <>
+__device__ __forceinline__ float2 Pairs<float>::get(int i) const
+{
+    return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+}
+template <>
+__device__ __forceinline__ void Pairs<float>::set(int i, float2 v)
+{
+    w[2 * i] = __float_as_uint(v.x);
+    w[2 * i + 1] = __float_as_uint(v.y);
+}
+template <>
+__device__ __forceinline__ float2 Pairs<__nv_bfloat16>::get(int i) const
+{
+    return make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+}
+template <>
+__device__ __forceinline__ void Pairs<__nv_bfloat16>::set(int i, float2 v)
+{
+    w[i] = pack2<__nv_bfloat16>(v.x, v.y);
+}
+template <>
+__device__ __forceinline__ float2 Pairs<__half>::get(int i) const
+{
+    return __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+}
+template <>
+__device__ __forceinline__ void Pairs<__half>::set(int i, float2 v)
+{
+    w[i] = pack2<__half>(v.x, v.y);
+}
+// `count` pairs of a parameter vector, or a constant where there is none
+template <typename P, int PAIRS>
+__device__ __forceinline__ void load_pairs(const P *p, long long c, bool there, float missing, float2 *out)
+{
+    if (p && there) {
+#pragma unroll
+        for (int k = 0; k < PAIRS / Pairs<P>::N; ++k) {
+            Pairs<P> v;
+            v.load(p + c + k * (16 / (int)sizeof(P)));
+#pragma unroll
+            for (int i = 0; i < Pairs<P>::N; ++i) out[k * Pairs<P>::N + i] = v.get(i);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) out[i] = make_float2(missing, missing);
+    }
+}
+
 // Sum over the threads of one row.  One warp per row: shuffles only.  Otherwise the whole CTA, one slot of
 // `part` per warp; the caller alternates between two buffers, so that one barrier per sum is enough.
 template <bool WARP>
@@ -69,13 +133,140 @@ __device__ __forceinline__ float2 row_sum2(float x, float y, float2 *part)
     return make_float2(warp_sum(z.x), warp_sum(z.y));
 }
 
+// A ring of stages in shared memory, each `operands` rows, filled by bulk copies that run `stages` - 1 (or more) rows
+// ahead, so that a CTA has tens of KB on their way whatever its threads wait for.
+struct RowRing {
+    uint32_t base, full;   // shared-memory addresses: rows, barriers (8 bytes each)
+    uint32_t stage_bytes;
+    int stages;
+    bool arrived;          // false once a wait has given up: the results are void, as the status says
+    unsigned int *status;
+
+    __device__ __forceinline__ uint32_t bar(int i) const { return full + 8 * (i % stages); }
+    __device__ __forceinline__ uint32_t at(int i) const { return base + (i % stages) * stage_bytes; }
+    // bounded; after a failure the others poll once
+    __device__ __forceinline__ void wait(int i)
+    {
+        unsigned left = arrived ? kNormSpin : 1u;
+        bool here = false;
+        while (left-- && !(here = barrier_try(bar(i), (uint32_t)(i / stages) & 1u))) {}
+        if (!here && arrived) {
+            arrived = false;
+            atomicOr(status, RSDGC_STATUS_TIMEOUT);
+        }
+    }
+    // copies under way after a failure land in this CTA's memory: wait for them (bounded)
+    __device__ __forceinline__ void drain(int from, int to) const
+    {
+        for (int i = from < 0 ? 0 : from; i < to; ++i)
+            for (unsigned q = 0; q < kNormSpin && !barrier_try(bar(i), (uint32_t)(i / stages) & 1u); ++q) {}
+    }
+};
+template <typename T>
+__device__ __forceinline__ const T *shared_row(uint32_t addr)
+{
+    return reinterpret_cast<const T *>(__cvta_shared_to_generic(addr));
+}
+
 // ---- forward ----------------------------------------------------------------------------------
-// WARP: a warp per row (rows of at most 32 * NV packs), kNormWarps rows per CTA; else a CTA per row.
+// Aligned rows: a CTA walks the rows blockIdx.x, blockIdx.x + gridDim.x, ...; its threads keep their columns' weight
+// and bias as binary32 pairs.  Two barriers per row (mean, then the centred squares); the next rows arrive meanwhile.
+template <typename T, typename P, int E>
+__global__ void __launch_bounds__(kNormRingThreads, E <= 16 ? 2 : 1)
+k_norm_forward_ring(const T *__restrict__ x, long long xs, const P *__restrict__ w, const P *__restrict__ b,
+                    T *__restrict__ y, long long ys, float *__restrict__ mean, float *__restrict__ rstd, int n, int d,
+                    float inv_d, float root_inv_d, float eps, int stages, unsigned int *status)
+{
+    constexpr int VEC = 16 / (int)sizeof(T), NV = E / VEC, NP = Pairs<T>::N;
+    extern __shared__ __align__(128) unsigned char rows[];
+    __shared__ float part[2][32];
+    __shared__ __align__(8) unsigned long long full[kNormMaxStages];
+    const int step = blockDim.x;
+    const uint32_t row_bytes = (uint32_t)d * sizeof(T);
+    RowRing ring = {smem_addr(rows), smem_addr(full), row_bytes, stages, true, status};
+    if (threadIdx.x < stages) barrier_init(ring.bar(threadIdx.x), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncthreads();
+    grid_dependency_wait();
+    grid_dependency_launch_next();
+    auto load = [&](int i) {
+        const long long row = blockIdx.x + (long long)i * gridDim.x;
+        if (row >= n) return;
+        barrier_expect(ring.bar(i), row_bytes);
+        bulk_copy(ring.at(i), x + row * xs, row_bytes, ring.bar(i));
+    };
+    if (threadIdx.x == 0)
+        for (int i = 0; i < stages; ++i) load(i);
+    float2 wv[NV][NP], bv[NV][NP];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (threadIdx.x + i * step) * VEC;
+        load_pairs<P, NP>(w, c, c < d, 1.0f, wv[i]);
+        load_pairs<P, NP>(b, c, c < d, 0.0f, bv[i]);
+    }
+    int it = 0;
+    for (int row = blockIdx.x; row < n; row += gridDim.x, ++it) {
+        ring.wait(it);
+        const T *src = shared_row<T>(ring.at(it));
+        Pairs<T> in[NV];
+        float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (threadIdx.x + i * step) * VEC;
+            if (c < d) {
+                in[i].load(src + c);
+#pragma unroll
+                for (int k = 0; k < NP; ++k) sum = add2(sum, in[i].get(k));
+            }
+        }
+        const float mu = row_sum<false>(sum.x + sum.y, part[0]) * inv_d;
+        if (threadIdx.x == 0) load(it + stages);  // every thread has read the stage
+        // the squares are scaled term by term: their sum may leave the range where their mean does not
+        const float2 rr = make_float2(root_inv_d, root_inv_d), m2 = make_float2(-mu, -mu);
+        float2 sq = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (threadIdx.x + i * step) * VEC;
+            if (c < d) {
+#pragma unroll
+                for (int k = 0; k < NP; ++k) {
+                    const float2 e = mul2(add2(in[i].get(k), m2), rr);
+                    sq = fma2(e, e, sq);
+                }
+            }
+        }
+        const float r = rsqrtf(row_sum<false>(sq.x + sq.y, part[1]) + eps);
+        if (threadIdx.x == 0) {
+            if (mean) mean[row] = mu;
+            if (rstd) rstd[row] = r;
+        }
+        const float2 r2 = make_float2(r, r);
+        T *dst = y + row * ys;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (threadIdx.x + i * step) * VEC;
+            if (c < d) {
+                Pairs<T> out;
+#pragma unroll
+                for (int k = 0; k < NP; ++k)
+                    out.set(k, fma2(mul2(add2(in[i].get(k), m2), r2), wv[i][k], bv[i][k]));
+                out.store(dst + c);
+            }
+        }
+    }
+    if (!ring.arrived && threadIdx.x == 0) {
+        const long long mine = (n - (long long)blockIdx.x + gridDim.x - 1) / gridDim.x;
+        ring.drain(it - 1, (int)min(mine, (long long)it + stages));
+    }
+}
+
+// Rows in registers: a warp per row (aligned rows of at most 32 * kNormVecs packs, others of at most 32 * kNormScalars
+// values), or, where rows are not aligned and longer, a CTA per row.
 template <typename T, typename P, int VEC, int NV, bool WARP>
 __global__ void __launch_bounds__(WARP ? 32 * kNormWarps : kNormMaxThreads)
 k_norm_forward(const T *__restrict__ x, long long xs, const P *__restrict__ w, const P *__restrict__ b,
                T *__restrict__ y, long long ys, float *__restrict__ mean, float *__restrict__ rstd, long long n,
-               int d, float inv_d, float eps)
+               int d, float inv_d, float root_inv_d, float eps)
 {
     __shared__ float part[2][32];
     const int tid = WARP ? (threadIdx.x & 31) : threadIdx.x;
@@ -108,8 +299,8 @@ k_norm_forward(const T *__restrict__ x, long long xs, const P *__restrict__ w, c
         if (c < d) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const float e = to_f32(in[i].v[j]) - mu;
-                sq = fmaf(e * inv_d, e, sq);  // the mean, term by term: the sum itself may leave the range
+                const float e = (to_f32(in[i].v[j]) - mu) * root_inv_d;
+                sq = fmaf(e, e, sq);
             }
         }
     }
@@ -124,14 +315,13 @@ k_norm_forward(const T *__restrict__ x, long long xs, const P *__restrict__ w, c
         const int c = (tid + i * step) * VEC;
         if (c < d) {
             float wv[VEC], bv[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) wv[j] = 1.0f, bv[j] = 0.0f;
             if (w) load_param<P, VEC>(w, c, wv);
             if (b) load_param<P, VEC>(b, c, bv);
             Pack<T, VEC> out;
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float xhat = (to_f32(in[i].v[j]) - mu) * r;
-                out.v[j] = from_f32<T>(fmaf(xhat, w ? wv[j] : 1.0f, b ? bv[j] : 0.0f));
-            }
+            for (int j = 0; j < VEC; ++j) out.v[j] = from_f32<T>(fmaf((to_f32(in[i].v[j]) - mu) * r, wv[j], bv[j]));
             *reinterpret_cast<Pack<T, VEC> *>(yr + c) = out;
         }
     }
@@ -142,7 +332,7 @@ template <typename T, typename P>
 __global__ void __launch_bounds__(kNormMaxThreads)
 k_norm_forward_long(const T *__restrict__ x, long long xs, const P *__restrict__ w, const P *__restrict__ b,
                     T *__restrict__ y, long long ys, float *__restrict__ mean, float *__restrict__ rstd,
-                    int d, float inv_d, float eps)
+                    int d, float inv_d, float root_inv_d, float eps)
 {
     __shared__ float part[2][32];
     grid_dependency_wait();
@@ -153,8 +343,8 @@ k_norm_forward_long(const T *__restrict__ x, long long xs, const P *__restrict__
     for (int c = threadIdx.x; c < d; c += blockDim.x) sum += to_f32(xr[c]);
     const float mu = row_sum<false>(sum, part[0]) * inv_d;
     for (int c = threadIdx.x; c < d; c += blockDim.x) {
-        const float e = to_f32(xr[c]) - mu;
-        sq = fmaf(e * inv_d, e, sq);  // the mean, term by term: the sum itself may leave the range
+        const float e = (to_f32(xr[c]) - mu) * root_inv_d;
+        sq = fmaf(e, e, sq);
     }
     const float r = rsqrtf(row_sum<false>(sq, part[1]) + eps);
     if (threadIdx.x == 0) {
@@ -171,9 +361,8 @@ k_norm_forward_long(const T *__restrict__ x, long long xs, const P *__restrict__
 // bits from run to run.
 constexpr int kBackElems = 16;  // columns of a thread
 
-// Rows in shared memory: a ring of stages, each ROWS rows of x and dy, filled by bulk copies that run kStages - 1
-// stages ahead, so that a CTA has tens of KB on their way whatever its threads wait for.  One barrier per stage: it
-// ends the sums of this stage and, with it, all reads of the one before, which is refilled behind it.
+// Aligned rows: ROWS rows of x and dy per stage of the ring.  One barrier per stage: it ends the sums of this stage
+// and, with it, all reads of the one before, which is refilled behind it.
 template <typename T, int E, int ROWS, typename P>
 __global__ void __launch_bounds__(kNormBackThreads)
 k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
@@ -181,104 +370,90 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
                      T *__restrict__ dx, long long dxs, float *__restrict__ partial, int n, int d, float inv_d, int stages,
                      unsigned int *status)
 {
-    constexpr int VEC = 16 / (int)sizeof(T), NV = E / VEC;
-    constexpr bool KEEP = E <= 16;  // x and dy stay in registers between the two passes over a row
-    extern __shared__ __align__(128) unsigned char ring[];
+    constexpr int VEC = 16 / (int)sizeof(T), NV = E / VEC, NP = Pairs<T>::N;
+    constexpr bool KEEP = E <= 16;  // weight, x and dy stay in registers between the two passes over a row
+    extern __shared__ __align__(128) unsigned char rows[];
     __shared__ float2 part[2][ROWS][32];
     __shared__ __align__(8) unsigned long long full[kNormMaxStages];
     const int step = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t row_bytes = (uint32_t)d * sizeof(T), stage_bytes = ROWS * 2 * row_bytes;
+    const uint32_t row_bytes = (uint32_t)d * sizeof(T);
     const int groups = (n + ROWS - 1) / ROWS;
-    if (threadIdx.x < stages) barrier_init(smem_addr(&full[threadIdx.x]), 1);
+    RowRing ring = {smem_addr(rows), smem_addr(full), ROWS * 2 * row_bytes, stages, true, status};
+    if (threadIdx.x < stages) barrier_init(ring.bar(threadIdx.x), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
     grid_dependency_wait();
     grid_dependency_launch_next();
-
-    auto load = [&](int i) {  // stage i of this CTA, by one thread
-        const int g = blockIdx.x + i * (int)gridDim.x;
+    auto load = [&](int i) {  // by one thread
+        const long long g = blockIdx.x + (long long)i * gridDim.x;
         if (g >= groups) return;
-        const int s = i % stages, rows = min(ROWS, n - g * ROWS);
-        const uint32_t bar = smem_addr(&full[s]), dst = smem_addr(ring) + s * stage_bytes;
-        barrier_expect(bar, 2 * rows * row_bytes);
-        for (int r = 0; r < rows; ++r) {
-            bulk_copy(dst + 2 * r * row_bytes, x + (long long)(g * ROWS + r) * xs, row_bytes, bar);
-            bulk_copy(dst + (2 * r + 1) * row_bytes, dy + (long long)(g * ROWS + r) * dys, row_bytes, bar);
+        const int count = min(ROWS, n - (int)g * ROWS);
+        barrier_expect(ring.bar(i), 2 * count * row_bytes);
+        for (int r = 0; r < count; ++r) {
+            bulk_copy(ring.at(i) + 2 * r * row_bytes, x + (g * ROWS + r) * xs, row_bytes, ring.bar(i));
+            bulk_copy(ring.at(i) + (2 * r + 1) * row_bytes, dy + (g * ROWS + r) * dys, row_bytes, ring.bar(i));
         }
     };
     if (threadIdx.x == 0)
         for (int i = 0; i + 1 < stages; ++i) load(i);
 
-    float dw[NV][VEC] = {}, db[NV][VEC] = {}, wv[KEEP ? NV : 1][VEC];
-    if constexpr (KEEP) {
+    float2 dw[NV][NP], db[NV][NP], wv[KEEP ? NV : 1][NP];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (threadIdx.x + i * step) * VEC;
+    for (int i = 0; i < NV; ++i) {
+        const int c = (threadIdx.x + i * step) * VEC;
+        if constexpr (KEEP) load_pairs<P, NP>(w, c, c < d, 1.0f, wv[i]);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) wv[i][j] = 1.0f;
-            if (w && c < d) load_param<P, VEC>(w, c, wv[i]);
-        }
+        for (int k = 0; k < NP; ++k) dw[i][k] = db[i][k] = make_float2(0.0f, 0.0f);
     }
     float nmu[ROWS], nr[ROWS];  // the next stage's statistics
-    auto statistics = [&](int g) {
+    auto statistics = [&](long long g) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            const int row = g * ROWS + r;
+            const long long row = g * ROWS + r;
             nmu[r] = row < n ? mean[row] : 0.0f;
             nr[r] = row < n ? rstd[row] : 0.0f;
         }
     };
     statistics(blockIdx.x);
-    bool arrived = true;
     int it = 0;
     for (int g = blockIdx.x; g < groups; g += gridDim.x, ++it) {
-        const int s = it % stages, turn = it & 1;
-        const unsigned char *stage = ring + s * stage_bytes;
-        float mu[ROWS], rs[ROWS], s1[ROWS], s2[ROWS];
+        const int turn = it & 1;
+        float mu[ROWS], rs[ROWS];
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) mu[r] = nmu[r], rs[r] = nr[r], s1[r] = s2[r] = 0.0f;
-        statistics(g + gridDim.x);
-        // bounded; once a wait has given up the results are void (the status says so) and the others poll once
-        unsigned left = arrived ? kNormSpin : 1u;
-        bool here = false;
-        while (left-- && !(here = barrier_try(smem_addr(&full[s]), (uint32_t)(it / stages) & 1u))) {}
-        if (!here && arrived) {
-            arrived = false;
-            atomicOr(status, RSDGC_STATUS_TIMEOUT);
-        }
-        Pack<T, VEC> px[KEEP ? ROWS : 1][KEEP ? NV : 1], pg[KEEP ? ROWS : 1][KEEP ? NV : 1];
+        for (int r = 0; r < ROWS; ++r) mu[r] = nmu[r], rs[r] = nr[r];
+        statistics((long long)g + gridDim.x);
+        ring.wait(it);
+        Pairs<T> px[KEEP ? ROWS : 1][KEEP ? NV : 1], pg[KEEP ? ROWS : 1][KEEP ? NV : 1];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            const T *sx = reinterpret_cast<const T *>(stage + 2 * r * row_bytes);
-            const T *sg = reinterpret_cast<const T *>(stage + (2 * r + 1) * row_bytes);
+            const T *sx = shared_row<T>(ring.at(it) + 2 * r * row_bytes), *sg = shared_row<T>(ring.at(it) + (2 * r + 1) * row_bytes);
+            const float2 m2 = make_float2(-mu[r], -mu[r]), r2 = make_float2(rs[r], rs[r]);
+            float2 s1 = make_float2(0.0f, 0.0f), s2 = s1;
             if (g * ROWS + r < n) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     const int c = (threadIdx.x + i * step) * VEC;
                     if (c < d) {
-                        const Pack<T, VEC> vx = load_pack<T, VEC>(sx + c), vg = load_pack<T, VEC>(sg + c);
+                        Pairs<T> vx, vg;
+                        vx.load(sx + c);
+                        vg.load(sg + c);
                         if constexpr (KEEP) px[r][i] = vx, pg[r][i] = vg;
-                        float wl[VEC];
-                        if constexpr (!KEEP)
-                            if (w) load_param<P, VEC>(w, c, wl);
+                        float2 wl[NP];
+                        if constexpr (!KEEP) load_pairs<P, NP>(w, c, true, 1.0f, wl);
 #pragma unroll
-                        for (int j = 0; j < VEC; ++j) {
-                            const float gv = to_f32(vg.v[j]), xhat = (to_f32(vx.v[j]) - mu[r]) * rs[r];
-                            const float gw = KEEP ? gv * wv[KEEP ? i : 0][j] : w ? gv * wl[j] : gv;
-                            s1[r] += gw;
-                            s2[r] = fmaf(gw, xhat, s2[r]);
-                            dw[i][j] = fmaf(gv, xhat, dw[i][j]);
-                            db[i][j] += gv;
+                        for (int k = 0; k < NP; ++k) {
+                            const float2 gv = vg.get(k), xhat = mul2(add2(vx.get(k), m2), r2);
+                            const float2 gw = mul2(gv, KEEP ? wv[KEEP ? i : 0][k] : wl[k]);
+                            s1 = add2(s1, gw);
+                            s2 = fma2(gw, xhat, s2);
+                            dw[i][k] = fma2(gv, xhat, dw[i][k]);
+                            db[i][k] = add2(db[i][k], gv);
                         }
                     }
                 }
             }
-        }
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            s1[r] = warp_sum(s1[r]);
-            s2[r] = warp_sum(s2[r]);
-            if (lane == 0) part[turn][r][warp] = make_float2(s1[r], s2[r]);
+            const float a = warp_sum(s1.x + s1.y), b = warp_sum(s2.x + s2.y);
+            if (lane == 0) part[turn][r][warp] = make_float2(a, b);
         }
         __syncthreads();
         if (threadIdx.x == 0) load(it + stages - 1);
@@ -288,37 +463,39 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
             const int row = g * ROWS + r;
             if (row >= n) break;
             const float2 t = lane < (step >> 5) ? part[turn][r][lane] : make_float2(0.0f, 0.0f);
-            const float m1 = warp_sum(t.x) * inv_d, m2 = warp_sum(t.y) * inv_d;
-            const T *sx = reinterpret_cast<const T *>(stage + 2 * r * row_bytes);
-            const T *sg = reinterpret_cast<const T *>(stage + (2 * r + 1) * row_bytes);
+            // dx = rstd g w - rstd mean(g w) - xhat rstd mean(g w xhat)
+            const float c1 = -rs[r] * (warp_sum(t.x) * inv_d), c2 = -rs[r] * (warp_sum(t.y) * inv_d);
+            const float2 m2 = make_float2(-mu[r], -mu[r]), r2 = make_float2(rs[r], rs[r]), f1 = make_float2(c1, c1),
+                         f2 = make_float2(c2, c2);
+            const T *sx = shared_row<T>(ring.at(it) + 2 * r * row_bytes), *sg = shared_row<T>(ring.at(it) + (2 * r + 1) * row_bytes);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (threadIdx.x + i * step) * VEC;
                 if (c < d) {
-                    Pack<T, VEC> vx, vg;
-                    if constexpr (KEEP)
+                    Pairs<T> vx, vg, out;
+                    if constexpr (KEEP) {
                         vx = px[r][i], vg = pg[r][i];
-                    else
-                        vx = load_pack<T, VEC>(sx + c), vg = load_pack<T, VEC>(sg + c);
-                    float wl[VEC];
-                    if constexpr (!KEEP)
-                        if (w) load_param<P, VEC>(w, c, wl);
-                    Pack<T, VEC> out;
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        const float gv = to_f32(vg.v[j]), xhat = (to_f32(vx.v[j]) - mu[r]) * rs[r];
-                        const float gw = KEEP ? gv * wv[KEEP ? i : 0][j] : w ? gv * wl[j] : gv;
-                        out.v[j] = from_f32<T>(rs[r] * (gw - m1 - xhat * m2));
+                    } else {
+                        vx.load(sx + c);
+                        vg.load(sg + c);
                     }
-                    *reinterpret_cast<Pack<T, VEC> *>(dx + (long long)row * dxs + c) = out;
+                    float2 wl[NP];
+                    if constexpr (!KEEP) load_pairs<P, NP>(w, c, true, 1.0f, wl);
+#pragma unroll
+                    for (int k = 0; k < NP; ++k) {
+                        const float2 xhat = mul2(add2(vx.get(k), m2), r2);
+                        const float2 gw = mul2(vg.get(k), KEEP ? wv[KEEP ? i : 0][k] : wl[k]);
+                        out.set(k, fma2(xhat, f2, fma2(gw, r2, f1)));
+                    }
+                    out.store(dx + (long long)row * dxs + c);
                 }
             }
         }
     }
-    if (!arrived && threadIdx.x == 0)  // copies still under way land in this CTA's memory: wait for them (bounded)
-        for (int i = it > stages ? it - stages : 0; i < it + stages - 1; ++i)
-            if (blockIdx.x + (long long)i * gridDim.x < groups)
-                for (unsigned q = 0; q < kNormSpin && !barrier_try(smem_addr(&full[i % stages]), (uint32_t)(i / stages) & 1u); ++q) {}
+    if (!ring.arrived && threadIdx.x == 0) {
+        const long long mine = ((long long)groups - blockIdx.x + gridDim.x - 1) / gridDim.x;
+        ring.drain(it - 1, (int)min(mine, (long long)it + stages - 1));
+    }
     if (!partial) return;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -326,9 +503,9 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
         if (c < d) {
             float *a = partial + (long long)blockIdx.x * d + c, *b = a + (long long)gridDim.x * d;
 #pragma unroll
-            for (int j = 0; j < VEC; j += 4) {
-                *reinterpret_cast<float4 *>(a + j) = make_float4(dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]);
-                *reinterpret_cast<float4 *>(b + j) = make_float4(db[i][j], db[i][j + 1], db[i][j + 2], db[i][j + 3]);
+            for (int k = 0; k < NP; k += 2) {
+                *reinterpret_cast<float4 *>(a + 2 * k) = make_float4(dw[i][k].x, dw[i][k].y, dw[i][k + 1].x, dw[i][k + 1].y);
+                *reinterpret_cast<float4 *>(b + 2 * k) = make_float4(db[i][k].x, db[i][k].y, db[i][k + 1].x, db[i][k + 1].y);
             }
         }
     }
@@ -506,16 +683,16 @@ k_norm_param_gradient(const float *__restrict__ partial, int slots, int d, Q *__
     grid_dependency_launch_next();
     if (!out) return;
     const float *src = partial + (long long)blockIdx.y * slots * d + c;
-    float a = 0.0f, b = 0.0f;
+    float a[4] = {};
     if (c < d) {
         int i = k;
-        for (; i + 8 < slots; i += 16) {
-            a += src[(long long)i * d];
-            b += src[(long long)(i + 8) * d];
+        for (; i + 24 < slots; i += 32) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) a[u] += src[(long long)(i + 8 * u) * d];
         }
-        if (i < slots) a += src[(long long)i * d];
+        for (; i < slots; i += 8) a[0] += src[(long long)i * d];
     }
-    sum[k][lane] = a + b;
+    sum[k][lane] = (a[0] + a[1]) + (a[2] + a[3]);
     __syncthreads();
     if (k == 0 && c < d) {
         float t = 0.0f;
@@ -548,8 +725,53 @@ bool rows_aligned(const void *p, long long stride, int elem) { return pointer_al
 
 // CTAs whose sums of dw and db are added up at the end: what they write and what is read again stays under a tenth of
 // the rows' own traffic (16 bytes per slot and column against 6 per row and column), unless rows are few.
-int norm_slots(long long n) { return (int)(n / 27 > current_device_sms() ? n / 27 : current_device_sms()); }
+int norm_slots(long long n) { return (int)(n / 27 > 2 * current_device_sms() ? n / 27 : 2 * current_device_sms()); }
 int norm_slots_max() { return 6 * current_device_sms(); }
+
+// Lets `kernel` have the rings' shared memory, once per device (`ready`: a bit per device).
+template <typename K>
+cudaError_t allow_ring(K kernel, std::atomic<uint64_t> &ready)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (ready.load() >> (dev & 63) & 1)) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormRingBytes);
+    if (e == cudaSuccess) ready.fetch_or(1ull << (dev & 63));
+    return e;
+}
+
+// CTAs per multiprocessor and stages per ring: as many CTAs as the registers allow and the shared memory holds with three
+// stages each.
+struct RingShape {
+    int ctas, stages;
+};
+RingShape ring_shape(int threads, int registers, int stage, int least)
+{
+    RingShape r{65536 / (registers * threads), 0};
+    if (r.ctas > 2048 / threads) r.ctas = 2048 / threads;
+    if (r.ctas > 16) r.ctas = 16;
+    while (r.ctas > 1 && kNormRingBytes / r.ctas < 3 * stage) --r.ctas;
+    if (r.ctas < 1) r.ctas = 1;
+    r.stages = kNormRingBytes / r.ctas / stage;
+    if (r.stages > kNormMaxStages) r.stages = kNormMaxStages;
+    if (r.stages < least) r.stages = 0;
+    return r;
+}
+
+template <typename T, typename P, int E>
+cudaError_t forward_ring(RingShape ring, int threads, const T *xp, long long xs, const P *wp, const P *bp, T *yp, long long ys,
+                         float *mean, float *rstd, long long n, int d, float eps, cudaStream_t s)
+{
+    static std::atomic<uint64_t> ready{0};
+    unsigned int *status = nullptr;
+    cudaError_t e = operator_status_ptr(&status);
+    if (e == cudaSuccess) e = allow_ring(k_norm_forward_ring<T, P, E>, ready);
+    if (e != cudaSuccess) return e;
+    const long long most = (long long)ring.ctas * current_device_sms();
+    return launch_chained(k_norm_forward_ring<T, P, E>, (unsigned)(n < most ? n : most), threads,
+                          (size_t)ring.stages * d * sizeof(T), s, 1, xp, xs, wp, bp, yp, ys, mean, rstd, (int)n, d,
+                          1.0f / (float)d, 1.0f / sqrtf((float)d), eps, ring.stages, status);
+}
 
 template <typename T, typename P>
 cudaError_t norm_forward(const void *x, long long xs, const void *w, const void *b, void *y, long long ys, float *mean,
@@ -557,31 +779,34 @@ cudaError_t norm_forward(const void *x, long long xs, const void *w, const void 
 {
     constexpr int V = 16 / (int)sizeof(T), E = (int)sizeof(T);
     const NormShape sh = norm_shape(d, E, rows_aligned(x, xs, E) && rows_aligned(y, ys, E) && pointer_aligned(w, 16) &&
-                                              pointer_aligned(b, 16), kNormVecs, kNormScalars);
-    const float inv = 1.0f / (float)d;
+                                              pointer_aligned(b, 16), 16 / V, kNormScalars);
+    const float inv = 1.0f / (float)d, root = 1.0f / sqrtf((float)d);
     const T *xp = (const T *)x;
     const P *wp = (const P *)w, *bp = (const P *)b;
     T *yp = (T *)y;
     const unsigned rows = (unsigned)n, groups = (unsigned)((n + kNormWarps - 1) / kNormWarps);
-    if (sh.threads > kNormMaxThreads)
-        return launch_chained(k_norm_forward_long<T, P>, rows, kNormMaxThreads, 0, s, 1, xp, xs, wp, bp, yp, ys, mean,
-                              rstd, d, inv, eps);
-    // a warp per row: always for short rows, for long ones where rows are enough to fill the device with such warps
-    const bool many = groups >= 2u * (unsigned)current_device_sms();
     if (sh.vec && sh.units <= 32 * kNormVecs)
         return launch_chained(k_norm_forward<T, P, V, kNormVecs, true>, groups, 32 * kNormWarps, 0, s, 1, xp, xs, wp,
-                              bp, yp, ys, mean, rstd, n, d, inv, eps);
-    if (sh.vec && sh.units <= 32 * kNormVecsWarp && many)
-        return launch_chained(k_norm_forward<T, P, V, kNormVecsWarp, true>, groups, 32 * kNormWarps, 0, s, 1, xp, xs, wp,
-                              bp, yp, ys, mean, rstd, n, d, inv, eps);
-    if (sh.vec)
-        return launch_chained(k_norm_forward<T, P, V, kNormVecs, false>, rows, sh.threads, 0, s, 1, xp, xs, wp, bp, yp,
-                              ys, mean, rstd, n, d, inv, eps);
-    if (sh.units <= 32 * kNormScalars)
+                              bp, yp, ys, mean, rstd, n, d, inv, root, eps);
+    if (sh.vec) {
+        const int wide = (sh.threads / 2 + 31) / 32 * 32;  // threads that hold twice as many columns
+        if (sh.threads <= kNormRingThreads) {
+            const RingShape ring = ring_shape(sh.threads, 64, d * E, 2);
+            if (ring.stages)
+                return forward_ring<T, P, 16>(ring, sh.threads, xp, xs, wp, bp, yp, ys, mean, rstd, n, d, eps, s);
+        } else if (wide <= kNormRingThreads) {
+            const RingShape ring = ring_shape(wide, 128, d * E, 2);
+            if (ring.stages) return forward_ring<T, P, 32>(ring, wide, xp, xs, wp, bp, yp, ys, mean, rstd, n, d, eps, s);
+        }
+    }
+    if (!sh.vec && sh.units <= 32 * kNormScalars)
         return launch_chained(k_norm_forward<T, P, 1, kNormScalars, true>, groups, 32 * kNormWarps, 0, s, 1, xp, xs,
-                              wp, bp, yp, ys, mean, rstd, n, d, inv, eps);
-    return launch_chained(k_norm_forward<T, P, 1, kNormScalars, false>, rows, sh.threads, 0, s, 1, xp, xs, wp, bp, yp,
-                          ys, mean, rstd, n, d, inv, eps);
+                              wp, bp, yp, ys, mean, rstd, n, d, inv, root, eps);
+    if (!sh.vec && sh.threads <= kNormMaxThreads)
+        return launch_chained(k_norm_forward<T, P, 1, kNormScalars, false>, rows, sh.threads, 0, s, 1, xp, xs, wp, bp, yp,
+                              ys, mean, rstd, n, d, inv, root, eps);
+    return launch_chained(k_norm_forward_long<T, P>, rows, kNormMaxThreads, 0, s, 1, xp, xs, wp, bp, yp, ys, mean, rstd, d,
+                          inv, root, eps);
 }
 
 // Launches the ring kernel with `rows` rows per stage if its shared memory holds two stages at least.
@@ -591,31 +816,20 @@ bool launch_ring(cudaError_t *e, int *slots, int threads, const T *gp, long long
                  cudaStream_t s)
 {
     const int stage = ROWS * 2 * d * (int)sizeof(T);
-    int ctas = 65536 / (128 * threads);                     // registers
-    if (ctas > 2048 / threads) ctas = 2048 / threads;
-    while (ctas > 1 && kNormRingBytes / ctas < 3 * stage) --ctas;  // rather fewer CTAs with three stages
-    if (ctas < 1) ctas = 1;
-    int stages = kNormRingBytes / ctas / stage;
-    if (stages > kNormMaxStages) stages = kNormMaxStages;
-    if (stages < (ROWS > 1 ? 3 : 2)) return false;
+    const RingShape ring = ring_shape(threads, 128, stage, ROWS > 1 ? 3 : 2);
+    if (!ring.stages) return false;
+    static std::atomic<uint64_t> ready{0};
     unsigned int *status = nullptr;
     *e = operator_status_ptr(&status);
-    static std::atomic<uint64_t> ready{0};  // devices on which the kernel may have that much shared memory
-    int dev = 0;
-    if (*e == cudaSuccess) *e = cudaGetDevice(&dev);
-    if (*e == cudaSuccess && !(ready.load() >> (dev & 63) & 1)) {
-        *e = cudaFuncSetAttribute(k_norm_backward_ring<T, E, ROWS, P>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  kNormRingBytes);
-        if (*e == cudaSuccess) ready.fetch_or(1ull << (dev & 63));
-    }
+    if (*e == cudaSuccess) *e = allow_ring(k_norm_backward_ring<T, E, ROWS, P>, ready);
     if (*e != cudaSuccess) return true;
-    long long grid = (n + ROWS - 1) / ROWS, most = (long long)ctas * current_device_sms();
+    long long grid = (n + ROWS - 1) / ROWS, most = (long long)ring.ctas * current_device_sms();
     if (most > norm_slots(n)) most = norm_slots(n);
     if (most > norm_slots_max()) most = norm_slots_max();
     if (grid > most) grid = most;
     *slots = (int)grid;
-    *e = launch_chained(k_norm_backward_ring<T, E, ROWS, P>, (unsigned)grid, threads, (size_t)stages * stage, s, 1, gp, dys, xp,
-                        xs, wp, mean, rstd, dxp, dxs, part, (int)n, d, inv, stages, status);
+    *e = launch_chained(k_norm_backward_ring<T, E, ROWS, P>, (unsigned)grid, threads, (size_t)ring.stages * stage, s, 1, gp, dys, xp,
+                        xs, wp, mean, rstd, dxp, dxs, part, (int)n, d, inv, ring.stages, status);
     return true;
 }
 
@@ -652,7 +866,9 @@ cudaError_t norm_backward(const void *dy, long long dys, const void *x, long lon
     } else if (sh.vec && wide <= kNormBackThreads &&
                launch_ring<T, 32, 1, P>(&e, &slots, wide, gp, dys, xp, xs, wp, mean, rstd, dxp, dxs, part, n, d, inv, s)) {
     } else if (!sh.vec && sh.threads <= kNormBackThreads) {
-        const long long most = current_device_sms();
+        long long most = (long long)(65536 / (128 * sh.threads)) * current_device_sms();
+        if (most > norm_slots(n)) most = norm_slots(n);
+        if (most > norm_slots_max()) most = norm_slots_max();
         slots = (int)(n < most ? n : most);
         e = launch_chained(k_norm_backward<T, P, 1, false>, (unsigned)slots, sh.threads, 0, s, 1, gp, dys, xp, xs, wp, mean,
                            rstd, dxp, dxs, part, n, d, inv);
