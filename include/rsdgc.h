@@ -357,7 +357,7 @@ int rsdgc_payload_to_coo(rsdgc_plan *plan, const int32_t *idx_dev, const int32_t
  * x, y: `dtype`; weight, bias (both optional: 1 and 0): param_dtype, which is `dtype` or binary32.
  * mean_dev, rstd_dev: optional, binary32, what the backward pass takes.  n_rows = 0 does nothing.
  * Errors: INVALID (a needed pointer NULL, stride < width, width < 1, eps negative or NaN, types),
- * ALIGNMENT (a pointer that is not a multiple of its element size), CAPACITY (n_rows >= 2^31,
+ * ALIGNMENT (a pointer that is not a multiple of its element size), CAPACITY (n_rows > 2^30,
  * width > 2^24), CUDA.
  */
 int rsdgc_layer_norm_forward(const void *x_dev, int64_t x_stride, const void *weight_dev, const void *bias_dev,

@@ -3,61 +3,83 @@
 //   mean = sum x / D,  rstd = (sum (x - mean)^2 / D + eps)^(-1/2),  xhat = (x - mean) rstd,  y = xhat w + b
 //   dx = rstd (g w - mean(g w) - xhat mean(g w xhat)),  dw = sum_n g xhat,  db = sum_n g
 //
-// Bound: memory (about 2 flop per byte).  A row is read once and stays in registers: the mean, then the
-// centred squares (two reductions, no cancellation), then the output.  All statistics and sums are binary32.
+// Bound: memory, as long as the instructions per value stay few: a row is read once, in 16-byte packs, and its
+// arithmetic runs on pairs of binary32 values.  The mean, then the centred squares (two reductions, no cancellation),
+// then the output.  All statistics and sums are binary32.
+//
+// Rows that do not start on 16-byte boundaries (an odd width, say) keep the packs: what a thread owns is a 16-byte
+// granule of memory, and with it columns shifted by the row's phase, the number of elements between the granule's start
+// and the row's.  Phases repeat with a short period (at most 8 rows), so a CTA or warp takes rows of one phase only:
+// its threads then own the same columns in every row, as the sums of dw and db over the rows need it.  The first and
+// the last granule of a row are masked; where they would reach beyond the operand they are read element by element.
 #include <atomic>
 #include <climits>
+#include <cmath>
+#include <initializer_list>
 
 #include "device_utils.cuh"
 #include "operators_internal.cuh"
 
 namespace rsdgc {
 
-constexpr int kNormVecs = 2;          // 16-byte packs of a row that a lane holds where a warp takes the row
-constexpr int kNormScalars = 16;      // elements a thread holds where rows are not 16-byte aligned
+constexpr int kNormWarps = 4;              // warps of a CTA whose rows take one warp each, forward
+constexpr int kBackWarps = 8;              // ... backward
+constexpr int kNormElems = 16;             // columns of a thread (32 in the widest variants)
 constexpr int kNormRingThreads = 512;
-constexpr int kNormMaxThreads = 1024;
-constexpr int kNormBackThreads = 512; // backward: 128 registers for the columns' sums and the rows' operands
-constexpr int kBackWarps = 8;         // warps of a CTA whose rows take one warp each, backward
+constexpr int kNormLongThreads = 1024;
 constexpr int kNormMaxStages = 4;
 constexpr int kNormRingBytes = 200 << 10;  // shared memory of a multiprocessor's rings
 constexpr unsigned kNormSpin = 1u << 20;   // polls of a wait before it gives up
-constexpr int kNormWarps = 4;         // warps of a CTA whose rows take one warp each
 
-// Elements of a row as `VEC` packed values; VEC = 1 where rows do not start on 16-byte boundaries.
-template <typename T, int VEC>
-struct __align__(sizeof(T) * VEC < 16 ? sizeof(T) * VEC : 16) Pack {
-    T v[VEC];
-};
-
-template <typename T, int VEC>
-__device__ __forceinline__ Pack<T, VEC> load_pack(const T *p)
-{
-    return *reinterpret_cast<const Pack<T, VEC> *>(p);
-}
-// parameters may have another type than the rows: the widest load that their own alignment allows
-template <typename P, int VEC>
-__device__ __forceinline__ void load_param(const P *p, long long i, float *out)
-{
-    const Pack<P, VEC> k = *reinterpret_cast<const Pack<P, VEC> *>(p + i);
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) out[j] = to_f32(k.v[j]);
-}
-
-// A 16-byte pack as pairs of binary32 values: the arithmetic runs two values per instruction (f32x2), which matters
-// because rows of 16-bit values are bound by the issue rate, not by memory, at one instruction per value and step.
+// A 16-byte pack as pairs of binary32 values (f32x2 arithmetic: two values per instruction).
 template <typename T>
 struct Pairs {
-    static constexpr int N = 8 / (int)sizeof(T);  // pairs of a pack
+    static constexpr int N = 8 / (int)sizeof(T);   // pairs
+    static constexpr int V = 16 / (int)sizeof(T);  // elements
     uint32_t w[4];
     __device__ __forceinline__ void load(const T *p)
     {
         const uint4 v = *reinterpret_cast<const uint4 *>(p);
         w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
     }
-    __device__ __forceinline__ void store(T *p) const { *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]); }
+    __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = 0u; }
     __device__ __forceinline__ float2 get(int i) const;
     __device__ __forceinline__ void set(int i, float2 v);
+    // element j out of / into the pack
+    __device__ __forceinline__ T element(int j) const;
+    __device__ __forceinline__ void put(int j, T x);
+    // keeps the elements of columns 0 .. d - 1, the pack starting at column c
+    __device__ __forceinline__ void mask(int c, int d)
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = (unsigned)(c + j) < (unsigned)d ? w[j] : 0u;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                w[j] &= ((unsigned)(c + 2 * j) < (unsigned)d ? 0x0000FFFFu : 0u) |
+                        ((unsigned)(c + 2 * j + 1) < (unsigned)d ? 0xFFFF0000u : 0u);
+        }
+    }
+    // row: column 0 of a row whose granule `c` is wanted; only existing columns are touched
+    __device__ __forceinline__ void load_elements(const T *row, int c, int d)
+    {
+        clear();
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if ((unsigned)(c + j) < (unsigned)d) put(j, row[c + j]);
+    }
+    // whole: all of it exists and lies on a 16-byte boundary
+    __device__ __forceinline__ void store(T *row, bool whole, int c, int d) const
+    {
+        if (whole) {
+            *reinterpret_cast<uint4 *>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if ((unsigned)(c + j) < (unsigned)d) row[c + j] = element(j);
+        }
+    }
 };
 template <>
 __device__ __forceinline__ float2 Pairs<float>::get(int i) const
@@ -90,15 +112,47 @@ __device__ __forceinline__ void Pairs<__half>::set(int i, float2 v)
 {
     w[i] = pack2<__half>(v.x, v.y);
 }
-// `count` pairs of a parameter vector, or a constant where there is none
-template <typename P, int PAIRS>
-__device__ __forceinline__ void load_pairs(const P *p, long long c, bool there, float missing, float2 *out)
+template <>
+__device__ __forceinline__ float Pairs<float>::element(int j) const { return __uint_as_float(w[j]); }
+template <>
+__device__ __forceinline__ void Pairs<float>::put(int j, float x) { w[j] = __float_as_uint(x); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 Pairs<__nv_bfloat16>::element(int j) const
 {
-    if (p && there) {
+    return __ushort_as_bfloat16((unsigned short)(w[j >> 1] >> (16 * (j & 1))));
+}
+template <>
+__device__ __forceinline__ void Pairs<__nv_bfloat16>::put(int j, __nv_bfloat16 x)
+{
+    w[j >> 1] |= (uint32_t)__bfloat16_as_ushort(x) << (16 * (j & 1));
+}
+template <>
+__device__ __forceinline__ __half Pairs<__half>::element(int j) const
+{
+    return __ushort_as_half((unsigned short)(w[j >> 1] >> (16 * (j & 1))));
+}
+template <>
+__device__ __forceinline__ void Pairs<__half>::put(int j, __half x)
+{
+    w[j >> 1] |= (uint32_t)__half_as_ushort(x) << (16 * (j & 1));
+}
+
+// The parameters of the 2 * PAIRS columns from c on (those that exist), or a constant where there is no vector.
+template <bool SHIFT, typename P, int PAIRS>
+__device__ __forceinline__ void load_params(const P *p, int c, int d, float missing, float2 *out)
+{
+    if constexpr (SHIFT) {
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            const int a = c + 2 * i;
+            out[i].x = p && (unsigned)a < (unsigned)d ? to_f32(p[a]) : missing;
+            out[i].y = p && (unsigned)(a + 1) < (unsigned)d ? to_f32(p[a + 1]) : missing;
+        }
+    } else if (p && c < d) {
 #pragma unroll
         for (int k = 0; k < PAIRS / Pairs<P>::N; ++k) {
             Pairs<P> v;
-            v.load(p + c + k * (16 / (int)sizeof(P)));
+            v.load(p + c + k * Pairs<P>::V);
 #pragma unroll
             for (int i = 0; i < Pairs<P>::N; ++i) out[k * Pairs<P>::N + i] = v.get(i);
         }
@@ -108,8 +162,52 @@ __device__ __forceinline__ void load_pairs(const P *p, long long c, bool there, 
     }
 }
 
-// Sum over the threads of one row.  One warp per row: shuffles only.  Otherwise the whole CTA, one slot of
-// `part` per warp; the caller alternates between two buffers, so that one barrier per sum is enough.
+// Which rows a walker (CTA or warp) takes: those of one phase.
+struct PhaseRows {
+    int period, phase0, step;   // rows r and r + period have the same phase, (phase0 + r * step) mod V elements
+    bool same_out;              // the output's rows too
+};
+struct Walk {
+    int row0, period, phase;    // its rows: row0 + period * j
+    int count;                  // rows of this phase
+    int first, stride;          // it takes j = first, first + stride, ...
+};
+template <int V>
+__device__ __forceinline__ Walk walk_of(const PhaseRows &p, int walker, int walkers, int n)
+{
+    Walk w;
+    w.period = p.period;
+    w.row0 = walker % p.period;
+    w.phase = (p.phase0 + w.row0 * p.step) & (V - 1);
+    w.count = n > w.row0 ? (n - w.row0 + p.period - 1) / p.period : 0;
+    w.first = walker / p.period;
+    w.stride = walkers / p.period;  // a multiple of the period is launched
+    return w;
+}
+
+// The granules of a thread: columns start + i * pitch on.  SHIFT: rows are shifted, or the width is no whole number of
+// granules, or an output's rows lie elsewhere; without it every granule is whole.
+template <bool SHIFT, int V, int NV>
+struct Columns {
+    int start, pitch, d;
+    unsigned whole_bits, store_bits;
+    __device__ __forceinline__ Columns(int thread, int threads, int phase, int width, bool same_out)
+        : start(thread * V - phase), pitch(threads * V), d(width), whole_bits(0), store_bits(0)
+    {
+        if constexpr (SHIFT) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) whole_bits |= (unsigned)(at(i) >= 0 && at(i) + V <= d) << i;
+            store_bits = same_out ? whole_bits : 0u;
+        }
+    }
+    __device__ __forceinline__ int at(int i) const { return start + i * pitch; }
+    __device__ __forceinline__ bool any(int i) const { return at(i) < d; }
+    __device__ __forceinline__ bool whole(int i) const { return !SHIFT || (whole_bits >> i & 1); }
+    __device__ __forceinline__ bool stored_whole(int i) const { return !SHIFT || (store_bits >> i & 1); }
+};
+
+// Sum over the threads of one row: a warp, or the CTA with one slot of `part` per warp (the caller alternates between
+// two buffers, so that one barrier per sum is enough).
 template <bool WARP>
 __device__ __forceinline__ float row_sum(float x, float *part)
 {
@@ -120,21 +218,9 @@ __device__ __forceinline__ float row_sum(float x, float *part)
     __syncthreads();
     return warp_sum(lane < warps ? part[lane] : 0.0f);
 }
-template <bool WARP>
-__device__ __forceinline__ float2 row_sum2(float x, float y, float2 *part)
-{
-    x = warp_sum(x);
-    y = warp_sum(y);
-    if (WARP) return make_float2(x, y);
-    const int warps = (int)(blockDim.x >> 5), lane = threadIdx.x & 31;
-    if (lane == 0) part[threadIdx.x >> 5] = make_float2(x, y);
-    __syncthreads();
-    const float2 z = lane < warps ? part[lane] : make_float2(0.0f, 0.0f);
-    return make_float2(warp_sum(z.x), warp_sum(z.y));
-}
 
-// A ring of stages in shared memory, each `operands` rows, filled by bulk copies that run `stages` - 1 (or more) rows
-// ahead, so that a CTA has tens of KB on their way whatever its threads wait for.
+// A ring of stages in shared memory, each one or several rows, filled by bulk copies that run ahead of the threads, so
+// that a CTA has tens of KB on their way whatever its threads wait for.
 struct RowRing {
     uint32_t base, full;   // shared-memory addresses: rows, barriers (8 bytes each)
     uint32_t stage_bytes;
@@ -162,177 +248,229 @@ struct RowRing {
             for (unsigned q = 0; q < kNormSpin && !barrier_try(bar(i), (uint32_t)(i / stages) & 1u); ++q) {}
     }
 };
+
+// The granules of a row that lie inside the operand, as a bulk copy: all of them but the first of the operand's first
+// row and the last of its last, where these reach beyond it.
+struct RowCopy {
+    uint32_t skip, bytes;  // bytes left out at the front, bytes copied
+};
 template <typename T>
-__device__ __forceinline__ const T *shared_row(uint32_t addr)
+__device__ __forceinline__ RowCopy row_copy(int row, int n, int phase, int d)
 {
-    return reinterpret_cast<const T *>(__cvta_shared_to_generic(addr));
+    constexpr int V = Pairs<T>::V;
+    int g0 = 0, g1 = (phase + d + V - 1) / V;
+    if (row == 0 && phase) g0 = 1;
+    if (row == n - 1 && (phase + d) % V) --g1;
+    return {(uint32_t)g0 * 16u, g1 > g0 ? (uint32_t)(g1 - g0) * 16u : 0u};
+}
+// Granule i of `row` (column 0) from its copy in shared memory; masked at the row's ends.
+template <bool SHIFT, typename T, int NV>
+__device__ __forceinline__ void take(Pairs<T> &v, const Columns<SHIFT, Pairs<T>::V, NV> &cols, int i, uint32_t copy, int phase,
+                                     const T *row, bool edge)
+{
+    const int c = cols.at(i);
+    if (SHIFT && edge && !cols.whole(i)) {
+        v.load_elements(row, c, cols.d);
+        return;
+    }
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3])
+                 : "r"(copy + (uint32_t)(c + phase) * (uint32_t)sizeof(T)));
+    if (SHIFT && !cols.whole(i)) v.mask(c, cols.d);
+}
+// Rows whose granules may reach beyond the operand's first or last value (one row at either end unless rows are
+// shorter than a granule).
+template <int V>
+__device__ __forceinline__ bool near_end(long long row, int n, int d)
+{
+    return row * d < V || (n - 1 - row) * d < V;
+}
+// ... straight from global memory
+template <bool SHIFT, typename T, int NV>
+__device__ __forceinline__ void take(Pairs<T> &v, const Columns<SHIFT, Pairs<T>::V, NV> &cols, int i, const T *row, bool edge)
+{
+    const int c = cols.at(i);
+    if (SHIFT && edge && !cols.whole(i)) {
+        v.load_elements(row, c, cols.d);
+        return;
+    }
+    v.load(row + c);
+    if (SHIFT && !cols.whole(i)) v.mask(c, cols.d);
 }
 
 // ---- forward ----------------------------------------------------------------------------------
-// Aligned rows: a CTA walks the rows blockIdx.x, blockIdx.x + gridDim.x, ...; its threads keep their columns' weight
-// and bias as binary32 pairs.  Two barriers per row (mean, then the centred squares); the next rows arrive meanwhile.
-template <typename T, typename P, int E>
+// The two passes over a row that is in registers.
+template <bool SHIFT, typename T, int NV, bool WARP>
+__device__ __forceinline__ void row_statistics(const Pairs<T> (&in)[NV], const Columns<SHIFT, Pairs<T>::V, NV> &cols, float inv_d,
+                                               float root_inv_d, float eps, float (*part)[32], float *mu, float *r)
+{
+    constexpr int NP = Pairs<T>::N;
+    float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (cols.any(i)) {
+#pragma unroll
+            for (int k = 0; k < NP; ++k) sum = add2(sum, in[i].get(k));  // masked columns are zero
+        }
+    *mu = row_sum<WARP>(sum.x + sum.y, part[0]) * inv_d;
+    // the squares are scaled term by term: their sum may leave the range where their mean does not
+    const float2 rr = make_float2(root_inv_d, root_inv_d), m2 = make_float2(-*mu, -*mu);
+    float2 sq = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (cols.any(i)) {
+            if (cols.whole(i)) {
+#pragma unroll
+                for (int k = 0; k < NP; ++k) {
+                    const float2 e = mul2(add2(in[i].get(k), m2), rr);
+                    sq = fma2(e, e, sq);
+                }
+            } else {
+                const int c = cols.at(i);
+#pragma unroll
+                for (int k = 0; k < NP; ++k) {
+                    float2 e = mul2(add2(in[i].get(k), m2), rr);
+                    e.x = (unsigned)(c + 2 * k) < (unsigned)cols.d ? e.x : 0.0f;
+                    e.y = (unsigned)(c + 2 * k + 1) < (unsigned)cols.d ? e.y : 0.0f;
+                    sq = fma2(e, e, sq);
+                }
+            }
+        }
+    *r = rsqrtf(row_sum<WARP>(sq.x + sq.y, part[1]) + eps);
+}
+
+template <bool SHIFT, typename T, int NV>
+__device__ __forceinline__ void write_row(const Pairs<T> (&in)[NV], T *row, const Columns<SHIFT, Pairs<T>::V, NV> &cols, float mu,
+                                          float r, const float2 (*wv)[Pairs<T>::N], const float2 (*bv)[Pairs<T>::N])
+{
+    const float2 m2 = make_float2(-mu, -mu), r2 = make_float2(r, r);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (cols.any(i)) {
+            Pairs<T> out;
+#pragma unroll
+            for (int k = 0; k < Pairs<T>::N; ++k) out.set(k, fma2(mul2(add2(in[i].get(k), m2), r2), wv[i][k], bv[i][k]));
+            out.store(row, cols.stored_whole(i), cols.at(i), cols.d);
+        }
+    }
+}
+
+// A CTA per row, rows through the ring; the threads keep their columns' weight and bias as binary32 pairs.  Two barriers
+// per row (mean, squares); the next rows arrive meanwhile.
+template <bool SHIFT, typename T, typename P, int E>
 __global__ void __launch_bounds__(kNormRingThreads, E <= 16 ? 2 : 1)
 k_norm_forward_ring(const T *__restrict__ x, long long xs, const P *__restrict__ w, const P *__restrict__ b,
                     T *__restrict__ y, long long ys, float *__restrict__ mean, float *__restrict__ rstd, int n, int d,
-                    float inv_d, float root_inv_d, float eps, int stages, unsigned int *status)
+                    PhaseRows phases, float inv_d, float root_inv_d, float eps, int stages, uint32_t stage_bytes,
+                    unsigned int *status)
 {
-    constexpr int VEC = 16 / (int)sizeof(T), NV = E / VEC, NP = Pairs<T>::N;
+    constexpr int V = Pairs<T>::V, NV = E / V, NP = Pairs<T>::N;
     extern __shared__ __align__(128) unsigned char rows[];
     __shared__ float part[2][32];
     __shared__ __align__(8) unsigned long long full[kNormMaxStages];
-    const int step = blockDim.x;
-    const uint32_t row_bytes = (uint32_t)d * sizeof(T);
-    RowRing ring = {smem_addr(rows), smem_addr(full), row_bytes, stages, true, status};
+    const Walk walk = walk_of<V>(phases, blockIdx.x, gridDim.x, n);
+    RowRing ring = {smem_addr(rows), smem_addr(full), stage_bytes, stages, true, status};
     if (threadIdx.x < stages) barrier_init(ring.bar(threadIdx.x), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
     grid_dependency_wait();
     grid_dependency_launch_next();
     auto load = [&](int i) {
-        const long long row = blockIdx.x + (long long)i * gridDim.x;
-        if (row >= n) return;
-        barrier_expect(ring.bar(i), row_bytes);
-        bulk_copy(ring.at(i), x + row * xs, row_bytes, ring.bar(i));
+        const int j = walk.first + i * walk.stride;
+        if (j >= walk.count) return;
+        const int row = walk.row0 + walk.period * j;
+        const RowCopy copy = row_copy<T>(row, n, walk.phase, d);
+        barrier_expect(ring.bar(i), copy.bytes);
+        if (copy.bytes)
+            bulk_copy(ring.at(i) + copy.skip, reinterpret_cast<const unsigned char *>(x + row * xs - walk.phase) + copy.skip,
+                      copy.bytes, ring.bar(i));
     };
     if (threadIdx.x == 0)
         for (int i = 0; i < stages; ++i) load(i);
+    const Columns<SHIFT, V, NV> cols(threadIdx.x, blockDim.x, SHIFT ? walk.phase : 0, d, phases.same_out);
     float2 wv[NV][NP], bv[NV][NP];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (threadIdx.x + i * step) * VEC;
-        load_pairs<P, NP>(w, c, c < d, 1.0f, wv[i]);
-        load_pairs<P, NP>(b, c, c < d, 0.0f, bv[i]);
+        load_params<SHIFT, P, NP>(w, cols.at(i), d, 1.0f, wv[i]);
+        load_params<SHIFT, P, NP>(b, cols.at(i), d, 0.0f, bv[i]);
     }
     int it = 0;
-    for (int row = blockIdx.x; row < n; row += gridDim.x, ++it) {
+    for (int j = walk.first; j < walk.count; j += walk.stride, ++it) {
+        const int row = walk.row0 + walk.period * j;
+        const bool edge = row == 0 || row == n - 1;
         ring.wait(it);
-        const T *src = shared_row<T>(ring.at(it));
         Pairs<T> in[NV];
-        float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (threadIdx.x + i * step) * VEC;
-            if (c < d) {
-                in[i].load(src + c);
-#pragma unroll
-                for (int k = 0; k < NP; ++k) sum = add2(sum, in[i].get(k));
-            }
+            if (cols.any(i)) take(in[i], cols, i, ring.at(it), SHIFT ? walk.phase : 0, x + row * xs, edge);
         }
-        const float mu = row_sum<false>(sum.x + sum.y, part[0]) * inv_d;
-        if (threadIdx.x == 0) load(it + stages);  // every thread has read the stage
-        // the squares are scaled term by term: their sum may leave the range where their mean does not
-        const float2 rr = make_float2(root_inv_d, root_inv_d), m2 = make_float2(-mu, -mu);
-        float2 sq = make_float2(0.0f, 0.0f);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (threadIdx.x + i * step) * VEC;
-            if (c < d) {
-#pragma unroll
-                for (int k = 0; k < NP; ++k) {
-                    const float2 e = mul2(add2(in[i].get(k), m2), rr);
-                    sq = fma2(e, e, sq);
-                }
-            }
-        }
-        const float r = rsqrtf(row_sum<false>(sq.x + sq.y, part[1]) + eps);
+        float mu, r;
+        row_statistics<SHIFT, T, NV, false>(in, cols, inv_d, root_inv_d, eps, part, &mu, &r);
         if (threadIdx.x == 0) {
+            load(it + stages);  // behind the statistics' barriers: every thread has read the stage
             if (mean) mean[row] = mu;
             if (rstd) rstd[row] = r;
         }
-        const float2 r2 = make_float2(r, r);
-        T *dst = y + row * ys;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (threadIdx.x + i * step) * VEC;
-            if (c < d) {
-                Pairs<T> out;
-#pragma unroll
-                for (int k = 0; k < NP; ++k)
-                    out.set(k, fma2(mul2(add2(in[i].get(k), m2), r2), wv[i][k], bv[i][k]));
-                out.store(dst + c);
-            }
-        }
+        write_row<SHIFT, T, NV>(in, y + row * ys, cols, mu, r, wv, bv);
     }
     if (!ring.arrived && threadIdx.x == 0) {
-        const long long mine = (n - (long long)blockIdx.x + gridDim.x - 1) / gridDim.x;
-        ring.drain(it - 1, (int)min(mine, (long long)it + stages));
+        const int mine = (walk.count - walk.first + walk.stride - 1) / walk.stride;
+        ring.drain(it - 1, min(mine, it + stages));
     }
 }
 
-// Rows in registers: a warp per row (aligned rows of at most 32 * kNormVecs packs, others of at most 32 * kNormScalars
-// values), or, where rows are not aligned and longer, a CTA per row.
-template <typename T, typename P, int VEC, int NV, bool WARP>
-__global__ void __launch_bounds__(WARP ? 32 * kNormWarps : kNormMaxThreads)
-k_norm_forward(const T *__restrict__ x, long long xs, const P *__restrict__ w, const P *__restrict__ b,
-               T *__restrict__ y, long long ys, float *__restrict__ mean, float *__restrict__ rstd, long long n,
-               int d, float inv_d, float root_inv_d, float eps)
+// A warp per row, kNormWarps walkers per CTA; the next row is loaded while this one is reduced.
+template <bool SHIFT, typename T, typename P>
+__global__ void __launch_bounds__(32 * kNormWarps)
+k_norm_forward_warp(const T *__restrict__ x, long long xs, const P *__restrict__ w, const P *__restrict__ b,
+                    T *__restrict__ y, long long ys, float *__restrict__ mean, float *__restrict__ rstd, int n, int d,
+                    PhaseRows phases, float inv_d, float root_inv_d, float eps)
 {
-    __shared__ float part[2][32];
-    const int tid = WARP ? (threadIdx.x & 31) : threadIdx.x;
-    const int step = WARP ? 32 : blockDim.x;
-    const long long row = WARP ? (long long)blockIdx.x * kNormWarps + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    constexpr int V = Pairs<T>::V, NV = kNormElems / V, NP = Pairs<T>::N;
+    float part[2][32];  // not used: a warp sums by shuffles
+    const int lane = threadIdx.x & 31;
+    const Walk walk = walk_of<V>(phases, blockIdx.x * kNormWarps + (threadIdx.x >> 5), gridDim.x * kNormWarps, n);
+    const Columns<SHIFT, V, NV> cols(lane, 32, SHIFT ? walk.phase : 0, d, phases.same_out);
     grid_dependency_wait();
     grid_dependency_launch_next();
-    if (row >= n) return;
-    const T *xr = x + row * xs;
-    Pack<T, VEC> in[NV];
-    float sum = 0.0f;
+    Pairs<T> next[NV];
+    auto fetch = [&](int j) {
+        const int row = walk.row0 + walk.period * j;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (tid + i * step) * VEC;
-        if (c < d) in[i] = load_pack<T, VEC>(xr + c);
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (tid + i * step) * VEC;
-        if (c < d) {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) sum += to_f32(in[i].v[j]);
+        for (int i = 0; i < NV; ++i) {
+            if (j < walk.count && cols.any(i)) take(next[i], cols, i, x + row * xs, near_end<V>(row, n, d));
         }
-    }
-    const float mu = row_sum<WARP>(sum, part[0]) * inv_d;
-    float sq = 0.0f;
+    };
+    fetch(walk.first);
+    float2 wv[NV][NP], bv[NV][NP];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (tid + i * step) * VEC;
-        if (c < d) {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float e = (to_f32(in[i].v[j]) - mu) * root_inv_d;
-                sq = fmaf(e, e, sq);
-            }
-        }
+        load_params<SHIFT, P, NP>(w, cols.at(i), d, 1.0f, wv[i]);
+        load_params<SHIFT, P, NP>(b, cols.at(i), d, 0.0f, bv[i]);
     }
-    const float r = rsqrtf(row_sum<WARP>(sq, part[1]) + eps);
-    if (tid == 0) {
-        if (mean) mean[row] = mu;
-        if (rstd) rstd[row] = r;
-    }
-    T *yr = y + row * ys;
+    for (int j = walk.first; j < walk.count; j += walk.stride) {
+        const int row = walk.row0 + walk.period * j;
+        Pairs<T> in[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (tid + i * step) * VEC;
-        if (c < d) {
-            float wv[VEC], bv[VEC];
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) wv[j] = 1.0f, bv[j] = 0.0f;
-            if (w) load_param<P, VEC>(w, c, wv);
-            if (b) load_param<P, VEC>(b, c, bv);
-            Pack<T, VEC> out;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) out.v[j] = from_f32<T>(fmaf((to_f32(in[i].v[j]) - mu) * r, wv[j], bv[j]));
-            *reinterpret_cast<Pack<T, VEC> *>(yr + c) = out;
+        for (int i = 0; i < NV; ++i) in[i] = next[i];
+        fetch(j + walk.stride);
+        float mu, r;
+        row_statistics<SHIFT, T, NV, true>(in, cols, inv_d, root_inv_d, eps, part, &mu, &r);
+        if (lane == 0) {
+            if (mean) mean[row] = mu;
+            if (rstd) rstd[row] = r;
         }
+        write_row<SHIFT, T, NV>(in, y + row * ys, cols, mu, r, wv, bv);
     }
 }
 
-// Rows longer than a CTA's registers hold: the row is read three times, the last two out of L2.
+// Any layout and width, a value at a time: rows longer than the ring holds, and operands whose rows have different
+// phases.  The row is read three times, the last two out of L2.
 template <typename T, typename P>
-__global__ void __launch_bounds__(kNormMaxThreads)
-k_norm_forward_long(const T *__restrict__ x, long long xs, const P *__restrict__ w, const P *__restrict__ b,
-                    T *__restrict__ y, long long ys, float *__restrict__ mean, float *__restrict__ rstd,
-                    int d, float inv_d, float root_inv_d, float eps)
+__global__ void __launch_bounds__(kNormLongThreads)
+k_norm_forward_any(const T *__restrict__ x, long long xs, const P *__restrict__ w, const P *__restrict__ b,
+                   T *__restrict__ y, long long ys, float *__restrict__ mean, float *__restrict__ rstd,
+                   int d, float inv_d, float root_inv_d, float eps)
 {
     __shared__ float part[2][32];
     grid_dependency_wait();
@@ -359,100 +497,154 @@ k_norm_forward_long(const T *__restrict__ x, long long xs, const P *__restrict__
 // Sums of dw and db: every thread keeps those of its columns over all rows its CTA takes, and writes them to
 // `partial` ([2][CTAs][d]) at the end; k_norm_param_gradient adds them up in a fixed order.  No atomics: the same
 // bits from run to run.
-constexpr int kBackElems = 16;  // columns of a thread
+template <typename T>
+struct BackSums {
+    float2 s1, s2;
+    // g w, its sums, and the columns' sums, for one granule
+    __device__ __forceinline__ void add(const Pairs<T> &vx, const Pairs<T> &vg, const float2 *wv, float2 m2, float2 r2,
+                                        float2 *dw, float2 *db)
+    {
+#pragma unroll
+        for (int k = 0; k < Pairs<T>::N; ++k) {
+            const float2 gv = vg.get(k), xhat = mul2(add2(vx.get(k), m2), r2);
+            const float2 gw = mul2(gv, wv[k]);
+            s1 = add2(s1, gw);
+            s2 = fma2(gw, xhat, s2);
+            dw[k] = fma2(gv, xhat, dw[k]);
+            db[k] = add2(db[k], gv);
+        }
+    }
+};
+// dx = rstd g w - rstd mean(g w) - xhat rstd mean(g w xhat) of one granule; f1 and f2 are the two means times -rstd
+template <typename T>
+__device__ __forceinline__ Pairs<T> input_gradient(const Pairs<T> &vx, const Pairs<T> &vg, const float2 *wv, float2 m2, float2 r2,
+                                                   float2 f1, float2 f2)
+{
+    Pairs<T> out;
+#pragma unroll
+    for (int k = 0; k < Pairs<T>::N; ++k) {
+        const float2 xhat = mul2(add2(vx.get(k), m2), r2);
+        out.set(k, fma2(xhat, f2, fma2(mul2(vg.get(k), wv[k]), r2, f1)));
+    }
+    return out;
+}
 
-// Aligned rows: ROWS rows of x and dy per stage of the ring.  One barrier per stage: it ends the sums of this stage
-// and, with it, all reads of the one before, which is refilled behind it.
-template <typename T, int E, int ROWS, typename P>
-__global__ void __launch_bounds__(kNormBackThreads)
+// A CTA per row, ROWS rows of x and dy per stage of the ring.  One barrier per stage: it ends the sums of this stage
+// and, with it, all reads of the one before, which is refilled behind it.  E <= 16: weight, x and dy stay in registers
+// between the two passes; E = 32: x and dy are read again, the weight lies in shared memory in the threads' order.
+template <bool SHIFT, typename T, int E, int ROWS, typename P>
+__global__ void __launch_bounds__(kNormRingThreads)
 k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
                      const P *__restrict__ w, const float *__restrict__ mean, const float *__restrict__ rstd,
-                     T *__restrict__ dx, long long dxs, float *__restrict__ partial, int n, int d, float inv_d, int stages,
-                     unsigned int *status)
+                     T *__restrict__ dx, long long dxs, float *__restrict__ partial, int n, int d, PhaseRows phases,
+                     float inv_d, int stages, uint32_t row_bytes, unsigned int *status)
 {
-    constexpr int VEC = 16 / (int)sizeof(T), NV = E / VEC, NP = Pairs<T>::N;
-    constexpr bool KEEP = E <= 16;  // weight, x and dy stay in registers between the two passes over a row
+    constexpr int V = Pairs<T>::V, NV = E / V, NP = Pairs<T>::N;
+    constexpr bool KEEP = E <= 16;
     extern __shared__ __align__(128) unsigned char rows[];
     __shared__ float2 part[2][ROWS][32];
     __shared__ __align__(8) unsigned long long full[kNormMaxStages];
-    const int step = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t row_bytes = (uint32_t)d * sizeof(T);
-    const int groups = (n + ROWS - 1) / ROWS;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const Walk walk = walk_of<V>(phases, blockIdx.x, gridDim.x, n);
+    const int groups = (walk.count + ROWS - 1) / ROWS;
     RowRing ring = {smem_addr(rows), smem_addr(full), ROWS * 2 * row_bytes, stages, true, status};
     if (threadIdx.x < stages) barrier_init(ring.bar(threadIdx.x), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
     grid_dependency_wait();
     grid_dependency_launch_next();
+    auto row_of = [&](int g, int r) { return walk.row0 + walk.period * (g * ROWS + r); };
     auto load = [&](int i) {  // by one thread
-        const long long g = blockIdx.x + (long long)i * gridDim.x;
+        const int g = walk.first + i * walk.stride;
         if (g >= groups) return;
-        const int count = min(ROWS, n - (int)g * ROWS);
-        barrier_expect(ring.bar(i), 2 * count * row_bytes);
+        const int count = min(ROWS, walk.count - g * ROWS);
+        RowCopy copy[ROWS];
+        uint32_t bytes = 0;
         for (int r = 0; r < count; ++r) {
-            bulk_copy(ring.at(i) + 2 * r * row_bytes, x + (g * ROWS + r) * xs, row_bytes, ring.bar(i));
-            bulk_copy(ring.at(i) + (2 * r + 1) * row_bytes, dy + (g * ROWS + r) * dys, row_bytes, ring.bar(i));
+            copy[r] = row_copy<T>(row_of(g, r), n, walk.phase, d);
+            bytes += 2 * copy[r].bytes;
+        }
+        barrier_expect(ring.bar(i), bytes);
+        for (int r = 0; r < count; ++r) {
+            const long long row = row_of(g, r);
+            const uint32_t dst = ring.at(i) + 2 * r * row_bytes + copy[r].skip;
+            if (!copy[r].bytes) continue;
+            bulk_copy(dst, reinterpret_cast<const unsigned char *>(x + row * xs - walk.phase) + copy[r].skip, copy[r].bytes,
+                      ring.bar(i));
+            bulk_copy(dst + row_bytes, reinterpret_cast<const unsigned char *>(dy + row * dys - walk.phase) + copy[r].skip,
+                      copy[r].bytes, ring.bar(i));
         }
     };
     if (threadIdx.x == 0)
         for (int i = 0; i + 1 < stages; ++i) load(i);
 
+    const Columns<SHIFT, V, NV> cols(threadIdx.x, blockDim.x, SHIFT ? walk.phase : 0, d, phases.same_out);
     float2 dw[NV][NP], db[NV][NP], wv[KEEP ? NV : 1][NP];
+    float2 *const shared_w = reinterpret_cast<float2 *>(rows + stages * ROWS * 2 * row_bytes);
+    auto weight = [&](int i, float2 *out) {
+#pragma unroll
+        for (int k = 0; k < NP; ++k) out[k] = shared_w[(i * NP + k) * blockDim.x + threadIdx.x];
+    };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (threadIdx.x + i * step) * VEC;
-        if constexpr (KEEP) load_pairs<P, NP>(w, c, c < d, 1.0f, wv[i]);
+        if constexpr (KEEP) {
+            load_params<SHIFT, P, NP>(w, cols.at(i), d, 1.0f, wv[i]);
+        } else {
+            load_params<SHIFT, P, NP>(w, cols.at(i), d, 1.0f, wv[0]);
+#pragma unroll
+            for (int k = 0; k < NP; ++k) shared_w[(i * NP + k) * blockDim.x + threadIdx.x] = wv[0][k];  // read by this thread
+        }
 #pragma unroll
         for (int k = 0; k < NP; ++k) dw[i][k] = db[i][k] = make_float2(0.0f, 0.0f);
     }
     float nmu[ROWS], nr[ROWS];  // the next stage's statistics
-    auto statistics = [&](long long g) {
+    auto statistics = [&](int g) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            const long long row = g * ROWS + r;
-            nmu[r] = row < n ? mean[row] : 0.0f;
-            nr[r] = row < n ? rstd[row] : 0.0f;
+            const bool there = g * ROWS + r < walk.count;
+            nmu[r] = there ? mean[row_of(g, r)] : 0.0f;
+            nr[r] = there ? rstd[row_of(g, r)] : 0.0f;
         }
     };
-    statistics(blockIdx.x);
+    statistics(walk.first);
     int it = 0;
-    for (int g = blockIdx.x; g < groups; g += gridDim.x, ++it) {
+    for (int g = walk.first; g < groups; g += walk.stride, ++it) {
         const int turn = it & 1;
         float mu[ROWS], rs[ROWS];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) mu[r] = nmu[r], rs[r] = nr[r];
-        statistics((long long)g + gridDim.x);
+        statistics(g + walk.stride);
         ring.wait(it);
         Pairs<T> px[KEEP ? ROWS : 1][KEEP ? NV : 1], pg[KEEP ? ROWS : 1][KEEP ? NV : 1];
+        auto operands = [&](int r, int i, Pairs<T> &vx, Pairs<T> &vg) {
+            const long long row = row_of(g, r);
+            const bool edge = row == 0 || row == n - 1;
+            const uint32_t copy = ring.at(it) + 2 * r * row_bytes;
+            take(vx, cols, i, copy, SHIFT ? walk.phase : 0, x + row * xs, edge);
+            take(vg, cols, i, copy + row_bytes, SHIFT ? walk.phase : 0, dy + row * dys, edge);
+        };
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            const T *sx = shared_row<T>(ring.at(it) + 2 * r * row_bytes), *sg = shared_row<T>(ring.at(it) + (2 * r + 1) * row_bytes);
             const float2 m2 = make_float2(-mu[r], -mu[r]), r2 = make_float2(rs[r], rs[r]);
-            float2 s1 = make_float2(0.0f, 0.0f), s2 = s1;
-            if (g * ROWS + r < n) {
+            BackSums<T> sums = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+            if (g * ROWS + r < walk.count) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
-                    const int c = (threadIdx.x + i * step) * VEC;
-                    if (c < d) {
+                    if (cols.any(i)) {
                         Pairs<T> vx, vg;
-                        vx.load(sx + c);
-                        vg.load(sg + c);
-                        if constexpr (KEEP) px[r][i] = vx, pg[r][i] = vg;
-                        float2 wl[NP];
-                        if constexpr (!KEEP) load_pairs<P, NP>(w, c, true, 1.0f, wl);
-#pragma unroll
-                        for (int k = 0; k < NP; ++k) {
-                            const float2 gv = vg.get(k), xhat = mul2(add2(vx.get(k), m2), r2);
-                            const float2 gw = mul2(gv, KEEP ? wv[KEEP ? i : 0][k] : wl[k]);
-                            s1 = add2(s1, gw);
-                            s2 = fma2(gw, xhat, s2);
-                            dw[i][k] = fma2(gv, xhat, dw[i][k]);
-                            db[i][k] = add2(db[i][k], gv);
+                        operands(r, i, vx, vg);
+                        if constexpr (KEEP) {
+                            px[r][i] = vx, pg[r][i] = vg;
+                            sums.add(vx, vg, wv[i], m2, r2, dw[i], db[i]);
+                        } else {
+                            float2 wl[NP];
+                            weight(i, wl);
+                            sums.add(vx, vg, wl, m2, r2, dw[i], db[i]);
                         }
                     }
                 }
             }
-            const float a = warp_sum(s1.x + s1.y), b = warp_sum(s2.x + s2.y);
+            const float a = warp_sum(sums.s1.x + sums.s1.y), b = warp_sum(sums.s2.x + sums.s2.y);
             if (lane == 0) part[turn][r][warp] = make_float2(a, b);
         }
         __syncthreads();
@@ -460,176 +652,140 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
         if (!dx) continue;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            const int row = g * ROWS + r;
-            if (row >= n) break;
-            const float2 t = lane < (step >> 5) ? part[turn][r][lane] : make_float2(0.0f, 0.0f);
-            // dx = rstd g w - rstd mean(g w) - xhat rstd mean(g w xhat)
+            if (g * ROWS + r >= walk.count) break;
+            const float2 t = lane < warps ? part[turn][r][lane] : make_float2(0.0f, 0.0f);
             const float c1 = -rs[r] * (warp_sum(t.x) * inv_d), c2 = -rs[r] * (warp_sum(t.y) * inv_d);
             const float2 m2 = make_float2(-mu[r], -mu[r]), r2 = make_float2(rs[r], rs[r]), f1 = make_float2(c1, c1),
                          f2 = make_float2(c2, c2);
-            const T *sx = shared_row<T>(ring.at(it) + 2 * r * row_bytes), *sg = shared_row<T>(ring.at(it) + (2 * r + 1) * row_bytes);
+            T *dst = dx + (long long)row_of(g, r) * dxs;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int c = (threadIdx.x + i * step) * VEC;
-                if (c < d) {
-                    Pairs<T> vx, vg, out;
+                if (cols.any(i)) {
                     if constexpr (KEEP) {
-                        vx = px[r][i], vg = pg[r][i];
+                        input_gradient<T>(px[r][i], pg[r][i], wv[i], m2, r2, f1, f2)
+                            .store(dst, cols.stored_whole(i), cols.at(i), d);
                     } else {
-                        vx.load(sx + c);
-                        vg.load(sg + c);
+                        Pairs<T> vx, vg;
+                        float2 wl[NP];
+                        operands(r, i, vx, vg);
+                        weight(i, wl);
+                        input_gradient<T>(vx, vg, wl, m2, r2, f1, f2).store(dst, cols.stored_whole(i), cols.at(i), d);
                     }
-                    float2 wl[NP];
-                    if constexpr (!KEEP) load_pairs<P, NP>(w, c, true, 1.0f, wl);
-#pragma unroll
-                    for (int k = 0; k < NP; ++k) {
-                        const float2 xhat = mul2(add2(vx.get(k), m2), r2);
-                        const float2 gw = mul2(vg.get(k), KEEP ? wv[KEEP ? i : 0][k] : wl[k]);
-                        out.set(k, fma2(xhat, f2, fma2(gw, r2, f1)));
-                    }
-                    out.store(dx + (long long)row * dxs + c);
                 }
             }
         }
     }
     if (!ring.arrived && threadIdx.x == 0) {
-        const long long mine = ((long long)groups - blockIdx.x + gridDim.x - 1) / gridDim.x;
-        ring.drain(it - 1, (int)min(mine, (long long)it + stages - 1));
+        const int mine = (groups - walk.first + walk.stride - 1) / walk.stride;
+        ring.drain(it - 1, min(mine, it + stages - 1));
     }
     if (!partial) return;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (threadIdx.x + i * step) * VEC;
-        if (c < d) {
-            float *a = partial + (long long)blockIdx.x * d + c, *b = a + (long long)gridDim.x * d;
+        float *a = partial + (long long)blockIdx.x * d, *b = a + (long long)gridDim.x * d;
 #pragma unroll
-            for (int k = 0; k < NP; k += 2) {
-                *reinterpret_cast<float4 *>(a + 2 * k) = make_float4(dw[i][k].x, dw[i][k].y, dw[i][k + 1].x, dw[i][k + 1].y);
-                *reinterpret_cast<float4 *>(b + 2 * k) = make_float4(db[i][k].x, db[i][k].y, db[i][k + 1].x, db[i][k + 1].y);
-            }
+        for (int k = 0; k < NP; ++k) {
+            const int c = cols.at(i) + 2 * k;
+            if ((unsigned)c < (unsigned)d) a[c] = dw[i][k].x, b[c] = db[i][k].x;
+            if ((unsigned)(c + 1) < (unsigned)d) a[c + 1] = dw[i][k].y, b[c + 1] = db[i][k].y;
         }
     }
 }
 
-// Rows in registers: a warp per row (rows of at most 32 * kBackElems columns), or, where rows are not 16-byte aligned
-// and longer, a CTA per row.  The next row is loaded while this one is reduced.
-template <typename T, typename P, int VEC, bool WARP>
-__global__ void __launch_bounds__(WARP ? 32 * kBackWarps : kNormBackThreads)
-k_norm_backward(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
-                const P *__restrict__ w, const float *__restrict__ mean, const float *__restrict__ rstd,
-                T *__restrict__ dx, long long dxs, float *__restrict__ partial, long long n, int d, float inv_d)
+// A warp per row, a CTA's warps on rows of one phase; the next row is loaded while this one is reduced; the warps' column
+// sums are joined in order at the end.
+template <bool SHIFT, typename T, typename P>
+__global__ void __launch_bounds__(32 * kBackWarps)
+k_norm_backward_warp(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
+                     const P *__restrict__ w, const float *__restrict__ mean, const float *__restrict__ rstd,
+                     T *__restrict__ dx, long long dxs, float *__restrict__ partial, int n, int d, PhaseRows phases,
+                     float inv_d)
 {
-    constexpr int NV = kBackElems / VEC;
-    __shared__ float2 part[2][32];
-    __shared__ float joined[WARP ? kBackWarps : 1][WARP ? 32 * kBackElems : 1];
-    const int tid = WARP ? (threadIdx.x & 31) : threadIdx.x;
-    const int step = WARP ? 32 : blockDim.x;
-    const long long first = WARP ? (long long)blockIdx.x * kBackWarps + (threadIdx.x >> 5) : (long long)blockIdx.x;
-    const long long stride = WARP ? (long long)gridDim.x * kBackWarps : (long long)gridDim.x;
+    constexpr int V = Pairs<T>::V, NV = kNormElems / V, NP = Pairs<T>::N;
+    __shared__ float joined[kBackWarps][32 * kNormElems];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Walk walk = walk_of<V>(phases, blockIdx.x, gridDim.x, n);  // the CTA's phase, dealt to its warps
+    walk.first = walk.first * kBackWarps + warp;
+    walk.stride *= kBackWarps;
+    const Columns<SHIFT, V, NV> cols(lane, 32, SHIFT ? walk.phase : 0, d, phases.same_out);
     grid_dependency_wait();
     grid_dependency_launch_next();
-    float dw[NV][VEC] = {}, db[NV][VEC] = {};
-    Pack<T, VEC> nx[NV], ng[NV];
+    Pairs<T> nx[NV], ng[NV];
     float nmu = 0.0f, nr = 0.0f;
-    auto fetch = [&](long long row) {
-        if (row >= n) return;
+    auto fetch = [&](int j) {
+        if (j >= walk.count) return;
+        const long long row = walk.row0 + walk.period * j;
+        const bool edge = near_end<V>(row, n, d);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (tid + i * step) * VEC;
-            if (c < d) {
-                nx[i] = load_pack<T, VEC>(x + row * xs + c);
-                ng[i] = load_pack<T, VEC>(dy + row * dys + c);
+        for (int i = 0; i < NV; ++i)
+            if (cols.any(i)) {
+                take(nx[i], cols, i, x + row * xs, edge);
+                take(ng[i], cols, i, dy + row * dys, edge);
             }
-        }
         nmu = mean[row];
         nr = rstd[row];
     };
-    fetch(first);
-    int turn = 0;
-    for (long long row = first; row < n; row += stride, turn ^= 1) {
-        Pack<T, VEC> cx[NV], cg[NV];
+    fetch(walk.first);
+    float2 dw[NV][NP], db[NV][NP], wv[NV][NP];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        load_params<SHIFT, P, NP>(w, cols.at(i), d, 1.0f, wv[i]);
+#pragma unroll
+        for (int k = 0; k < NP; ++k) dw[i][k] = db[i][k] = make_float2(0.0f, 0.0f);
+    }
+    for (int j = walk.first; j < walk.count; j += walk.stride) {
+        Pairs<T> cx[NV], cg[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) cx[i] = nx[i], cg[i] = ng[i];
         const float mu = nmu, r = nr;
-        fetch(row + stride);
-        float s1 = 0.0f, s2 = 0.0f;
+        fetch(j + walk.stride);
+        const float2 m2 = make_float2(-mu, -mu), r2 = make_float2(r, r);
+        BackSums<T> sums = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (tid + i * step) * VEC;
-            if (c < d) {
-                float wv[VEC];
-                if (w) load_param<P, VEC>(w, c, wv);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const float g = to_f32(cg[i].v[j]), xhat = (to_f32(cx[i].v[j]) - mu) * r;
-                    const float gw = w ? g * wv[j] : g;
-                    s1 += gw;
-                    s2 = fmaf(gw, xhat, s2);
-                    dw[i][j] = fmaf(g, xhat, dw[i][j]);
-                    db[i][j] += g;
-                }
-            }
-        }
-        const float2 s = row_sum2<WARP>(s1, s2, part[turn]);
-        const float m1 = s.x * inv_d, m2 = s.y * inv_d;
+        for (int i = 0; i < NV; ++i)
+            if (cols.any(i)) sums.add(cx[i], cg[i], wv[i], m2, r2, dw[i], db[i]);
+        const float c1 = -r * (warp_sum(sums.s1.x + sums.s1.y) * inv_d), c2 = -r * (warp_sum(sums.s2.x + sums.s2.y) * inv_d);
         if (dx) {
+            T *dst = dx + (long long)(walk.row0 + walk.period * j) * dxs;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = (tid + i * step) * VEC;
-                if (c < d) {
-                    float wv[VEC];
-                    if (w) load_param<P, VEC>(w, c, wv);
-                    Pack<T, VEC> out;
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) {
-                        const float g = to_f32(cg[i].v[j]), xhat = (to_f32(cx[i].v[j]) - mu) * r;
-                        const float gw = w ? g * wv[j] : g;
-                        out.v[j] = from_f32<T>(r * (gw - m1 - xhat * m2));
-                    }
-                    *reinterpret_cast<Pack<T, VEC> *>(dx + row * dxs + c) = out;
-                }
-            }
+            for (int i = 0; i < NV; ++i)
+                if (cols.any(i))
+                    input_gradient<T>(cx[i], cg[i], wv[i], m2, r2, make_float2(c1, c1), make_float2(c2, c2))
+                        .store(dst, cols.stored_whole(i), cols.at(i), d);
         }
     }
     if (!partial) return;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         float *dst = partial + ((long long)which * gridDim.x + blockIdx.x) * d;
-        if constexpr (WARP) {  // the CTA's warps first, in order
-            __syncthreads();
+        __syncthreads();
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    joined[threadIdx.x >> 5][(tid + i * 32) * VEC + j] = which ? db[i][j] : dw[i][j];
-            __syncthreads();
-            for (int c = threadIdx.x; c < d; c += 32 * kBackWarps) {
-                float t = joined[0][c];
-#pragma unroll
-                for (int k = 1; k < kBackWarps; ++k) t += joined[k][c];
-                dst[c] = t;
+            for (int k = 0; k < NP; ++k) {
+                const int c = cols.at(i) + 2 * k;
+                const float2 v = which ? db[i][k] : dw[i][k];
+                if ((unsigned)c < (unsigned)d) joined[warp][c] = v.x;
+                if ((unsigned)(c + 1) < (unsigned)d) joined[warp][c + 1] = v.y;
             }
-        } else {
+        __syncthreads();
+        for (int c = threadIdx.x; c < d; c += 32 * kBackWarps) {
+            float t = joined[0][c];
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = (tid + i * step) * VEC;
-                if (c < d) {
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) dst[c + j] = which ? db[i][j] : dw[i][j];
-                }
-            }
+            for (int k = 1; k < kBackWarps; ++k) t += joined[k][c];
+            dst[c] = t;
         }
     }
 }
 
-// Rows longer than a CTA's registers hold: two reads of the row; a second kernel walks the columns.
+// Any layout and width, a value at a time: two reads of the row; a second kernel walks the columns.
 template <typename T, typename P>
-__global__ void __launch_bounds__(kNormMaxThreads)
-k_norm_backward_long(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
-                     const P *__restrict__ w, const float *__restrict__ mean, const float *__restrict__ rstd,
-                     T *__restrict__ dx, long long dxs, int d, float inv_d)
+__global__ void __launch_bounds__(kNormLongThreads)
+k_norm_backward_any(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
+                    const P *__restrict__ w, const float *__restrict__ mean, const float *__restrict__ rstd,
+                    T *__restrict__ dx, long long dxs, int d, float inv_d)
 {
-    __shared__ float2 part[32];
+    __shared__ float part[2][32];
     grid_dependency_wait();
     grid_dependency_launch_next();
     const long long row = blockIdx.x;
@@ -640,20 +796,18 @@ k_norm_backward_long(const T *__restrict__ dy, long long dys, const T *__restric
         s1 += gw;
         s2 = fmaf(gw, (to_f32(x[row * xs + c]) - mu) * r, s2);
     }
-    const float2 s = row_sum2<false>(s1, s2, part);
-    const float m1 = s.x * inv_d, m2 = s.y * inv_d;
+    const float m1 = row_sum<false>(s1, part[0]) * inv_d, m2 = row_sum<false>(s2, part[1]) * inv_d;
     for (int c = threadIdx.x; c < d; c += blockDim.x) {
         const float gw = to_f32(dy[row * dys + c]) * (w ? to_f32(w[c]) : 1.0f);
         dx[row * dxs + c] = from_f32<T>(r * (gw - m1 - (to_f32(x[row * xs + c]) - mu) * r * m2));
     }
 }
-
-// Column sums of long rows: a thread per column, a range of rows per CTA row.
+// ... a thread per column, a range of rows per CTA row
 template <typename T>
 __global__ void __launch_bounds__(256)
-k_norm_columns_long(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
-                    const float *__restrict__ mean, const float *__restrict__ rstd, float *__restrict__ partial,
-                    long long n, int d)
+k_norm_columns_any(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
+                   const float *__restrict__ mean, const float *__restrict__ rstd, float *__restrict__ partial,
+                   long long n, int d)
 {
     grid_dependency_wait();
     grid_dependency_launch_next();
@@ -670,12 +824,12 @@ k_norm_columns_long(const T *__restrict__ dy, long long dys, const T *__restrict
     partial[((long long)gridDim.y + blockIdx.y) * d + c] = db;
 }
 
-// dw[c] = sum over the slots of partial[0][slot][c], db likewise: 32 columns x 8 slot lanes per CTA.
+// dw[c] = sum over the slots of partial[0][slot][c], db likewise: 32 columns x 32 slot lanes per CTA.
 template <typename Q>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 k_norm_param_gradient(const float *__restrict__ partial, int slots, int d, Q *__restrict__ dw, Q *__restrict__ db)
 {
-    __shared__ float sum[8][33];
+    __shared__ float sum[32][33];
     const int lane = threadIdx.x & 31, k = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
     Q *out = blockIdx.y ? db : dw;
@@ -686,47 +840,72 @@ k_norm_param_gradient(const float *__restrict__ partial, int slots, int d, Q *__
     float a[4] = {};
     if (c < d) {
         int i = k;
-        for (; i + 24 < slots; i += 32) {
+        for (; i + 96 < slots; i += 128) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) a[u] += src[(long long)(i + 8 * u) * d];
+            for (int u = 0; u < 4; ++u) a[u] += src[(long long)(i + 32 * u) * d];
         }
-        for (; i < slots; i += 8) a[0] += src[(long long)i * d];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i + 32 * u < slots) a[u] += src[(long long)(i + 32 * u) * d];
     }
     sum[k][lane] = (a[0] + a[1]) + (a[2] + a[3]);
     __syncthreads();
-    if (k == 0 && c < d) {
-        float t = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) t += sum[i][lane];
-        out[c] = from_f32<Q>(t);
-    }
+    const float t = warp_sum(sum[lane][k]);  // a warp per column
+    if (lane == 0 && blockIdx.x * 32 + k < d) out[blockIdx.x * 32 + k] = from_f32<Q>(t);
 }
 
 namespace {
 
-// 16-byte accesses where every row of every operand starts on such a boundary and the width is a whole number of
-// packs.
+// How the rows of a call can be walked: `packs` granules at most, in PhaseRows, if all inputs' rows have the same
+// phases.  The sums' order depends on the inputs' layout alone, the output's decides how it is stored.
 struct NormShape {
-    bool vec;
-    int units, threads;   // packs (or elements) of a row; threads of a CTA that takes one row
+    bool packed, shift;
+    int packs;
+    PhaseRows phases;
+    int threads(int elems, int v) const { return ((packs * v + elems - 1) / elems + 31) / 32 * 32; }
 };
-NormShape norm_shape(int d, int elem, bool aligned, int per_vec, int per_scalar)
+struct Operand {
+    const void *p;
+    long long stride;
+};
+NormShape norm_shape(int d, int elem, std::initializer_list<Operand> inputs, Operand output,
+                     std::initializer_list<const void *> params, long long n)
 {
-    NormShape s{};
-    const int vec = 16 / elem;
-    s.vec = aligned && d % vec == 0;
-    s.units = s.vec ? d / vec : d;
-    const int per = s.vec ? per_vec : per_scalar;
-    s.threads = ((s.units + per - 1) / per + 31) / 32 * 32;
+    const int v = 16 / elem;
+    NormShape s{true, d % v != 0, 0, {1, 0, 0, true}};
+    auto phase = [&](const Operand &o) { return (int)((reinterpret_cast<uintptr_t>(o.p) & 15) / elem); };
+    auto step = [&](const Operand &o) { return n > 1 ? (int)(o.stride & (v - 1)) : 0; };
+    s.phases.phase0 = phase(*inputs.begin());
+    s.phases.step = step(*inputs.begin());
+    for (const Operand &o : inputs)
+        if (phase(o) != s.phases.phase0 || step(o) != s.phases.step) s.packed = false;
+    if (output.p) s.phases.same_out = phase(output) == s.phases.phase0 && step(output) == s.phases.step;
+    while ((s.phases.period * s.phases.step) & (v - 1)) s.phases.period *= 2;
+    const bool shifted = s.phases.phase0 || s.phases.step;
+    s.packs = (d + (shifted ? v - 1 : 0) + v - 1) / v;
+    if (shifted || !s.phases.same_out) s.shift = true;
+    for (const void *p : params)
+        if (!pointer_aligned(p, 16)) s.shift = true;
     return s;
 }
 
-bool rows_aligned(const void *p, long long stride, int elem) { return pointer_aligned(p, 16) && (stride * elem) % 16 == 0; }
+// walkers, a multiple of the period, at most `most` and no more than there are rows for
+unsigned walkers(long long rows, long long most, int period)
+{
+    long long g = rows < most ? rows : most;
+    g = (g + period - 1) / period * period;
+    return (unsigned)g;
+}
 
 // CTAs whose sums of dw and db are added up at the end: what they write and what is read again stays under a tenth of
 // the rows' own traffic (16 bytes per slot and column against 6 per row and column), unless rows are few.
-int norm_slots(long long n) { return (int)(n / 27 > 2 * current_device_sms() ? n / 27 : 2 * current_device_sms()); }
-int norm_slots_max() { return 6 * current_device_sms(); }
+int norm_slots(long long n)
+{
+    const long long few = 2ll * current_device_sms(), most = 6ll * current_device_sms();
+    const long long s = n / 27 > few ? n / 27 : few;
+    return (int)(s < most ? s : most);
+}
+int norm_slots_max() { return 6 * current_device_sms() + 8; }  // rounded up to a period
 
 // Lets `kernel` have the rings' shared memory, once per device (`ready`: a bit per device).
 template <typename K>
@@ -741,155 +920,159 @@ cudaError_t allow_ring(K kernel, std::atomic<uint64_t> &ready)
 }
 
 // CTAs per multiprocessor and stages per ring: as many CTAs as the registers allow and the shared memory holds with three
-// stages each.
+// stages each (`more` bytes per CTA besides); no stages if there is not room for `least`.
 struct RingShape {
     int ctas, stages;
 };
-RingShape ring_shape(int threads, int registers, int stage, int least)
+RingShape ring_shape(int threads, int registers, long long stage, int least, long long more = 0)
 {
     RingShape r{65536 / (registers * threads), 0};
     if (r.ctas > 2048 / threads) r.ctas = 2048 / threads;
     if (r.ctas > 16) r.ctas = 16;
-    while (r.ctas > 1 && kNormRingBytes / r.ctas < 3 * stage) --r.ctas;
+    while (r.ctas > 1 && kNormRingBytes / r.ctas < 3 * stage + more) --r.ctas;
     if (r.ctas < 1) r.ctas = 1;
-    r.stages = kNormRingBytes / r.ctas / stage;
+    r.stages = (int)((kNormRingBytes / r.ctas - more) / stage);
     if (r.stages > kNormMaxStages) r.stages = kNormMaxStages;
     if (r.stages < least) r.stages = 0;
     return r;
 }
 
-template <typename T, typename P, int E>
-cudaError_t forward_ring(RingShape ring, int threads, const T *xp, long long xs, const P *wp, const P *bp, T *yp, long long ys,
-                         float *mean, float *rstd, long long n, int d, float eps, cudaStream_t s)
-{
-    static std::atomic<uint64_t> ready{0};
-    unsigned int *status = nullptr;
-    cudaError_t e = operator_status_ptr(&status);
-    if (e == cudaSuccess) e = allow_ring(k_norm_forward_ring<T, P, E>, ready);
-    if (e != cudaSuccess) return e;
-    const long long most = (long long)ring.ctas * current_device_sms();
-    return launch_chained(k_norm_forward_ring<T, P, E>, (unsigned)(n < most ? n : most), threads,
-                          (size_t)ring.stages * d * sizeof(T), s, 1, xp, xs, wp, bp, yp, ys, mean, rstd, (int)n, d,
-                          1.0f / (float)d, 1.0f / sqrtf((float)d), eps, ring.stages, status);
-}
-
 template <typename T, typename P>
-cudaError_t norm_forward(const void *x, long long xs, const void *w, const void *b, void *y, long long ys, float *mean,
-                         float *rstd, long long n, int d, float eps, cudaStream_t s)
-{
-    constexpr int V = 16 / (int)sizeof(T), E = (int)sizeof(T);
-    const NormShape sh = norm_shape(d, E, rows_aligned(x, xs, E) && rows_aligned(y, ys, E) && pointer_aligned(w, 16) &&
-                                              pointer_aligned(b, 16), 16 / V, kNormScalars);
-    const float inv = 1.0f / (float)d, root = 1.0f / sqrtf((float)d);
-    const T *xp = (const T *)x;
-    const P *wp = (const P *)w, *bp = (const P *)b;
-    T *yp = (T *)y;
-    const unsigned rows = (unsigned)n, groups = (unsigned)((n + kNormWarps - 1) / kNormWarps);
-    if (sh.vec && sh.units <= 32 * kNormVecs)
-        return launch_chained(k_norm_forward<T, P, V, kNormVecs, true>, groups, 32 * kNormWarps, 0, s, 1, xp, xs, wp,
-                              bp, yp, ys, mean, rstd, n, d, inv, root, eps);
-    if (sh.vec) {
-        const int wide = (sh.threads / 2 + 31) / 32 * 32;  // threads that hold twice as many columns
-        if (sh.threads <= kNormRingThreads) {
-            const RingShape ring = ring_shape(sh.threads, 64, d * E, 2);
-            if (ring.stages)
-                return forward_ring<T, P, 16>(ring, sh.threads, xp, xs, wp, bp, yp, ys, mean, rstd, n, d, eps, s);
-        } else if (wide <= kNormRingThreads) {
-            const RingShape ring = ring_shape(wide, 128, d * E, 2);
-            if (ring.stages) return forward_ring<T, P, 32>(ring, wide, xp, xs, wp, bp, yp, ys, mean, rstd, n, d, eps, s);
-        }
-    }
-    if (!sh.vec && sh.units <= 32 * kNormScalars)
-        return launch_chained(k_norm_forward<T, P, 1, kNormScalars, true>, groups, 32 * kNormWarps, 0, s, 1, xp, xs,
-                              wp, bp, yp, ys, mean, rstd, n, d, inv, root, eps);
-    if (!sh.vec && sh.threads <= kNormMaxThreads)
-        return launch_chained(k_norm_forward<T, P, 1, kNormScalars, false>, rows, sh.threads, 0, s, 1, xp, xs, wp, bp, yp,
-                              ys, mean, rstd, n, d, inv, root, eps);
-    return launch_chained(k_norm_forward_long<T, P>, rows, kNormMaxThreads, 0, s, 1, xp, xs, wp, bp, yp, ys, mean, rstd, d,
-                          inv, root, eps);
-}
+struct ForwardArgs {
+    const T *x;
+    long long xs;
+    const P *w, *b;
+    T *y;
+    long long ys;
+    float *mean, *rstd;
+    int n, d;
+    float inv, root, eps;
+    cudaStream_t s;
+};
 
-// Launches the ring kernel with `rows` rows per stage if its shared memory holds two stages at least.
-template <typename T, int E, int ROWS, typename P>
-bool launch_ring(cudaError_t *e, int *slots, int threads, const T *gp, long long dys, const T *xp, long long xs, const P *wp,
-                 const float *mean, const float *rstd, T *dxp, long long dxs, float *part, long long n, int d, float inv,
-                 cudaStream_t s)
+template <bool SHIFT, typename T, typename P, int E>
+bool forward_ring(cudaError_t *e, const ForwardArgs<T, P> &a, const NormShape &sh)
 {
-    const int stage = ROWS * 2 * d * (int)sizeof(T);
-    const RingShape ring = ring_shape(threads, 128, stage, ROWS > 1 ? 3 : 2);
+    const int threads = sh.threads(E, Pairs<T>::V);
+    if (threads > kNormRingThreads) return false;
+    const RingShape ring = ring_shape(threads, E <= 16 ? 64 : 128, 16ll * sh.packs, 2);
     if (!ring.stages) return false;
     static std::atomic<uint64_t> ready{0};
     unsigned int *status = nullptr;
     *e = operator_status_ptr(&status);
-    if (*e == cudaSuccess) *e = allow_ring(k_norm_backward_ring<T, E, ROWS, P>, ready);
+    if (*e == cudaSuccess) *e = allow_ring(k_norm_forward_ring<SHIFT, T, P, E>, ready);
     if (*e != cudaSuccess) return true;
-    long long grid = (n + ROWS - 1) / ROWS, most = (long long)ring.ctas * current_device_sms();
-    if (most > norm_slots(n)) most = norm_slots(n);
-    if (most > norm_slots_max()) most = norm_slots_max();
-    if (grid > most) grid = most;
-    *slots = (int)grid;
-    *e = launch_chained(k_norm_backward_ring<T, E, ROWS, P>, (unsigned)grid, threads, (size_t)ring.stages * stage, s, 1, gp, dys, xp,
-                        xs, wp, mean, rstd, dxp, dxs, part, (int)n, d, inv, ring.stages, status);
+    *e = launch_chained(k_norm_forward_ring<SHIFT, T, P, E>,
+                        walkers(a.n, (long long)ring.ctas * current_device_sms() / sh.phases.period * sh.phases.period,
+                                sh.phases.period),
+                        threads, (size_t)ring.stages * 16 * sh.packs, a.s, 1, a.x, a.xs, a.w, a.b, a.y, a.ys, a.mean, a.rstd, a.n,
+                        a.d, sh.phases, a.inv, a.root, a.eps, ring.stages, 16u * (uint32_t)sh.packs, status);
     return true;
 }
 
-template <typename T, typename P>
-cudaError_t norm_backward(const void *dy, long long dys, const void *x, long long xs, const void *w, const float *mean,
-                          const float *rstd, void *dx, long long dxs, void *dw, void *db, int grad_type, long long n,
-                          int d, float *partial, cudaStream_t s)
+template <bool SHIFT, typename T, typename P>
+bool norm_forward_packed(cudaError_t *e, const ForwardArgs<T, P> &a, const NormShape &sh)
 {
-    constexpr int V = 16 / (int)sizeof(T), E = (int)sizeof(T);
-    const NormShape sh = norm_shape(d, E, rows_aligned(x, xs, E) && rows_aligned(dy, dys, E) &&
-                                              (!dx || rows_aligned(dx, dxs, E)) && pointer_aligned(w, 16),
-                                    kBackElems / V, kBackElems);
-    const float inv = 1.0f / (float)d;
-    const T *xp = (const T *)x, *gp = (const T *)dy;
-    const P *wp = (const P *)w;
-    T *dxp = (T *)dx;
-    float *part = dw || db ? partial : nullptr;
+    if (sh.packs <= 32 * kNormElems / Pairs<T>::V) {
+        // as many warps as fit the device at a time, a row each at least
+        const unsigned g = walkers((a.n + kNormWarps - 1) / kNormWarps, 8ll * current_device_sms(), sh.phases.period);
+        *e = launch_chained(k_norm_forward_warp<SHIFT, T, P>, g, 32 * kNormWarps, 0, a.s, 1, a.x, a.xs, a.w, a.b, a.y, a.ys,
+                            a.mean, a.rstd, a.n, a.d, sh.phases, a.inv, a.root, a.eps);
+        return true;
+    }
+    return forward_ring<SHIFT, T, P, 16>(e, a, sh) || forward_ring<SHIFT, T, P, 32>(e, a, sh);
+}
+
+template <typename T, typename P>
+cudaError_t norm_forward(const ForwardArgs<T, P> &a)
+{
+    const NormShape sh = norm_shape(a.d, (int)sizeof(T), {{a.x, a.xs}}, {a.y, a.ys}, {a.w, a.b}, a.n);
+    cudaError_t e = cudaSuccess;
+    if (sh.packed && (sh.shift ? norm_forward_packed<true>(&e, a, sh) : norm_forward_packed<false>(&e, a, sh))) return e;
+    return launch_chained(k_norm_forward_any<T, P>, (unsigned)a.n, kNormLongThreads, 0, a.s, 1, a.x, a.xs, a.w, a.b, a.y, a.ys,
+                          a.mean, a.rstd, a.d, a.inv, a.root, a.eps);
+}
+
+template <typename T, typename P>
+struct BackwardArgs {
+    const T *dy;
+    long long dys;
+    const T *x;
+    long long xs;
+    const P *w;
+    const float *mean, *rstd;
+    T *dx;
+    long long dxs;
+    float *partial;   // NULL: no dw, no db
+    int n, d;
+    float inv;
+    cudaStream_t s;
+};
+
+template <bool SHIFT, typename T, int E, int ROWS, typename P>
+bool backward_ring(cudaError_t *e, int *slots, const BackwardArgs<T, P> &a, const NormShape &sh)
+{
+    const int threads = sh.threads(E, Pairs<T>::V);
+    if (threads > kNormRingThreads) return false;
+    const uint32_t row = 16u * (uint32_t)sh.packs;
+    const long long weight = E > 16 ? 4ll * E * threads : 0;
+    const RingShape ring = ring_shape(threads, 128, 2ll * ROWS * row, ROWS > 1 ? 3 : 2, weight);
+    if (!ring.stages) return false;
+    static std::atomic<uint64_t> ready{0};
+    unsigned int *status = nullptr;
+    *e = operator_status_ptr(&status);
+    if (*e == cudaSuccess) *e = allow_ring(k_norm_backward_ring<SHIFT, T, E, ROWS, P>, ready);
+    if (*e != cudaSuccess) return true;
+    long long most = (long long)ring.ctas * current_device_sms();
+    if (most > norm_slots(a.n)) most = norm_slots(a.n);
+    *slots = (int)walkers((a.n + ROWS - 1) / ROWS, most / sh.phases.period * sh.phases.period, sh.phases.period);
+    *e = launch_chained(k_norm_backward_ring<SHIFT, T, E, ROWS, P>, (unsigned)*slots, threads,
+                        (size_t)(ring.stages * 2ll * ROWS * row + weight), a.s, 1, a.dy, a.dys, a.x, a.xs, a.w, a.mean, a.rstd,
+                        a.dx, a.dxs, a.partial, a.n, a.d, sh.phases, a.inv, ring.stages, row, status);
+    return true;
+}
+
+template <bool SHIFT, typename T, typename P>
+bool norm_backward_packed(cudaError_t *e, int *slots, const BackwardArgs<T, P> &a, const NormShape &sh)
+{
+    if (sh.packs <= 32 * kNormElems / Pairs<T>::V) {
+        long long most = 3ll * current_device_sms();
+        if (most > norm_slots(a.n)) most = norm_slots(a.n);
+        *slots = (int)walkers((a.n + kBackWarps - 1) / kBackWarps, most, sh.phases.period);
+        *e = launch_chained(k_norm_backward_warp<SHIFT, T, P>, (unsigned)*slots, 32 * kBackWarps, 0, a.s, 1, a.dy, a.dys, a.x, a.xs,
+                            a.w, a.mean, a.rstd, a.dx, a.dxs, a.partial, a.n, a.d, sh.phases, a.inv);
+        return true;
+    }
+    return backward_ring<SHIFT, T, 16, 2, P>(e, slots, a, sh) || backward_ring<SHIFT, T, 16, 1, P>(e, slots, a, sh) ||
+           backward_ring<SHIFT, T, 32, 1, P>(e, slots, a, sh);
+}
+
+template <typename T, typename P>
+cudaError_t norm_backward(const BackwardArgs<T, P> &a, void *dw, void *db, int grad_type)
+{
+    const NormShape sh = norm_shape(a.d, (int)sizeof(T), {{a.x, a.xs}, {a.dy, a.dys}}, {a.dx, a.dxs}, {a.w}, a.n);
     int slots = 0;
     cudaError_t e = cudaSuccess;
-    const int wide = (sh.threads / 2 + 31) / 32 * 32;  // threads that hold twice as many columns
-    if (d <= 32 * kBackElems) {
-        const long long groups = (n + kBackWarps - 1) / kBackWarps, most = 3ll * current_device_sms();
-        long long g = groups < most ? groups : most;
-        if (g > norm_slots(n)) g = norm_slots(n);
-        slots = (int)g;
-        e = sh.vec ? launch_chained(k_norm_backward<T, P, V, true>, (unsigned)g, 32 * kBackWarps, 0, s, 1, gp, dys, xp, xs, wp,
-                                    mean, rstd, dxp, dxs, part, n, d, inv)
-                   : launch_chained(k_norm_backward<T, P, 1, true>, (unsigned)g, 32 * kBackWarps, 0, s, 1, gp, dys, xp, xs, wp,
-                                    mean, rstd, dxp, dxs, part, n, d, inv);
-    } else if (sh.vec && sh.threads <= kNormBackThreads &&
-               launch_ring<T, 16, 2, P>(&e, &slots, sh.threads, gp, dys, xp, xs, wp, mean, rstd, dxp, dxs, part, n, d, inv, s)) {
-    } else if (sh.vec && sh.threads <= kNormBackThreads &&
-               launch_ring<T, 16, 1, P>(&e, &slots, sh.threads, gp, dys, xp, xs, wp, mean, rstd, dxp, dxs, part, n, d, inv, s)) {
-    } else if (sh.vec && wide <= kNormBackThreads &&
-               launch_ring<T, 32, 1, P>(&e, &slots, wide, gp, dys, xp, xs, wp, mean, rstd, dxp, dxs, part, n, d, inv, s)) {
-    } else if (!sh.vec && sh.threads <= kNormBackThreads) {
-        long long most = (long long)(65536 / (128 * sh.threads)) * current_device_sms();
-        if (most > norm_slots(n)) most = norm_slots(n);
-        if (most > norm_slots_max()) most = norm_slots_max();
-        slots = (int)(n < most ? n : most);
-        e = launch_chained(k_norm_backward<T, P, 1, false>, (unsigned)slots, sh.threads, 0, s, 1, gp, dys, xp, xs, wp, mean,
-                           rstd, dxp, dxs, part, n, d, inv);
-    } else {
-        if (dx)
-            e = launch_chained(k_norm_backward_long<T, P>, (unsigned)n, kNormMaxThreads, 0, s, 1, gp, dys, xp, xs, wp,
-                               mean, rstd, dxp, dxs, d, inv);
-        if (e == cudaSuccess && part) {
-            slots = (int)(n < 64 ? n : 64);
-            e = launch_chained(k_norm_columns_long<T>, dim3((unsigned)((d + 255) / 256), (unsigned)slots), 256, 0, s, 1,
-                               gp, dys, xp, xs, mean, rstd, part, n, d);
+    if (!sh.packed ||
+        !(sh.shift ? norm_backward_packed<true>(&e, &slots, a, sh) : norm_backward_packed<false>(&e, &slots, a, sh))) {
+        if (a.dx)
+            e = launch_chained(k_norm_backward_any<T, P>, (unsigned)a.n, kNormLongThreads, 0, a.s, 1, a.dy, a.dys, a.x, a.xs,
+                               a.w, a.mean, a.rstd, a.dx, a.dxs, a.d, a.inv);
+        if (e == cudaSuccess && a.partial) {
+            slots = a.n < 64 ? a.n : 64;
+            e = launch_chained(k_norm_columns_any<T>, dim3((unsigned)((a.d + 255) / 256), (unsigned)slots), 256, 0, a.s, 1,
+                               a.dy, a.dys, a.x, a.xs, a.mean, a.rstd, a.partial, (long long)a.n, a.d);
         }
     }
-    if (e != cudaSuccess || !part) return e;
-    const dim3 grid((unsigned)((d + 31) / 32), 2);
+    if (e != cudaSuccess || !a.partial) return e;
+    const dim3 grid((unsigned)((a.d + 31) / 32), 2);
+    const float *part = a.partial;
     if (grad_type == RSDGC_F32)
-        return launch_chained(k_norm_param_gradient<float>, grid, 256, 0, s, 1, part, slots, d, (float *)dw, (float *)db);
+        return launch_chained(k_norm_param_gradient<float>, grid, 1024, 0, a.s, 1, part, slots, a.d, (float *)dw, (float *)db);
     if (grad_type == RSDGC_BF16)
-        return launch_chained(k_norm_param_gradient<__nv_bfloat16>, grid, 256, 0, s, 1, part, slots, d,
+        return launch_chained(k_norm_param_gradient<__nv_bfloat16>, grid, 1024, 0, a.s, 1, part, slots, a.d,
                               (__nv_bfloat16 *)dw, (__nv_bfloat16 *)db);
-    return launch_chained(k_norm_param_gradient<__half>, grid, 256, 0, s, 1, part, slots, d, (__half *)dw, (__half *)db);
+    return launch_chained(k_norm_param_gradient<__half>, grid, 1024, 0, a.s, 1, part, slots, a.d, (__half *)dw, (__half *)db);
 }
 
 // Element and parameter type of a call: the parameters have the rows' type or binary32.
@@ -906,7 +1089,7 @@ int norm_check(int64_t n, int64_t d, int dtype, int param)
 {
     if (n < 0 || d < 1 || !known_dtype(dtype) || !known_dtype(param)) return RSDGC_ERR_INVALID;
     if (param != dtype && param != RSDGC_F32) return RSDGC_ERR_INVALID;
-    if (n > INT_MAX || d > (1 << 24)) return RSDGC_ERR_CAPACITY;
+    if (n > (1 << 30) || d > (1 << 24)) return RSDGC_ERR_CAPACITY;
     return RSDGC_OK;
 }
 
@@ -918,8 +1101,8 @@ using namespace rsdgc;
 extern "C" int64_t rsdgc_layer_norm_workspace_bytes(int64_t n_rows, int64_t width)
 {
     if (n_rows < 0 || width < 1) return RSDGC_ERR_INVALID;
-    const int64_t slots = norm_slots_max();
-    return 2 * 4 * slots * width;
+    if (n_rows > (1 << 30) || width > (1 << 24)) return RSDGC_ERR_CAPACITY;
+    return 2 * 4 * (int64_t)norm_slots_max() * width;
 }
 
 extern "C" int rsdgc_layer_norm_forward(const void *x_dev, int64_t x_stride, const void *weight_dev,
@@ -938,8 +1121,11 @@ extern "C" int rsdgc_layer_norm_forward(const void *x_dev, int64_t x_stride, con
         return RSDGC_ERR_ALIGNMENT;
     OperatorRange range("rsdgc_layer_norm_forward");
     const cudaError_t e = with_types(dtype, param_dtype, [&](auto t, auto p) {
-        return norm_forward<decltype(t), decltype(p)>(x_dev, x_stride, weight_dev, bias_dev, y_dev, y_stride, mean_dev,
-                                                      rstd_dev, n_rows, (int)width, eps, (cudaStream_t)stream);
+        typedef decltype(t) T;
+        typedef decltype(p) P;
+        return norm_forward<T, P>({(const T *)x_dev, x_stride, (const P *)weight_dev, (const P *)bias_dev, (T *)y_dev, y_stride,
+                                   mean_dev, rstd_dev, (int)n_rows, (int)width, 1.0f / (float)width,
+                                   1.0f / std::sqrt((float)width), eps, (cudaStream_t)stream});
     });
     return operator_result(e);
 }
@@ -978,9 +1164,13 @@ extern "C" int rsdgc_layer_norm_backward(const void *dy_dev, int64_t dy_stride, 
         return operator_result(e);
     }
     const cudaError_t e = with_types(dtype, param_dtype, [&](auto t, auto p) {
-        return norm_backward<decltype(t), decltype(p)>(dy_dev, dy_stride, x_dev, x_stride, weight_dev, mean_dev, rstd_dev,
-                                                       dx_dev, dx_stride, dweight_dev, dbias_dev, grad_dtype, n_rows,
-                                                       (int)width, (float *)workspace_dev, s);
+        typedef decltype(t) T;
+        typedef decltype(p) P;
+        return norm_backward<T, P>({(const T *)dy_dev, dy_stride, (const T *)x_dev, x_stride, (const P *)weight_dev, mean_dev,
+                                    rstd_dev, (T *)dx_dev, dx_stride,
+                                    dweight_dev || dbias_dev ? (float *)workspace_dev : nullptr, (int)n_rows, (int)width,
+                                    1.0f / (float)width, s},
+                                   dweight_dev, dbias_dev, grad_dtype);
     });
     return operator_result(e);
 }
