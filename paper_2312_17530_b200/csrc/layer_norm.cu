@@ -16,6 +16,7 @@
 #include <climits>
 #include <cmath>
 #include <initializer_list>
+#include <type_traits>
 
 #include "device_utils.cuh"
 #include "operators_internal.cuh"
@@ -28,6 +29,7 @@ constexpr int kNormElems = 16;             // columns of a thread (32 in the wid
 constexpr int kNormRingThreads = 512;
 constexpr int kNormLongThreads = 1024;
 constexpr int kNormMaxStages = 4;
+constexpr int kNormMaxTeams = 8;
 constexpr int kNormRingBytes = 200 << 10;  // shared memory of a multiprocessor's rings
 constexpr unsigned kNormSpin = 1u << 20;   // polls of a wait before it gives up
 
@@ -186,24 +188,28 @@ __device__ __forceinline__ Walk walk_of(const PhaseRows &p, int walker, int walk
 }
 
 // The granules of a thread: columns start + i * pitch on.  SHIFT: rows are shifted, or the width is no whole number of
-// granules, or an output's rows lie elsewhere; without it every granule is whole.
+// granules, or an output's rows lie elsewhere; without it every granule that exists is whole.  `fast`: all granules of the
+// whole warp exist and are whole, so that its code (FAST) needs no tests; only a row's first and last warps differ.
 template <bool SHIFT, int V, int NV>
 struct Columns {
     int start, pitch, d;
     unsigned whole_bits, store_bits;
+    bool fast;
     __device__ __forceinline__ Columns(int thread, int threads, int phase, int width, bool same_out)
-        : start(thread * V - phase), pitch(threads * V), d(width), whole_bits(0), store_bits(0)
+        : start(thread * V - phase), pitch(threads * V), d(width), whole_bits(0)
     {
-        if constexpr (SHIFT) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) whole_bits |= (unsigned)(at(i) >= 0 && at(i) + V <= d) << i;
-            store_bits = same_out ? whole_bits : 0u;
-        }
+        for (int i = 0; i < NV; ++i) whole_bits |= (unsigned)(at(i) >= 0 && at(i) + V <= d) << i;
+        store_bits = !SHIFT || same_out ? whole_bits : 0u;
+        fast = __all_sync(0xFFFFFFFFu, store_bits == (1u << NV) - 1u);
     }
     __device__ __forceinline__ int at(int i) const { return start + i * pitch; }
-    __device__ __forceinline__ bool any(int i) const { return at(i) < d; }
-    __device__ __forceinline__ bool whole(int i) const { return !SHIFT || (whole_bits >> i & 1); }
-    __device__ __forceinline__ bool stored_whole(int i) const { return !SHIFT || (store_bits >> i & 1); }
+    template <bool FAST>
+    __device__ __forceinline__ bool any(int i) const { return FAST || at(i) < d; }
+    template <bool FAST>
+    __device__ __forceinline__ bool whole(int i) const { return FAST || !SHIFT || (whole_bits >> i & 1); }
+    template <bool FAST>
+    __device__ __forceinline__ bool stored_whole(int i) const { return FAST || !SHIFT || (store_bits >> i & 1); }
 };
 
 // Sum over the threads of one row: a warp, or the CTA with one slot of `part` per warp (the caller alternates between
@@ -229,7 +235,8 @@ struct RowRing {
     unsigned int *status;
 
     __device__ __forceinline__ uint32_t bar(int i) const { return full + 8 * (i % stages); }
-    __device__ __forceinline__ uint32_t at(int i) const { return base + (i % stages) * stage_bytes; }
+    __device__ __forceinline__ uint32_t offset(int i) const { return (i % stages) * stage_bytes; }
+    __device__ __forceinline__ uint32_t at(int i) const { return base + offset(i); }
     // bounded; after a failure the others poll once
     __device__ __forceinline__ void wait(int i)
     {
@@ -264,19 +271,17 @@ __device__ __forceinline__ RowCopy row_copy(int row, int n, int phase, int d)
     return {(uint32_t)g0 * 16u, g1 > g0 ? (uint32_t)(g1 - g0) * 16u : 0u};
 }
 // Granule i of `row` (column 0) from its copy in shared memory; masked at the row's ends.
-template <bool SHIFT, typename T, int NV>
-__device__ __forceinline__ void take(Pairs<T> &v, const Columns<SHIFT, Pairs<T>::V, NV> &cols, int i, uint32_t copy, int phase,
-                                     const T *row, bool edge)
+template <bool FAST, bool SHIFT, typename T, int NV>
+__device__ __forceinline__ void take(Pairs<T> &v, const Columns<SHIFT, Pairs<T>::V, NV> &cols, int i,
+                                     const unsigned char *copy, int phase, const T *row, bool edge)
 {
     const int c = cols.at(i);
-    if (SHIFT && edge && !cols.whole(i)) {
+    if (edge && !cols.template whole<FAST>(i)) {
         v.load_elements(row, c, cols.d);
         return;
     }
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3])
-                 : "r"(copy + (uint32_t)(c + phase) * (uint32_t)sizeof(T)));
-    if (SHIFT && !cols.whole(i)) v.mask(c, cols.d);
+    v.load(reinterpret_cast<const T *>(copy + (c + phase) * (int)sizeof(T)));
+    if (!cols.template whole<FAST>(i)) v.mask(c, cols.d);
 }
 // Rows whose granules may reach beyond the operand's first or last value (one row at either end unless rows are
 // shorter than a granule).
@@ -286,73 +291,76 @@ __device__ __forceinline__ bool near_end(long long row, int n, int d)
     return row * d < V || (n - 1 - row) * d < V;
 }
 // ... straight from global memory
-template <bool SHIFT, typename T, int NV>
+template <bool FAST, bool SHIFT, typename T, int NV>
 __device__ __forceinline__ void take(Pairs<T> &v, const Columns<SHIFT, Pairs<T>::V, NV> &cols, int i, const T *row, bool edge)
 {
     const int c = cols.at(i);
-    if (SHIFT && edge && !cols.whole(i)) {
+    if (edge && !cols.template whole<FAST>(i)) {
         v.load_elements(row, c, cols.d);
         return;
     }
     v.load(row + c);
-    if (SHIFT && !cols.whole(i)) v.mask(c, cols.d);
+    if (!cols.template whole<FAST>(i)) v.mask(c, cols.d);
 }
 
 // ---- forward ----------------------------------------------------------------------------------
-// The two passes over a row that is in registers.
-template <bool SHIFT, typename T, int NV, bool WARP>
-__device__ __forceinline__ void row_statistics(const Pairs<T> (&in)[NV], const Columns<SHIFT, Pairs<T>::V, NV> &cols, float inv_d,
-                                               float root_inv_d, float eps, float (*part)[32], float *mu, float *r)
+// A thread's share of the passes over a row in registers: the sum, the centred squares (scaled term by term: their sum
+// may leave the range where their mean does not), the output.
+template <bool FAST, bool SHIFT, typename T, int NV>
+__device__ __forceinline__ float sum_of(const Pairs<T> (&in)[NV], const Columns<SHIFT, Pairs<T>::V, NV> &cols)
 {
-    constexpr int NP = Pairs<T>::N;
     float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if (cols.any(i)) {
+        if (cols.template any<FAST>(i)) {
 #pragma unroll
-            for (int k = 0; k < NP; ++k) sum = add2(sum, in[i].get(k));  // masked columns are zero
+            for (int k = 0; k < Pairs<T>::N; ++k) sum = add2(sum, in[i].get(k));  // masked columns are zero
         }
-    *mu = row_sum<WARP>(sum.x + sum.y, part[0]) * inv_d;
-    // the squares are scaled term by term: their sum may leave the range where their mean does not
-    const float2 rr = make_float2(root_inv_d, root_inv_d), m2 = make_float2(-*mu, -*mu);
+    return sum.x + sum.y;
+}
+template <bool FAST, bool SHIFT, typename T, int NV>
+__device__ __forceinline__ float squares_of(const Pairs<T> (&in)[NV], const Columns<SHIFT, Pairs<T>::V, NV> &cols, float mu,
+                                            float root_inv_d)
+{
+    const float2 rr = make_float2(root_inv_d, root_inv_d), m2 = make_float2(-mu, -mu);
     float2 sq = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if (cols.any(i)) {
-            if (cols.whole(i)) {
+        if (cols.template any<FAST>(i)) {
+            const int c = cols.at(i);
+            const bool whole = cols.template whole<FAST>(i);
 #pragma unroll
-                for (int k = 0; k < NP; ++k) {
-                    const float2 e = mul2(add2(in[i].get(k), m2), rr);
-                    sq = fma2(e, e, sq);
-                }
-            } else {
-                const int c = cols.at(i);
-#pragma unroll
-                for (int k = 0; k < NP; ++k) {
-                    float2 e = mul2(add2(in[i].get(k), m2), rr);
+            for (int k = 0; k < Pairs<T>::N; ++k) {
+                float2 e = mul2(add2(in[i].get(k), m2), rr);
+                if (!whole) {
                     e.x = (unsigned)(c + 2 * k) < (unsigned)cols.d ? e.x : 0.0f;
                     e.y = (unsigned)(c + 2 * k + 1) < (unsigned)cols.d ? e.y : 0.0f;
-                    sq = fma2(e, e, sq);
                 }
+                sq = fma2(e, e, sq);
             }
         }
-    *r = rsqrtf(row_sum<WARP>(sq.x + sq.y, part[1]) + eps);
+    return sq.x + sq.y;
 }
-
-template <bool SHIFT, typename T, int NV>
+template <bool FAST, bool SHIFT, typename T, int NV>
 __device__ __forceinline__ void write_row(const Pairs<T> (&in)[NV], T *row, const Columns<SHIFT, Pairs<T>::V, NV> &cols, float mu,
                                           float r, const float2 (*wv)[Pairs<T>::N], const float2 (*bv)[Pairs<T>::N])
 {
     const float2 m2 = make_float2(-mu, -mu), r2 = make_float2(r, r);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        if (cols.any(i)) {
+        if (cols.template any<FAST>(i)) {
             Pairs<T> out;
 #pragma unroll
             for (int k = 0; k < Pairs<T>::N; ++k) out.set(k, fma2(mul2(add2(in[i].get(k), m2), r2), wv[i][k], bv[i][k]));
-            out.store(row, cols.stored_whole(i), cols.at(i), cols.d);
+            out.store(row, cols.template stored_whole<FAST>(i), cols.at(i), cols.d);
         }
     }
+}
+// Both forms of a warp's code: f(std::true_type) where all its granules are whole.
+template <typename F>
+__device__ __forceinline__ void by_warp(bool fast, F f)
+{
+    if (fast) f(std::true_type{}); else f(std::false_type{});
 }
 
 // A CTA per row, rows through the ring; the threads keep their columns' weight and bias as binary32 pairs.  Two barriers
@@ -400,18 +408,24 @@ k_norm_forward_ring(const T *__restrict__ x, long long xs, const P *__restrict__
         const bool edge = row == 0 || row == n - 1;
         ring.wait(it);
         Pairs<T> in[NV];
+        float sum = 0.0f, sq = 0.0f;
+        by_warp(cols.fast, [&](auto fast) {
+            constexpr bool FAST = decltype(fast)::value;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (cols.any(i)) take(in[i], cols, i, ring.at(it), SHIFT ? walk.phase : 0, x + row * xs, edge);
-        }
-        float mu, r;
-        row_statistics<SHIFT, T, NV, false>(in, cols, inv_d, root_inv_d, eps, part, &mu, &r);
+            for (int i = 0; i < NV; ++i)
+                if (cols.template any<FAST>(i))
+                    take<FAST>(in[i], cols, i, rows + ring.offset(it), SHIFT ? walk.phase : 0, x + row * xs, edge);
+            sum = sum_of<FAST>(in, cols);
+        });
+        const float mu = row_sum<false>(sum, part[0]) * inv_d;
+        by_warp(cols.fast, [&](auto fast) { sq = squares_of<decltype(fast)::value>(in, cols, mu, root_inv_d); });
+        const float r = rsqrtf(row_sum<false>(sq, part[1]) + eps);
         if (threadIdx.x == 0) {
             load(it + stages);  // behind the statistics' barriers: every thread has read the stage
             if (mean) mean[row] = mu;
             if (rstd) rstd[row] = r;
         }
-        write_row<SHIFT, T, NV>(in, y + row * ys, cols, mu, r, wv, bv);
+        by_warp(cols.fast, [&](auto fast) { write_row<decltype(fast)::value>(in, y + row * ys, cols, mu, r, wv, bv); });
     }
     if (!ring.arrived && threadIdx.x == 0) {
         const int mine = (walk.count - walk.first + walk.stride - 1) / walk.stride;
@@ -427,7 +441,6 @@ k_norm_forward_warp(const T *__restrict__ x, long long xs, const P *__restrict__
                     PhaseRows phases, float inv_d, float root_inv_d, float eps)
 {
     constexpr int V = Pairs<T>::V, NV = kNormElems / V, NP = Pairs<T>::N;
-    float part[2][32];  // not used: a warp sums by shuffles
     const int lane = threadIdx.x & 31;
     const Walk walk = walk_of<V>(phases, blockIdx.x * kNormWarps + (threadIdx.x >> 5), gridDim.x * kNormWarps, n);
     const Columns<SHIFT, V, NV> cols(lane, 32, SHIFT ? walk.phase : 0, d, phases.same_out);
@@ -436,10 +449,13 @@ k_norm_forward_warp(const T *__restrict__ x, long long xs, const P *__restrict__
     Pairs<T> next[NV];
     auto fetch = [&](int j) {
         const int row = walk.row0 + walk.period * j;
+        if (j >= walk.count) return;
+        by_warp(cols.fast, [&](auto fast) {
+            constexpr bool FAST = decltype(fast)::value;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (j < walk.count && cols.any(i)) take(next[i], cols, i, x + row * xs, near_end<V>(row, n, d));
-        }
+            for (int i = 0; i < NV; ++i)
+                if (cols.template any<FAST>(i)) take<FAST>(next[i], cols, i, x + row * xs, near_end<V>(row, n, d));
+        });
     };
     fetch(walk.first);
     float2 wv[NV][NP], bv[NV][NP];
@@ -454,13 +470,16 @@ k_norm_forward_warp(const T *__restrict__ x, long long xs, const P *__restrict__
 #pragma unroll
         for (int i = 0; i < NV; ++i) in[i] = next[i];
         fetch(j + walk.stride);
-        float mu, r;
-        row_statistics<SHIFT, T, NV, true>(in, cols, inv_d, root_inv_d, eps, part, &mu, &r);
+        float sum = 0.0f, sq = 0.0f;
+        by_warp(cols.fast, [&](auto fast) { sum = sum_of<decltype(fast)::value>(in, cols); });
+        const float mu = warp_sum(sum) * inv_d;
+        by_warp(cols.fast, [&](auto fast) { sq = squares_of<decltype(fast)::value>(in, cols, mu, root_inv_d); });
+        const float r = rsqrtf(warp_sum(sq) + eps);
         if (lane == 0) {
             if (mean) mean[row] = mu;
             if (rstd) rstd[row] = r;
         }
-        write_row<SHIFT, T, NV>(in, y + row * ys, cols, mu, r, wv, bv);
+        by_warp(cols.fast, [&](auto fast) { write_row<decltype(fast)::value>(in, y + row * ys, cols, mu, r, wv, bv); });
     }
 }
 
@@ -529,30 +548,37 @@ __device__ __forceinline__ Pairs<T> input_gradient(const Pairs<T> &vx, const Pai
     return out;
 }
 
-// A CTA per row, ROWS rows of x and dy per stage of the ring.  One barrier per stage: it ends the sums of this stage
-// and, with it, all reads of the one before, which is refilled behind it.  E <= 16: weight, x and dy stay in registers
-// between the two passes; E = 32: x and dy are read again, the weight lies in shared memory in the threads' order.
+// A CTA is made of teams of `team_threads`, each with its own rows, ring and barrier, so that narrow rows still fill the
+// multiprocessor while its columns' sums leave it once.  A team takes ROWS rows of x and dy per stage.  One barrier per
+// stage: it ends the sums of this stage and, with it, all reads of the one before, which is refilled behind it.  E <= 16:
+// weight, x and dy stay in registers between the two passes; E = 32: x and dy are read again, the weight lies in shared
+// memory in the threads' order.
 template <bool SHIFT, typename T, int E, int ROWS, typename P>
 __global__ void __launch_bounds__(kNormRingThreads)
 k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
                      const P *__restrict__ w, const float *__restrict__ mean, const float *__restrict__ rstd,
                      T *__restrict__ dx, long long dxs, float *__restrict__ partial, int n, int d, PhaseRows phases,
-                     float inv_d, int stages, uint32_t row_bytes, unsigned int *status)
+                     float inv_d, int team_threads, int stages, uint32_t row_bytes, unsigned int *status)
 {
     constexpr int V = Pairs<T>::V, NV = E / V, NP = Pairs<T>::N;
     constexpr bool KEEP = E <= 16;
     extern __shared__ __align__(128) unsigned char rows[];
-    __shared__ float2 part[2][ROWS][32];
-    __shared__ __align__(8) unsigned long long full[kNormMaxStages];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const Walk walk = walk_of<V>(phases, blockIdx.x, gridDim.x, n);
+    __shared__ float2 part[2][ROWS][kNormRingThreads / 32];
+    __shared__ __align__(8) unsigned long long full[kNormMaxTeams][kNormMaxStages];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = team_threads >> 5;
+    const int team = threadIdx.x / team_threads, teams = blockDim.x / team_threads, tid = threadIdx.x - team * team_threads;
+    Walk walk = walk_of<V>(phases, blockIdx.x, gridDim.x, n);  // the CTA's phase, dealt to its teams
+    walk.first = walk.first * teams + team;
+    walk.stride *= teams;
     const int groups = (walk.count + ROWS - 1) / ROWS;
-    RowRing ring = {smem_addr(rows), smem_addr(full), ROWS * 2 * row_bytes, stages, true, status};
-    if (threadIdx.x < stages) barrier_init(ring.bar(threadIdx.x), 1);
+    const uint32_t ring_bytes = stages * ROWS * 2 * row_bytes;
+    RowRing ring = {smem_addr(rows) + team * ring_bytes, smem_addr(full[team]), ROWS * 2 * row_bytes, stages, true, status};
+    if (tid < stages) barrier_init(ring.bar(tid), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
     grid_dependency_wait();
     grid_dependency_launch_next();
+    auto team_barrier = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(team_threads) : "memory"); };
     auto row_of = [&](int g, int r) { return walk.row0 + walk.period * (g * ROWS + r); };
     auto load = [&](int i) {  // by one thread
         const int g = walk.first + i * walk.stride;
@@ -575,15 +601,15 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
                       copy[r].bytes, ring.bar(i));
         }
     };
-    if (threadIdx.x == 0)
+    if (tid == 0)
         for (int i = 0; i + 1 < stages; ++i) load(i);
 
-    const Columns<SHIFT, V, NV> cols(threadIdx.x, blockDim.x, SHIFT ? walk.phase : 0, d, phases.same_out);
+    const Columns<SHIFT, V, NV> cols(tid, team_threads, SHIFT ? walk.phase : 0, d, phases.same_out);
     float2 dw[NV][NP], db[NV][NP], wv[KEEP ? NV : 1][NP];
-    float2 *const shared_w = reinterpret_cast<float2 *>(rows + stages * ROWS * 2 * row_bytes);
+    float2 *const shared_w = reinterpret_cast<float2 *>(rows + teams * ring_bytes);  // the teams' columns are the same
     auto weight = [&](int i, float2 *out) {
 #pragma unroll
-        for (int k = 0; k < NP; ++k) out[k] = shared_w[(i * NP + k) * blockDim.x + threadIdx.x];
+        for (int k = 0; k < NP; ++k) out[k] = shared_w[(i * NP + k) * team_threads + tid];
     };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -592,7 +618,7 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
         } else {
             load_params<SHIFT, P, NP>(w, cols.at(i), d, 1.0f, wv[0]);
 #pragma unroll
-            for (int k = 0; k < NP; ++k) shared_w[(i * NP + k) * blockDim.x + threadIdx.x] = wv[0][k];  // read by this thread
+            for (int k = 0; k < NP; ++k) shared_w[(i * NP + k) * team_threads + tid] = wv[0][k];
         }
 #pragma unroll
         for (int k = 0; k < NP; ++k) dw[i][k] = db[i][k] = make_float2(0.0f, 0.0f);
@@ -616,78 +642,101 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
         statistics(g + walk.stride);
         ring.wait(it);
         Pairs<T> px[KEEP ? ROWS : 1][KEEP ? NV : 1], pg[KEEP ? ROWS : 1][KEEP ? NV : 1];
-        auto operands = [&](int r, int i, Pairs<T> &vx, Pairs<T> &vg) {
+        auto operands = [&](auto fast, int r, int i, Pairs<T> &vx, Pairs<T> &vg) {
+            constexpr bool FAST = decltype(fast)::value;
             const long long row = row_of(g, r);
             const bool edge = row == 0 || row == n - 1;
-            const uint32_t copy = ring.at(it) + 2 * r * row_bytes;
-            take(vx, cols, i, copy, SHIFT ? walk.phase : 0, x + row * xs, edge);
-            take(vg, cols, i, copy + row_bytes, SHIFT ? walk.phase : 0, dy + row * dys, edge);
+            const unsigned char *copy = rows + team * ring_bytes + ring.offset(it) + 2 * r * row_bytes;
+            take<FAST>(vx, cols, i, copy, SHIFT ? walk.phase : 0, x + row * xs, edge);
+            take<FAST>(vg, cols, i, copy + row_bytes, SHIFT ? walk.phase : 0, dy + row * dys, edge);
         };
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             const float2 m2 = make_float2(-mu[r], -mu[r]), r2 = make_float2(rs[r], rs[r]);
             BackSums<T> sums = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-            if (g * ROWS + r < walk.count) {
+            if (g * ROWS + r < walk.count)
+                by_warp(cols.fast, [&](auto fast) {
 #pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (cols.any(i)) {
-                        Pairs<T> vx, vg;
-                        operands(r, i, vx, vg);
-                        if constexpr (KEEP) {
-                            px[r][i] = vx, pg[r][i] = vg;
-                            sums.add(vx, vg, wv[i], m2, r2, dw[i], db[i]);
-                        } else {
-                            float2 wl[NP];
-                            weight(i, wl);
-                            sums.add(vx, vg, wl, m2, r2, dw[i], db[i]);
+                    for (int i = 0; i < NV; ++i) {
+                        if (cols.template any<decltype(fast)::value>(i)) {
+                            Pairs<T> vx, vg;
+                            operands(fast, r, i, vx, vg);
+                            if constexpr (KEEP) {
+                                px[r][i] = vx, pg[r][i] = vg;
+                                sums.add(vx, vg, wv[i], m2, r2, dw[i], db[i]);
+                            } else {
+                                float2 wl[NP];
+                                weight(i, wl);
+                                sums.add(vx, vg, wl, m2, r2, dw[i], db[i]);
+                            }
                         }
                     }
-                }
-            }
+                });
             const float a = warp_sum(sums.s1.x + sums.s1.y), b = warp_sum(sums.s2.x + sums.s2.y);
             if (lane == 0) part[turn][r][warp] = make_float2(a, b);
         }
-        __syncthreads();
-        if (threadIdx.x == 0) load(it + stages - 1);
+        team_barrier();
+        if (tid == 0) load(it + stages - 1);
         if (!dx) continue;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             if (g * ROWS + r >= walk.count) break;
-            const float2 t = lane < warps ? part[turn][r][lane] : make_float2(0.0f, 0.0f);
+            const float2 t = lane < warps ? part[turn][r][team * warps + lane] : make_float2(0.0f, 0.0f);
             const float c1 = -rs[r] * (warp_sum(t.x) * inv_d), c2 = -rs[r] * (warp_sum(t.y) * inv_d);
             const float2 m2 = make_float2(-mu[r], -mu[r]), r2 = make_float2(rs[r], rs[r]), f1 = make_float2(c1, c1),
                          f2 = make_float2(c2, c2);
             T *dst = dx + (long long)row_of(g, r) * dxs;
+            by_warp(cols.fast, [&](auto fast) {
+                constexpr bool FAST = decltype(fast)::value;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (cols.any(i)) {
-                    if constexpr (KEEP) {
-                        input_gradient<T>(px[r][i], pg[r][i], wv[i], m2, r2, f1, f2)
-                            .store(dst, cols.stored_whole(i), cols.at(i), d);
-                    } else {
-                        Pairs<T> vx, vg;
-                        float2 wl[NP];
-                        operands(r, i, vx, vg);
-                        weight(i, wl);
-                        input_gradient<T>(vx, vg, wl, m2, r2, f1, f2).store(dst, cols.stored_whole(i), cols.at(i), d);
+                for (int i = 0; i < NV; ++i) {
+                    if (cols.template any<FAST>(i)) {
+                        Pairs<T> out;
+                        if constexpr (KEEP) {
+                            out = input_gradient<T>(px[r][i], pg[r][i], wv[i], m2, r2, f1, f2);
+                        } else {
+                            Pairs<T> vx, vg;
+                            float2 wl[NP];
+                            operands(fast, r, i, vx, vg);
+                            weight(i, wl);
+                            out = input_gradient<T>(vx, vg, wl, m2, r2, f1, f2);
+                        }
+                        out.store(dst, cols.template stored_whole<FAST>(i), cols.at(i), d);
                     }
                 }
-            }
+            });
         }
     }
-    if (!ring.arrived && threadIdx.x == 0) {
+    if (!ring.arrived && tid == 0) {
         const int mine = (groups - walk.first + walk.stride - 1) / walk.stride;
         ring.drain(it - 1, min(mine, it + stages - 1));
     }
     if (!partial) return;
+    // The teams' sums are added up, the last team's first, in the rings' memory (everything has arrived and been read): value
+    // e of a thread's granules at [e][thread], 4 words of padding, so that neither the threads nor the columns' order
+    // meets a bank conflict.
+    float *const joined = reinterpret_cast<float *>(rows);
+    const int across = team_threads + 4;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        float *a = partial + (long long)blockIdx.x * d, *b = a + (long long)gridDim.x * d;
+    for (int which = 0; which < 2; ++which) {
+        for (int turn = teams - 1; turn >= 0; --turn) {
+            __syncthreads();
+            if (team != turn) continue;
 #pragma unroll
-        for (int k = 0; k < NP; ++k) {
-            const int c = cols.at(i) + 2 * k;
-            if ((unsigned)c < (unsigned)d) a[c] = dw[i][k].x, b[c] = db[i][k].x;
-            if ((unsigned)(c + 1) < (unsigned)d) a[c + 1] = dw[i][k].y, b[c + 1] = db[i][k].y;
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < NP; ++k) {
+                    const float2 v = which ? db[i][k] : dw[i][k];
+                    float *x = joined + (i * V + 2 * k) * across + tid, *y = x + across;
+                    *x = turn < teams - 1 ? *x + v.x : v.x;
+                    *y = turn < teams - 1 ? *y + v.y : v.y;
+                }
+        }
+        __syncthreads();
+        float *dst = partial + ((long long)which * gridDim.x + blockIdx.x) * d;
+        for (int c = threadIdx.x; c < d; c += blockDim.x) {
+            const int at = c + (SHIFT ? walk.phase : 0), granule = at / V, i = granule / team_threads;
+            dst[c] = joined[(i * V + at % V) * across + granule - i * team_threads];
         }
     }
 }
@@ -716,12 +765,15 @@ k_norm_backward_warp(const T *__restrict__ dy, long long dys, const T *__restric
         if (j >= walk.count) return;
         const long long row = walk.row0 + walk.period * j;
         const bool edge = near_end<V>(row, n, d);
+        by_warp(cols.fast, [&](auto fast) {
+            constexpr bool FAST = decltype(fast)::value;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (cols.any(i)) {
-                take(nx[i], cols, i, x + row * xs, edge);
-                take(ng[i], cols, i, dy + row * dys, edge);
-            }
+            for (int i = 0; i < NV; ++i)
+                if (cols.template any<FAST>(i)) {
+                    take<FAST>(nx[i], cols, i, x + row * xs, edge);
+                    take<FAST>(ng[i], cols, i, dy + row * dys, edge);
+                }
+        });
         nmu = mean[row];
         nr = rstd[row];
     };
@@ -741,17 +793,22 @@ k_norm_backward_warp(const T *__restrict__ dy, long long dys, const T *__restric
         fetch(j + walk.stride);
         const float2 m2 = make_float2(-mu, -mu), r2 = make_float2(r, r);
         BackSums<T> sums = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+        by_warp(cols.fast, [&](auto fast) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (cols.any(i)) sums.add(cx[i], cg[i], wv[i], m2, r2, dw[i], db[i]);
+            for (int i = 0; i < NV; ++i)
+                if (cols.template any<decltype(fast)::value>(i)) sums.add(cx[i], cg[i], wv[i], m2, r2, dw[i], db[i]);
+        });
         const float c1 = -r * (warp_sum(sums.s1.x + sums.s1.y) * inv_d), c2 = -r * (warp_sum(sums.s2.x + sums.s2.y) * inv_d);
         if (dx) {
             T *dst = dx + (long long)(walk.row0 + walk.period * j) * dxs;
+            by_warp(cols.fast, [&](auto fast) {
+                constexpr bool FAST = decltype(fast)::value;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (cols.any(i))
-                    input_gradient<T>(cx[i], cg[i], wv[i], m2, r2, make_float2(c1, c1), make_float2(c2, c2))
-                        .store(dst, cols.stored_whole(i), cols.at(i), d);
+                for (int i = 0; i < NV; ++i)
+                    if (cols.template any<FAST>(i))
+                        input_gradient<T>(cx[i], cg[i], wv[i], m2, r2, make_float2(c1, c1), make_float2(c2, c2))
+                            .store(dst, cols.template stored_whole<FAST>(i), cols.at(i), d);
+            });
         }
     }
     if (!partial) return;
@@ -824,13 +881,13 @@ k_norm_columns_any(const T *__restrict__ dy, long long dys, const T *__restrict_
     partial[((long long)gridDim.y + blockIdx.y) * d + c] = db;
 }
 
-// dw[c] = sum over the slots of partial[0][slot][c], db likewise: 32 columns x 32 slot lanes per CTA.
+// dw[c] = sum over the slots of partial[0][slot][c], db likewise: 32 columns x blockDim.x / 32 slot lanes per CTA.
 template <typename Q>
 __global__ void __launch_bounds__(1024)
 k_norm_param_gradient(const float *__restrict__ partial, int slots, int d, Q *__restrict__ dw, Q *__restrict__ db)
 {
     __shared__ float sum[32][33];
-    const int lane = threadIdx.x & 31, k = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, k = threadIdx.x >> 5, lanes = blockDim.x >> 5;
     const int c = blockIdx.x * 32 + lane;
     Q *out = blockIdx.y ? db : dw;
     grid_dependency_wait();
@@ -839,19 +896,18 @@ k_norm_param_gradient(const float *__restrict__ partial, int slots, int d, Q *__
     const float *src = partial + (long long)blockIdx.y * slots * d + c;
     float a[4] = {};
     if (c < d) {
-        int i = k;
-        for (; i + 96 < slots; i += 128) {
+        for (int i = k; i < slots; i += 4 * lanes) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) a[u] += src[(long long)(i + 32 * u) * d];
+            for (int u = 0; u < 4; ++u)
+                if (i + u * lanes < slots) a[u] += src[(long long)(i + u * lanes) * d];
         }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (i + 32 * u < slots) a[u] += src[(long long)(i + 32 * u) * d];
     }
     sum[k][lane] = (a[0] + a[1]) + (a[2] + a[3]);
     __syncthreads();
-    const float t = warp_sum(sum[lane][k]);  // a warp per column
-    if (lane == 0 && blockIdx.x * 32 + k < d) out[blockIdx.x * 32 + k] = from_f32<Q>(t);
+    if (k || c >= d) return;
+    float t = sum[0][lane];
+    for (int i = 1; i < lanes; ++i) t += sum[i][lane];
+    out[c] = from_f32<Q>(t);
 }
 
 namespace {
@@ -1009,27 +1065,44 @@ struct BackwardArgs {
     cudaStream_t s;
 };
 
-template <bool SHIFT, typename T, int E, int ROWS, typename P>
-bool backward_ring(cudaError_t *e, int *slots, const BackwardArgs<T, P> &a, const NormShape &sh)
+// Teams of the backward ring: as many as the registers (128 a thread) and the shared memory hold, unless rows are so few
+// that they rather spread over the device.
+struct TeamShape {
+    int threads, teams, stages;
+    int warps() const { return threads / 32 * teams; }
+};
+template <typename T>
+TeamShape team_shape(const NormShape &sh, int elems, int rows, long long n)
 {
-    const int threads = sh.threads(E, Pairs<T>::V);
-    if (threads > kNormRingThreads) return false;
+    TeamShape t{sh.threads(elems, Pairs<T>::V), 0, 0};
+    if (t.threads > kNormRingThreads) return t;
+    const long long stage = 2ll * rows * 16 * sh.packs, weight = elems > 16 ? 4ll * elems * t.threads : 0;
+    const long long groups = (n + rows - 1) / rows, share = groups / current_device_sms();
+    t.teams = kNormRingThreads / t.threads;
+    if (t.teams > kNormMaxTeams) t.teams = kNormMaxTeams;
+    if (t.teams > share) t.teams = share > 1 ? (int)share : 1;
+    while (t.teams > 1 && (kNormRingBytes - weight) / t.teams < 3 * stage) --t.teams;
+    t.stages = (int)((kNormRingBytes - weight) / t.teams / stage);
+    if (t.stages > kNormMaxStages) t.stages = kNormMaxStages;
+    if (t.stages < (rows > 1 ? 3 : 2)) t.teams = 0;
+    return t;
+}
+
+template <bool SHIFT, typename T, int E, int ROWS, typename P>
+cudaError_t backward_ring(int *slots, const BackwardArgs<T, P> &a, const NormShape &sh, const TeamShape &t)
+{
     const uint32_t row = 16u * (uint32_t)sh.packs;
-    const long long weight = E > 16 ? 4ll * E * threads : 0;
-    const RingShape ring = ring_shape(threads, 128, 2ll * ROWS * row, ROWS > 1 ? 3 : 2, weight);
-    if (!ring.stages) return false;
+    const long long smem = (long long)t.teams * t.stages * 2 * ROWS * row + (E > 16 ? 4ll * E * t.threads : 0);
     static std::atomic<uint64_t> ready{0};
     unsigned int *status = nullptr;
-    *e = operator_status_ptr(&status);
-    if (*e == cudaSuccess) *e = allow_ring(k_norm_backward_ring<SHIFT, T, E, ROWS, P>, ready);
-    if (*e != cudaSuccess) return true;
-    long long most = (long long)ring.ctas * current_device_sms();
-    if (most > norm_slots(a.n)) most = norm_slots(a.n);
-    *slots = (int)walkers((a.n + ROWS - 1) / ROWS, most / sh.phases.period * sh.phases.period, sh.phases.period);
-    *e = launch_chained(k_norm_backward_ring<SHIFT, T, E, ROWS, P>, (unsigned)*slots, threads,
-                        (size_t)(ring.stages * 2ll * ROWS * row + weight), a.s, 1, a.dy, a.dys, a.x, a.xs, a.w, a.mean, a.rstd,
-                        a.dx, a.dxs, a.partial, a.n, a.d, sh.phases, a.inv, ring.stages, row, status);
-    return true;
+    cudaError_t e = operator_status_ptr(&status);
+    if (e == cudaSuccess) e = allow_ring(k_norm_backward_ring<SHIFT, T, E, ROWS, P>, ready);
+    if (e != cudaSuccess) return e;
+    const int per = ROWS * t.teams;
+    *slots = (int)walkers((a.n + per - 1) / per, current_device_sms() / sh.phases.period * sh.phases.period, sh.phases.period);
+    return launch_chained(k_norm_backward_ring<SHIFT, T, E, ROWS, P>, (unsigned)*slots, t.threads * t.teams, (size_t)smem, a.s, 1,
+                          a.dy, a.dys, a.x, a.xs, a.w, a.mean, a.rstd, a.dx, a.dxs, a.partial, a.n, a.d, sh.phases, a.inv,
+                          t.threads, t.stages, row, status);
 }
 
 template <bool SHIFT, typename T, typename P>
@@ -1043,8 +1116,16 @@ bool norm_backward_packed(cudaError_t *e, int *slots, const BackwardArgs<T, P> &
                             a.w, a.mean, a.rstd, a.dx, a.dxs, a.partial, a.n, a.d, sh.phases, a.inv);
         return true;
     }
-    return backward_ring<SHIFT, T, 16, 2, P>(e, slots, a, sh) || backward_ring<SHIFT, T, 16, 1, P>(e, slots, a, sh) ||
-           backward_ring<SHIFT, T, 32, 1, P>(e, slots, a, sh);
+    // two rows per stage where they fit; twice the columns per thread where that fills the multiprocessor better (a row
+    // of 4100 columns takes 9 of its 16 warps, or three rows 15)
+    const TeamShape two = team_shape<T>(sh, 16, 2, a.n), one = team_shape<T>(sh, 16, 1, a.n), wide = team_shape<T>(sh, 32, 1, a.n);
+    const TeamShape &narrow = two.teams ? two : one;
+    if (narrow.teams && 3 * wide.warps() < 4 * narrow.warps()) {
+        *e = two.teams ? backward_ring<SHIFT, T, 16, 2, P>(slots, a, sh, two) : backward_ring<SHIFT, T, 16, 1, P>(slots, a, sh, one);
+        return true;
+    }
+    if (wide.teams) *e = backward_ring<SHIFT, T, 32, 1, P>(slots, a, sh, wide);
+    return wide.teams > 0;
 }
 
 template <typename T, typename P>
@@ -1066,13 +1147,14 @@ cudaError_t norm_backward(const BackwardArgs<T, P> &a, void *dw, void *db, int g
     }
     if (e != cudaSuccess || !a.partial) return e;
     const dim3 grid((unsigned)((a.d + 31) / 32), 2);
+    const int lanes = slots >= 128 ? 16 : slots >= 16 ? 8 : 1;
     const float *part = a.partial;
     if (grad_type == RSDGC_F32)
-        return launch_chained(k_norm_param_gradient<float>, grid, 1024, 0, a.s, 1, part, slots, a.d, (float *)dw, (float *)db);
+        return launch_chained(k_norm_param_gradient<float>, grid, 32 * lanes, 0, a.s, 1, part, slots, a.d, (float *)dw, (float *)db);
     if (grad_type == RSDGC_BF16)
-        return launch_chained(k_norm_param_gradient<__nv_bfloat16>, grid, 1024, 0, a.s, 1, part, slots, a.d,
+        return launch_chained(k_norm_param_gradient<__nv_bfloat16>, grid, 32 * lanes, 0, a.s, 1, part, slots, a.d,
                               (__nv_bfloat16 *)dw, (__nv_bfloat16 *)db);
-    return launch_chained(k_norm_param_gradient<__half>, grid, 1024, 0, a.s, 1, part, slots, a.d, (__half *)dw, (__half *)db);
+    return launch_chained(k_norm_param_gradient<__half>, grid, 32 * lanes, 0, a.s, 1, part, slots, a.d, (__half *)dw, (__half *)db);
 }
 
 // Element and parameter type of a call: the parameters have the rows' type or binary32.
