@@ -7,6 +7,7 @@ CPU fallback: if the shared library is missing, :func:`lib` raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import List, Optional, Sequence, Tuple
 
@@ -382,7 +383,7 @@ def _on_device(*tensors) -> int:
 
 def _rows(t, n: int, d: int, what: str) -> int:
     """Row stride of an n x d matrix whose rows are contiguous."""
-    if t.dim() != 2 or t.size(0) != n or t.size(1) != d:
+    if t.shape != (n, d):
         raise ValueError("%s: a %d x %d matrix is wanted, got %s" % (what, n, d, tuple(t.shape)))
     row, col = t.stride()
     if col != 1 and d > 1:
@@ -394,9 +395,9 @@ def _vector(t, n: int, dtype, what: str) -> Optional[int]:
     """Address of n contiguous values (of `dtype`, where one is given), or None."""
     if t is None:
         return None
-    if t.dim() != 1 or t.size(0) != n or (n > 1 and t.stride(0) != 1):
+    if t.numel() != n or t.dim() != 1 or not t.is_contiguous():
         raise ValueError("%s: %d contiguous values are wanted, got %s" % (what, n, tuple(t.shape)))
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise ValueError("%s: %s is wanted, got %s" % (what, dtype, t.dtype))
     return t.data_ptr()
 
@@ -407,6 +408,7 @@ def _holds(workspace, size: int) -> int:
     return workspace.data_ptr()
 
 
+@functools.lru_cache(maxsize=4096)
 def layer_norm_workspace_bytes(n_rows: int, width: int) -> int:
     """Bytes of workspace layer_norm_backward() needs for a weight's or bias's gradient."""
     return _size(lib().rsdgc_layer_norm_workspace_bytes(n_rows, width), "rsdgc_layer_norm_workspace_bytes")
@@ -458,6 +460,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=
         _check(code, "rsdgc_layer_norm_backward")
 
 
+@functools.lru_cache(maxsize=4096)
 def head_workspace_bytes(n_tokens: int, vocab: int, width: int, n_targets: int = 1) -> int:
     """Bytes of workspace (256-byte aligned) that the calls on a vocabulary head need; ``n_targets``: entries of the
     teacher per token (1 for labels)."""
@@ -468,7 +471,7 @@ def _head_args(hidden, weight, workspace, n_targets: int):
     """(n, v, d, hidden stride, weight stride, type, workspace's address) of a vocabulary head, after the checks that all
     its calls share."""
     n, d = hidden.shape
-    v = weight.size(0)
+    v = weight.shape[0]
     if weight.dtype != hidden.dtype:
         raise ValueError("weight: %s is wanted, got %s" % (hidden.dtype, weight.dtype))
     hs, ws = _rows(hidden, n, d, "hidden"), _rows(weight, v, d, "weight")
@@ -481,8 +484,8 @@ def _head_grads(hidden, weight, dhidden, dweight):
     """(dhidden's stride, dweight's stride, dweight's type)"""
     if dhidden.dtype != hidden.dtype:
         raise ValueError("dhidden: %s is wanted, got %s" % (hidden.dtype, dhidden.dtype))
-    d = hidden.size(1)
-    return _rows(dhidden, hidden.size(0), d, "dhidden"), _rows(dweight, weight.size(0), d, "dweight"), _dtype_code(dweight)
+    n, d = hidden.shape
+    return _rows(dhidden, n, d, "dhidden"), _rows(dweight, weight.shape[0], d, "dweight"), _dtype_code(dweight)
 
 
 def _matrix(t, what: str) -> None:
@@ -530,7 +533,7 @@ def _top_args(top_index, top_logit, n: int):
     _matrix(top_index, "top_index")
     if top_index.dtype != _tt().i64:
         raise ValueError("top_index: int64 is wanted, got %s" % top_index.dtype)
-    k = top_index.size(1)
+    k = top_index.shape[1]
     return k, _rows(top_index, n, k, "top_index"), _rows(top_logit, n, k, "top_logit"), _dtype_code(top_logit)
 
 
@@ -540,7 +543,7 @@ def head_distill_forward(hidden, weight, top_index, top_logit, temperature: floa
     ``weight``.T, both at temperature T; ``lse`` = log-sum-exp of the student's logits / T."""
     _matrix(hidden, "hidden")
     stream = _on_device(hidden, weight, workspace, top_index, top_logit, loss, lse)
-    k, istride, lstride, tcode = _top_args(top_index, top_logit, hidden.size(0))
+    k, istride, lstride, tcode = _top_args(top_index, top_logit, hidden.shape[0])
     n, v, d, hs, ws, code, space = _head_args(hidden, weight, workspace, k)
     f32 = _torch.f32
     code = lib().rsdgc_head_distill_forward(hidden.data_ptr(), hs, weight.data_ptr(), ws, top_index.data_ptr(), istride,
@@ -556,7 +559,7 @@ def head_distill_backward(hidden, weight, top_index, top_logit, temperature: flo
     """Gradients of head_distill_forward(), as head_loss_backward() gives them."""
     _matrix(hidden, "hidden")
     stream = _on_device(hidden, weight, workspace, top_index, top_logit, lse, grad_loss, dhidden, dweight)
-    k, istride, lstride, tcode = _top_args(top_index, top_logit, hidden.size(0))
+    k, istride, lstride, tcode = _top_args(top_index, top_logit, hidden.shape[0])
     n, v, d, hs, ws, code, space = _head_args(hidden, weight, workspace, k)
     dhs, dws, dwt = _head_grads(hidden, weight, dhidden, dweight)
     f32 = _torch.f32
