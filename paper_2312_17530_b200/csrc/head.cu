@@ -8,14 +8,14 @@
 //
 // Both losses are the same computation: a target distribution with k entries per row.  Three matrix products
 // carry it, all by one persistent kernel (k_head) that differs only in what it does with a finished tile:
-//   forward   z tile -> per row and 128 columns the maximum and the sum of exponentials, and z at the targets
+//   forward   z tile -> per row and 256 columns the maximum and the sum of exponentials, and z at the targets
 //   backward  z tile again (recomputed) -> dz of one piece of the vocabulary, 16 bits, in the workspace
 //             dz W_piece -> added to dh;  dz^T h -> the piece's rows of dW
 // A piece is as wide as keeps dz in the L2 cache between its writer and its two readers.
 //
 // The tile kernel: pairs of CTAs (cluster of 2) compute 256 x 256 tiles with tcgen05.mma.cta_group::2, K in steps
 // of 64; each CTA loads its 128 rows of either operand by TMA (128-byte swizzle) through a ring of kStages
-// stages, the accumulators of two tiles alternate in the 512 TMEM columns, so that eight warps empty one while
+// stages, the accumulators of two tiles alternate in the 512 TMEM columns, so that sixteen warps empty one while
 // the other is filled.  Operands whose contraction index is not the contiguous one (W in dz W, both in dz^T h)
 // are read as they lie in memory: the MMA takes them as MN-major.
 #include <cuda.h>
@@ -39,9 +39,10 @@ constexpr int kBoxBytes = 64 * kStepK * 2;
 constexpr int kBlockBytes = 2 * kBoxBytes;
 constexpr int kRingBlocks = 12;     // of A and B blocks: 4 stages of 1 + 2 blocks, or 6 stages of 1 + 1
 constexpr int kMaxStages = kRingBlocks / 2;
-constexpr int kEpilogueWarps = 8;
+constexpr int kEpilogueWarps = 16;                       // four per quarter of an accumulator's columns
+constexpr int kQuarter = 64;
 constexpr int kHeadThreads = 128 + 32 * kEpilogueWarps;  // producer, MMA, two idle warps, epilogue
-constexpr int kStagingBytes = 4096;  // per epilogue warp: 32 rows of 128 bytes on their way out
+constexpr int kStagingBytes = 2048;  // per epilogue warp: 32 rows of 64 bytes on their way out
 constexpr int kHeadSmem = kRingBlocks * kBlockBytes + kEpilogueWarps * kStagingBytes + 1024;
 constexpr int kSlots = 4;                                // tiles announced ahead
 constexpr unsigned kHeadSpin = 1u << 20;                 // polls of a wait before it gives up
@@ -55,7 +56,7 @@ enum { kForward = 0, kLogitGrad = 1, kHiddenGrad = 2, kWeightGrad = 3 };
 enum { kOut16 = 0, kOutF32 = 1, kOutAddF32 = 2 };
 
 struct __align__(64) HeadJob {
-    CUtensorMap a, b, out;   // out: boxes of 32 rows x 128 bytes
+    CUtensorMap a, b, out;   // out: boxes of 32 rows x 64 bytes
     int a_mn, b_mn;          // the operand lies with its rows (not k) contiguous
     int m_tiles, n_tiles, k_steps, band;
     int halves;              // accumulators of a tile: 256 x 256 or 256 x 512
@@ -80,7 +81,7 @@ struct HeadParams {
     const float *target_q;
     int k;
     // forward
-    float2 *partial;         // [2 * columns / 256][n]: (maximum in log2 units, sum)
+    float2 *partial;         // [columns / 256][n]: (maximum in log2 units, sum)
     int parts;
     float *target_z;         // [n][max(k, 1)]
     // gradients
@@ -309,35 +310,35 @@ struct Targets {
     }
 };
 
-// A warp's 32 rows x 128 bytes on their way to global memory: staged in shared memory in the 128-byte swizzle (the
-// 16-byte piece c of row r lies at c ^ (r & 7), so neither side meets a bank conflict), then one bulk store per box.
+// A warp's 32 rows x 64 bytes on their way to global memory: staged in shared memory in the 64-byte swizzle (the
+// 16-byte piece c of row r lies at c ^ (r / 2 & 3), so neither side meets a bank conflict), then one bulk store per box.
 // Stores straight from the rows' registers take 1.6 cycles per 16 bytes of a row, 6700 cycles per 128 x 256 accumulator.
 template <typename T>
 struct RowsOut {
     uint32_t buf;
     int lane;
-    // 32 columns as part `part` (0, 1) of a 64-column box of 16-bit values
-    __device__ __forceinline__ void put16(int part, const float (&z)[32]) const
+    __device__ __forceinline__ uint32_t piece(int i) const { return buf + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4); }
+    __device__ __forceinline__ void put16(const float (&z)[32]) const  // 32 columns
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            store_shared16(buf + lane * 128 + (((part * 4 + i) ^ (lane & 7)) << 4), pack2<T>(z[8 * i], z[8 * i + 1]),
-                           pack2<T>(z[8 * i + 2], z[8 * i + 3]), pack2<T>(z[8 * i + 4], z[8 * i + 5]),
-                           pack2<T>(z[8 * i + 6], z[8 * i + 7]));
+            store_shared16(piece(i), pack2<T>(z[8 * i], z[8 * i + 1]), pack2<T>(z[8 * i + 2], z[8 * i + 3]),
+                           pack2<T>(z[8 * i + 4], z[8 * i + 5]), pack2<T>(z[8 * i + 6], z[8 * i + 7]));
     }
-    __device__ __forceinline__ void put32(const float (&z)[32]) const
+    template <int PART>
+    __device__ __forceinline__ void put32(const float (&z)[32]) const  // columns 16 PART .. 16 PART + 15
     {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            store_shared16(buf + lane * 128 + ((i ^ (lane & 7)) << 4), __float_as_uint(z[4 * i]), __float_as_uint(z[4 * i + 1]),
-                           __float_as_uint(z[4 * i + 2]), __float_as_uint(z[4 * i + 3]));
+        for (int i = 0; i < 4; ++i)
+            store_shared16(piece(i), __float_as_uint(z[16 * PART + 4 * i]), __float_as_uint(z[16 * PART + 4 * i + 1]),
+                           __float_as_uint(z[16 * PART + 4 * i + 2]), __float_as_uint(z[16 * PART + 4 * i + 3]));
     }
     __device__ __forceinline__ void wait_free() const  // the last box has left the buffer
     {
         if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
         __syncwarp();
     }
-    // row0, col: of the box in C; count: columns of a box
+    // row0, col: of the box in C
     __device__ __forceinline__ void flush(const HeadJob &j, int row0, int col, int split) const
     {
         if (!j.out_plain) {
@@ -354,24 +355,23 @@ struct RowsOut {
         }
         __syncwarp();
         const int rows = min(32, j.out_rows - row0);
-        for (int r = 0; r < rows; ++r) {
-            if (j.out_mode == kOut16) {
-                uint16_t *dst = (uint16_t *)j.out_ptr + (long long)(row0 + r) * j.out_stride + col;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int c = lane + 32 * h;
-                    uint16_t v;
-                    asm volatile("ld.shared.u16 %0, [%1];"
-                                 : "=h"(v)
-                                 : "r"(buf + r * 128 + (((c >> 3) ^ (r & 7)) << 4) + (c & 7) * 2));
-                    if (col + c < j.out_cols) dst[c] = v;
-                }
-            } else {
+        if (j.out_mode == kOut16) {  // a row per round, a column per lane
+            uint16_t *dst = (uint16_t *)j.out_ptr + (long long)row0 * j.out_stride + col + lane;
+            for (int r = 0; r < rows; ++r, dst += j.out_stride) {
+                uint16_t v;
+                asm volatile("ld.shared.u16 %0, [%1];"
+                             : "=h"(v)
+                             : "r"(buf + r * 64 + (((lane >> 3) ^ ((r >> 1) & 3)) << 4) + (lane & 7) * 2));
+                if (col + lane < j.out_cols) *dst = v;
+            }
+        } else {  // two rows per round
+            const int c = lane & 15;
+            for (int r = lane >> 4; r < rows; r += 2) {
                 float v;
                 asm volatile("ld.shared.f32 %0, [%1];"
                              : "=f"(v)
-                             : "r"(buf + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4));
-                if (col + lane < j.out_cols) ((float *)j.out_ptr)[(long long)(row0 + r) * j.out_stride + col + lane] = v;
+                             : "r"(buf + r * 64 + (((c >> 2) ^ ((r >> 1) & 3)) << 4) + (c & 3) * 4));
+                if (col + c < j.out_cols) ((float *)j.out_ptr)[(long long)(row0 + r) * j.out_stride + col + c] = v;
             }
         }
     }
@@ -606,8 +606,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 for (unsigned n = 0; n < kHeadSpin && !barrier_try(smem_addr(&drain), 0); ++n) {}
             }
         }
-    } else {  // ---- epilogue: a thread owns one row and half of an accumulator's columns
-        const int quad = warp & 3, half = (warp - 4) >> 2;
+    } else {  // ---- epilogue: a thread owns one row and a quarter of an accumulator's columns
+        const int quad = warp & 3, quarter = (warp - 4) >> 2;
         const float c2 = p.c2;
         const RowsOut<T> out = {ring + kRingBlocks * kBlockBytes + (warp - 4) * kStagingBytes, lane};
         int sub = 0;
@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
             if (logits) {
                 const long long y = live && !p.k ? p.labels[row] : -1;
                 if (p.k)
-                    tg.start(p, row, v0 + tp.n * j.halves * kTile + half * kHalf, live);
+                    tg.start(p, row, v0 + tp.n * j.halves * kTile + quarter * kQuarter, live);
                 else if (y >= j.v0 && y < j.v0 + j.vocab)
                     label = (int)(y - j.v0);
                 if (BACK && live) {
@@ -641,22 +641,22 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
             const float back = BACK && !logits && p.scale ? p.scale[1] : 1.0f;
             for (int h = 0; h < j.halves; ++h, ++sub) {
                 const int acc = sub & 1;
-                const int col0 = (tp.n * j.halves + h) * kTile + half * kHalf;
-                const uint32_t src = tmem_base + (uint32_t)acc * kTile + half * kHalf + ((uint32_t)(quad * 32) << 16);
+                const int col0 = (tp.n * j.halves + h) * kTile + quarter * kQuarter;
+                const uint32_t src = tmem_base + (uint32_t)acc * kTile + quarter * kQuarter + ((uint32_t)(quad * 32) << 16);
                 if (logits && p.k) tg.skip_to(v0 + col0);
                 ok = __all_sync(0xFFFFFFFFu, wait(smem_addr(&acc_full[acc]), (uint32_t)((sub >> 1) & 1)));
                 if (!ok) break;
                 tmem_fence_after();
                 [[maybe_unused]] float m = -INFINITY, s = 0.0f;
-                // A loop of 32 columns that stays rolled: unrolled over the 128 columns the code outgrows the
+                // A loop of 32 columns that stays rolled: unrolled over all columns the code outgrows the
                 // instruction cache and fetching it takes longer (5000 cycles per accumulator) than running it.
 #pragma unroll 1
-                for (int ch = 0; ch < kHalf / 32; ++ch) {
+                for (int ch = 0; ch < kQuarter / 32; ++ch) {
                     const int col = col0 + 32 * ch;
                     uint32_t raw[32];
                     tmem_load32(src + 32 * ch, raw);
                     tmem_wait_load(raw);
-                    if (ch + 1 == kHalf / 32) {  // the accumulator is read: the tile after the next may overwrite it
+                    if (ch + 1 == kQuarter / 32) {  // the accumulator is read: the tile after the next may overwrite it
                         tmem_fence_before();
                         __syncwarp();
                         if (lane == 0) barrier_arrive_leader(smem_addr(&acc_empty[acc]));
@@ -725,18 +725,34 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                             for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(raw[i]) * back;
                         }
                         // dz leaves in 16 bits, as both products' operand: their sums run over it in binary32
-                        const bool wide = j.out_mode != kOut16;
-                        if (wide || !(ch & 1)) out.wait_free();
-                        if (wide)
-                            out.put32(z);
-                        else
-                            out.put16(ch & 1, z);
-                        if (wide || (ch & 1)) out.flush(j, row0, wide ? col : col - 32, tp.split);
+                        out.wait_free();
+                        if (j.out_mode == kOut16) {
+                            out.put16(z);
+                        } else {
+                            out.template put32<0>(z);
+                            out.flush(j, row0, col, tp.split);
+                            out.wait_free();
+                            out.template put32<1>(z);
+                        }
+                        out.flush(j, row0, j.out_mode == kOut16 ? col : col + 16, tp.split);
                     }
                 }
-                if constexpr (!BACK) {
-                    const int part = col0 / kHalf;
-                    if (live && part < p.parts) p.partial[(long long)part * p.n + row] = make_float2(m, s);
+                if constexpr (!BACK) {  // the row's four quarters are joined before they leave
+                    const uint32_t slot = ring + kRingBlocks * kBlockBytes + ((sub & 1) * 4 * kHalf + quad * 32 + lane) * 8;
+                    asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(slot + quarter * kHalf * 8), "f"(m), "f"(s) : "memory");
+                    asm volatile("bar.sync %0, 128;" ::"r"(1 + quad) : "memory");
+                    const int part = tp.n * j.halves + h;
+                    if (quarter == 0 && live && part < p.parts) {
+#pragma unroll
+                        for (int q = 1; q < 4; ++q) {
+                            float om, os;
+                            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(om), "=f"(os) : "r"(slot + q * kHalf * 8));
+                            const float now = fmaxf(m, om), ref = now == -INFINITY ? 0.0f : now;
+                            s = s * exp2_approx(m - ref) + os * exp2_approx(om - ref);
+                            m = now;
+                        }
+                        p.partial[(long long)part * p.n + row] = make_float2(m, s);
+                    }
                 }
             }
             if (!ok) break;
@@ -852,7 +868,7 @@ k_head_scale(const float *__restrict__ grad, const long long *__restrict__ label
     }
 }
 
-// Joins a row's partial maxima and sums (one per 128 columns) to its log-sum-exp, and forms the loss.  Eight rows
+// Joins a row's partial maxima and sums (one per 256 columns) to its log-sum-exp, and forms the loss.  Eight rows
 // per CTA; the partials of a row are dealt to 32 threads, four loads at a time.
 constexpr int kJoinRows = 8;
 __global__ void __launch_bounds__(256)
@@ -993,7 +1009,7 @@ cudaError_t encode(CUtensorMap *map, int dtype, const void *base, long long rows
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-// C of a job: parts x rows x cols values of `elem` bytes in boxes of 32 rows x 128 bytes; falls back to plain stores
+// C of a job: parts x rows x cols values of `elem` bytes in boxes of 32 rows x 64 bytes; falls back to plain stores
 // where rows do not start on 16-byte boundaries
 cudaError_t set_output(HeadJob &j, int mode, int dtype, void *base, long long rows, long long cols, long long stride,
                        long long parts = 1)
@@ -1010,11 +1026,11 @@ cudaError_t set_output(HeadJob &j, int mode, int dtype, void *base, long long ro
     if (!fn) return cudaErrorNotSupported;
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
     const cuuint64_t strides[2] = {(cuuint64_t)stride * elem, (cuuint64_t)stride * elem * rows};
-    const cuuint32_t box[3] = {(cuuint32_t)(128 / elem), 32, 1}, one[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {(cuuint32_t)(64 / elem), 32, 1}, one[3] = {1, 1, 1};
     const CUresult r = fn(&j.out, mode != kOut16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                   : dtype == RSDGC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                                         : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-                          3, base, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          3, base, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
                           CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
@@ -1066,7 +1082,7 @@ HeadLayout head_layout(int64_t n, int64_t v, int64_t d, int64_t k)
     L.scale = take(8);
     L.counter = take(4 * L.pieces);
     const int64_t shared = at;  // the forward pass's partials and the backward pass's dz share the rest
-    L.partial = take(8 * n * 2 * tiles_of(v));
+    L.partial = take(8 * n * tiles_of(v));
     L.bytes = at;
     at = shared;
     L.dz[0] = take(2 * n * L.piece);
@@ -1244,7 +1260,7 @@ int head_forward(const HeadCall &c, float *loss, float *lse)
     cudaError_t e = operator_status_ptr(&p.status);
     common_params(p, c, L);
     p.n_jobs = 1;
-    p.parts = 2 * tiles_of(c.v);
+    p.parts = tiles_of(c.v);
     p.partial = (float2 *)(c.workspace + L.partial);
     p.target_z = (float *)(c.workspace + L.target_z);
     if (e == cudaSuccess)
