@@ -1166,12 +1166,50 @@ int head_pairs(cudaError_t *e)
     return m = n;
 }
 
+// Tiles of one (256 x 256) or two accumulators (256 x 512) for a launch's jobs.  With two, every operand block brought in
+// serves more products (48 instead of 64 bytes per cycle and SM at the full MMA rate) and the ring holds twice the work:
+// forward 2048 x 32000 x 2048 takes 219 us against 286.  With one there are twice as many tiles to deal out: 64 x 8000 x
+// 512, 32 tiles, takes 11.0 us against 13.8 forward and 25.5 against 31.2 backward.  Which is better follows from the
+// cycles a tile takes (512 per contraction step and accumulator, some 3000 to empty one) dealt to the pairs of CTAs.
+void choose_halves(HeadParams &p, int pairs)
+{
+    double best = 0.0;
+    int take = 2;
+    for (int h = 1; h <= 2; ++h) {
+        double total = 0.0, longest = 0.0;
+        long long tiles = 0;
+        for (int i = 0; i < p.n_jobs; ++i) {
+            const HeadJob &j = p.job[i];
+            const int jh = j.n_tiles > 1 ? h : 1;
+            const long long t = (long long)j.m_tiles * ((j.n_tiles + jh - 1) / jh) * j.splits;
+            const double time = jh * (512.0 * j.split_steps + 3000.0) * (jh == 1 ? 1.25 : 1.0);
+            total += t * time;
+            tiles += t;
+            if (time > longest) longest = time;
+        }
+        // one job's tiles come in rounds, several jobs' fill one another's gaps
+        const double rounds = p.n_jobs == 1 ? (double)((tiles + pairs - 1) / pairs) * longest : total / pairs;
+        const double cost = rounds > longest ? rounds : longest;
+        if (h == 1 || cost <= best) best = cost, take = h;
+    }
+    for (int i = 0; i < p.n_jobs; ++i) {
+        HeadJob &j = p.job[i];
+        j.halves = j.n_tiles > 1 ? take : 1;
+        j.n_tiles = (j.n_tiles + j.halves - 1) / j.halves;
+    }
+}
+
 template <bool BACK, typename T>
 cudaError_t launch_tiles(HeadParams &p, int *counter, cudaStream_t s)
 {
     cudaError_t e = cudaSuccess;
     const int most = head_pairs<BACK, T>(&e);
     if (e != cudaSuccess) return e;
+    choose_halves(p, most);
+    auto length = [](const HeadJob &j) { return j.split_steps * j.halves; };  // longest tiles first
+    for (int a = 0; a < p.n_jobs; ++a)
+        for (int b = a + 1; b < p.n_jobs; ++b)
+            if (length(p.job[b]) > length(p.job[a])) std::swap(p.job[a], p.job[b]);
     long long tiles = 0;
     int halves = 1;
     for (int i = 0; i < p.n_jobs; ++i) {
@@ -1188,15 +1226,6 @@ cudaError_t launch_tiles(HeadParams &p, int *counter, cudaStream_t s)
 
 constexpr double kTruncationBf16 = 0.26, kTruncationF16 = 0.29;
 constexpr int kBand = 16;
-// Two accumulators per tile (256 x 512) unless all 256 x 256 tiles run at a time: every operand block brought in serves
-// more products, 48 instead of 64 bytes per cycle and SM at the full MMA rate, and the ring holds twice the work.
-// (Forward 2048 x 32000 x 2048: 219 us against 286; 333 x 10007 x 776, 80 tiles: 20 against 24; 64 x 32000 x 4096: 64
-// against 82.  One accumulator for 64 x 8000 x 512, 32 tiles: see the head's notes on short launches.)
-bool two_accumulators(int64_t m, int64_t n)
-{
-    return n > kTile && (int64_t)tiles_of(m) * tiles_of(n) > current_device_sms() / 2;
-}
-
 cudaError_t set_job(HeadJob &j, int kind, int dtype, const void *a, bool a_mn, long long ar, long long ac, long long as,
                     const void *b, bool b_mn, long long br, long long bc, long long bs, long long m, long long n, long long k)
 {
@@ -1206,8 +1235,7 @@ cudaError_t set_job(HeadJob &j, int kind, int dtype, const void *a, bool a_mn, l
     j.b_mn = b_mn;
     j.k_steps = (int)((k + kStepK - 1) / kStepK);
     j.m_tiles = tiles_of(m);
-    j.halves = two_accumulators(m, n) ? 2 : 1;
-    j.n_tiles = (tiles_of(n) + j.halves - 1) / j.halves;
+    j.n_tiles = tiles_of(n);  // of one accumulator; choose_halves() pairs them
     j.band = j.m_tiles < kBand ? j.m_tiles : kBand;
     j.splits = 1;
     j.split_steps = j.k_steps;
@@ -1330,10 +1358,6 @@ cudaError_t backward_pieces(const HeadCall &c, const HeadLayout &L, HeadParams &
             }
         }
         if (e != cudaSuccess) return e;
-        auto length = [](const HeadJob &j) { return j.split_steps * j.halves; };
-        for (int a = 0; a < p.n_jobs; ++a)
-            for (int b = a + 1; b < p.n_jobs; ++b)
-                if (length(p.job[b]) > length(p.job[a])) std::swap(p.job[a], p.job[b]);
         // the first launch has tiles of one length and deals them out in rounds; it clears the others' counters
         p.clear = counter;
         p.n_clear = i == 0 ? (int)L.pieces : 0;
