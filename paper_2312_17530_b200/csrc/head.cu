@@ -1040,14 +1040,14 @@ inline int tiles_of(int64_t a) { return (int)((a + kTile - 1) / kTile); }
 
 // A piece of the vocabulary: dz (n x piece, 16 bits) of at most kPieceBytes, in two buffers (one is written while the
 // other is read); never under kPieceMin columns, because every piece adds to dh once.  A launch ends on its longest
-// tiles, so few large pieces are better than what L2 would hold: 8192 x 128000 x 4096 takes 22.2 / 20.7 / 20.1 / 19.9 ms
-// with pieces of 64 / 128 / 256 / 512 MB.
-constexpr int64_t kPieceBytes = 256ll << 20;
+// tiles, so few large pieces are better than what L2 would hold: 8192 x 128000 x 4096 takes 22.2 / 20.7 / 20.1 ms with
+// pieces of 64 / 128 / 256 MB (19.4 and 19.2 with 128 and 256 by now: not worth twice the memory).
+constexpr int64_t kPieceBytes = 128ll << 20;
 constexpr int64_t kPieceMin = 2048;
 // With few tokens dh has few tiles, each with a contraction over the whole piece: it is cut into parts that are added
 // up at the end, in order, so that about kSplitTiles tiles share a launch with dW's, none longer than the launch's fair
-// share.  More parts cost more in sums than they balance (1023 x 50001 x 1000: 369 us with 5 parts, 392 with 10, 417
-// with 19, 660 with one).
+// share.  More parts cost more in sums than they balance (1023 x 50001 x 1000: 522 us with one part, 345 with 3, 311
+// with 5, 331 with 10).
 constexpr int64_t kSplitTiles = 37, kSplitSteps = 8;
 
 struct HeadLayout {
