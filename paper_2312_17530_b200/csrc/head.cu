@@ -455,7 +455,10 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
     };
 
     if (warp < 4) {
-        if (warp == 0 && lane == 0) {  // ---- producer, in both CTAs; all bytes count on the first CTA's barriers
+        auto wait_warp = [&](uint32_t bar, uint32_t ph) -> bool { return __all_sync(0xFFFFFFFFu, wait(bar, ph)); };
+        // ---- producer, in both CTAs; all bytes count on the first CTA's barriers.  As the MMAs, the copies are issued by
+        // one elected thread of a warp that walks together: a thread of a diverged warp takes some 200 cycles for each.
+        if (warp == 0) {
             int stage = 0, it = 0;
             uint32_t parity = 0;
             bool ok = true;
@@ -464,29 +467,42 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
             asm volatile("fence.proxy.async.global;" ::: "memory");  // TMA reads what ordinary stores wrote
             for (int t = pair, i = 0; t < p.tiles; ++i) {
                 // the tile after this one: asked for here, announced behind this one's loads
-                const int after = rank != 0 ? 0 : p.next_tile ? pairs + atomicAdd(p.next_tile, 1) : t + pairs;
+                int after = 0;
+                if (rank == 0 && lane == 0) after = p.next_tile ? pairs + atomicAdd(p.next_tile, 1) : t + pairs;
                 if (i) tp = tile_pos(p, t);
                 const HeadJob &j = p.job[tp.job];
-                const int halves = j.halves;
-                const int ra = tp.m * kTile + (int)rank * kHalf, rb = tp.n * halves * kTile + (int)rank * kHalf;
+                const int halves = j.halves, a_mn = j.a_mn, b_mn = j.b_mn;
+                const uint32_t bytes = 2u * (uint32_t)((1 + halves) * kBlockBytes);
+                const int ra = tp.m * kTile + (int)rank * kHalf;
+                const int rb = tp.n * halves * kTile + (int)rank * kHalf;
+                // coordinates of a box: (k, row), or (row, k) where the rows are contiguous
                 for (int k = 0; k < tp.steps; ++k) {
-                    if (!wait(smem_addr(&empty[stage]), parity ^ 1u)) {
-                        ok = false;
-                        break;
-                    }
-                    if (rank == 0) barrier_expect(smem_addr(&full[stage]), 2 * (1 + halves) * kBlockBytes);
+                    ok = wait_warp(smem_addr(&empty[stage]), parity ^ 1u);
+                    if (!ok) break;
                     const uint32_t bar = leader_addr(smem_addr(&full[stage])), dst = ring + stage * stage_bytes;
                     const int kc = (tp.k0 + k) * kStepK;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        load_box(dst + i * kBoxBytes, &j.a, j.a_mn ? ra + 64 * i : kc, j.a_mn ? kc : ra + 64 * i, bar);
-                    for (int h = 0; h < halves; ++h) {
-                        const int r = rb + h * kTile;
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            load_box(dst + (1 + h) * kBlockBytes + i * kBoxBytes, &j.b, j.b_mn ? r + 64 * i : kc,
-                                     j.b_mn ? kc : r + 64 * i, bar);
+                    if (elect_one()) {
+                        if (rank == 0) barrier_expect(smem_addr(&full[stage]), bytes);
+                        if (a_mn) {
+                            load_box(dst, &j.a, ra, kc, bar);
+                            load_box(dst + kBoxBytes, &j.a, ra + 64, kc, bar);
+                        } else {
+                            load_box(dst, &j.a, kc, ra, bar);
+                            load_box(dst + kBoxBytes, &j.a, kc, ra + 64, bar);
+                        }
+                        if (b_mn) {
+                            for (int h = 0; h < halves; ++h) {
+                                load_box(dst + (1 + h) * kBlockBytes, &j.b, rb + h * kTile, kc, bar);
+                                load_box(dst + (1 + h) * kBlockBytes + kBoxBytes, &j.b, rb + h * kTile + 64, kc, bar);
+                            }
+                        } else {
+                            for (int h = 0; h < halves; ++h) {
+                                load_box(dst + (1 + h) * kBlockBytes, &j.b, kc, rb + h * kTile, bar);
+                                load_box(dst + (1 + h) * kBlockBytes + kBoxBytes, &j.b, kc, rb + h * kTile + 64, bar);
+                            }
+                        }
                     }
+                    __syncwarp();
                     ++it;
                     if (++stage == stages) {
                         stage = 0;
@@ -495,27 +511,28 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 }
                 if (!ok) break;
                 if (rank == 0) {
-                    if (!wait(smem_addr(&slot_empty[i % kSlots]), ((uint32_t)(i / kSlots) & 1u) ^ 1u)) {
-                        ok = false;
-                        break;
+                    ok = wait_warp(smem_addr(&slot_empty[i % kSlots]), ((uint32_t)(i / kSlots) & 1u) ^ 1u);
+                    if (!ok) break;
+                    after = __shfl_sync(0xFFFFFFFFu, after, 0);
+                    if (elect_one()) {
+                        for (uint32_t r = 0; r < 2; ++r) {
+                            store_in(smem_addr(&slot_tile[i % kSlots]), after, r);
+                            barrier_arrive_in(smem_addr(&slot_full[i % kSlots]), r);
+                        }
                     }
-                    for (uint32_t r = 0; r < 2; ++r) {
-                        store_in(smem_addr(&slot_tile[i % kSlots]), after, r);
-                        barrier_arrive_in(smem_addr(&slot_full[i % kSlots]), r);
-                    }
+                    __syncwarp();
                     t = after;
                 } else {
                     t = next_tile(i);
-                    if (t < 0) {
-                        ok = false;
-                        break;
-                    }
-                    barrier_arrive_leader(smem_addr(&slot_empty[i % kSlots]));
+                    ok = __all_sync(0xFFFFFFFFu, t >= 0);
+                    if (!ok) break;
+                    if (elect_one()) barrier_arrive_leader(smem_addr(&slot_empty[i % kSlots]));
+                    __syncwarp();
                 }
             }
             // the last commits arrive on this CTA's barriers: it must not leave before they have
             for (int i = 0; i < stages && ok; ++i) {
-                ok = wait(smem_addr(&empty[stage]), parity ^ 1u);
+                ok = wait_warp(smem_addr(&empty[stage]), parity ^ 1u);
                 if (++stage == stages) {
                     stage = 0;
                     parity ^= 1u;
@@ -532,7 +549,6 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
             uint32_t parity = 0;
             bool ok = true;
             constexpr uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
-            auto wait_warp = [&](uint32_t bar, uint32_t ph) -> bool { return __all_sync(0xFFFFFFFFu, wait(bar, ph)); };
             for (int t = pair, i = 0; t < p.tiles; ++i) {
                 const TilePos tp = tile_pos(p, t);
                 const HeadJob &j = p.job[tp.job];
