@@ -40,7 +40,6 @@ constexpr int kBlockBytes = 2 * kBoxBytes;
 constexpr int kRingBlocks = 12;     // of A and B blocks: 4 stages of 1 + 2 blocks, or 6 stages of 1 + 1
 constexpr int kMaxStages = kRingBlocks / 2;
 constexpr int kEpilogueWarps = 16;                       // four per quarter of an accumulator's columns
-constexpr int kQuarter = 64;
 constexpr int kHeadThreads = 128 + 32 * kEpilogueWarps;  // producer, MMA, two idle warps, epilogue
 constexpr int kStagingBytes = 2048;  // per epilogue warp: 32 rows of 64 bytes on their way out
 constexpr int kHeadSmem = kRingBlocks * kBlockBytes + kEpilogueWarps * kStagingBytes + 1024;
@@ -59,7 +58,8 @@ struct __align__(64) HeadJob {
     CUtensorMap a, b, out;   // out: boxes of 32 rows x 64 bytes
     int a_mn, b_mn;          // the operand lies with its rows (not k) contiguous
     int m_tiles, n_tiles, k_steps, band;
-    int halves;              // accumulators of a tile: 256 x 256 or 256 x 512
+    long long columns;       // of C
+    int halves, cols;        // accumulators of a tile, and their columns: 256 x 512, 256 x 256 or 256 x 128 tiles
     int splits, split_steps; // parts of the contraction, each a tile of its own
     int kind;
     int vocab;               // entries of the vocabulary this job is about (all, or a piece's)
@@ -81,7 +81,7 @@ struct HeadParams {
     const float *target_q;
     int k;
     // forward
-    float2 *partial;         // [columns / 256][n]: (maximum in log2 units, sum)
+    float2 *partial;         // [tile columns][n]: (maximum in log2 units, sum)
     int parts;
     float *target_z;         // [n][max(k, 1)]
     // gradients
@@ -472,9 +472,10 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 if (i) tp = tile_pos(p, t);
                 const HeadJob &j = p.job[tp.job];
                 const int halves = j.halves, a_mn = j.a_mn, b_mn = j.b_mn;
-                const uint32_t bytes = 2u * (uint32_t)((1 + halves) * kBlockBytes);
+                const uint32_t bytes = 2u * (uint32_t)(kBlockBytes + halves * j.cols * kStepK);
                 const int ra = tp.m * kTile + (int)rank * kHalf;
-                const int rb = tp.n * halves * kTile + (int)rank * kHalf;
+                const int rb = tp.n * halves * j.cols + (int)rank * (j.cols >> 1);
+                const bool whole = j.cols == kTile;  // of an accumulator's columns a CTA holds half: one box or two
                 // coordinates of a box: (k, row), or (row, k) where the rows are contiguous
                 for (int k = 0; k < tp.steps; ++k) {
                     ok = wait_warp(smem_addr(&empty[stage]), parity ^ 1u);
@@ -493,12 +494,12 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                         if (b_mn) {
                             for (int h = 0; h < halves; ++h) {
                                 load_box(dst + (1 + h) * kBlockBytes, &j.b, rb + h * kTile, kc, bar);
-                                load_box(dst + (1 + h) * kBlockBytes + kBoxBytes, &j.b, rb + h * kTile + 64, kc, bar);
+                                if (whole) load_box(dst + (1 + h) * kBlockBytes + kBoxBytes, &j.b, rb + h * kTile + 64, kc, bar);
                             }
                         } else {
                             for (int h = 0; h < halves; ++h) {
                                 load_box(dst + (1 + h) * kBlockBytes, &j.b, kc, rb + h * kTile, bar);
-                                load_box(dst + (1 + h) * kBlockBytes + kBoxBytes, &j.b, kc, rb + h * kTile + 64, bar);
+                                if (whole) load_box(dst + (1 + h) * kBlockBytes + kBoxBytes, &j.b, kc, rb + h * kTile + 64, bar);
                             }
                         }
                     }
@@ -554,7 +555,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 const HeadJob &j = p.job[tp.job];
                 const int a_mn = j.a_mn, b_mn = j.b_mn, steps = tp.steps, halves = j.halves;
                 const uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)a_mn << 15) |
-                                       ((uint32_t)b_mn << 16) | ((uint32_t)(kTile >> 3) << 17) |
+                                       ((uint32_t)b_mn << 16) | ((uint32_t)(j.cols >> 3) << 17) |
                                        ((uint32_t)(kTile >> 4) << 24);
                 const uint32_t da = a_mn ? 2048 >> 4 : 32 >> 4, db = b_mn ? 2048 >> 4 : 32 >> 4;
                 const uint64_t a_base = operand_desc(ring, a_mn), b_base = operand_desc(ring + kBlockBytes, b_mn);
@@ -637,6 +638,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
             const HeadJob &j = p.job[tp.job];
             const int row0 = tp.m * kTile + (int)rank * kHalf + quad * 32, row = row0 + lane;
             const bool live = row < p.n, logits = !BACK || j.kind == kLogitGrad;
+            const int width = j.cols >> 2;          // columns of this thread: 64 or 32
             // what a row needs, loaded before the tile is ready
             [[maybe_unused]] float gs = 0.0f, l2 = 0.0f;
             [[maybe_unused]] Targets tg;
@@ -645,7 +647,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
             if (logits) {
                 const long long y = live && !p.k ? p.labels[row] : -1;
                 if (p.k)
-                    tg.start(p, row, v0 + tp.n * j.halves * kTile + quarter * kQuarter, live);
+                    tg.start(p, row, v0 + tp.n * j.halves * j.cols + quarter * width, live);
                 else if (y >= j.v0 && y < j.v0 + j.vocab)
                     label = (int)(y - j.v0);
                 if (BACK && live) {
@@ -657,8 +659,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
             const float back = BACK && !logits && p.scale ? p.scale[1] : 1.0f;
             for (int h = 0; h < j.halves; ++h, ++sub) {
                 const int acc = sub & 1;
-                const int col0 = (tp.n * j.halves + h) * kTile + quarter * kQuarter;
-                const uint32_t src = tmem_base + (uint32_t)acc * kTile + quarter * kQuarter + ((uint32_t)(quad * 32) << 16);
+                const int col0 = (tp.n * j.halves + h) * j.cols + quarter * width;
+                const uint32_t src = tmem_base + (uint32_t)acc * kTile + quarter * width + ((uint32_t)(quad * 32) << 16);
                 if (logits && p.k) tg.skip_to(v0 + col0);
                 ok = __all_sync(0xFFFFFFFFu, wait(smem_addr(&acc_full[acc]), (uint32_t)((sub >> 1) & 1)));
                 if (!ok) break;
@@ -667,12 +669,12 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 // A loop of 32 columns that stays rolled: unrolled over all columns the code outgrows the
                 // instruction cache and fetching it takes longer (5000 cycles per accumulator) than running it.
 #pragma unroll 1
-                for (int ch = 0; ch < kQuarter / 32; ++ch) {
-                    const int col = col0 + 32 * ch;
+                for (int at = 0; at < width; at += 32) {
+                    const int col = col0 + at;
                     uint32_t raw[32];
-                    tmem_load32(src + 32 * ch, raw);
+                    tmem_load32(src + at, raw);
                     tmem_wait_load(raw);
-                    if (ch + 1 == kQuarter / 32) {  // the accumulator is read: the tile after the next may overwrite it
+                    if (at + 32 == width) {  // the accumulator is read: the tile after the next may overwrite it
                         tmem_fence_before();
                         __syncwarp();
                         if (lane == 0) barrier_arrive_leader(smem_addr(&acc_empty[acc]));
@@ -1098,7 +1100,7 @@ HeadLayout head_layout(int64_t n, int64_t v, int64_t d, int64_t k)
     L.scale = take(8);
     L.counter = take(4 * L.pieces);
     const int64_t shared = at;  // the forward pass's partials and the backward pass's dz share the rest
-    L.partial = take(8 * n * tiles_of(v));
+    L.partial = take(8 * n * ((v + kTile / 2 - 1) / (kTile / 2)));  // at most one per 128 columns
     L.bytes = at;
     at = shared;
     L.dz[0] = take(2 * n * L.piece);
@@ -1182,23 +1184,25 @@ int head_pairs(cudaError_t *e)
     return m = n;
 }
 
-// Tiles of one (256 x 256) or two accumulators (256 x 512) for a launch's jobs.  With two, every operand block brought in
-// serves more products (48 instead of 64 bytes per cycle and SM at the full MMA rate) and the ring holds twice the work:
-// forward 2048 x 32000 x 2048 takes 219 us against 286.  With one there are twice as many tiles to deal out: 64 x 8000 x
-// 512, 32 tiles, takes 11.0 us against 13.8 forward and 25.5 against 31.2 backward.  Which is better follows from the
-// cycles a tile takes (512 per contraction step and accumulator, some 3000 to empty one) dealt to the pairs of CTAs.
-void choose_halves(HeadParams &p, int pairs)
+// Tiles of 256 x 128, 256 x 256 or 256 x 512 (two accumulators) for a launch's jobs.  The wider the tile, the more products
+// an operand block serves (48 bytes per cycle and SM at the full MMA rate for 512 columns, 64 for 256) and the more work
+// the ring holds: forward 2048 x 32000 x 2048 takes 219 us with 512 columns against 286 with 256.  The narrower, the more
+// tiles there are to deal out: 64 x 8000 x 512, 32 tiles of 256 columns, takes 11.0 us against 13.8 with 512, and 25.5
+// against 31.2 backward.  Which is best follows from the cycles a tile takes (512 per contraction step and 256 columns,
+// some 3000 to empty an accumulator) dealt to the pairs of CTAs.
+void choose_columns(HeadParams &p, int pairs)
 {
     double best = 0.0;
-    int take = 2;
-    for (int h = 1; h <= 2; ++h) {
+    int take = kTile;
+    for (int wide = kTile / 2; wide <= 2 * kTile; wide *= 2) {
         double total = 0.0, longest = 0.0;
         long long tiles = 0;
         for (int i = 0; i < p.n_jobs; ++i) {
             const HeadJob &j = p.job[i];
-            const int jh = j.n_tiles > 1 ? h : 1;
-            const long long t = (long long)j.m_tiles * ((j.n_tiles + jh - 1) / jh) * j.splits;
-            const double time = jh * (512.0 * j.split_steps + 3000.0) * (jh == 1 ? 1.25 : 1.0);
+            const int w = wide > kTile && j.columns <= kTile ? kTile : wide;
+            const long long t = (long long)j.m_tiles * ((j.columns + w - 1) / w) * j.splits;
+            const double part = (double)w / kTile, loss = w > kTile ? 1.0 : w == kTile ? 1.25 : 1.6;
+            const double time = loss * part * (512.0 * j.split_steps + 3000.0);
             total += t * time;
             tiles += t;
             if (time > longest) longest = time;
@@ -1206,12 +1210,14 @@ void choose_halves(HeadParams &p, int pairs)
         // one job's tiles come in rounds, several jobs' fill one another's gaps
         const double rounds = p.n_jobs == 1 ? (double)((tiles + pairs - 1) / pairs) * longest : total / pairs;
         const double cost = rounds > longest ? rounds : longest;
-        if (h == 1 || cost <= best) best = cost, take = h;
+        if (wide < kTile || cost <= best) best = cost, take = wide;
     }
     for (int i = 0; i < p.n_jobs; ++i) {
         HeadJob &j = p.job[i];
-        j.halves = j.n_tiles > 1 ? take : 1;
-        j.n_tiles = (j.n_tiles + j.halves - 1) / j.halves;
+        const int w = take > kTile && j.columns <= kTile ? kTile : take;
+        j.halves = w > kTile ? 2 : 1;
+        j.cols = w < kTile ? w : kTile;
+        j.n_tiles = (int)((j.columns + w - 1) / w);
     }
 }
 
@@ -1221,8 +1227,8 @@ cudaError_t launch_tiles(HeadParams &p, int *counter, cudaStream_t s)
     cudaError_t e = cudaSuccess;
     const int most = head_pairs<BACK, T>(&e);
     if (e != cudaSuccess) return e;
-    choose_halves(p, most);
-    auto length = [](const HeadJob &j) { return j.split_steps * j.halves; };  // longest tiles first
+    choose_columns(p, most);
+    auto length = [](const HeadJob &j) { return (long long)j.split_steps * j.halves * j.cols; };  // longest tiles first
     for (int a = 0; a < p.n_jobs; ++a)
         for (int b = a + 1; b < p.n_jobs; ++b)
             if (length(p.job[b]) > length(p.job[a])) std::swap(p.job[a], p.job[b]);
@@ -1235,6 +1241,7 @@ cudaError_t launch_tiles(HeadParams &p, int *counter, cudaStream_t s)
     p.stages = kRingBlocks / (1 + halves);
     if (tiles > INT_MAX / 2) return cudaErrorInvalidValue;
     p.tiles = (int)tiles;
+    p.parts = p.job[0].n_tiles * p.job[0].halves;
     p.next_tile = counter;
     const unsigned pairs = (unsigned)(tiles < most ? tiles : most);
     return launch_chained(k_head<BACK, T>, 2 * pairs, kHeadThreads, kHeadSmem, s, 2, p);
@@ -1251,7 +1258,7 @@ cudaError_t set_job(HeadJob &j, int kind, int dtype, const void *a, bool a_mn, l
     j.b_mn = b_mn;
     j.k_steps = (int)((k + kStepK - 1) / kStepK);
     j.m_tiles = tiles_of(m);
-    j.n_tiles = tiles_of(n);  // of one accumulator; choose_halves() pairs them
+    j.columns = n;  // cut into tiles by choose_columns()
     j.band = j.m_tiles < kBand ? j.m_tiles : kBand;
     j.splits = 1;
     j.split_steps = j.k_steps;
@@ -1304,7 +1311,6 @@ int head_forward(const HeadCall &c, float *loss, float *lse)
     cudaError_t e = operator_status_ptr(&p.status);
     common_params(p, c, L);
     p.n_jobs = 1;
-    p.parts = tiles_of(c.v);
     p.partial = (float2 *)(c.workspace + L.partial);
     p.target_z = (float *)(c.workspace + L.target_z);
     if (e == cudaSuccess)
