@@ -343,7 +343,8 @@ int rsdgc_payload_to_coo(rsdgc_plan *plan, const int32_t *idx_dev, const int32_t
  * gradient may be written straight into a layer of a gradient arena (same type, elem_offset_l).
  *
  * All calls work on the current device, are enqueued on `stream`, allocate nothing, keep nothing
- * from call to call and may be captured into a graph.  Matrices are row-major with a row stride in
+ * from call to call and may be captured into a graph (make a first call of each kind before: it
+ * loads the kernels and asks the device for their limits).  Matrices are row-major with a row stride in
  * elements (>= the width); 16-byte alignment of rows is used where it is there and never required
  * unless a call says so.  Where nothing else is said an optional pointer may be NULL.  Sums,
  * statistics and losses are binary32; an output of fewer bits is rounded once, to nearest even.

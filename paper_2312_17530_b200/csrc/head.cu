@@ -8,16 +8,22 @@
 //
 // Both losses are the same computation: a target distribution with k entries per row.  Three matrix products
 // carry it, all by one persistent kernel (k_head) that differs only in what it does with a finished tile:
-//   forward   z tile -> per row and 256 columns the maximum and the sum of exponentials, and z at the targets
+//   forward   z tile -> per row the maximum and the sum of exponentials of the tile's columns, and z at the targets
 //   backward  z tile again (recomputed) -> dz of one piece of the vocabulary, 16 bits, in the workspace
 //             dz W_piece -> added to dh;  dz^T h -> the piece's rows of dW
-// A piece is as wide as keeps dz in the L2 cache between its writer and its two readers.
+// A launch of the backward pass holds both products of one piece and the dz of the next, from one queue of tiles.
 //
-// The tile kernel: pairs of CTAs (cluster of 2) compute 256 x 256 tiles with tcgen05.mma.cta_group::2, K in steps
-// of 64; each CTA loads its 128 rows of either operand by TMA (128-byte swizzle) through a ring of kStages
-// stages, the accumulators of two tiles alternate in the 512 TMEM columns, so that sixteen warps empty one while
-// the other is filled.  Operands whose contraction index is not the contiguous one (W in dz W, both in dz^T h)
-// are read as they lie in memory: the MMA takes them as MN-major.
+// The tile kernel: pairs of CTAs (cluster of 2, one pair per two multiprocessors) compute tiles of 256 rows and 128 to 512
+// columns with tcgen05.mma.cta_group::2, K in steps of 64.  One warp brings the operands by TMA (128-byte swizzle) through a
+// ring of 4 to 6 stages, 192 KB per CTA; one thread issues the MMAs; sixteen warps empty an accumulator from tensor memory
+// while the other one (256 columns each, 512 in all) is filled.  Operands whose contraction index is not the contiguous one
+// (W in dz W, both in dz^T h) are read as they lie in memory: the MMA takes them as MN-major.
+//
+// What bounds it: the tensor cores, and in long calls the power limit.  Rates by the products that are computed (one
+// forward, three backward): 2048 x 32000 x 2048 (tokens, vocabulary, width; bfloat16) forward 174 us, 1.54 PFLOP/s, backward
+// 539 us, 1.49; x 4096 1.61 and 1.62; 8192 x 128000 x 4096 backward 18.2 ms, 1.42.  With up to a few hundred tokens it is W's
+// way from memory: 64 x 32000 x 8192 forward takes 96 us, W at 5.4 TB/s, backward 301 us (W twice and dW at 5.2).  Small
+// calls are bound by the launches and the fill of the ring: 5 x 1000 x 256 takes 8.4 us forward and 16.4 backward.
 #include <cuda.h>
 
 #include <climits>
@@ -886,7 +892,7 @@ k_head_scale(const float *__restrict__ grad, const long long *__restrict__ label
     }
 }
 
-// Joins a row's partial maxima and sums (one per 256 columns) to its log-sum-exp, and forms the loss.  Eight rows
+// Joins a row's partial maxima and sums (one per accumulator, 128 or 256 columns) to its log-sum-exp, and forms the loss.  Eight rows
 // per CTA; the partials of a row are dealt to 32 threads, four loads at a time.
 constexpr int kJoinRows = 8;
 __global__ void __launch_bounds__(256)
