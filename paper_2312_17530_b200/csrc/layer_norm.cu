@@ -30,6 +30,7 @@ constexpr int kNormWarps = 4;              // warps of a CTA whose rows take one
 constexpr int kBackWarps = 8;              // ... backward
 constexpr int kNormElems = 16;             // columns of a thread (32 in the widest variants)
 constexpr int kNormRingThreads = 512;
+constexpr int kNormJoin = kNormRingThreads + 4;
 constexpr int kNormLongThreads = 1024;
 constexpr int kNormMaxStages = 4;
 constexpr int kNormMaxTeams = 8;
@@ -715,31 +716,41 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
         ring.drain(it - 1, min(mine, it + stages - 1));
     }
     if (!partial) return;
-    // The teams' sums are added up, the last team's first, in the rings' memory (everything has arrived and been read): value
-    // e of a thread's granules at [e][thread], 4 words of padding, so that neither the threads nor the columns' order
-    // meets a bank conflict.
+    // The teams' sums are added up in order, in the rings' memory (everything has arrived and been read): value e of a
+    // thread's granules at [e][thread], 4 words of padding, so that neither the threads nor the columns' order meets a bank
+    // conflict.
     float *const joined = reinterpret_cast<float *>(rows);
-    const int across = team_threads + 4;
+    int self, all;  // read anew: what follows from them need not live in registers through the rows' loop
+    asm volatile("mov.u32 %0, %%tid.x;\n\tmov.u32 %1, %%ntid.x;" : "=r"(self), "=r"(all));
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        for (int turn = teams - 1; turn >= 0; --turn) {
-            __syncthreads();
-            if (team != turn) continue;
+        __syncthreads();
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int k = 0; k < NP; ++k) {
-                    const float2 v = which ? db[i][k] : dw[i][k];
-                    float *x = joined + (i * V + 2 * k) * across + tid, *y = x + across;
-                    *x = turn < teams - 1 ? *x + v.x : v.x;
-                    *y = turn < teams - 1 ? *y + v.y : v.y;
-                }
-        }
+            for (int k = 0; k < NP; ++k) {
+                const float2 v = which ? db[i][k] : dw[i][k];
+                joined[(i * V + 2 * k) * kNormJoin + self] = v.x;
+                joined[(i * V + 2 * k + 1) * kNormJoin + self] = v.y;
+            }
         __syncthreads();
         float *dst = partial + ((long long)which * gridDim.x + blockIdx.x) * d;
-        for (int c = threadIdx.x; c < d; c += blockDim.x) {
-            const int at = c + (SHIFT ? walk.phase : 0), granule = at / V, i = granule / team_threads;
-            dst[c] = joined[(i * V + at % V) * across + granule - i * team_threads];
+        for (int c0 = self; c0 < d; c0 += 4 * all) {  // four columns at a time, so that their loads overlap
+            int from[4];
+            float sum[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int at = min(c0 + u * all, d - 1) + (SHIFT ? walk.phase : 0), granule = at / V;
+                const int i = granule / team_threads;
+                from[u] = (i * V + at % V) * kNormJoin + granule - i * team_threads;
+                sum[u] = joined[from[u]];
+            }
+            for (int k = 1; k < all / team_threads; ++k)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) sum[u] += joined[k * team_threads + from[u]];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (c0 + u * all < d) dst[c0 + u * all] = sum[u];
         }
     }
 }
@@ -1080,10 +1091,10 @@ TeamShape team_shape(const NormShape &sh, int elems, int rows, long long n)
     TeamShape t{sh.threads(elems, Pairs<T>::V), 0, 0};
     if (t.threads > kNormRingThreads) return t;
     const long long stage = 2ll * rows * 16 * sh.packs, weight = elems > 16 ? 4ll * elems * t.threads : 0;
-    const long long groups = (n + rows - 1) / rows, share = groups / current_device_sms();
+    const long long groups = (n + rows - 1) / rows, share = (groups + current_device_sms() - 1) / current_device_sms();
     t.teams = kNormRingThreads / t.threads;
     if (t.teams > kNormMaxTeams) t.teams = kNormMaxTeams;
-    if (t.teams > share) t.teams = share > 1 ? (int)share : 1;
+    if (t.teams > share) t.teams = (int)share;
     while (t.teams > 1 && (kNormRingBytes - weight) / t.teams < 3 * stage) --t.teams;
     t.stages = (int)((kNormRingBytes - weight) / t.teams / stage);
     if (t.stages > kNormMaxStages) t.stages = kNormMaxStages;
@@ -1095,7 +1106,8 @@ template <bool SHIFT, typename T, int E, int ROWS, typename P>
 cudaError_t backward_ring(int *slots, const BackwardArgs<T, P> &a, const NormShape &sh, const TeamShape &t)
 {
     const uint32_t row = 16u * (uint32_t)sh.packs;
-    const long long smem = (long long)t.teams * t.stages * 2 * ROWS * row + (E > 16 ? 4ll * E * t.threads : 0);
+    const long long loop = (long long)t.teams * t.stages * 2 * ROWS * row + (E > 16 ? 4ll * E * t.threads : 0);
+    const long long join = 4ll * E * kNormJoin, smem = loop > join ? loop : join;
     static std::atomic<uint64_t> ready{0};
     unsigned int *status = nullptr;
     cudaError_t e = operator_status_ptr(&status);
@@ -1150,7 +1162,7 @@ cudaError_t norm_backward(const BackwardArgs<T, P> &a, void *dw, void *db, int g
     }
     if (e != cudaSuccess || !a.partial) return e;
     const dim3 grid((unsigned)((a.d + 31) / 32), 2);
-    const int lanes = slots >= 128 ? 16 : slots >= 16 ? 8 : 1;
+    const int lanes = slots >= 256 ? 32 : slots >= 128 ? 16 : slots >= 16 ? 8 : 1;
     const float *part = a.partial;
     if (grad_type == RSDGC_F32)
         return launch_chained(k_norm_param_gradient<float>, grid, 32 * lanes, 0, a.s, 1, part, slots, a.d, (float *)dw, (float *)db);
