@@ -3,9 +3,9 @@
 //   mean = sum x / D,  rstd = (sum (x - mean)^2 / D + eps)^(-1/2),  xhat = (x - mean) rstd,  y = xhat w + b
 //   dx = rstd (g w - mean(g w) - xhat mean(g w xhat)),  dw = sum_n g xhat,  db = sum_n g
 //
-// Bound: memory for binary32 rows (8192 x 8192: forward 98 us, 5.5 TB/s, gradient 140 us, 5.8 TB/s), the issue rate for
+// Bound: memory for binary32 rows (8192 x 8192: forward 98 us, 5.5 TB/s, gradient 137 us, 5.9 TB/s), the issue rate for
 // 16-bit rows (16384 x 4096 bfloat16: forward 53 us, 5.1 TB/s at 68 % of the issue slots, 19 instructions per value;
-// gradient of 16384 x 8192 161 us, 5.0 TB/s), the launch for a few rows (1 x 4096: 2.3 us).  So a row is read once, in
+// gradient of 16384 x 8192 158 us, 5.1 TB/s), the launch for a few rows (1 x 4096: 2.3 us).  So a row is read once, in
 // 16-byte packs, and its arithmetic runs on pairs of binary32 values.  The mean, then the centred squares (two reductions,
 // no cancellation), then the output.  All statistics and sums are binary32.
 //
@@ -14,7 +14,7 @@
 // and the row's.  Phases repeat with a short period (at most 8 rows), so a CTA or warp takes rows of one phase only:
 // its threads then own the same columns in every row, as the sums of dw and db over the rows need it.  The first and
 // the last granule of a row are masked; where they would reach beyond the operand they are read element by element.
-// (8192 x 4097 bfloat16: forward 47 us and gradient 104 us, against 81 and 269 a value at a time.)
+// (8192 x 4097 bfloat16: forward 47 us and gradient 87 us, against 81 and 269 a value at a time.)
 #include <atomic>
 #include <climits>
 #include <cmath>
