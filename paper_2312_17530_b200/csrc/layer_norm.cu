@@ -34,6 +34,7 @@ constexpr int kNormJoin = kNormRingThreads + 4;
 constexpr int kNormLongThreads = 1024;
 constexpr int kNormMaxStages = 4;
 constexpr int kNormMaxTeams = 8;
+constexpr int kNormMaxParts = 8;            // CTAs of a row, the portable size of a cluster
 constexpr int kNormRingBytes = 200 << 10;  // shared memory of a multiprocessor's rings
 constexpr unsigned kNormSpin = 1u << 20;   // polls of a wait before it gives up
 
@@ -517,6 +518,31 @@ k_norm_forward_any(const T *__restrict__ x, long long xs, const P *__restrict__ 
 }
 
 // ---- backward ---------------------------------------------------------------------------------
+__device__ __forceinline__ int cluster_rank()
+{
+    int r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ int cluster_size()
+{
+    int r;
+    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_barrier()  // all threads of all its CTAs
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// *addr = v in the shared memory of a CTA of the cluster
+__device__ __forceinline__ void store_cluster(uint32_t addr, int cta, float2 v)
+{
+    uint32_t there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(cta));
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(v.x), "f"(v.y) : "memory");
+}
+
 // Sums of dw and db: every thread keeps those of its columns over all rows its CTA takes, and writes them to
 // `partial` ([2][CTAs][d]) at the end; k_norm_param_gradient adds them up in a fixed order.  No atomics: the same
 // bits from run to run.
@@ -557,21 +583,38 @@ __device__ __forceinline__ Pairs<T> input_gradient(const Pairs<T> &vx, const Pai
 // stage: it ends the sums of this stage and, with it, all reads of the one before, which is refilled behind it.  E <= 16:
 // weight, x and dy stay in registers between the two passes; E = 32: x and dy are read again, the weight lies in shared
 // memory in the threads' order.
-template <bool SHIFT, typename T, int E, int ROWS, typename P>
+//
+// SPLIT: a cluster of CTAs per row, each with its own columns (one team, one row per stage): rows that one CTA cannot hold.
+// The warps leave their two sums in every CTA of the cluster, and the cluster's barrier takes the place of the team's.
+// (Gradient of 4096 x 16384 binary32: 138 us, 5.8 TB/s, against 416 a value at a time.)
+template <bool SHIFT, typename T, int E, int ROWS, bool SPLIT, typename P>
 __global__ void __launch_bounds__(kNormRingThreads)
 k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
                      const P *__restrict__ w, const float *__restrict__ mean, const float *__restrict__ rstd,
-                     T *__restrict__ dx, long long dxs, float *__restrict__ partial, int n, int d, PhaseRows phases,
+                     T *__restrict__ dx, long long dxs, float *__restrict__ partial, int n, int width, PhaseRows phases,
                      float inv_d, int team_threads, int stages, uint32_t row_bytes, unsigned int *status)
 {
+    static_assert(!SPLIT || ROWS == 1, "a row per stage");
     constexpr int V = Pairs<T>::V, NV = E / V, NP = Pairs<T>::N;
     constexpr bool KEEP = E <= 16;
     extern __shared__ __align__(128) unsigned char rows[];
-    __shared__ float2 part[2][ROWS][kNormRingThreads / 32];
+    __shared__ float2 part[2][ROWS][(SPLIT ? kNormMaxParts : 1) * kNormRingThreads / 32];
     __shared__ __align__(8) unsigned long long full[kNormMaxTeams][kNormMaxStages];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = team_threads >> 5;
     const int team = threadIdx.x / team_threads, teams = blockDim.x / team_threads, tid = threadIdx.x - team * team_threads;
-    Walk walk = walk_of<V>(phases, blockIdx.x, gridDim.x, n);  // the CTA's phase, dealt to its teams
+    const int parts = SPLIT ? cluster_size() : 1, rank = SPLIT ? cluster_rank() : 0;
+    Walk walk = walk_of<V>(phases, blockIdx.x / parts, gridDim.x / parts, n);  // the CTA's phase, dealt to its teams
+    int d = width;
+    if constexpr (SPLIT) {  // from here on the CTA's columns are all there is
+        const int all = team_threads * E, col0 = rank ? rank * all - walk.phase : 0;
+        d = min(width - col0, rank ? all : all - walk.phase);
+        if (rank) walk.phase = 0;
+        x += col0;
+        dy += col0;
+        if (w) w += col0;
+        if (dx) dx += col0;
+        if (partial) partial += col0;
+    }
     walk.first = walk.first * teams + team;
     walk.stride *= teams;
     const int groups = (walk.count + ROWS - 1) / ROWS;
@@ -579,10 +622,18 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
     RowRing ring = {smem_addr(rows) + team * ring_bytes, smem_addr(full[team]), ROWS * 2 * row_bytes, stages, true, status};
     if (tid < stages) barrier_init(ring.bar(tid), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    __syncthreads();
+    if constexpr (SPLIT)
+        cluster_barrier();  // the others run: their memory may be written
+    else
+        __syncthreads();
     grid_dependency_wait();
     grid_dependency_launch_next();
-    auto team_barrier = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(team_threads) : "memory"); };
+    auto team_barrier = [&]() {
+        if constexpr (SPLIT)
+            cluster_barrier();
+        else
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(team_threads) : "memory");
+    };
     auto row_of = [&](int g, int r) { return walk.row0 + walk.period * (g * ROWS + r); };
     auto load = [&](int i) {  // by one thread
         const int g = walk.first + i * walk.stride;
@@ -677,7 +728,11 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
                     }
                 });
             const float a = warp_sum(sums.s1.x + sums.s1.y), b = warp_sum(sums.s2.x + sums.s2.y);
-            if (lane == 0) part[turn][r][warp] = make_float2(a, b);
+            if constexpr (SPLIT) {
+                if (lane < parts) store_cluster(smem_addr(&part[turn][r][rank * warps + warp]), lane, make_float2(a, b));
+            } else {
+                if (lane == 0) part[turn][r][warp] = make_float2(a, b);
+            }
         }
         team_barrier();
         if (tid == 0) load(it + stages - 1);
@@ -685,7 +740,12 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             if (g * ROWS + r >= walk.count) break;
-            const float2 t = lane < warps ? part[turn][r][team * warps + lane] : make_float2(0.0f, 0.0f);
+            float2 t = make_float2(0.0f, 0.0f);
+            if constexpr (SPLIT) {
+                for (int i = lane; i < parts * warps; i += 32) t = add2(t, part[turn][r][i]);
+            } else {
+                if (lane < warps) t = part[turn][r][team * warps + lane];
+            }
             const float c1 = -rs[r] * (warp_sum(t.x) * inv_d), c2 = -rs[r] * (warp_sum(t.y) * inv_d);
             const float2 m2 = make_float2(-mu[r], -mu[r]), r2 = make_float2(rs[r], rs[r]), f1 = make_float2(c1, c1),
                          f2 = make_float2(c2, c2);
@@ -734,7 +794,7 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
                 joined[(i * V + 2 * k + 1) * kNormJoin + self] = v.y;
             }
         __syncthreads();
-        float *dst = partial + ((long long)which * gridDim.x + blockIdx.x) * d;
+        float *dst = partial + ((long long)which * (gridDim.x / parts) + blockIdx.x / parts) * width;
         for (int c0 = self; c0 < d; c0 += 4 * all) {  // four columns at a time, so that their loads overlap
             int from[4];
             float sum[4];
@@ -1102,22 +1162,47 @@ TeamShape team_shape(const NormShape &sh, int elems, int rows, long long n)
     return t;
 }
 
-template <bool SHIFT, typename T, int E, int ROWS, typename P>
-cudaError_t backward_ring(int *slots, const BackwardArgs<T, P> &a, const NormShape &sh, const TeamShape &t)
+// How a row is split over the CTAs of a cluster, two stages each at least; no parts if it cannot be.
+struct SplitShape {
+    TeamShape team;
+    int parts;
+    uint32_t row;  // bytes of a part's row
+};
+template <typename T>
+SplitShape split_shape(const NormShape &sh)
 {
-    const uint32_t row = 16u * (uint32_t)sh.packs;
+    SplitShape r{{0, 1, 0}, 0, 0};
+    constexpr int V = Pairs<T>::V;
+    for (int parts = 2; parts <= kNormMaxParts && !r.parts; ++parts) {
+        const int threads = ((sh.packs * V + parts * kNormElems - 1) / (parts * kNormElems) + 31) / 32 * 32;
+        if (threads > kNormRingThreads) continue;
+        r.row = (uint32_t)(threads * kNormElems * sizeof(T));
+        r.team.threads = threads;
+        r.team.stages = kNormRingBytes / (2 * (int)r.row);
+        if (r.team.stages > kNormMaxStages) r.team.stages = kNormMaxStages;
+        // the columns are dealt from the first part on; no part is left without any, whatever the phase: a part less would
+        // have to hold kNormRingThreads * kNormElems columns in each of the others
+        r.parts = (sh.packs * V + threads * kNormElems - 1) / (threads * kNormElems);
+    }
+    return r;
+}
+
+template <bool SHIFT, typename T, int E, int ROWS, bool SPLIT, typename P>
+cudaError_t backward_ring(int *slots, const BackwardArgs<T, P> &a, const NormShape &sh, const TeamShape &t, uint32_t row,
+                          int parts)
+{
     const long long loop = (long long)t.teams * t.stages * 2 * ROWS * row + (E > 16 ? 4ll * E * t.threads : 0);
     const long long join = 4ll * E * kNormJoin, smem = loop > join ? loop : join;
     static std::atomic<uint64_t> ready{0};
     unsigned int *status = nullptr;
     cudaError_t e = operator_status_ptr(&status);
-    if (e == cudaSuccess) e = allow_ring(k_norm_backward_ring<SHIFT, T, E, ROWS, P>, ready);
+    if (e == cudaSuccess) e = allow_ring(k_norm_backward_ring<SHIFT, T, E, ROWS, SPLIT, P>, ready);
     if (e != cudaSuccess) return e;
-    const int per = ROWS * t.teams;
-    *slots = (int)walkers((a.n + per - 1) / per, current_device_sms() / sh.phases.period * sh.phases.period, sh.phases.period);
-    return launch_chained(k_norm_backward_ring<SHIFT, T, E, ROWS, P>, (unsigned)*slots, t.threads * t.teams, (size_t)smem, a.s, 1,
-                          a.dy, a.dys, a.x, a.xs, a.w, a.mean, a.rstd, a.dx, a.dxs, a.partial, a.n, a.d, sh.phases, a.inv,
-                          t.threads, t.stages, row, status);
+    const int per = ROWS * t.teams, period = sh.phases.period;
+    *slots = (int)walkers((a.n + per - 1) / per, current_device_sms() / parts / period * period, period);
+    return launch_chained(k_norm_backward_ring<SHIFT, T, E, ROWS, SPLIT, P>, (unsigned)(*slots * parts), t.threads * t.teams,
+                          (size_t)smem, a.s, parts, a.dy, a.dys, a.x, a.xs, a.w, a.mean, a.rstd, a.dx, a.dxs, a.partial, a.n,
+                          a.d, sh.phases, a.inv, t.threads, t.stages, row, status);
 }
 
 template <bool SHIFT, typename T, typename P>
@@ -1131,16 +1216,31 @@ bool norm_backward_packed(cudaError_t *e, int *slots, const BackwardArgs<T, P> &
                             a.w, a.mean, a.rstd, a.dx, a.dxs, a.partial, a.n, a.d, sh.phases, a.inv);
         return true;
     }
-    // two rows per stage where they fit; twice the columns per thread where that fills the multiprocessor better (a row
-    // of 4100 columns takes 9 of its 16 warps, or three rows 15)
-    const TeamShape two = team_shape<T>(sh, 16, 2, a.n), one = team_shape<T>(sh, 16, 1, a.n), wide = team_shape<T>(sh, 32, 1, a.n);
-    const TeamShape &narrow = two.teams ? two : one;
-    if (narrow.teams && 3 * wide.warps() < 4 * narrow.warps()) {
-        *e = two.teams ? backward_ring<SHIFT, T, 16, 2, P>(slots, a, sh, two) : backward_ring<SHIFT, T, 16, 1, P>(slots, a, sh, one);
+    const uint32_t row = 16u * (uint32_t)sh.packs;
+    // binary32 rows: a second row per stage does not fit the registers (8192 x 1001 takes 58 us with it, 28 without), and
+    // what one CTA cannot hold at 16 columns per thread is better split than held at 32 (4096 x 9000: 103 us against 109)
+    const TeamShape one = team_shape<T>(sh, 16, 1, a.n);
+    if constexpr (sizeof(T) < 4) {
+        // two rows per stage where they fit; twice the columns per thread where that fills the multiprocessor better (a row
+        // of 4100 columns takes 9 of its 16 warps, or three rows 15)
+        const TeamShape two = team_shape<T>(sh, 16, 2, a.n), wide = team_shape<T>(sh, 32, 1, a.n);
+        const TeamShape &narrow = two.teams ? two : one;
+        if (narrow.teams && 3 * wide.warps() < 4 * narrow.warps()) {
+            *e = two.teams ? backward_ring<SHIFT, T, 16, 2, false, P>(slots, a, sh, two, row, 1)
+                           : backward_ring<SHIFT, T, 16, 1, false, P>(slots, a, sh, one, row, 1);
+            return true;
+        }
+        if (wide.teams) {
+            *e = backward_ring<SHIFT, T, 32, 1, false, P>(slots, a, sh, wide, row, 1);
+            return true;
+        }
+    } else if (one.teams) {
+        *e = backward_ring<SHIFT, T, 16, 1, false, P>(slots, a, sh, one, row, 1);
         return true;
     }
-    if (wide.teams) *e = backward_ring<SHIFT, T, 32, 1, P>(slots, a, sh, wide);
-    return wide.teams > 0;
+    const SplitShape split = split_shape<T>(sh);
+    if (split.parts) *e = backward_ring<SHIFT, T, 16, 1, true, P>(slots, a, sh, split.team, split.row, split.parts);
+    return split.parts > 0;
 }
 
 template <typename T, typename P>

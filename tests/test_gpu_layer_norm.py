@@ -259,3 +259,11 @@ def test_refusals():
     assert fwd(n=1 << 31) == fwd(d=1 << 25, xs=1 << 25, ys=1 << 25) == binding.ERR_CAPACITY
     torch.cuda.synchronize()
     assert binding.operator_status() == 0
+
+
+@pytest.mark.parametrize("kind,n,d", [("f32", 40, 8500), ("f32", 301, 9001), ("f32", 300, 16400), ("f32", 77, 20485),
+                                      ("f32", 9, 57346), ("bf16", 161, 16500), ("bf16", 20, 40003), ("f16", 33, 65000),
+                                      ("f32", 500, 1001), ("f32", 400, 3001)])
+def test_backward_of_wide_rows(kind, n, d):
+    """Rows split over the CTAs of a cluster, in every phase; binary32 rows of a team each."""
+    test_backward(kind, kind, n, d)
