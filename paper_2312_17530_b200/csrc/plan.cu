@@ -433,6 +433,7 @@ extern "C" int rsdgc_plan_create(const rsdgc_layer_desc *layers_host, int32_t n_
     if (device >= 0) {
         DeviceGuard guard(device);
         cudaError_t e = guard.err;
+        if (e == cudaSuccess) e = load_noalloc_kernels();
         if (e == cudaSuccess) e = upload(&p->d_layers, p->layers);
         if (e == cudaSuccess) e = upload(&p->d_items, p->items_dev);
         if (e == cudaSuccess) e = upload(&p->d_cta_begin_bulk, p->cta_begin_bulk);

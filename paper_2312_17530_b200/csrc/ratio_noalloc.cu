@@ -80,6 +80,19 @@ static cudaError_t noalloc_scratch_ptr(NoAllocScratch **out)
     return cudaSuccess;
 }
 
+// A kernel's code reaches the device when it is first asked for, and the driver may take memory for it: a plan's
+// creation asks for these, so that no later call does.
+cudaError_t load_noalloc_kernels()
+{
+    NoAllocScratch *sc = nullptr;
+    cudaFuncAttributes a;
+    cudaError_t e = noalloc_scratch_ptr(&sc);
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&a, k_ratio_noalloc<1>);
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&a, k_ratio_noalloc<2>);
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&a, k_ratio_noalloc<3>);
+    return e;
+}
+
 }  // namespace rsdgc
 
 using namespace rsdgc;

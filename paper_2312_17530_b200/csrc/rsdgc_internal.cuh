@@ -236,6 +236,7 @@ cudaError_t launch_compress_workers(rsdgc_plan *p, int n_workers, const void *co
                                     int64_t val_cap, int32_t *const *counts, uint32_t *keys_all, cudaStream_t s);
 cudaError_t launch_update_ratios(rsdgc_plan *p, const float *weights, long long n_keep,
                                  float *ratios, cudaStream_t s);
+cudaError_t load_noalloc_kernels();  // on the current device
 cudaError_t launch_decompress(rsdgc_plan *p, int n_workers, const int32_t *const *idx, const void *const *val,
                               const int32_t *const *counts, long long idx_cap, long long val_cap, float scale,
                               float *dense, bool assign, cudaStream_t s);
