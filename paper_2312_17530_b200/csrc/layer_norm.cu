@@ -3,11 +3,12 @@
 //   mean = sum x / D,  rstd = (sum (x - mean)^2 / D + eps)^(-1/2),  xhat = (x - mean) rstd,  y = xhat w + b
 //   dx = rstd (g w - mean(g w) - xhat mean(g w xhat)),  dw = sum_n g xhat,  db = sum_n g
 //
-// Bound: memory for binary32 rows (8192 x 8192: forward 98 us, 5.5 TB/s, gradient 137 us, 5.9 TB/s), the issue rate for
-// 16-bit rows (16384 x 4096 bfloat16: forward 53 us, 5.1 TB/s at 68 % of the issue slots, 19 instructions per value;
-// gradient of 16384 x 8192 158 us, 5.1 TB/s), the launch for a few rows (1 x 4096: 2.3 us).  So a row is read once, in
-// 16-byte packs, and its arithmetic runs on pairs of binary32 values.  The mean, then the centred squares (two reductions,
-// no cancellation), then the output.  All statistics and sums are binary32.
+// Bound: memory for binary32 rows (8192 x 8192: forward 98 us, 5.5 TB/s, gradient 137 us, 5.9 TB/s); the issue rate for
+// 16-bit rows forward (16384 x 4096 bfloat16: 53 us, 5.1 TB/s at 68 % of the issue slots, 19 instructions per value); the
+// latency between a row's passes for their gradient (16384 x 8192: 158 us, 5.1 TB/s; 55 % of the issue slots at 16384 x
+// 4096); the launch for a few rows (1 x 4096: 2.3 us).  So a row is read once, in 16-byte packs, and its arithmetic runs on
+// pairs of binary32 values.  The mean, then the centred squares (two reductions, no cancellation), then the output.  All
+// statistics and sums are binary32.
 //
 // Rows that do not start on 16-byte boundaries (an odd width, say) keep the packs: what a thread owns is a 16-byte
 // granule of memory, and with it columns shifted by the row's phase, the number of elements between the granule's start
