@@ -807,6 +807,9 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
 }
 
 // ---- the small kernels around the tiles -----------------------------------------------------------
+// Latency bounds them all: a few dependent loads and a launch.  Alone and with cold caches, at 2048 x 32000 x 2048 with
+// 64 targets: k_head_targets 8.7 us, k_head_scale 3.6, k_head_join 7.7, k_head_hidden_sum 8.0 (two parts, 42 MB, 5.2 TB/s);
+// in a stream each starts while the one before it ends.
 
 // Top logits -> per row the sorted vocabulary indices with their probabilities q (binary32 softmax of the k
 // logits / T) and sum q log q.  Entries with a negative index are left out; a row without entries gets +inf
@@ -1229,10 +1232,12 @@ int head_pairs(cudaError_t *e)
 
 // Tiles of 256 x 128, 256 x 256 or 256 x 512 (two accumulators) for a launch's jobs.  The wider the tile, the more products
 // an operand block serves (48 bytes per cycle and SM at the full MMA rate for 512 columns, 64 for 256) and the more work
-// the ring holds: forward 2048 x 32000 x 2048 takes 219 us with 512 columns against 286 with 256.  The narrower, the more
-// tiles there are to deal out: 64 x 8000 x 512, 32 tiles of 256 columns, takes 11.0 us against 13.8 with 512, and 25.5
-// against 31.2 backward.  Which is best follows from the cycles a tile takes (512 per contraction step and 256 columns,
-// some 3000 to empty an accumulator) dealt to the pairs of CTAs.
+// the ring holds: forward 2048 x 32000 x 2048 took 219 us with 512 columns against 286 with 256, measured side by side (174
+// by now).  The narrower, the more tiles there are to deal out: 64 x 8000 x 512, 32 tiles of 256 columns, took 11.0 us
+// against 13.8 with 512, and 25.5 against 31.2 backward; with 128 columns 10.0 and 24.9, and 5 x 1000 x 256 7.7 and 16.0
+// against 8.4 and 18.5 with 256.  Which is best follows from the cycles a tile takes (512 per contraction step and 256
+// columns, some 3000 to empty an accumulator; 1.25 and 1.6 times that for the lost operand reuse of 256 and 128 columns)
+// dealt to the pairs of CTAs.
 void choose_columns(HeadParams &p, int pairs)
 {
     double best = 0.0;
