@@ -446,6 +446,11 @@ int rsdgc_head_distill_backward(const void *hidden_dev, int64_t hidden_stride, c
  * results are invalid) and clears them. */
 int rsdgc_operator_status(void *stream, uint32_t *flags_host);
 
+/* Self-test of the operators' bounded waits: operator calls made from now on (by any thread) give up a wait after `polls`
+ * polls instead of 2^20, so that a few polls make waits run out although everything that they wait for is under way.  Such
+ * a call ends as any other; its results are invalid if RSDGC_STATUS_TIMEOUT is raised.  0 restores the limit.  INVALID: polls < 0 or > 2^20. */
+int rsdgc_selftest_operator_polls(int32_t polls);
+
 /* Waits for the stream, copies the device status word to *out_host and clears it. */
 int rsdgc_get_status(rsdgc_plan *plan, void *stream, rsdgc_status *out_host);
 

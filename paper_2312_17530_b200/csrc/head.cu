@@ -50,7 +50,6 @@ constexpr int kHeadThreads = 128 + 32 * kEpilogueWarps;  // producer, MMA, two i
 constexpr int kStagingBytes = 2048;  // per epilogue warp: 32 rows of 64 bytes on their way out
 constexpr int kHeadSmem = kRingBlocks * kBlockBytes + kEpilogueWarps * kStagingBytes + 1024;
 constexpr int kSlots = 4;                                // tiles announced ahead
-constexpr unsigned kHeadSpin = 1u << 20;                 // polls of a wait before it gives up
 constexpr int kMaxTargets = 1024;
 constexpr int kNoTarget = INT_MAX;
 constexpr int kMaxJobs = 3;
@@ -97,6 +96,7 @@ struct HeadParams {
     int *clear;              // counters of the launches after this one
     int n_clear;
     unsigned int *status;
+    unsigned polls;          // of a wait before it gives up
 };
 
 // ---- PTX ----------------------------------------------------------------------------------------
@@ -153,6 +153,11 @@ __device__ __forceinline__ void barrier_arrive_leader(uint32_t bar)
 __device__ __forceinline__ void store_in(uint32_t addr, int value, uint32_t rank)
 {
     asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(addr_in(addr, rank)), "r"(value) : "memory");
+}
+// `bytes` of a stage whose copies were announced and will not come
+__device__ __forceinline__ void barrier_complete(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
 {
@@ -405,6 +410,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
     __shared__ int slot_tile[kSlots];
     __shared__ uint32_t tmem_base;
     __shared__ volatile int dead;
+    // after a give-up: which CTAs had one; stages each CTA's producer issued, and its bytes in the latest of each place
+    __shared__ int failed[2], issued[2], sent[2][kMaxStages];
 
     const uint32_t ring = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -455,7 +462,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
         return false;
     };
     auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
-        for (unsigned i = 0; i < kHeadSpin; ++i) {
+        for (unsigned i = 0; i < p.polls; ++i) {
             if (barrier_try(bar, parity)) return true;
             if (dead) return false;
         }
@@ -464,7 +471,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
     // The pair's next tile, announced by the first CTA's producer `i` tiles after the first; -1 after a wait that gave up.
     auto next_tile = [&](int i) -> int {
         const uint32_t bar = smem_addr(&slot_full[i % kSlots]), parity = (uint32_t)(i / kSlots) & 1u;
-        for (unsigned n = 0; n < kHeadSpin; ++n) {
+        for (unsigned n = 0; n < p.polls; ++n) {
             if (barrier_try_cluster(bar, parity)) return *(volatile int *)&slot_tile[i % kSlots];
             if (dead) return -1;
         }
@@ -502,6 +509,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                     const int kc = (tp.k0 + k) * kStepK;
                     if (elect_one()) {
                         if (rank == 0) barrier_expect(smem_addr(&full[stage]), bytes);
+                        sent[rank][stage] = (int)(bytes / 2);
                         if (a_mn) {
                             load_box(dst, &j.a, ra, kc, bar);
                             load_box(dst + kBoxBytes, &j.a, ra + 64, kc, bar);
@@ -557,11 +565,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                     parity ^= 1u;
                 }
             }
-            if (!ok && rank == 0)  // what is still in flight lands in this pair's shared memory: wait for it (bounded)
-                for (int i = it < stages ? 0 : it - stages; i < it; ++i) {
-                    const uint32_t bar = smem_addr(&full[i % stages]), ph = (uint32_t)(i / stages) & 1u;
-                    for (unsigned n = 0; n < kHeadSpin && !barrier_try(bar, ph); ++n) {}
-                }
+            if (lane == 0) issued[rank] = it;
         }
         if (warp == 1 && rank == 0) {  // ---- MMA, the pair's first CTA: the warp walks together, one thread issues
             int stage = 0, sub = 0;    // sub: accumulators used so far; they alternate
@@ -634,11 +638,6 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 if (!ok) break;
                 if (elect_one()) barrier_arrive_leader(smem_addr(&slot_empty[i % kSlots]));
                 __syncwarp();
-            }
-            if (!ok) {  // the MMAs issued so far still read shared memory and write TMEM: let them end (bounded)
-                if (elect_one()) mma_commit_both(smem_addr(&drain));
-                __syncwarp();
-                for (unsigned n = 0; n < kHeadSpin && !barrier_try(smem_addr(&drain), 0); ++n) {}
             }
         }
     } else {  // ---- epilogue: a thread owns one row and a quarter of an accumulator's columns
@@ -801,7 +800,36 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
     }
     __syncwarp();
     __syncthreads();
+    if (threadIdx.x < 2) store_in(smem_addr(&failed[rank]), dead, threadIdx.x);
+    __syncwarp();
     cluster_sync_all();  // the peer may still signal this CTA's barriers, and its MMAs read this CTA's memory
+    if (failed[0] | failed[1]) {
+        // A wait gave up in one of the CTAs, and both have left their loops: what they have in flight still reads and
+        // writes their shared memory and TMEM.  Let it end (bounded).
+        if (rank == 1 && warp == 0 && lane <= stages)
+            store_in(lane < stages ? smem_addr(&sent[1][lane]) : smem_addr(&issued[1]), lane < stages ? sent[1][lane] : issued[1], 0);
+        __syncwarp();
+        cluster_sync_all();
+        if (warp == 0 && rank == 0 && lane < stages) {
+            // a lane per place in the ring, its latest stage `i`; a producer is at most a ring ahead of the other, so that the
+            // barrier is in that stage's phase and lacks at most what only one of the two has issued
+            const int most = max(issued[0], issued[1]), i = most - 1 - (most - 1 - lane + stages) % stages;
+            if (i >= 0 && i < most) {
+                const uint32_t bar = smem_addr(&full[lane]);
+                if (i >= issued[1]) barrier_complete(bar, (uint32_t)sent[0][lane]);
+                if (i >= issued[0]) barrier_expect(bar, (uint32_t)sent[1][lane]);
+                for (unsigned n = 0; n < kOperatorPolls && !barrier_try(bar, (uint32_t)(i / stages) & 1u); ++n) {}
+            }
+        }
+        if (warp == 1) {
+            if (rank == 0 && elect_one()) mma_commit_both(smem_addr(&drain));  // by the thread that issued them
+            __syncwarp();
+            for (unsigned n = 0; n < kOperatorPolls && !barrier_try(smem_addr(&drain), 0); ++n) {}
+        }
+        __syncwarp();
+        __syncthreads();
+        cluster_sync_all();
+    }
     if (warp == 2)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem_base));
 }
@@ -1360,6 +1388,7 @@ int head_forward(const HeadCall &c, float *loss, float *lse)
     HeadParams p;
     std::memset(&p, 0, sizeof p);
     cudaError_t e = operator_status_ptr(&p.status);
+    p.polls = operator_polls();
     common_params(p, c, L);
     p.n_jobs = 1;
     p.partial = (float2 *)(c.workspace + L.partial);
@@ -1467,6 +1496,7 @@ int head_backward(const HeadCall &c, const float *lse, const float *grad, void *
     HeadParams p;
     std::memset(&p, 0, sizeof p);
     e = operator_status_ptr(&p.status);
+    p.polls = operator_polls();
     common_params(p, c, L);
     p.lse = lse;
     p.grad = grad;

@@ -1,4 +1,5 @@
 // What the language-model operators share on the host: the per-device status word, NVTX ranges, results.
+#include <atomic>
 #include <mutex>
 
 #include "operators_internal.cuh"
@@ -12,7 +13,10 @@ namespace rsdgc {
 namespace {
 constexpr int kMaxDevices = 64;
 __device__ unsigned int g_operator_status;
+std::atomic<unsigned> g_polls{kOperatorPolls};
 }  // namespace
+
+unsigned operator_polls() { return g_polls.load(std::memory_order_relaxed); }
 
 cudaError_t operator_status_ptr(unsigned int **out)
 {
@@ -70,6 +74,13 @@ int operator_result(cudaError_t e)
 }  // namespace rsdgc
 
 using namespace rsdgc;
+
+extern "C" int rsdgc_selftest_operator_polls(int32_t polls)
+{
+    if (polls < 0 || polls > (int32_t)kOperatorPolls) return RSDGC_ERR_INVALID;
+    g_polls.store(polls ? (unsigned)polls : kOperatorPolls, std::memory_order_relaxed);
+    return RSDGC_OK;
+}
 
 extern "C" int rsdgc_operator_status(void *stream, uint32_t *flags_host)
 {

@@ -109,6 +109,11 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, uint32_
                  : "memory");
 }
 
+// Polls of a wait before it gives up.  operator_polls(): the limit of the launches to come, lower only in self-tests; what
+// waits for a kernel's own copies and MMAs in flight always has the full one.
+constexpr unsigned kOperatorPolls = 1u << 20;
+unsigned operator_polls();
+
 // The status word of calls that take no plan: one per device, raised by the kernels, read and cleared by
 // rsdgc_operator_status().  *out is its device address on the current device.
 cudaError_t operator_status_ptr(unsigned int **out);

@@ -1,0 +1,63 @@
+"""The operators' bounded waits: with a limit of a few polls a wait runs out although everything it waits for is under way.
+The call ends all the same with nothing of its own left in flight, the status word tells, and later calls give what they
+gave before."""
+import math
+
+import pytest
+import torch
+
+from paper_2312_17530_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture
+def polls():
+    yield binding.selftest_operator_polls
+    binding.selftest_operator_polls(0)
+
+
+def give_up_and_recover(polls, call, outputs):
+    """`call` with ever larger limits, each followed by a call without one; both have to end."""
+    assert binding.operator_status() == 0
+    call()
+    assert binding.operator_status() == 0
+    want = [t.clone() for t in outputs]
+    seen = 0
+    for limit in (1, 2, 3, 5, 9, 17, 33, 65, 129, 257):
+        for _ in range(4):
+            polls(limit)
+            call()
+            flags = binding.operator_status()
+            assert flags in (0, binding.STATUS_TIMEOUT)
+            seen |= flags
+            if not flags:
+                assert all(torch.equal(a, b) for a, b in zip(want, outputs))
+            polls(0)
+            for t in outputs:
+                t.fill_(3.0)
+            call()
+            assert binding.operator_status() == 0
+            assert all(torch.equal(a, b) for a, b in zip(want, outputs))
+    return seen
+
+
+def test_limits_are_checked(polls):
+    for bad in (-1, (1 << 20) + 1):
+        with pytest.raises(binding.RsdgcError) as e:
+            polls(bad)
+        assert e.value.code == binding.ERR_INVALID
+    polls(1 << 20)
+
+
+@pytest.mark.parametrize("n,v,d", [(60, 3000, 136), (700, 9000, 520)])
+def test_head_gradient(polls, n, v, d):
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    H = torch.randn(n, d, generator=gen, device="cuda").bfloat16()
+    W = (torch.randn(v, d, generator=gen, device="cuda") * (2 / math.sqrt(d))).bfloat16()
+    labels = torch.randint(0, v, (n,), generator=gen, device="cuda")
+    g, lse = torch.rand(n, generator=gen, device="cuda"), torch.logsumexp(H.float() @ W.float().T, 1)
+    dh, dw = torch.empty_like(H), torch.empty_like(W)
+    ws = torch.zeros(binding.head_workspace_bytes(n, v, d), dtype=torch.uint8, device="cuda")
+    seen = give_up_and_recover(polls, lambda: binding.head_loss_backward(H, W, labels, lse, g, dh, dw, ws), (dh, dw))
+    assert seen == binding.STATUS_TIMEOUT
