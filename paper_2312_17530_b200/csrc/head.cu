@@ -646,6 +646,12 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
         const RowsOut<T> out = {ring + kRingBlocks * kBlockBytes + (warp - 4) * kStagingBytes, lane};
         int sub = 0;
         bool ok = true;
+        // The four warps of a quad meet at a named barrier, which has no limit, once per accumulator of the forward pass.  So a
+        // warp that leaves its loop early (`dead` is set by then) arrives on the barrier that the others meet at next; they
+        // see `dead` behind it and leave too.
+        auto leave_quad = [&]() {
+            if (!BACK) asm volatile("bar.arrive %0, 128;" ::"r"(1 + quad) : "memory");
+        };
         TilePos tp = tile_pos(p, pair);
         start();
         if (BACK && blockIdx.x == 0)
@@ -776,6 +782,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                     const uint32_t slot = ring + kRingBlocks * kBlockBytes + ((sub & 1) * 4 * kHalf + quad * 32 + lane) * 8;
                     asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(slot + quarter * kHalf * 8), "f"(m), "f"(s) : "memory");
                     asm volatile("bar.sync %0, 128;" ::"r"(1 + quad) : "memory");
+                    ok = __all_sync(0xFFFFFFFFu, !dead);
+                    if (!ok) break;
                     const int part = tp.n * j.halves + h;
                     if (quarter == 0 && live && part < p.parts) {
 #pragma unroll
@@ -796,6 +804,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
             if (!ok) break;
             if (lane == 0) barrier_arrive_leader(smem_addr(&slot_empty[i % kSlots]));
         }
+        if (!ok) leave_quad();
         if (BACK && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();

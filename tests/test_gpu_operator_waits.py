@@ -61,3 +61,24 @@ def test_head_gradient(polls, n, v, d):
     ws = torch.zeros(binding.head_workspace_bytes(n, v, d), dtype=torch.uint8, device="cuda")
     seen = give_up_and_recover(polls, lambda: binding.head_loss_backward(H, W, labels, lse, g, dh, dw, ws), (dh, dw))
     assert seen == binding.STATUS_TIMEOUT
+
+
+@pytest.mark.parametrize("n,v,d,k", [(60, 3000, 136, 0), (700, 9000, 520, 0), (300, 20000, 264, 9), (60, 3000, 16384, 0),
+                                     (300, 5000, 16384, 9)])
+def test_head_forward(polls, n, v, d, k):
+    """The warps that join a row's columns leave together, whichever of them gave up first.  (A poll waits some microseconds
+    by itself: short contractions are over before the first ends.)"""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    H = torch.randn(n, d, generator=gen, device="cuda").bfloat16()
+    W = (torch.randn(v, d, generator=gen, device="cuda") * (2 / math.sqrt(d))).bfloat16()
+    ws = torch.zeros(binding.head_workspace_bytes(n, v, d, max(k, 1)), dtype=torch.uint8, device="cuda")
+    loss, lse = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    if k:
+        index = torch.randint(0, v, (n, k), generator=gen, device="cuda")
+        logit = torch.randn(n, k, generator=gen, device="cuda")
+        call = lambda: binding.head_distill_forward(H, W, index, logit, 2.0, loss, lse, ws)  # noqa: E731
+    else:
+        labels = torch.randint(0, v, (n,), generator=gen, device="cuda")
+        call = lambda: binding.head_loss_forward(H, W, labels, loss, lse, ws)  # noqa: E731
+    seen = give_up_and_recover(polls, call, (loss, lse))
+    assert seen == binding.STATUS_TIMEOUT or d < 16384
