@@ -695,6 +695,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 for (int at = 0; at < width; at += 32) {
                     const int col = col0 + at;
                     uint32_t raw[32];
+                    __syncwarp();  // lanes part over their rows' targets; the load is one of the whole warp
                     tmem_load32(src + at, raw);
                     tmem_wait_load(raw);
                     if (at + 32 == width) {  // the accumulator is read: the tile after the next may overwrite it
