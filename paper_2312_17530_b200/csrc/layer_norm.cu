@@ -37,7 +37,6 @@ constexpr int kNormMaxStages = 4;
 constexpr int kNormMaxTeams = 8;
 constexpr int kNormMaxParts = 8;            // CTAs of a row, the portable size of a cluster
 constexpr int kNormRingBytes = 200 << 10;  // shared memory of a multiprocessor's rings
-constexpr unsigned kNormSpin = 1u << 20;   // polls of a wait before it gives up
 
 // A 16-byte pack as pairs of binary32 values (f32x2 arithmetic: two values per instruction).
 template <typename T>
@@ -238,27 +237,39 @@ struct RowRing {
     uint32_t stage_bytes;
     int stages;
     bool arrived;          // false once a wait has given up: the results are void, as the status says
+    int step;              // a wait gives up after kOperatorPolls / step polls
     unsigned int *status;
 
     __device__ __forceinline__ uint32_t bar(int i) const { return full + 8 * (i % stages); }
     __device__ __forceinline__ uint32_t offset(int i) const { return (i % stages) * stage_bytes; }
     __device__ __forceinline__ uint32_t at(int i) const { return base + offset(i); }
-    // bounded; after a failure the others poll once
-    __device__ __forceinline__ void wait(int i)
+    // Bounded; after one that gave up the others poll once.  `lost` (shared): the stage whose wait gave up, set by the thread
+    // that fills the ring; it fills nothing more then, for a stage may be refilled only once its copies have arrived.
+    // TRY_FIRST: the loop's form decides how the rows' loop around it gets along with its registers.  Gradient of 16384 x 8192
+    // bfloat16 (weight in registers) 161 us with it, 174 without; of 8192 x 4097 (weight in shared memory) 96 and 91.
+    template <bool TRY_FIRST>
+    __device__ __forceinline__ void wait(int i, bool fills, int &lost)
     {
-        unsigned left = arrived ? kNormSpin : 1u;
+        int left = arrived ? (int)kOperatorPolls : 1;
         bool here = false;
-        while (left-- && !(here = barrier_try(bar(i), (uint32_t)(i / stages) & 1u))) {}
+        if constexpr (TRY_FIRST) {
+            do here = barrier_try(bar(i), (uint32_t)(i / stages) & 1u);
+            while (!here && (left -= step) > 0);
+        } else {
+            while (left > 0 && !(here = barrier_try(bar(i), (uint32_t)(i / stages) & 1u))) left -= step;
+        }
         if (!here && arrived) {
             arrived = false;
+            if (fills) lost = i;
             atomicOr(status, RSDGC_STATUS_TIMEOUT);
         }
     }
-    // copies under way after a failure land in this CTA's memory: wait for them (bounded)
-    __device__ __forceinline__ void drain(int from, int to) const
+    // After a failure, by the thread that filled the ring: the copies under way, of its last stages before `end`, land in this
+    // CTA's memory.
+    __device__ __forceinline__ void drain(int end) const
     {
-        for (int i = from < 0 ? 0 : from; i < to; ++i)
-            for (unsigned q = 0; q < kNormSpin && !barrier_try(bar(i), (uint32_t)(i / stages) & 1u); ++q) {}
+        for (int i = max(0, end - stages); i < end; ++i)
+            for (unsigned q = 0; q < kOperatorPolls && !barrier_try(bar(i), (uint32_t)(i / stages) & 1u); ++q) {}
     }
 };
 
@@ -375,15 +386,16 @@ template <bool SHIFT, typename T, typename P, int E>
 __global__ void __launch_bounds__(kNormRingThreads, E <= 16 ? 2 : 1)
 k_norm_forward_ring(const T *__restrict__ x, long long xs, const P *__restrict__ w, const P *__restrict__ b,
                     T *__restrict__ y, long long ys, float *__restrict__ mean, float *__restrict__ rstd, int n, int d,
-                    PhaseRows phases, float inv_d, float root_inv_d, float eps, int stages, uint32_t stage_bytes,
+                    PhaseRows phases, float inv_d, float root_inv_d, float eps, int stages, uint32_t stage_bytes, int step,
                     unsigned int *status)
 {
     constexpr int V = Pairs<T>::V, NV = E / V, NP = Pairs<T>::N;
     extern __shared__ __align__(128) unsigned char rows[];
     __shared__ float part[2][32];
     __shared__ __align__(8) unsigned long long full[kNormMaxStages];
+    __shared__ int lost;
     const Walk walk = walk_of<V>(phases, blockIdx.x, gridDim.x, n);
-    RowRing ring = {smem_addr(rows), smem_addr(full), stage_bytes, stages, true, status};
+    RowRing ring = {smem_addr(rows), smem_addr(full), stage_bytes, stages, true, step, status};
     if (threadIdx.x < stages) barrier_init(ring.bar(threadIdx.x), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
@@ -412,7 +424,7 @@ k_norm_forward_ring(const T *__restrict__ x, long long xs, const P *__restrict__
     for (int j = walk.first; j < walk.count; j += walk.stride, ++it) {
         const int row = walk.row0 + walk.period * j;
         const bool edge = row == 0 || row == n - 1;
-        ring.wait(it);
+        ring.wait<true>(it, threadIdx.x == 0, lost);
         Pairs<T> in[NV];
         float sum = 0.0f, sq = 0.0f;
         by_warp(cols.fast, [&](auto fast) {
@@ -427,16 +439,14 @@ k_norm_forward_ring(const T *__restrict__ x, long long xs, const P *__restrict__
         by_warp(cols.fast, [&](auto fast) { sq = squares_of<decltype(fast)::value>(in, cols, mu, root_inv_d); });
         const float r = rsqrtf(row_sum<false>(sq, part[1]) + eps);
         if (threadIdx.x == 0) {
-            load(it + stages);  // behind the statistics' barriers: every thread has read the stage
+            if (ring.arrived) load(it + stages);  // behind the statistics' barriers: every thread has read the stage
             if (mean) mean[row] = mu;
             if (rstd) rstd[row] = r;
         }
         by_warp(cols.fast, [&](auto fast) { write_row<decltype(fast)::value>(in, y + row * ys, cols, mu, r, wv, bv); });
     }
-    if (!ring.arrived && threadIdx.x == 0) {
-        const int mine = (walk.count - walk.first + walk.stride - 1) / walk.stride;
-        ring.drain(it - 1, min(mine, it + stages));
-    }
+    if (!ring.arrived && threadIdx.x == 0)
+        ring.drain(min((walk.count - walk.first + walk.stride - 1) / walk.stride, lost + stages));
 }
 
 // A warp per row, kNormWarps walkers per CTA; the next row is loaded while this one is reduced.  (16384 x 512 bfloat16:
@@ -594,7 +604,7 @@ __global__ void __launch_bounds__(kNormRingThreads)
 k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
                      const P *__restrict__ w, const float *__restrict__ mean, const float *__restrict__ rstd,
                      T *__restrict__ dx, long long dxs, float *__restrict__ partial, int n, int width, PhaseRows phases,
-                     float inv_d, int team_threads, int stages, uint32_t row_bytes, unsigned int *status)
+                     float inv_d, int team_threads, int stages, uint32_t row_bytes, int step, unsigned int *status)
 {
     static_assert(!SPLIT || ROWS == 1, "a row per stage");
     constexpr int V = Pairs<T>::V, NV = E / V, NP = Pairs<T>::N;
@@ -602,6 +612,7 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
     extern __shared__ __align__(128) unsigned char rows[];
     __shared__ float2 part[2][ROWS][(SPLIT ? kNormMaxParts : 1) * kNormRingThreads / 32];
     __shared__ __align__(8) unsigned long long full[kNormMaxTeams][kNormMaxStages];
+    __shared__ int lost[kNormMaxTeams];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = team_threads >> 5;
     const int team = threadIdx.x / team_threads, teams = blockDim.x / team_threads, tid = threadIdx.x - team * team_threads;
     const int parts = SPLIT ? cluster_size() : 1, rank = SPLIT ? cluster_rank() : 0;
@@ -621,7 +632,7 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
     walk.stride *= teams;
     const int groups = (walk.count + ROWS - 1) / ROWS;
     const uint32_t ring_bytes = stages * ROWS * 2 * row_bytes;
-    RowRing ring = {smem_addr(rows) + team * ring_bytes, smem_addr(full[team]), ROWS * 2 * row_bytes, stages, true, status};
+    RowRing ring = {smem_addr(rows) + team * ring_bytes, smem_addr(full[team]), ROWS * 2 * row_bytes, stages, true, step, status};
     if (tid < stages) barrier_init(ring.bar(tid), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if constexpr (SPLIT)
@@ -697,7 +708,7 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) mu[r] = nmu[r], rs[r] = nr[r];
         statistics(g + walk.stride);
-        ring.wait(it);
+        ring.wait<KEEP>(it, tid == 0, lost[team]);
         Pairs<T> px[KEEP ? ROWS : 1][KEEP ? NV : 1], pg[KEEP ? ROWS : 1][KEEP ? NV : 1];
         auto operands = [&](auto fast, int r, int i, Pairs<T> &vx, Pairs<T> &vg) {
             constexpr bool FAST = decltype(fast)::value;
@@ -737,7 +748,7 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
             }
         }
         team_barrier();
-        if (tid == 0) load(it + stages - 1);
+        if (tid == 0 && ring.arrived) load(it + stages - 1);
         if (!dx) continue;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
@@ -773,10 +784,8 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
             });
         }
     }
-    if (!ring.arrived && tid == 0) {
-        const int mine = (groups - walk.first + walk.stride - 1) / walk.stride;
-        ring.drain(it - 1, min(mine, it + stages - 1));
-    }
+    if (!ring.arrived && tid == 0)
+        ring.drain(min((groups - walk.first + walk.stride - 1) / walk.stride, lost[team] + stages - 1));
     if (!partial) return;
     // The teams' sums are added up in order, in the rings' memory (everything has arrived and been read): value e of a
     // thread's granules at [e][thread], 4 words of padding, so that neither the threads nor the columns' order meets a bank
@@ -1040,6 +1049,8 @@ int norm_slots(long long n)
 }
 int norm_slots_max() { return 6 * current_device_sms() + 8; }  // rounded up to a period
 
+int poll_step() { return (int)(kOperatorPolls / operator_polls()); }
+
 // Lets `kernel` have the rings' shared memory, once per device (`ready`: a bit per device).
 template <typename K>
 cudaError_t allow_ring(K kernel, std::atomic<uint64_t> &ready)
@@ -1099,7 +1110,7 @@ bool forward_ring(cudaError_t *e, const ForwardArgs<T, P> &a, const NormShape &s
                         walkers(a.n, (long long)ring.ctas * current_device_sms() / sh.phases.period * sh.phases.period,
                                 sh.phases.period),
                         threads, (size_t)ring.stages * 16 * sh.packs, a.s, 1, a.x, a.xs, a.w, a.b, a.y, a.ys, a.mean, a.rstd, a.n,
-                        a.d, sh.phases, a.inv, a.root, a.eps, ring.stages, 16u * (uint32_t)sh.packs, status);
+                        a.d, sh.phases, a.inv, a.root, a.eps, ring.stages, 16u * (uint32_t)sh.packs, poll_step(), status);
     return true;
 }
 
@@ -1205,7 +1216,7 @@ cudaError_t backward_ring(int *slots, const BackwardArgs<T, P> &a, const NormSha
     *slots = (int)walkers((a.n + per - 1) / per, current_device_sms() / parts / period * period, period);
     return launch_chained(k_norm_backward_ring<SHIFT, T, E, ROWS, SPLIT, P>, (unsigned)(*slots * parts), t.threads * t.teams,
                           (size_t)smem, a.s, parts, a.dy, a.dys, a.x, a.xs, a.w, a.mean, a.rstd, a.dx, a.dxs, a.partial, a.n,
-                          a.d, sh.phases, a.inv, t.threads, t.stages, row, status);
+                          a.d, sh.phases, a.inv, t.threads, t.stages, row, poll_step(), status);
 }
 
 template <bool SHIFT, typename T, typename P>

@@ -82,3 +82,18 @@ def test_head_forward(polls, n, v, d, k):
         call = lambda: binding.head_loss_forward(H, W, labels, loss, lse, ws)  # noqa: E731
     seen = give_up_and_recover(polls, call, (loss, lse))
     assert seen == binding.STATUS_TIMEOUT or d < 16384
+
+
+@pytest.mark.parametrize("kind,n,d", [(torch.float32, 2000, 1000), (torch.float32, 3000, 8200), (torch.bfloat16, 6000, 4100),
+                                      (torch.bfloat16, 6000, 8192), (torch.float16, 3000, 16500)])
+def test_layer_norm(polls, kind, n, d):
+    """Rows through the rings, the teams' and the clusters'."""
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    x, dy = (torch.randn(n, d, generator=gen, device="cuda").to(kind) for _ in range(2))
+    w = torch.randn(d, generator=gen, device="cuda").to(kind)
+    y, dx, dw, db = torch.empty_like(x), torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
+    mean, rstd = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    give_up_and_recover(polls, lambda: binding.layer_norm_forward(x, w, None, y, mean, rstd), (y, mean, rstd))
+    binding.layer_norm_forward(x, w, None, y, mean, rstd)
+    ws = torch.zeros(binding.layer_norm_workspace_bytes(n, d), dtype=torch.uint8, device="cuda")
+    give_up_and_recover(polls, lambda: binding.layer_norm_backward(dy, x, w, mean, rstd, dx, dw, db, ws), (dx, dw, db))
