@@ -403,13 +403,14 @@ int rsdgc_head_loss_forward(const void *hidden_dev, int64_t hidden_stride, const
  * Its gradient for a given d(sum)/d(loss[n]) = grad_loss[n] (binary32):
  *   dz[n][v] = grad_loss[n] * (exp(z[n][v] - lse[n]) - [v == labels[n]]),
  *   dhidden = dz weight,  dweight = dz^T hidden.
- * The logits are computed again, a piece of the vocabulary at a time.  dz is rounded to `dtype` as the two
- * products' operand, after one scaling for all tokens that brings the largest |grad_loss| to 2^13; the products add up in
- * binary32.  In binary16 the largest gradient so decides how much the others keep: a token whose |grad_loss| is 2^-k of the
- * largest keeps its probabilities down to 2^-(27-k) in full and loses those below 2^-(38-k); bfloat16 has no such limit.
- * dhidden: `dtype`; dweight: dweight_dtype, which is `dtype` or binary32 (then still with dz's rounding in
- * it); both are overwritten; any stride >= width.  n_tokens = 0 sets dweight to zero.  A row of hidden that
- * is not finite makes dweight NaN even where its label is negative (0 * NaN), as the formula does.
+ * The logits are computed again, a piece of the vocabulary at a time.  dz becomes the two products' operand in
+ * `dtype`, rounded, after one scaling for all tokens that brings the largest |grad_loss| to 2^13; with up to 128
+ * tokens it is kept as the rounded value and the rest, 16 bits each.  The products add up in binary32.  In binary16
+ * the largest gradient so decides how much the others keep: a token whose |grad_loss| is 2^-k of the largest keeps
+ * its probabilities down to 2^-(27-k) in full and loses those below 2^-(38-k); bfloat16 has no such limit.
+ * dhidden: `dtype`; dweight: dweight_dtype, which is `dtype` or binary32 (from 129 tokens on still with dz's
+ * rounding in it); both are overwritten; any stride >= width.  n_tokens = 0 sets dweight to zero.  A row of hidden
+ * that is not finite makes dweight NaN even where its label is negative (0 * NaN), as the formula does.
  * Errors: as above.
  */
 int rsdgc_head_loss_backward(const void *hidden_dev, int64_t hidden_stride, const void *weight_dev,

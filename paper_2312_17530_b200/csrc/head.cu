@@ -66,6 +66,8 @@ struct __align__(64) HeadJob {
     long long columns;       // of C
     int halves, cols;        // accumulators of a tile, and their columns: 256 x 512, 256 x 256 or 256 x 128 tiles
     int splits, split_steps; // parts of the contraction, each a tile of its own
+    int plane;               // few tokens: dz comes in two planes, the second one this many rows on; 0: in one
+    int plane_steps;         // dW: contraction steps of a plane
     int kind;
     int vocab;               // entries of the vocabulary this job is about (all, or a piece's)
     long long v0;            // first of them
@@ -300,6 +302,14 @@ __device__ __forceinline__ void subtract32(float (&z)[32], int i, float x)
     for (int j = 0; j < 32; ++j) z[j] -= i == j ? x : 0.0f;
 }
 
+// What rounding to T leaves of the values
+template <typename T>
+__device__ __forceinline__ void remainders(float (&z)[32])
+{
+#pragma unroll
+    for (int j = 0; j < 32; ++j) z[j] -= to_f32(from_f32<T>(z[j]));
+}
+
 // A row's targets from a column on, in ascending order; entry j of the rows lies at [j][row], so that a warp's rows, whose
 // places differ little, share the sectors they read.  The entry after the next is loaded ahead.
 struct Targets {
@@ -498,7 +508,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 const HeadJob &j = p.job[tp.job];
                 const int halves = j.halves, a_mn = j.a_mn, b_mn = j.b_mn;
                 const uint32_t bytes = 2u * (uint32_t)(kBlockBytes + halves * j.cols * kStepK);
-                const int ra = tp.m * kTile + (int)rank * kHalf;
+                // dh from two planes: a tile's second half is the second plane's rows
+                const int ra = tp.m * kTile + (int)rank * (j.plane && !a_mn ? j.plane : kHalf);
                 const int rb = tp.n * halves * j.cols + (int)rank * (j.cols >> 1);
                 const bool whole = j.cols == kTile;  // of an accumulator's columns a CTA holds half: one box or two
                 // coordinates of a box: (k, row), or (row, k) where the rows are contiguous
@@ -506,13 +517,17 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                     ok = wait_warp(smem_addr(&empty[stage]), parity ^ 1u);
                     if (!ok) break;
                     const uint32_t bar = leader_addr(smem_addr(&full[stage])), dst = ring + stage * stage_bytes;
-                    const int kc = (tp.k0 + k) * kStepK;
+                    int kc = (tp.k0 + k) * kStepK, ka = kc;
+                    if (a_mn && j.plane && tp.k0 + k >= j.plane_steps) {  // dW: the second plane, the same tokens again
+                        kc -= j.plane_steps * kStepK;
+                        ka = j.plane + kc;
+                    }
                     if (elect_one()) {
                         if (rank == 0) barrier_expect(smem_addr(&full[stage]), bytes);
                         sent[rank][stage] = (int)(bytes / 2);
                         if (a_mn) {
-                            load_box(dst, &j.a, ra, kc, bar);
-                            load_box(dst + kBoxBytes, &j.a, ra + 64, kc, bar);
+                            load_box(dst, &j.a, ra, ka, bar);
+                            load_box(dst + kBoxBytes, &j.a, ra + 64, ka, bar);
                         } else {
                             load_box(dst, &j.a, kc, ra, bar);
                             load_box(dst + kBoxBytes, &j.a, kc, ra + 64, bar);
@@ -680,6 +695,9 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                 }
             }
             const float back = BACK && !logits ? p.scale[1] : 1.0f;
+            // where the rows go: dh of the second plane is a part of its own
+            const bool apart = BACK && j.plane && j.kind == kHiddenGrad;
+            [[maybe_unused]] const int out_row0 = apart ? quad * 32 : row0, out_part = apart ? 2 * tp.split + (int)rank : tp.split;
             for (int h = 0; h < j.halves; ++h, ++sub) {
                 const int acc = sub & 1;
                 const int col0 = (tp.n * j.halves + h) * j.cols + quarter * width;
@@ -772,11 +790,17 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                             out.put16(z);
                         } else {
                             out.template put32<0>(z);
-                            out.flush(j, row0, col, tp.split);
+                            out.flush(j, out_row0, col, out_part);
                             out.wait_free();
                             out.template put32<1>(z);
                         }
-                        out.flush(j, row0, j.out_mode == kOut16 ? col : col + 16, tp.split);
+                        out.flush(j, out_row0, j.out_mode == kOut16 ? col : col + 16, out_part);
+                        if (logits && j.plane) {
+                            remainders<T>(z);
+                            out.wait_free();
+                            out.put16(z);
+                            out.flush(j, row0, col, 1);
+                        }
                     }
                 }
                 if constexpr (!BACK) {  // the row's four quarters are joined before they leave
@@ -1156,8 +1180,15 @@ constexpr int64_t kPieceMin = 2048;
 // with 5, 331 with 10).
 constexpr int64_t kSplitTiles = 37, kSplitSteps = 8;
 
+// With few tokens there is little to average a rounding out over: a row of dW is one dz times a row of h where a token stands
+// alone.  dz is then kept in two planes of 16 bits, the rounded values and what the rounding left (16 bits together in bfloat16,
+// 22 in binary16).  Up to kHalf tokens that costs no product more: the second plane takes a tile's empty second half for dh, and
+// as many contraction steps again for dW, whose tiles are bound by their stores.  (64 x 8000 x 512, binary16, forward and
+// backward: FIGURE.)
+constexpr int64_t kFewTokens = kHalf;
+
 struct HeadLayout {
-    int64_t piece, pieces, splits;
+    int64_t piece, pieces, splits, planes;
     int64_t partial, target_z, index, q, entropy, scale, counter, dz[2], dh_sum, bytes;
     int64_t dh_pitch;
 };
@@ -1165,7 +1196,8 @@ struct HeadLayout {
 HeadLayout head_layout(int64_t n, int64_t v, int64_t d, int64_t k)
 {
     HeadLayout L{};
-    int64_t most = kPieceBytes / (2 * (n > 0 ? n : 1)) / kTile * kTile;
+    L.planes = n <= kFewTokens ? 2 : 1;
+    int64_t most = kPieceBytes / (2 * L.planes * (n > 0 ? n : 1)) / kTile * kTile;
     if (most < kPieceMin) most = kPieceMin;
     L.pieces = (v + most - 1) / most;
     L.piece = up((v + L.pieces - 1) / L.pieces, kTile);
@@ -1191,9 +1223,9 @@ HeadLayout head_layout(int64_t n, int64_t v, int64_t d, int64_t k)
     L.partial = take(8 * n * ((v + kTile / 2 - 1) / (kTile / 2)));  // at most one per 128 columns
     L.bytes = at;
     at = shared;
-    L.dz[0] = take(2 * n * L.piece);
-    L.dz[1] = take(L.pieces > 1 ? 2 * n * L.piece : 0);
-    L.dh_sum = take(L.pieces > 1 || L.splits > 1 ? 4 * n * L.dh_pitch * L.splits : 0);
+    L.dz[0] = take(2 * L.planes * n * L.piece);
+    L.dz[1] = take(L.pieces > 1 ? 2 * L.planes * n * L.piece : 0);
+    L.dh_sum = take(L.pieces > 1 || L.splits * L.planes > 1 ? 4 * n * L.dh_pitch * L.splits * L.planes : 0);
     if (at > L.bytes) L.bytes = at;
     return L;
 }
@@ -1434,7 +1466,8 @@ struct HeadGrads {
 template <typename T>
 cudaError_t backward_pieces(const HeadCall &c, const HeadLayout &L, HeadParams &p, const HeadGrads &g)
 {
-    int parts = 1;
+    const int planes = (int)L.planes;
+    int parts = 1;  // of dh
     float *sum = (float *)(c.workspace + L.dh_sum);
     int *counter = (int *)(c.workspace + L.counter);
     for (int64_t i = 0; i <= L.pieces; ++i) {
@@ -1449,24 +1482,32 @@ cudaError_t backward_pieces(const HeadCall &c, const HeadLayout &L, HeadParams &
                         rows(i), c.d);
             j.v0 = i * L.piece;
             j.vocab = (int)rows(i);
-            if (e == cudaSuccess) e = set_output(j, kOut16, c.dtype, buffer(i), c.n, L.piece, L.piece);
+            j.plane = planes > 1 ? (int)c.n : 0;
+            if (e == cudaSuccess) e = set_output(j, kOut16, c.dtype, buffer(i), c.n, L.piece, L.piece, planes);
         }
         if (i > 0 && e == cudaSuccess) {
             const int64_t at = i - 1, v = rows(at);
             const void *dz = buffer(at);
             // the tiles of dz are whole: zeros beyond the vocabulary, so the contraction may run over whole steps
             HeadJob &j = p.job[p.n_jobs++];
-            e = set_job(j, kHiddenGrad, c.dtype, dz, false, c.n, L.piece, L.piece, weight(at), true, v, c.d, c.ws, c.n, c.d, v);
+            e = set_job(j, kHiddenGrad, c.dtype, dz, false, planes * c.n, L.piece, L.piece, weight(at), true, v, c.d, c.ws, c.n, c.d, v);
+            j.plane = planes > 1 ? (int)c.n : 0;
             j.split_steps = (j.k_steps + (int)L.splits - 1) / (int)L.splits;
             j.splits = (j.k_steps + j.split_steps - 1) / j.split_steps;
-            if (at == 0) parts = j.splits;  // the other pieces are no longer: they have no more parts
+            if (at == 0) parts = planes * j.splits;  // the other pieces are no longer: they have no more parts
             if (e == cudaSuccess)
                 e = L.pieces == 1 && parts == 1
                         ? set_output(j, kOut16, c.dtype, g.dh, c.n, c.d, g.dh_stride)
                         : set_output(j, at == 0 ? kOutF32 : kOutAddF32, c.dtype, sum, c.n, c.d, L.dh_pitch, parts);
             if (e == cudaSuccess) {
                 HeadJob &w = p.job[p.n_jobs++];
-                e = set_job(w, kWeightGrad, c.dtype, dz, true, c.n, L.piece, L.piece, c.hidden, true, c.n, c.d, c.hs, v, c.d, c.n);
+                e = set_job(w, kWeightGrad, c.dtype, dz, true, planes * c.n, L.piece, L.piece, c.hidden, true, c.n, c.d, c.hs, v, c.d,
+                            c.n);
+                if (planes > 1) {  // the tokens twice; what lies beyond them in a plane meets the zeros beyond them in h
+                    w.plane = (int)c.n;
+                    w.plane_steps = w.k_steps;
+                    w.k_steps = w.split_steps = 2 * w.k_steps;
+                }
                 const bool wide = g.dw_dtype == RSDGC_F32;
                 if (e == cudaSuccess)
                     e = set_output(w, wide ? kOutF32 : kOut16, c.dtype,
