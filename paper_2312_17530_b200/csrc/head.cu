@@ -1370,7 +1370,7 @@ cudaError_t launch_tiles(HeadParams &p, int *counter, cudaStream_t s)
     return launch_chained(k_head<BACK, T>, 2 * pairs, kHeadThreads, kHeadSmem, s, 2, p);
 }
 
-constexpr double kTruncationBf16 = 0.26, kTruncationF16 = 0.29;
+constexpr double kTruncationBf16 = 0.26, kTruncationF16 = 0.27;
 constexpr int kBand = 16;
 cudaError_t set_job(HeadJob &j, int kind, int dtype, const void *a, bool a_mn, long long ar, long long ac, long long as,
                     const void *b, bool b_mn, long long br, long long bc, long long bs, long long m, long long n, long long k)
@@ -1411,9 +1411,13 @@ void common_params(HeadParams &p, const HeadCall &c, const HeadLayout &L)
 {
     p.n = (int)c.n;
     p.vocab_total = c.v;
-    // The tensor core truncates its running sum: a step of 16 terms takes about kTruncation * 2^-24 of the final value
-    // off it (measured on sums of 512 to 8192 terms; 4.2e-6 of z at 4096 before, 1.1e-6 after).  The exponent's factor
-    // puts the mean of that back.
+    // The tensor core truncates its running sum, so that a step of 16 terms takes a part of 2^-24 off it, towards zero.  What a
+    // whole sum loses depends on how it grows: per step and in 2^-24 of the final value 0.21 to 0.27 (bfloat16) or 0.22 to 0.28
+    // (binary16) for terms of random signs, at every width from 256 to 2^20; 0.3 to 0.9 where the terms lean to one sign, 0.5
+    // to 1.8 where all have one; 0.05 to 0.2 where most comes from the last eighth of the columns.  The exponent's factor puts
+    // back what random signs lose (root mean square over 4096 bfloat16 columns 4.5e-6 of z without it, 2.2e-6 with it; leaning
+    // 5.8e-6 and 1.8e-6), less than the other forms lose except for the last, where the factor is most of what is left (0.95e-6
+    // without it, 3.0e-6 with it).  All of it lies within the products' bound, 2^-23 of |h| |W| per step.
     const double steps = (double)((c.d + 15) / 16), lost = c.dtype == RSDGC_BF16 ? kTruncationBf16 : kTruncationF16;
     p.c2 = (float)(1.4426950408889634 / c.temperature * (1.0 + lost * steps * 0x1p-24));
     p.labels = c.labels;
