@@ -1039,15 +1039,32 @@ unsigned walkers(long long rows, long long most, int period)
     return (unsigned)g;
 }
 
-// CTAs whose sums of dw and db are added up at the end: what they write and what is read again stays under a tenth of
-// the rows' own traffic (16 bytes per slot and column against 6 per row and column), unless rows are few.
-int norm_slots(long long n)
+// Slots: CTAs whose sums of dw and db are added up at the end; at most one per multiprocessor in the ring, kNormAnySlots in the
+// general form, two to three per multiprocessor in the warp's form: what they write and what is read again, 16 bytes per slot
+// and column, stays under a tenth of the rows' own traffic, 6 bytes per row and column, unless rows are few.  Multiprocessors
+// beyond a B200's 148 get no slots, so that the workspace's size does not depend on the device.
+constexpr int kNormSlotSms = 148;
+constexpr int kNormAnySlots = 64;
+constexpr int kNormMaxPeriod = 8;
+int slot_sms()
 {
-    const long long few = 2ll * current_device_sms(), most = 6ll * current_device_sms();
-    const long long s = n / 27 > few ? n / 27 : few;
-    return (int)(s < most ? s : most);
+    const int sms = current_device_sms();
+    return sms < kNormSlotSms ? sms : kNormSlotSms;
 }
-int norm_slots_max() { return 6 * current_device_sms() + 8; }  // rounded up to a period
+int warp_slots(long long n)
+{
+    const long long few = 2ll * slot_sms(), most = 3ll * slot_sms(), s = n / 27;
+    return (int)(s < few ? few : s < most ? s : most);
+}
+// The most that a gradient of n rows may use, whatever their layout and width: a row per CTA of the ring, a row per warp,
+// rounded up to a period; one for none.
+int64_t norm_slots(int64_t n)
+{
+    const int64_t ring = n < kNormSlotSms ? n : kNormSlotSms, rows = (n + kBackWarps - 1) / kBackWarps,
+                  warp = rows < 3 * kNormSlotSms ? rows : 3 * kNormSlotSms, most = ring > warp ? ring : warp;
+    static_assert(kNormAnySlots <= kNormSlotSms, "the general form has no more than the ring");
+    return most ? (most + kNormMaxPeriod - 1) / kNormMaxPeriod * kNormMaxPeriod : 1;
+}
 
 int poll_step() { return (int)(kOperatorPolls / operator_polls()); }
 
@@ -1213,7 +1230,7 @@ cudaError_t backward_ring(int *slots, const BackwardArgs<T, P> &a, const NormSha
     if (e == cudaSuccess) e = allow_ring(k_norm_backward_ring<SHIFT, T, E, ROWS, SPLIT, P>, ready);
     if (e != cudaSuccess) return e;
     const int per = ROWS * t.teams, period = sh.phases.period;
-    *slots = (int)walkers((a.n + per - 1) / per, current_device_sms() / parts / period * period, period);
+    *slots = (int)walkers((a.n + per - 1) / per, slot_sms() / parts / period * period, period);
     return launch_chained(k_norm_backward_ring<SHIFT, T, E, ROWS, SPLIT, P>, (unsigned)(*slots * parts), t.threads * t.teams,
                           (size_t)smem, a.s, parts, a.dy, a.dys, a.x, a.xs, a.w, a.mean, a.rstd, a.dx, a.dxs, a.partial, a.n,
                           a.d, sh.phases, a.inv, t.threads, t.stages, row, poll_step(), status);
@@ -1223,9 +1240,7 @@ template <bool SHIFT, typename T, typename P>
 bool norm_backward_packed(cudaError_t *e, int *slots, const BackwardArgs<T, P> &a, const NormShape &sh)
 {
     if (sh.packs <= 32 * kNormElems / Pairs<T>::V) {
-        long long most = 3ll * current_device_sms();
-        if (most > norm_slots(a.n)) most = norm_slots(a.n);
-        *slots = (int)walkers((a.n + kBackWarps - 1) / kBackWarps, most, sh.phases.period);
+        *slots = (int)walkers((a.n + kBackWarps - 1) / kBackWarps, warp_slots(a.n), sh.phases.period);
         *e = launch_chained(k_norm_backward_warp<SHIFT, T, P>, (unsigned)*slots, 32 * kBackWarps, 0, a.s, 1, a.dy, a.dys, a.x, a.xs,
                             a.w, a.mean, a.rstd, a.dx, a.dxs, a.partial, a.n, a.d, sh.phases, a.inv);
         return true;
@@ -1269,7 +1284,7 @@ cudaError_t norm_backward(const BackwardArgs<T, P> &a, void *dw, void *db, int g
             e = launch_chained(k_norm_backward_any<T, P>, (unsigned)a.n, kNormLongThreads, 0, a.s, 1, a.dy, a.dys, a.x, a.xs,
                                a.w, a.mean, a.rstd, a.dx, a.dxs, a.d, a.inv);
         if (e == cudaSuccess && a.partial) {
-            slots = a.n < 64 ? a.n : 64;
+            slots = a.n < kNormAnySlots ? a.n : kNormAnySlots;
             e = launch_chained(k_norm_columns_any<T>, dim3((unsigned)((a.d + 255) / 256), (unsigned)slots), 256, 0, a.s, 1,
                                a.dy, a.dys, a.x, a.xs, a.mean, a.rstd, a.partial, (long long)a.n, a.d);
         }
@@ -1313,7 +1328,7 @@ extern "C" int64_t rsdgc_layer_norm_workspace_bytes(int64_t n_rows, int64_t widt
 {
     if (n_rows < 0 || width < 1) return RSDGC_ERR_INVALID;
     if (n_rows > (1 << 30) || width > (1 << 24)) return RSDGC_ERR_CAPACITY;
-    return 2 * 4 * (int64_t)norm_slots_max() * width;
+    return 2 * 4 * norm_slots(n_rows) * width;
 }
 
 extern "C" int rsdgc_layer_norm_forward(const void *x_dev, int64_t x_stride, const void *weight_dev,
