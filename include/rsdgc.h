@@ -446,15 +446,18 @@ int rsdgc_head_distill_backward(const void *hidden_dev, int64_t hidden_stride, c
                                 void *dweight_dev, int64_t dweight_stride, int32_t dweight_dtype, int64_t n_tokens,
                                 int64_t vocab, int64_t width, int32_t dtype, void *workspace_dev, void *stream);
 
-/* Waits for the stream, copies the status bits that the operators above have raised on the current
- * device since the last call to *flags_host (RSDGC_STATUS_TIMEOUT: a bounded on-chip wait gave up,
- * results are invalid) and clears them. */
+/* Waits for the stream, reports the status bits that the operators above have raised on the current device since the last
+ * report (RSDGC_STATUS_TIMEOUT: a bounded on-chip wait gave up, results are invalid) and clears what it reports.  One
+ * word per device: whoever asks first is told, for all threads and streams; a bit raised meanwhile by another
+ * stream's kernel is either in this report or in the next. */
 int rsdgc_operator_status(void *stream, uint32_t *flags_host);
 
 /* Self-test of the operators' bounded waits: operator calls made from now on (by any thread) give up a wait after `polls`
  * polls instead of 2^20, so that a few polls make waits run out although everything that they wait for is under way.  Such
  * a call ends as any other; its results are invalid if RSDGC_STATUS_TIMEOUT is raised.  0 restores the limit.  INVALID: polls < 0 or > 2^20. */
 int rsdgc_selftest_operator_polls(int32_t polls);
+/* Makes a wait run out on `stream` that nothing will ever end (nothing is in flight either), after `polls` polls, 1 to 2^20. */
+int rsdgc_selftest_operator_wait(int32_t polls, void *stream);
 
 /* Waits for the stream, copies the device status word to *out_host and clears it. */
 int rsdgc_get_status(rsdgc_plan *plan, void *stream, rsdgc_status *out_host);

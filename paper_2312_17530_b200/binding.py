@@ -35,6 +35,7 @@ EXPORTS = [
     "rsdgc_layer_norm_workspace_bytes", "rsdgc_layer_norm_forward", "rsdgc_layer_norm_backward",
     "rsdgc_head_workspace_bytes", "rsdgc_head_loss_forward", "rsdgc_head_loss_backward", "rsdgc_head_distill_forward",
     "rsdgc_head_distill_backward", "rsdgc_selftest_operator_polls",
+    "rsdgc_selftest_operator_wait",
 ]
 NOALLOC_MAX_LAYERS = 64
 N_COMPRESS_KERNELS = 5
@@ -114,6 +115,7 @@ def lib():
         L.rsdgc_plan_tail_slices.restype = i64
         L.rsdgc_operator_status.argtypes = [vp, C.POINTER(u32)]
         L.rsdgc_selftest_operator_polls.argtypes = [i32]
+        L.rsdgc_selftest_operator_wait.argtypes = [i32, vp]
         L.rsdgc_layer_norm_workspace_bytes.argtypes = [i64, i64]
         L.rsdgc_layer_norm_workspace_bytes.restype = i64
         L.rsdgc_layer_norm_forward.argtypes = [vp, i64, vp, vp, vp, i64, vp, vp, i64, i64, i32, i32, f32, vp]
@@ -583,6 +585,11 @@ def operator_status() -> int:
 def selftest_operator_polls(polls: int = 0) -> None:
     """Operator calls made from now on give up a wait after ``polls`` polls (0: the library's own limit again)."""
     _check(lib().rsdgc_selftest_operator_polls(polls), "rsdgc_selftest_operator_polls")
+
+
+def selftest_operator_wait(polls: int = 256) -> None:
+    """A wait that runs out after ``polls`` polls on the current stream."""
+    _check(lib().rsdgc_selftest_operator_wait(polls, _stream()), "rsdgc_selftest_operator_wait")
 
 
 def launch_count() -> int:

@@ -14,6 +14,22 @@ namespace {
 constexpr int kMaxDevices = 64;
 __device__ unsigned int g_operator_status;
 std::atomic<unsigned> g_polls{kOperatorPolls};
+
+// Clears the bits that were read, and no others.
+__global__ void k_operator_status_clear(unsigned int *status, unsigned int seen) { atomicAnd(status, ~seen); }
+
+// The wait of the self-test: a barrier armed for bytes that nothing will deliver, with nothing in flight.
+__global__ void k_selftest_operator_wait(unsigned int *status, unsigned int polls)
+{
+    __shared__ __align__(8) unsigned long long bar;
+    barrier_init(smem_addr(&bar), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    barrier_expect(smem_addr(&bar), 16);
+    bool here = false;
+    for (unsigned i = 0; i < polls && !here; ++i) here = barrier_try(smem_addr(&bar), 0);
+    if (!here) atomicOr(status, RSDGC_STATUS_TIMEOUT);
+    asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(smem_addr(&bar)) : "memory");
+}
 }  // namespace
 
 unsigned operator_polls() { return g_polls.load(std::memory_order_relaxed); }
@@ -88,8 +104,29 @@ extern "C" int rsdgc_operator_status(void *stream, uint32_t *flags_host)
     unsigned int *p = nullptr;
     cudaStream_t s = (cudaStream_t)stream;
     cudaError_t e = operator_status_ptr(&p);
-    if (e == cudaSuccess) e = cudaMemcpyAsync(flags_host, p, sizeof(unsigned int), cudaMemcpyDeviceToHost, s);
-    if (e == cudaSuccess) e = cudaMemsetAsync(p, 0, sizeof(unsigned int), s);
+    unsigned int seen = 0;
+    if (e == cudaSuccess) e = cudaMemcpyAsync(&seen, p, sizeof(unsigned int), cudaMemcpyDeviceToHost, s);
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    // Kernels on other streams may raise bits meanwhile: only what this call reports is cleared.
+    if (e == cudaSuccess && seen) {
+        k_operator_status_clear<<<1, 1, 0, s>>>(p, seen);
+        e = cudaGetLastError();
+        count_launch(1);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    }
+    if (e == cudaSuccess) *flags_host = seen;
+    return operator_result(e);
+}
+
+extern "C" int rsdgc_selftest_operator_wait(int32_t polls, void *stream)
+{
+    if (polls < 1 || polls > (int32_t)kOperatorPolls) return RSDGC_ERR_INVALID;
+    unsigned int *p = nullptr;
+    cudaError_t e = operator_status_ptr(&p);
+    if (e == cudaSuccess) {
+        k_selftest_operator_wait<<<1, 1, 0, (cudaStream_t)stream>>>(p, (unsigned)polls);
+        e = cudaGetLastError();
+        count_launch(1);
+    }
     return operator_result(e);
 }

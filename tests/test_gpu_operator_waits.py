@@ -97,3 +97,34 @@ def test_layer_norm(polls, kind, n, d):
     binding.layer_norm_forward(x, w, None, y, mean, rstd)
     ws = torch.zeros(binding.layer_norm_workspace_bytes(n, d), dtype=torch.uint8, device="cuda")
     give_up_and_recover(polls, lambda: binding.layer_norm_backward(dy, x, w, mean, rstd, dx, dw, db, ws), (dx, dw, db))
+
+
+def test_status_is_reported_once_and_by_any_stream():
+    assert binding.operator_status() == 0
+    binding.selftest_operator_wait(300)
+    assert binding.operator_status() == binding.STATUS_TIMEOUT and binding.operator_status() == 0
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        binding.selftest_operator_wait(10)
+    side.synchronize()
+    assert binding.operator_status() == binding.STATUS_TIMEOUT and binding.operator_status() == 0
+    for bad in (0, -1, (1 << 20) + 1):
+        with pytest.raises(binding.RsdgcError) as e:
+            binding.selftest_operator_wait(bad)
+        assert e.value.code == binding.ERR_INVALID
+
+
+def test_no_status_is_lost_between_reading_and_clearing():
+    """Waits run out on one stream while another asks all the time: each of them is reported at the latest when all is over, and a
+    report that found nothing clears nothing."""
+    side, asks = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(50):
+        with torch.cuda.stream(side):
+            binding.selftest_operator_wait(1)
+        told = 0
+        with torch.cuda.stream(asks):
+            while not side.query():
+                told |= binding.operator_status()
+            told |= binding.operator_status()
+        assert told == binding.STATUS_TIMEOUT
+    assert binding.operator_status() == 0
