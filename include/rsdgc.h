@@ -172,10 +172,10 @@ int rsdgc_update_ratios(rsdgc_plan *plan, const float *weights_dev, float global
  * Limits: 1 <= n_layers <= RSDGC_NOALLOC_MAX_LAYERS, each layer below 2^31 elements; beyond
  *   them the call returns RSDGC_ERR_CAPACITY and does nothing.  Other errors: INVALID,
  *   ALIGNMENT, CUDA.
- * The first call on a device, or the creation of a plan on it, looks up the device address of
- * the scratch array and loads the kernels (with that device current): make one of them before
- * any stream capture begins.  The driver may take memory for the kernels' code when it loads
- * them; otherwise no call allocates or frees memory.
+ * The first call on a device looks up the device address of the scratch array and loads the
+ * kernels (with that device current; so do the creation of a plan on it and the first call of
+ * a language-model operator on it, before they load their own): make one of them before any
+ * stream capture begins.  No call allocates or frees memory.
  * All calls on a device share the scratch array, and it keeps what the previous call left in
  * it, so each call starts by clearing it on `stream`.  Two calls whose work overlaps on the
  * GPU (different streams, or different threads) race on it and give wrong ratios: order them.

@@ -1438,7 +1438,8 @@ int head_forward(const HeadCall &c, float *loss, float *lse)
     const HeadLayout L = head_layout(c.n, c.v, c.d, c.k ? c.k : 1);
     HeadParams p;
     std::memset(&p, 0, sizeof p);
-    cudaError_t e = operator_status_ptr(&p.status);
+    cudaError_t e = operators_ready();
+    if (e == cudaSuccess) e = operator_status_ptr(&p.status);
     p.polls = operator_polls();
     common_params(p, c, L);
     p.n_jobs = 1;
@@ -1555,7 +1556,8 @@ int head_backward(const HeadCall &c, const float *lse, const float *grad, void *
     const HeadLayout L = head_layout(c.n, c.v, c.d, c.k ? c.k : 1);
     HeadParams p;
     std::memset(&p, 0, sizeof p);
-    e = operator_status_ptr(&p.status);
+    e = operators_ready();
+    if (e == cudaSuccess) e = operator_status_ptr(&p.status);
     p.polls = operator_polls();
     common_params(p, c, L);
     p.lse = lse;

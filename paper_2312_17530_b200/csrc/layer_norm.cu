@@ -1346,7 +1346,9 @@ extern "C" int rsdgc_layer_norm_forward(const void *x_dev, int64_t x_stride, con
         !pointer_aligned(mean_dev, 4) || !pointer_aligned(rstd_dev, 4))
         return RSDGC_ERR_ALIGNMENT;
     OperatorRange range("rsdgc_layer_norm_forward");
-    const cudaError_t e = with_types(dtype, param_dtype, [&](auto t, auto p) {
+    cudaError_t e = operators_ready();
+    if (e != cudaSuccess) return operator_result(e);
+    e = with_types(dtype, param_dtype, [&](auto t, auto p) {
         typedef decltype(t) T;
         typedef decltype(p) P;
         return norm_forward<T, P>({(const T *)x_dev, x_stride, (const P *)weight_dev, (const P *)bias_dev, (T *)y_dev, y_stride,
@@ -1389,7 +1391,9 @@ extern "C" int rsdgc_layer_norm_backward(const void *dy_dev, int64_t dy_stride, 
         if (dbias_dev && e == cudaSuccess) e = cudaMemsetAsync(dbias_dev, 0, bytes, s);
         return operator_result(e);
     }
-    const cudaError_t e = with_types(dtype, param_dtype, [&](auto t, auto p) {
+    cudaError_t e = operators_ready();
+    if (e != cudaSuccess) return operator_result(e);
+    e = with_types(dtype, param_dtype, [&](auto t, auto p) {
         typedef decltype(t) T;
         typedef decltype(p) P;
         return norm_backward<T, P>({(const T *)dy_dev, dy_stride, (const T *)x_dev, x_stride, (const P *)weight_dev, mean_dev,

@@ -53,6 +53,19 @@ cudaError_t operator_status_ptr(unsigned int **out)
     return cudaSuccess;
 }
 
+cudaError_t operators_ready()
+{
+    static std::atomic<uint64_t> ready{0};
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    if (ready.load(std::memory_order_acquire) >> dev & 1) return cudaSuccess;
+    e = load_noalloc_kernels();
+    if (e == cudaSuccess) ready.fetch_or(1ull << dev, std::memory_order_release);
+    return e;
+}
+
 int current_device_sms()
 {
     static std::mutex mu;

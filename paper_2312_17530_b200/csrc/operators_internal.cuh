@@ -118,6 +118,10 @@ unsigned operator_polls();
 // rsdgc_operator_status().  *out is its device address on the current device.
 cudaError_t operator_status_ptr(unsigned int **out);
 
+// Every entry point's first step: on a device's first call loads the kernels of the entry point that promises to allocate
+// nothing, before the operators' own kernels use up the room that the driver has set aside for code.
+cudaError_t operators_ready();
+
 // Multiprocessors of the current device, asked once per device.
 int current_device_sms();
 
