@@ -389,7 +389,8 @@ int rsdgc_layer_norm_backward(const void *dy_dev, int64_t dy_stride, const void 
  * strides multiples of 8 (any width).  labels: int64; a negative label means "no loss here" (loss 0, no
  * gradient), one >= vocab gives a NaN loss and no gradient.  loss, lse: binary32; lse is what the
  * backward pass takes and may be NULL.  workspace_dev: rsdgc_head_workspace_bytes() bytes with
- * n_targets = 1, 256-byte aligned; nothing in it has to survive between calls.
+ * n_targets = 1, 256-byte aligned; nothing in it has to survive between calls.  One sized for a call does for calls with
+ * fewer tokens or targets.
  * Accuracy: the logits are sums of the tensor cores, binary32 but truncated after every 16 terms, each off by up to
  * width / 16 * 2^-23 of sum |hidden| |weight|; the mean of that is put back for terms of random signs.
  * Errors: INVALID (a needed pointer NULL, stride < width, sizes < 1, types), ALIGNMENT,

@@ -1219,7 +1219,7 @@ HeadLayout head_layout(int64_t n, int64_t v, int64_t d, int64_t k)
     L.q = take(4 * n * k);
     L.entropy = take(4 * n);
     L.scale = take(8);
-    L.counter = take(4 * L.pieces);
+    L.counter = take(4 * ((v + kPieceMin - 1) / kPieceMin));  // a piece each
     const int64_t shared = at;  // the forward pass's partials and the backward pass's dz share the rest
     L.partial = take(8 * n * ((v + kTile / 2 - 1) / (kTile / 2)));  // at most one per 128 columns
     L.bytes = at;
@@ -1229,6 +1229,32 @@ HeadLayout head_layout(int64_t n, int64_t v, int64_t d, int64_t k)
     L.dh_sum = take(L.pieces > 1 || L.splits * L.planes > 1 ? 4 * n * L.dh_pitch * L.splits * L.planes : 0);
     if (at > L.bytes) L.bytes = at;
     return L;
+}
+
+// What a call of n tokens, or fewer, needs at most: fewer tokens may come in more parts, in two planes, or in fewer and larger
+// pieces.  The layout's own sizes where they grow with n, bounds of the others'.
+int64_t head_bytes(int64_t n, int64_t v, int64_t d, int64_t k)
+{
+    const HeadLayout L = head_layout(n, v, d, k);
+    const int64_t few = n < kFewTokens ? n : kFewTokens, rows = n > 2 * few ? n : 2 * few;  // of dz's planes
+    // dz: one buffer of the whole vocabulary, or two of at most a piece
+    const int64_t whole = 2 * rows * up(v, kTile), least = 2 * rows * kPieceMin, piece = least > kPieceBytes ? least : kPieceBytes;
+    int64_t dz = whole;
+    if (whole > kPieceBytes && v > kPieceMin) {
+        dz = whole + 2 * 2 * rows * kTile;
+        if (dz > 2 * piece) dz = 2 * piece;
+    }
+    // dh's parts: n ceil(kSplitTiles / (m across)) rows for n <= m kTile tokens
+    const int64_t across = (tiles_of(d) + 1) / 2, longest = up(v, kTile) / kStepK / kSplitSteps;
+    int64_t most = (kSplitTiles + across - 1) / across;
+    if (most > longest) most = longest > 1 ? longest : 1;
+    int64_t parts = 2 * few * most;
+    if (n > kFewTokens && (most > 1 || L.pieces > 1)) {
+        const int64_t spread = (kTile * kSplitTiles + across - 1) / across + n, all = n * most < spread ? n * most : spread;
+        if (all > parts) parts = all;
+    }
+    const int64_t back = L.partial + up(dz, 256) + 256 + up(4 * parts * L.dh_pitch, 256);
+    return back > L.bytes ? back : L.bytes;
 }
 
 int head_check(int64_t n, int64_t v, int64_t d, int64_t k)
@@ -1582,7 +1608,7 @@ using namespace rsdgc;
 extern "C" int64_t rsdgc_head_workspace_bytes(int64_t n_tokens, int64_t vocab, int64_t width, int64_t n_targets)
 {
     const int rc = head_check(n_tokens, vocab, width, n_targets);
-    return rc ? rc : head_layout(n_tokens, vocab, width, n_targets).bytes;
+    return rc ? rc : head_bytes(n_tokens, vocab, width, n_targets);
 }
 
 extern "C" int rsdgc_head_loss_forward(const void *hidden_dev, int64_t hidden_stride, const void *weight_dev,

@@ -22,3 +22,22 @@ def test_layer_norm_workspace_follows_the_rows():
     assert size(4, 1 << 20) <= 64 << 20
     rows = [1, 2, 7, 8, 9, 63, 100, 148, 149, 1000, 1184, 1185, 3000, 3551, 4000, 1 << 20]
     assert sorted(size(n, 100) for n in rows) == [size(n, 100) for n in rows]
+
+
+@pytest.mark.parametrize("v", [1, 500, 2048, 2049, 20000, 128000, 600000])
+@pytest.mark.parametrize("d", [8, 512, 513, 2000, 8192, 20000])
+def test_head_workspace_does_for_fewer_tokens(v, d):
+    """The last batch is often a smaller one."""
+    size = binding.lib().rsdgc_head_workspace_bytes
+    n = list(range(0, 1600)) + list(range(1600, 40000, 509)) + [16383, 16384, 16385, 32768, 32769]
+    got = [size(t, v, d, 3) for t in sorted(n)]
+    assert got[0] >= 0 and got == sorted(got)
+    for t in (1, 100, 128, 129, 2000):
+        assert size(t, v, d, 1) <= size(t, v, d, 2) <= size(t, v, d, 100)
+
+
+def test_head_workspace_stays_small():
+    size = binding.head_workspace_bytes
+    assert size(64, 8000, 512) <= 16 << 20            # two planes of dz, dhidden's parts
+    assert size(2048, 32000, 2048) <= 300 << 20       # two pieces of dz, dhidden's parts
+    assert size(8192, 128000, 4096) <= 500 << 20
