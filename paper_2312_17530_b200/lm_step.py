@@ -91,6 +91,11 @@ class Worker:
 def run(steps: int = 40, n_workers: int = 2, n_tokens: int = 512, vocab: int = 2000, width: int = 256, n_top: int = 16,
         ratio: float = 1 / 16, rate: float = 8.0, temperature: float = 2.0, seed: int = 0):
     """Trains and returns the mean loss per step as a list."""
+    if width < 8 or width % 8:
+        # the head lies in an arena's layer, whose rows have no padding, and its rows have to start on 16-byte boundaries
+        raise ValueError("width: a multiple of 8 is wanted, got %d" % width)
+    if n_tokens < 2 or not 1 <= n_top <= min(vocab, 1024):
+        raise ValueError("two tokens or more, and 1 to min(vocab, 1024) top logits are wanted")
     gen = torch.Generator(device="cuda").manual_seed(seed)
     teacher = torch.randn(vocab, width, generator=gen, device="cuda") * (3.0 / width ** 0.5)
     student = Student(vocab, width, seed + 1)

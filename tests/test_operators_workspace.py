@@ -41,3 +41,11 @@ def test_head_workspace_stays_small():
     assert size(64, 8000, 512) <= 16 << 20            # two planes of dz, dhidden's parts
     assert size(2048, 32000, 2048) <= 300 << 20       # two pieces of dz, dhidden's parts
     assert size(8192, 128000, 4096) <= 500 << 20
+
+
+def test_example_says_what_it_does_not_take():
+    from paper_2312_17530_b200 import lm_step
+
+    for bad in (dict(width=100), dict(width=0), dict(n_tokens=1), dict(n_top=0), dict(vocab=10, n_top=11), dict(n_top=1025)):
+        with pytest.raises(ValueError):
+            lm_step.run(**bad)
