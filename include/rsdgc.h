@@ -448,7 +448,8 @@ int rsdgc_head_distill_backward(const void *hidden_dev, int64_t hidden_stride, c
                                 int64_t vocab, int64_t width, int32_t dtype, void *workspace_dev, void *stream);
 
 /* Waits for the stream, reports the status bits that the operators above have raised on the current device since the last
- * report (RSDGC_STATUS_TIMEOUT: a bounded on-chip wait gave up, results are invalid) and clears what it reports.  One
+ * report (RSDGC_STATUS_TIMEOUT: a bounded on-chip wait gave up, results are invalid; RSDGC_STATUS_BOUNDS, bounds-checked
+ * builds only: an index outside its extents was skipped) and clears what it reports.  One
  * word per device: whoever asks first is told, for all threads and streams; a bit raised meanwhile by another
  * stream's kernel is either in this report or in the next. */
 int rsdgc_operator_status(void *stream, uint32_t *flags_host);

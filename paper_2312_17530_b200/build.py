@@ -27,8 +27,9 @@ DEBUG_LIB_PATH = os.path.join(_HERE, "librsdgc_b200_debug.so")
 
 def build_library(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
     """nvcc -> librsdgc_b200.so next to this file; returns its path.  ``debug``: the bounds-checked
-    build (-DRSDGC_DEBUG: every index the kernels form is tested against the plan's extents, failures
-    raise RSDGC_STATUS_BOUNDS and skip the access) -> librsdgc_b200_debug.so; load it by pointing the
+    build (-DRSDGC_DEBUG: the indices that the kernels form are tested against the plan's extents, the
+    language-model operators' against their operands, rings and workspace; failures raise
+    RSDGC_STATUS_BOUNDS and skip the access) -> librsdgc_b200_debug.so; load it by pointing the
     environment variable RSDGC_LIBRARY at it."""
     if debug:
         return _compile(DEBUG_LIB_PATH, verbose, ["-DRSDGC_DEBUG"])

@@ -73,7 +73,7 @@ struct __align__(64) HeadJob {
     long long v0;            // first of them
     void *out_ptr;           // C is written through `out`, or, where its rows are not 16-byte aligned, by plain stores
     long long out_stride;
-    int out_rows, out_cols, out_mode, out_plain;
+    int out_rows, out_cols, out_parts, out_mode, out_plain;
 };
 
 struct HeadParams {
@@ -377,7 +377,9 @@ struct RowsOut {
         if (!j.out_plain) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0 && row0 < j.out_rows && col < j.out_cols) {
+            if (lane == 0 && row0 < j.out_rows && col < j.out_cols &&
+                RSDGC_IN_BOUNDS(row0 >= 0 && col >= 0 && split >= 0 && split < j.out_parts &&
+                                col % (j.out_mode == kOut16 ? 8 : 4) == 0)) {
                 if (j.out_mode == kOutAddF32)
                     add_box(&j.out, col, row0, split, buf);
                 else
@@ -395,7 +397,7 @@ struct RowsOut {
                 asm volatile("ld.shared.u16 %0, [%1];"
                              : "=h"(v)
                              : "r"(buf + r * 64 + (((lane >> 3) ^ ((r >> 1) & 3)) << 4) + (lane & 7) * 2));
-                if (col + lane < j.out_cols) *dst = v;
+                if (col + lane < j.out_cols && RSDGC_IN_BOUNDS(row0 >= 0 && row0 + r < j.out_rows && col >= 0)) *dst = v;
             }
         } else {  // two rows per round
             const int c = lane & 15;
@@ -404,7 +406,8 @@ struct RowsOut {
                 asm volatile("ld.shared.f32 %0, [%1];"
                              : "=f"(v)
                              : "r"(buf + r * 64 + (((c >> 2) ^ ((r >> 1) & 3)) << 4) + (c & 3) * 4));
-                if (col + c < j.out_cols) ((float *)j.out_ptr)[(long long)(row0 + r) * j.out_stride + col + c] = v;
+                if (col + c < j.out_cols && RSDGC_IN_BOUNDS(row0 >= 0 && row0 + r < j.out_rows && col >= 0))
+                    ((float *)j.out_ptr)[(long long)(row0 + r) * j.out_stride + col + c] = v;
             }
         }
     }
@@ -522,7 +525,10 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                         kc -= j.plane_steps * kStepK;
                         ka = j.plane + kc;
                     }
-                    if (elect_one()) {
+                    // a row coordinate in front of a contiguous row index starts a copy: 16-byte boundaries
+                    if (elect_one() && RSDGC_IN_BOUNDS(kc >= 0 && ka >= 0 && ra >= 0 && rb >= 0 && (!a_mn || ra % 64 == 0) &&
+                                                       (!b_mn || rb % 64 == 0) && (a_mn || ka % 64 == 0) && (b_mn || kc % 64 == 0) &&
+                                                       stage < stages && tp.job < p.n_jobs && tp.m < j.m_tiles && tp.n < j.n_tiles)) {
                         if (rank == 0) barrier_expect(smem_addr(&full[stage]), bytes);
                         sent[rank][stage] = (int)(bytes / 2);
                         if (a_mn) {
@@ -724,11 +730,12 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                     if constexpr (!BACK) {
                         if (p.k) {
                             while (tg.next < col + 32) {
-                                p.target_z[tg.j * p.n + row] = pick32(raw, tg.next - col);
+                                if (RSDGC_IN_BOUNDS(tg.j >= 0 && tg.j < p.k && row < p.n && tg.next >= col))
+                                    p.target_z[tg.j * p.n + row] = pick32(raw, tg.next - col);
                                 tg.advance(p, row);
                             }
                         } else if (label >= col && label < col + 32) {
-                            p.target_z[row] = pick32(raw, label - col);
+                            if (RSDGC_IN_BOUNDS(row < p.n)) p.target_z[row] = pick32(raw, label - col);
                         }
                         if (col + 32 > j.vocab) {
 #pragma unroll
@@ -769,7 +776,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
                             }
                             if (p.k) {
                                 while (tg.next < v0 + col + 32) {
-                                    subtract32(z, tg.next - v0 - col, gs * p.target_q[tg.j * p.n + row]);
+                                    if (RSDGC_IN_BOUNDS(tg.j >= 0 && tg.j < p.k && row < p.n && tg.next >= v0 + col))
+                                        subtract32(z, tg.next - v0 - col, gs * p.target_q[tg.j * p.n + row]);
                                     tg.advance(p, row);
                                 }
                             } else if (label >= col && label < col + 32) {
@@ -931,6 +939,7 @@ k_head_targets(const long long *__restrict__ index, long long is, const L *__res
             q = expf(u) * inv;
             if (!(q == 0.0f)) ent = fmaf(q, u - log_sum, ent);
         }
+        if (!RSDGC_IN_BOUNDS(place >= 0 && place < k && from >= 0 && from < (i == kNoTarget ? wide : k))) return;
         out_index[place * n + row] = i;
         out_q[place * n + row] = q;
     };
@@ -1078,7 +1087,7 @@ k_head_hidden_sum(const float *__restrict__ sum, long long pitch, int parts, int
     grid_dependency_wait();
     grid_dependency_launch_next();
     const int row = blockIdx.y, col = 4 * (blockIdx.x * 256 + threadIdx.x);
-    if (col >= d) return;
+    if (col >= d || !RSDGC_IN_BOUNDS(row < n && col + 4 <= pitch)) return;
     const float *src = sum + (long long)row * pitch + col;
     const long long slab = (long long)n * pitch;
     float4 t = *reinterpret_cast<const float4 *>(src);
@@ -1102,6 +1111,8 @@ k_head_hidden_sum(const float *__restrict__ sum, long long pitch, int parts, int
 }
 
 // ---- host ---------------------------------------------------------------------------------------
+RSDGC_DEFINE_DEBUG_BOUNDS(head_debug_bounds)
+
 namespace {
 
 typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -1150,6 +1161,7 @@ cudaError_t set_output(HeadJob &j, int mode, int dtype, void *base, long long ro
     j.out_stride = stride;
     j.out_rows = (int)rows;
     j.out_cols = (int)cols;
+    j.out_parts = (int)parts;
     j.out_plain = !pointer_aligned(base, 16) || (stride * elem) % 16 != 0;
     if (j.out_plain) return parts == 1 && mode != kOutAddF32 ? cudaSuccess : cudaErrorInvalidValue;
     EncodeFn fn = encode_fn();

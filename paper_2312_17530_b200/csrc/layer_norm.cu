@@ -80,7 +80,8 @@ struct Pairs {
     __device__ __forceinline__ void store(T *row, bool whole, int c, int d) const
     {
         if (whole) {
-            *reinterpret_cast<uint4 *>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            if (RSDGC_IN_BOUNDS(c >= 0 && c + V <= d && (reinterpret_cast<uintptr_t>(row + c) & 15) == 0))
+                *reinterpret_cast<uint4 *>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j)
@@ -300,6 +301,20 @@ __device__ __forceinline__ void take(Pairs<T> &v, const Columns<SHIFT, Pairs<T>:
     v.load(reinterpret_cast<const T *>(copy + (c + phase) * (int)sizeof(T)));
     if (!cols.template whole<FAST>(i)) v.mask(c, cols.d);
 }
+// Whether an operand of n rows of d values has the values [first, first + count), counted from its first one; what lies between
+// its rows counts as its own.
+__device__ __forceinline__ bool exist(long long first, int count, long long stride, int n, int d)
+{
+    return first >= 0 && first + count <= (n - 1) * stride + d;
+}
+// ... and a bulk copy of a row's granules, inside a row of `room` bytes of the ring
+template <typename T>
+__device__ __forceinline__ bool copy_exists(const T *x, long long stride, int row, int phase, RowCopy copy, uint32_t room, int n, int d)
+{
+    const long long first = row * stride - phase + copy.skip / (int)sizeof(T);
+    return row >= 0 && row < n && exist(first, copy.bytes / (int)sizeof(T), stride, n, d) && copy.skip + copy.bytes <= room &&
+           (reinterpret_cast<uintptr_t>(x + first) & 15) == 0;
+}
 // Rows whose granules may reach beyond the operand's first or last value (one row at either end unless rows are
 // shorter than a granule).
 template <int V>
@@ -407,7 +422,7 @@ k_norm_forward_ring(const T *__restrict__ x, long long xs, const P *__restrict__
         const int row = walk.row0 + walk.period * j;
         const RowCopy copy = row_copy<T>(row, n, walk.phase, d);
         barrier_expect(ring.bar(i), copy.bytes);
-        if (copy.bytes)
+        if (copy.bytes && RSDGC_IN_BOUNDS(copy_exists(x, xs, row, walk.phase, copy, stage_bytes, n, d)))
             bulk_copy(ring.at(i) + copy.skip, reinterpret_cast<const unsigned char *>(x + row * xs - walk.phase) + copy.skip,
                       copy.bytes, ring.bar(i));
     };
@@ -431,7 +446,8 @@ k_norm_forward_ring(const T *__restrict__ x, long long xs, const P *__restrict__
             constexpr bool FAST = decltype(fast)::value;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (cols.template any<FAST>(i))
+                if (cols.template any<FAST>(i) &&
+                    RSDGC_IN_BOUNDS(cols.at(i) + walk.phase >= 0 && (cols.at(i) + walk.phase + V) * (int)sizeof(T) <= (int)stage_bytes))
                     take<FAST>(in[i], cols, i, rows + ring.offset(it), SHIFT ? walk.phase : 0, x + row * xs, edge);
             sum = sum_of<FAST>(in, cols);
         });
@@ -471,7 +487,10 @@ k_norm_forward_warp(const T *__restrict__ x, long long xs, const P *__restrict__
             constexpr bool FAST = decltype(fast)::value;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (cols.template any<FAST>(i)) take<FAST>(next[i], cols, i, x + row * xs, near_end<V>(row, n, d));
+                if (cols.template any<FAST>(i) &&
+                    RSDGC_IN_BOUNDS(row < n && ((near_end<V>(row, n, d) && !cols.template whole<FAST>(i)) ||
+                                                exist(row * xs + cols.at(i), V, xs, n, d))))
+                    take<FAST>(next[i], cols, i, x + row * xs, near_end<V>(row, n, d));
         });
     };
     fetch(walk.first);
@@ -662,7 +681,9 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
         for (int r = 0; r < count; ++r) {
             const long long row = row_of(g, r);
             const uint32_t dst = ring.at(i) + 2 * r * row_bytes + copy[r].skip;
-            if (!copy[r].bytes) continue;
+            if (!copy[r].bytes || !RSDGC_IN_BOUNDS(copy_exists(x, xs, (int)row, walk.phase, copy[r], row_bytes, n, d) &&
+                                                   copy_exists(dy, dys, (int)row, walk.phase, copy[r], row_bytes, n, d)))
+                continue;
             bulk_copy(dst, reinterpret_cast<const unsigned char *>(x + row * xs - walk.phase) + copy[r].skip, copy[r].bytes,
                       ring.bar(i));
             bulk_copy(dst + row_bytes, reinterpret_cast<const unsigned char *>(dy + row * dys - walk.phase) + copy[r].skip,
@@ -695,7 +716,7 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
     auto statistics = [&](int g) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            const bool there = g * ROWS + r < walk.count;
+            const bool there = g * ROWS + r < walk.count && RSDGC_IN_BOUNDS(row_of(g, r) < n);
             nmu[r] = there ? mean[row_of(g, r)] : 0.0f;
             nr[r] = there ? rstd[row_of(g, r)] : 0.0f;
         }
@@ -715,6 +736,9 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
             const long long row = row_of(g, r);
             const bool edge = row == 0 || row == n - 1;
             const unsigned char *copy = rows + team * ring_bytes + ring.offset(it) + 2 * r * row_bytes;
+            if (!RSDGC_IN_BOUNDS(row < n && cols.at(i) + walk.phase >= 0 &&
+                                 (cols.at(i) + walk.phase + V) * (int)sizeof(T) <= (int)row_bytes))
+                return;
             take<FAST>(vx, cols, i, copy, SHIFT ? walk.phase : 0, x + row * xs, edge);
             take<FAST>(vg, cols, i, copy + row_bytes, SHIFT ? walk.phase : 0, dy + row * dys, edge);
         };
@@ -814,6 +838,7 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
                 const int at = min(c0 + u * all, d - 1) + (SHIFT ? walk.phase : 0), granule = at / V;
                 const int i = granule / team_threads;
                 from[u] = (i * V + at % V) * kNormJoin + granule - i * team_threads;
+                if (!RSDGC_IN_BOUNDS(i < NV && from[u] >= 0 && from[u] + (all / team_threads - 1) * team_threads < E * kNormJoin)) from[u] = 0;
                 sum[u] = joined[from[u]];
             }
             for (int k = 1; k < all / team_threads; ++k)
@@ -854,7 +879,9 @@ k_norm_backward_warp(const T *__restrict__ dy, long long dys, const T *__restric
             constexpr bool FAST = decltype(fast)::value;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (cols.template any<FAST>(i)) {
+                if (cols.template any<FAST>(i) &&
+                    RSDGC_IN_BOUNDS(row < n && ((edge && !cols.template whole<FAST>(i)) ||
+                                                (exist(row * xs + cols.at(i), V, xs, n, d) && exist(row * dys + cols.at(i), V, dys, n, d))))) {
                     take<FAST>(nx[i], cols, i, x + row * xs, edge);
                     take<FAST>(ng[i], cols, i, dy + row * dys, edge);
                 }
@@ -907,6 +934,7 @@ k_norm_backward_warp(const T *__restrict__ dy, long long dys, const T *__restric
             for (int k = 0; k < NP; ++k) {
                 const int c = cols.at(i) + 2 * k;
                 const float2 v = which ? db[i][k] : dw[i][k];
+                if (!RSDGC_IN_BOUNDS(d <= 32 * kNormElems)) continue;
                 if ((unsigned)c < (unsigned)d) joined[warp][c] = v.x;
                 if ((unsigned)(c + 1) < (unsigned)d) joined[warp][c + 1] = v.y;
             }
@@ -995,6 +1023,8 @@ k_norm_param_gradient(const float *__restrict__ partial, int slots, int d, Q *__
     for (int i = 1; i < lanes; ++i) t += sum[i][lane];
     out[c] = from_f32<Q>(t);
 }
+
+RSDGC_DEFINE_DEBUG_BOUNDS(layer_norm_debug_bounds)
 
 namespace {
 

@@ -127,6 +127,13 @@ extern "C" int rsdgc_operator_status(void *stream, uint32_t *flags_host)
         count_launch(1);
         if (e == cudaSuccess) e = cudaStreamSynchronize(s);
     }
+#ifdef RSDGC_DEBUG
+    unsigned int more[2] = {0, 0};
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = head_debug_bounds(&more[0]);
+    if (e == cudaSuccess) e = layer_norm_debug_bounds(&more[1]);
+    seen |= more[0] | more[1];
+#endif
     if (e == cudaSuccess) *flags_host = seen;
     return operator_result(e);
 }

@@ -114,6 +114,33 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, uint32_
 constexpr unsigned kOperatorPolls = 1u << 20;
 unsigned operator_polls();
 
+// Bounds-checked build: every index that an operator's kernel forms into an operand, a result, the workspace or a ring is
+// tested; a failure is noted in the source file's own word (operators' kernels do not all know the status word, which
+// rsdgc_operator_status() joins these to) and the access is skipped.  In the normal build the test is not compiled.
+#ifdef RSDGC_DEBUG
+static __device__ unsigned int debug_operator_bounds;
+__device__ __forceinline__ bool debug_operator_in_bounds(bool ok)
+{
+    if (!ok) atomicOr(&debug_operator_bounds, RSDGC_STATUS_BOUNDS);
+    return ok;
+}
+#define RSDGC_IN_BOUNDS(cond) debug_operator_in_bounds(cond)
+// Reads and clears the word of the source file that it is expanded in.
+#define RSDGC_DEFINE_DEBUG_BOUNDS(name)                                                                       \
+    cudaError_t name(unsigned int *seen)                                                                      \
+    {                                                                                                         \
+        const unsigned int none = 0;                                                                          \
+        cudaError_t e = cudaMemcpyFromSymbol(seen, debug_operator_bounds, sizeof none);                       \
+        if (e == cudaSuccess && *seen) e = cudaMemcpyToSymbol(debug_operator_bounds, &none, sizeof none);     \
+        return e;                                                                                             \
+    }
+cudaError_t head_debug_bounds(unsigned int *seen);
+cudaError_t layer_norm_debug_bounds(unsigned int *seen);
+#else
+#define RSDGC_IN_BOUNDS(cond) true
+#define RSDGC_DEFINE_DEBUG_BOUNDS(name)
+#endif
+
 // The status word of calls that take no plan: one per device, raised by the kernels, read and cleared by
 // rsdgc_operator_status().  *out is its device address on the current device.
 cudaError_t operator_status_ptr(unsigned int **out);
