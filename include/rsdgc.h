@@ -390,13 +390,15 @@ int rsdgc_layer_norm_backward(const void *dy_dev, int64_t dy_stride, const void 
  * gradient), one >= vocab gives a NaN loss and no gradient.  loss, lse: binary32; lse is what the
  * backward pass takes and may be NULL.  workspace_dev: rsdgc_head_workspace_bytes() bytes with
  * n_targets = 1, 256-byte aligned; nothing in it has to survive between calls.  One sized for a call does for calls with
- * fewer tokens or targets.
+ * fewer tokens or targets.  A forward call by itself (scoring) needs rsdgc_head_forward_workspace_bytes(), less where
+ * there are many tokens.
  * Accuracy: the logits are sums of the tensor cores, binary32 but truncated after every 16 terms, each off by up to
  * width / 16 * 2^-23 of sum |hidden| |weight|; the mean of that is put back for terms of random signs.
  * Errors: INVALID (a needed pointer NULL, stride < width, sizes < 1, types), ALIGNMENT,
  * CAPACITY (n_tokens > 2^24, vocab > 2^28, width > 2^20, n_targets > 1024), CUDA.
  */
 int64_t rsdgc_head_workspace_bytes(int64_t n_tokens, int64_t vocab, int64_t width, int64_t n_targets);
+int64_t rsdgc_head_forward_workspace_bytes(int64_t n_tokens, int64_t vocab, int64_t width, int64_t n_targets);
 int rsdgc_head_loss_forward(const void *hidden_dev, int64_t hidden_stride, const void *weight_dev,
                             int64_t weight_stride, const int64_t *labels_dev, float *loss_dev, float *lse_dev,
                             int64_t n_tokens, int64_t vocab, int64_t width, int32_t dtype, void *workspace_dev,

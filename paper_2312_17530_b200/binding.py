@@ -35,7 +35,7 @@ EXPORTS = [
     "rsdgc_layer_norm_workspace_bytes", "rsdgc_layer_norm_forward", "rsdgc_layer_norm_backward",
     "rsdgc_head_workspace_bytes", "rsdgc_head_loss_forward", "rsdgc_head_loss_backward", "rsdgc_head_distill_forward",
     "rsdgc_head_distill_backward", "rsdgc_selftest_operator_polls",
-    "rsdgc_selftest_operator_wait",
+    "rsdgc_selftest_operator_wait", "rsdgc_head_forward_workspace_bytes",
 ]
 NOALLOC_MAX_LAYERS = 64
 N_COMPRESS_KERNELS = 5
@@ -123,6 +123,8 @@ def lib():
                                                 vp, vp]
         L.rsdgc_head_workspace_bytes.argtypes = [i64, i64, i64, i64]
         L.rsdgc_head_workspace_bytes.restype = i64
+        L.rsdgc_head_forward_workspace_bytes.argtypes = [i64, i64, i64, i64]
+        L.rsdgc_head_forward_workspace_bytes.restype = i64
         L.rsdgc_head_loss_forward.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, i64, i64, i32, vp, vp]
         L.rsdgc_head_loss_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, i32, i64, i64, i64, i32, vp,
                                                vp]
@@ -470,7 +472,14 @@ def head_workspace_bytes(n_tokens: int, vocab: int, width: int, n_targets: int =
     return _size(lib().rsdgc_head_workspace_bytes(n_tokens, vocab, width, n_targets), "rsdgc_head_workspace_bytes")
 
 
-def _head_args(hidden, weight, workspace, n_targets: int):
+@functools.lru_cache(maxsize=4096)
+def head_forward_workspace_bytes(n_tokens: int, vocab: int, width: int, n_targets: int = 1) -> int:
+    """... that a forward call alone needs (scoring, evaluation)."""
+    return _size(lib().rsdgc_head_forward_workspace_bytes(n_tokens, vocab, width, n_targets),
+                 "rsdgc_head_forward_workspace_bytes")
+
+
+def _head_args(hidden, weight, workspace, n_targets: int, size=head_workspace_bytes):
     """(n, v, d, hidden stride, weight stride, type, workspace's address) of a vocabulary head, after the checks that all
     its calls share."""
     n, d = hidden.shape
@@ -480,7 +489,7 @@ def _head_args(hidden, weight, workspace, n_targets: int):
     hs, ws = _rows(hidden, n, d, "hidden"), _rows(weight, v, d, "weight")
     # the stride of a single row is free
     hs, ws = hs if n > 1 else (d + 7) // 8 * 8, ws if v > 1 else (d + 7) // 8 * 8
-    return n, v, d, hs, ws, _dtype_code(hidden), _holds(workspace, head_workspace_bytes(n, v, d, n_targets))
+    return n, v, d, hs, ws, _dtype_code(hidden), _holds(workspace, size(n, v, d, n_targets))
 
 
 def _head_grads(hidden, weight, dhidden, dweight):
@@ -502,7 +511,7 @@ def head_loss_forward(hidden, weight, labels, loss, lse, workspace) -> None:
     float16, rows 16-byte aligned."""
     _matrix(hidden, "hidden")
     stream = _on_device(hidden, weight, workspace, labels, loss, lse)
-    n, v, d, hs, ws, code, space = _head_args(hidden, weight, workspace, 1)
+    n, v, d, hs, ws, code, space = _head_args(hidden, weight, workspace, 1, head_forward_workspace_bytes)
     f32 = _torch.f32
     if labels is None:
         raise ValueError("labels are wanted")
@@ -547,7 +556,7 @@ def head_distill_forward(hidden, weight, top_index, top_logit, temperature: floa
     _matrix(hidden, "hidden")
     stream = _on_device(hidden, weight, workspace, top_index, top_logit, loss, lse)
     k, istride, lstride, tcode = _top_args(top_index, top_logit, hidden.shape[0])
-    n, v, d, hs, ws, code, space = _head_args(hidden, weight, workspace, k)
+    n, v, d, hs, ws, code, space = _head_args(hidden, weight, workspace, k, head_forward_workspace_bytes)
     f32 = _torch.f32
     code = lib().rsdgc_head_distill_forward(hidden.data_ptr(), hs, weight.data_ptr(), ws, top_index.data_ptr(), istride,
                                             top_logit.data_ptr(), lstride, tcode, k, temperature,

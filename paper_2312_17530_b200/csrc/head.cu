@@ -1202,7 +1202,7 @@ constexpr int64_t kFewTokens = kHalf;
 
 struct HeadLayout {
     int64_t piece, pieces, splits, planes;
-    int64_t partial, target_z, index, q, entropy, scale, counter, dz[2], dh_sum, bytes;
+    int64_t partial, target_z, index, q, entropy, scale, counter, dz[2], dh_sum, forward_bytes, bytes;
     int64_t dh_pitch;
 };
 
@@ -1234,7 +1234,7 @@ HeadLayout head_layout(int64_t n, int64_t v, int64_t d, int64_t k)
     L.counter = take(4 * ((v + kPieceMin - 1) / kPieceMin));  // a piece each
     const int64_t shared = at;  // the forward pass's partials and the backward pass's dz share the rest
     L.partial = take(8 * n * ((v + kTile / 2 - 1) / (kTile / 2)));  // at most one per 128 columns
-    L.bytes = at;
+    L.forward_bytes = L.bytes = at;
     at = shared;
     L.dz[0] = take(2 * L.planes * n * L.piece);
     L.dz[1] = take(L.pieces > 1 ? 2 * L.planes * n * L.piece : 0);
@@ -1621,6 +1621,12 @@ extern "C" int64_t rsdgc_head_workspace_bytes(int64_t n_tokens, int64_t vocab, i
 {
     const int rc = head_check(n_tokens, vocab, width, n_targets);
     return rc ? rc : head_bytes(n_tokens, vocab, width, n_targets);
+}
+
+extern "C" int64_t rsdgc_head_forward_workspace_bytes(int64_t n_tokens, int64_t vocab, int64_t width, int64_t n_targets)
+{
+    const int rc = head_check(n_tokens, vocab, width, n_targets);
+    return rc ? rc : head_layout(n_tokens, vocab, width, n_targets).forward_bytes;
 }
 
 extern "C" int rsdgc_head_loss_forward(const void *hidden_dev, int64_t hidden_stride, const void *weight_dev,

@@ -49,3 +49,31 @@ def test_three_pieces(kind, n, v, d, k):
     else:
         binding.head_loss_backward(H, W, labels, lse, g, dh, dw, ws)
     assert torch.equal(first[0], dh) and torch.equal(first[1], dw)
+
+
+@pytest.mark.parametrize("k", [0, 11])
+def test_scoring_stays_inside_its_workspace(k):
+    n, v, d = 3000, 9001, 72
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    H, W = operand(gen, n, d, torch.bfloat16), operand(gen, v, d, torch.bfloat16, 0, 0.2)
+    size = binding.head_forward_workspace_bytes(n, v, d, max(k, 1))
+    assert size < binding.head_workspace_bytes(n, v, d, max(k, 1)) // 4
+    space = torch.full((size + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    loss, lse = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    if k:
+        index = torch.randint(0, v, (n, k), generator=gen, device="cuda")
+        logit = torch.randn(n, k, generator=gen, device="cuda")
+        call = lambda ws: binding.head_distill_forward(H, W, index, logit, 2.0, loss, lse, ws)  # noqa: E731
+        want = top_want(H, W, index, logit, 2.0)
+    else:
+        labels = torch.randint(-1, v, (n,), generator=gen, device="cuda")
+        call = lambda ws: binding.head_loss_forward(H, W, labels, loss, lse, ws)  # noqa: E731
+        want = label_want(H, W, labels)
+    call(space[:size])
+    want.check_forward(loss, lse)
+    assert (space[size:] == 0xFF).all() and binding.operator_status() == 0
+    with pytest.raises(ValueError):
+        call(space[:size - 1])
+    with pytest.raises(ValueError):  # the gradient needs more
+        binding.head_loss_backward(H, W, torch.zeros(n, dtype=torch.int64, device="cuda"), lse, loss, H.clone(), W.clone(),
+                                   space[:size])

@@ -49,3 +49,15 @@ def test_example_says_what_it_does_not_take():
     for bad in (dict(width=100), dict(width=0), dict(n_tokens=1), dict(n_top=0), dict(vocab=10, n_top=11), dict(n_top=1025)):
         with pytest.raises(ValueError):
             lm_step.run(**bad)
+
+
+def test_scoring_needs_what_the_forward_pass_uses():
+    """A pair of binary32 per token and 128 entries of the vocabulary, the targets, and little more."""
+    size, train = binding.head_forward_workspace_bytes, binding.head_workspace_bytes
+    for n, v, d, k in ((1, 1, 1, 1), (64, 8000, 512, 8), (8192, 128000, 4096, 1), (333, 10007, 776, 1024)):
+        least = 8 * n * -(-v // 128) + 12 * n * k
+        assert least <= size(n, v, d, k) <= least + 4 * n + 4 * -(-v // 2048) + 4096
+        assert size(n, v, d, k) <= train(n, v, d, k) and size(n, v, d, k) <= size(n + 1, v, d, k)
+    for bad in ((-1, 10, 10, 1), (1, 0, 10, 1), (1, 10, 10, 0), (1, 10, 10, 1025)):
+        with pytest.raises(binding.RsdgcError):
+            size(*bad)
