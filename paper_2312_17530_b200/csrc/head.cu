@@ -74,6 +74,7 @@ struct __align__(64) HeadJob {
     void *out_ptr;           // C is written through `out`, or, where its rows are not 16-byte aligned, by plain stores
     long long out_stride;
     int out_rows, out_cols, out_parts, out_mode, out_plain;
+    int out_bulk;            // columns in whole 16-byte granules: a bulk store writes no less
 };
 
 struct HeadParams {
@@ -377,7 +378,7 @@ struct RowsOut {
         if (!j.out_plain) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0 && row0 < j.out_rows && col < j.out_cols &&
+            if (lane == 0 && row0 < j.out_rows && col < j.out_bulk &&
                 RSDGC_IN_BOUNDS(row0 >= 0 && col >= 0 && split >= 0 && split < j.out_parts &&
                                 col % (j.out_mode == kOut16 ? 8 : 4) == 0)) {
                 if (j.out_mode == kOutAddF32)
@@ -386,6 +387,22 @@ struct RowsOut {
                     store_box(&j.out, col, row0, split, buf);
                 asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             }
+            // the values of a row's last, partial granule, from the lane's own row of the box
+            const int elems = j.out_mode == kOut16 ? 32 : 16;
+            if (j.out_bulk < j.out_cols && col < j.out_cols && col + elems > j.out_bulk && row0 + lane < j.out_rows)
+                for (int c = max(col, j.out_bulk); c < min(col + elems, j.out_cols); ++c) {
+                    const long long at = (long long)(row0 + lane) * j.out_stride + c;
+                    if (!RSDGC_IN_BOUNDS(row0 >= 0 && c >= 0 && c < j.out_cols)) continue;
+                    if (j.out_mode == kOut16) {
+                        uint16_t v;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(piece((c - col) >> 3) + ((c - col) & 7) * 2));
+                        ((uint16_t *)j.out_ptr)[at] = v;
+                    } else {
+                        float v;
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(piece((c - col) >> 2) + ((c - col) & 3) * 4));
+                        ((float *)j.out_ptr)[at] = v;
+                    }
+                }
             return;
         }
         __syncwarp();
@@ -1150,8 +1167,9 @@ cudaError_t encode(CUtensorMap *map, int dtype, const void *base, long long rows
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-// C of a job: parts x rows x cols values of `elem` bytes in boxes of 32 rows x 64 bytes; falls back to plain stores
-// where rows do not start on 16-byte boundaries
+// C of a job: parts x rows x cols values of `elem` bytes in boxes of 32 rows x 64 bytes, the columns beyond whole 16-byte granules
+// by plain stores; all of it by plain stores where rows do not start on 16-byte boundaries.  (A bulk store clips a box to the
+// tensor by granules, not by elements: the rest of a granule would be overwritten with zeros.)
 cudaError_t set_output(HeadJob &j, int mode, int dtype, void *base, long long rows, long long cols, long long stride,
                        long long parts = 1)
 {
@@ -1162,11 +1180,15 @@ cudaError_t set_output(HeadJob &j, int mode, int dtype, void *base, long long ro
     j.out_rows = (int)rows;
     j.out_cols = (int)cols;
     j.out_parts = (int)parts;
-    j.out_plain = !pointer_aligned(base, 16) || (stride * elem) % 16 != 0;
-    if (j.out_plain) return parts == 1 && mode != kOutAddF32 ? cudaSuccess : cudaErrorInvalidValue;
+    j.out_bulk = (int)(cols / (16 / elem) * (16 / elem));
+    j.out_plain = !pointer_aligned(base, 16) || (stride * elem) % 16 != 0 || j.out_bulk == 0;
+    if (j.out_plain || j.out_bulk < cols) {
+        if (parts > 1 || mode == kOutAddF32) return cudaErrorInvalidValue;  // the workspace's rows are whole
+        if (j.out_plain) return cudaSuccess;
+    }
     EncodeFn fn = encode_fn();
     if (!fn) return cudaErrorNotSupported;
-    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
+    const cuuint64_t dims[3] = {(cuuint64_t)j.out_bulk, (cuuint64_t)rows, (cuuint64_t)parts};
     const cuuint64_t strides[2] = {(cuuint64_t)stride * elem, (cuuint64_t)stride * elem * rows};
     const cuuint32_t box[3] = {(cuuint32_t)(64 / elem), 32, 1}, one[3] = {1, 1, 1};
     const CUresult r = fn(&j.out, mode != kOut16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
@@ -1542,7 +1564,7 @@ cudaError_t backward_pieces(const HeadCall &c, const HeadLayout &L, HeadParams &
             if (e == cudaSuccess)
                 e = L.pieces == 1 && parts == 1
                         ? set_output(j, kOut16, c.dtype, g.dh, c.n, c.d, g.dh_stride)
-                        : set_output(j, at == 0 ? kOutF32 : kOutAddF32, c.dtype, sum, c.n, c.d, L.dh_pitch, parts);
+                        : set_output(j, at == 0 ? kOutF32 : kOutAddF32, c.dtype, sum, c.n, L.dh_pitch, L.dh_pitch, parts);
             if (e == cudaSuccess) {
                 HeadJob &w = p.job[p.n_jobs++];
                 e = set_job(w, kWeightGrad, c.dtype, dz, true, planes * c.n, L.piece, L.piece, c.hidden, true, c.n, c.d, c.hs, v, c.d,
