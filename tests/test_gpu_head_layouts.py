@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2312_17530_b200 import binding
-from test_gpu_head import TYPES, label_want, operand, run_labels
+from test_gpu_head import TYPES, label_want, operand, run_labels, run_top
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +38,28 @@ def test_nothing_beyond_the_width_is_written(kind, grads, n, v, d):
         want.check_forward(loss, lse)
         want.check_backward(g, dh, dw, dtype, 1)
         assert untouched(around_h, d) and untouched(around_w, d)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("n,v,d,k", [(50, 700, 72, 9), (300, 3000, 136, 80)])
+def test_what_is_masked_is_not_read(kind, n, v, d, k):
+    """Logits of left-out entries and gradients of tokens without a loss may be anything: the same bits as with zeros there."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    dtype = TYPES[kind]
+    H, W = operand(gen, n, d, dtype), operand(gen, v, d, dtype, 0, 2 / math.sqrt(d))
+    index = torch.rand(n, v, generator=gen, device="cuda").argsort(1)[:, :k].contiguous()
+    index[torch.rand(n, k, generator=gen, device="cuda") < 0.3] = -1
+    index[::7] = -1
+    labels = torch.randint(0, v, (n,), generator=gen, device="cuda")
+    labels[::7] = -100
+    logit, g = torch.randn(n, k, generator=gen, device="cuda"), torch.rand(n, generator=gen, device="cuda")
+    out = []
+    for junk in (0.0, float("nan"), float("inf"), float("-inf"), torch.finfo(torch.float32).min):
+        bad_logit, bad_g = torch.where(index < 0, junk, logit), g.clone()
+        bad_g[::7] = junk
+        dh, dw = [torch.empty_like(H) for _ in range(2)], [torch.empty_like(W) for _ in range(2)]
+        a = run_labels(H, W, labels, bad_g, dh[0], dw[0])
+        b = run_top(H, W, index, bad_logit, 2.0, bad_g, dh[1], dw[1])
+        out.append([t.clone() for t in (*a, *b, *dh, *dw)])
+        assert all(torch.equal(s, t) for s, t in zip(out[0], out[-1]))
+        assert all(torch.isfinite(t).all() for t in out[-1])
