@@ -19,11 +19,14 @@
 // while the other one (256 columns each, 512 in all) is filled.  Operands whose contraction index is not the contiguous one
 // (W in dz W, both in dz^T h) are read as they lie in memory: the MMA takes them as MN-major.
 //
-// What bounds it: the tensor cores, and in long calls the power limit.  Rates by the products that are computed (one
-// forward, three backward): 2048 x 32000 x 2048 (tokens, vocabulary, width; bfloat16) forward 174 us, 1.54 PFLOP/s, backward
-// 539 us, 1.49; x 4096 1.61 and 1.62; 8192 x 128000 x 4096 backward 18.2 ms, 1.42.  With up to a few hundred tokens it is W's
-// way from memory: 64 x 32000 x 8192 forward takes 96 us, W at 5.4 TB/s, backward 301 us (W twice and dW at 5.2).  Small
-// calls are bound by the launches and the fill of the ring: 5 x 1000 x 256 takes 8.4 us forward and 16.4 backward.
+// What bounds it: the tensor cores, and in long runs the power limit.  Rates by the products that are computed (one
+// forward, three backward), bfloat16, sizes as tokens x vocabulary x width, medians of 12 graphs of five calls: 2048 x 32000 x
+// 2048 forward 174 us, 1.54 PFLOP/s, backward 539 us, 1.49; x 4096 330 us, 1.63, and 1.06 to 1.11 ms, 1.45 to 1.52; 8192 x
+// 128000 x 4096 5.8 to 6.1 ms, 1.41 to 1.48, and 19.0 ms, 1.36.  (Whole calls for seconds on end: 8192 x 128000 x 4096 25.0 ms
+// for both, 1.37.)  With up to a few hundred tokens it is W's way from memory: 64 x 32000 x 8192 forward takes 98 us, W at 5.3
+// TB/s, backward 332 us (W twice and dW at 4.7).  Small calls are bound by the launches and the fill of the ring: 5 x 1000 x 256
+// takes 9 us forward and 20 backward.  Widths that are no multiple of 8, whose outputs leave value by value: 2048 x 32000 x 2047
+// 175 and 559 us, 300 x 4000 x 2001 backward 74 us where 2008 takes 67.
 #include <cuda.h>
 
 #include <climits>
@@ -894,8 +897,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) k_head(const __grid_constant_
 }
 
 // ---- the small kernels around the tiles -----------------------------------------------------------
-// Latency bounds them all: a few dependent loads and a launch.  Alone and with cold caches, at 2048 x 32000 x 2048 with
-// 64 targets: k_head_targets 8.7 us, k_head_scale 3.6, k_head_join 7.7, k_head_hidden_sum 8.0 (two parts, 42 MB, 5.2 TB/s);
+// Latency bounds them all: a few dependent loads and a launch.  Alone and with cold caches, at 2048 x 32000 x 2048:
+// k_head_targets with 64 targets 8.7 us, k_head_scale for labels 6.1, k_head_join 6.7, k_head_hidden_sum 11.9 (two parts, 42 MB);
 // in a stream each starts while the one before it ends.
 
 // Top logits -> per row the sorted vocabulary indices with their probabilities q (binary32 softmax of the k
@@ -1204,14 +1207,14 @@ inline int tiles_of(int64_t a) { return (int)((a + kTile - 1) / kTile); }
 
 // A piece of the vocabulary: dz (n x piece, 16 bits) of at most kPieceBytes, in two buffers (one is written while the
 // other is read); never under kPieceMin columns, because every piece adds to dh once.  A launch ends on its longest
-// tiles, so few large pieces are better than what L2 would hold: 8192 x 128000 x 4096 takes 22.2 / 20.7 / 20.1 ms with
-// pieces of 64 / 128 / 256 MB (19.4 and 19.2 with 128 and 256 by now: not worth twice the memory).
+// tiles, so few large pieces are better than what L2 would hold: 8192 x 128000 x 4096 backward takes 19.8 / 19.0 /
+// 18.7 ms with pieces of 64 / 128 / 256 MB (the last is not worth twice the memory).
 constexpr int64_t kPieceBytes = 128ll << 20;
 constexpr int64_t kPieceMin = 2048;
 // With few tokens dh has few tiles, each with a contraction over the whole piece: it is cut into parts that are added
 // up at the end, in order, so that about kSplitTiles tiles share a launch with dW's, none longer than the launch's fair
-// share.  More parts cost more in sums than they balance (1023 x 50001 x 1000: 522 us with one part, 345 with 3, 311
-// with 5, 331 with 10).
+// share.  More parts cost more in sums than they balance (1023 x 50001 x 1000 backward: 431 us with one part, 294 with
+// 3, 270 with 5, 275 with 10).
 constexpr int64_t kSplitTiles = 37, kSplitSteps = 8;
 
 // With few tokens there is little to average a rounding out over: a row of dW is one dz times a row of h where a token stands
@@ -1367,10 +1370,10 @@ int head_pairs(cudaError_t *e)
 
 // Tiles of 256 x 128, 256 x 256 or 256 x 512 (two accumulators) for a launch's jobs.  The wider the tile, the more products
 // an operand block serves (48 bytes per cycle and SM at the full MMA rate for 512 columns, 64 for 256) and the more work
-// the ring holds: forward 2048 x 32000 x 2048 took 219 us with 512 columns against 286 with 256, measured side by side (174
-// by now).  The narrower, the more tiles there are to deal out: 64 x 8000 x 512, 32 tiles of 256 columns, took 11.0 us
-// against 13.8 with 512, and 25.5 against 31.2 backward; with 128 columns 10.0 and 24.9, and 5 x 1000 x 256 7.7 and 16.0
-// against 8.4 and 18.5 with 256.  Which is best follows from the cycles a tile takes (512 per contraction step and 256
+// the ring holds: 2048 x 32000 x 2048 takes 180 us forward and 560 backward with 512 columns throughout, 218 and 682 with 256,
+// 402 and 1185 with 128.  The narrower, the more tiles there are to deal out: 64 x 8000 x 512 takes 19.1 and 48.6 us with 512
+// columns, 11.8 and 31.0 with 256, 11.0 and 31.4 with 128, and 5 x 1000 x 256 15.8 and 36.7, 9.7 and 23.2, 8.9 and 19.6.
+// Which is best follows from the cycles a tile takes (512 per contraction step and 256
 // columns, some 3000 to empty an accumulator; 1.25 and 1.6 times that for the lost operand reuse of 256 and 128 columns)
 // dealt to the pairs of CTAs.
 void choose_columns(HeadParams &p, int pairs)

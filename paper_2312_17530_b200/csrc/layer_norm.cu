@@ -3,9 +3,9 @@
 //   mean = sum x / D,  rstd = (sum (x - mean)^2 / D + eps)^(-1/2),  xhat = (x - mean) rstd,  y = xhat w + b
 //   dx = rstd (g w - mean(g w) - xhat mean(g w xhat)),  dw = sum_n g xhat,  db = sum_n g
 //
-// Bound: memory for binary32 rows (8192 x 8192: forward 98 us, 5.5 TB/s, gradient 137 us, 5.9 TB/s); the issue rate for
+// Bound: memory for binary32 rows (8192 x 8192: forward 98 us, 5.5 TB/s, gradient 141 us, 5.7 TB/s); the issue rate for
 // 16-bit rows forward (16384 x 4096 bfloat16: 53 us, 5.1 TB/s at 68 % of the issue slots, 19 instructions per value); the
-// latency between a row's passes for their gradient (16384 x 8192: 158 us, 5.1 TB/s; 55 % of the issue slots at 16384 x
+// latency between a row's passes for their gradient (16384 x 8192: 160 us, 5.0 TB/s; 55 % of the issue slots at 16384 x
 // 4096); the launch for a few rows (1 x 4096: 2.3 us).  So a row is read once, in 16-byte packs, and its arithmetic runs on
 // pairs of binary32 values.  The mean, then the centred squares (two reductions, no cancellation), then the output.  All
 // statistics and sums are binary32.
@@ -15,7 +15,7 @@
 // and the row's.  Phases repeat with a short period (at most 8 rows), so a CTA or warp takes rows of one phase only:
 // its threads then own the same columns in every row, as the sums of dw and db over the rows need it.  The first and
 // the last granule of a row are masked; where they would reach beyond the operand they are read element by element.
-// (8192 x 4097 bfloat16: forward 47 us and gradient 87 us, against 81 and 269 a value at a time.)
+// (8192 x 4097 bfloat16: forward 48 us and gradient 92 us, against 81 and 269 a value at a time.)
 #include <atomic>
 #include <climits>
 #include <cmath>
@@ -520,7 +520,7 @@ k_norm_forward_warp(const T *__restrict__ x, long long xs, const P *__restrict__
 }
 
 // Any layout and width, a value at a time: rows longer than the ring holds, and operands whose rows have different
-// phases.  The row is read three times, the last two out of L2.  (8192 x 4097 bfloat16: 81 us against the ring's 47.)
+// phases.  The row is read three times, the last two out of L2.  (8192 x 4097 bfloat16: 81 us against the ring's 48.)
 template <typename T, typename P>
 __global__ void __launch_bounds__(kNormLongThreads)
 k_norm_forward_any(const T *__restrict__ x, long long xs, const P *__restrict__ w, const P *__restrict__ b,
@@ -617,7 +617,7 @@ __device__ __forceinline__ Pairs<T> input_gradient(const Pairs<T> &vx, const Pai
 //
 // SPLIT: a cluster of CTAs per row, each with its own columns (one team, one row per stage): rows that one CTA cannot hold.
 // The warps leave their two sums in every CTA of the cluster, and the cluster's barrier takes the place of the team's.
-// (Gradient of 4096 x 16384 binary32: 138 us, 5.8 TB/s, against 416 a value at a time.)
+// (Gradient of 4096 x 16384 binary32: 141 us, 5.7 TB/s, against 416 a value at a time.)
 template <bool SHIFT, typename T, int E, int ROWS, bool SPLIT, typename P>
 __global__ void __launch_bounds__(kNormRingThreads)
 k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
@@ -852,7 +852,7 @@ k_norm_backward_ring(const T *__restrict__ dy, long long dys, const T *__restric
 }
 
 // A warp per row, a CTA's warps on rows of one phase; the next row is loaded while this one is reduced; the warps' column
-// sums are joined in order at the end.  (16384 x 512 bfloat16: 20 us with k_norm_param_gradient.)
+// sums are joined in order at the end.  (16384 x 512 bfloat16: 16 us with k_norm_param_gradient, out of L2 in part.)
 template <bool SHIFT, typename T, typename P>
 __global__ void __launch_bounds__(32 * kBackWarps)
 k_norm_backward_warp(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
@@ -949,7 +949,7 @@ k_norm_backward_warp(const T *__restrict__ dy, long long dys, const T *__restric
 }
 
 // Any layout and width, a value at a time: two reads of the row; a second kernel walks the columns.  (4096 x 16384
-// binary32: 242 and 172 us, where the split rows take 138 for both.)
+// binary32: 242 and 172 us, where the split rows take 141 for both.)
 template <typename T, typename P>
 __global__ void __launch_bounds__(kNormLongThreads)
 k_norm_backward_any(const T *__restrict__ dy, long long dys, const T *__restrict__ x, long long xs,
@@ -1277,7 +1277,8 @@ bool norm_backward_packed(cudaError_t *e, int *slots, const BackwardArgs<T, P> &
     }
     const uint32_t row = 16u * (uint32_t)sh.packs;
     // binary32 rows: a second row per stage does not fit the registers (8192 x 1001 takes 58 us with it, 28 without), and
-    // what one CTA cannot hold at 16 columns per thread is better split than held at 32 (4096 x 9000: 103 us against 109)
+    // what one CTA cannot hold at 16 columns per thread is better split than held at 32 (4096 x 9000: 103 us against 109, side by
+    // side)
     const TeamShape one = team_shape<T>(sh, 16, 1, a.n);
     if constexpr (sizeof(T) < 4) {
         // two rows per stage where they fit; twice the columns per thread where that fills the multiprocessor better (a row
