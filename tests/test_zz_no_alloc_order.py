@@ -1,6 +1,7 @@
 """rsdgc_update_ratios_noalloc() without a plan, after the language-model operators: they load many kernels, and the room that the
 driver had set aside for code may be full when this one's are asked for.  Each order in a process of its own, which has loaded
 nothing before."""
+import os
 import subprocess
 import sys
 
@@ -56,6 +57,8 @@ print("taken", before - torch.cuda.mem_get_info()[0])
 
 @pytest.mark.parametrize("calls", [0, 4, 26])
 def test_nothing_is_allocated_after_operators(calls):
-    out = subprocess.run([sys.executable, "-c", SCRIPT, str(calls)], capture_output=True, text=True, timeout=300)
+    """After the first `calls` of the list, none among them."""
+    out = subprocess.run([sys.executable, "-c", SCRIPT, str(calls)], capture_output=True, text=True, timeout=300,
+                         cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     assert out.returncode == 0, out.stderr[-2000:]
     assert out.stdout.split() == ["taken", "0"]
