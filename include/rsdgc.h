@@ -449,6 +449,47 @@ int rsdgc_head_distill_backward(const void *hidden_dev, int64_t hidden_stride, c
                                 void *dweight_dev, int64_t dweight_stride, int32_t dweight_dtype, int64_t n_tokens,
                                 int64_t vocab, int64_t width, int32_t dtype, void *workspace_dev, void *stream);
 
+/*
+ * Gated scan: a recurrence over the steps of each of n_seq sequences, channel by channel (`width` channels):
+ *   a[t] = 1 / (1 + exp(-(gate[t] + gate_bias))),  h[t] = a[t] * h[t-1] + (1 - a[t]) * x[t],  y[t] = h[t].
+ * x, gate, y: `dtype`, [sequence][step][channel], channels contiguous, any strides of sequences and steps (in elements; >= width
+ * where there are several).  gate_bias: optional (0), one value per channel, param_dtype (`dtype` or binary32).
+ * first_dev, last_dev: optional, binary32, n_seq x width: the state before the first step (0) and behind the last; they
+ * may be the same array.  restart_dev: optional, one byte per step with a row stride; where it is not 0 the step's h[t-1] is 0
+ * (texts packed one behind the other).  lengths_dev: optional, int64 per sequence, clamped to 0 .. n_steps: the steps behind it
+ * are neither read nor written, `last` is the state there.  states_dev: optional, what the backward pass takes: binary32,
+ * n_seq x ceil(n_steps / RSDGC_SCAN_STATE_STEPS) x width.  The state is binary32 throughout; one that is no longer finite stays
+ * not finite until a restart.  n_seq = 0 does nothing.
+ * Errors: INVALID (a needed pointer NULL, a stride too small, sizes < 0, width < 1, types), ALIGNMENT (a pointer that is not a
+ * multiple of its element size), CAPACITY (n_seq or n_steps > 2^30, width > 2^24, n_seq * ceil(width / 64) > 2^28 - 1), CUDA.
+ */
+#define RSDGC_SCAN_STATE_STEPS 64
+int rsdgc_gated_scan_forward(const void *x_dev, int64_t x_seq, int64_t x_step, const void *gate_dev, int64_t gate_seq,
+                             int64_t gate_step, const void *gate_bias_dev, void *y_dev, int64_t y_seq, int64_t y_step,
+                             const float *first_dev, float *last_dev, const uint8_t *restart_dev, int64_t restart_stride,
+                             const int64_t *lengths_dev, float *states_dev, int64_t n_seq, int64_t n_steps, int64_t width,
+                             int32_t dtype, int32_t param_dtype, void *stream);
+
+/*
+ * Its gradient for given dy and, optionally, dlast (binary32, of `last`), with delta the gradient of h:
+ *   delta[t] = dy[t] + a[t+1] * delta[t+1] (0 across a restart; dlast behind the last step),
+ *   dx[t] = (1 - a[t]) * delta[t],  dgate[t] = delta[t] * a[t] * (1 - a[t]) * (h[t-1] - x[t]),
+ *   dbias = sum over sequences and steps of dgate,  dfirst = a[0] * delta[0] (0 if step 0 is a restart).
+ * The states within a block of RSDGC_SCAN_STATE_STEPS steps are computed again from the saved ones, in binary32.
+ * dx, dgate (`dtype`), dbias (grad_dtype, any of the three types), dfirst (binary32, may be dlast's array): each optional, one at least.
+ * restart, lengths: as in the forward call; dx and dgate behind a length are not written.  workspace_dev:
+ * rsdgc_gated_scan_workspace_bytes() bytes, 16-byte aligned, needed for dbias.  n_seq = 0 or n_steps = 0: dbias = 0, dfirst =
+ * dlast.  Errors: as above.
+ */
+int64_t rsdgc_gated_scan_workspace_bytes(int64_t n_seq, int64_t n_steps, int64_t width);
+int rsdgc_gated_scan_backward(const void *dy_dev, int64_t dy_seq, int64_t dy_step, const void *x_dev, int64_t x_seq,
+                              int64_t x_step, const void *gate_dev, int64_t gate_seq, int64_t gate_step,
+                              const void *gate_bias_dev, const float *states_dev, const float *dlast_dev, void *dx_dev,
+                              int64_t dx_seq, int64_t dx_step, void *dgate_dev, int64_t dgate_seq, int64_t dgate_step,
+                              void *dbias_dev, float *dfirst_dev, const uint8_t *restart_dev, int64_t restart_stride,
+                              const int64_t *lengths_dev, int64_t n_seq, int64_t n_steps, int64_t width, int32_t dtype,
+                              int32_t param_dtype, int32_t grad_dtype, void *workspace_dev, void *stream);
+
 /* Waits for the stream, reports the status bits that the operators above have raised on the current device since the last
  * report (RSDGC_STATUS_TIMEOUT: a bounded on-chip wait gave up, results are invalid; RSDGC_STATUS_BOUNDS, bounds-checked
  * builds only: an index outside its extents was skipped) and clears what it reports.  One

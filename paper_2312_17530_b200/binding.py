@@ -35,7 +35,8 @@ EXPORTS = [
     "rsdgc_layer_norm_workspace_bytes", "rsdgc_layer_norm_forward", "rsdgc_layer_norm_backward",
     "rsdgc_head_workspace_bytes", "rsdgc_head_loss_forward", "rsdgc_head_loss_backward", "rsdgc_head_distill_forward",
     "rsdgc_head_distill_backward", "rsdgc_selftest_operator_polls",
-    "rsdgc_selftest_operator_wait", "rsdgc_head_forward_workspace_bytes",
+    "rsdgc_selftest_operator_wait", "rsdgc_head_forward_workspace_bytes", "rsdgc_gated_scan_workspace_bytes",
+    "rsdgc_gated_scan_forward", "rsdgc_gated_scan_backward",
 ]
 NOALLOC_MAX_LAYERS = 64
 N_COMPRESS_KERNELS = 5
@@ -132,6 +133,12 @@ def lib():
                                                  i32, vp, vp]
         L.rsdgc_head_distill_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i32, i64, f32, vp, vp, vp, i64, vp,
                                                   i64, i32, i64, i64, i64, i32, vp, vp]
+        L.rsdgc_gated_scan_workspace_bytes.argtypes = [i64, i64, i64]
+        L.rsdgc_gated_scan_workspace_bytes.restype = i64
+        L.rsdgc_gated_scan_forward.argtypes = [vp, i64, i64, vp, i64, i64, vp, vp, i64, i64, vp, vp, vp, i64, vp, vp, i64, i64,
+                                               i64, i32, i32, vp]
+        L.rsdgc_gated_scan_backward.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, i64, i64, vp, i64, i64,
+                                                vp, vp, vp, i64, vp, i64, i64, i64, i32, i32, i32, vp, vp]
         L.rsdgc_launch_count.argtypes = []
         L.rsdgc_launch_count.restype = i64
         L.rsdgc_strerror.argtypes = [C.c_int]
@@ -582,6 +589,100 @@ def head_distill_backward(hidden, weight, top_index, top_logit, temperature: flo
                                              stream)
     if code:
         _check(code, "rsdgc_head_distill_backward")
+
+
+SCAN_STATE_STEPS = 64
+
+
+def gated_scan_states_shape(n_seq: int, n_steps: int, width: int) -> Tuple[int, int, int]:
+    """Shape of the float32 states that gated_scan_forward() leaves for gated_scan_backward()."""
+    return n_seq, -(-n_steps // SCAN_STATE_STEPS), width
+
+
+@functools.lru_cache(maxsize=4096)
+def gated_scan_workspace_bytes(n_seq: int, n_steps: int, width: int) -> int:
+    """Bytes of workspace gated_scan_backward() needs for the gate bias's gradient."""
+    return _size(lib().rsdgc_gated_scan_workspace_bytes(n_seq, n_steps, width), "rsdgc_gated_scan_workspace_bytes")
+
+
+def _steps(t, shape, dtype, what: str):
+    """(address, sequence stride, step stride) of a [sequence][step][channel] operand whose channels are contiguous."""
+    if t is None:
+        return None, 0, 0
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError("%s: %s of %s is wanted, got %s of %s" % (what, tuple(shape), dtype, tuple(t.shape), t.dtype))
+    seq, step, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError("%s: channels have to be contiguous" % what)
+    return t.data_ptr(), seq, step
+
+
+def _whole(t, shape, dtype, what: str) -> Optional[int]:
+    """Address of a contiguous tensor, or None."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
+        raise ValueError("%s: contiguous %s of %s is wanted, got %s of %s" % (what, tuple(shape), dtype, tuple(t.shape), t.dtype))
+    return t.data_ptr()
+
+
+def _restarts(t, n: int, steps: int):
+    """(address, row stride) of one byte per step"""
+    if t is None:
+        return None, 0
+    if t.shape != (n, steps) or t.element_size() != 1 or t.dtype.is_floating_point:
+        raise ValueError("restart: %d x %d values of one byte are wanted, got %s of %s" % (n, steps, tuple(t.shape), t.dtype))
+    row, one = t.stride()
+    if one != 1 and steps > 1:
+        raise ValueError("restart: rows have to be contiguous")
+    return t.data_ptr(), row
+
+
+def _sequences(x):
+    if x.dim() != 3:
+        raise ValueError("x: sequences x steps x channels are wanted, got %s" % (tuple(x.shape),))
+    return x.shape
+
+
+def gated_scan_forward(x, gate, y, gate_bias=None, first=None, last=None, restart=None, lengths=None, states=None) -> None:
+    """``y[s, t]`` = h[t] = a[t] h[t-1] + (1 - a[t]) x[s, t] with a[t] = sigmoid(gate[s, t] + gate_bias), channel by channel, over the
+    steps t of each sequence s.  ``x``, ``gate``, ``y``: sequences x steps x channels of one type (float32, bfloat16 or
+    float16), channels contiguous.  ``gate_bias``: one value per channel, that type or float32.  ``first``, ``last``: float32,
+    sequences x channels, the state before the first step and behind the last (may be one tensor).  ``restart`` (bool, sequences
+    x steps): the state is 0 before this step.  ``lengths`` (int64): steps of each sequence that exist.  ``states``: float32 of
+    gated_scan_states_shape(), for the backward pass."""
+    shape = n, steps, d = _sequences(x)
+    stream = _on_device(x, gate, y, gate_bias, first, last, restart, lengths, states)
+    f32 = _torch.f32
+    code = lib().rsdgc_gated_scan_forward(
+        *_steps(x, shape, x.dtype, "x"), *_steps(gate, shape, x.dtype, "gate"), _vector(gate_bias, d, None, "gate_bias"),
+        *_steps(y, shape, x.dtype, "y"), _whole(first, (n, d), f32, "first"), _whole(last, (n, d), f32, "last"),
+        *_restarts(restart, n, steps), _vector(lengths, n, _torch.i64, "lengths"),
+        _whole(states, gated_scan_states_shape(n, steps, d), f32, "states"), n, steps, d, _dtype_code(x),
+        _dtype_code(x if gate_bias is None else gate_bias), stream)
+    if code:
+        _check(code, "rsdgc_gated_scan_forward")
+
+
+def gated_scan_backward(dy, x, gate, states, dx=None, dgate=None, gate_bias=None, dbias=None, dlast=None, dfirst=None,
+                        restart=None, lengths=None, workspace=None) -> None:
+    """Gradients of gated_scan_forward() for ``dy`` and ``dlast`` (of ``last``; float32 or None): ``dx`` and ``dgate`` like ``x``,
+    ``dbias`` (one value per channel, any of the three types, e.g. a layer of a gradient arena), ``dfirst`` (float32, like
+    ``first``).  Each may be None.  ``states``: what the forward call left.  ``workspace``: gated_scan_workspace_bytes() bytes,
+    needed for ``dbias``."""
+    shape = n, steps, d = _sequences(x)
+    stream = _on_device(dy, x, gate, states, dx, dgate, gate_bias, dbias, dlast, dfirst, restart, lengths, workspace)
+    f32 = _torch.f32
+    code = lib().rsdgc_gated_scan_backward(
+        *_steps(dy, shape, x.dtype, "dy"), *_steps(x, shape, x.dtype, "x"), *_steps(gate, shape, x.dtype, "gate"),
+        _vector(gate_bias, d, None, "gate_bias"), _whole(states, gated_scan_states_shape(n, steps, d), f32, "states"),
+        _whole(dlast, (n, d), f32, "dlast"), *_steps(dx, shape, x.dtype, "dx"), *_steps(dgate, shape, x.dtype, "dgate"),
+        _vector(dbias, d, None, "dbias"), _whole(dfirst, (n, d), f32, "dfirst"), *_restarts(restart, n, steps),
+        _vector(lengths, n, _torch.i64, "lengths"), n, steps, d, _dtype_code(x),
+        _dtype_code(x if gate_bias is None else gate_bias), RSDGC_F32 if dbias is None else _dtype_code(dbias),
+        None if dbias is None else _holds(workspace, gated_scan_workspace_bytes(n, steps, d)), stream)
+    if code:
+        _check(code, "rsdgc_gated_scan_backward")
 
 
 def operator_status() -> int:
