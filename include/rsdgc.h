@@ -490,6 +490,27 @@ int rsdgc_gated_scan_backward(const void *dy_dev, int64_t dy_seq, int64_t dy_ste
                               const int64_t *lengths_dev, int64_t n_seq, int64_t n_steps, int64_t width, int32_t dtype,
                               int32_t param_dtype, int32_t grad_dtype, void *workspace_dev, void *stream);
 
+/*
+ * Orthogonalised update: each of n_matrices matrices X (n_rows x n_cols) is brought near to the matrix with its singular directions and
+ * singular values near 1, by n_steps odd polynomials (Newton-Schulz steps) with the coefficients (a, b, c) of each:
+ *   Y = X / (|X|_F + eps);  per step Y = a Y + (b A + c A A) Y with A = Y Y^T.
+ * (3.4445, -4.7750, 2.0315) five times brings singular values of 0.01 .. 1 of the largest to about 0.7 .. 1.2.
+ * x: `dtype`; out: out_dtype, bfloat16 or binary16; row and matrix strides in elements, any alignment.  coefficients_host: 3 * n_steps
+ * binary32 on the host, read during the call; n_steps 1 to 32.  workspace_dev: rsdgc_orthogonalize_workspace_bytes() bytes, 256-byte
+ * aligned; nothing in it has to survive between calls.  A matrix of zeros gives zeros, one that is not finite NaN.
+ * Accuracy: sums in binary32, operands of 11 bits (22 for a Y); the result is within 0.002 (relative 2-norm) of the formula's, before
+ * its own rounding, for the coefficients above.  For binary16 results, and where the shorter side has at most 256, each product is made of three with
+ * 22-bit operands: within 1e-4.
+ * Errors: INVALID (a pointer NULL, strides, sizes < 0, types, eps negative or not finite, coefficients with which a singular value
+ * could exceed 2 or |b s^2 + c s^4| 7.5), ALIGNMENT, CAPACITY (n_rows or n_cols > 2^24, the shorter one > 2^15, n_matrices > 2^20, or
+ * more than 2^25 tiles of 256 x 128 in all), CUDA.
+ */
+int64_t rsdgc_orthogonalize_workspace_bytes(int64_t n_matrices, int64_t n_rows, int64_t n_cols, int32_t out_dtype);
+int rsdgc_orthogonalize(const void *x_dev, int64_t x_row_stride, int64_t x_matrix_stride, int32_t dtype, void *out_dev,
+                        int64_t out_row_stride, int64_t out_matrix_stride, int32_t out_dtype, int64_t n_matrices, int64_t n_rows,
+                        int64_t n_cols, const float *coefficients_host, int32_t n_steps, float eps, void *workspace_dev,
+                        void *stream);
+
 /* Waits for the stream, reports the status bits that the operators above have raised on the current device since the last
  * report (RSDGC_STATUS_TIMEOUT: a bounded on-chip wait gave up, results are invalid; RSDGC_STATUS_BOUNDS, bounds-checked
  * builds only: an index outside its extents was skipped) and clears what it reports.  One

@@ -36,7 +36,7 @@ EXPORTS = [
     "rsdgc_head_workspace_bytes", "rsdgc_head_loss_forward", "rsdgc_head_loss_backward", "rsdgc_head_distill_forward",
     "rsdgc_head_distill_backward", "rsdgc_selftest_operator_polls",
     "rsdgc_selftest_operator_wait", "rsdgc_head_forward_workspace_bytes", "rsdgc_gated_scan_workspace_bytes",
-    "rsdgc_gated_scan_forward", "rsdgc_gated_scan_backward",
+    "rsdgc_gated_scan_forward", "rsdgc_gated_scan_backward", "rsdgc_orthogonalize_workspace_bytes", "rsdgc_orthogonalize",
 ]
 NOALLOC_MAX_LAYERS = 64
 N_COMPRESS_KERNELS = 5
@@ -139,6 +139,9 @@ def lib():
                                                i64, i32, i32, vp]
         L.rsdgc_gated_scan_backward.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, i64, i64, vp, i64, i64,
                                                 vp, vp, vp, i64, vp, i64, i64, i64, i32, i32, i32, vp, vp]
+        L.rsdgc_orthogonalize_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.rsdgc_orthogonalize_workspace_bytes.restype = i64
+        L.rsdgc_orthogonalize.argtypes = [vp, i64, i64, i32, vp, i64, i64, i32, i64, i64, i64, vp, i32, f32, vp, vp]
         L.rsdgc_launch_count.argtypes = []
         L.rsdgc_launch_count.restype = i64
         L.rsdgc_strerror.argtypes = [C.c_int]
@@ -683,6 +686,51 @@ def gated_scan_backward(dy, x, gate, states, dx=None, dgate=None, gate_bias=None
         None if dbias is None else _holds(workspace, gated_scan_workspace_bytes(n, steps, d)), stream)
     if code:
         _check(code, "rsdgc_gated_scan_backward")
+
+
+# five steps that bring singular values of 0.01 .. 1 of the largest to about 0.7 .. 1.2
+ORTHOGONAL_COEFFICIENTS = ((3.4445, -4.7750, 2.0315),) * 5
+
+
+def orthogonalize_workspace_bytes(n_matrices: int, n_rows: int, n_cols: int, out_dtype) -> int:
+    """Bytes of workspace (256-byte aligned) that orthogonalize() needs; ``out_dtype``: the result's torch type."""
+    return _orthogonal_bytes(n_matrices, n_rows, n_cols, _tt().codes.get(out_dtype, -1))
+
+
+@functools.lru_cache(maxsize=4096)
+def _orthogonal_bytes(n_matrices: int, n_rows: int, n_cols: int, code: int) -> int:
+    return _size(lib().rsdgc_orthogonalize_workspace_bytes(n_matrices, n_rows, n_cols, code), "rsdgc_orthogonalize_workspace_bytes")
+
+
+@functools.lru_cache(maxsize=256)
+def _coefficients(rows):
+    if not rows or any(len(r) != 3 for r in rows):
+        raise ValueError("coefficients: three per step are wanted")
+    flat = [float(v) for r in rows for v in r]
+    return (C.c_float * len(flat))(*flat), len(rows)
+
+
+def orthogonalize(x, out, workspace, coefficients=ORTHOGONAL_COEFFICIENTS, eps: float = 1e-7) -> None:
+    """``out`` = the matrix near ``x`` whose singular values are near 1, by Newton-Schulz steps: ``Y = x / (|x| + eps)``, then ``Y = a Y +
+    (b A + c A A) Y`` with ``A = Y Y^T`` for each ``(a, b, c)`` of ``coefficients``.  ``x`` (float32, bfloat16 or float16; e.g. a
+    matrix of the dense gradient that the aggregation leaves): rows x columns, or a stack of such matrices; rows contiguous.
+    ``out``: its shape, bfloat16 or float16.  ``workspace``: orthogonalize_workspace_bytes() bytes."""
+    if x.dim() not in (2, 3) or out.shape != x.shape:
+        raise ValueError("x and out: matrices, or stacks of matrices, of one shape are wanted, got %s and %s" % (
+            tuple(x.shape), tuple(out.shape)))
+    stream = _on_device(x, out, workspace)
+    n, rows, cols = x.shape if x.dim() == 3 else (1, *x.shape)
+    places = []
+    for t, what in ((x, "x"), (out, "out")):
+        matrix, row, one = t.stride() if t.dim() == 3 else (0, *t.stride())
+        if one != 1 and cols > 1:
+            raise ValueError("%s: rows have to be contiguous" % what)
+        places.append((t.data_ptr(), row, matrix, _dtype_code(t)))
+    flat, steps = _coefficients(tuple(map(tuple, coefficients)))
+    code = lib().rsdgc_orthogonalize(*places[0], *places[1], n, rows, cols, flat, steps, eps,
+                                     _holds(workspace, _orthogonal_bytes(n, rows, cols, places[1][3])), stream)
+    if code:
+        _check(code, "rsdgc_orthogonalize")
 
 
 def operator_status() -> int:

@@ -10,8 +10,9 @@ _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "librsdgc_b200.so")
 SOURCES = ["plan.cu", "accumulate_nsi.cu", "compress.cu", "ratio.cu", "decompress.cu", "ratio_noalloc.cu", "coo.cu", "tail.cu",
-           "operators.cu", "layer_norm.cu", "head.cu", "gated_scan.cu"]
-HEADERS = ["rsdgc_internal.cuh", "device_utils.cuh", "ratio_common.cuh", "operators_internal.cuh"]
+           "operators.cu", "layer_norm.cu", "head.cu", "gated_scan.cu",
+           "orthogonal.cu"]
+HEADERS = ["rsdgc_internal.cuh", "device_utils.cuh", "ratio_common.cuh", "operators_internal.cuh", "tensor_core.cuh"]
 
 
 def _stale() -> bool:

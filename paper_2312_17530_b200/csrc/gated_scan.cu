@@ -21,6 +21,7 @@
 
 #include "device_utils.cuh"
 #include "operators_internal.cuh"
+#include "tensor_core.cuh"
 
 namespace rsdgc {
 
@@ -51,21 +52,9 @@ struct ScanParams {
     int vec;                        // pairs of channels may be accessed at once
 };
 
-__device__ __forceinline__ uint32_t scan_cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void scan_cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ void scan_store_in(uint32_t addr, uint32_t rank, float4 v)  // to a CTA of the cluster
 {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(r), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr_in(addr, rank)), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 
 // Two neighbouring channels as they lie in memory.  `pair`: one access; otherwise `n` of the two values are there.
@@ -224,13 +213,13 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W) k_scan_
     __shared__ float4 parts[W == 1 ? 1 : 2][W == 1 ? 1 : kScanCluster][32];   // ... and each CTA's W runs
     typedef typename Channels<T>::Raw Raw;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int cluster = W == 1 ? 1 : p.cluster, rank = cluster > 1 ? (int)scan_cluster_rank() : 0;
+    const int cluster = W == 1 ? 1 : p.cluster, rank = cluster > 1 ? (int)cluster_rank() : 0;
     const int unit = W == 1 ? blockIdx.x * kScanLoneWarps + warp : (int)blockIdx.x / cluster;
     grid_dependency_wait();
     grid_dependency_launch_next();
     const int seq = unit / p.groups, group = unit - seq * p.groups;
     if (seq >= p.n_seq) return;  // W = 1 only: a warp too many
-    if (cluster > 1) scan_cluster_sync();  // nothing is written to a CTA that has not begun
+    if (cluster > 1) cluster_sync_all();  // nothing is written to a CTA that has not begun
     const ScanPlace at(p, group, lane);
     const float2 bias = at.bias(p), scale = make_float2(-kScanLog2e, -kScanLog2e);
     const int len = scan_length(p, seq);
@@ -296,7 +285,7 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W) k_scan_
                     }
                     for (int k = warp; k < cluster; k += W) scan_store_in(smem_addr(&parts[parity][rank][lane]), (uint32_t)k, all);
                 }
-                scan_cluster_sync();
+                cluster_sync_all();
                 for (int k = 0; k < cluster; ++k) {
                     if (k == rank) in = h;
                     h = scan_apply(parts[parity][k][lane], h);
@@ -347,12 +336,12 @@ __global__ void __launch_bounds__(32 * W) k_scan_backward(const ScanParams p)
     __shared__ float4 parts[2][kScanCluster][32];  // of a CTA's W runs: (R, P)
     typedef typename Channels<T>::Raw Raw;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int cluster = p.cluster, rank = cluster > 1 ? (int)scan_cluster_rank() : 0;
+    const int cluster = p.cluster, rank = cluster > 1 ? (int)cluster_rank() : 0;
     const int unit = (int)blockIdx.x / cluster;
     grid_dependency_wait();
     grid_dependency_launch_next();
     const int part = unit / p.groups, group = unit - part * p.groups;
-    if (cluster > 1) scan_cluster_sync();  // nothing is written to a CTA that has not begun
+    if (cluster > 1) cluster_sync_all();  // nothing is written to a CTA that has not begun
     const ScanPlace at(p, group, lane);
     const float2 bias = at.bias(p), scale = make_float2(-kScanLog2e, -kScanLog2e);
     constexpr int tile = S * W;
@@ -440,7 +429,7 @@ __global__ void __launch_bounds__(32 * W) k_scan_backward(const ScanParams p)
                     for (int to = warp; to < cluster; to += W)
                         scan_store_in(smem_addr(&parts[parity][rank][lane]), (uint32_t)to, make_float4(all.x, all.y, k.x, k.y));
                 }
-                scan_cluster_sync();
+                cluster_sync_all();
                 for (int k = 0; k < cluster; ++k) {
                     const float4 o = parts[parity][k][lane];
                     if (k == rank) in = e;

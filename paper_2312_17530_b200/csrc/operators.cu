@@ -128,12 +128,13 @@ extern "C" int rsdgc_operator_status(void *stream, uint32_t *flags_host)
         if (e == cudaSuccess) e = cudaStreamSynchronize(s);
     }
 #ifdef RSDGC_DEBUG
-    unsigned int more[3] = {0, 0, 0};
+    unsigned int more[4] = {0, 0, 0, 0};
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e == cudaSuccess) e = head_debug_bounds(&more[0]);
     if (e == cudaSuccess) e = layer_norm_debug_bounds(&more[1]);
     if (e == cudaSuccess) e = gated_scan_debug_bounds(&more[2]);
-    seen |= more[0] | more[1] | more[2];
+    if (e == cudaSuccess) e = orthogonal_debug_bounds(&more[3]);
+    seen |= more[0] | more[1] | more[2] | more[3];
 #endif
     if (e == cudaSuccess) *flags_host = seen;
     return operator_result(e);

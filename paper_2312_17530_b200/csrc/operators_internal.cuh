@@ -137,6 +137,7 @@ __device__ __forceinline__ bool debug_operator_in_bounds(bool ok)
 cudaError_t head_debug_bounds(unsigned int *seen);
 cudaError_t layer_norm_debug_bounds(unsigned int *seen);
 cudaError_t gated_scan_debug_bounds(unsigned int *seen);
+cudaError_t orthogonal_debug_bounds(unsigned int *seen);
 #else
 #define RSDGC_IN_BOUNDS(cond) true
 #define RSDGC_DEFINE_DEBUG_BOUNDS(name)

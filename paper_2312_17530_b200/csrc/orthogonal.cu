@@ -1,0 +1,986 @@
+// Orthogonalised update: a matrix is brought near to one with the same singular directions and all singular values near 1, by a few
+// odd polynomials of it (Newton-Schulz steps), which need products only.
+//
+//   Y = X / (|X|_F + eps);   A = Y Y^T,  B = b A + c A^2,  Y <- a Y + B Y   with (a, b, c) of the step;   A = Y^T Y and Y <- a Y + Y B for
+//   matrices with more rows than columns, so that A has the shorter side
+//
+// Numbers.  The products' operands are binary16 (11 bits; bfloat16's 8 leave an error of 0.01, and 0.07 where a few directions carry
+// the gradient), scaled by powers of two: Y by 2^12, A and B by 2^13.  The host refuses coefficients with which Y could outgrow
+// them.  The small directions are brought up by a, step after step, while B Y is small there: so Y itself is kept in
+// two binary16 planes, the rounded value and the rest (22 bits), for a Y, which is added in binary32.  That costs bytes and no
+// product (gradient of 16 directions plus 3 % noise: error 1.6e-4 with it, 9e-3 without).  Where one product's 11 bits do not do - a binary16
+// result, small matrices - A and B have two planes too and each product is three: hi hi + hi lo + lo hi.
+//
+// The products are one tile kernel, pairs of CTAs as for the vocabulary head: TMA brings the operands through a ring, one
+// thread issues the MMAs, sixteen warps empty the accumulator.  A and B are symmetric: tiles on and below the diagonal are computed, and
+// written a second time across it.  Y is read as it lies, once with its rows and once with its columns contracted.  Where A has
+// few tiles and a long contraction, the contraction is cut into parts which k_ortho_join adds up, in order.
+//
+// What bounds it: the tensor cores.
+#include <climits>
+#include <cmath>
+#include <cstring>
+#include <mutex>
+
+#include "device_utils.cuh"
+#include "operators_internal.cuh"
+#include "tensor_core.cuh"
+
+namespace rsdgc {
+
+constexpr int kOrthoWarps = 16;                           // of the epilogue, four per quarter of an accumulator's columns
+constexpr int kOrthoThreads = 128 + 32 * kOrthoWarps;     // producer, MMA, two idle warps, epilogue
+constexpr int kOrthoStaging = 2048;                       // per epilogue warp: 32 rows of 64 bytes
+constexpr int kOrthoSmem = kRingBlocks * kBlockBytes + kOrthoWarps * kOrthoStaging + 1024;
+constexpr int kOrthoMaxSteps = 32;
+constexpr float kOrthoScale = 4096.0f;                    // of Y's planes; A's and B's have 2^13
+
+// What becomes of a product.  kGram: A; kGramPart: binary32 parts of A; kPoly: B from A A; kUpdate: the next Y; kResult: the result.
+enum { kGram = 0, kGramPart = 1, kPoly = 2, kUpdate = 3, kResult = 4 };
+
+struct __align__(64) OrthoParams {
+    CUtensorMap a, b;        // [matrix x plane][rows][columns], boxes of 64 x 64
+    int a_mn, b_mn;          // the operand lies with its rows (not k) contiguous
+    int a_planes, b_planes;  // stored
+    int segments;            // products: hi hi, or hi hi + hi lo + lo hi
+    int k_steps;             // of one of them
+    int m_tiles, n_tiles, per, band;  // tiles of a matrix: per, in bands of `band` tile rows
+    int symmetric;           // only tiles that reach the diagonal or lie below it
+    int cols, halves;        // columns of an accumulator, accumulators of a tile
+    int splits, split_steps; // parts of the contraction
+    int tiles, stages;
+    int rows, columns;       // of the product
+    long long pitch;         // of the planes below, a multiple of 8
+    const __half *in;        // kPoly: A, kUpdate and kResult: Y; in_planes planes of rows x pitch per matrix
+    __half *out;             // out_planes planes
+    int in_planes, out_planes;
+    float in_scale, acc_scale;
+    float *part;             // kGramPart: [matrix][split][rows][pitch]
+    void *result;            // kResult: row and matrix stride in elements
+    long long result_row, result_matrix;
+    int result_wide;         // its rows lie on 16-byte boundaries
+    unsigned int *status;
+    unsigned polls;
+};
+
+struct OrthoTile {
+    int matrix, split, m, n, k0, steps;
+};
+__device__ __forceinline__ OrthoTile ortho_tile(const OrthoParams &p, int t)
+{
+    OrthoTile r;
+    const int each = p.per * p.splits;
+    r.matrix = t / each;
+    t -= r.matrix * each;
+    r.split = t / p.per;
+    t -= r.split * p.per;
+    r.k0 = r.split * p.split_steps;
+    r.steps = min(p.split_steps, p.segments * p.k_steps - r.k0);
+    if (p.symmetric) {
+        const int wide = p.cols * p.halves;
+        for (r.m = 0;; ++r.m) {
+            const int here = min(p.n_tiles, ((r.m + 1) * kTile + wide - 1) / wide);
+            if (t < here) break;
+            t -= here;
+        }
+        r.n = t;
+    } else {
+        const int per = p.band * p.n_tiles, b = t / per, i = t - b * per, rows = min(p.band, p.m_tiles - b * p.band);
+        r.n = i / rows;
+        r.m = b * p.band + i - r.n * rows;
+    }
+    return r;
+}
+
+__device__ __forceinline__ void load_shared16(uint32_t addr, uint32_t &a, uint32_t &b, uint32_t &c, uint32_t &d)
+{
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(addr) : "memory");
+}
+
+// A warp's 32 rows x 32 16-bit values between its lanes' rows and memory, where four lanes take a row's 64 bytes, eight rows at
+// a time.  In shared memory the 16-byte piece c of row r lies at c ^ (r / 2 & 3): neither side meets a bank conflict.
+struct OrthoStage {
+    uint32_t buf;
+    int lane;
+    __device__ __forceinline__ uint32_t at(int row, int piece) const { return buf + row * 64 + ((piece ^ ((row >> 1) & 3)) << 4); }
+    // this lane's four pieces of rows row0.. and columns col.. of a plane (rows x pitch values)
+    __device__ __forceinline__ void fetch(uint4 (&v)[4], const __half *plane, long long pitch, int row0, int rows, int col) const
+    {
+        const int c = col + (lane & 3) * 8;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int row = row0 + j * 8 + (lane >> 2);
+            v[j] = make_uint4(0, 0, 0, 0);
+            if (row < rows && c < pitch && RSDGC_IN_BOUNDS(row >= 0 && c >= 0 && c + 8 <= pitch))
+                v[j] = *reinterpret_cast<const uint4 *>(plane + row * pitch + c);
+        }
+    }
+    __device__ __forceinline__ void deal(const uint4 (&v)[4]) const
+    {
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) store_shared16(at(j * 8 + (lane >> 2), lane & 3), v[j].x, v[j].y, v[j].z, v[j].w);
+        __syncwarp();
+    }
+    // adds scale * (this lane's row) to z
+    __device__ __forceinline__ void add_row(float (&z)[32], float scale) const
+    {
+        const float2 s = make_float2(scale, scale);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t v[4];
+            load_shared16(at(lane, i), v[0], v[1], v[2], v[3]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&v[j]));
+                const float2 y = fma2(x, s, make_float2(z[8 * i + 2 * j], z[8 * i + 2 * j + 1]));
+                z[8 * i + 2 * j] = y.x;
+                z[8 * i + 2 * j + 1] = y.y;
+            }
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void put_row(const float (&z)[32]) const
+    {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            store_shared16(at(lane, i), pack2<T>(z[8 * i], z[8 * i + 1]), pack2<T>(z[8 * i + 2], z[8 * i + 3]),
+                           pack2<T>(z[8 * i + 4], z[8 * i + 5]), pack2<T>(z[8 * i + 6], z[8 * i + 7]));
+        __syncwarp();
+    }
+    // the block across the diagonal: this lane's row becomes a column
+    __device__ __forceinline__ void put_column(const float (&z)[32]) const
+    {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const __half h = __float2half_rn(z[i]);
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(at(i, lane >> 3) + (lane & 7) * 2), "h"(*reinterpret_cast<const uint16_t *>(&h))
+                         : "memory");
+        }
+        __syncwarp();
+    }
+    __device__ __forceinline__ void store(__half *plane, long long pitch, int row0, int rows, int col) const
+    {
+        const int c = col + (lane & 3) * 8;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int row = row0 + j * 8 + (lane >> 2);
+            uint4 v;
+            load_shared16(at(j * 8 + (lane >> 2), lane & 3), v.x, v.y, v.z, v.w);
+            if (row < rows && c < pitch && RSDGC_IN_BOUNDS(row >= 0 && c >= 0 && c + 8 <= pitch))
+                *reinterpret_cast<uint4 *>(plane + row * pitch + c) = v;
+        }
+    }
+    // ... to the caller's matrix, which has neither padding nor alignment
+    __device__ __forceinline__ void store_result(uint16_t *dst, long long stride, int row0, int rows, int col, int columns, bool wide) const
+    {
+        if (wide) {
+            const int c = col + (lane & 3) * 8;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = row0 + j * 8 + (lane >> 2);
+                uint4 v;
+                load_shared16(at(j * 8 + (lane >> 2), lane & 3), v.x, v.y, v.z, v.w);
+                if (row >= rows || !RSDGC_IN_BOUNDS(row >= 0 && c >= 0)) continue;
+                uint16_t *q = dst + row * stride + c;
+                if (c + 8 <= columns) {
+                    *reinterpret_cast<uint4 *>(q) = v;
+                } else {
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (c + i < columns) q[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+                }
+            }
+        } else {  // a row per round, a column per lane
+            for (int r = 0; r < min(32, rows - row0); ++r) {
+                uint16_t v;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at(r, lane >> 3) + (lane & 7) * 2) : "memory");
+                if (col + lane < columns && RSDGC_IN_BOUNDS(row0 >= 0 && col >= 0)) dst[(row0 + r) * stride + col + lane] = v;
+            }
+        }
+    }
+};
+
+// What rounding to binary16 leaves of the values
+__device__ __forceinline__ void ortho_rest(float (&z)[32])
+{
+#pragma unroll
+    for (int i = 0; i < 32; ++i) z[i] -= __half2float(__float2half_rn(z[i]));
+}
+
+// T: type of the result (kResult)
+template <int KIND, typename T>
+__global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constant__ OrthoParams p)
+{
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) unsigned long long full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
+    __shared__ uint32_t tmem_base;
+    __shared__ volatile int dead;
+    // after a give-up: which CTAs had one; stages each CTA's producer issued, and its bytes in the latest of each place
+    __shared__ int failed[2], issued[2], sent[2][kMaxStages];
+
+    const uint32_t ring = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int stages = p.stages, stage_bytes = kRingBlocks / stages * kBlockBytes;
+
+    if (warp == 0) {  // a lane per barrier
+        if (lane < kMaxStages) {
+            barrier_init(smem_addr(&full[lane]), 1);
+            barrier_init(smem_addr(&empty[lane]), 1);
+        } else if (lane < kMaxStages + 2) {
+            barrier_init(smem_addr(&acc_full[lane - kMaxStages]), 1);
+            barrier_init(smem_addr(&acc_empty[lane - kMaxStages]), 2 * kOrthoWarps);
+        } else if (lane == 31) {
+            barrier_init(smem_addr(&drain), 1);
+            dead = 0;
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 3 && lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane ? &p.b : &p.a) : "memory");
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&tmem_base))
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    tmem_fence_before();
+    __syncthreads();
+    cluster_sync_all();  // the peer's barriers exist before anything arrives on them
+    tmem_fence_after();
+    grid_dependency_wait();
+    grid_dependency_launch_next();
+
+    // Bounded: a wait that gives up marks the CTA dead, raises the status bit, and every role leaves its loop.
+    auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+        for (unsigned i = 0; i < p.polls; ++i) {
+            if (barrier_try(bar, parity)) return true;
+            if (dead) return false;
+        }
+        dead = 1;
+        atomicOr(p.status, RSDGC_STATUS_TIMEOUT);
+        return false;
+    };
+
+    if (warp < 4) {
+        auto wait_warp = [&](uint32_t bar, uint32_t ph) -> bool { return __all_sync(0xFFFFFFFFu, wait(bar, ph)); };
+        // ---- producer, in both CTAs; all bytes count on the first CTA's barriers
+        if (warp == 0) {
+            int stage = 0, it = 0;
+            uint32_t parity = 0;
+            bool ok = true;
+            asm volatile("fence.proxy.async.global;" ::: "memory");  // TMA reads what ordinary stores wrote
+            const bool whole = p.cols == kTile;  // of an accumulator's columns a CTA holds half: one box or two
+            const uint32_t bytes = 2u * (uint32_t)(kBlockBytes + p.halves * p.cols * kStepK);
+            for (int t = pair; t < p.tiles && ok; t += pairs) {
+                const OrthoTile tp = ortho_tile(p, t);
+                const int ra = tp.m * kTile + (int)rank * kHalf, rb = tp.n * p.halves * p.cols + (int)rank * (p.cols >> 1);
+                for (int k = 0; k < tp.steps; ++k) {
+                    ok = wait_warp(smem_addr(&empty[stage]), parity ^ 1u);
+                    if (!ok) break;
+                    const uint32_t bar = leader_addr(smem_addr(&full[stage])), dst = ring + stage * stage_bytes;
+                    const int seg = (tp.k0 + k) / p.k_steps, kc = (tp.k0 + k - seg * p.k_steps) * kStepK;
+                    const int za = tp.matrix * p.a_planes + (seg == 2), zb = tp.matrix * p.b_planes + (seg == 1);
+                    if (elect_one() && RSDGC_IN_BOUNDS(kc >= 0 && ra >= 0 && rb >= 0 && ra % 64 == 0 && rb % 64 == 0 && kc % 64 == 0 &&
+                                                       seg < p.segments && stage < stages && tp.m < p.m_tiles && tp.n < p.n_tiles)) {
+                        if (rank == 0) barrier_expect(smem_addr(&full[stage]), bytes);
+                        sent[rank][stage] = (int)(bytes / 2);
+                        // coordinates of a box: (k, row), or (row, k) where the rows are contiguous
+                        for (int i = 0; i < 2; ++i)
+                            load_box(dst + i * kBoxBytes, &p.a, p.a_mn ? ra + 64 * i : kc, p.a_mn ? kc : ra + 64 * i, za, bar);
+                        for (int h = 0; h < p.halves; ++h)
+                            for (int i = 0; i < (whole ? 2 : 1); ++i) {
+                                const int r = rb + h * kTile + 64 * i;
+                                load_box(dst + (1 + h) * kBlockBytes + i * kBoxBytes, &p.b, p.b_mn ? r : kc, p.b_mn ? kc : r, zb, bar);
+                            }
+                    }
+                    __syncwarp();
+                    ++it;
+                    if (++stage == stages) {
+                        stage = 0;
+                        parity ^= 1u;
+                    }
+                }
+            }
+            // the last commits arrive on this CTA's barriers: it must not leave before they have
+            for (int i = 0; i < stages && ok; ++i) {
+                ok = wait_warp(smem_addr(&empty[stage]), parity ^ 1u);
+                if (++stage == stages) {
+                    stage = 0;
+                    parity ^= 1u;
+                }
+            }
+            if (lane == 0) issued[rank] = it;
+        }
+        if (warp == 1 && rank == 0) {  // ---- MMA, the pair's first CTA: the warp walks together, one thread issues
+            int stage = 0, sub = 0;    // sub: accumulators used so far; they alternate
+            uint32_t parity = 0;
+            bool ok = true;
+            const int halves = p.halves;
+            const uint32_t idesc = (1u << 4) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) | ((uint32_t)(p.cols >> 3) << 17) |
+                                   ((uint32_t)(kTile >> 4) << 24);  // binary16 operands, binary32 sums
+            const uint32_t da = p.a_mn ? 2048 >> 4 : 32 >> 4, db = p.b_mn ? 2048 >> 4 : 32 >> 4;
+            const uint64_t a_base = operand_desc(ring, p.a_mn), b_base = operand_desc(ring + kBlockBytes, p.b_mn);
+            auto issue = [&](int st, int h, int acc, int k) {
+                const uint64_t a = a_base + (uint32_t)(st * (stage_bytes >> 4));
+                const uint64_t b = b_base + (uint32_t)(st * (stage_bytes >> 4) + h * (kBlockBytes >> 4));
+#pragma unroll
+                for (int i = 0; i < kStepK / 16; ++i)
+                    mma_f16(tmem_base + (uint32_t)acc * kTile, a + i * da, b + i * db, idesc, (uint32_t)(k | i));
+            };
+            for (int t = pair; t < p.tiles; t += pairs) {
+                const int steps = ortho_tile(p, t).steps;
+                const int acc0 = sub & 1, acc1 = acc0 ^ 1;
+                const uint32_t parity0 = (uint32_t)((sub >> 1) & 1) ^ 1u, parity1 = (uint32_t)(((sub + 1) >> 1) & 1) ^ 1u;
+                ok = wait_warp(smem_addr(&acc_empty[acc0]), parity0);
+                if (!ok) break;
+                tmem_fence_after();
+                // With two accumulators the second may still be read when the first is free: its products follow
+                // as soon as it is, at the latest when the ring is full of stages that wait for it.
+                bool second = halves == 1;
+                int behind = 0, tail = stage, kb = 0;
+                for (int k = 0; k < steps; ++k) {
+                    ok = wait_warp(smem_addr(&full[stage]), parity);
+                    if (!ok) break;
+                    if (elect_one()) {
+                        issue(stage, 0, acc0, k);
+                        if (k + 1 == steps) mma_commit_both(smem_addr(&acc_full[acc0]));
+                    }
+                    __syncwarp();
+                    ++behind;
+                    if (!second) {
+                        if (behind == stages || k + 1 == steps) {
+                            ok = wait_warp(smem_addr(&acc_empty[acc1]), parity1);
+                            if (!ok) break;
+                            second = true;
+                        } else {
+                            second = __all_sync(0xFFFFFFFFu, barrier_test(smem_addr(&acc_empty[acc1]), parity1));
+                        }
+                        if (second) tmem_fence_after();
+                    }
+                    for (; second && behind; --behind, ++kb) {
+                        if (elect_one()) {
+                            if (halves == 2) issue(tail, 1, acc1, kb);
+                            mma_commit_both(smem_addr(&empty[tail]));
+                        }
+                        __syncwarp();
+                        if (++tail == stages) tail = 0;
+                    }
+                    if (++stage == stages) {
+                        stage = 0;
+                        parity ^= 1u;
+                    }
+                }
+                if (!ok) break;
+                if (halves == 2 && elect_one()) mma_commit_both(smem_addr(&acc_full[acc1]));
+                __syncwarp();
+                sub += halves;
+            }
+        }
+    } else {  // ---- epilogue: a thread owns one row and a quarter of an accumulator's columns
+        const int quad = warp & 3, quarter = (warp - 4) >> 2;
+        const OrthoStage stg = {ring + kRingBlocks * kBlockBytes + (warp - 4) * kOrthoStaging, lane};
+        const int width = p.cols >> 2;  // columns of this thread: 64 or 32
+        const long long plane = (long long)p.rows * p.pitch;
+        const int tile_cols = p.cols * p.halves;
+        int sub = 0;
+        bool ok = true;
+        for (int t = pair; t < p.tiles && ok; t += pairs) {
+            const OrthoTile tp = ortho_tile(p, t);
+            const int row0 = tp.m * kTile + (int)rank * kHalf + quad * 32, row = row0 + lane;
+            const __half *in = KIND == kPoly || KIND >= kUpdate ? p.in + (long long)tp.matrix * p.in_planes * plane : nullptr;
+            __half *out = KIND == kGram || KIND == kPoly || KIND == kUpdate ? p.out + (long long)tp.matrix * p.out_planes * plane : nullptr;
+            for (int h = 0; h < p.halves; ++h, ++sub) {
+                const int acc = sub & 1, col0 = (tp.n * p.halves + h) * p.cols + quarter * width;
+                const uint32_t src = tmem_base + (uint32_t)acc * kTile + quarter * width + ((uint32_t)(quad * 32) << 16);
+                [[maybe_unused]] uint4 hi[4], lo[4];  // of the tile of A or Y that is added, fetched ahead
+                auto fetch = [&](int col) {
+                    stg.fetch(hi, in, p.pitch, row0, p.rows, col);
+                    if (p.in_planes > 1) stg.fetch(lo, in + plane, p.pitch, row0, p.rows, col);
+                };
+                if (KIND == kPoly || KIND >= kUpdate) fetch(col0);
+                ok = __all_sync(0xFFFFFFFFu, wait(smem_addr(&acc_full[acc]), (uint32_t)((sub >> 1) & 1)));
+                if (!ok) break;
+                tmem_fence_after();
+#pragma unroll 1
+                for (int at = 0; at < width; at += 32) {
+                    const int col = col0 + at;
+                    uint32_t raw[32];
+                    __syncwarp();
+                    tmem_load32(src + at, raw);
+                    tmem_wait_load(raw);
+                    if (at + 32 == width) {  // the accumulator is read: the tile after the next may overwrite it
+                        tmem_fence_before();
+                        __syncwarp();
+                        if (lane == 0) barrier_arrive_leader(smem_addr(&acc_empty[acc]));
+                    }
+                    float z[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(raw[i]) * p.acc_scale;
+                    if (row0 >= p.rows || col >= (KIND == kResult ? p.columns : p.pitch)) continue;
+                    if constexpr (KIND == kGramPart) {
+                        float *dst = p.part + ((long long)(tp.matrix * p.splits + tp.split) * p.rows + row) * p.pitch + col;
+                        if (row < p.rows) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4)
+                                if (col + i < p.pitch && RSDGC_IN_BOUNDS(col + i + 4 <= p.pitch && tp.split < p.splits))
+                                    *reinterpret_cast<float4 *>(dst + i) = make_float4(z[i], z[i + 1], z[i + 2], z[i + 3]);
+                        }
+                        continue;
+                    }
+                    if constexpr (KIND == kPoly || KIND >= kUpdate) {
+                        stg.deal(hi);
+                        stg.add_row(z, p.in_scale);
+                        if (p.in_planes > 1) {
+                            stg.deal(lo);
+                            stg.add_row(z, p.in_scale);
+                        }
+                        if (at + 32 < width) fetch(col + 32);
+                    }
+                    if constexpr (KIND == kResult) {
+                        stg.template put_row<T>(z);
+                        stg.store_result((uint16_t *)p.result + tp.matrix * p.result_matrix, p.result_row, row0, p.rows, col, p.columns,
+                                         p.result_wide);
+                        continue;
+                    }
+                    // across the diagonal unless the tile there is computed itself
+                    const bool across = KIND != kUpdate && row0 / tile_cols * tile_cols >= (col / kTile + 1) * kTile;
+                    for (int i = 0;; ++i) {
+                        stg.template put_row<__half>(z);
+                        stg.store(out + i * plane, p.pitch, row0, p.rows, col);
+                        if (across) {
+                            stg.put_column(z);
+                            stg.store(out + i * plane, p.pitch, col, p.rows, row0);
+                        }
+                        if (i + 1 == p.out_planes) break;
+                        ortho_rest(z);
+                    }
+                }
+            }
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (threadIdx.x < 2) store_in(smem_addr(&failed[rank]), dead, threadIdx.x);
+    __syncwarp();
+    cluster_sync_all();  // the peer may still signal this CTA's barriers, and its MMAs read this CTA's memory
+    if (failed[0] | failed[1]) {
+        // A wait gave up in one of the CTAs, and both have left their loops: what they have in flight still reads and
+        // writes their shared memory and TMEM.  Let it end (bounded).
+        if (rank == 1 && warp == 0 && lane <= stages)
+            store_in(lane < stages ? smem_addr(&sent[1][lane]) : smem_addr(&issued[1]), lane < stages ? sent[1][lane] : issued[1], 0);
+        __syncwarp();
+        cluster_sync_all();
+        if (warp == 0 && rank == 0 && lane < stages) {
+            // a lane per place in the ring, its latest stage `i`; a producer is at most a ring ahead of the other, so that the
+            // barrier is in that stage's phase and lacks at most what only one of the two has issued
+            const int most = max(issued[0], issued[1]), i = most - 1 - (most - 1 - lane + stages) % stages;
+            if (i >= 0 && i < most) {
+                const uint32_t bar = smem_addr(&full[lane]);
+                if (i >= issued[1]) barrier_complete(bar, (uint32_t)sent[0][lane]);
+                if (i >= issued[0]) barrier_expect(bar, (uint32_t)sent[1][lane]);
+                for (unsigned n = 0; n < kOperatorPolls && !barrier_try(bar, (uint32_t)(i / stages) & 1u); ++n) {}
+            }
+        }
+        if (warp == 1) {
+            if (rank == 0 && elect_one()) mma_commit_both(smem_addr(&drain));  // by the thread that issued them
+            __syncwarp();
+            for (unsigned n = 0; n < kOperatorPolls && !barrier_try(smem_addr(&drain), 0); ++n) {}
+        }
+        __syncwarp();
+        __syncthreads();
+        cluster_sync_all();
+    }
+    if (warp == 2)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem_base));
+}
+
+// ---- the kernels around the products ------------------------------------------------------------------
+constexpr int kOrthoItem = 1024;   // columns of a row that a warp takes at a time, eight per lane
+constexpr int kOrthoLoadWarps = 8;
+
+// Eight values of a row from p on, of which n exist.
+template <typename T>
+__device__ __forceinline__ void ortho_load8(float (&v)[8], const T *p, int n, bool wide)
+{
+    if (wide && n >= 8) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        } else {
+            const uint4 a = __ldg(reinterpret_cast<const uint4 *>(p));
+            T t[8];
+            *reinterpret_cast<uint4 *>(t) = a;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = to_f32(t[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(p[i]) : 0.0f;
+    }
+}
+
+// |X|^2 of each matrix in `parts` parts, in binary64 (neither the squares of large nor of small gradients leave its range).
+template <typename T>
+__global__ void __launch_bounds__(32 * kOrthoLoadWarps)
+k_ortho_norm(const T *__restrict__ x, long long row_stride, long long matrix_stride, int rows, int cols, int wide, int parts,
+             double *__restrict__ partial)
+{
+    __shared__ double sums[kOrthoLoadWarps];
+    const int matrix = blockIdx.x / parts, part = blockIdx.x - matrix * parts, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    grid_dependency_wait();
+    grid_dependency_launch_next();
+    const T *m = x + matrix * matrix_stride;
+    const int across = (cols + kOrthoItem - 1) / kOrthoItem;
+    double s = 0.0;
+    for (long long i = part * kOrthoLoadWarps + warp; i < (long long)rows * across; i += parts * kOrthoLoadWarps) {
+        const long long row = i / across;
+        const int c0 = (int)(i - row * across) * kOrthoItem;
+#pragma unroll
+        for (int j = 0; j < kOrthoItem / 256; ++j) {
+            const int c = c0 + j * 256 + lane * 8;
+            float v[8];
+            if (c < cols) {
+                ortho_load8(v, m + row * row_stride + c, cols - c, wide);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s = fma((double)v[k], (double)v[k], s);
+            }
+        }
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    if (lane == 0) sums[warp] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kOrthoLoadWarps; ++w) s += sums[w];
+        partial[blockIdx.x] = s;
+    }
+}
+
+// Y = X / (|X| + eps), scaled, in two binary16 planes.  A matrix of zeros stays one; one that is not finite becomes NaN.
+template <typename T>
+__global__ void __launch_bounds__(32 * kOrthoLoadWarps)
+k_ortho_load(const T *__restrict__ x, long long row_stride, long long matrix_stride, int rows, int cols, int wide, int parts,
+             const double *__restrict__ partial, float eps, __half *__restrict__ y, long long pitch)
+{
+    const int matrix = blockIdx.x / parts, part = blockIdx.x - matrix * parts, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    grid_dependency_wait();
+    grid_dependency_launch_next();
+    double s = 0.0;
+    for (int i = lane; i < parts; i += 32) s += partial[matrix * parts + i];
+#pragma unroll
+    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    const double norm = sqrt(s);
+    // in two factors, so that neither leaves binary32's range
+    const double first = norm < 1e-20 ? 0x1p60 : norm > 1e20 ? 0x1p-60 : 1.0;
+    const float f1 = (float)first, f2 = norm == 0.0 ? 0.0f : norm < INFINITY ? (float)(kOrthoScale / ((norm + eps) * first)) : NAN;
+    const T *m = x + matrix * matrix_stride;
+    __half *hi = y + matrix * 2 * (long long)rows * pitch, *lo = hi + (long long)rows * pitch;
+    const int across = (cols + kOrthoItem - 1) / kOrthoItem;
+    for (long long i = part * kOrthoLoadWarps + warp; i < (long long)rows * across; i += parts * kOrthoLoadWarps) {
+        const long long row = i / across;
+        const int c0 = (int)(i - row * across) * kOrthoItem;
+#pragma unroll
+        for (int j = 0; j < kOrthoItem / 256; ++j) {
+            const int c = c0 + j * 256 + lane * 8;
+            if (c >= pitch || !RSDGC_IN_BOUNDS(row < rows && c + 8 <= pitch)) continue;
+            float v[8];
+            ortho_load8(v, m + row * row_stride + c, cols - c, wide);
+            uint32_t a[4], b[4];
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+                const float u = v[k] * f1 * f2, w = v[k + 1] * f1 * f2;
+                a[k >> 1] = pack2<__half>(u, w);
+                b[k >> 1] = pack2<__half>(u - __half2float(__float2half_rn(u)), w - __half2float(__float2half_rn(w)));
+            }
+            *reinterpret_cast<uint4 *>(hi + row * pitch + c) = make_uint4(a[0], a[1], a[2], a[3]);
+            *reinterpret_cast<uint4 *>(lo + row * pitch + c) = make_uint4(b[0], b[1], b[2], b[3]);
+        }
+    }
+}
+
+// A = the sum of its parts, in order: a CTA per block of 32 x 32 on or below the diagonal, which it also writes across it.
+__global__ void __launch_bounds__(256)
+k_ortho_join(const float *__restrict__ part, int splits, int n, long long pitch, int blocks, __half *__restrict__ out, int planes)
+{
+    __shared__ float block[32][33];
+    int i = blockIdx.x % (blocks * (blocks + 1) / 2);
+    const int matrix = blockIdx.x / (blocks * (blocks + 1) / 2);
+    int bi = (int)((sqrtf(8.0f * i + 1.0f) - 1.0f) * 0.5f);
+    while (bi * (bi + 1) / 2 > i) --bi;
+    while ((bi + 1) * (bi + 2) / 2 <= i) ++bi;
+    i -= bi * (bi + 1) / 2;
+    const int lane = threadIdx.x & 31, row0 = threadIdx.x >> 5;
+    grid_dependency_wait();
+    grid_dependency_launch_next();
+    const long long plane = (long long)n * pitch;
+    out += matrix * planes * plane;
+    part += matrix * splits * plane;
+    auto put = [&](int r, int c, float v) {
+        if (r >= n || c >= pitch || !RSDGC_IN_BOUNDS(r >= 0 && c >= 0)) return;
+        const __half h = __float2half_rn(v);
+        out[r * pitch + c] = h;
+        if (planes > 1) out[plane + r * pitch + c] = __float2half_rn(v - __half2float(h));
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = bi * 32 + row0 + 8 * j, c = i * 32 + lane;
+        float v = 0.0f;
+        if (r < n && c < pitch)
+            for (int s = 0; s < splits; ++s) v += part[s * plane + r * pitch + c];
+        block[row0 + 8 * j][lane] = v;
+        put(r, c, v);
+    }
+    if (bi == i) return;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) put(i * 32 + row0 + 8 * j, bi * 32 + lane, block[lane][row0 + 8 * j]);
+}
+
+// ---- host -----------------------------------------------------------------------------------------------
+RSDGC_DEFINE_DEBUG_BOUNDS(orthogonal_debug_bounds)
+
+namespace {
+
+constexpr int kOrthoPairs = 74;          // of CTAs on the device, for what workspaces depend on
+constexpr int kOrthoLoadParts = 296;     // most CTAs per matrix of the two passes over X
+constexpr int64_t kOrthoPrecise = 256;   // shorter sides up to this take three products for every result
+
+inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
+inline int tiles_of(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+// What a call does with its sizes.
+struct OrthoLayout {
+    int64_t batch, rows, cols, side, pitch, side_pitch;  // side: of A
+    bool tall;
+    int segments, planes, parts, splits, split_steps;
+    int64_t y[2], a, b, norm, sums, bytes;
+};
+
+OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols, int out_dtype)
+{
+    OrthoLayout L{};
+    L.batch = batch;
+    L.rows = rows;
+    L.cols = cols;
+    L.tall = rows > cols;
+    L.side = L.tall ? cols : rows;
+    L.pitch = up(cols, 8);
+    L.side_pitch = up(L.side, 8);
+    L.planes = out_dtype == RSDGC_F16 || L.side <= kOrthoPrecise ? 2 : 1;
+    L.segments = L.planes == 2 ? 3 : 1;
+    const int64_t items = rows * ((cols + kOrthoItem - 1) / kOrthoItem), want = (items + kOrthoLoadWarps - 1) / kOrthoLoadWarps;
+    L.parts = (int)(want < kOrthoLoadParts ? want : kOrthoLoadParts);
+    // A's tiles are few where it is small: its contraction is cut so that every pair of CTAs has a part, of 8 steps at least
+    const int64_t m = tiles_of(L.side, kTile), tiles = batch * m * (m + 1) / 2;
+    const int64_t steps = (int64_t)L.segments * tiles_of(L.tall ? rows : cols, kStepK);
+    int64_t s = tiles > 0 ? kOrthoPairs / tiles : 1;
+    if (s > steps / 8) s = steps / 8;
+    if (s < 1) s = 1;
+    L.split_steps = (int)((steps + s - 1) / s);
+    L.splits = (int)((steps + L.split_steps - 1) / L.split_steps);
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t p = at;
+        at = up(at + bytes, 256);
+        return p;
+    };
+    for (int i = 0; i < 2; ++i) L.y[i] = take(batch * 2 * rows * L.pitch * 2);
+    L.a = take(batch * L.planes * L.side * L.side_pitch * 2);
+    L.b = take(batch * L.planes * L.side * L.side_pitch * 2);
+    L.norm = take(batch * L.parts * 8);
+    L.sums = take(L.splits > 1 ? batch * L.splits * L.side * L.side_pitch * 4 : 0);
+    L.bytes = at;
+    return L;
+}
+
+int ortho_check(int64_t batch, int64_t rows, int64_t cols, int out_dtype)
+{
+    if (batch < 0 || rows < 0 || cols < 0 || (out_dtype != RSDGC_BF16 && out_dtype != RSDGC_F16)) return RSDGC_ERR_INVALID;
+    if (rows > (1 << 24) || cols > (1 << 24) || (rows < cols ? rows : cols) > (1 << 15) || batch > (1 << 20)) return RSDGC_ERR_CAPACITY;
+    // tiles of 256 x 128 of all matrices, and the grids of the other kernels
+    const int64_t tiles = batch * tiles_of(rows, kTile) * tiles_of(cols, kTile / 2) * 64;
+    return tiles > INT_MAX || batch * kOrthoLoadParts > INT_MAX ? RSDGC_ERR_CAPACITY : RSDGC_OK;
+}
+
+// The polynomials as a whole keep singular values within [0, most], most <= 2, and |b x + c x^2| <= 7.5 for x = s^2: what the scaled
+// binary16 planes hold.  s is at most 1 at first; a step's largest value lies at an end or where a + 3 b s^2 + 5 c s^4 = 0.
+bool ortho_bounded(const float *coef, int steps)
+{
+    double most = 1.0;
+    for (int i = 0; i < steps; ++i) {
+        const double a = coef[3 * i], b = coef[3 * i + 1], c = coef[3 * i + 2];
+        if (!(std::fabs(a) < 1e3 && std::fabs(b) < 1e3 && std::fabs(c) < 1e3)) return false;
+        double top = 0.0, poly = 0.0;
+        auto at = [&](double s2) {
+            if (!(s2 >= 0.0 && s2 <= most * most)) return;
+            const double v = std::fabs(std::sqrt(s2) * (a + s2 * (b + s2 * c)));
+            if (v > top) top = v;
+        };
+        auto inner = [&](double s2) {
+            if (!(s2 >= 0.0 && s2 <= most * most)) return;
+            const double v = std::fabs(s2 * (b + s2 * c));
+            if (v > poly) poly = v;
+        };
+        at(most * most);
+        inner(most * most);
+        if (c != 0.0) {
+            const double root = 9.0 * b * b - 20.0 * a * c;
+            if (root >= 0.0) {
+                at((-3.0 * b + std::sqrt(root)) / (10.0 * c));
+                at((-3.0 * b - std::sqrt(root)) / (10.0 * c));
+            }
+            inner(-b / (2.0 * c));
+        } else if (b != 0.0) {
+            at(-a / (3.0 * b));
+        }
+        most = top * (1.0 + 0x1p-7);  // and what the roundings add
+        if (most > 2.0 || poly > 7.5) return false;
+    }
+    return true;
+}
+
+// [matrix x plane][rows][cols] binary16 values, boxes of 64 x 64; what lies outside reads as zero
+cudaError_t ortho_map(CUtensorMap *map, const void *base, int64_t slabs, int64_t rows, int64_t cols, int64_t pitch)
+{
+    EncodeFn fn = encode_fn();
+    if (!fn) return cudaErrorNotSupported;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)slabs};
+    const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)pitch * 2 * (cuuint64_t)rows};
+    const cuuint32_t box[3] = {64, 64, 1}, one[3] = {1, 1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base), dims, strides, box, one,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+// Pairs of CTAs that the device holds at a time; 0 and an error in *e if the kernel cannot run.
+template <int KIND, typename T>
+int ortho_pairs(cudaError_t *e)
+{
+    static std::mutex mu;
+    static int most[64];
+    int dev = 0;
+    *e = cudaGetDevice(&dev);
+    if (*e != cudaSuccess) return 0;
+    std::lock_guard<std::mutex> lock(mu);
+    int &m = most[dev & 63];
+    if (m) return m;
+    *e = cudaFuncSetAttribute(k_ortho<KIND, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOrthoSmem);
+    if (*e != cudaSuccess) return 0;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = (unsigned)current_device_sms();
+    cfg.blockDim = kOrthoThreads;
+    cfg.dynamicSmemBytes = kOrthoSmem;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = 2;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    int n = 0;
+    *e = cudaOccupancyMaxActiveClusters(&n, k_ortho<KIND, T>, &cfg);
+    if (*e == cudaSuccess && n < 1) *e = cudaErrorLaunchOutOfResources;
+    return *e == cudaSuccess ? m = n : 0;
+}
+
+// Tiles of 256 x 128, 256 x 256 or 256 x 512 by the cycles that they take dealt to the pairs (512 per contraction step and
+// 256 columns, some 6000 to empty an accumulator; 1.25 and 1.6 times that for the lost operand reuse of 256 and 128 columns).
+void ortho_columns(OrthoParams &p, int64_t batch, int pairs)
+{
+    double best = 0.0;
+    for (int wide = kTile / 2; wide <= 2 * kTile; wide *= 2) {
+        if (wide > kTile && p.columns <= kTile) break;
+        const int across = tiles_of(p.columns, wide);
+        long long per = (long long)p.m_tiles * across;
+        if (p.symmetric) {
+            per = 0;
+            for (int m = 0; m < p.m_tiles; ++m) {
+                const int here = ((m + 1) * kTile + wide - 1) / wide;
+                per += here < across ? here : across;
+            }
+        }
+        const long long tiles = per * batch * p.splits;
+        const double part = (double)wide / kTile, loss = wide > kTile ? 1.0 : wide == kTile ? 1.25 : 1.6;
+        const double cost = (double)((tiles + pairs - 1) / pairs) * loss * part * (512.0 * p.split_steps + 6000.0);
+        if (best > 0.0 && cost > best) continue;
+        best = cost;
+        p.halves = wide > kTile ? 2 : 1;
+        p.cols = wide < kTile ? wide : kTile;
+        p.n_tiles = across;
+        p.per = (int)per;
+        p.tiles = (int)tiles;
+    }
+    p.stages = kRingBlocks / (1 + p.halves);
+}
+
+struct OrthoCall {
+    OrthoLayout l;
+    const void *x;
+    int64_t x_row, x_matrix;
+    int dtype;
+    void *out;
+    int64_t out_row, out_matrix;
+    int out_dtype;
+    const float *coef;
+    int steps;
+    float eps;
+    unsigned char *workspace;
+    cudaStream_t s;
+};
+
+template <int KIND, typename T>
+cudaError_t ortho_product(OrthoParams &p, const OrthoCall &c)
+{
+    cudaError_t e = cudaSuccess;
+    const int most = ortho_pairs<KIND, T>(&e);
+    if (e != cudaSuccess) return e;
+    ortho_columns(p, c.l.batch, most);
+    const unsigned pairs = (unsigned)(p.tiles < most ? p.tiles : most);
+    return launch_chained(k_ortho<KIND, T>, 2 * pairs, kOrthoThreads, kOrthoSmem, c.s, 2, p);
+}
+
+template <typename T>
+cudaError_t ortho_load(const OrthoCall &c)
+{
+    const OrthoLayout &L = c.l;
+    const unsigned grid = (unsigned)(L.batch * L.parts);
+    const int wide = pointer_aligned(c.x, 16) && c.x_row * sizeof(T) % 16 == 0 && c.x_matrix * sizeof(T) % 16 == 0;
+    double *norm = (double *)(c.workspace + L.norm);
+    cudaError_t e = launch_chained(k_ortho_norm<T>, grid, 32 * kOrthoLoadWarps, 0, c.s, 1, (const T *)c.x, (long long)c.x_row,
+                                   (long long)c.x_matrix, (int)L.rows, (int)L.cols, wide, L.parts, norm);
+    if (e == cudaSuccess)
+        e = launch_chained(k_ortho_load<T>, grid, 32 * kOrthoLoadWarps, 0, c.s, 1, (const T *)c.x, (long long)c.x_row,
+                           (long long)c.x_matrix, (int)L.rows, (int)L.cols, wide, L.parts, (const double *)norm, c.eps,
+                           (__half *)(c.workspace + L.y[0]), (long long)L.pitch);
+    return e;
+}
+
+cudaError_t orthogonalize(const OrthoCall &c)
+{
+    const OrthoLayout &L = c.l;
+    cudaError_t e = operators_ready();
+    OrthoParams base;
+    std::memset(&base, 0, sizeof base);
+    base.polls = operator_polls();
+    base.segments = L.segments;
+    base.splits = 1;
+    if (e == cudaSuccess) e = operator_status_ptr(&base.status);
+    CUtensorMap y[2], a, b;
+    for (int i = 0; i < 2 && e == cudaSuccess; ++i) e = ortho_map(&y[i], c.workspace + L.y[i], 2 * L.batch, L.rows, L.cols, L.pitch);
+    if (e == cudaSuccess) e = ortho_map(&a, c.workspace + L.a, L.planes * L.batch, L.side, L.side, L.side_pitch);
+    if (e == cudaSuccess) e = ortho_map(&b, c.workspace + L.b, L.planes * L.batch, L.side, L.side, L.side_pitch);
+    if (e == cudaSuccess)
+        e = c.dtype == RSDGC_F32 ? ortho_load<float>(c) : c.dtype == RSDGC_BF16 ? ortho_load<__nv_bfloat16>(c) : ortho_load<__half>(c);
+    __half *const ap = (__half *)(c.workspace + L.a), *const bp = (__half *)(c.workspace + L.b);
+    for (int i = 0; i < c.steps && e == cudaSuccess; ++i) {
+        const CUtensorMap &from = y[i & 1];
+        __half *const yp = (__half *)(c.workspace + L.y[i & 1]);
+        OrthoParams p = base;  // A = Y Y^T or Y^T Y
+        p.a = p.b = from;
+        p.a_mn = p.b_mn = L.tall;
+        p.a_planes = p.b_planes = 2;
+        p.k_steps = tiles_of(L.tall ? L.rows : L.cols, kStepK);
+        p.rows = p.columns = (int)L.side;
+        p.pitch = L.side_pitch;
+        p.m_tiles = tiles_of(L.side, kTile);
+        p.symmetric = 1;
+        p.splits = L.splits;
+        p.split_steps = L.split_steps;
+        p.acc_scale = 0x1p-11f;  // 2^24 to 2^13
+        p.out = ap;
+        p.out_planes = L.planes;
+        p.part = (float *)(c.workspace + L.sums);
+        if (L.splits > 1) {
+            e = ortho_product<kGramPart, __half>(p, c);
+            const int blocks = tiles_of(L.side, 32);
+            if (e == cudaSuccess)
+                e = launch_chained(k_ortho_join, (unsigned)(L.batch * blocks * (blocks + 1) / 2), 256, 0, c.s, 1, (const float *)p.part,
+                                   L.splits, (int)L.side, (long long)L.side_pitch, blocks, ap, L.planes);
+        } else {
+            e = ortho_product<kGram, __half>(p, c);
+        }
+        if (e != cudaSuccess) break;
+        p.a = p.b = a;  // B = b A + c A A
+        p.a_mn = p.b_mn = 0;
+        p.a_planes = p.b_planes = p.in_planes = L.planes;
+        p.k_steps = tiles_of(L.side, kStepK);
+        p.splits = 1;
+        p.split_steps = L.segments * p.k_steps;
+        p.in = ap;
+        p.in_scale = c.coef[3 * i + 1];
+        p.acc_scale = c.coef[3 * i + 2] * 0x1p-13f;
+        p.out = bp;
+        e = ortho_product<kPoly, __half>(p, c);
+        if (e != cudaSuccess) break;
+        // B Y, or Y B where B is as good as its transpose
+        p.a = L.tall ? from : b;
+        p.b = L.tall ? b : from;
+        p.b_mn = !L.tall;
+        p.a_planes = L.tall ? 2 : L.planes;
+        p.b_planes = L.tall ? L.planes : 2;
+        p.symmetric = 0;
+        p.rows = (int)L.rows;
+        p.columns = (int)L.cols;
+        p.pitch = L.pitch;
+        p.m_tiles = tiles_of(L.rows, kTile);
+        p.band = p.m_tiles < 16 ? p.m_tiles : 16;
+        p.in = yp;
+        p.in_planes = 2;
+        p.in_scale = c.coef[3 * i];
+        p.acc_scale = 0x1p-13f;
+        p.out = (__half *)(c.workspace + L.y[(i + 1) & 1]);
+        p.out_planes = 2;
+        if (i + 1 < c.steps) {
+            e = ortho_product<kUpdate, __half>(p, c);
+        } else {
+            p.in_scale *= 1.0f / kOrthoScale;
+            p.acc_scale *= 1.0f / kOrthoScale;
+            p.result = c.out;
+            p.result_row = c.out_row;
+            p.result_matrix = c.out_matrix;
+            p.result_wide = pointer_aligned(c.out, 16) && c.out_row % 8 == 0 && c.out_matrix % 8 == 0;
+            e = c.out_dtype == RSDGC_BF16 ? ortho_product<kResult, __nv_bfloat16>(p, c) : ortho_product<kResult, __half>(p, c);
+        }
+    }
+    return e;
+}
+
+}  // namespace
+}  // namespace rsdgc
+
+using namespace rsdgc;
+
+extern "C" int64_t rsdgc_orthogonalize_workspace_bytes(int64_t n_matrices, int64_t n_rows, int64_t n_cols, int32_t out_dtype)
+{
+    const int rc = ortho_check(n_matrices, n_rows, n_cols, out_dtype);
+    return rc ? rc : ortho_layout(n_matrices, n_rows, n_cols, out_dtype).bytes;
+}
+
+extern "C" int rsdgc_orthogonalize(const void *x_dev, int64_t x_row_stride, int64_t x_matrix_stride, int32_t dtype, void *out_dev,
+                                   int64_t out_row_stride, int64_t out_matrix_stride, int32_t out_dtype, int64_t n_matrices,
+                                   int64_t n_rows, int64_t n_cols, const float *coefficients_host, int32_t n_steps, float eps,
+                                   void *workspace_dev, void *stream)
+{
+    const int rc = ortho_check(n_matrices, n_rows, n_cols, out_dtype);
+    if (rc) return rc;
+    if (!known_dtype(dtype) || !coefficients_host || n_steps < 1 || n_steps > kOrthoMaxSteps || !(eps >= 0.0f && eps < INFINITY))
+        return RSDGC_ERR_INVALID;
+    if (!ortho_bounded(coefficients_host, n_steps)) return RSDGC_ERR_INVALID;
+    if (n_matrices == 0 || n_rows == 0 || n_cols == 0) return RSDGC_OK;
+    if (!x_dev || !out_dev || !workspace_dev || (n_rows > 1 && (x_row_stride < n_cols || out_row_stride < n_cols)) ||
+        (n_matrices > 1 && (x_matrix_stride < n_cols || out_matrix_stride < n_cols)))
+        return RSDGC_ERR_INVALID;
+    if (!pointer_aligned(x_dev, dtype_bytes(dtype)) || !pointer_aligned(out_dev, 2) || !pointer_aligned(workspace_dev, 256))
+        return RSDGC_ERR_ALIGNMENT;
+    OperatorRange range("rsdgc_orthogonalize");
+    if (n_matrices == 1) x_matrix_stride = out_matrix_stride = 0;  // free, and so are a single row's
+    if (n_rows == 1) x_row_stride = out_row_stride = 0;
+    const OrthoCall c = {ortho_layout(n_matrices, n_rows, n_cols, out_dtype), x_dev, x_row_stride, x_matrix_stride, dtype, out_dev,
+                         out_row_stride, out_matrix_stride, out_dtype, coefficients_host, n_steps, eps, (unsigned char *)workspace_dev,
+                         (cudaStream_t)stream};
+    return operator_result(orthogonalize(c));
+}
