@@ -463,7 +463,7 @@ int rsdgc_head_distill_backward(const void *hidden_dev, int64_t hidden_stride, c
  * Errors: INVALID (a needed pointer NULL, a stride too small, sizes < 0, width < 1, types), ALIGNMENT (a pointer that is not a
  * multiple of its element size), CAPACITY (n_seq or n_steps > 2^30, width > 2^24, n_seq * ceil(width / 64) > 2^28 - 1), CUDA.
  */
-#define RSDGC_SCAN_STATE_STEPS 64
+#define RSDGC_SCAN_STATE_STEPS 16
 int rsdgc_gated_scan_forward(const void *x_dev, int64_t x_seq, int64_t x_step, const void *gate_dev, int64_t gate_seq,
                              int64_t gate_step, const void *gate_bias_dev, void *y_dev, int64_t y_seq, int64_t y_step,
                              const float *first_dev, float *last_dev, const uint8_t *restart_dev, int64_t restart_stride,
@@ -475,7 +475,7 @@ int rsdgc_gated_scan_forward(const void *x_dev, int64_t x_seq, int64_t x_step, c
  *   delta[t] = dy[t] + a[t+1] * delta[t+1] (0 across a restart; dlast behind the last step),
  *   dx[t] = (1 - a[t]) * delta[t],  dgate[t] = delta[t] * a[t] * (1 - a[t]) * (h[t-1] - x[t]),
  *   dbias = sum over sequences and steps of dgate,  dfirst = a[0] * delta[0] (0 if step 0 is a restart).
- * The states within a block of RSDGC_SCAN_STATE_STEPS steps are computed again from the saved ones, in binary32.
+ * The states within a run of RSDGC_SCAN_STATE_STEPS steps are computed again from the saved ones, in binary32.
  * dx, dgate (`dtype`), dbias (grad_dtype, any of the three types), dfirst (binary32, may be dlast's array): each optional, one at least.
  * restart, lengths: as in the forward call; dx and dgate behind a length are not written.  workspace_dev:
  * rsdgc_gated_scan_workspace_bytes() bytes, 16-byte aligned, needed for dbias.  n_seq = 0 or n_steps = 0: dbias = 0, dfirst =

@@ -594,7 +594,7 @@ def head_distill_backward(hidden, weight, top_index, top_logit, temperature: flo
         _check(code, "rsdgc_head_distill_backward")
 
 
-SCAN_STATE_STEPS = 64
+SCAN_STATE_STEPS = 16
 
 
 def gated_scan_states_shape(n_seq: int, n_steps: int, width: int) -> Tuple[int, int, int]:
