@@ -7,14 +7,19 @@
 // computed side by side and joined.  b is formed as a value of its own and the state as h + b (x - h), so that a slow
 // channel (b of 1e-5) keeps its digits, which a, next to 1, would round away.
 //
-// A warp takes 64 channels (two a lane, one 4-byte or 8-byte access per row) and runs of S steps, straight from memory to
-// registers; the next run's rows are on their way while a run is computed.  Where there are sequences enough for every warp
-// to have one, it walks alone.  Otherwise W warps of a CTA take W runs side by side, say what their runs do to a state (L, Q)
-// in shared memory and start again from the state that follows; and the CTAs of a cluster do the same with W runs each,
-// through one another's shared memory.  Runs are joined in the order of time, whoever is first: results are the same bits from
-// call to call.
+// A warp takes 64 channels (two a lane) and runs of 16 steps; the next two runs' rows are on their way through its own ring in shared
+// memory while a run is computed.  Three ways to deal the runs, by how many (sequence, 64 channels) units there are:
+//  - every warp walks a unit of its own (W = 1);
+//  - a CTA's W warps take a unit's runs in turn and hand the state on from warp to warp.  With W = 8 and 12 the critical path is not a run's 16
+//    steps but one step of its (L, Q), which the warp has formed beforehand: 4 x 8192 x 2048 bfloat16, 128 units: 115 us before, 74 us after;
+//  - few units: the CTAs of a cluster take W runs each side by side, tell one another what those do to a state, and each run starts from
+//    the state that follows (1 x 65536 x 1024 binary16: 469 us with one CTA a unit, 192 us with 7).
+// Runs are joined in the order of time, whoever is first: results are the same bits from call to call.
+// Rows that do not start on 16-byte boundaries arrive in 16-byte pieces too, one more a row, and are shifted when they are read
+// (8 x 4096 x 2047 bfloat16: 129 us forward, 594 us with loads of single values).
 //
-// What bounds it: memory.
+// What bounds it: memory where there are units for all multiprocessors (8 x 4096 x 4096 bfloat16: 153 us forward, 5.2 TB/s; 253 us
+// backward, 5.3 TB/s), the instructions of a run on the units' multiprocessors where there are not.
 #include <atomic>
 #include <climits>
 #include <mutex>
@@ -29,6 +34,15 @@ constexpr int kScanGroup = 64;      // channels of a warp
 constexpr int kRun = RSDGC_SCAN_STATE_STEPS;  // steps of a run
 constexpr int kScanCluster = 8;     // most CTAs that share a sequence's group
 constexpr int kScanLoneWarps = 4;   // of a CTA whose warps walk alone
+
+constexpr int kScanAhead = 8;       // chains of so many warps and more hand a state on before they compute their run's steps
+
+// Warps of a multiprocessor that the registers are cut for.  Few with many registers do better than many with few: backward with
+// 8 warps 253 us, with 12 warps 286 us, with 16 261 us, with 6 407 us (8 x 4096 x 4096 bfloat16); a chain of 12 has a multiprocessor to itself.
+template <typename T>
+constexpr int scan_forward_warps(int w) { return sizeof(T) == 4 || w == 12 ? 12 : 16; }
+template <typename T>
+constexpr int scan_backward_warps(int w) { return w == 12 ? 12 : 8; }
 
 struct ScanView {                   // a [sequences][steps][width] operand
     const void *p;
@@ -49,7 +63,7 @@ struct ScanParams {
     float *partial;                 // backward: [sequence parts x cluster][width], or NULL
     int n_seq, n_steps, width, groups, runs;
     int cluster, seq_parts;
-    int vec, wide;                  // pairs of channels may be accessed at once; 16 bytes may be read at once
+    int vec, wide;                  // results: pairs of channels may be written at once; operands: rows start on 16-byte boundaries
 };
 
 __device__ __forceinline__ void scan_store_in(uint32_t addr, uint32_t rank, float4 v)  // to a CTA of the cluster
@@ -61,12 +75,6 @@ __device__ __forceinline__ void scan_store_in(uint32_t addr, uint32_t rank, floa
 template <typename T>
 struct Channels {
     typedef uint32_t Raw;
-    static __device__ __forceinline__ Raw load(const T *p, bool pair, int n)
-    {
-        if (pair) return __ldg(reinterpret_cast<const uint32_t *>(p));
-        const unsigned short *q = reinterpret_cast<const unsigned short *>(p);
-        return (n > 0 ? (uint32_t)__ldg(q) : 0u) | (n > 1 ? (uint32_t)__ldg(q + 1) << 16 : 0u);
-    }
     static __device__ __forceinline__ Raw none() { return 0u; }
     static __device__ __forceinline__ float2 widen(Raw r)
     {
@@ -74,9 +82,9 @@ struct Channels {
         *reinterpret_cast<uint32_t *>(v) = r;
         return make_float2(to_f32(v[0]), to_f32(v[1]));
     }
-    static __device__ __forceinline__ void store(T *p, bool pair, int n, float2 v)
+    static __device__ __forceinline__ Raw narrow(float2 v) { return pack2<T>(v.x, v.y); }
+    static __device__ __forceinline__ void store(T *p, bool pair, int n, Raw r)
     {
-        const uint32_t r = pack2<T>(v.x, v.y);
         if (pair) {
             *reinterpret_cast<uint32_t *>(p) = r;
         } else {
@@ -89,14 +97,10 @@ struct Channels {
 template <>
 struct Channels<float> {
     typedef float2 Raw;
-    static __device__ __forceinline__ Raw load(const float *p, bool pair, int n)
-    {
-        if (pair) return __ldg(reinterpret_cast<const float2 *>(p));
-        return make_float2(n > 0 ? __ldg(p) : 0.0f, n > 1 ? __ldg(p + 1) : 0.0f);
-    }
     static __device__ __forceinline__ Raw none() { return make_float2(0.0f, 0.0f); }
     static __device__ __forceinline__ float2 widen(Raw r) { return r; }
-    static __device__ __forceinline__ void store(float *p, bool pair, int n, float2 v)
+    static __device__ __forceinline__ Raw narrow(float2 v) { return v; }
+    static __device__ __forceinline__ void store(float *p, bool pair, int n, Raw v)
     {
         if (pair) {
             *reinterpret_cast<float2 *>(p) = v;
@@ -149,14 +153,30 @@ constexpr float kScanLeast = 1.2e-38f;
 __device__ __forceinline__ float scan_through(float p, float q) { return p == 0.0f || q == 0.0f ? 0.0f : fmaxf(p * q, kScanLeast); }
 
 // A warp hands a state on to the next one: written to that warp's place, then the two meet at its barrier.
+template <int W>
 __device__ __forceinline__ void scan_hand_on(float2 *place, int warp, int lane, float2 v)
 {
     place[warp * 32 + lane] = v;
-    asm volatile("bar.arrive %0, 64;" ::"r"(1 + warp) : "memory");
+    if constexpr (W == 2) {  // constants: with a number from a register a CTA holds all sixteen, of a multiprocessor's 64
+        if (warp)
+            asm volatile("bar.arrive 2, 64;" ::: "memory");
+        else
+            asm volatile("bar.arrive 1, 64;" ::: "memory");
+    } else {
+        asm volatile("bar.arrive %0, 64;" ::"r"(1 + warp) : "memory");
+    }
 }
+template <int W>
 __device__ __forceinline__ float2 scan_take_over(const float2 *place, int warp, int lane)
 {
-    asm volatile("bar.sync %0, 64;" ::"r"(1 + warp) : "memory");
+    if constexpr (W == 2) {
+        if (warp)
+            asm volatile("bar.sync 2, 64;" ::: "memory");
+        else
+            asm volatile("bar.sync 1, 64;" ::: "memory");
+    } else {
+        asm volatile("bar.sync %0, 64;" ::"r"(1 + warp) : "memory");
+    }
     return place[warp * 32 + lane];
 }
 
@@ -196,31 +216,38 @@ __device__ __forceinline__ int scan_length(const ScanParams &p, int seq)
     return l < 0 ? 0 : l > p.n_steps ? p.n_steps : (int)l;
 }
 
-__device__ __forceinline__ void scan_copy(uint32_t dst, const void *src, int bytes, int size)  // what is missing becomes zeros
+__device__ __forceinline__ void scan_copy(uint32_t dst, const void *src, int bytes)  // 16 bytes; what is missing becomes zeros
 {
-    if (size == 16)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(__cvta_generic_to_global(src)), "r"(bytes) : "memory");
-    else if (size == 8)
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(__cvta_generic_to_global(src)), "r"(bytes) : "memory");
-    else
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(__cvta_generic_to_global(src)), "r"(bytes) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(__cvta_generic_to_global(src)), "r"(bytes) : "memory");
 }
 
-// A warp's own ring in shared memory: two stages with a run's rows of OPS operands each.
-template <typename T, int OPS>
+// A warp's own ring in shared memory: two stages with a run's rows of OPS operands each.  Rows arrive in pieces of 16 bytes.  SHIFT: they need not
+// start on such a boundary; a row then has one piece more, and its values lie as far into the first one as they do in memory.
+template <typename T, int OPS, bool SHIFT>
 struct ScanRing {
     typedef typename Channels<T>::Raw Raw;
-    static constexpr int kRow = kScanGroup * (int)sizeof(T), kTileBytes = kRun * kRow, kStage = OPS * kTileBytes, kBytes = 2 * kStage;
+    static constexpr int kRow = kScanGroup * (int)sizeof(T) + (SHIFT ? 16 : 0), kTileBytes = kRun * kRow, kStage = OPS * kTileBytes,
+                         kBytes = 2 * kStage;
     uint32_t base;
     int lane, stage;
+    uint32_t first[SHIFT ? OPS : 1], down[SHIFT ? OPS : 1];  // where a run's first row lies in its piece, and how far on the next one
     __device__ __forceinline__ ScanRing(unsigned char *smem, int warp, int lane_) : base(smem_addr(smem) + warp * kBytes), lane(lane_), stage(0) {}
+    // ... of a sequence: runs start at multiples of 16 steps, so all of them lie alike
+    __device__ __forceinline__ void start(int op, const ScanView &v, int seq, const ScanPlace &at)
+    {
+        if constexpr (SHIFT) {
+            first[op] = (uint32_t)(uintptr_t)((const T *)v.p + seq * v.seq + (at.c - 2 * lane)) & 15u;
+            down[op] = (uint32_t)(v.step * (int)sizeof(T)) & 15u;
+        }
+    }
     // the rows of a run from step t on; rows outside [0, len) are not read, they become zeros
     __device__ __forceinline__ void fetch(int op, const ScanParams &p, const ScanView &v, int seq, const ScanPlace &at, int t, int len) const
     {
         const uint32_t to = base + stage * kStage + op * kTileBytes;
         const T *src = (const T *)v.p + seq * v.seq;
-        if (p.wide) {
-            constexpr int kPieces = kRow / 16, kRows = 32 / kPieces, V = 16 / (int)sizeof(T);
+        constexpr int kPieces = kRow / 16, V = 16 / (int)sizeof(T);
+        if constexpr (!SHIFT) {
+            constexpr int kRows = 32 / kPieces;
             const int row = lane / kPieces, c = (at.c - 2 * lane) + lane % kPieces * V;
             const int bytes = min(max(p.width - c, 0), V) * (int)sizeof(T);
             const T *q = src + (long long)(t + row) * v.step + c;
@@ -230,26 +257,40 @@ struct ScanRing {
             for (int j = 0; j < kRun / kRows; ++j, q += down) {
                 const bool there = t + row + j * kRows >= 0 && t + row + j * kRows < len && bytes > 0 &&
                                    RSDGC_IN_BOUNDS(seq < p.n_seq && len <= p.n_steps && c + bytes / (int)sizeof(T) <= p.width);
-                scan_copy(dst + j * 512, there ? (const void *)q : v.p, there ? bytes : 0, 16);
+                scan_copy(dst + j * 512, there ? (const void *)q : v.p, there ? bytes : 0);
             }
-            return;
-        }
-        src += (long long)t * v.step + at.c;
-        const uint32_t dst = to + lane * 2 * (int)sizeof(T);
+        } else {
+            const int c = at.c - 2 * lane, here = min(max(p.width - c, 0), kScanGroup) * (int)sizeof(T);
+            const long long pitch = v.step * (long long)sizeof(T);
+            const char *const row0 = reinterpret_cast<const char *>(src + (long long)t * v.step + c);
+            const bool inside = here > 0 && RSDGC_IN_BOUNDS(seq < p.n_seq && len <= p.n_steps && c + here / (int)sizeof(T) <= p.width);
+            if (row0 - 15 < (const char *)v.p) {
+                // a first piece may begin before the operand: its values one by one (what lies before any other row is the operand's)
+                for (int i = lane; i < kRun * kScanGroup; i += 32) {
+                    const int row = i / kScanGroup, at_byte = i % kScanGroup * (int)sizeof(T);
+                    const bool there = t + row >= 0 && t + row < len && at_byte < here && inside;
+                    const char *const q = row0 + row * pitch + at_byte;
+                    const uint32_t dst = to + row * kRow + ((first[op] + row * down[op]) & 15u) + at_byte;
+                    if constexpr (sizeof(T) == 4)
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(dst), "f"(there ? *(const float *)q : 0.0f) : "memory");
+                    else
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst), "h"(there ? *(const unsigned short *)q : (unsigned short)0)
+                                     : "memory");
+                }
+                return;
+            }
+            // the rows' last pieces in a round of their own
+            constexpr int kMost = kPieces - 1, kRows = 32 / kMost;
+            auto copy = [&](const char *row_at, int row, int piece) {
+                const uint32_t in = (uint32_t)(uintptr_t)row_at & 15u;
+                const int bytes = t + row >= 0 && t + row < len && inside ? min(max((int)in + here - 16 * piece, 0), 16) : 0;
+                const char *const q = row_at - in + 16 * piece;
+                scan_copy(to + row * kRow + 16 * piece, bytes ? q : reinterpret_cast<const char *>((uintptr_t)v.p & ~(uintptr_t)15), bytes);
+            };
+            const char *row_at = row0 + lane / kMost * pitch;
 #pragma unroll
-        for (int i = 0; i < kRun; ++i, src += v.step) {
-            const bool there = t + i >= 0 && t + i < len && at.n > 0 &&
-                               RSDGC_IN_BOUNDS(seq < p.n_seq && len <= p.n_steps && at.c + at.n <= p.width);
-            if (p.vec) {  // (the address is used for nothing where nothing is there, but has to be one)
-                scan_copy(dst + i * kRow, there ? (const void *)src : v.p, there ? at.n * (int)sizeof(T) : 0, 2 * (int)sizeof(T));
-            } else if constexpr (sizeof(T) == 4) {
-                scan_copy(dst + i * kRow, there ? (const void *)src : v.p, there ? 4 : 0, 4);
-                scan_copy(dst + i * kRow + 4, there && at.n > 1 ? (const void *)(src + 1) : v.p, there && at.n > 1 ? 4 : 0, 4);
-            } else {
-                Raw r = Channels<T>::none();
-                if (there) r = Channels<T>::load(src, false, at.n);
-                asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst + i * kRow), "r"(r) : "memory");
-            }
+            for (int j = 0; j < kRun / kRows; ++j, row_at += kRows * pitch) copy(row_at, j * kRows + lane / kMost, lane % kMost);
+            if (lane < kRun) copy(row0 + lane * pitch, lane, kMost);
         }
     }
     __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); stage ^= 1; }
@@ -261,34 +302,42 @@ struct ScanRing {
     }
     __device__ __forceinline__ Raw read(int op, int i) const
     {
-        const uint32_t from = base + stage * kStage + op * kTileBytes + i * kRow + lane * 2 * (int)sizeof(T);
+        uint32_t from = base + stage * kStage + op * kTileBytes + i * kRow + lane * 2 * (int)sizeof(T);
+        if constexpr (SHIFT) from += (first[op] + i * down[op]) & 15u;
+        Raw r;
         if constexpr (sizeof(T) == 4) {
-            Raw r;
-            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(r.x), "=f"(r.y) : "r"(from) : "memory");
-            return r;
+            if constexpr (SHIFT) {
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(r.x) : "r"(from) : "memory");
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(r.y) : "r"(from + 4) : "memory");
+            } else {
+                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(r.x), "=f"(r.y) : "r"(from) : "memory");
+            }
+        } else if constexpr (SHIFT) {
+            asm volatile("{\n\t.reg .b16 a, b;\n\tld.shared.b16 a, [%1];\n\tld.shared.b16 b, [%1 + 2];\n\tmov.b32 %0, {a, b};\n\t}"
+                         : "=r"(r)
+                         : "r"(from)
+                         : "memory");
         } else {
-            Raw r;
             asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(from) : "memory");
-            return r;
         }
+        return r;
     }
 };
-// ... and back, negated
+// A run's rows of a result from step t on
 template <typename T>
-__device__ __forceinline__ void scan_write(const float2 (&m)[kRun], const ScanParams &p, const ScanView &v, int seq,
+__device__ __forceinline__ void scan_write(const typename Channels<T>::Raw (&v)[kRun], const ScanParams &p, const ScanView &to, int seq,
                                            const ScanPlace &at, int t, int len)
 {
-    T *dst = (T *)const_cast<void *>(v.p) + seq * v.seq + t * v.step + at.c;
+    T *dst = (T *)const_cast<void *>(to.p) + seq * to.seq + t * to.step + at.c;
     if (at.pair && t + kRun <= len && RSDGC_IN_BOUNDS(t >= 0 && seq < p.n_seq && len <= p.n_steps && at.c + 2 <= p.width)) {
-        const uint32_t step = (uint32_t)v.step;
+        const uint32_t step = (uint32_t)to.step;  // pairs: below 2^32
 #pragma unroll
-        for (int i = 0; i < kRun; ++i)
-            Channels<T>::store(dst + (unsigned long long)step * i, true, 2, make_float2(-m[i].x, -m[i].y));
+        for (int i = 0; i < kRun; ++i) Channels<T>::store(dst + (unsigned long long)step * i, true, 2, v[i]);
     } else {
 #pragma unroll
-        for (int i = 0; i < kRun; ++i, dst += v.step)
+        for (int i = 0; i < kRun; ++i, dst += to.step)
             if (t + i < len && RSDGC_IN_BOUNDS(t >= 0 && seq < p.n_seq && len <= p.n_steps))
-                Channels<T>::store(dst, at.pair, at.n, make_float2(-m[i].x, -m[i].y));
+                Channels<T>::store(dst, at.pair, at.n, v[i]);
     }
 }
 
@@ -299,8 +348,8 @@ __device__ __forceinline__ bool scan_restarts(const ScanParams &p, int seq, int 
 }
 
 // -b of a run's steps; steps that do not exist leave the state as it is
-template <typename T, int OPS>
-__device__ __forceinline__ void scan_gates(float2 (&nb)[kRun], const ScanRing<T, OPS> &ring, int op, float2 bias, int t, int len)
+template <typename T, int OPS, bool SHIFT>
+__device__ __forceinline__ void scan_gates(float2 (&nb)[kRun], const ScanRing<T, OPS, SHIFT> &ring, int op, float2 bias, int t, int len)
 {
     const float2 scale = make_float2(kScanLog2e, kScanLog2e);
 #pragma unroll
@@ -314,19 +363,46 @@ __device__ __forceinline__ void scan_gates(float2 (&nb)[kRun], const ScanRing<T,
             if (t + i < 0 || t + i >= len) nb[i] = make_float2(0.0f, 0.0f);
     }
 }
-// The run from the negated state m, which each step's y = -x replaces
-__device__ __forceinline__ void scan_steps(float2 (&x)[kRun], const float2 (&nb)[kRun], float2 &m, uint32_t restart)
+// The run from the negated state m; y = -m, in the operand's type, replaces each step's x
+template <typename T>
+__device__ __forceinline__ void scan_steps(typename Channels<T>::Raw (&x)[kRun], const float2 (&nb)[kRun], float2 &m, uint32_t restart)
 {
     if (!restart) {
 #pragma unroll
-        for (int i = 0; i < kRun; ++i) x[i] = m = fma2(nb[i], add2(x[i], m), m);
+        for (int i = 0; i < kRun; ++i) {
+            m = fma2(nb[i], add2(Channels<T>::widen(x[i]), m), m);
+            x[i] = Channels<T>::narrow(make_float2(-m.x, -m.y));
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
             if (restart >> i & 1) m = make_float2(0.0f, 0.0f);
-            x[i] = m = fma2(nb[i], add2(x[i], m), m);
+            m = fma2(nb[i], add2(Channels<T>::widen(x[i]), m), m);
+            x[i] = Channels<T>::narrow(make_float2(-m.x, -m.y));
         }
     }
+}
+// What the run does to a state
+template <typename T>
+__device__ __forceinline__ float4 scan_whole(const typename Channels<T>::Raw (&x)[kRun], const float2 (&nb)[kRun], uint32_t restart)
+{
+    float2 l = make_float2(0.0f, 0.0f), nq = l, r = make_float2(1.0f, 1.0f);  // r = 1 - q, of its own digits
+    if (!restart) {
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+            l = fma2(nb[i], add2(Channels<T>::widen(x[i]), l), l);
+            nq = fma2(nb[i], r, nq);
+            r = fma2(nb[i], r, r);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+            if (restart >> i & 1) l = make_float2(0.0f, 0.0f);
+            l = fma2(nb[i], add2(Channels<T>::widen(x[i]), l), l);
+        }
+        nq = make_float2(-kScanCut, -kScanCut);
+    }
+    return make_float4(l.x, l.y, -nq.x, -nq.y);
 }
 __device__ __forceinline__ void scan_save(const ScanParams &p, int seq, const ScanPlace &at, int t, float2 m)
 {
@@ -337,10 +413,12 @@ __device__ __forceinline__ void scan_save(const ScanParams &p, int seq, const Sc
 // ---- forward --------------------------------------------------------------------------------------
 // The chain: W warps of a CTA take a sequence's runs in turn, all but the recurrence side by side; the state is handed from
 // warp to warp.  W = 1: kScanLoneWarps warps with a sequence's group each.
-template <typename T, int W>
-__global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W) k_scan_forward(const ScanParams p)
+template <typename T, int W, bool SHIFT>
+__global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W, scan_forward_warps<T>(W) / (W == 1 ? kScanLoneWarps : W)) k_scan_forward(const ScanParams p)
 {
+    constexpr bool ahead = W >= kScanAhead;
     __shared__ float2 place[W][32];
+    __shared__ float4 whole[ahead ? W : 1][32];  // kept here so that it is there before the state is waited for
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, run = W == 1 ? 0 : warp;
     const int unit = W == 1 ? blockIdx.x * kScanLoneWarps + warp : (int)blockIdx.x;
     grid_dependency_wait();
@@ -358,7 +436,9 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W) k_scan_
     if (len == 0 && run == 0 && p.last) scan_store2(p.last + (long long)seq * p.width + at.c, at.n, make_float2(-m.x, -m.y));
     int t = run * kRun;
     extern __shared__ __align__(16) unsigned char smem[];
-    ScanRing<T, 2> ring(smem, warp, lane);
+    ScanRing<T, 2, SHIFT> ring(smem, warp, lane);
+    ring.start(0, p.x, seq, at);
+    ring.start(1, p.gate, seq, at);
     auto fetch = [&](int at_step) {
         if (at_step < len) {
             ring.fetch(0, p, p.x, seq, at, at_step, len);
@@ -370,22 +450,26 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W) k_scan_
     fetch(t + W * kRun);
     bool starts = scan_restarts(p, seq, t, len, lane);
     for (; t < len; t += W * kRun) {
-        float2 x[kRun], nb[kRun];
+        typename Channels<T>::Raw x[kRun];
+        float2 nb[kRun];
         const uint32_t restart = __ballot_sync(0xFFFFFFFFu, starts);
         ring.wait();
         scan_gates(nb, ring, 1, bias, t, len);
 #pragma unroll
-        for (int i = 0; i < kRun; ++i) x[i] = Channels<T>::widen(ring.read(0, i));
+        for (int i = 0; i < kRun; ++i) x[i] = ring.read(0, i);
         __syncwarp();
         fetch(t + 2 * W * kRun);
         starts = scan_restarts(p, seq, t + W * kRun, len, lane);
-        if (W > 1 && t > 0) m = scan_take_over(&place[0][0], warp, lane);
+        if constexpr (ahead) whole[warp][lane] = scan_whole<T>(x, nb, restart);
+        if (W > 1 && t > 0) m = scan_take_over<W>(&place[0][0], warp, lane);
+        if constexpr (ahead)
+            if (t + kRun < len) scan_hand_on<W>(&place[0][0], warp + 1 < W ? warp + 1 : 0, lane, scan_apply(whole[warp][lane], m));
         scan_save(p, seq, at, t, m);
-        scan_steps(x, nb, m, restart);
+        scan_steps<T>(x, nb, m, restart);
         if (t + kRun >= len) {
             if (p.last) scan_store2(p.last + (long long)seq * p.width + at.c, at.n, make_float2(-m.x, -m.y));
-        } else if (W > 1) {
-            scan_hand_on(&place[0][0], warp + 1 < W ? warp + 1 : 0, lane, m);
+        } else if (W > 1 && !ahead) {
+            scan_hand_on<W>(&place[0][0], warp + 1 < W ? warp + 1 : 0, lane, m);
         }
         scan_write<T>(x, p, p.y, seq, at, t, len);
     }
@@ -393,7 +477,7 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W) k_scan_
 
 // Few channels and many steps: W warps of each of p.cluster CTAs take W runs each side by side, from no state; what they do to a
 // state is told to all of them, and each starts again from the state that it then knows.
-template <typename T, int W>
+template <typename T, int W, bool SHIFT>
 __global__ void __launch_bounds__(32 * W) k_scan_forward_split(const ScanParams p)
 {
     __shared__ float4 runs[2][W][32];              // by round: what each warp's run does
@@ -415,7 +499,9 @@ __global__ void __launch_bounds__(32 * W) k_scan_forward_split(const ScanParams 
     }
     int t = (rank * W + warp) * kRun, parity = 0;
     extern __shared__ __align__(16) unsigned char smem[];
-    ScanRing<T, 2> ring(smem, warp, lane);
+    ScanRing<T, 2, SHIFT> ring(smem, warp, lane);
+    ring.start(0, p.x, seq, at);
+    ring.start(1, p.gate, seq, at);
     auto fetch = [&](int at_step) {
         if (at_step < len) {
             ring.fetch(0, p, p.x, seq, at, at_step, len);
@@ -427,32 +513,17 @@ __global__ void __launch_bounds__(32 * W) k_scan_forward_split(const ScanParams 
     fetch(t + stride);
     bool starts = scan_restarts(p, seq, t, len, lane);
     for (int t0 = 0; t0 < len; t0 += stride, t += stride, parity ^= 1) {
-        float2 x[kRun], nb[kRun];
+        typename Channels<T>::Raw x[kRun];
+        float2 nb[kRun];
         const uint32_t restart = __ballot_sync(0xFFFFFFFFu, starts);
         ring.wait();
         scan_gates(nb, ring, 1, bias, t, len);
 #pragma unroll
-        for (int i = 0; i < kRun; ++i) x[i] = t < len ? Channels<T>::widen(ring.read(0, i)) : make_float2(0.0f, 0.0f);
+        for (int i = 0; i < kRun; ++i) x[i] = t < len ? ring.read(0, i) : Channels<T>::none();
         __syncwarp();
         fetch(t + 2 * stride);
         starts = scan_restarts(p, seq, t + stride, len, lane);
-        float2 l = make_float2(0.0f, 0.0f), nq = l, r = make_float2(1.0f, 1.0f);  // r = 1 - q, of its own digits
-        if (!restart) {
-#pragma unroll
-            for (int i = 0; i < kRun; ++i) {
-                l = fma2(nb[i], add2(x[i], l), l);
-                nq = fma2(nb[i], r, nq);
-                r = fma2(nb[i], r, r);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kRun; ++i) {
-                if (restart >> i & 1) l = make_float2(0.0f, 0.0f);
-                l = fma2(nb[i], add2(x[i], l), l);
-            }
-            nq = make_float2(-kScanCut, -kScanCut);
-        }
-        runs[parity][warp][lane] = make_float4(l.x, l.y, -nq.x, -nq.y);
+        runs[parity][warp][lane] = scan_whole<T>(x, nb, restart);
         __syncthreads();
         float2 in = m;
         if (cluster > 1) {
@@ -480,7 +551,7 @@ __global__ void __launch_bounds__(32 * W) k_scan_forward_split(const ScanParams 
         }
         if (t >= len) continue;
         scan_save(p, seq, at, t, in);
-        scan_steps(x, nb, in, restart);
+        scan_steps<T>(x, nb, in, restart);
         scan_write<T>(x, p, p.y, seq, at, t, len);
     }
     if (p.last && rank == 0 && warp == 0)
@@ -489,11 +560,18 @@ __global__ void __launch_bounds__(32 * W) k_scan_forward_split(const ScanParams 
 
 // ---- backward -------------------------------------------------------------------------------------
 // A run's operands on their way through the ring, the state before it and its restarts in registers
-template <typename T>
+template <typename T, bool SHIFT>
 struct ScanBack {
-    ScanRing<T, 3> ring;
+    typedef typename Channels<T>::Raw Raw;
+    ScanRing<T, 3, SHIFT> ring;
     float2 from;
     bool starts;
+    __device__ __forceinline__ void start(const ScanParams &p, int seq, const ScanPlace &at)
+    {
+        ring.start(0, p.x, seq, at);
+        ring.start(1, p.gate, seq, at);
+        ring.start(2, p.y, seq, at);
+    }
     __device__ __forceinline__ void rows(const ScanParams &p, int seq, const ScanPlace &at, int t, int len)
     {
         if (t >= 0 && t < len) {
@@ -511,7 +589,7 @@ struct ScanBack {
             from = scan_load2(p.states + ((long long)seq * p.runs + t / kRun) * p.width + at.c, at.n);
     }
     // the run's -b, x and dy; the place is filled again with the run after the next
-    __device__ __forceinline__ void take(float2 (&nb)[kRun], float2 (&x)[kRun], float2 (&dy)[kRun], float2 bias, const ScanParams &p,
+    __device__ __forceinline__ void take(float2 (&nb)[kRun], Raw (&x)[kRun], Raw (&dy)[kRun], float2 bias, const ScanParams &p,
                                          int seq, const ScanPlace &at, int t, int len, int ahead)
     {
         const bool there = t >= 0 && t < len;
@@ -519,51 +597,63 @@ struct ScanBack {
         scan_gates(nb, ring, 1, bias, t, len);
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-            x[i] = there ? Channels<T>::widen(ring.read(0, i)) : make_float2(0.0f, 0.0f);
-            dy[i] = there ? Channels<T>::widen(ring.read(2, i)) : make_float2(0.0f, 0.0f);
+            x[i] = there ? ring.read(0, i) : Channels<T>::none();
+            dy[i] = there ? ring.read(2, i) : Channels<T>::none();
         }
         __syncwarp();
         rows(p, seq, at, t - 2 * ahead, len);
     }
 };
-// x becomes x_t - h_{t-1}, from the state before the run
-__device__ __forceinline__ void scan_again(float2 (&x)[kRun], const float2 (&nb)[kRun], float2 from, uint32_t restart)
+// What the run does to the gradient that comes into it from behind
+template <typename T>
+__device__ __forceinline__ float4 scan_back_whole(const typename Channels<T>::Raw (&dy)[kRun], const float2 (&nb)[kRun], uint32_t restart)
+{
+    float2 r = make_float2(0.0f, 0.0f), q = make_float2(1.0f, 1.0f);
+#pragma unroll
+    for (int i = kRun - 1; i >= 0; --i) {
+        const float2 d = add2(Channels<T>::widen(dy[i]), r);
+        r = fma2(nb[i], d, d);
+        q = fma2(nb[i], q, q);
+        if (restart >> i & 1) r = make_float2(0.0f, 0.0f);
+    }
+    q = restart ? make_float2(0.0f, 0.0f) : make_float2(fmaxf(q.x, kScanLeast), fmaxf(q.y, kScanLeast));
+    return make_float4(r.x, r.y, q.x, q.y);
+}
+// u_t = x_t - h_{t-1}, from the state before the run
+template <typename T>
+__device__ __forceinline__ void scan_again(float2 (&u)[kRun], const typename Channels<T>::Raw (&x)[kRun], const float2 (&nb)[kRun],
+                                           float2 from, uint32_t restart)
 {
     float2 m = make_float2(-from.x, -from.y);
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
         if (restart >> i & 1) m = make_float2(0.0f, 0.0f);
-        x[i] = add2(x[i], m);
-        m = fma2(nb[i], x[i], m);
+        u[i] = add2(Channels<T>::widen(x[i]), m);
+        m = fma2(nb[i], u[i], m);
     }
 }
-// dy becomes delta; e: the gradient from behind, and at the end the one that goes on
-__device__ __forceinline__ void scan_deltas(float2 (&dy)[kRun], const float2 (&nb)[kRun], float2 &e, uint32_t restart)
+// From the last step to the first: delta, dx, dgate (into dy's and x's places) and dgate's sum.  e: the gradient from behind, and at the
+// end the one that goes on.
+template <typename T>
+__device__ __forceinline__ void scan_deltas(typename Channels<T>::Raw (&dy)[kRun], typename Channels<T>::Raw (&x)[kRun],
+                                            const float2 (&u)[kRun], const float2 (&nb)[kRun], float2 &e, float2 &add, uint32_t restart)
 {
+    add = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int i = kRun - 1; i >= 0; --i) {
-        dy[i] = add2(dy[i], e);
-        e = fma2(nb[i], dy[i], dy[i]);
+        const float2 d = add2(Channels<T>::widen(dy[i]), e);
+        e = fma2(nb[i], d, d);                             // a delta
+        const float2 z = mul2(mul2(e, nb[i]), u[i]);       // a delta (-b) (x - h)
+        const float2 ndx = mul2(nb[i], d);
+        dy[i] = Channels<T>::narrow(make_float2(-ndx.x, -ndx.y));
+        x[i] = Channels<T>::narrow(z);
+        add = add2(add, z);
         if (restart >> i & 1) e = make_float2(0.0f, 0.0f);
     }
 }
-// dx and dgate of a run; adds up dgate
-template <typename T>
-__device__ __forceinline__ void scan_gradients(float2 (&x)[kRun], float2 (&dy)[kRun], const float2 (&nb)[kRun], float2 &sum, float2 &rest,
-                                               const ScanParams &p, int seq, const ScanPlace &at, int t, int len)
+// Kahan's sum: a channel may have millions of steps
+__device__ __forceinline__ void scan_sum(float2 &sum, float2 &rest, float2 add)
 {
-    float2 add = make_float2(0.0f, 0.0f);
-#pragma unroll
-    for (int i = 0; i < kRun; ++i) {
-        const float2 d = dy[i];
-        dy[i] = mul2(nb[i], d);                              // -dx
-        x[i] = mul2(mul2(add2(d, dy[i]), nb[i]), x[i]);      // a d (-b) (x - h): dgate
-        add = add2(add, x[i]);
-        x[i] = make_float2(-x[i].x, -x[i].y);
-    }
-    if (p.dx.p) scan_write<T>(dy, p, p.dx, seq, at, t, len);
-    if (p.dgate.p) scan_write<T>(x, p, p.dgate, seq, at, t, len);
-    // Kahan's sum: a channel may have millions of steps
     const float2 y = make_float2(add.x - rest.x, add.y - rest.y), s = make_float2(sum.x + y.x, sum.y + y.y);
     rest = make_float2((s.x - sum.x) - y.x, (s.y - sum.y) - y.y);
     sum = s;
@@ -584,10 +674,12 @@ __device__ __forceinline__ void scan_sums(float2 *place, float2 sum, const ScanP
 }
 
 // The chain, the last run first.  A run's states are computed again from the one saved before it.
-template <typename T, int W>
-__global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W) k_scan_backward(const ScanParams p)
+template <typename T, int W, bool SHIFT>
+__global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W, scan_backward_warps<T>(W) / (W == 1 ? kScanLoneWarps : W)) k_scan_backward(const ScanParams p)
 {
+    constexpr bool ahead = W >= kScanAhead;
     __shared__ float2 place[W][32];
+    __shared__ float4 whole[ahead ? W : 1][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, run = W == 1 ? 0 : warp;
     const int unit = W == 1 ? blockIdx.x * kScanLoneWarps + warp : (int)blockIdx.x;
     grid_dependency_wait();
@@ -598,31 +690,38 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W) k_scan_
     const float2 bias = at.bias(p);
     float2 sum = make_float2(0.0f, 0.0f), rest = sum;  // of dgate, with what the sum's rounding left out
     extern __shared__ __align__(16) unsigned char smem[];
-    ScanBack<T> next = {ScanRing<T, 3>(smem, warp, lane), sum, false};
+    ScanBack<T, SHIFT> next = {ScanRing<T, 3, SHIFT>(smem, warp, lane), sum, false};
     for (int seq = part; seq < p.n_seq; seq += p.seq_parts) {
         const int len = scan_length(p, seq), runs = (len + kRun - 1) / kRun;
         float2 e = make_float2(0.0f, 0.0f);
         if (p.first && run == 0) e = scan_load2(p.first + (long long)seq * p.width + at.c, at.n);
         if (len == 0 && run == 0 && p.last) scan_store2(p.last + (long long)seq * p.width + at.c, at.n, e);
         int t = (runs - 1 - run) * kRun;
+        next.start(p, seq, at);
         next.rows(p, seq, at, t, len);
         next.rows(p, seq, at, t - W * kRun, len);
         next.state(p, seq, at, t, len, lane);
         for (; t >= 0; t -= W * kRun) {
-            float2 x[kRun], nb[kRun], dy[kRun];
+            typename Channels<T>::Raw x[kRun], dy[kRun];
+            float2 nb[kRun], u[kRun], add;
             const uint32_t restart = __ballot_sync(0xFFFFFFFFu, next.starts);
             const float2 from = next.from;
             next.take(nb, x, dy, bias, p, seq, at, t, len, W * kRun);
             next.state(p, seq, at, t - W * kRun, len, lane);
-            scan_again(x, nb, from, restart);
-            if (W > 1 && t + kRun < len) e = scan_take_over(&place[0][0], warp, lane);
-            scan_deltas(dy, nb, e, restart);
+            scan_again<T>(u, x, nb, from, restart);
+            if constexpr (ahead) whole[warp][lane] = scan_back_whole<T>(dy, nb, restart);
+            if (W > 1 && t + kRun < len) e = scan_take_over<W>(&place[0][0], warp, lane);
+            if constexpr (ahead)
+                if (t > 0) scan_hand_on<W>(&place[0][0], warp + 1 < W ? warp + 1 : 0, lane, scan_back(whole[warp][lane], e));
+            scan_deltas<T>(dy, x, u, nb, e, add, restart);
             if (t == 0) {
                 if (p.last) scan_store2(p.last + (long long)seq * p.width + at.c, at.n, e);
-            } else if (W > 1) {
-                scan_hand_on(&place[0][0], warp + 1 < W ? warp + 1 : 0, lane, e);
+            } else if (W > 1 && !ahead) {
+                scan_hand_on<W>(&place[0][0], warp + 1 < W ? warp + 1 : 0, lane, e);
             }
-            scan_gradients<T>(x, dy, nb, sum, rest, p, seq, at, t, len);
+            if (p.dx.p) scan_write<T>(dy, p, p.dx, seq, at, t, len);
+            if (p.dgate.p) scan_write<T>(x, p, p.dgate, seq, at, t, len);
+            scan_sum(sum, rest, add);
         }
         if (W > 1) __syncthreads();  // the next sequence's first run waits for no one: the places are to be free
     }
@@ -631,7 +730,7 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W) k_scan_
 
 // Few channels and many steps, as forward: what a run does to the gradient that comes into it from behind is e -> R + P e, P the
 // product of its a.
-template <typename T, int W>
+template <typename T, int W, bool SHIFT>
 __global__ void __launch_bounds__(32 * W) k_scan_backward_split(const ScanParams p)
 {
     __shared__ float4 runs[2][W][32];              // (R, P) of the two channels
@@ -648,32 +747,25 @@ __global__ void __launch_bounds__(32 * W) k_scan_backward_split(const ScanParams
     constexpr int tile = W * kRun;
     float2 sum = make_float2(0.0f, 0.0f), rest = sum;
     extern __shared__ __align__(16) unsigned char smem[];
-    ScanBack<T> next = {ScanRing<T, 3>(smem, warp, lane), sum, false};
+    ScanBack<T, SHIFT> next = {ScanRing<T, 3, SHIFT>(smem, warp, lane), sum, false};
     int parity = 0;
     for (int seq = part; seq < p.n_seq; seq += p.seq_parts) {
         const int len = scan_length(p, seq), tiles = (len + tile - 1) / tile;
         float2 e = make_float2(0.0f, 0.0f);  // the gradient that comes into the round from behind
         if (p.first) e = scan_load2(p.first + (long long)seq * p.width + at.c, at.n);
         int t = (tiles - 1 - rank) * tile + warp * kRun;
+        next.start(p, seq, at);
         next.rows(p, seq, at, t, len);
         next.rows(p, seq, at, t - tile * cluster, len);
         next.state(p, seq, at, t, len, lane);
         for (int left = tiles; left > 0; left -= cluster, t -= tile * cluster, parity ^= 1) {
-            float2 x[kRun], nb[kRun], dy[kRun];
+            typename Channels<T>::Raw x[kRun], dy[kRun];
+            float2 nb[kRun], u[kRun], add;
             const uint32_t restart = __ballot_sync(0xFFFFFFFFu, next.starts);
             const float2 from = next.from;
             next.take(nb, x, dy, bias, p, seq, at, t, len, tile * cluster);
             next.state(p, seq, at, t - tile * cluster, len, lane);
-            float2 r = make_float2(0.0f, 0.0f), q = make_float2(1.0f, 1.0f);
-#pragma unroll
-            for (int i = kRun - 1; i >= 0; --i) {
-                const float2 d = add2(dy[i], r);
-                r = fma2(nb[i], d, d);
-                q = fma2(nb[i], q, q);
-                if (restart >> i & 1) r = make_float2(0.0f, 0.0f);
-            }
-            q = restart ? make_float2(0.0f, 0.0f) : make_float2(fmaxf(q.x, kScanLeast), fmaxf(q.y, kScanLeast));
-            runs[parity][warp][lane] = make_float4(r.x, r.y, q.x, q.y);
+            runs[parity][warp][lane] = scan_back_whole<T>(dy, nb, restart);
             __syncthreads();
             float2 in = e;
             if (cluster > 1) {
@@ -700,9 +792,11 @@ __global__ void __launch_bounds__(32 * W) k_scan_backward_split(const ScanParams
                 }
             }
             if (t < 0 || t >= len) continue;
-            scan_again(x, nb, from, restart);
-            scan_deltas(dy, nb, in, restart);
-            scan_gradients<T>(x, dy, nb, sum, rest, p, seq, at, t, len);
+            scan_again<T>(u, x, nb, from, restart);
+            scan_deltas<T>(dy, x, u, nb, in, add, restart);
+            if (p.dx.p) scan_write<T>(dy, p, p.dx, seq, at, t, len);
+            if (p.dgate.p) scan_write<T>(x, p, p.dgate, seq, at, t, len);
+            scan_sum(sum, rest, add);
         }
         if (p.last && rank == 0 && warp == 0) scan_store2(p.last + (long long)seq * p.width + at.c, at.n, e);
     }
@@ -735,11 +829,6 @@ RSDGC_DEFINE_DEBUG_BOUNDS(gated_scan_debug_bounds)
 namespace {
 
 constexpr int kScanSms = 148;
-#ifndef SCAN_WARPS_F
-#define SCAN_WARPS_F 16
-#define SCAN_WARPS_B 12
-#define SCAN_SPLIT 6
-#endif
 constexpr int64_t kScanParts = 16 * kScanSms;  // sequence groups from which on the backward pass gives a warp several
 
 int scan_check(int64_t n, int64_t t, int64_t d)
@@ -753,24 +842,20 @@ int scan_check(int64_t n, int64_t t, int64_t d)
 inline int scan_groups(int64_t d) { return (int)((d + kScanGroup - 1) / kScanGroup); }
 inline int scan_runs(int64_t t) { return (int)((t + kRun - 1) / kRun); }
 
-// How a call's sequences' groups (units) are dealt: warps of a CTA that form a chain, or CTAs of a cluster that split the steps.
-struct ScanShape {
-    int warps, cluster;
-    bool split;
-};
-ScanShape scan_shape(int64_t units, int64_t steps, int per_sm, int elem)
+// The longest chain of warps per CTA, of at most `most`, with which all units are on the device at a time
+template <typename F>
+int scan_warps(int64_t units, int64_t steps, int most, F per_sm)
 {
-    const int64_t runs = scan_runs(steps);
-    const int wide = elem == 4 ? 8 : 16;
-    if (units * 12 < (int64_t)kScanSms * SCAN_SPLIT && runs > 2 * wide) {
-        int k = 1;
-        while (k < kScanCluster && units * 2 * k <= kScanSms && runs > 2 * k * wide) k *= 2;
-        return {wide, k, true};
-    }
     int warps = 1;
     for (int w : {2, 4, 8, 12})
-        if (units * w <= (int64_t)kScanSms * per_sm && runs >= w && (elem < 4 || w <= 8)) warps = w;
-    return {warps, 1, false};
+        if (w <= most && units * w <= (int64_t)kScanSms * per_sm(w) && scan_runs(steps) >= w) warps = w;
+    return warps;
+}
+// Most CTAs that may share a unit's steps
+int scan_most_cluster(int64_t units)
+{
+    const int64_t k = units > 0 ? kScanSms / units : 1;
+    return k > kScanCluster ? kScanCluster : k < 1 ? 1 : (int)k;
 }
 
 int64_t scan_seq_parts(int64_t n, int64_t d)
@@ -778,11 +863,6 @@ int64_t scan_seq_parts(int64_t n, int64_t d)
     const int64_t most = kScanParts / scan_groups(d) > 1 ? kScanParts / scan_groups(d) : 1;
     return n < most ? n : most;
 }
-ScanShape scan_backward_shape(int64_t n, int64_t t, int64_t d, int elem)
-{
-    return scan_shape(scan_seq_parts(n, d) * scan_groups(d), t, SCAN_WARPS_B, elem);
-}
-
 bool scan_pairs(const ScanView &v, int elem)
 {
     return pointer_aligned(v.p, 2 * elem) && v.seq % 2 == 0 && v.step % 2 == 0 && v.step >> 32 == 0;
@@ -801,18 +881,21 @@ cudaError_t scan_type(int dtype, F f)
 
 // Launches a kernel with `bytes` of ring per warp; what the device has to be told before is told once per device.
 template <typename K>
+cudaError_t scan_ready(K kernel, std::atomic<uint64_t> &ready, int bytes, int *dev)
+{
+    cudaError_t e = cudaGetDevice(dev);
+    if (e != cudaSuccess || bytes <= (40 << 10) || (ready.load(std::memory_order_acquire) >> (*dev & 63) & 1)) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) ready.fetch_or(1ull << (*dev & 63), std::memory_order_release);
+    return e;
+}
+template <typename K>
 cudaError_t scan_launch(K kernel, std::atomic<uint64_t> &ready, unsigned grid, int warps, int bytes, int cluster, cudaStream_t s,
                         const ScanParams &p)
 {
     int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (warps * bytes > (40 << 10) && !(ready.load(std::memory_order_acquire) >> (dev & 63) & 1)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, warps * bytes);
-        if (e != cudaSuccess) return e;
-        ready.fetch_or(1ull << (dev & 63), std::memory_order_release);
-    }
-    return launch_chained(kernel, grid, 32 * warps, (size_t)warps * bytes, s, cluster, p);
+    const cudaError_t e = scan_ready(kernel, ready, warps * bytes, &dev);
+    return e != cudaSuccess ? e : launch_chained(kernel, grid, 32 * warps, (size_t)warps * bytes, s, cluster, p);
 }
 #define SCAN_LAUNCH(kernel, grid, warps, cluster)                                                          \
     [&] {                                                                                                  \
@@ -820,39 +903,86 @@ cudaError_t scan_launch(K kernel, std::atomic<uint64_t> &ready, unsigned grid, i
         return scan_launch(kernel, ready, (unsigned)(grid), warps, bytes, cluster, s, p);                  \
     }()
 
-template <typename T>
+// The kernel that splits the steps, in clusters of p.cluster CTAs; *done = false if fewer than `least` would be on the device at
+// a time with all units: a second wave costs more than the split gains (16 units of 65536 steps: 287 us with 8 CTAs each, of which 15
+// clusters fit, 192 us with 7).
+template <typename K>
+cudaError_t scan_split(K kernel, std::atomic<uint64_t> &ready, std::atomic<int> (&fit)[64][kScanCluster + 1], long long units, int warps,
+                       int bytes, int least, cudaStream_t s, ScanParams &p, bool *done)
+{
+    *done = false;
+    int k = scan_most_cluster(units);
+    while (k > 1 && p.runs < 2 * k * warps) --k;
+    if (k < least) return cudaSuccess;
+    int dev = 0;
+    cudaError_t e = scan_ready(kernel, ready, warps * bytes, &dev);
+    for (; e == cudaSuccess && k >= least; --k) {
+        std::atomic<int> &known = fit[dev & 63][k];
+        int n = known.load(std::memory_order_relaxed);
+        if (n == 0) {
+            cudaLaunchConfig_t cfg{};
+            cfg.gridDim = (unsigned)k * kScanSms;
+            cfg.blockDim = 32 * warps;
+            cfg.dynamicSmemBytes = (size_t)warps * bytes;
+            cudaLaunchAttribute at{};
+            at.id = cudaLaunchAttributeClusterDimension;
+            at.val.clusterDim.x = k;
+            at.val.clusterDim.y = at.val.clusterDim.z = 1;
+            cfg.attrs = &at;
+            cfg.numAttrs = 1;
+            e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+            if (e != cudaSuccess) return e;
+            known.store(n < 1 ? -1 : n, std::memory_order_relaxed);
+        }
+        if (n < units) continue;
+        p.cluster = k;
+        *done = true;
+        return launch_chained(kernel, (unsigned)(units * k), 32 * warps, (size_t)warps * bytes, s, k, p);
+    }
+    return e;
+}
+#define SCAN_SPLIT(kernel, units, warps, least, done)                                                      \
+    [&] {                                                                                                  \
+        static std::atomic<uint64_t> ready{0};                                                             \
+        static std::atomic<int> fit[64][kScanCluster + 1] = {};                                            \
+        return scan_split(kernel, ready, fit, units, warps, bytes, least, s, p, done);                     \
+    }()
+
+template <typename T, bool SHIFT>
 cudaError_t scan_forward(ScanParams &p, cudaStream_t s)
 {
     const long long units = (long long)p.n_seq * p.groups;
-    const ScanShape shape = scan_shape(units, p.n_steps, SCAN_WARPS_F, sizeof(T));
-    constexpr int bytes = ScanRing<T, 2>::kBytes, wide = sizeof(T) == 4 ? 8 : 16;
-    p.cluster = shape.cluster;
-    if (shape.split) return SCAN_LAUNCH((k_scan_forward_split<T, wide>), units * shape.cluster, wide, shape.cluster);
-    switch (shape.warps) {
-    case 1: return SCAN_LAUNCH((k_scan_forward<T, 1>), (units + kScanLoneWarps - 1) / kScanLoneWarps, kScanLoneWarps, 1);
-    case 2: return SCAN_LAUNCH((k_scan_forward<T, 2>), units, 2, 1);
-    case 4: return SCAN_LAUNCH((k_scan_forward<T, 4>), units, 4, 1);
-    case 8: return SCAN_LAUNCH((k_scan_forward<T, 8>), units, 8, 1);
+    constexpr int bytes = ScanRing<T, 2, SHIFT>::kBytes, wide = sizeof(T) == 4 ? 8 : 16;
+    p.cluster = 1;
+    bool done = false;
+    // with 2 CTAs a unit the joins take as long as they save: 2 x 8192 x 2048 bfloat16 79 us, 72 us with a chain of 12 (backward 108 and 209 us)
+    const cudaError_t e = SCAN_SPLIT((k_scan_forward_split<T, wide, SHIFT>), units, wide, 3, &done);
+    if (done || e != cudaSuccess) return e;
+    switch (scan_warps(units, p.n_steps, 12, scan_forward_warps<T>)) {
+    case 1: return SCAN_LAUNCH((k_scan_forward<T, 1, SHIFT>), (units + kScanLoneWarps - 1) / kScanLoneWarps, kScanLoneWarps, 1);
+    case 2: return SCAN_LAUNCH((k_scan_forward<T, 2, SHIFT>), units, 2, 1);
+    case 4: return SCAN_LAUNCH((k_scan_forward<T, 4, SHIFT>), units, 4, 1);
+    case 8: return SCAN_LAUNCH((k_scan_forward<T, 8, SHIFT>), units, 8, 1);
     }
-    if constexpr (sizeof(T) < 4) return SCAN_LAUNCH((k_scan_forward<T, 12>), units, 12, 1);
-    return cudaErrorInvalidValue;
+    return SCAN_LAUNCH((k_scan_forward<T, 12, SHIFT>), units, 12, 1);
 }
 
-template <typename T>
+template <typename T, bool SHIFT>
 cudaError_t scan_backward(ScanParams &p, cudaStream_t s)
 {
     const long long units = (long long)p.seq_parts * p.groups;
-    const ScanShape shape = scan_backward_shape(p.n_seq, p.n_steps, p.width, sizeof(T));
-    constexpr int bytes = ScanRing<T, 3>::kBytes, wide = sizeof(T) == 4 ? 8 : 16;
-    p.cluster = shape.cluster;
-    if (shape.split) return SCAN_LAUNCH((k_scan_backward_split<T, wide>), units * shape.cluster, wide, shape.cluster);
-    switch (shape.warps) {
-    case 1: return SCAN_LAUNCH((k_scan_backward<T, 1>), (units + kScanLoneWarps - 1) / kScanLoneWarps, kScanLoneWarps, 1);
-    case 2: return SCAN_LAUNCH((k_scan_backward<T, 2>), units, 2, 1);
-    case 4: return SCAN_LAUNCH((k_scan_backward<T, 4>), units, 4, 1);
-    case 8: return SCAN_LAUNCH((k_scan_backward<T, 8>), units, 8, 1);
+    constexpr int bytes = ScanRing<T, 3, SHIFT>::kBytes, wide = sizeof(T) == 4 ? 8 : SHIFT ? 12 : 16;  // what shared memory holds
+    p.cluster = 1;
+    bool done = false;
+    const cudaError_t e = SCAN_SPLIT((k_scan_backward_split<T, wide, SHIFT>), units, wide, 2, &done);
+    if (done || e != cudaSuccess) return e;
+    switch (scan_warps(units, p.n_steps, sizeof(T) == 4 ? 8 : 12, scan_backward_warps<T>)) {
+    case 1: return SCAN_LAUNCH((k_scan_backward<T, 1, SHIFT>), (units + kScanLoneWarps - 1) / kScanLoneWarps, kScanLoneWarps, 1);
+    case 2: return SCAN_LAUNCH((k_scan_backward<T, 2, SHIFT>), units, 2, 1);
+    case 4: return SCAN_LAUNCH((k_scan_backward<T, 4, SHIFT>), units, 4, 1);
+    case 8: return SCAN_LAUNCH((k_scan_backward<T, 8, SHIFT>), units, 8, 1);
     }
-    if constexpr (sizeof(T) < 4) return SCAN_LAUNCH((k_scan_backward<T, 12>), units, 12, 1);
+    if constexpr (sizeof(T) < 4) return SCAN_LAUNCH((k_scan_backward<T, 12, SHIFT>), units, 12, 1);
     return cudaErrorInvalidValue;
 }
 
@@ -872,9 +1002,8 @@ extern "C" int64_t rsdgc_gated_scan_workspace_bytes(int64_t n_seq, int64_t n_ste
 {
     const int rc = scan_check(n_seq, n_steps, width);
     if (rc) return rc;
-    // the same for every type: the wider rows split sooner
-    const int a = scan_backward_shape(n_seq, n_steps, width, 2).cluster, b = scan_backward_shape(n_seq, n_steps, width, 4).cluster;
-    return 4 * width * scan_seq_parts(n_seq, width) * (a > b ? a : b);
+    const int64_t parts = scan_seq_parts(n_seq, width);
+    return 4 * width * parts * scan_most_cluster(parts * scan_groups(width));
 }
 
 extern "C" int rsdgc_gated_scan_forward(const void *x_dev, int64_t x_seq, int64_t x_step, const void *gate_dev, int64_t gate_seq,
@@ -914,10 +1043,11 @@ extern "C" int rsdgc_gated_scan_forward(const void *x_dev, int64_t x_seq, int64_
     p.width = (int)width;
     p.groups = scan_groups(width);
     p.runs = scan_runs(n_steps);
-    p.vec = scan_pairs(p.x, elem) && scan_pairs(p.gate, elem) && scan_pairs(p.y, elem);
+    p.vec = scan_pairs(p.y, elem);
     p.wide = scan_wide(p.x, elem) && scan_wide(p.gate, elem);
+    cudaStream_t s = (cudaStream_t)stream;
     cudaError_t e = operators_ready();
-    if (e == cudaSuccess) e = scan_type(dtype, [&](auto t) { return scan_forward<decltype(t)>(p, (cudaStream_t)stream); });
+    if (e == cudaSuccess) e = scan_type(dtype, [&](auto t) { return p.wide ? scan_forward<decltype(t), false>(p, s) : scan_forward<decltype(t), true>(p, s); });
     return operator_result(e);
 }
 
@@ -979,11 +1109,10 @@ extern "C" int rsdgc_gated_scan_backward(const void *dy_dev, int64_t dy_seq, int
     p.groups = scan_groups(width);
     p.runs = scan_runs(n_steps);
     p.seq_parts = (int)scan_seq_parts(n_seq, width);
-    p.vec = scan_pairs(p.x, elem) && scan_pairs(p.gate, elem) && scan_pairs(p.y, elem) && (!dx_dev || scan_pairs(p.dx, elem)) &&
-            (!dgate_dev || scan_pairs(p.dgate, elem));
+    p.vec = (!dx_dev || scan_pairs(p.dx, elem)) && (!dgate_dev || scan_pairs(p.dgate, elem));
     p.wide = scan_wide(p.x, elem) && scan_wide(p.gate, elem) && scan_wide(p.y, elem);
     cudaError_t e = operators_ready();
-    if (e == cudaSuccess) e = scan_type(dtype, [&](auto t) { return scan_backward<decltype(t)>(p, s); });
+    if (e == cudaSuccess) e = scan_type(dtype, [&](auto t) { return p.wide ? scan_backward<decltype(t), false>(p, s) : scan_backward<decltype(t), true>(p, s); });
     if (e == cudaSuccess && dbias_dev)
         e = scan_type(grad_dtype, [&](auto g) {
             typedef decltype(g) G;
