@@ -33,10 +33,12 @@ constexpr int kOrthoThreads = 128 + 32 * kOrthoWarps;     // producer, MMA, two 
 constexpr int kOrthoStaging = 2048;                       // per epilogue warp: 32 rows of 64 bytes
 constexpr int kOrthoSmem = kRingBlocks * kBlockBytes + kOrthoWarps * kOrthoStaging + 1024;
 constexpr int kOrthoMaxSteps = 32;
-constexpr float kOrthoScale = 4096.0f;                    // of Y's planes; A's and B's have 2^13
+constexpr float kOrthoScale = 4096.0f;                    // of Y's planes
+constexpr float kOrthoScaleA = 8192.0f;                   // of A's and B's
 
-// What becomes of a product.  kGram: A; kGramPart: binary32 parts of A; kPoly: B from A A; kUpdate: the next Y; kResult: the result.
-enum { kGram = 0, kGramPart = 1, kPoly = 2, kUpdate = 3, kResult = 4 };
+// What becomes of a product.  kGram: A; kGramPart: binary32 parts of A; kPoly: B from A A; kSquare: a + B from the square of a shifted A;
+// kUpdate: the next Y; kResult: the result.
+enum { kGram = 0, kGramPart = 1, kPoly = 2, kUpdate = 3, kResult = 4, kSquare = 5 };
 
 struct __align__(64) OrthoParams {
     CUtensorMap a, b;        // [matrix x plane][rows][columns], boxes of 64 x 64
@@ -51,7 +53,8 @@ struct __align__(64) OrthoParams {
     int tiles, stages;
     int rows, columns;       // of the product
     long long pitch;         // of the planes below, a multiple of 8
-    const __half *in;        // kPoly: A, kUpdate and kResult: Y; in_planes planes of rows x pitch per matrix
+    float diag;              // added to the product's diagonal
+    const __half *in;        // kPoly: A, kUpdate and kResult: Y; in_planes (0: none) planes of rows x pitch per matrix
     __half *out;             // out_planes planes
     int in_planes, out_planes;
     float in_scale, acc_scale;
@@ -173,6 +176,28 @@ struct OrthoStage {
                 *reinterpret_cast<uint4 *>(plane + row * pitch + c) = v;
         }
     }
+    // 32 x 32 binary32 values, 16 columns at a time
+    __device__ __forceinline__ void store_part(const float (&z)[32], float *plane, long long pitch, int row0, int rows, int col) const
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                store_shared16(at(lane, i), __float_as_uint(z[16 * h + 4 * i]), __float_as_uint(z[16 * h + 4 * i + 1]),
+                               __float_as_uint(z[16 * h + 4 * i + 2]), __float_as_uint(z[16 * h + 4 * i + 3]));
+            __syncwarp();
+            const int c = col + 16 * h + (lane & 3) * 4;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = row0 + j * 8 + (lane >> 2);
+                uint4 v;
+                load_shared16(at(j * 8 + (lane >> 2), lane & 3), v.x, v.y, v.z, v.w);
+                if (row < rows && c < pitch && RSDGC_IN_BOUNDS(row >= 0 && c >= 0 && c + 4 <= pitch))
+                    *reinterpret_cast<uint4 *>(plane + row * pitch + c) = v;
+            }
+        }
+    }
     // ... to the caller's matrix, which has neither padding nor alignment
     __device__ __forceinline__ void store_result(uint16_t *dst, long long stride, int row0, int rows, int col, int columns, bool wide) const
     {
@@ -226,7 +251,7 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int stages = p.stages, stage_bytes = kRingBlocks / stages * kBlockBytes;
+    const int stages = p.stages, stage_bytes = (1 + p.halves) * kBlockBytes;
 
     if (warp == 0) {  // a lane per barrier
         if (lane < kMaxStages) {
@@ -266,56 +291,80 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
     };
 
     if (warp < 4) {
-        auto wait_warp = [&](uint32_t bar, uint32_t ph) -> bool { return __all_sync(0xFFFFFFFFu, wait(bar, ph)); };
-        // ---- producer, in both CTAs; all bytes count on the first CTA's barriers
-        if (warp == 0) {
+        // One thread of each of two warps walks alone: a stage of the ring is 256 to 512 cycles of MMAs, which a loop that the whole warp
+        // walks, with coordinates formed anew for each box, takes longer to issue (2048 x 2048: 425 us then, 350 us now).
+        if (warp == 0 && elect_one()) {  // ---- producer, in both CTAs; all bytes count on the first CTA's barriers
             int stage = 0, it = 0;
-            uint32_t parity = 0;
+            uint32_t parity = 0, dst = ring;
             bool ok = true;
             asm volatile("fence.proxy.async.global;" ::: "memory");  // TMA reads what ordinary stores wrote
-            const bool whole = p.cols == kTile;  // of an accumulator's columns a CTA holds half: one box or two
-            const uint32_t bytes = 2u * (uint32_t)(kBlockBytes + p.halves * p.cols * kStepK);
+            const int halves = p.halves;
+            const uint32_t bytes = 2u * (uint32_t)(kBlockBytes + halves * p.cols * kStepK);
+            const uint32_t full0 = leader_addr(smem_addr(&full[0])), empty0 = smem_addr(&empty[0]);
+            // coordinates of a box: (k, row), or (row, k) where the rows are contiguous: then of an operand's 128 rows in this CTA two boxes
+            const int ak = p.a_mn ? 0 : kStepK, bk = p.b_mn ? 0 : kStepK, br = p.b_mn ? 64 : 0;
+            const bool a_two = p.a_mn, b_two = p.b_mn && p.cols == kTile;
+            auto next = [&] {
+                ++it;
+                dst += stage_bytes;
+                if (++stage == stages) {
+                    stage = 0;
+                    dst = ring;
+                    parity ^= 1u;
+                }
+            };
+            auto announce = [&] {
+                if (rank == 0) barrier_expect(smem_addr(&full[stage]), bytes);
+                sent[rank][stage] = (int)(bytes / 2);
+            };
             for (int t = pair; t < p.tiles && ok; t += pairs) {
                 const OrthoTile tp = ortho_tile(p, t);
-                const int ra = tp.m * kTile + (int)rank * kHalf, rb = tp.n * p.halves * p.cols + (int)rank * (p.cols >> 1);
-                for (int k = 0; k < tp.steps; ++k) {
-                    ok = wait_warp(smem_addr(&empty[stage]), parity ^ 1u);
-                    if (!ok) break;
-                    const uint32_t bar = leader_addr(smem_addr(&full[stage])), dst = ring + stage * stage_bytes;
-                    const int seg = (tp.k0 + k) / p.k_steps, kc = (tp.k0 + k - seg * p.k_steps) * kStepK;
-                    const int za = tp.matrix * p.a_planes + (seg == 2), zb = tp.matrix * p.b_planes + (seg == 1);
-                    if (elect_one() && RSDGC_IN_BOUNDS(kc >= 0 && ra >= 0 && rb >= 0 && ra % 64 == 0 && rb % 64 == 0 && kc % 64 == 0 &&
-                                                       seg < p.segments && stage < stages && tp.m < p.m_tiles && tp.n < p.n_tiles)) {
-                        if (rank == 0) barrier_expect(smem_addr(&full[stage]), bytes);
-                        sent[rank][stage] = (int)(bytes / 2);
-                        // coordinates of a box: (k, row), or (row, k) where the rows are contiguous
-                        for (int i = 0; i < 2; ++i)
-                            load_box(dst + i * kBoxBytes, &p.a, p.a_mn ? ra + 64 * i : kc, p.a_mn ? kc : ra + 64 * i, za, bar);
-                        for (int h = 0; h < p.halves; ++h)
-                            for (int i = 0; i < (whole ? 2 : 1); ++i) {
-                                const int r = rb + h * kTile + 64 * i;
-                                load_box(dst + (1 + h) * kBlockBytes + i * kBoxBytes, &p.b, p.b_mn ? r : kc, p.b_mn ? kc : r, zb, bar);
+                const int ra = tp.m * kTile + (int)rank * kHalf, rb = tp.n * halves * p.cols + (int)rank * (p.cols >> 1);
+                const int steps = tp.steps;
+                int seg = tp.k0 / p.k_steps, at = tp.k0 - seg * p.k_steps;
+                for (int k = 0; k < steps && ok;) {
+                    // the steps up to the segment's end
+                    const int end = min(steps, k + p.k_steps - at), za = tp.matrix * p.a_planes + (seg == 2),
+                              zb = tp.matrix * p.b_planes + (seg == 1), kc = at * kStepK;
+                    int ax = p.a_mn ? ra : kc, ay = p.a_mn ? kc : ra, bx = p.b_mn ? rb : kc, by = p.b_mn ? kc : rb;
+                    const bool inside = RSDGC_IN_BOUNDS(ra >= 0 && rb >= 0 && at >= 0 && ra % 64 == 0 && rb % 64 == 0 && seg < p.segments &&
+                                                        tp.m < p.m_tiles && tp.n < p.n_tiles && tp.k0 + steps <= p.segments * p.k_steps);
+                    for (; k < end; ++k) {
+                        ok = wait(empty0 + 8 * stage, parity ^ 1u);
+                        if (!ok) break;
+                        if (inside) {
+                            const uint32_t bar = full0 + 8 * stage;
+                            announce();
+                            load_box(dst, &p.a, ax, ay, za, bar);
+                            if (a_two) load_box(dst + kBoxBytes, &p.a, ax + 64, ay, za, bar);
+                            load_box(dst + kBlockBytes, &p.b, bx, by, zb, bar);
+                            if (b_two) load_box(dst + kBlockBytes + kBoxBytes, &p.b, bx + 64, by, zb, bar);
+                            if (halves == 2) {
+                                load_box(dst + 2 * kBlockBytes, &p.b, bx + 4 * br, by + 4 * (64 - br), zb, bar);
+                                if (b_two) load_box(dst + 2 * kBlockBytes + kBoxBytes, &p.b, bx + 5 * 64, by, zb, bar);
                             }
+                            ax += ak;
+                            ay += kStepK - ak;
+                            bx += bk;
+                            by += kStepK - bk;
+                        }
+                        next();
                     }
-                    __syncwarp();
-                    ++it;
-                    if (++stage == stages) {
-                        stage = 0;
-                        parity ^= 1u;
-                    }
+                    at = 0;
+                    ++seg;
                 }
             }
             // the last commits arrive on this CTA's barriers: it must not leave before they have
             for (int i = 0; i < stages && ok; ++i) {
-                ok = wait_warp(smem_addr(&empty[stage]), parity ^ 1u);
+                ok = wait(empty0 + 8 * stage, parity ^ 1u);
                 if (++stage == stages) {
                     stage = 0;
                     parity ^= 1u;
                 }
             }
-            if (lane == 0) issued[rank] = it;
+            issued[rank] = it;
         }
-        if (warp == 1 && rank == 0) {  // ---- MMA, the pair's first CTA: the warp walks together, one thread issues
+        if (warp == 1 && rank == 0 && elect_one()) {  // ---- MMA, the pair's first CTA
             int stage = 0, sub = 0;    // sub: accumulators used so far; they alternate
             uint32_t parity = 0;
             bool ok = true;
@@ -324,6 +373,8 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
                                    ((uint32_t)(kTile >> 4) << 24);  // binary16 operands, binary32 sums
             const uint32_t da = p.a_mn ? 2048 >> 4 : 32 >> 4, db = p.b_mn ? 2048 >> 4 : 32 >> 4;
             const uint64_t a_base = operand_desc(ring, p.a_mn), b_base = operand_desc(ring + kBlockBytes, p.b_mn);
+            const uint32_t full0 = smem_addr(&full[0]), empty0 = smem_addr(&empty[0]), acc_full0 = smem_addr(&acc_full[0]),
+                           acc_empty0 = smem_addr(&acc_empty[0]);
             auto issue = [&](int st, int h, int acc, int k) {
                 const uint64_t a = a_base + (uint32_t)(st * (stage_bytes >> 4));
                 const uint64_t b = b_base + (uint32_t)(st * (stage_bytes >> 4) + h * (kBlockBytes >> 4));
@@ -335,7 +386,7 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
                 const int steps = ortho_tile(p, t).steps;
                 const int acc0 = sub & 1, acc1 = acc0 ^ 1;
                 const uint32_t parity0 = (uint32_t)((sub >> 1) & 1) ^ 1u, parity1 = (uint32_t)(((sub + 1) >> 1) & 1) ^ 1u;
-                ok = wait_warp(smem_addr(&acc_empty[acc0]), parity0);
+                ok = wait(acc_empty0 + 8 * acc0, parity0);
                 if (!ok) break;
                 tmem_fence_after();
                 // With two accumulators the second may still be read when the first is free: its products follow
@@ -343,30 +394,24 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
                 bool second = halves == 1;
                 int behind = 0, tail = stage, kb = 0;
                 for (int k = 0; k < steps; ++k) {
-                    ok = wait_warp(smem_addr(&full[stage]), parity);
+                    ok = wait(full0 + 8 * stage, parity);
                     if (!ok) break;
-                    if (elect_one()) {
-                        issue(stage, 0, acc0, k);
-                        if (k + 1 == steps) mma_commit_both(smem_addr(&acc_full[acc0]));
-                    }
-                    __syncwarp();
+                    issue(stage, 0, acc0, k);
+                    if (k + 1 == steps) mma_commit_both(acc_full0 + 8 * acc0);
                     ++behind;
                     if (!second) {
                         if (behind == stages || k + 1 == steps) {
-                            ok = wait_warp(smem_addr(&acc_empty[acc1]), parity1);
+                            ok = wait(acc_empty0 + 8 * acc1, parity1);
                             if (!ok) break;
                             second = true;
                         } else {
-                            second = __all_sync(0xFFFFFFFFu, barrier_test(smem_addr(&acc_empty[acc1]), parity1));
+                            second = barrier_test(acc_empty0 + 8 * acc1, parity1);
                         }
                         if (second) tmem_fence_after();
                     }
                     for (; second && behind; --behind, ++kb) {
-                        if (elect_one()) {
-                            if (halves == 2) issue(tail, 1, acc1, kb);
-                            mma_commit_both(smem_addr(&empty[tail]));
-                        }
-                        __syncwarp();
+                        if (halves == 2) issue(tail, 1, acc1, kb);
+                        mma_commit_both(empty0 + 8 * tail);
                         if (++tail == stages) tail = 0;
                     }
                     if (++stage == stages) {
@@ -375,8 +420,7 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
                     }
                 }
                 if (!ok) break;
-                if (halves == 2 && elect_one()) mma_commit_both(smem_addr(&acc_full[acc1]));
-                __syncwarp();
+                if (halves == 2) mma_commit_both(acc_full0 + 8 * acc1);
                 sub += halves;
             }
         }
@@ -391,8 +435,8 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
         for (int t = pair; t < p.tiles && ok; t += pairs) {
             const OrthoTile tp = ortho_tile(p, t);
             const int row0 = tp.m * kTile + (int)rank * kHalf + quad * 32, row = row0 + lane;
-            const __half *in = KIND == kPoly || KIND >= kUpdate ? p.in + (long long)tp.matrix * p.in_planes * plane : nullptr;
-            __half *out = KIND == kGram || KIND == kPoly || KIND == kUpdate ? p.out + (long long)tp.matrix * p.out_planes * plane : nullptr;
+            const __half *in = KIND == kPoly || KIND == kUpdate || KIND == kResult ? p.in + (long long)tp.matrix * p.in_planes * plane : nullptr;
+            __half *out = KIND != kGramPart && KIND != kResult ? p.out + (long long)tp.matrix * p.out_planes * plane : nullptr;
             for (int h = 0; h < p.halves; ++h, ++sub) {
                 const int acc = sub & 1, col0 = (tp.n * p.halves + h) * p.cols + quarter * width;
                 const uint32_t src = tmem_base + (uint32_t)acc * kTile + quarter * width + ((uint32_t)(quad * 32) << 16);
@@ -401,7 +445,8 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
                     stg.fetch(hi, in, p.pitch, row0, p.rows, col);
                     if (p.in_planes > 1) stg.fetch(lo, in + plane, p.pitch, row0, p.rows, col);
                 };
-                if (KIND == kPoly || KIND >= kUpdate) fetch(col0);
+                constexpr bool adds = KIND == kPoly || KIND == kUpdate || KIND == kResult;
+                if (adds && p.in_planes > 0) fetch(col0);
                 ok = __all_sync(0xFFFFFFFFu, wait(smem_addr(&acc_full[acc]), (uint32_t)((sub >> 1) & 1)));
                 if (!ok) break;
                 tmem_fence_after();
@@ -422,16 +467,11 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
                     for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(raw[i]) * p.acc_scale;
                     if (row0 >= p.rows || col >= (KIND == kResult ? p.columns : p.pitch)) continue;
                     if constexpr (KIND == kGramPart) {
-                        float *dst = p.part + ((long long)(tp.matrix * p.splits + tp.split) * p.rows + row) * p.pitch + col;
-                        if (row < p.rows) {
-#pragma unroll
-                            for (int i = 0; i < 32; i += 4)
-                                if (col + i < p.pitch && RSDGC_IN_BOUNDS(col + i + 4 <= p.pitch && tp.split < p.splits))
-                                    *reinterpret_cast<float4 *>(dst + i) = make_float4(z[i], z[i + 1], z[i + 2], z[i + 3]);
-                        }
+                        float *dst = p.part + (long long)(tp.matrix * p.splits + tp.split) * p.rows * p.pitch;
+                        stg.store_part(z, dst, p.pitch, row0, p.rows, col);
                         continue;
                     }
-                    if constexpr (KIND == kPoly || KIND >= kUpdate) {
+                    if (adds && p.in_planes > 0) {
                         stg.deal(hi);
                         stg.add_row(z, p.in_scale);
                         if (p.in_planes > 1) {
@@ -439,6 +479,13 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
                             stg.add_row(z, p.in_scale);
                         }
                         if (at + 32 < width) fetch(col + 32);
+                    }
+                    if constexpr (KIND == kGram || KIND == kSquare) {
+                        if (p.diag != 0.0f && col <= row0 + 31 && col + 31 >= row0) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (col + i == row && row < p.rows) z[i] += p.diag;
+                        }
                     }
                     if constexpr (KIND == kResult) {
                         stg.template put_row<T>(z);
@@ -535,7 +582,7 @@ k_ortho_norm(const T *__restrict__ x, long long row_stride, long long matrix_str
     grid_dependency_launch_next();
     const T *m = x + matrix * matrix_stride;
     const int across = (cols + kOrthoItem - 1) / kOrthoItem;
-    double s = 0.0;
+    double some[4] = {};
     for (long long i = part * kOrthoLoadWarps + warp; i < (long long)rows * across; i += parts * kOrthoLoadWarps) {
         const long long row = i / across;
         const int c0 = (int)(i - row * across) * kOrthoItem;
@@ -546,10 +593,11 @@ k_ortho_norm(const T *__restrict__ x, long long row_stride, long long matrix_str
             if (c < cols) {
                 ortho_load8(v, m + row * row_stride + c, cols - c, wide);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) s = fma((double)v[k], (double)v[k], s);
+                for (int k = 0; k < 8; ++k) some[k & 3] = fma((double)v[k], (double)v[k], some[k & 3]);
             }
         }
     }
+    double s = (some[0] + some[1]) + (some[2] + some[3]);
 #pragma unroll
     for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
     if (lane == 0) sums[warp] = s;
@@ -604,7 +652,7 @@ k_ortho_load(const T *__restrict__ x, long long row_stride, long long matrix_str
 
 // A = the sum of its parts, in order: a CTA per block of 32 x 32 on or below the diagonal, which it also writes across it.
 __global__ void __launch_bounds__(256)
-k_ortho_join(const float *__restrict__ part, int splits, int n, long long pitch, int blocks, __half *__restrict__ out, int planes)
+k_ortho_join(const float *__restrict__ part, int splits, int n, long long pitch, int blocks, float diag, __half *__restrict__ out, int planes)
 {
     __shared__ float block[32][33];
     int i = blockIdx.x % (blocks * (blocks + 1) / 2);
@@ -631,6 +679,7 @@ k_ortho_join(const float *__restrict__ part, int splits, int n, long long pitch,
         float v = 0.0f;
         if (r < n && c < pitch)
             for (int s = 0; s < splits; ++s) v += part[s * plane + r * pitch + c];
+        if (r == c) v += diag;
         block[row0 + 8 * j][lane] = v;
         put(r, c, v);
     }
@@ -674,12 +723,13 @@ OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols, int out_dtyp
     L.segments = L.planes == 2 ? 3 : 1;
     const int64_t items = rows * ((cols + kOrthoItem - 1) / kOrthoItem), want = (items + kOrthoLoadWarps - 1) / kOrthoLoadWarps;
     L.parts = (int)(want < kOrthoLoadParts ? want : kOrthoLoadParts);
-    // A's tiles are few where it is small: its contraction is cut so that every pair of CTAs has a part, of 8 steps at least
+    // A's tiles are few where it is small: its contraction is cut so that every pair of CTAs has a part, where the steps that this
+    // saves are more than the second kernel takes (about 7 us, 26 steps; a part's bytes about two)
     const int64_t m = tiles_of(L.side, kTile), tiles = batch * m * (m + 1) / 2;
     const int64_t steps = (int64_t)L.segments * tiles_of(L.tall ? rows : cols, kStepK);
-    int64_t s = tiles > 0 ? kOrthoPairs / tiles : 1;
-    if (s > steps / 8) s = steps / 8;
-    if (s < 1) s = 1;
+    int64_t s = 1, least = steps;
+    for (int64_t i = 2; i <= (tiles > 0 ? kOrthoPairs / tiles : 1) && i <= steps / 8; ++i)
+        if ((steps + i - 1) / i + 26 + 2 * i < least) least = (steps + i - 1) / i + 26 + 2 * i, s = i;
     L.split_steps = (int)((steps + s - 1) / s);
     L.splits = (int)((steps + L.split_steps - 1) / L.split_steps);
     int64_t at = 0;
@@ -708,7 +758,8 @@ int ortho_check(int64_t batch, int64_t rows, int64_t cols, int out_dtype)
 
 // The polynomials as a whole keep singular values within [0, most], most <= 2, and |b x + c x^2| <= 7.5 for x = s^2: what the scaled
 // binary16 planes hold.  s is at most 1 at first; a step's largest value lies at an end or where a + 3 b s^2 + 5 c s^4 = 0.
-bool ortho_bounded(const float *coef, int steps)
+// square[i]: whether they hold A + b / 2c and a + b x + c x^2 = c (x + b / 2c)^2 + a - b^2 / 4c as well.
+bool ortho_bounded(const float *coef, int steps, bool *square)
 {
     double most = 1.0;
     for (int i = 0; i < steps; ++i) {
@@ -737,24 +788,35 @@ bool ortho_bounded(const float *coef, int steps)
         } else if (b != 0.0) {
             at(-a / (3.0 * b));
         }
+        square[i] = std::fabs(c) > 0.1 && std::fabs(b / (2.0 * c)) + most * most <= 7.5 && std::fabs(a) + poly <= 7.5;
         most = top * (1.0 + 0x1p-7);  // and what the roundings add
         if (most > 2.0 || poly > 7.5) return false;
     }
     return true;
 }
 
-// [matrix x plane][rows][cols] binary16 values, boxes of 64 x 64; what lies outside reads as zero
-cudaError_t ortho_map(CUtensorMap *map, const void *base, int64_t slabs, int64_t rows, int64_t cols, int64_t pitch)
+// [matrix x plane][rows][cols] binary16 values, boxes of 64 columns; what lies outside reads as zero
+cudaError_t ortho_map(CUtensorMap *map, const void *base, int64_t slabs, int64_t rows, int64_t cols, int64_t pitch, int box_rows)
 {
     EncodeFn fn = encode_fn();
     if (!fn) return cudaErrorNotSupported;
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)slabs};
     const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)pitch * 2 * (cuuint64_t)rows};
-    const cuuint32_t box[3] = {64, 64, 1}, one[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, one[3] = {1, 1, 1};
     const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base), dims, strides, box, one,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+// ... with boxes of 64 rows, and of 128: all rows of a CTA's block, where they do not lie contiguous
+struct OrthoMaps {
+    CUtensorMap of[2];
+};
+cudaError_t ortho_maps(OrthoMaps *m, const void *base, int64_t slabs, int64_t rows, int64_t cols, int64_t pitch)
+{
+    const cudaError_t e = ortho_map(&m->of[0], base, slabs, rows, cols, pitch, 64);
+    return e != cudaSuccess ? e : ortho_map(&m->of[1], base, slabs, rows, cols, pitch, kHalf);
 }
 
 // Pairs of CTAs that the device holds at a time; 0 and an error in *e if the kernel cannot run.
@@ -826,6 +888,7 @@ struct OrthoCall {
     int64_t out_row, out_matrix;
     int out_dtype;
     const float *coef;
+    const bool *square;
     int steps;
     float eps;
     unsigned char *workspace;
@@ -833,12 +896,14 @@ struct OrthoCall {
 };
 
 template <int KIND, typename T>
-cudaError_t ortho_product(OrthoParams &p, const OrthoCall &c)
+cudaError_t ortho_product(OrthoParams &p, const OrthoMaps &left, const OrthoMaps &right, const OrthoCall &c)
 {
     cudaError_t e = cudaSuccess;
     const int most = ortho_pairs<KIND, T>(&e);
     if (e != cudaSuccess) return e;
     ortho_columns(p, c.l.batch, most);
+    p.a = left.of[!p.a_mn];
+    p.b = right.of[!p.b_mn && p.cols == kTile];
     const unsigned pairs = (unsigned)(p.tiles < most ? p.tiles : most);
     return launch_chained(k_ortho<KIND, T>, 2 * pairs, kOrthoThreads, kOrthoSmem, c.s, 2, p);
 }
@@ -869,18 +934,22 @@ cudaError_t orthogonalize(const OrthoCall &c)
     base.segments = L.segments;
     base.splits = 1;
     if (e == cudaSuccess) e = operator_status_ptr(&base.status);
-    CUtensorMap y[2], a, b;
-    for (int i = 0; i < 2 && e == cudaSuccess; ++i) e = ortho_map(&y[i], c.workspace + L.y[i], 2 * L.batch, L.rows, L.cols, L.pitch);
-    if (e == cudaSuccess) e = ortho_map(&a, c.workspace + L.a, L.planes * L.batch, L.side, L.side, L.side_pitch);
-    if (e == cudaSuccess) e = ortho_map(&b, c.workspace + L.b, L.planes * L.batch, L.side, L.side, L.side_pitch);
+    OrthoMaps y[2], a, b;
+    for (int i = 0; i < 2 && e == cudaSuccess; ++i) e = ortho_maps(&y[i], c.workspace + L.y[i], 2 * L.batch, L.rows, L.cols, L.pitch);
+    if (e == cudaSuccess) e = ortho_maps(&a, c.workspace + L.a, L.planes * L.batch, L.side, L.side, L.side_pitch);
+    if (e == cudaSuccess) e = ortho_maps(&b, c.workspace + L.b, L.planes * L.batch, L.side, L.side, L.side_pitch);
     if (e == cudaSuccess)
         e = c.dtype == RSDGC_F32 ? ortho_load<float>(c) : c.dtype == RSDGC_BF16 ? ortho_load<__nv_bfloat16>(c) : ortho_load<__half>(c);
     __half *const ap = (__half *)(c.workspace + L.a), *const bp = (__half *)(c.workspace + L.b);
     for (int i = 0; i < c.steps && e == cudaSuccess; ++i) {
-        const CUtensorMap &from = y[i & 1];
+        const OrthoMaps &from = y[i & 1];
         __half *const yp = (__half *)(c.workspace + L.y[i & 1]);
+        const double ca = c.coef[3 * i], cb = c.coef[3 * i + 1], cc = c.coef[3 * i + 2];
+        // Three products: 22 bits hold a + B as well as B, so that a Y needs no addition of its own; nor does b A with the square completed.
+        // The epilogues then read nothing (256 x 1024: 24 matrices' update 34 us with that, 25 us without).
+        const bool square = L.segments == 3 && c.square[i];
         OrthoParams p = base;  // A = Y Y^T or Y^T Y
-        p.a = p.b = from;
+        p.diag = square ? (float)(cb / (2.0 * cc)) * kOrthoScaleA : 0.0f;
         p.a_mn = p.b_mn = L.tall;
         p.a_planes = p.b_planes = 2;
         p.k_steps = tiles_of(L.tall ? L.rows : L.cols, kStepK);
@@ -895,30 +964,31 @@ cudaError_t orthogonalize(const OrthoCall &c)
         p.out_planes = L.planes;
         p.part = (float *)(c.workspace + L.sums);
         if (L.splits > 1) {
-            e = ortho_product<kGramPart, __half>(p, c);
+            e = ortho_product<kGramPart, __half>(p, from, from, c);
             const int blocks = tiles_of(L.side, 32);
             if (e == cudaSuccess)
                 e = launch_chained(k_ortho_join, (unsigned)(L.batch * blocks * (blocks + 1) / 2), 256, 0, c.s, 1, (const float *)p.part,
-                                   L.splits, (int)L.side, (long long)L.side_pitch, blocks, ap, L.planes);
+                                   L.splits, (int)L.side, (long long)L.side_pitch, blocks, p.diag, ap, L.planes);
         } else {
-            e = ortho_product<kGram, __half>(p, c);
+            e = ortho_product<kGram, __half>(p, from, from, c);
         }
         if (e != cudaSuccess) break;
-        p.a = p.b = a;  // B = b A + c A A
+        // B = b A + c A A
         p.a_mn = p.b_mn = 0;
-        p.a_planes = p.b_planes = p.in_planes = L.planes;
+        p.a_planes = p.b_planes = L.planes;
+        p.in_planes = square ? 0 : L.planes;
         p.k_steps = tiles_of(L.side, kStepK);
         p.splits = 1;
         p.split_steps = L.segments * p.k_steps;
         p.in = ap;
-        p.in_scale = c.coef[3 * i + 1];
-        p.acc_scale = c.coef[3 * i + 2] * 0x1p-13f;
+        p.in_scale = (float)cb;
+        p.acc_scale = (float)cc * 0x1p-13f;
+        p.diag = square ? (float)(ca - cb * cb / (4.0 * cc)) * kOrthoScaleA : 0.0f;
         p.out = bp;
-        e = ortho_product<kPoly, __half>(p, c);
+        e = square ? ortho_product<kSquare, __half>(p, a, a, c) : ortho_product<kPoly, __half>(p, a, a, c);
         if (e != cudaSuccess) break;
         // B Y, or Y B where B is as good as its transpose
-        p.a = L.tall ? from : b;
-        p.b = L.tall ? b : from;
+        const OrthoMaps &left = L.tall ? from : b, &right = L.tall ? b : from;
         p.b_mn = !L.tall;
         p.a_planes = L.tall ? 2 : L.planes;
         p.b_planes = L.tall ? L.planes : 2;
@@ -929,13 +999,14 @@ cudaError_t orthogonalize(const OrthoCall &c)
         p.m_tiles = tiles_of(L.rows, kTile);
         p.band = p.m_tiles < 16 ? p.m_tiles : 16;
         p.in = yp;
-        p.in_planes = 2;
-        p.in_scale = c.coef[3 * i];
+        p.in_planes = square ? 0 : 2;
+        p.in_scale = (float)ca;
         p.acc_scale = 0x1p-13f;
+        p.diag = 0.0f;
         p.out = (__half *)(c.workspace + L.y[(i + 1) & 1]);
         p.out_planes = 2;
         if (i + 1 < c.steps) {
-            e = ortho_product<kUpdate, __half>(p, c);
+            e = ortho_product<kUpdate, __half>(p, left, right, c);
         } else {
             p.in_scale *= 1.0f / kOrthoScale;
             p.acc_scale *= 1.0f / kOrthoScale;
@@ -943,7 +1014,7 @@ cudaError_t orthogonalize(const OrthoCall &c)
             p.result_row = c.out_row;
             p.result_matrix = c.out_matrix;
             p.result_wide = pointer_aligned(c.out, 16) && c.out_row % 8 == 0 && c.out_matrix % 8 == 0;
-            e = c.out_dtype == RSDGC_BF16 ? ortho_product<kResult, __nv_bfloat16>(p, c) : ortho_product<kResult, __half>(p, c);
+            e = c.out_dtype == RSDGC_BF16 ? ortho_product<kResult, __nv_bfloat16>(p, left, right, c) : ortho_product<kResult, __half>(p, left, right, c);
         }
     }
     return e;
@@ -969,7 +1040,8 @@ extern "C" int rsdgc_orthogonalize(const void *x_dev, int64_t x_row_stride, int6
     if (rc) return rc;
     if (!known_dtype(dtype) || !coefficients_host || n_steps < 1 || n_steps > kOrthoMaxSteps || !(eps >= 0.0f && eps < INFINITY))
         return RSDGC_ERR_INVALID;
-    if (!ortho_bounded(coefficients_host, n_steps)) return RSDGC_ERR_INVALID;
+    bool square[kOrthoMaxSteps];
+    if (!ortho_bounded(coefficients_host, n_steps, square)) return RSDGC_ERR_INVALID;
     if (n_matrices == 0 || n_rows == 0 || n_cols == 0) return RSDGC_OK;
     if (!x_dev || !out_dev || !workspace_dev || (n_rows > 1 && (x_row_stride < n_cols || out_row_stride < n_cols)) ||
         (n_matrices > 1 && (x_matrix_stride < n_cols || out_matrix_stride < n_cols)))
@@ -980,7 +1052,7 @@ extern "C" int rsdgc_orthogonalize(const void *x_dev, int64_t x_row_stride, int6
     if (n_matrices == 1) x_matrix_stride = out_matrix_stride = 0;  // free, and so are a single row's
     if (n_rows == 1) x_row_stride = out_row_stride = 0;
     const OrthoCall c = {ortho_layout(n_matrices, n_rows, n_cols, out_dtype), x_dev, x_row_stride, x_matrix_stride, dtype, out_dev,
-                         out_row_stride, out_matrix_stride, out_dtype, coefficients_host, n_steps, eps, (unsigned char *)workspace_dev,
+                         out_row_stride, out_matrix_stride, out_dtype, coefficients_host, square, n_steps, eps, (unsigned char *)workspace_dev,
                          (cudaStream_t)stream};
     return operator_result(orthogonalize(c));
 }
