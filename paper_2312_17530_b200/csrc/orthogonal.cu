@@ -16,7 +16,11 @@
 // written a second time across it.  Y is read as it lies, once with its rows and once with its columns contracted.  Where A has
 // few tiles and a long contraction, the contraction is cut into parts which k_ortho_join adds up, in order.
 //
-// What bounds it: the tensor cores.
+// What bounds it: the tensor cores where matrices are large (4096 x 4096: 1088 cycles a step of 1024 cycles of MMAs); latency where they are
+// small (256 x 512: 141 us, 17 launches of 8 us each: 0.8 us until the first operands are there, 0.16 us a contraction step, 2.5 us of epilogue,
+// the rest is a launch's; all products in one launch, whose CTAs count one another's epilogues, were 8 % faster at 256 x 512 and 9 % slower at
+// 2048 x 2048: not worth its waits); the epilogue's
+// memory traffic where one side is far longer than the other.
 #include <climits>
 #include <cmath>
 #include <cstring>
@@ -81,7 +85,7 @@ __device__ __forceinline__ OrthoTile ortho_tile(const OrthoParams &p, int t)
     r.steps = min(p.split_steps, p.segments * p.k_steps - r.k0);
     if (p.symmetric) {
         const int wide = p.cols * p.halves;
-        for (r.m = 0;; ++r.m) {
+        for (r.m = 0; r.m < p.m_tiles; ++r.m) {
             const int here = min(p.n_tiles, ((r.m + 1) * kTile + wide - 1) / wide);
             if (t < here) break;
             t -= here;
@@ -236,6 +240,15 @@ __device__ __forceinline__ void ortho_rest(float (&z)[32])
     for (int i = 0; i < 32; ++i) z[i] -= __half2float(__float2half_rn(z[i]));
 }
 
+// A parameter that stays in a register: what the issuing loops need of the kernel's parameters is otherwise read anew in each round, at some
+// 150 cycles a time.
+template <typename V>
+__device__ __forceinline__ V ortho_keep(V v)
+{
+    asm volatile("" : "+r"(v));
+    return v;
+}
+
 // T: type of the result (kResult)
 template <int KIND, typename T>
 __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constant__ OrthoParams p)
@@ -251,7 +264,8 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int stages = p.stages, stage_bytes = (1 + p.halves) * kBlockBytes;
+    const int stages = ortho_keep(p.stages), stage_bytes = ortho_keep((1 + p.halves) * kBlockBytes);
+    const unsigned polls = ortho_keep(p.polls);
 
     if (warp == 0) {  // a lane per barrier
         if (lane < kMaxStages) {
@@ -281,9 +295,10 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
 
     // Bounded: a wait that gives up marks the CTA dead, raises the status bit, and every role leaves its loop.
     auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
-        for (unsigned i = 0; i < p.polls; ++i) {
-            if (barrier_try(bar, parity)) return true;
+        if (barrier_try(bar, parity)) return true;
+        for (unsigned i = 1; i < polls; ++i) {
             if (dead) return false;
+            if (barrier_try(bar, parity)) return true;
         }
         dead = 1;
         atomicOr(p.status, RSDGC_STATUS_TIMEOUT);
@@ -292,26 +307,25 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
 
     if (warp < 4) {
         // One thread of each of two warps walks alone: a stage of the ring is 256 to 512 cycles of MMAs, which a loop that the whole warp
-        // walks, with coordinates formed anew for each box, takes longer to issue (2048 x 2048: 425 us then, 350 us now).
+        // walks, with coordinates formed and parameters read anew for each box, takes longer to issue (some 700 cycles a step; 320 so.  2048 x 2048: 425
+        // and 281 us).
         if (warp == 0 && elect_one()) {  // ---- producer, in both CTAs; all bytes count on the first CTA's barriers
             int stage = 0, it = 0;
             uint32_t parity = 0, dst = ring;
             bool ok = true;
             asm volatile("fence.proxy.async.global;" ::: "memory");  // TMA reads what ordinary stores wrote
-            const int halves = p.halves;
-            const uint32_t bytes = 2u * (uint32_t)(kBlockBytes + halves * p.cols * kStepK);
-            const uint32_t full0 = leader_addr(smem_addr(&full[0])), empty0 = smem_addr(&empty[0]);
+            const int halves = ortho_keep(p.halves);
+            const uint32_t bytes = ortho_keep(2u * (uint32_t)(kBlockBytes + halves * p.cols * kStepK));
+            const uint32_t full0 = ortho_keep(leader_addr(smem_addr(&full[0]))), empty0 = ortho_keep(smem_addr(&empty[0]));
             // coordinates of a box: (k, row), or (row, k) where the rows are contiguous: then of an operand's 128 rows in this CTA two boxes
-            const int ak = p.a_mn ? 0 : kStepK, bk = p.b_mn ? 0 : kStepK, br = p.b_mn ? 64 : 0;
-            const bool a_two = p.a_mn, b_two = p.b_mn && p.cols == kTile;
+            const int ak = ortho_keep(p.a_mn ? 0 : kStepK), bk = ortho_keep(p.b_mn ? 0 : kStepK), br = ortho_keep(p.b_mn ? 64 : 0);
+            const int a_two = ortho_keep((int)p.a_mn), b_two = ortho_keep((int)(p.b_mn && p.cols == kTile));
             auto next = [&] {
                 ++it;
-                dst += stage_bytes;
-                if (++stage == stages) {
-                    stage = 0;
-                    dst = ring;
-                    parity ^= 1u;
-                }
+                ++stage;
+                parity ^= (uint32_t)(stage == stages);
+                dst = stage == stages ? ring : dst + stage_bytes;
+                stage = stage == stages ? 0 : stage;
             };
             auto announce = [&] {
                 if (rank == 0) barrier_expect(smem_addr(&full[stage]), bytes);
@@ -320,7 +334,7 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
             for (int t = pair; t < p.tiles && ok; t += pairs) {
                 const OrthoTile tp = ortho_tile(p, t);
                 const int ra = tp.m * kTile + (int)rank * kHalf, rb = tp.n * halves * p.cols + (int)rank * (p.cols >> 1);
-                const int steps = tp.steps;
+                const int steps = ortho_keep(tp.steps);
                 int seg = tp.k0 / p.k_steps, at = tp.k0 - seg * p.k_steps;
                 for (int k = 0; k < steps && ok;) {
                     // the steps up to the segment's end
@@ -366,32 +380,47 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
         }
         if (warp == 1 && rank == 0 && elect_one()) {  // ---- MMA, the pair's first CTA
             int stage = 0, sub = 0;    // sub: accumulators used so far; they alternate
+            const uint32_t tmem = ortho_keep(tmem_base);
             uint32_t parity = 0;
             bool ok = true;
-            const int halves = p.halves;
-            const uint32_t idesc = (1u << 4) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) | ((uint32_t)(p.cols >> 3) << 17) |
-                                   ((uint32_t)(kTile >> 4) << 24);  // binary16 operands, binary32 sums
-            const uint32_t da = p.a_mn ? 2048 >> 4 : 32 >> 4, db = p.b_mn ? 2048 >> 4 : 32 >> 4;
+            const int halves = ortho_keep(p.halves);
+            const uint32_t idesc = ortho_keep((1u << 4) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) |
+                                              ((uint32_t)(p.cols >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24));  // binary16 operands, binary32 sums
+            const uint32_t da = ortho_keep(p.a_mn ? 2048u >> 4 : 32u >> 4), db = ortho_keep(p.b_mn ? 2048u >> 4 : 32u >> 4);
             const uint64_t a_base = operand_desc(ring, p.a_mn), b_base = operand_desc(ring + kBlockBytes, p.b_mn);
-            const uint32_t full0 = smem_addr(&full[0]), empty0 = smem_addr(&empty[0]), acc_full0 = smem_addr(&acc_full[0]),
-                           acc_empty0 = smem_addr(&acc_empty[0]);
+            const uint32_t full0 = ortho_keep(smem_addr(&full[0])), empty0 = ortho_keep(smem_addr(&empty[0])),
+                           acc_full0 = ortho_keep(smem_addr(&acc_full[0])), acc_empty0 = ortho_keep(smem_addr(&acc_empty[0]));
             auto issue = [&](int st, int h, int acc, int k) {
                 const uint64_t a = a_base + (uint32_t)(st * (stage_bytes >> 4));
                 const uint64_t b = b_base + (uint32_t)(st * (stage_bytes >> 4) + h * (kBlockBytes >> 4));
 #pragma unroll
                 for (int i = 0; i < kStepK / 16; ++i)
-                    mma_f16(tmem_base + (uint32_t)acc * kTile, a + i * da, b + i * db, idesc, (uint32_t)(k | i));
+                    mma_f16(tmem + (uint32_t)acc * kTile, a + i * da, b + i * db, idesc, (uint32_t)(k | i));
             };
             for (int t = pair; t < p.tiles; t += pairs) {
-                const int steps = ortho_tile(p, t).steps;
+                const int steps = ortho_keep(ortho_tile(p, t).steps);
                 const int acc0 = sub & 1, acc1 = acc0 ^ 1;
                 const uint32_t parity0 = (uint32_t)((sub >> 1) & 1) ^ 1u, parity1 = (uint32_t)(((sub + 1) >> 1) & 1) ^ 1u;
                 ok = wait(acc_empty0 + 8 * acc0, parity0);
                 if (!ok) break;
                 tmem_fence_after();
+                if (halves == 1) {
+                    for (int k = 0; k < steps; ++k) {
+                        if (!(ok = wait(full0 + 8 * stage, parity))) break;
+                        issue(stage, 0, acc0, k);
+                        mma_commit_both(empty0 + 8 * stage);
+                        ++stage;
+                        parity ^= (uint32_t)(stage == stages);
+                        stage = stage == stages ? 0 : stage;
+                    }
+                    if (!ok) break;
+                    mma_commit_both(acc_full0 + 8 * acc0);
+                    ++sub;
+                    continue;
+                }
                 // With two accumulators the second may still be read when the first is free: its products follow
                 // as soon as it is, at the latest when the ring is full of stages that wait for it.
-                bool second = halves == 1;
+                bool second = false;
                 int behind = 0, tail = stage, kb = 0;
                 for (int k = 0; k < steps; ++k) {
                     ok = wait(full0 + 8 * stage, parity);
@@ -410,7 +439,7 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
                         if (second) tmem_fence_after();
                     }
                     for (; second && behind; --behind, ++kb) {
-                        if (halves == 2) issue(tail, 1, acc1, kb);
+                        issue(tail, 1, acc1, kb);
                         mma_commit_both(empty0 + 8 * tail);
                         if (++tail == stages) tail = 0;
                     }
@@ -420,8 +449,8 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
                     }
                 }
                 if (!ok) break;
-                if (halves == 2) mma_commit_both(acc_full0 + 8 * acc1);
-                sub += halves;
+                mma_commit_both(acc_full0 + 8 * acc1);
+                sub += 2;
             }
         }
     } else {  // ---- epilogue: a thread owns one row and a quarter of an accumulator's columns
