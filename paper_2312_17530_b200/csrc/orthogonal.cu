@@ -724,7 +724,7 @@ RSDGC_DEFINE_DEBUG_BOUNDS(orthogonal_debug_bounds)
 namespace {
 
 constexpr int kOrthoPairs = 74;          // of CTAs on the device, for what workspaces depend on
-constexpr int kOrthoLoadParts = 296;     // most CTAs per matrix of the two passes over X
+constexpr int kOrthoLoadParts = 1184;    // most CTAs per matrix of the two passes over X: eight a multiprocessor (two: 32000 x 1024 859 us, 830 us so)
 constexpr int64_t kOrthoPrecise = 256;   // shorter sides up to this take three products for every result
 
 inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
