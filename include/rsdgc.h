@@ -498,7 +498,8 @@ int rsdgc_gated_scan_backward(const void *dy_dev, int64_t dy_seq, int64_t dy_ste
  * x: `dtype`; out: out_dtype, bfloat16 or binary16; row and matrix strides in elements, any alignment.  coefficients_host: 3 * n_steps
  * binary32 on the host, read during the call; n_steps 1 to 32.  workspace_dev: rsdgc_orthogonalize_workspace_bytes() bytes, 256-byte
  * aligned; nothing in it has to survive between calls.  A matrix of zeros gives zeros, one that is not finite NaN.
- * Accuracy: sums in binary32, operands of 11 bits (22 for a Y); the result is within 0.002 (relative 2-norm) of the formula's, before
+ * Accuracy: sums in binary32, operands of 11 bits (22 for a Y); the result is within 0.003 (relative 2-norm; typically 0.0015 of its Frobenius norm) of
+ * the formula's, before
  * its own rounding, for the coefficients above.  For binary16 results, and where the shorter side has at most 256, each product is made of three with
  * 22-bit operands: within 1e-4.
  * Errors: INVALID (a pointer NULL, strides, sizes < 0, types, eps negative or not finite, coefficients with which a singular value
