@@ -868,6 +868,13 @@ bool scan_pairs(const ScanView &v, int elem)
     return pointer_aligned(v.p, 2 * elem) && v.seq % 2 == 0 && v.step % 2 == 0 && v.step >> 32 == 0;
 }
 
+// The strides of what there is one of are free: they decide nothing.
+void scan_free_strides(ScanView &v, int64_t n, int64_t t)
+{
+    if (n == 1) v.seq = 0;
+    if (t == 1) v.step = 0;
+}
+
 bool scan_wide(const ScanView &v, int elem)
 {
     return pointer_aligned(v.p, 16) && v.seq * elem % 16 == 0 && v.step * elem % 16 == 0;
@@ -1043,6 +1050,7 @@ extern "C" int rsdgc_gated_scan_forward(const void *x_dev, int64_t x_seq, int64_
     p.width = (int)width;
     p.groups = scan_groups(width);
     p.runs = scan_runs(n_steps);
+    for (ScanView *v : {&p.x, &p.gate, &p.y}) scan_free_strides(*v, n_seq, n_steps);
     p.vec = scan_pairs(p.y, elem);
     p.wide = scan_wide(p.x, elem) && scan_wide(p.gate, elem);
     cudaStream_t s = (cudaStream_t)stream;
@@ -1109,6 +1117,7 @@ extern "C" int rsdgc_gated_scan_backward(const void *dy_dev, int64_t dy_seq, int
     p.groups = scan_groups(width);
     p.runs = scan_runs(n_steps);
     p.seq_parts = (int)scan_seq_parts(n_seq, width);
+    for (ScanView *v : {&p.x, &p.gate, &p.y, &p.dx, &p.dgate}) scan_free_strides(*v, n_seq, n_steps);
     p.vec = (!dx_dev || scan_pairs(p.dx, elem)) && (!dgate_dev || scan_pairs(p.dgate, elem));
     p.wide = scan_wide(p.x, elem) && scan_wide(p.gate, elem) && scan_wide(p.y, elem);
     cudaError_t e = operators_ready();

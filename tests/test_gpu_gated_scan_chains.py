@@ -93,3 +93,23 @@ def test_a_graph_gives_the_same_bits_as_calls(n, t, d):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, (y, dx, dgate, dbias)))
     assert binding.operator_status() == 0
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_strides_of_what_there_is_one_of(kind):
+    """A single sequence, and a single step of each, out of tensors whose other stride is odd."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    big = torch.randn(6 * 5 * 65 + 1, generator=gen, device="cuda").to(TYPES[kind])
+    whole = big[:6 * 5 * 64].view(6, 5, 64)
+    one = torch.as_strided(big, (1, 5, 64), (333, 64, 1))
+    last = torch.as_strided(big, (6, 1, 64), (320, 77, 1))
+    results = []
+    for x in (one, one.contiguous(), last, last.contiguous()):
+        y, states = torch.empty(x.shape, dtype=x.dtype, device="cuda"), torch.empty(binding.gated_scan_states_shape(*x.shape), device="cuda")
+        binding.gated_scan_forward(x, x, y, states=states)
+        dx, dgate = torch.empty_like(y), torch.empty_like(y)
+        binding.gated_scan_backward(x, x, x, states, dx, dgate)
+        results.append((y, dx, dgate))
+    for a, b in (results[:2], results[2:]):
+        assert all(torch.equal(u, v) for u, v in zip(a, b))
+    assert torch.equal(whole[:1], one) and binding.operator_status() == 0
