@@ -13,7 +13,7 @@
 //  - a CTA's W warps take a unit's runs in turn and hand the state on from warp to warp.  With W = 8 and 12 the critical path is not a run's 16
 //    steps but one step of its (L, Q), which the warp has formed beforehand: 4 x 8192 x 2048 bfloat16, 128 units: 115 us before, 74 us after;
 //  - few units: the CTAs of a cluster take W runs each side by side, tell one another what those do to a state, and each run starts from
-//    the state that follows (1 x 65536 x 1024 binary16: 469 us with one CTA a unit, 192 us with 7).
+//    the state that follows (1 x 65536 x 1024 binary16: 469 us with one CTA a unit, 180 us with 7).
 // Runs are joined in the order of time, whoever is first: results are the same bits from call to call.
 // Rows that do not start on 16-byte boundaries arrive in 16-byte pieces too, one more a row, and are shifted when they are read
 // (8 x 4096 x 2047 bfloat16: 129 us forward, 594 us with loads of single values).
@@ -66,6 +66,10 @@ struct ScanParams {
     int vec, wide;                  // results: pairs of channels may be written at once; operands: rows start on 16-byte boundaries
 };
 
+// The cluster's barrier in two halves: what lies between them needs nothing of the other CTAs (1 x 65536 x 2048 bfloat16: 287 us with the
+// copies' issue and the CTA's own joins before it, 256 us with them between)
+__device__ __forceinline__ void scan_cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void scan_cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void scan_store_in(uint32_t addr, uint32_t rank, float4 v)  // to a CTA of the cluster
 {
     asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr_in(addr, rank)), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
@@ -483,12 +487,12 @@ __global__ void __launch_bounds__(32 * W) k_scan_forward_split(const ScanParams 
     __shared__ float4 runs[2][W][32];              // by round: what each warp's run does
     __shared__ float4 parts[2][kScanCluster][32];  // ... and each CTA's W runs
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int cluster = p.cluster, rank = cluster > 1 ? (int)cluster_rank() : 0;
+    const int cluster = p.cluster, rank = (int)cluster_rank();
     const int unit = (int)blockIdx.x / cluster;
     grid_dependency_wait();
     grid_dependency_launch_next();
     const int seq = unit / p.groups, group = unit - seq * p.groups;
-    if (cluster > 1) cluster_sync_all();  // nothing is written to a CTA that has not begun
+    cluster_sync_all();  // nothing is written to a CTA that has not begun
     const ScanPlace at(p, group, lane);
     const float2 bias = at.bias(p);
     const int len = scan_length(p, seq), stride = W * kRun * cluster;
@@ -512,6 +516,11 @@ __global__ void __launch_bounds__(32 * W) k_scan_forward_split(const ScanParams 
     fetch(t);
     fetch(t + stride);
     bool starts = scan_restarts(p, seq, t, len, lane);
+    auto next_rows = [&] {  // into the places just read
+        __syncwarp();
+        fetch(t + 2 * stride);
+        starts = scan_restarts(p, seq, t + stride, len, lane);
+    };
     for (int t0 = 0; t0 < len; t0 += stride, t += stride, parity ^= 1) {
         typename Channels<T>::Raw x[kRun];
         float2 nb[kRun];
@@ -520,35 +529,33 @@ __global__ void __launch_bounds__(32 * W) k_scan_forward_split(const ScanParams 
         scan_gates(nb, ring, 1, bias, t, len);
 #pragma unroll
         for (int i = 0; i < kRun; ++i) x[i] = t < len ? ring.read(0, i) : Channels<T>::none();
-        __syncwarp();
-        fetch(t + 2 * stride);
-        starts = scan_restarts(p, seq, t + stride, len, lane);
         runs[parity][warp][lane] = scan_whole<T>(x, nb, restart);
         __syncthreads();
         float2 in = m;
-        if (cluster > 1) {
-            // warp k tells CTA k what this CTA's runs do
-            if (warp < cluster) {
-                float4 all = runs[parity][0][lane];
-                for (int w = 1; w < W; ++w) {
-                    const float4 o = runs[parity][w][lane];
-                    scan_join(all.x, all.z, o.x, o.z);
-                    scan_join(all.y, all.w, o.y, o.w);
-                }
-                for (int k = warp; k < cluster; k += W) scan_store_in(smem_addr(&parts[parity][rank][lane]), (uint32_t)k, all);
+        // warp k tells CTA k what this CTA's runs do
+        if (warp < cluster) {
+            float4 all = runs[parity][0][lane];
+            for (int w = 1; w < W; ++w) {
+                const float4 o = runs[parity][w][lane];
+                scan_join(all.x, all.z, o.x, o.z);
+                scan_join(all.y, all.w, o.y, o.w);
             }
-            cluster_sync_all();
-            for (int k = 0; k < cluster; ++k) {
-                if (k == rank) in = m;
-                m = scan_apply(parts[parity][k][lane], m);
-            }
-            for (int w = 0; w < warp; ++w) in = scan_apply(runs[parity][w][lane], in);
-        } else {
-            for (int w = 0; w < W; ++w) {
-                if (w == warp) in = m;
-                m = scan_apply(runs[parity][w][lane], m);
-            }
+            for (int k = warp; k < cluster; k += W) scan_store_in(smem_addr(&parts[parity][rank][lane]), (uint32_t)k, all);
         }
+        scan_cluster_arrive();
+        next_rows();
+        float4 before = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // what this CTA's runs before this one do
+        for (int w = 0; w < warp; ++w) {
+            const float4 o = runs[parity][w][lane];
+            scan_join(before.x, before.z, o.x, o.z);
+            scan_join(before.y, before.w, o.y, o.w);
+        }
+        scan_cluster_wait();
+        for (int k = 0; k < cluster; ++k) {
+            if (k == rank) in = m;
+            m = scan_apply(parts[parity][k][lane], m);
+        }
+        in = scan_apply(before, in);
         if (t >= len) continue;
         scan_save(p, seq, at, t, in);
         scan_steps<T>(x, nb, in, restart);
@@ -588,9 +595,8 @@ struct ScanBack {
         if (t >= 0 && t < len && RSDGC_IN_BOUNDS(t / kRun < p.runs && seq < p.n_seq))
             from = scan_load2(p.states + ((long long)seq * p.runs + t / kRun) * p.width + at.c, at.n);
     }
-    // the run's -b, x and dy; the place is filled again with the run after the next
-    __device__ __forceinline__ void take(float2 (&nb)[kRun], Raw (&x)[kRun], Raw (&dy)[kRun], float2 bias, const ScanParams &p,
-                                         int seq, const ScanPlace &at, int t, int len, int ahead)
+    // the run's -b, x and dy
+    __device__ __forceinline__ void take(float2 (&nb)[kRun], Raw (&x)[kRun], Raw (&dy)[kRun], float2 bias, const ScanParams &p, int t, int len)
     {
         const bool there = t >= 0 && t < len;
         ring.wait();
@@ -600,6 +606,10 @@ struct ScanBack {
             x[i] = there ? ring.read(0, i) : Channels<T>::none();
             dy[i] = there ? ring.read(2, i) : Channels<T>::none();
         }
+    }
+    // ... whose place is filled with the run after the next
+    __device__ __forceinline__ void refill(const ScanParams &p, int seq, const ScanPlace &at, int t, int len, int ahead)
+    {
         __syncwarp();
         rows(p, seq, at, t - 2 * ahead, len);
     }
@@ -706,7 +716,8 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W, scan_ba
             float2 nb[kRun], u[kRun], add;
             const uint32_t restart = __ballot_sync(0xFFFFFFFFu, next.starts);
             const float2 from = next.from;
-            next.take(nb, x, dy, bias, p, seq, at, t, len, W * kRun);
+            next.take(nb, x, dy, bias, p, t, len);
+            next.refill(p, seq, at, t, len, W * kRun);
             next.state(p, seq, at, t - W * kRun, len, lane);
             scan_again<T>(u, x, nb, from, restart);
             if constexpr (ahead) whole[warp][lane] = scan_back_whole<T>(dy, nb, restart);
@@ -736,12 +747,12 @@ __global__ void __launch_bounds__(32 * W) k_scan_backward_split(const ScanParams
     __shared__ float4 runs[2][W][32];              // (R, P) of the two channels
     __shared__ float4 parts[2][kScanCluster][32];  // ... of a CTA's W runs
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int cluster = p.cluster, rank = cluster > 1 ? (int)cluster_rank() : 0;
+    const int cluster = p.cluster, rank = (int)cluster_rank();
     const int unit = (int)blockIdx.x / cluster;
     grid_dependency_wait();
     grid_dependency_launch_next();
     const int part = unit / p.groups, group = unit - part * p.groups;
-    if (cluster > 1) cluster_sync_all();  // nothing is written to a CTA that has not begun
+    cluster_sync_all();  // nothing is written to a CTA that has not begun
     const ScanPlace at(p, group, lane);
     const float2 bias = at.bias(p);
     constexpr int tile = W * kRun;
@@ -763,34 +774,35 @@ __global__ void __launch_bounds__(32 * W) k_scan_backward_split(const ScanParams
             float2 nb[kRun], u[kRun], add;
             const uint32_t restart = __ballot_sync(0xFFFFFFFFu, next.starts);
             const float2 from = next.from;
-            next.take(nb, x, dy, bias, p, seq, at, t, len, tile * cluster);
-            next.state(p, seq, at, t - tile * cluster, len, lane);
+            next.take(nb, x, dy, bias, p, t, len);
             runs[parity][warp][lane] = scan_back_whole<T>(dy, nb, restart);
             __syncthreads();
             float2 in = e;
-            if (cluster > 1) {
-                if (warp < cluster) {
-                    float2 all = make_float2(0.0f, 0.0f), k = make_float2(1.0f, 1.0f);
-                    for (int w = W - 1; w >= 0; --w) {
-                        const float4 o = runs[parity][w][lane];
-                        all = scan_back(o, all);
-                        k = make_float2(scan_through(k.x, o.z), scan_through(k.y, o.w));
-                    }
-                    for (int to = warp; to < cluster; to += W)
-                        scan_store_in(smem_addr(&parts[parity][rank][lane]), (uint32_t)to, make_float4(all.x, all.y, k.x, k.y));
-                }
-                cluster_sync_all();
-                for (int k = 0; k < cluster; ++k) {
-                    if (k == rank) in = e;
-                    e = scan_back(parts[parity][k][lane], e);
-                }
-                for (int w = W - 1; w > warp; --w) in = scan_back(runs[parity][w][lane], in);
-            } else {
+            if (warp < cluster) {
+                float2 all = make_float2(0.0f, 0.0f), k = make_float2(1.0f, 1.0f);
                 for (int w = W - 1; w >= 0; --w) {
-                    if (w == warp) in = e;
-                    e = scan_back(runs[parity][w][lane], e);
+                    const float4 o = runs[parity][w][lane];
+                    all = scan_back(o, all);
+                    k = make_float2(scan_through(k.x, o.z), scan_through(k.y, o.w));
                 }
+                for (int to = warp; to < cluster; to += W)
+                    scan_store_in(smem_addr(&parts[parity][rank][lane]), (uint32_t)to, make_float4(all.x, all.y, k.x, k.y));
             }
+            scan_cluster_arrive();
+            next.refill(p, seq, at, t, len, tile * cluster);
+            next.state(p, seq, at, t - tile * cluster, len, lane);
+            float4 behind = make_float4(0.0f, 0.0f, 1.0f, 1.0f);  // what this CTA's runs behind this one do
+            for (int w = W - 1; w > warp; --w) {
+                const float4 o = runs[parity][w][lane];
+                const float2 r = scan_back(o, make_float2(behind.x, behind.y));
+                behind = make_float4(r.x, r.y, scan_through(behind.z, o.z), scan_through(behind.w, o.w));
+            }
+            scan_cluster_wait();
+            for (int k = 0; k < cluster; ++k) {
+                if (k == rank) in = e;
+                e = scan_back(parts[parity][k][lane], e);
+            }
+            in = scan_back(behind, in);
             if (t < 0 || t >= len) continue;
             scan_again<T>(u, x, nb, from, restart);
             scan_deltas<T>(dy, x, u, nb, in, add, restart);
