@@ -4,8 +4,9 @@
 //   delta_t = dy_t + a_{t+1} delta_{t+1},  dx_t = b_t delta_t,  dgate_t = delta_t a_t b_t (h_{t-1} - x_t)
 //
 // The step is affine in the state, and so is a run of steps: h -> h + (L - Q h) with Q = 1 - (product of a), which is how runs are
-// computed side by side and joined.  b is formed as a value of its own and the state as h + b (x - h), so that a slow
-// channel (b of 1e-5) keeps its digits, which a, next to 1, would round away.
+// computed side by side and joined.  Of a and b the smaller one is formed to its own digits, and a step adds it, times a difference, to what it
+// is near to: h + b (x - h) where the gate is open, x + a (h - x) where it is nearly closed.  A slow channel (b of 1e-5) keeps its digits,
+// which a, next to 1, would round away, and so does what a closed gate (a of 1e-6) lets through of the state and of the gradient.
 //
 // A warp takes 64 channels (two a lane) and runs of 16 steps; the next two runs' rows are on their way through its own ring in shared
 // memory while a run is computed.  Three ways to deal the runs, by how many (sequence, 64 channels) units there are:
@@ -23,6 +24,7 @@
 #include <atomic>
 #include <climits>
 #include <mutex>
+#include <type_traits>
 
 #include "device_utils.cuh"
 #include "operators_internal.cuh"
@@ -87,6 +89,15 @@ struct Channels {
         return make_float2(to_f32(v[0]), to_f32(v[1]));
     }
     static __device__ __forceinline__ Raw narrow(float2 v) { return pack2<T>(v.x, v.y); }
+    static __device__ __forceinline__ Raw least(Raw a, Raw b)  // of each channel; NaN only of two
+    {
+        Raw r;
+        if constexpr (std::is_same_v<T, __half>)
+            asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        else
+            asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
     static __device__ __forceinline__ void store(T *p, bool pair, int n, Raw r)
     {
         if (pair) {
@@ -104,6 +115,7 @@ struct Channels<float> {
     static __device__ __forceinline__ Raw none() { return make_float2(0.0f, 0.0f); }
     static __device__ __forceinline__ float2 widen(Raw r) { return r; }
     static __device__ __forceinline__ Raw narrow(float2 v) { return v; }
+    static __device__ __forceinline__ Raw least(Raw a, Raw b) { return make_float2(fminf(a.x, b.x), fminf(a.y, b.y)); }
     static __device__ __forceinline__ void store(float *p, bool pair, int n, Raw v)
     {
         if (pair) {
@@ -125,13 +137,43 @@ __device__ __forceinline__ void scan_store2(float *p, int n, float2 v)
     if (n > 1) p[1] = v.y;
 }
 
-// -b = -1 / (1 + exp(z)) for z log2(e) = u.  It never leaves [-1, 0], whatever u is; NaN stays NaN.
+// A step's coefficient c, from u = z log2(e), by whether some gate of the warp's run is nearly closed (u < kScanShut, a < 1/33).  Where none
+// is (SHUT false), c = -b = -1 / (1 + exp(z)), and 1 - b has a to 2^-17 of itself.  Where one is, the smaller one of a and b, to its own digits,
+// and which one its sign bit tells: -b where the gate is open (z > 0), a = exp(z) / (1 + exp(z)) where it is not.  That costs a selection a channel
+// in each use: with selections in every run 4 x 8192 x 2048 bfloat16 takes 104 us, 80 us so, backward 213 and 136 us.  c never leaves
+// [-1, 1/2], whatever u is; NaN stays NaN.
+constexpr float kScanShut = -5.0f;
+constexpr float kScanStays = -0.0f;  // the coefficient of a step that does not exist: b = 0
+template <bool SHUT>
 __device__ __forceinline__ float scan_gate(float u)
 {
-    float e, nb;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(nb) : "f"(-1.0f - e));
-    return nb;
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(SHUT ? -fabsf(u) : u));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(SHUT ? 1.0f + e : -1.0f - e));
+    return SHUT ? __uint_as_float(__float_as_uint(e * r) | (~__float_as_uint(u) & 0x80000000u)) : r;
+}
+__device__ __forceinline__ float2 scan_by_gate(float2 c, float2 open, float2 closed)
+{
+    return make_float2(__float_as_int(c.x) < 0 ? open.x : closed.x, __float_as_int(c.y) < 0 ? open.y : closed.y);
+}
+// The step from the negated state m; u = x - h, the state before it
+template <bool SHUT>
+__device__ __forceinline__ float2 scan_step(float2 c, float2 x, float2 m, float2 &u)
+{
+    u = add2(x, m);
+    return fma2(c, u, SHUT ? scan_by_gate(c, m, make_float2(-x.x, -x.y)) : m);
+}
+// a v
+template <bool SHUT>
+__device__ __forceinline__ float2 scan_keep(float2 c, float2 v)
+{
+    return fma2(c, v, SHUT ? scan_by_gate(c, v, make_float2(0.0f, 0.0f)) : v);
+}
+// -b
+template <bool SHUT>
+__device__ __forceinline__ float2 scan_take(float2 c)
+{
+    return SHUT ? add2(c, scan_by_gate(c, make_float2(0.0f, 0.0f), make_float2(-1.0f, -1.0f))) : c;
 }
 
 // What a run does to the (negated) state that comes into it: m -> m + (L - Q m).  Q = kScanCut: the state does not come through.
@@ -351,58 +393,67 @@ __device__ __forceinline__ bool scan_restarts(const ScanParams &p, int seq, int 
     return p.restart && lane < kRun && t + lane >= 0 && t + lane < len && p.restart[seq * p.restart_stride + t + lane] != 0;
 }
 
-// -b of a run's steps; steps that do not exist leave the state as it is
-template <typename T, int OPS, bool SHIFT>
-__device__ __forceinline__ void scan_gates(float2 (&nb)[kRun], const ScanRing<T, OPS, SHIFT> &ring, int op, float2 bias, int t, int len)
+// The coefficients of a run's steps; steps that do not exist leave the state as it is.  Returns, the same for the whole warp, whether a gate of
+// the run is nearly closed.
+template <bool SHUT, typename T, int OPS, bool SHIFT>
+__device__ __forceinline__ bool scan_gates(float2 (&c)[kRun], const ScanRing<T, OPS, SHIFT> &ring, int op, float2 bias, int t, int len)
 {
     const float2 scale = make_float2(kScanLog2e, kScanLog2e);
+    typename Channels<T>::Raw least;
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
-        const float2 u = fma2(Channels<T>::widen(ring.read(op, i)), scale, bias);
-        nb[i] = make_float2(scan_gate(u.x), scan_gate(u.y));
+        const typename Channels<T>::Raw gate = ring.read(op, i);
+        const float2 u = fma2(Channels<T>::widen(gate), scale, bias);
+        c[i] = make_float2(scan_gate<SHUT>(u.x), scan_gate<SHUT>(u.y));
+        least = i ? Channels<T>::least(least, gate) : gate;
     }
     if (t < 0 || t + kRun > len) {
 #pragma unroll
         for (int i = 0; i < kRun; ++i)
-            if (t + i < 0 || t + i >= len) nb[i] = make_float2(0.0f, 0.0f);
+            if (t + i < 0 || t + i >= len) c[i] = make_float2(kScanStays, kScanStays);
     }
+    const float2 low = fma2(Channels<T>::widen(least), scale, bias);
+    return SHUT || __any_sync(0xFFFFFFFFu, fminf(low.x, low.y) < kScanShut);
 }
 // The run from the negated state m; y = -m, in the operand's type, replaces each step's x
-template <typename T>
-__device__ __forceinline__ void scan_steps(typename Channels<T>::Raw (&x)[kRun], const float2 (&nb)[kRun], float2 &m, uint32_t restart)
+template <bool SHUT, typename T>
+__device__ __forceinline__ void scan_steps(typename Channels<T>::Raw (&x)[kRun], const float2 (&c)[kRun], float2 &m, uint32_t restart)
 {
-    if (!restart) {
+    float2 u;
+    if (!SHUT && !restart) {
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-            m = fma2(nb[i], add2(Channels<T>::widen(x[i]), m), m);
+            m = scan_step<SHUT>(c[i], Channels<T>::widen(x[i]), m, u);
             x[i] = Channels<T>::narrow(make_float2(-m.x, -m.y));
         }
     } else {
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
             if (restart >> i & 1) m = make_float2(0.0f, 0.0f);
-            m = fma2(nb[i], add2(Channels<T>::widen(x[i]), m), m);
+            m = scan_step<SHUT>(c[i], Channels<T>::widen(x[i]), m, u);
             x[i] = Channels<T>::narrow(make_float2(-m.x, -m.y));
         }
     }
 }
 // What the run does to a state
-template <typename T>
-__device__ __forceinline__ float4 scan_whole(const typename Channels<T>::Raw (&x)[kRun], const float2 (&nb)[kRun], uint32_t restart)
+template <bool SHUT, typename T>
+__device__ __forceinline__ float4 scan_whole(const typename Channels<T>::Raw (&x)[kRun], const float2 (&c)[kRun], uint32_t restart)
 {
-    float2 l = make_float2(0.0f, 0.0f), nq = l, r = make_float2(1.0f, 1.0f);  // r = 1 - q, of its own digits
+    float2 l = make_float2(0.0f, 0.0f), nq = l, r = make_float2(1.0f, 1.0f), u;
     if (!restart) {
+        // r = 1 - q, of its own digits; so is q while all gates are open, and where one is not, r is at most 1/2
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-            l = fma2(nb[i], add2(Channels<T>::widen(x[i]), l), l);
-            nq = fma2(nb[i], r, nq);
-            r = fma2(nb[i], r, r);
+            l = scan_step<SHUT>(c[i], Channels<T>::widen(x[i]), l, u);
+            nq = fma2(c[i], r, nq);
+            r = scan_keep<SHUT>(c[i], r);
         }
+        nq = make_float2(r.x > 0.5f ? nq.x : r.x - 1.0f, r.y > 0.5f ? nq.y : r.y - 1.0f);
     } else {
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
             if (restart >> i & 1) l = make_float2(0.0f, 0.0f);
-            l = fma2(nb[i], add2(Channels<T>::widen(x[i]), l), l);
+            l = scan_step<SHUT>(c[i], Channels<T>::widen(x[i]), l, u);
         }
         nq = make_float2(-kScanCut, -kScanCut);
     }
@@ -455,26 +506,34 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W, scan_fo
     bool starts = scan_restarts(p, seq, t, len, lane);
     for (; t < len; t += W * kRun) {
         typename Channels<T>::Raw x[kRun];
-        float2 nb[kRun];
+        float2 c[kRun];
         const uint32_t restart = __ballot_sync(0xFFFFFFFFu, starts);
         ring.wait();
-        scan_gates(nb, ring, 1, bias, t, len);
+        const bool shut = scan_gates<false>(c, ring, 1, bias, t, len);
+        if (shut) scan_gates<true>(c, ring, 1, bias, t, len);
 #pragma unroll
         for (int i = 0; i < kRun; ++i) x[i] = ring.read(0, i);
         __syncwarp();
         fetch(t + 2 * W * kRun);
         starts = scan_restarts(p, seq, t + W * kRun, len, lane);
-        if constexpr (ahead) whole[warp][lane] = scan_whole<T>(x, nb, restart);
-        if (W > 1 && t > 0) m = scan_take_over<W>(&place[0][0], warp, lane);
-        if constexpr (ahead)
-            if (t + kRun < len) scan_hand_on<W>(&place[0][0], warp + 1 < W ? warp + 1 : 0, lane, scan_apply(whole[warp][lane], m));
-        scan_save(p, seq, at, t, m);
-        scan_steps<T>(x, nb, m, restart);
-        if (t + kRun >= len) {
-            if (p.last) scan_store2(p.last + (long long)seq * p.width + at.c, at.n, make_float2(-m.x, -m.y));
-        } else if (W > 1 && !ahead) {
-            scan_hand_on<W>(&place[0][0], warp + 1 < W ? warp + 1 : 0, lane, m);
-        }
+        auto walk = [&](auto is_shut) {
+            constexpr bool SHUT = decltype(is_shut)::value;
+            if constexpr (ahead) whole[warp][lane] = scan_whole<SHUT, T>(x, c, restart);
+            if (W > 1 && t > 0) m = scan_take_over<W>(&place[0][0], warp, lane);
+            if constexpr (ahead)
+                if (t + kRun < len) scan_hand_on<W>(&place[0][0], warp + 1 < W ? warp + 1 : 0, lane, scan_apply(whole[warp][lane], m));
+            scan_save(p, seq, at, t, m);
+            scan_steps<SHUT, T>(x, c, m, restart);
+            if (t + kRun >= len) {
+                if (p.last) scan_store2(p.last + (long long)seq * p.width + at.c, at.n, make_float2(-m.x, -m.y));
+            } else if (W > 1 && !ahead) {
+                scan_hand_on<W>(&place[0][0], warp + 1 < W ? warp + 1 : 0, lane, m);
+            }
+        };
+        if (shut)
+            walk(std::true_type());
+        else
+            walk(std::false_type());
         scan_write<T>(x, p, p.y, seq, at, t, len);
     }
 }
@@ -523,13 +582,14 @@ __global__ void __launch_bounds__(32 * W) k_scan_forward_split(const ScanParams 
     };
     for (int t0 = 0; t0 < len; t0 += stride, t += stride, parity ^= 1) {
         typename Channels<T>::Raw x[kRun];
-        float2 nb[kRun];
+        float2 c[kRun];
         const uint32_t restart = __ballot_sync(0xFFFFFFFFu, starts);
         ring.wait();
-        scan_gates(nb, ring, 1, bias, t, len);
+        const bool shut = scan_gates<false>(c, ring, 1, bias, t, len);
+        if (shut) scan_gates<true>(c, ring, 1, bias, t, len);
 #pragma unroll
         for (int i = 0; i < kRun; ++i) x[i] = t < len ? ring.read(0, i) : Channels<T>::none();
-        runs[parity][warp][lane] = scan_whole<T>(x, nb, restart);
+        runs[parity][warp][lane] = shut ? scan_whole<true, T>(x, c, restart) : scan_whole<false, T>(x, c, restart);
         __syncthreads();
         float2 in = m;
         // warp k tells CTA k what this CTA's runs do
@@ -558,7 +618,7 @@ __global__ void __launch_bounds__(32 * W) k_scan_forward_split(const ScanParams 
         in = scan_apply(before, in);
         if (t >= len) continue;
         scan_save(p, seq, at, t, in);
-        scan_steps<T>(x, nb, in, restart);
+        shut ? scan_steps<true, T>(x, c, in, restart) : scan_steps<false, T>(x, c, in, restart);
         scan_write<T>(x, p, p.y, seq, at, t, len);
     }
     if (p.last && rank == 0 && warp == 0)
@@ -595,17 +655,23 @@ struct ScanBack {
         if (t >= 0 && t < len && RSDGC_IN_BOUNDS(t / kRun < p.runs && seq < p.n_seq))
             from = scan_load2(p.states + ((long long)seq * p.runs + t / kRun) * p.width + at.c, at.n);
     }
-    // the run's -b, x and dy
-    __device__ __forceinline__ void take(float2 (&nb)[kRun], Raw (&x)[kRun], Raw (&dy)[kRun], float2 bias, const ScanParams &p, int t, int len)
+    // the run's x and dy
+    __device__ __forceinline__ void operands(Raw (&x)[kRun], Raw (&dy)[kRun], int t, int len) const
     {
         const bool there = t >= 0 && t < len;
-        ring.wait();
-        scan_gates(nb, ring, 1, bias, t, len);
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
             x[i] = there ? ring.read(0, i) : Channels<T>::none();
             dy[i] = there ? ring.read(2, i) : Channels<T>::none();
         }
+    }
+    // ... and its coefficients; returns whether a gate is nearly closed
+    __device__ __forceinline__ bool take(float2 (&c)[kRun], Raw (&x)[kRun], Raw (&dy)[kRun], float2 bias, int t, int len) const
+    {
+        ring.wait();
+        const bool shut = scan_gates<false>(c, ring, 1, bias, t, len);
+        operands(x, dy, t, len);
+        return shut;
     }
     // ... whose place is filled with the run after the next
     __device__ __forceinline__ void refill(const ScanParams &p, int seq, const ScanPlace &at, int t, int len, int ahead)
@@ -615,46 +681,44 @@ struct ScanBack {
     }
 };
 // What the run does to the gradient that comes into it from behind
-template <typename T>
-__device__ __forceinline__ float4 scan_back_whole(const typename Channels<T>::Raw (&dy)[kRun], const float2 (&nb)[kRun], uint32_t restart)
+template <bool SHUT, typename T>
+__device__ __forceinline__ float4 scan_back_whole(const typename Channels<T>::Raw (&dy)[kRun], const float2 (&c)[kRun], uint32_t restart)
 {
     float2 r = make_float2(0.0f, 0.0f), q = make_float2(1.0f, 1.0f);
 #pragma unroll
     for (int i = kRun - 1; i >= 0; --i) {
-        const float2 d = add2(Channels<T>::widen(dy[i]), r);
-        r = fma2(nb[i], d, d);
-        q = fma2(nb[i], q, q);
+        r = scan_keep<SHUT>(c[i], add2(Channels<T>::widen(dy[i]), r));
+        q = scan_keep<SHUT>(c[i], q);
         if (restart >> i & 1) r = make_float2(0.0f, 0.0f);
     }
     q = restart ? make_float2(0.0f, 0.0f) : make_float2(fmaxf(q.x, kScanLeast), fmaxf(q.y, kScanLeast));
     return make_float4(r.x, r.y, q.x, q.y);
 }
 // u_t = x_t - h_{t-1}, from the state before the run
-template <typename T>
-__device__ __forceinline__ void scan_again(float2 (&u)[kRun], const typename Channels<T>::Raw (&x)[kRun], const float2 (&nb)[kRun],
+template <bool SHUT, typename T>
+__device__ __forceinline__ void scan_again(float2 (&u)[kRun], const typename Channels<T>::Raw (&x)[kRun], const float2 (&c)[kRun],
                                            float2 from, uint32_t restart)
 {
     float2 m = make_float2(-from.x, -from.y);
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
         if (restart >> i & 1) m = make_float2(0.0f, 0.0f);
-        u[i] = add2(Channels<T>::widen(x[i]), m);
-        m = fma2(nb[i], u[i], m);
+        m = scan_step<SHUT>(c[i], Channels<T>::widen(x[i]), m, u[i]);
     }
 }
 // From the last step to the first: delta, dx, dgate (into dy's and x's places) and dgate's sum.  e: the gradient from behind, and at the
 // end the one that goes on.
-template <typename T>
+template <bool SHUT, typename T>
 __device__ __forceinline__ void scan_deltas(typename Channels<T>::Raw (&dy)[kRun], typename Channels<T>::Raw (&x)[kRun],
-                                            const float2 (&u)[kRun], const float2 (&nb)[kRun], float2 &e, float2 &add, uint32_t restart)
+                                            const float2 (&u)[kRun], const float2 (&c)[kRun], float2 &e, float2 &add, uint32_t restart)
 {
     add = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int i = kRun - 1; i >= 0; --i) {
-        const float2 d = add2(Channels<T>::widen(dy[i]), e);
-        e = fma2(nb[i], d, d);                             // a delta
-        const float2 z = mul2(mul2(e, nb[i]), u[i]);       // a delta (-b) (x - h)
-        const float2 ndx = mul2(nb[i], d);
+        const float2 d = add2(Channels<T>::widen(dy[i]), e), nb = scan_take<SHUT>(c[i]);
+        e = scan_keep<SHUT>(c[i], d);              // a delta
+        const float2 z = mul2(mul2(e, nb), u[i]);  // a delta (-b) (x - h)
+        const float2 ndx = mul2(nb, d);
         dy[i] = Channels<T>::narrow(make_float2(-ndx.x, -ndx.y));
         x[i] = Channels<T>::narrow(z);
         add = add2(add, z);
@@ -713,18 +777,31 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W, scan_ba
         next.state(p, seq, at, t, len, lane);
         for (; t >= 0; t -= W * kRun) {
             typename Channels<T>::Raw x[kRun], dy[kRun];
-            float2 nb[kRun], u[kRun], add;
+            float2 c[kRun], u[kRun], add;
             const uint32_t restart = __ballot_sync(0xFFFFFFFFu, next.starts);
             const float2 from = next.from;
-            next.take(nb, x, dy, bias, p, t, len);
-            next.refill(p, seq, at, t, len, W * kRun);
+            const bool shut = next.take(c, x, dy, bias, t, len);
+            if (!shut) next.refill(p, seq, at, t, len, W * kRun);
             next.state(p, seq, at, t - W * kRun, len, lane);
-            scan_again<T>(u, x, nb, from, restart);
-            if constexpr (ahead) whole[warp][lane] = scan_back_whole<T>(dy, nb, restart);
+            // a run with a nearly closed gate is computed again, with selections, and its rows stay until then
+            scan_again<false, T>(u, x, c, from, restart);
+            if constexpr (ahead) whole[warp][lane] = scan_back_whole<false, T>(dy, c, restart);
+            if (shut) {
+                scan_gates<true>(c, next.ring, 1, bias, t, len);
+                scan_again<true, T>(u, x, c, from, restart);
+                if constexpr (ahead) whole[warp][lane] = scan_back_whole<true, T>(dy, c, restart);
+            }
             if (W > 1 && t + kRun < len) e = scan_take_over<W>(&place[0][0], warp, lane);
             if constexpr (ahead)
                 if (t > 0) scan_hand_on<W>(&place[0][0], warp + 1 < W ? warp + 1 : 0, lane, scan_back(whole[warp][lane], e));
-            scan_deltas<T>(dy, x, u, nb, e, add, restart);
+            const float2 behind = e;
+            scan_deltas<false, T>(dy, x, u, c, e, add, restart);
+            if (shut) {
+                next.operands(x, dy, t, len);
+                e = behind;
+                scan_deltas<true, T>(dy, x, u, c, e, add, restart);
+                next.refill(p, seq, at, t, len, W * kRun);
+            }
             if (t == 0) {
                 if (p.last) scan_store2(p.last + (long long)seq * p.width + at.c, at.n, e);
             } else if (W > 1 && !ahead) {
@@ -771,11 +848,12 @@ __global__ void __launch_bounds__(32 * W) k_scan_backward_split(const ScanParams
         next.state(p, seq, at, t, len, lane);
         for (int left = tiles; left > 0; left -= cluster, t -= tile * cluster, parity ^= 1) {
             typename Channels<T>::Raw x[kRun], dy[kRun];
-            float2 nb[kRun], u[kRun], add;
+            float2 c[kRun], u[kRun], add;
             const uint32_t restart = __ballot_sync(0xFFFFFFFFu, next.starts);
             const float2 from = next.from;
-            next.take(nb, x, dy, bias, p, t, len);
-            runs[parity][warp][lane] = scan_back_whole<T>(dy, nb, restart);
+            const bool shut = next.take(c, x, dy, bias, t, len);
+            if (shut) scan_gates<true>(c, next.ring, 1, bias, t, len);
+            runs[parity][warp][lane] = shut ? scan_back_whole<true, T>(dy, c, restart) : scan_back_whole<false, T>(dy, c, restart);
             __syncthreads();
             float2 in = e;
             if (warp < cluster) {
@@ -804,8 +882,8 @@ __global__ void __launch_bounds__(32 * W) k_scan_backward_split(const ScanParams
             }
             in = scan_back(behind, in);
             if (t < 0 || t >= len) continue;
-            scan_again<T>(u, x, nb, from, restart);
-            scan_deltas<T>(dy, x, u, nb, in, add, restart);
+            shut ? scan_again<true, T>(u, x, c, from, restart) : scan_again<false, T>(u, x, c, from, restart);
+            shut ? scan_deltas<true, T>(dy, x, u, c, in, add, restart) : scan_deltas<false, T>(dy, x, u, c, in, add, restart);
             if (p.dx.p) scan_write<T>(dy, p, p.dx, seq, at, t, len);
             if (p.dgate.p) scan_write<T>(x, p, p.dgate, seq, at, t, len);
             scan_sum(sum, rest, add);
