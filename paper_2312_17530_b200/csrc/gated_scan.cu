@@ -3,7 +3,7 @@
 //   a_t = 1 / (1 + exp(-(gate_t + bias))),  b_t = 1 - a_t,  h_t = a_t h_{t-1} + b_t x_t,  y_t = h_t
 //   delta_t = dy_t + a_{t+1} delta_{t+1},  dx_t = b_t delta_t,  dgate_t = delta_t a_t b_t (h_{t-1} - x_t)
 //
-// The step is affine in the state, and so is a run of steps: h -> h + (L - Q h) with Q = 1 - (product of a), which is how runs are
+// The step is affine in the state, and so is a run of steps: h -> L + P h = h + (L - Q h), P the product of its a, Q = 1 - P, which is how runs are
 // computed side by side and joined.  Of a and b the smaller one is formed to its own digits, and a step adds it, times a difference, to what it
 // is near to: h + b (x - h) where the gate is open, x + a (h - x) where it is nearly closed.  A slow channel (b of 1e-5) keeps its digits,
 // which a, next to 1, would round away, and so does what a closed gate (a of 1e-6) lets through of the state and of the gradient.
@@ -137,6 +137,8 @@ __device__ __forceinline__ void scan_store2(float *p, int n, float2 v)
     if (n > 1) p[1] = v.y;
 }
 
+__device__ __forceinline__ bool scan_negative(float v) { return __float_as_int(v) < 0; }  // by the sign bit
+
 // A step's coefficient c, from u = z log2(e), by whether some gate of the warp's run is nearly closed (u < kScanShut, a < 1/33).  Where none
 // is (SHUT false), c = -b = -1 / (1 + exp(z)), and 1 - b has a to 2^-17 of itself.  Where one is, the smaller one of a and b, to its own digits,
 // and which one its sign bit tells: -b where the gate is open (z > 0), a = exp(z) / (1 + exp(z)) where it is not.  That costs a selection a channel
@@ -154,7 +156,7 @@ __device__ __forceinline__ float scan_gate(float u)
 }
 __device__ __forceinline__ float2 scan_by_gate(float2 c, float2 open, float2 closed)
 {
-    return make_float2(__float_as_int(c.x) < 0 ? open.x : closed.x, __float_as_int(c.y) < 0 ? open.y : closed.y);
+    return make_float2(scan_negative(c.x) ? open.x : closed.x, scan_negative(c.y) ? open.y : closed.y);
 }
 // The step from the negated state m; u = x - h, the state before it
 template <bool SHUT>
@@ -176,20 +178,33 @@ __device__ __forceinline__ float2 scan_take(float2 c)
     return SHUT ? add2(c, scan_by_gate(c, make_float2(0.0f, 0.0f), make_float2(-1.0f, -1.0f))) : c;
 }
 
-// What a run does to the (negated) state that comes into it: m -> m + (L - Q m).  Q = kScanCut: the state does not come through.
+// What a run does to the (negated) state that comes into it, as (L, S): m -> m + (L - Q m) with S = Q where Q is at most 1/2, m -> L + P m with S = -P
+// (sign bit set) where P = 1 - Q is: of P and Q the smaller one, to its own digits.  So neither a slow channel's state nor what is left behind
+// a large one is rounded away (a token of 1e6 among ordinary ones left 6 % of a unit with Q alone).  S = kScanCut: the state does not come through.
 constexpr float kScanCut = 2.0f;
-__device__ __forceinline__ float scan_apply(float l, float q, float m) { return q == kScanCut ? l : m + (l - q * m); }
+__device__ __forceinline__ float scan_apply(float l, float s, float m)
+{
+    return s == kScanCut ? l : (scan_negative(s) ? 0.0f : m) + fmaf(-s, m, l);
+}
 __device__ __forceinline__ float2 scan_apply(float4 r, float2 m)
 {
     return make_float2(scan_apply(r.x, r.z, m.x), scan_apply(r.y, r.w, m.y));
 }
-// ... and two runs, the second one behind the first
-__device__ __forceinline__ void scan_join(float &l, float &q, float l2, float q2)
-{
-    const bool cut = q == kScanCut || q2 == kScanCut;
-    l = scan_apply(l2, q2, l);
-    q = cut ? kScanCut : q + q2 * (1.0f - q);
-}
+// ... as it is formed: m -> L + P m.  P's sign bit: the state does not come through.  Q has its own digits where P is above 1/2.
+struct ScanRun {
+    float2 l, p, q;
+    static __device__ __forceinline__ float which(float p, float q) { return scan_negative(p) ? kScanCut : p > 0.5f ? q : -p; }
+    __device__ __forceinline__ float4 packed() const { return make_float4(l.x, l.y, which(p.x, q.x), which(p.y, q.y)); }
+    // This run and one behind it.  L + P L' will do: what it rounds away is not carried on beyond the joined runs.
+    __device__ __forceinline__ void join(const ScanRun &r)
+    {
+        l = fma2(r.p, l, r.l);
+        if (scan_negative(r.p.x)) l.x = r.l.x;
+        if (scan_negative(r.p.y)) l.y = r.l.y;
+        q = fma2(r.q, p, q);
+        p = mul2(p, r.p);
+    }
+};
 // The same of the gradient: e -> R + P e.  P = 0: it does not come through; a product too small for a number is not yet a cut.
 __device__ __forceinline__ float2 scan_back(float4 r, float2 e)
 {
@@ -437,27 +452,26 @@ __device__ __forceinline__ void scan_steps(typename Channels<T>::Raw (&x)[kRun],
 }
 // What the run does to a state
 template <bool SHUT, typename T>
-__device__ __forceinline__ float4 scan_whole(const typename Channels<T>::Raw (&x)[kRun], const float2 (&c)[kRun], uint32_t restart)
+__device__ __forceinline__ ScanRun scan_whole(const typename Channels<T>::Raw (&x)[kRun], const float2 (&c)[kRun], uint32_t restart)
 {
-    float2 l = make_float2(0.0f, 0.0f), nq = l, r = make_float2(1.0f, 1.0f), u;
+    float2 l = make_float2(0.0f, 0.0f), p = make_float2(-0.0f, -0.0f), nq = p, u;
     if (!restart) {
-        // r = 1 - q, of its own digits; so is q while all gates are open, and where one is not, r is at most 1/2
+        // P to its own digits; so is Q while all gates are open, and where one is not, P is at most 1/2
+        p = make_float2(1.0f, 1.0f);
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
             l = scan_step<SHUT>(c[i], Channels<T>::widen(x[i]), l, u);
-            nq = fma2(c[i], r, nq);
-            r = scan_keep<SHUT>(c[i], r);
+            nq = fma2(c[i], p, nq);
+            p = scan_keep<SHUT>(c[i], p);
         }
-        nq = make_float2(r.x > 0.5f ? nq.x : r.x - 1.0f, r.y > 0.5f ? nq.y : r.y - 1.0f);
     } else {
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
             if (restart >> i & 1) l = make_float2(0.0f, 0.0f);
             l = scan_step<SHUT>(c[i], Channels<T>::widen(x[i]), l, u);
         }
-        nq = make_float2(-kScanCut, -kScanCut);
     }
-    return make_float4(l.x, l.y, -nq.x, -nq.y);
+    return {l, p, make_float2(-nq.x, -nq.y)};
 }
 __device__ __forceinline__ void scan_save(const ScanParams &p, int seq, const ScanPlace &at, int t, float2 m)
 {
@@ -518,7 +532,7 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W, scan_fo
         starts = scan_restarts(p, seq, t + W * kRun, len, lane);
         auto walk = [&](auto is_shut) {
             constexpr bool SHUT = decltype(is_shut)::value;
-            if constexpr (ahead) whole[warp][lane] = scan_whole<SHUT, T>(x, c, restart);
+            if constexpr (ahead) whole[warp][lane] = scan_whole<SHUT, T>(x, c, restart).packed();
             if (W > 1 && t > 0) m = scan_take_over<W>(&place[0][0], warp, lane);
             if constexpr (ahead)
                 if (t + kRun < len) scan_hand_on<W>(&place[0][0], warp + 1 < W ? warp + 1 : 0, lane, scan_apply(whole[warp][lane], m));
@@ -543,7 +557,7 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W, scan_fo
 template <typename T, int W, bool SHIFT>
 __global__ void __launch_bounds__(32 * W) k_scan_forward_split(const ScanParams p)
 {
-    __shared__ float4 runs[2][W][32];              // by round: what each warp's run does
+    __shared__ ScanRun runs[2][W][32];             // by round: what each warp's run does
     __shared__ float4 parts[2][kScanCluster][32];  // ... and each CTA's W runs
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cluster = p.cluster, rank = (int)cluster_rank();
@@ -594,28 +608,20 @@ __global__ void __launch_bounds__(32 * W) k_scan_forward_split(const ScanParams 
         float2 in = m;
         // warp k tells CTA k what this CTA's runs do
         if (warp < cluster) {
-            float4 all = runs[parity][0][lane];
-            for (int w = 1; w < W; ++w) {
-                const float4 o = runs[parity][w][lane];
-                scan_join(all.x, all.z, o.x, o.z);
-                scan_join(all.y, all.w, o.y, o.w);
-            }
-            for (int k = warp; k < cluster; k += W) scan_store_in(smem_addr(&parts[parity][rank][lane]), (uint32_t)k, all);
+            ScanRun all = runs[parity][0][lane];
+            for (int w = 1; w < W; ++w) all.join(runs[parity][w][lane]);
+            for (int k = warp; k < cluster; k += W) scan_store_in(smem_addr(&parts[parity][rank][lane]), (uint32_t)k, all.packed());
         }
         scan_cluster_arrive();
         next_rows();
-        float4 before = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // what this CTA's runs before this one do
-        for (int w = 0; w < warp; ++w) {
-            const float4 o = runs[parity][w][lane];
-            scan_join(before.x, before.z, o.x, o.z);
-            scan_join(before.y, before.w, o.y, o.w);
-        }
+        ScanRun before = {make_float2(0.0f, 0.0f), make_float2(1.0f, 1.0f), make_float2(0.0f, 0.0f)};  // what this CTA's runs before this one do
+        for (int w = 0; w < warp; ++w) before.join(runs[parity][w][lane]);
         scan_cluster_wait();
         for (int k = 0; k < cluster; ++k) {
             if (k == rank) in = m;
             m = scan_apply(parts[parity][k][lane], m);
         }
-        in = scan_apply(before, in);
+        in = scan_apply(before.packed(), in);
         if (t >= len) continue;
         scan_save(p, seq, at, t, in);
         shut ? scan_steps<true, T>(x, c, in, restart) : scan_steps<false, T>(x, c, in, restart);

@@ -76,3 +76,20 @@ def test_nearly_closed_gates(n, t, d, kind):
     level = torch.linspace(-20, 8, d, device="cuda") if d > 1 else torch.full((1,), -14.0, device="cuda")
     x = normal(n, t, d) * 10.0 ** (3 * normal(n, t, 1).clamp(-1, 1)) * (torch.rand(n, t, d, generator=gen, device="cuda") < 0.7)
     check(x.to(dtype), normal(n, t, d).to(dtype), level.to(dtype), normal(n, d), normal(n, t, d).to(dtype), normal(n, d))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n,t,d", [(100, 250, 64), (75, 193, 70), (1, 2100, 200), (3, 1700, 64)])
+def test_behind_a_large_token(n, t, d, kind):
+    """Chains that hand the state on ahead of their steps, and clusters: a token of 1e6 among ordinary ones, and what has decayed of it some dozens of
+    steps on, by gates from open to closed and by slow channels."""
+    dtype = TYPES[kind]
+    gen = torch.Generator(device="cuda").manual_seed(n + t + d)
+
+    def normal(*shape):
+        return torch.randn(*shape, generator=gen, device="cuda")
+
+    x = normal(n, t, d)
+    x[:, 5::97] *= 1e6
+    level = torch.linspace(-2, 9, d, device="cuda")[torch.randperm(d, generator=gen, device="cuda")]
+    check(x.to(dtype), (0.3 * normal(n, t, d)).to(dtype), level.to(dtype), 1e6 * normal(n, d), normal(n, t, d).to(dtype), normal(n, d))
