@@ -8,7 +8,8 @@
 // the gradient), scaled by powers of two: Y by 2^12, A and B by 2^13.  The host refuses coefficients with which Y could outgrow
 // them.  The small directions are brought up by a, step after step, while B Y is small there: so Y itself is kept in
 // two binary16 planes, the rounded value and the rest (22 bits), for a Y, which is added in binary32.  That costs bytes and no
-// product (gradient of 16 directions plus 3 % noise: error 1.6e-4 with it, 9e-3 without).  Where one product's 11 bits do not do - a binary16
+// product (gradient of 16 directions plus 3 % noise: error 1.6e-4 with it, 9e-3 without).  A matrix whose norm is small beside eps begins
+// with small singular values in all directions: its planes have a power of two more, step by step, so that they are as full as another's.  Where one product's 11 bits do not do - a binary16
 // result, small matrices - A and B have two planes too and each product is three: hi hi + hi lo + lo hi.
 //
 // The products are one tile kernel, pairs of CTAs as for the vocabulary head: TMA brings the operands through a ring, one
@@ -39,6 +40,7 @@ constexpr int kOrthoSmem = kRingBlocks * kBlockBytes + kOrthoWarps * kOrthoStagi
 constexpr int kOrthoMaxSteps = 32;
 constexpr float kOrthoScale = 4096.0f;                    // of Y's planes
 constexpr float kOrthoScaleA = 8192.0f;                   // of A's and B's
+constexpr int kOrthoMostPower = 100;                      // of two that a matrix's Y may have beside its scale; what that leaves out is below 1e-30
 
 // What becomes of a product.  kGram: A; kGramPart: binary32 parts of A; kPoly: B from A A; kSquare: a + B from the square of a shifted A;
 // kUpdate: the next Y; kResult: the result.
@@ -62,6 +64,8 @@ struct __align__(64) OrthoParams {
     __half *out;             // out_planes planes
     int in_planes, out_planes;
     float in_scale, acc_scale;
+    const float2 *powers;    // [matrix][kOrthoMaxSteps]: what the powers of two of Y, before and behind each step, make of a product's scale: A's, Y's
+    int step;
     float *part;             // kGramPart: [matrix][split][rows][pitch]
     void *result;            // kResult: row and matrix stride in elements
     long long result_row, result_matrix;
@@ -233,6 +237,14 @@ struct OrthoStage {
     }
 };
 
+// By a power of two, which is 1 as a rule
+__device__ __forceinline__ void ortho_scale(float (&z)[32], float power)
+{
+    if (power != 1.0f) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) z[i] *= power;
+    }
+}
 // What rounding to binary16 leaves of the values
 __device__ __forceinline__ void ortho_rest(float (&z)[32])
 {
@@ -495,6 +507,9 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
 #pragma unroll
                     for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(raw[i]) * p.acc_scale;
                     if (row0 >= p.rows || col >= (KIND == kResult ? p.columns : p.pitch)) continue;
+                    // read anew in each round, from L1: held in a register, other values are spilled (32000 x 1024: 853 us, 832 us so)
+                    [[maybe_unused]] const float2 *const powers = p.powers + tp.matrix * kOrthoMaxSteps + p.step;
+                    if constexpr (KIND == kGram || KIND == kGramPart) ortho_scale(z, powers->x);
                     if constexpr (KIND == kGramPart) {
                         float *dst = p.part + (long long)(tp.matrix * p.splits + tp.split) * p.rows * p.pitch;
                         stg.store_part(z, dst, p.pitch, row0, p.rows, col);
@@ -509,6 +524,7 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
                         }
                         if (at + 32 < width) fetch(col + 32);
                     }
+                    if constexpr (KIND == kUpdate || KIND == kResult) ortho_scale(z, powers->y);
                     if constexpr (KIND == kGram || KIND == kSquare) {
                         if (p.diag != 0.0f && col <= row0 + 31 && col + 31 >= row0) {
 #pragma unroll
@@ -637,11 +653,24 @@ k_ortho_norm(const T *__restrict__ x, long long row_stride, long long matrix_str
     }
 }
 
+// By what a step may enlarge singular values at most: max |a + b s^2 + c s^4|
+struct OrthoGrowth {
+    float by[kOrthoMaxSteps];
+    int steps;
+};
+// With all singular values at most `bound`, a power of two that they may have beside Y's scale
+__device__ __forceinline__ int ortho_room(double bound)
+{
+    const int e = bound > 0.0 ? 1022 - (__double2hiint(bound) >> 20) : 0;  // bound 2^e is in [1/2, 1); NaN and zero: none
+    return min(max(e, 0), kOrthoMostPower);
+}
+
 // Y = X / (|X| + eps), scaled, in two binary16 planes.  A matrix of zeros stays one; one that is not finite becomes NaN.
 template <typename T>
 __global__ void __launch_bounds__(32 * kOrthoLoadWarps)
 k_ortho_load(const T *__restrict__ x, long long row_stride, long long matrix_stride, int rows, int cols, int wide, int parts,
-             const double *__restrict__ partial, float eps, __half *__restrict__ y, long long pitch)
+             const double *__restrict__ partial, float eps, __half *__restrict__ y, long long pitch, const OrthoGrowth growth,
+             float2 *__restrict__ powers)
 {
     const int matrix = blockIdx.x / parts, part = blockIdx.x - matrix * parts, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     grid_dependency_wait();
@@ -653,7 +682,18 @@ k_ortho_load(const T *__restrict__ x, long long row_stride, long long matrix_str
     const double norm = sqrt(s);
     // in two factors, so that neither leaves binary32's range
     const double first = norm < 1e-20 ? 0x1p60 : norm > 1e20 ? 0x1p-60 : 1.0;
-    const float f1 = (float)first, f2 = norm == 0.0 ? 0.0f : norm < INFINITY ? (float)(kOrthoScale / ((norm + eps) * first)) : NAN;
+    double bound = norm / (norm + eps);
+    const float f1 = (float)first,
+                f2 = norm == 0.0 ? 0.0f : norm < INFINITY ? (float)(ldexp((double)kOrthoScale, ortho_room(bound)) / ((norm + eps) * first)) : NAN;
+    if (part == 0 && threadIdx.x == 0) {
+        float2 *const to = powers + matrix * kOrthoMaxSteps;
+        for (int i = 0, k = ortho_room(bound); i < growth.steps; ++i) {
+            bound *= growth.by[i];
+            const int after = i + 1 < growth.steps ? ortho_room(bound) : 0;
+            to[i] = make_float2(exp2f((float)(-2 * k)), exp2f((float)(after - k)));
+            k = after;
+        }
+    }
     const T *m = x + matrix * matrix_stride;
     __half *hi = y + matrix * 2 * (long long)rows * pitch, *lo = hi + (long long)rows * pitch;
     const int across = (cols + kOrthoItem - 1) / kOrthoItem;
@@ -735,7 +775,7 @@ struct OrthoLayout {
     int64_t batch, rows, cols, side, pitch, side_pitch;  // side: of A
     bool tall;
     int segments, planes, parts, splits, split_steps;
-    int64_t y[2], a, b, norm, sums, bytes;
+    int64_t y[2], a, b, norm, powers, sums, bytes;
 };
 
 OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols, int out_dtype)
@@ -771,6 +811,7 @@ OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols, int out_dtyp
     L.a = take(batch * L.planes * L.side * L.side_pitch * 2);
     L.b = take(batch * L.planes * L.side * L.side_pitch * 2);
     L.norm = take(batch * L.parts * 8);
+    L.powers = take(rows > 0 && cols > 0 ? batch * kOrthoMaxSteps * 8 : 0);
     L.sums = take(L.splits > 1 ? batch * L.splits * L.side * L.side_pitch * 4 : 0);
     L.bytes = at;
     return L;
@@ -787,14 +828,18 @@ int ortho_check(int64_t batch, int64_t rows, int64_t cols, int out_dtype)
 
 // The polynomials as a whole keep singular values within [0, most], most <= 2, and |b x + c x^2| <= 7.5 for x = s^2: what the scaled
 // binary16 planes hold.  s is at most 1 at first; a step's largest value lies at an end or where a + 3 b s^2 + 5 c s^4 = 0.
-// square[i]: whether they hold A + b / 2c and a + b x + c x^2 = c (x + b / 2c)^2 + a - b^2 / 4c as well.
-bool ortho_bounded(const float *coef, int steps, bool *square)
+struct OrthoSteps {
+    bool square[kOrthoMaxSteps];  // whether they hold A + b / 2c and a + b x + c x^2 = c (x + b / 2c)^2 + a - b^2 / 4c as well
+    OrthoGrowth growth;
+};
+bool ortho_bounded(const float *coef, int steps, OrthoSteps *out)
 {
+    out->growth.steps = steps;
     double most = 1.0;
     for (int i = 0; i < steps; ++i) {
         const double a = coef[3 * i], b = coef[3 * i + 1], c = coef[3 * i + 2];
         if (!(std::fabs(a) < 1e3 && std::fabs(b) < 1e3 && std::fabs(c) < 1e3)) return false;
-        double top = 0.0, poly = 0.0;
+        double top = 0.0, poly = 0.0, grows = 0.0;
         auto at = [&](double s2) {
             if (!(s2 >= 0.0 && s2 <= most * most)) return;
             const double v = std::fabs(std::sqrt(s2) * (a + s2 * (b + s2 * c)));
@@ -804,7 +849,9 @@ bool ortho_bounded(const float *coef, int steps, bool *square)
             if (!(s2 >= 0.0 && s2 <= most * most)) return;
             const double v = std::fabs(s2 * (b + s2 * c));
             if (v > poly) poly = v;
+            grows = std::fmax(grows, std::fabs(a + s2 * (b + s2 * c)));
         };
+        inner(0.0);
         at(most * most);
         inner(most * most);
         if (c != 0.0) {
@@ -817,8 +864,9 @@ bool ortho_bounded(const float *coef, int steps, bool *square)
         } else if (b != 0.0) {
             at(-a / (3.0 * b));
         }
-        square[i] = std::fabs(c) > 0.1 && std::fabs(b / (2.0 * c)) + most * most <= 7.5 && std::fabs(a) + poly <= 7.5;
+        out->square[i] = std::fabs(c) > 0.1 && std::fabs(b / (2.0 * c)) + most * most <= 7.5 && std::fabs(a) + poly <= 7.5;
         most = top * (1.0 + 0x1p-7);  // and what the roundings add
+        out->growth.by[i] = (float)(grows * (1.0 + 0x1p-7));
         if (most > 2.0 || poly > 7.5) return false;
     }
     return true;
@@ -917,7 +965,7 @@ struct OrthoCall {
     int64_t out_row, out_matrix;
     int out_dtype;
     const float *coef;
-    const bool *square;
+    const OrthoSteps *about;
     int steps;
     float eps;
     unsigned char *workspace;
@@ -949,7 +997,7 @@ cudaError_t ortho_load(const OrthoCall &c)
     if (e == cudaSuccess)
         e = launch_chained(k_ortho_load<T>, grid, 32 * kOrthoLoadWarps, 0, c.s, 1, (const T *)c.x, (long long)c.x_row,
                            (long long)c.x_matrix, (int)L.rows, (int)L.cols, wide, L.parts, (const double *)norm, c.eps,
-                           (__half *)(c.workspace + L.y[0]), (long long)L.pitch);
+                           (__half *)(c.workspace + L.y[0]), (long long)L.pitch, c.about->growth, (float2 *)(c.workspace + L.powers));
     return e;
 }
 
@@ -962,6 +1010,7 @@ cudaError_t orthogonalize(const OrthoCall &c)
     base.polls = operator_polls();
     base.segments = L.segments;
     base.splits = 1;
+    base.powers = (const float2 *)(c.workspace + L.powers);
     if (e == cudaSuccess) e = operator_status_ptr(&base.status);
     OrthoMaps y[2], a, b;
     for (int i = 0; i < 2 && e == cudaSuccess; ++i) e = ortho_maps(&y[i], c.workspace + L.y[i], 2 * L.batch, L.rows, L.cols, L.pitch);
@@ -976,8 +1025,9 @@ cudaError_t orthogonalize(const OrthoCall &c)
         const double ca = c.coef[3 * i], cb = c.coef[3 * i + 1], cc = c.coef[3 * i + 2];
         // Three products: 22 bits hold a + B as well as B, so that a Y needs no addition of its own; nor does b A with the square completed.
         // The epilogues then read nothing (256 x 1024: 24 matrices' update 34 us with that, 25 us without).
-        const bool square = L.segments == 3 && c.square[i];
+        const bool square = L.segments == 3 && c.about->square[i];
         OrthoParams p = base;  // A = Y Y^T or Y^T Y
+        p.step = i;
         p.diag = square ? (float)(cb / (2.0 * cc)) * kOrthoScaleA : 0.0f;
         p.a_mn = p.b_mn = L.tall;
         p.a_planes = p.b_planes = 2;
@@ -1069,8 +1119,8 @@ extern "C" int rsdgc_orthogonalize(const void *x_dev, int64_t x_row_stride, int6
     if (rc) return rc;
     if (!known_dtype(dtype) || !coefficients_host || n_steps < 1 || n_steps > kOrthoMaxSteps || !(eps >= 0.0f && eps < INFINITY))
         return RSDGC_ERR_INVALID;
-    bool square[kOrthoMaxSteps];
-    if (!ortho_bounded(coefficients_host, n_steps, square)) return RSDGC_ERR_INVALID;
+    OrthoSteps about;
+    if (!ortho_bounded(coefficients_host, n_steps, &about)) return RSDGC_ERR_INVALID;
     if (n_matrices == 0 || n_rows == 0 || n_cols == 0) return RSDGC_OK;
     if (!x_dev || !out_dev || !workspace_dev || (n_rows > 1 && (x_row_stride < n_cols || out_row_stride < n_cols)) ||
         (n_matrices > 1 && (x_matrix_stride < n_cols || out_matrix_stride < n_cols)))
@@ -1081,7 +1131,7 @@ extern "C" int rsdgc_orthogonalize(const void *x_dev, int64_t x_row_stride, int6
     if (n_matrices == 1) x_matrix_stride = out_matrix_stride = 0;  // free, and so are a single row's
     if (n_rows == 1) x_row_stride = out_row_stride = 0;
     const OrthoCall c = {ortho_layout(n_matrices, n_rows, n_cols, out_dtype), x_dev, x_row_stride, x_matrix_stride, dtype, out_dev,
-                         out_row_stride, out_matrix_stride, out_dtype, coefficients_host, square, n_steps, eps, (unsigned char *)workspace_dev,
+                         out_row_stride, out_matrix_stride, out_dtype, coefficients_host, &about, n_steps, eps, (unsigned char *)workspace_dev,
                          (cudaStream_t)stream};
     return operator_result(orthogonalize(c));
 }
