@@ -854,16 +854,14 @@ bool ortho_bounded(const float *coef, int steps, OrthoSteps *out)
         inner(0.0);
         at(most * most);
         inner(most * most);
-        if (c != 0.0) {
-            const double root = 9.0 * b * b - 20.0 * a * c;
-            if (root >= 0.0) {
-                at((-3.0 * b + std::sqrt(root)) / (10.0 * c));
-                at((-3.0 * b - std::sqrt(root)) / (10.0 * c));
-            }
-            inner(-b / (2.0 * c));
-        } else if (b != 0.0) {
-            at(-a / (3.0 * b));
+        // the roots of a + 3 b x + 5 c x^2 without a difference of near values, whatever c is
+        const double root = 9.0 * b * b - 20.0 * a * c;
+        if (root >= 0.0) {
+            const double sum = -0.5 * (3.0 * b + std::copysign(std::sqrt(root), b));
+            if (sum != 0.0) at(a / sum);
+            if (c != 0.0) at(sum / (5.0 * c));
         }
+        if (c != 0.0) inner(-b / (2.0 * c));
         out->square[i] = std::fabs(c) > 0.1 && std::fabs(b / (2.0 * c)) + most * most <= 7.5 && std::fabs(a) + poly <= 7.5;
         most = top * (1.0 + 0x1p-7);  // and what the roundings add
         out->growth.by[i] = (float)(grows * (1.0 + 0x1p-7));
