@@ -504,7 +504,7 @@ int rsdgc_gated_scan_backward(const void *dy_dev, int64_t dy_seq, int64_t dy_ste
  * its own rounding, for the coefficients above.  For binary16 results, and where the shorter side has at most 256, each product is made of three with
  * 22-bit operands: within 1e-4.
  * Errors: INVALID (a pointer NULL, strides, sizes < 0, types, eps negative or not finite, coefficients with which a singular value
- * could exceed 2 or |b s^2 + c s^4| 7.5), ALIGNMENT, CAPACITY (n_rows or n_cols > 2^24, the shorter one > 2^15, n_matrices > 2^20, or
+ * could exceed 2 or |b s^2 + c s^4| 30), ALIGNMENT, CAPACITY (n_rows or n_cols > 2^24, the shorter one > 2^15, n_matrices > 2^20, or
  * more than 2^25 tiles of 256 x 128 in all), CUDA.
  */
 int64_t rsdgc_orthogonalize_workspace_bytes(int64_t n_matrices, int64_t n_rows, int64_t n_cols, int32_t out_dtype);

@@ -5,7 +5,7 @@
 //   matrices with more rows than columns, so that A has the shorter side
 //
 // Numbers.  The products' operands are binary16 (11 bits; bfloat16's 8 leave an error of 0.01, and 0.07 where a few directions carry
-// the gradient), scaled by powers of two: Y by 2^12, A and B by 2^13.  The host refuses coefficients with which Y could outgrow
+// the gradient), scaled by powers of two: Y by 2^12, A by 2^13, B by 2^13 or, where it is larger than 7.5, 2^12 or 2^11.  The host refuses coefficients with which Y could outgrow
 // them.  The small directions are brought up by a, step after step, while B Y is small there: so Y itself is kept in
 // two binary16 planes, the rounded value and the rest (22 bits), for a Y, which is added in binary32.  That costs bytes and no
 // product (gradient of 16 directions plus 3 % noise: error 1.6e-4 with it, 9e-3 without).  A matrix whose norm is small beside eps begins
@@ -39,7 +39,7 @@ constexpr int kOrthoStaging = 2048;                       // per epilogue warp: 
 constexpr int kOrthoSmem = kRingBlocks * kBlockBytes + kOrthoWarps * kOrthoStaging + 1024;
 constexpr int kOrthoMaxSteps = 32;
 constexpr float kOrthoScale = 4096.0f;                    // of Y's planes
-constexpr float kOrthoScaleA = 8192.0f;                   // of A's and B's
+constexpr float kOrthoScaleA = 8192.0f;                   // of A's, and of most B's
 constexpr int kOrthoMostPower = 100;                      // of two that a matrix's Y may have beside its scale; what that leaves out is below 1e-30
 
 // What becomes of a product.  kGram: A; kGramPart: binary32 parts of A; kPoly: B from A A; kSquare: a + B from the square of a shifted A;
@@ -826,10 +826,11 @@ int ortho_check(int64_t batch, int64_t rows, int64_t cols, int out_dtype)
     return tiles > INT_MAX || batch * kOrthoLoadParts > INT_MAX ? RSDGC_ERR_CAPACITY : RSDGC_OK;
 }
 
-// The polynomials as a whole keep singular values within [0, most], most <= 2, and |b x + c x^2| <= 7.5 for x = s^2: what the scaled
-// binary16 planes hold.  s is at most 1 at first; a step's largest value lies at an end or where a + 3 b s^2 + 5 c s^4 = 0.
+// The polynomials as a whole keep singular values within [0, most], at most 2 and what the roundings add, and |b x + c x^2| <= 30 for x = s^2: what the scaled
+// binary16 planes hold, with B's scale halved twice at most.  s is at most 1 at first; a step's largest value lies at an end or where a + 3 b s^2 + 5 c s^4 = 0.
 struct OrthoSteps {
     bool square[kOrthoMaxSteps];  // whether they hold A + b / 2c and a + b x + c x^2 = c (x + b / 2c)^2 + a - b^2 / 4c as well
+    float b_scale[kOrthoMaxSteps];  // B's beside kOrthoScaleA: 1, 1/2 or 1/4
     OrthoGrowth growth;
 };
 bool ortho_bounded(const float *coef, int steps, OrthoSteps *out)
@@ -865,7 +866,8 @@ bool ortho_bounded(const float *coef, int steps, OrthoSteps *out)
         out->square[i] = std::fabs(c) > 0.1 && std::fabs(b / (2.0 * c)) + most * most <= 7.5 && std::fabs(a) + poly <= 7.5;
         most = top * (1.0 + 0x1p-7);  // and what the roundings add
         out->growth.by[i] = (float)(grows * (1.0 + 0x1p-7));
-        if (most > 2.0 || poly > 7.5) return false;
+        if (top > 2.0 || poly > 30.0) return false;
+        out->b_scale[i] = poly <= 7.5 ? 1.0f : poly <= 15.0 ? 0.5f : 0.25f;
     }
     return true;
 }
@@ -1058,8 +1060,8 @@ cudaError_t orthogonalize(const OrthoCall &c)
         p.splits = 1;
         p.split_steps = L.segments * p.k_steps;
         p.in = ap;
-        p.in_scale = (float)cb;
-        p.acc_scale = (float)cc * 0x1p-13f;
+        p.in_scale = (float)cb * c.about->b_scale[i];
+        p.acc_scale = (float)cc * 0x1p-13f * c.about->b_scale[i];
         p.diag = square ? (float)(ca - cb * cb / (4.0 * cc)) * kOrthoScaleA : 0.0f;
         p.out = bp;
         e = square ? ortho_product<kSquare, __half>(p, a, a, c) : ortho_product<kPoly, __half>(p, a, a, c);
@@ -1078,7 +1080,7 @@ cudaError_t orthogonalize(const OrthoCall &c)
         p.in = yp;
         p.in_planes = square ? 0 : 2;
         p.in_scale = (float)ca;
-        p.acc_scale = 0x1p-13f;
+        p.acc_scale = 0x1p-13f / c.about->b_scale[i];
         p.diag = 0.0f;
         p.out = (__half *)(c.workspace + L.y[(i + 1) & 1]);
         p.out_planes = 2;

@@ -2,8 +2,10 @@
 
 Tolerances, derived before the first run.  `steps` makes the operator's roundings, relative to each value: operands of the products to 11 bits (or 22, with two
 planes), Y to 22 bits.  How far that is from the formula, t (2-norm), is what they cost on this input; the kernel's roundings fall elsewhere, each as large: 2 t.
-binary32's sums and what the smallest entries lose beside the largest (a plane ends 2^-37 below the norm's bound, of 2^20 entries and less: 2^-27 of the
-norm) add less than 2^-20 of the result for five steps, 2^-18 for twenty.
+The products' sums are binary32 and may be cut off instead of rounded, 16 terms at a time: where all terms have one sign, a product over K terms comes out
+smaller by up to (K / 16 + 1) 2^-23 (three times as many steps with two planes), in each step, and the polynomials enlarge that.  So `steps` is also computed
+with each of the three products smaller by that much; what this changes is added.  What the smallest entries lose beside the largest (a plane ends 2^-37
+below the norm's bound, of 2^20 entries and less: 2^-27 of the norm) is below 2^-20 of the result.
 """
 import math
 
@@ -21,7 +23,7 @@ def digits(v, bits):
     return torch.ldexp(torch.round(m * 2.0 ** bits), e - bits)
 
 
-def steps(x, coef, eps, bits=None):
+def steps(x, coef, eps, bits=None, smaller=(0.0, 0.0, 0.0)):
     y = x.double()
     tall = y.shape[-2] > y.shape[-1]
     y = y.mT if tall else y
@@ -29,18 +31,23 @@ def steps(x, coef, eps, bits=None):
     for a, b, c in coef:
         yy = y if bits is None else digits(y, 22)
         op = yy if bits is None else digits(yy, bits)
-        A = op @ op.mT
+        A = op @ op.mT * (1 - smaller[0])
         A = A if bits is None else digits(A, bits)
-        B = b * A + c * A @ A
-        y = a * yy + (B if bits is None else digits(B, bits)) @ op
+        B = b * A + c * A @ A * (1 - smaller[1])
+        y = a * yy + (B if bits is None else digits(B, bits)) @ op * (1 - smaller[2])
     return y.mT if tall else y
 
 
 def limits(x, out_dtype, coef, eps):
     want = steps(x, coef, eps)
-    bits = 22 if out_dtype == torch.float16 or min(x.shape[-2:]) <= 256 else 11
-    t = 2 * torch.linalg.matrix_norm(steps(x, coef, eps, bits) - want)
-    return want, t + (2.0 ** -20 if len(coef) <= 5 else 2.0 ** -18) * torch.linalg.matrix_norm(want)
+    side, long = sorted(x.shape[-2:])
+    precise = out_dtype == torch.float16 or side <= 256
+    t = 2 * torch.linalg.matrix_norm(steps(x, coef, eps, 22 if precise else 11) - want)
+    for i, terms in enumerate((long, side, side)):
+        smaller = [0.0, 0.0, 0.0]
+        smaller[i] = ((3 if precise else 1) * terms / 16 + 1) * 2.0 ** -23
+        t = t + torch.linalg.matrix_norm(steps(x, coef, eps, None, smaller) - want)
+    return want, t + 2.0 ** -20 * torch.linalg.matrix_norm(want)
 
 
 @pytest.mark.parametrize("out", ["bf16", "f16"])
@@ -55,3 +62,15 @@ def test_input_far_below_eps(b, m, n, out):
     coef = ((1.5, -0.5, 0.0),) * 20
     x = gradient(gen, (b, m, n)) / math.sqrt(m * n) * torch.logspace(-9, -3, b, device="cuda")[:, None, None]
     near(run(x, TYPES[out], coef, 1.0), *limits(x, TYPES[out], coef, 1.0))
+
+
+@pytest.mark.parametrize("out", ["bf16", "f16"])
+@pytest.mark.parametrize("m,n", [(100, 300), (300, 500), (700, 400)])
+def test_a_schedule_that_begins_steeply(m, n, out):
+    """Its first polynomial of A is beyond what B's planes hold at their usual scale; and a second step of 29.6, with nothing to spare."""
+    gen = torch.Generator(device="cuda").manual_seed(m)
+    steep = tuple((a / 1.01, b / 1.01 ** 3, c / 1.01 ** 5) for a, b, c in (
+        (8.2872, -23.5959, 17.3004), (4.1071, -2.9478, 0.5448), (3.9487, -2.9089, 0.5518), (3.3184, -2.4885, 0.51), (2.3007, -1.6689, 0.4188)))
+    for coef in (steep, ((0.1717, 0.0, 0.0), (29.0, -990.0, 0.0))):
+        for x in (gradient(gen, (m, n), "low"), torch.ones(m, n, device="cuda")):
+            near(run(x, TYPES[out], coef, 0.0), *limits(x, TYPES[out], coef, 0.0))

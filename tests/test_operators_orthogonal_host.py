@@ -42,9 +42,32 @@ def test_what_is_taken_is_what_sampling_finds(takes):
     for _ in range(3000):
         a, b, c = (float(np.float32(v)) for v in rng.normal(size=3) * rng.choice([1e-9, 1e-4, 1.0, 3.0], size=3))
         top, poly = largest(a, b, c)
-        if abs(top * (1 + 2.0 ** -7) - 2.0) < 1e-3 or poly > 7.4:
+        if abs(top - 2.0) < 1e-3 or poly > 7.4:
             continue  # next to a border, or beyond the other one
-        ok = top * (1 + 2.0 ** -7) < 2.0
+        ok = top < 2.0
         taken += ok
         assert takes((a, b, c)) == ok, (a, b, c, top, poly)
     assert taken > 500
+
+
+# a schedule that begins steeply, each step's argument divided by 1.01 so that roundings do not grow
+STEEP = tuple((a / 1.01, b / 1.01 ** 3, c / 1.01 ** 5) for a, b, c in (
+    (8.2872, -23.5959, 17.3004), (4.1071, -2.9478, 0.5448), (3.9487, -2.9089, 0.5518), (3.3184, -2.4885, 0.51), (2.3007, -1.6689, 0.4188)))
+
+
+def test_a_schedule_that_begins_steeply(takes):
+    """Its first polynomial of A reaches 7.97, its singular values stay below 2."""
+    top, poly = largest(*STEEP[0])
+    assert 7.9 < poly < 8 and top < 2 and takes(*STEEP)
+    for scale in (1.0, 1.9, 3.7):  # up to 29.9, where a makes up for it: s (a + b s^2 + c s^4) with a maximum next to 2
+        a, b, c = 8.2 * scale, -23.6 * scale ** 3, 17.3 * scale ** 5
+        top, poly = largest(a, b, c)
+        assert takes((a, b, c)) == (top < 2 and poly < 30)
+
+
+def test_polynomials_up_to_30(takes):
+    """A first step that leaves singular values up to m (and 2^-7 more for roundings), of which the second one's b s^2 reaches 29.64 and 30.27."""
+    for m, ok in ((0.1717, True), (0.1735, False)):
+        top, poly = largest(29.0, -990.0, 0.0, m * (1 + 2.0 ** -7))
+        assert top < 1.95 and (poly < 30) == ok and abs(poly - 30) > 0.2
+        assert takes((m, 0.0, 0.0), (29.0, -990.0, 0.0)) == ok
