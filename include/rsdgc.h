@@ -499,10 +499,12 @@ int rsdgc_gated_scan_backward(const void *dy_dev, int64_t dy_seq, int64_t dy_ste
  * x: `dtype`; out: out_dtype, bfloat16 or binary16; row and matrix strides in elements, any alignment.  coefficients_host: 3 * n_steps
  * binary32 on the host, read during the call; n_steps 1 to 32.  workspace_dev: rsdgc_orthogonalize_workspace_bytes() bytes, 256-byte
  * aligned; nothing in it has to survive between calls.  A matrix of zeros gives zeros, one that is not finite NaN.
- * Accuracy: sums in binary32, operands of 11 bits (22 for a Y); the result is within 0.003 (relative 2-norm; typically 0.0015 of its Frobenius norm) of
- * the formula's, before
- * its own rounding, for the coefficients above.  For binary16 results, and where the shorter side has at most 256, each product is made of three with
- * 22-bit operands: within 1e-4.
+ * Accuracy: sums in binary32, operands of 11 bits (22 for a Y).  For binary16 results, and where the shorter side has at most 256, each product is made
+ * of three with 22-bit operands (a caller who wants those for larger sides takes a binary16 result).  With the coefficients above the result, its own
+ * rounding included, is within 0.01 of the formula's (relative 2-norm; 11 bits), 0.001 (binary16) and 0.004 (bfloat16, short sides; its rounding
+ * alone makes 0.0033): the most that was found, in noise, uneven and dominant rows and columns, equal and decaying singular values, from 200 x 200
+ * to 4096 x 4096 and 32000 x 1024, is 0.0087 (equal singular values, 384 x 384), 0.0007 (four dominant columns, 4096 x 4096) and 0.0033; usual are
+ * 0.002 to 0.004 and 0.0002 to 0.0003.  Coefficients under which near singular values part faster than under these enlarge errors as well.
  * Errors: INVALID (a pointer NULL, strides, sizes < 0, types, eps negative or not finite, coefficients with which a singular value
  * could exceed 2 or |b s^2 + c s^4| 30), ALIGNMENT, CAPACITY (n_rows or n_cols > 2^24, the shorter one > 2^15, n_matrices > 2^20, or
  * more than 2^25 tiles of 256 x 128 in all), CUDA.

@@ -765,7 +765,10 @@ namespace {
 
 constexpr int kOrthoPairs = 74;          // of CTAs on the device, for what workspaces depend on
 constexpr int kOrthoLoadParts = 1184;    // most CTAs per matrix of the two passes over X: eight a multiprocessor (two: 32000 x 1024 859 us, 830 us so)
-constexpr int64_t kOrthoPrecise = 256;   // shorter sides up to this take three products for every result
+// Shorter sides up to this take three products for every result: there they cost a fifth of the call at most, beyond it more and more (bfloat16
+// results, one product and three: 128 x 512 122 and 142 us, 256 x 512 126 and 151, 24 x 256 x 1024 217 and 257, 512 x 1024 153 and 196, 8 x 512 x
+// 1024 192 and 261, 1024 x 1024 171 and 271).
+constexpr int64_t kOrthoPrecise = 256;
 
 inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 inline int tiles_of(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }

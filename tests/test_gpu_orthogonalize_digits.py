@@ -74,3 +74,37 @@ def test_a_schedule_that_begins_steeply(m, n, out):
     for coef in (steep, ((0.1717, 0.0, 0.0), (29.0, -990.0, 0.0))):
         for x in (gradient(gen, (m, n), "low"), torch.ones(m, n, device="cuda")):
             near(run(x, TYPES[out], coef, 0.0), *limits(x, TYPES[out], coef, 0.0))
+
+
+def norm(d):
+    """2-norm"""
+    d = d if d.shape[0] <= d.shape[1] else d.mT
+    return float(torch.linalg.eigvalsh(d @ d.mT)[-1].clamp(min=0).sqrt())
+
+
+def dominant(gen, m, n, rows, factor):
+    x = torch.randn(m, n, generator=gen, device="cuda")
+    x[:rows] *= factor
+    return x
+
+
+def equal(gen, m, n):
+    return torch.linalg.qr(torch.randn(m, n, generator=gen, device="cuda", dtype=torch.float64))[0].float().contiguous()
+
+
+def uneven(gen, m, n):
+    return torch.randn(m, n, generator=gen, device="cuda") * torch.logspace(-3, 0, m, device="cuda")[:, None]
+
+
+@pytest.mark.parametrize("m,n,make", [
+    (300, 300, equal), (384, 384, equal), (512, 512, lambda g, m, n: torch.eye(m, device="cuda")), (200, 200, equal), (300, 9000, uneven),
+    (257, 257, uneven), (9000, 300, uneven), (200, 3000, uneven), (300, 9000, lambda g, m, n: torch.randn(m, n, generator=g, device="cuda")),
+    (512, 3000, lambda g, m, n: dominant(g, m, n, 4, 100)), (512, 8000, lambda g, m, n: dominant(g, m, n, 32, 100)),
+    (2048, 2048, lambda g, m, n: dominant(g, m, n, 4, 1000).mT.contiguous()), (1000, 4000, lambda g, m, n: torch.rand(m, n, generator=g, device="cuda"))])
+def test_documented_accuracy(m, n, make):
+    """The header's numbers, the result's rounding included; they are what was measured, rounded up, and derive from nothing else."""
+    x = make(torch.Generator(device="cuda").manual_seed(m + n), m, n)
+    want = steps(x, COEF, 1e-7)
+    for out, limit in ((torch.float16, 0.001), (torch.bfloat16, 0.004 if min(m, n) <= 256 else 0.01)):
+        got = run(x, out)
+        assert norm(got.double() - want) <= limit * norm(want), out
