@@ -528,6 +528,9 @@ int rsdgc_operator_status(void *stream, uint32_t *flags_host);
 int rsdgc_selftest_operator_polls(int32_t polls);
 /* Makes a wait run out on `stream` that nothing will ever end (nothing is in flight either), after `polls` polls, 1 to 2^20. */
 int rsdgc_selftest_operator_wait(int32_t polls, void *stream);
+/* How the calling thread's latest gated scan, forward or backward, dealt a sequence's 64 channels: warps that take its steps in turn per
+ * CTA, and CTAs (0 and 0: none yet).  Results do not depend on it beyond roundings.  INVALID: a pointer NULL. */
+int rsdgc_selftest_scan_way(int32_t *warps_host, int32_t *ctas_host);
 
 /* Waits for the stream, copies the device status word to *out_host and clears it. */
 int rsdgc_get_status(rsdgc_plan *plan, void *stream, rsdgc_status *out_host);

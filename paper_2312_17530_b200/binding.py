@@ -37,6 +37,7 @@ EXPORTS = [
     "rsdgc_head_distill_backward", "rsdgc_selftest_operator_polls",
     "rsdgc_selftest_operator_wait", "rsdgc_head_forward_workspace_bytes", "rsdgc_gated_scan_workspace_bytes",
     "rsdgc_gated_scan_forward", "rsdgc_gated_scan_backward", "rsdgc_orthogonalize_workspace_bytes", "rsdgc_orthogonalize",
+    "rsdgc_selftest_scan_way",
 ]
 NOALLOC_MAX_LAYERS = 64
 N_COMPRESS_KERNELS = 5
@@ -117,6 +118,7 @@ def lib():
         L.rsdgc_operator_status.argtypes = [vp, C.POINTER(u32)]
         L.rsdgc_selftest_operator_polls.argtypes = [i32]
         L.rsdgc_selftest_operator_wait.argtypes = [i32, vp]
+        L.rsdgc_selftest_scan_way.argtypes = [C.POINTER(i32), C.POINTER(i32)]
         L.rsdgc_layer_norm_workspace_bytes.argtypes = [i64, i64]
         L.rsdgc_layer_norm_workspace_bytes.restype = i64
         L.rsdgc_layer_norm_forward.argtypes = [vp, i64, vp, vp, vp, i64, vp, vp, i64, i64, i32, i32, f32, vp]
@@ -752,3 +754,10 @@ def selftest_operator_wait(polls: int = 256) -> None:
 
 def launch_count() -> int:
     return int(lib().rsdgc_launch_count())
+
+
+def selftest_scan_way() -> Tuple[int, int]:
+    """(warps per CTA, CTAs) among which this thread's latest gated scan dealt the steps of a sequence's 64 channels."""
+    warps, ctas = C.c_int32(), C.c_int32()
+    _check(lib().rsdgc_selftest_scan_way(C.byref(warps), C.byref(ctas)), "rsdgc_selftest_scan_way")
+    return warps.value, ctas.value

@@ -992,18 +992,27 @@ cudaError_t scan_ready(K kernel, std::atomic<uint64_t> &ready, int bytes, int *d
     if (e == cudaSuccess) ready.fetch_or(1ull << (*dev & 63), std::memory_order_release);
     return e;
 }
-template <typename K>
-cudaError_t scan_launch(K kernel, std::atomic<uint64_t> &ready, unsigned grid, int warps, int bytes, int cluster, cudaStream_t s,
-                        const ScanParams &p)
+// What the calling thread's latest launch took: warps of a sequence's group per CTA, CTAs of it
+thread_local int scan_way_warps = 0, scan_way_ctas = 0;
+void scan_took(int warps, int ctas)
 {
-    int dev = 0;
-    const cudaError_t e = scan_ready(kernel, ready, warps * bytes, &dev);
-    return e != cudaSuccess ? e : launch_chained(kernel, grid, 32 * warps, (size_t)warps * bytes, s, cluster, p);
+    scan_way_warps = warps;
+    scan_way_ctas = ctas;
 }
-#define SCAN_LAUNCH(kernel, grid, warps, cluster)                                                          \
+
+template <typename K>
+cudaError_t scan_launch(K kernel, std::atomic<uint64_t> &ready, unsigned grid, int chain, int bytes, cudaStream_t s, const ScanParams &p)
+{
+    const int warps = chain == 1 ? kScanLoneWarps : chain;
+    int dev = 0;
+    scan_took(chain, 1);
+    const cudaError_t e = scan_ready(kernel, ready, warps * bytes, &dev);
+    return e != cudaSuccess ? e : launch_chained(kernel, grid, 32 * warps, (size_t)warps * bytes, s, 1, p);
+}
+#define SCAN_LAUNCH(kernel, grid, chain)                                                                   \
     [&] {                                                                                                  \
         static std::atomic<uint64_t> ready{0};                                                             \
-        return scan_launch(kernel, ready, (unsigned)(grid), warps, bytes, cluster, s, p);                  \
+        return scan_launch(kernel, ready, (unsigned)(grid), chain, bytes, s, p);                           \
     }()
 
 // The kernel that splits the steps, in clusters of p.cluster CTAs; *done = false if fewer than `least` would be on the device at
@@ -1040,6 +1049,7 @@ cudaError_t scan_split(K kernel, std::atomic<uint64_t> &ready, std::atomic<int> 
         if (n < units) continue;
         p.cluster = k;
         *done = true;
+        scan_took(warps, k);
         return launch_chained(kernel, (unsigned)(units * k), 32 * warps, (size_t)warps * bytes, s, k, p);
     }
     return e;
@@ -1062,12 +1072,12 @@ cudaError_t scan_forward(ScanParams &p, cudaStream_t s)
     const cudaError_t e = SCAN_SPLIT((k_scan_forward_split<T, wide, SHIFT>), units, wide, 3, &done);
     if (done || e != cudaSuccess) return e;
     switch (scan_warps(units, p.n_steps, 12, scan_forward_warps<T>)) {
-    case 1: return SCAN_LAUNCH((k_scan_forward<T, 1, SHIFT>), (units + kScanLoneWarps - 1) / kScanLoneWarps, kScanLoneWarps, 1);
-    case 2: return SCAN_LAUNCH((k_scan_forward<T, 2, SHIFT>), units, 2, 1);
-    case 4: return SCAN_LAUNCH((k_scan_forward<T, 4, SHIFT>), units, 4, 1);
-    case 8: return SCAN_LAUNCH((k_scan_forward<T, 8, SHIFT>), units, 8, 1);
+    case 1: return SCAN_LAUNCH((k_scan_forward<T, 1, SHIFT>), (units + kScanLoneWarps - 1) / kScanLoneWarps, 1);
+    case 2: return SCAN_LAUNCH((k_scan_forward<T, 2, SHIFT>), units, 2);
+    case 4: return SCAN_LAUNCH((k_scan_forward<T, 4, SHIFT>), units, 4);
+    case 8: return SCAN_LAUNCH((k_scan_forward<T, 8, SHIFT>), units, 8);
     }
-    return SCAN_LAUNCH((k_scan_forward<T, 12, SHIFT>), units, 12, 1);
+    return SCAN_LAUNCH((k_scan_forward<T, 12, SHIFT>), units, 12);
 }
 
 template <typename T, bool SHIFT>
@@ -1080,12 +1090,12 @@ cudaError_t scan_backward(ScanParams &p, cudaStream_t s)
     const cudaError_t e = SCAN_SPLIT((k_scan_backward_split<T, wide, SHIFT>), units, wide, 2, &done);
     if (done || e != cudaSuccess) return e;
     switch (scan_warps(units, p.n_steps, sizeof(T) == 4 ? 8 : 12, scan_backward_warps<T>)) {
-    case 1: return SCAN_LAUNCH((k_scan_backward<T, 1, SHIFT>), (units + kScanLoneWarps - 1) / kScanLoneWarps, kScanLoneWarps, 1);
-    case 2: return SCAN_LAUNCH((k_scan_backward<T, 2, SHIFT>), units, 2, 1);
-    case 4: return SCAN_LAUNCH((k_scan_backward<T, 4, SHIFT>), units, 4, 1);
-    case 8: return SCAN_LAUNCH((k_scan_backward<T, 8, SHIFT>), units, 8, 1);
+    case 1: return SCAN_LAUNCH((k_scan_backward<T, 1, SHIFT>), (units + kScanLoneWarps - 1) / kScanLoneWarps, 1);
+    case 2: return SCAN_LAUNCH((k_scan_backward<T, 2, SHIFT>), units, 2);
+    case 4: return SCAN_LAUNCH((k_scan_backward<T, 4, SHIFT>), units, 4);
+    case 8: return SCAN_LAUNCH((k_scan_backward<T, 8, SHIFT>), units, 8);
     }
-    if constexpr (sizeof(T) < 4) return SCAN_LAUNCH((k_scan_backward<T, 12, SHIFT>), units, 12, 1);
+    if constexpr (sizeof(T) < 4) return SCAN_LAUNCH((k_scan_backward<T, 12, SHIFT>), units, 12);
     return cudaErrorInvalidValue;
 }
 
@@ -1225,4 +1235,12 @@ extern "C" int rsdgc_gated_scan_backward(const void *dy_dev, int64_t dy_seq, int
                                   p.seq_parts * p.cluster, (int)width, (G *)dbias_dev);
         });
     return operator_result(e);
+}
+
+extern "C" int rsdgc_selftest_scan_way(int32_t *warps_host, int32_t *ctas_host)
+{
+    if (!warps_host || !ctas_host) return RSDGC_ERR_INVALID;
+    *warps_host = scan_way_warps;
+    *ctas_host = scan_way_ctas;
+    return RSDGC_OK;
 }
