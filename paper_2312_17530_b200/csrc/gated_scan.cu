@@ -771,7 +771,8 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W, scan_ba
     float2 sum = make_float2(0.0f, 0.0f), rest = sum;  // of dgate, with what the sum's rounding left out
     extern __shared__ __align__(16) unsigned char smem[];
     ScanBack<T, SHIFT> next = {ScanRing<T, 3, SHIFT>(smem, warp, lane), sum, false};
-    for (int seq = part; seq < p.n_seq; seq += p.seq_parts) {
+    // chains have one sequence: there are more only where the warps that walk alone fill the device several times
+    for (int seq = part; seq < p.n_seq; seq += W == 1 ? p.seq_parts : p.n_seq) {
         const int len = scan_length(p, seq), runs = (len + kRun - 1) / kRun;
         float2 e = make_float2(0.0f, 0.0f);
         if (p.first && run == 0) e = scan_load2(p.first + (long long)seq * p.width + at.c, at.n);
@@ -817,7 +818,6 @@ __global__ void __launch_bounds__(W == 1 ? 32 * kScanLoneWarps : 32 * W, scan_ba
             if (p.dgate.p) scan_write<T>(x, p, p.dgate, seq, at, t, len);
             scan_sum(sum, rest, add);
         }
-        if (W > 1) __syncthreads();  // the next sequence's first run waits for no one: the places are to be free
     }
     scan_sums<W>(&place[0][0], sum, p, at, part, run, lane);
 }
@@ -834,7 +834,7 @@ __global__ void __launch_bounds__(32 * W) k_scan_backward_split(const ScanParams
     const int unit = (int)blockIdx.x / cluster;
     grid_dependency_wait();
     grid_dependency_launch_next();
-    const int part = unit / p.groups, group = unit - part * p.groups;
+    const int seq = unit / p.groups, group = unit - seq * p.groups;
     cluster_sync_all();  // nothing is written to a CTA that has not begun
     const ScanPlace at(p, group, lane);
     const float2 bias = at.bias(p);
@@ -843,60 +843,58 @@ __global__ void __launch_bounds__(32 * W) k_scan_backward_split(const ScanParams
     extern __shared__ __align__(16) unsigned char smem[];
     ScanBack<T, SHIFT> next = {ScanRing<T, 3, SHIFT>(smem, warp, lane), sum, false};
     int parity = 0;
-    for (int seq = part; seq < p.n_seq; seq += p.seq_parts) {
-        const int len = scan_length(p, seq), tiles = (len + tile - 1) / tile;
-        float2 e = make_float2(0.0f, 0.0f);  // the gradient that comes into the round from behind
-        if (p.first) e = scan_load2(p.first + (long long)seq * p.width + at.c, at.n);
-        int t = (tiles - 1 - rank) * tile + warp * kRun;
-        next.start(p, seq, at);
-        next.rows(p, seq, at, t, len);
-        next.rows(p, seq, at, t - tile * cluster, len);
-        next.state(p, seq, at, t, len, lane);
-        for (int left = tiles; left > 0; left -= cluster, t -= tile * cluster, parity ^= 1) {
-            typename Channels<T>::Raw x[kRun], dy[kRun];
-            float2 c[kRun], u[kRun], add;
-            const uint32_t restart = __ballot_sync(0xFFFFFFFFu, next.starts);
-            const float2 from = next.from;
-            const bool shut = next.take(c, x, dy, bias, t, len);
-            if (shut) scan_gates<true>(c, next.ring, 1, bias, t, len);
-            runs[parity][warp][lane] = shut ? scan_back_whole<true, T>(dy, c, restart) : scan_back_whole<false, T>(dy, c, restart);
-            __syncthreads();
-            float2 in = e;
-            if (warp < cluster) {
-                float2 all = make_float2(0.0f, 0.0f), k = make_float2(1.0f, 1.0f);
-                for (int w = W - 1; w >= 0; --w) {
-                    const float4 o = runs[parity][w][lane];
-                    all = scan_back(o, all);
-                    k = make_float2(scan_through(k.x, o.z), scan_through(k.y, o.w));
-                }
-                for (int to = warp; to < cluster; to += W)
-                    scan_store_in(smem_addr(&parts[parity][rank][lane]), (uint32_t)to, make_float4(all.x, all.y, k.x, k.y));
-            }
-            scan_cluster_arrive();
-            next.refill(p, seq, at, t, len, tile * cluster);
-            next.state(p, seq, at, t - tile * cluster, len, lane);
-            float4 behind = make_float4(0.0f, 0.0f, 1.0f, 1.0f);  // what this CTA's runs behind this one do
-            for (int w = W - 1; w > warp; --w) {
+    const int len = scan_length(p, seq), tiles = (len + tile - 1) / tile;
+    float2 e = make_float2(0.0f, 0.0f);  // the gradient that comes into the round from behind
+    if (p.first) e = scan_load2(p.first + (long long)seq * p.width + at.c, at.n);
+    int t = (tiles - 1 - rank) * tile + warp * kRun;
+    next.start(p, seq, at);
+    next.rows(p, seq, at, t, len);
+    next.rows(p, seq, at, t - tile * cluster, len);
+    next.state(p, seq, at, t, len, lane);
+    for (int left = tiles; left > 0; left -= cluster, t -= tile * cluster, parity ^= 1) {
+        typename Channels<T>::Raw x[kRun], dy[kRun];
+        float2 c[kRun], u[kRun], add;
+        const uint32_t restart = __ballot_sync(0xFFFFFFFFu, next.starts);
+        const float2 from = next.from;
+        const bool shut = next.take(c, x, dy, bias, t, len);
+        if (shut) scan_gates<true>(c, next.ring, 1, bias, t, len);
+        runs[parity][warp][lane] = shut ? scan_back_whole<true, T>(dy, c, restart) : scan_back_whole<false, T>(dy, c, restart);
+        __syncthreads();
+        float2 in = e;
+        if (warp < cluster) {
+            float2 all = make_float2(0.0f, 0.0f), k = make_float2(1.0f, 1.0f);
+            for (int w = W - 1; w >= 0; --w) {
                 const float4 o = runs[parity][w][lane];
-                const float2 r = scan_back(o, make_float2(behind.x, behind.y));
-                behind = make_float4(r.x, r.y, scan_through(behind.z, o.z), scan_through(behind.w, o.w));
+                all = scan_back(o, all);
+                k = make_float2(scan_through(k.x, o.z), scan_through(k.y, o.w));
             }
-            scan_cluster_wait();
-            for (int k = 0; k < cluster; ++k) {
-                if (k == rank) in = e;
-                e = scan_back(parts[parity][k][lane], e);
-            }
-            in = scan_back(behind, in);
-            if (t < 0 || t >= len) continue;
-            shut ? scan_again<true, T>(u, x, c, from, restart) : scan_again<false, T>(u, x, c, from, restart);
-            shut ? scan_deltas<true, T>(dy, x, u, c, in, add, restart) : scan_deltas<false, T>(dy, x, u, c, in, add, restart);
-            if (p.dx.p) scan_write<T>(dy, p, p.dx, seq, at, t, len);
-            if (p.dgate.p) scan_write<T>(x, p, p.dgate, seq, at, t, len);
-            scan_sum(sum, rest, add);
+            for (int to = warp; to < cluster; to += W)
+                scan_store_in(smem_addr(&parts[parity][rank][lane]), (uint32_t)to, make_float4(all.x, all.y, k.x, k.y));
         }
-        if (p.last && rank == 0 && warp == 0) scan_store2(p.last + (long long)seq * p.width + at.c, at.n, e);
+        scan_cluster_arrive();
+        next.refill(p, seq, at, t, len, tile * cluster);
+        next.state(p, seq, at, t - tile * cluster, len, lane);
+        float4 behind = make_float4(0.0f, 0.0f, 1.0f, 1.0f);  // what this CTA's runs behind this one do
+        for (int w = W - 1; w > warp; --w) {
+            const float4 o = runs[parity][w][lane];
+            const float2 r = scan_back(o, make_float2(behind.x, behind.y));
+            behind = make_float4(r.x, r.y, scan_through(behind.z, o.z), scan_through(behind.w, o.w));
+        }
+        scan_cluster_wait();
+        for (int k = 0; k < cluster; ++k) {
+            if (k == rank) in = e;
+            e = scan_back(parts[parity][k][lane], e);
+        }
+        in = scan_back(behind, in);
+        if (t < 0 || t >= len) continue;
+        shut ? scan_again<true, T>(u, x, c, from, restart) : scan_again<false, T>(u, x, c, from, restart);
+        shut ? scan_deltas<true, T>(dy, x, u, c, in, add, restart) : scan_deltas<false, T>(dy, x, u, c, in, add, restart);
+        if (p.dx.p) scan_write<T>(dy, p, p.dx, seq, at, t, len);
+        if (p.dgate.p) scan_write<T>(x, p, p.dgate, seq, at, t, len);
+        scan_sum(sum, rest, add);
     }
-    scan_sums<W>(reinterpret_cast<float2 *>(&runs[0][0][0]), sum, p, at, part * cluster + rank, warp, lane);
+    if (p.last && rank == 0 && warp == 0) scan_store2(p.last + (long long)seq * p.width + at.c, at.n, e);
+    scan_sums<W>(reinterpret_cast<float2 *>(&runs[0][0][0]), sum, p, at, seq * cluster + rank, warp, lane);
 }
 
 // dbias = the sum of its parts, in order: eight threads a channel.
@@ -1087,9 +1085,10 @@ cudaError_t scan_backward(ScanParams &p, cudaStream_t s)
     constexpr int bytes = ScanRing<T, 3, SHIFT>::kBytes, wide = sizeof(T) == 4 ? 8 : SHIFT ? 12 : 16;  // what shared memory holds
     p.cluster = 1;
     bool done = false;
-    const cudaError_t e = SCAN_SPLIT((k_scan_backward_split<T, wide, SHIFT>), units, wide, 2, &done);
+    cudaError_t e = cudaSuccess;
+    if (p.seq_parts == p.n_seq) e = SCAN_SPLIT((k_scan_backward_split<T, wide, SHIFT>), units, wide, 2, &done);  // (as it is with few units)
     if (done || e != cudaSuccess) return e;
-    switch (scan_warps(units, p.n_steps, sizeof(T) == 4 ? 8 : 12, scan_backward_warps<T>)) {
+    switch (p.seq_parts < p.n_seq ? 1 : scan_warps(units, p.n_steps, sizeof(T) == 4 ? 8 : 12, scan_backward_warps<T>)) {
     case 1: return SCAN_LAUNCH((k_scan_backward<T, 1, SHIFT>), (units + kScanLoneWarps - 1) / kScanLoneWarps, 1);
     case 2: return SCAN_LAUNCH((k_scan_backward<T, 2, SHIFT>), units, 2);
     case 4: return SCAN_LAUNCH((k_scan_backward<T, 4, SHIFT>), units, 4);
