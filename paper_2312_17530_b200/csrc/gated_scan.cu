@@ -1098,10 +1098,11 @@ cudaError_t scan_backward(ScanParams &p, cudaStream_t s)
     return cudaErrorInvalidValue;
 }
 
-// A strided operand: its rows do not overlap, its values are aligned.
-int scan_view_check(const ScanView &v, int64_t n, int64_t t, int64_t d, int elem)
+// A strided operand: its values are aligned, the rows of a result do not overlap.
+int scan_view_check(const ScanView &v, int64_t n, int64_t t, int64_t d, int elem, bool result)
 {
     if (!v.p || (t > 1 && v.step < d) || (n > 1 && v.seq < d)) return RSDGC_ERR_INVALID;
+    if (result && !rows_apart(n, v.seq, t, v.step, d)) return RSDGC_ERR_INVALID;
     return pointer_aligned(v.p, elem) ? RSDGC_OK : RSDGC_ERR_ALIGNMENT;
 }
 
@@ -1135,7 +1136,7 @@ extern "C" int rsdgc_gated_scan_forward(const void *x_dev, int64_t x_seq, int64_
     const int elem = dtype_bytes(dtype);
     if (n_steps > 0) {
         for (const ScanView *v : {&p.x, &p.gate, &p.y})
-            if ((rc = scan_view_check(*v, n_seq, n_steps, width, elem))) return rc;
+            if ((rc = scan_view_check(*v, n_seq, n_steps, width, elem, v == &p.y))) return rc;
         if (restart_dev && n_seq > 1 && restart_stride < n_steps) return RSDGC_ERR_INVALID;
     }
     if (!pointer_aligned(gate_bias_dev, dtype_bytes(param_dtype)) || !pointer_aligned(first_dev, 4) || !pointer_aligned(last_dev, 4) ||
@@ -1186,9 +1187,9 @@ extern "C" int rsdgc_gated_scan_backward(const void *dy_dev, int64_t dy_seq, int
     const int elem = dtype_bytes(dtype);
     if (n_seq > 0 && n_steps > 0) {
         for (const ScanView *v : {&p.x, &p.gate, &p.y})
-            if ((rc = scan_view_check(*v, n_seq, n_steps, width, elem))) return rc;
+            if ((rc = scan_view_check(*v, n_seq, n_steps, width, elem, false))) return rc;
         for (const ScanView *v : {&p.dx, &p.dgate})
-            if (v->p && (rc = scan_view_check(*v, n_seq, n_steps, width, elem))) return rc;
+            if (v->p && (rc = scan_view_check(*v, n_seq, n_steps, width, elem, true))) return rc;
         if (!states_dev || (restart_dev && n_seq > 1 && restart_stride < n_steps)) return RSDGC_ERR_INVALID;
         if (dbias_dev && !workspace_dev) return RSDGC_ERR_INVALID;
     }

@@ -66,6 +66,22 @@ cudaError_t operators_ready()
     return e;
 }
 
+bool rows_apart(int64_t n, int64_t a, int64_t m, int64_t b, int64_t width)
+{
+    if (n <= 1 || m <= 1) return true;
+    if (a < b) return rows_apart(m, b, n, a, width);
+    typedef __int128 wide;
+    const wide reach = (wide)(m - 1) * b;            // of the rows for one i
+    if (a >= reach + width) return true;
+    if (b >= (wide)(n - 1) * a + width) return true;
+    for (wide i = 1; i < n && i * a < reach + width; ++i) {
+        // the j on either side of i a
+        const wide j = i * a / b, over = i * a - j * b;
+        if ((over < width && j < m) || (b - over < width && j + 1 < m)) return false;
+    }
+    return true;
+}
+
 int current_device_sms()
 {
     static std::mutex mu;

@@ -143,6 +143,9 @@ cudaError_t orthogonal_debug_bounds(unsigned int *seen);
 #define RSDGC_DEFINE_DEBUG_BOUNDS(name)
 #endif
 
+// Whether rows of `width` values at i a + j b (i < n, j < m; a, b >= width where there are several) have no value in common.
+bool rows_apart(int64_t n, int64_t a, int64_t m, int64_t b, int64_t width);
+
 // The status word of calls that take no plan: one per device, raised by the kernels, read and cleared by
 // rsdgc_operator_status().  *out is its device address on the current device.
 cudaError_t operator_status_ptr(unsigned int **out);

@@ -1126,7 +1126,8 @@ extern "C" int rsdgc_orthogonalize(const void *x_dev, int64_t x_row_stride, int6
     if (!ortho_bounded(coefficients_host, n_steps, &about)) return RSDGC_ERR_INVALID;
     if (n_matrices == 0 || n_rows == 0 || n_cols == 0) return RSDGC_OK;
     if (!x_dev || !out_dev || !workspace_dev || (n_rows > 1 && (x_row_stride < n_cols || out_row_stride < n_cols)) ||
-        (n_matrices > 1 && (x_matrix_stride < n_cols || out_matrix_stride < n_cols)))
+        (n_matrices > 1 && (x_matrix_stride < n_cols || out_matrix_stride < n_cols)) ||
+        !rows_apart(n_matrices, out_matrix_stride, n_rows, out_row_stride, n_cols))
         return RSDGC_ERR_INVALID;
     if (!pointer_aligned(x_dev, dtype_bytes(dtype)) || !pointer_aligned(out_dev, 2) || !pointer_aligned(workspace_dev, 256))
         return RSDGC_ERR_ALIGNMENT;
