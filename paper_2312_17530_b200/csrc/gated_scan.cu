@@ -12,15 +12,15 @@
 // memory while a run is computed.  Three ways to deal the runs, by how many (sequence, 64 channels) units there are:
 //  - every warp walks a unit of its own (W = 1);
 //  - a CTA's W warps take a unit's runs in turn and hand the state on from warp to warp.  With W = 8 and 12 the critical path is not a run's 16
-//    steps but one step of its (L, Q), which the warp has formed beforehand: 4 x 8192 x 2048 bfloat16, 128 units: 115 us before, 74 us after;
+//    steps but one step of its (L, Q), which the warp has formed beforehand: 4 x 8192 x 2048 bfloat16, 128 units: 113 us without, 80 us with;
 //  - few units: the CTAs of a cluster take W runs each side by side, tell one another what those do to a state, and each run starts from
-//    the state that follows (1 x 65536 x 1024 binary16: 469 us with one CTA a unit, 180 us with 7).
+//    the state that follows (1 x 65536 x 1024 binary16: 534 us with one CTA a unit, 180 us with 7).
 // Runs are joined in the order of time, whoever is first: results are the same bits from call to call.
 // Rows that do not start on 16-byte boundaries arrive in 16-byte pieces too, one more a row, and are shifted when they are read
-// (8 x 4096 x 2047 bfloat16: 129 us forward, 594 us with loads of single values).
+// (8 x 4096 x 2047 bfloat16: 137 us forward, 594 us with loads of single values).
 //
-// What bounds it: memory where there are units for all multiprocessors (8 x 4096 x 4096 bfloat16: 153 us forward, 5.2 TB/s; 253 us
-// backward, 5.3 TB/s), the instructions of a run on the units' multiprocessors where there are not.
+// What bounds it: memory where there are units for all multiprocessors (8 x 4096 x 4096 bfloat16: 154 us forward, 5.2 TB/s; 257 us
+// backward, 5.2 TB/s), the instructions of a run on the units' multiprocessors where there are not.
 #include <atomic>
 #include <climits>
 #include <mutex>
@@ -40,7 +40,7 @@ constexpr int kScanLoneWarps = 4;   // of a CTA whose warps walk alone
 constexpr int kScanAhead = 8;       // chains of so many warps and more hand a state on before they compute their run's steps
 
 // Warps of a multiprocessor that the registers are cut for.  Few with many registers do better than many with few: backward with
-// 8 warps 253 us, with 12 warps 286 us, with 16 261 us, with 6 407 us (8 x 4096 x 4096 bfloat16); a chain of 12 has a multiprocessor to itself.
+// 8 warps 257 us, with 12 warps 294 us, with 16 379 us, with 6 424 us (8 x 4096 x 4096 bfloat16); a chain of 12 has a multiprocessor to itself.
 template <typename T>
 constexpr int scan_forward_warps(int w) { return sizeof(T) == 4 || w == 12 ? 12 : 16; }
 template <typename T>
@@ -68,8 +68,8 @@ struct ScanParams {
     int vec, wide;                  // results: pairs of channels may be written at once; operands: rows start on 16-byte boundaries
 };
 
-// The cluster's barrier in two halves: what lies between them needs nothing of the other CTAs (1 x 65536 x 2048 bfloat16: 287 us with the
-// copies' issue and the CTA's own joins before it, 256 us with them between)
+// The cluster's barrier in two halves: what lies between them needs nothing of the other CTAs (1 x 65536 x 2048 bfloat16: 358 us with the
+// copies' issue and the CTA's own joins before it, 262 us with them between)
 __device__ __forceinline__ void scan_cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void scan_cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void scan_store_in(uint32_t addr, uint32_t rank, float4 v)  // to a CTA of the cluster
@@ -1014,8 +1014,8 @@ cudaError_t scan_launch(K kernel, std::atomic<uint64_t> &ready, unsigned grid, i
     }()
 
 // The kernel that splits the steps, in clusters of p.cluster CTAs; *done = false if fewer than `least` would be on the device at
-// a time with all units: a second wave costs more than the split gains (16 units of 65536 steps: 287 us with 8 CTAs each, of which 15
-// clusters fit, 192 us with 7).
+// a time with all units: a second wave costs more than the split gains (16 units of 65536 steps, binary16: 278 us with 8 CTAs each, of which
+// 15 clusters fit, 180 us with 7).
 template <typename K>
 cudaError_t scan_split(K kernel, std::atomic<uint64_t> &ready, std::atomic<int> (&fit)[64][kScanCluster + 1], long long units, int warps,
                        int bytes, int least, cudaStream_t s, ScanParams &p, bool *done)
@@ -1066,8 +1066,9 @@ cudaError_t scan_forward(ScanParams &p, cudaStream_t s)
     constexpr int bytes = ScanRing<T, 2, SHIFT>::kBytes, wide = sizeof(T) == 4 ? 8 : 16;
     p.cluster = 1;
     bool done = false;
-    // with 2 CTAs a unit the joins take as long as they save: 2 x 8192 x 2048 bfloat16 79 us, 72 us with a chain of 12 (backward 108 and 209 us)
-    const cudaError_t e = SCAN_SPLIT((k_scan_forward_split<T, wide, SHIFT>), units, wide, 3, &done);
+    // Two CTAs of 8 warps, binary32's, do not make up for their joins: 2 x 8192 x 2048 104 us, 80 us with a chain of 12.  Two of 16 warps do (bfloat16
+    // 72 and 78 us, 3 x 4000 x 1400 binary16 51 and 60), and so do two in the backward pass (113 and 129 us, binary32 158 and 159).
+    const cudaError_t e = SCAN_SPLIT((k_scan_forward_split<T, wide, SHIFT>), units, wide, wide == 16 ? 2 : 3, &done);
     if (done || e != cudaSuccess) return e;
     switch (scan_warps(units, p.n_steps, 12, scan_forward_warps<T>)) {
     case 1: return SCAN_LAUNCH((k_scan_forward<T, 1, SHIFT>), (units + kScanLoneWarps - 1) / kScanLoneWarps, 1);

@@ -20,8 +20,8 @@ ONE = (1,)
     (200, 700, 64, ((8, ONE), (4, ONE)), ((8, ONE), (4, ONE))),
     (140, 700, 64, ((12, ONE), (12, ONE)), ((12, ONE), (8, ONE))),
     (140, 175, 64, ((8, ONE), (8, ONE)), ((8, ONE), (8, ONE))),
-    # two CTAs do in the backward pass only; 16 warps of each take aligned rows of 16-bit types, 12 others
-    (7, 1100, 520, ((12, ONE), (0, (2,))), ((12, ONE), (8, (2,)))),
+    # two CTAs; forward not in binary32.  In the backward pass 16 warps of each take aligned rows of 16-bit types, 12 others
+    (7, 1100, 520, ((16, (2,)), (0, (2,))), ((12, ONE), (8, (2,)))),
     (1, 2100, 64, ((16, (4,)), (0, (4, 5))), ((8, (8,)), (8, (8,)))),
     # 17 groups: eight CTAs each, or as many as the device holds of all of them at a time
     (1, 4200, 1032, ((16, (6, 7, 8)), (0, (6, 7, 8))), ((8, (6, 7, 8)), (8, (6, 7, 8))))])
