@@ -459,7 +459,7 @@ int rsdgc_head_distill_backward(const void *hidden_dev, int64_t hidden_stride, c
  * (texts packed one behind the other).  lengths_dev: optional, int64 per sequence, clamped to 0 .. n_steps: the steps behind it
  * are neither read nor written, `last` is the state there.  states_dev: optional, what the backward pass takes: binary32,
  * n_seq x ceil(n_steps / RSDGC_SCAN_STATE_STEPS) x width.  The state is binary32 throughout; one that is no longer finite stays
- * not finite until a restart.  1 - a is within (3 |gate + bias| + 16) 2^-24 of itself, and so is a where it is below 1/33; above, a is within 2^-17.
+ * not finite until a restart (an infinity may become NaN, in dbias's sum as well).  A step forms x - h: both are to be below 2^127 in size.  1 - a is within (3 |gate + bias| + 16) 2^-24 of itself, and so is a where it is below 1/33; above, a is within 2^-17.
  * n_seq = 0 does nothing.
  * Errors: INVALID (a needed pointer NULL, a stride too small, results that overlap, sizes < 0, width < 1, types), ALIGNMENT (a pointer that is not a
  * multiple of its element size), CAPACITY (n_seq or n_steps > 2^30, width > 2^24, n_seq * ceil(width / 64) > 2^28 - 1), CUDA.

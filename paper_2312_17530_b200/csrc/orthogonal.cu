@@ -17,11 +17,11 @@
 // written a second time across it.  Y is read as it lies, once with its rows and once with its columns contracted.  Where A has
 // few tiles and a long contraction, the contraction is cut into parts which k_ortho_join adds up, in order.
 //
-// What bounds it: the tensor cores where matrices are large (4096 x 4096: 1088 cycles a step of 1024 cycles of MMAs); latency where they are
-// small (256 x 512: 141 us, 17 launches of 8 us each: 0.8 us until the first operands are there, 0.16 us a contraction step, 2.5 us of epilogue,
-// the rest is a launch's; all products in one launch, whose CTAs count one another's epilogues, were 8 % faster at 256 x 512 and 9 % slower at
-// 2048 x 2048: not worth its waits); the epilogue's
-// memory traffic where one side is far longer than the other.
+// What bounds it.  Large matrices: the tensor cores are busy for 52 to 62 % of a product (4096 x 4096; a step of the main loop takes 1088 cycles of
+// which 1024 are MMAs), the rest are the first operands' way, epilogues that nothing covers and rounds of tiles that are not full.  Small ones:
+// latency (256 x 512: 143 us, 17 launches of 8 us each: 0.8 us until the first operands are there, 0.16 us a contraction step, 2.5 us of epilogue, the
+// rest is a launch's; all products in one launch, whose CTAs count one another's epilogues, were 8 % faster at 256 x 512 and 9 % slower at
+// 2048 x 2048: not worth its waits).  One side far longer than the other: the epilogue's memory traffic (tensor cores 26 %, 3 TB/s).
 #include <climits>
 #include <cmath>
 #include <cstring>
@@ -319,8 +319,8 @@ __global__ void __launch_bounds__(kOrthoThreads, 1) k_ortho(const __grid_constan
 
     if (warp < 4) {
         // One thread of each of two warps walks alone: a stage of the ring is 256 to 512 cycles of MMAs, which a loop that the whole warp
-        // walks, with coordinates formed and parameters read anew for each box, takes longer to issue (some 700 cycles a step; 320 so.  2048 x 2048: 425
-        // and 281 us).
+        // walks, with coordinates formed and parameters read anew for each box, takes longer to issue (some 700 cycles a step; 320 so.  2048 x 2048: 425 us
+        // then, 275 us with this and what else has changed since).
         if (warp == 0 && elect_one()) {  // ---- producer, in both CTAs; all bytes count on the first CTA's barriers
             int stage = 0, it = 0;
             uint32_t parity = 0, dst = ring;
@@ -764,7 +764,7 @@ RSDGC_DEFINE_DEBUG_BOUNDS(orthogonal_debug_bounds)
 namespace {
 
 constexpr int kOrthoPairs = 74;          // of CTAs on the device, for what workspaces depend on
-constexpr int kOrthoLoadParts = 1184;    // most CTAs per matrix of the two passes over X: eight a multiprocessor (two: 32000 x 1024 859 us, 830 us so)
+constexpr int kOrthoLoadParts = 1184;    // most CTAs per matrix of the two passes over X: eight a multiprocessor (two: 32000 x 1024 36 us more)
 // Shorter sides up to this take three products for every result: there they cost a fifth of the call at most, beyond it more and more (bfloat16
 // results, one product and three: 128 x 512 122 and 142 us, 256 x 512 126 and 151, 24 x 256 x 1024 217 and 257, 512 x 1024 153 and 196, 8 x 512 x
 // 1024 192 and 261, 1024 x 1024 171 and 271).
