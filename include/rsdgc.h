@@ -453,13 +453,15 @@ int rsdgc_head_distill_backward(const void *hidden_dev, int64_t hidden_stride, c
  * Gated scan: a recurrence over the steps of each of n_seq sequences, channel by channel (`width` channels):
  *   a[t] = 1 / (1 + exp(-(gate[t] + gate_bias))),  h[t] = a[t] * h[t-1] + (1 - a[t]) * x[t],  y[t] = h[t].
  * x, gate, y: `dtype`, [sequence][step][channel], channels contiguous, any strides of sequences and steps (in elements; >= width
- * where there are several; the rows of y, and below of dx and dgate, do not overlap).  gate_bias: optional (0), one value per channel, param_dtype (`dtype` or binary32).
+ * where there are several; the rows of y, and below of dx and dgate, do not overlap).  gate_bias: optional (0), one value per
+ * channel, param_dtype (`dtype` or binary32).
  * first_dev, last_dev: optional, binary32, n_seq x width: the state before the first step (0) and behind the last; they
  * may be the same array.  restart_dev: optional, one byte per step with a row stride; where it is not 0 the step's h[t-1] is 0
  * (texts packed one behind the other).  lengths_dev: optional, int64 per sequence, clamped to 0 .. n_steps: the steps behind it
  * are neither read nor written, `last` is the state there.  states_dev: optional, what the backward pass takes: binary32,
  * n_seq x ceil(n_steps / RSDGC_SCAN_STATE_STEPS) x width.  The state is binary32 throughout; one that is no longer finite stays
- * not finite until a restart (an infinity may become NaN, in dbias's sum as well).  A step forms x - h: both are to be below 2^127 in size.  1 - a is within (3 |gate + bias| + 16) 2^-24 of itself, and so is a where it is below 1/33; above, a is within 2^-17.
+ * not finite until a restart (an infinity may become NaN, in dbias's sum as well).  A step forms x - h: both are to be below 2^127 in
+ * size.  1 - a is within (3 (|gate| + |gate_bias|) + 16) 2^-24 of itself, and so is a where it is below 1/33; above, a is within 2^-17.
  * n_seq = 0 does nothing.
  * Errors: INVALID (a needed pointer NULL, a stride too small, results that overlap, sizes < 0, width < 1, types), ALIGNMENT (a pointer that is not a
  * multiple of its element size), CAPACITY (n_seq or n_steps > 2^30, width > 2^24, n_seq * ceil(width / 64) > 2^28 - 1), CUDA.
@@ -496,8 +498,8 @@ int rsdgc_gated_scan_backward(const void *dy_dev, int64_t dy_seq, int64_t dy_ste
  * singular values near 1, by n_steps odd polynomials (Newton-Schulz steps) with the coefficients (a, b, c) of each:
  *   Y = X / (|X|_F + eps);  per step Y = a Y + (b A + c A A) Y with A = Y Y^T.
  * (3.4445, -4.7750, 2.0315) five times brings singular values of 0.01 .. 1 of the largest to about 0.7 .. 1.2.
- * x: `dtype`; out: out_dtype, bfloat16 or binary16; row and matrix strides in elements, any alignment; out's rows do not overlap.  coefficients_host: 3 * n_steps
- * binary32 on the host, read during the call; n_steps 1 to 32.  workspace_dev: rsdgc_orthogonalize_workspace_bytes() bytes, 256-byte
+ * x: `dtype`; out: out_dtype, bfloat16 or binary16; row and matrix strides in elements, any alignment; out's rows do not
+ * overlap.  coefficients_host: 3 * n_steps binary32 on the host, read during the call; n_steps 1 to 32.  workspace_dev: rsdgc_orthogonalize_workspace_bytes() bytes, 256-byte
  * aligned; nothing in it has to survive between calls.  A matrix of zeros gives zeros, one that is not finite NaN.
  * Accuracy: sums in binary32, operands of 11 bits (22 for a Y).  For binary16 results, and where the shorter side has at most 256, each product is made
  * of three with 22-bit operands (a caller who wants those for larger sides takes a binary16 result).  With the coefficients above the result, its own

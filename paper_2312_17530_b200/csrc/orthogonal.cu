@@ -4,13 +4,14 @@
 //   Y = X / (|X|_F + eps);   A = Y Y^T,  B = b A + c A^2,  Y <- a Y + B Y   with (a, b, c) of the step;   A = Y^T Y and Y <- a Y + Y B for
 //   matrices with more rows than columns, so that A has the shorter side
 //
-// Numbers.  The products' operands are binary16 (11 bits; bfloat16's 8 leave an error of 0.01, and 0.07 where a few directions carry
-// the gradient), scaled by powers of two: Y by 2^12, A by 2^13, B by 2^13 or, where it is larger than 7.5, 2^12 or 2^11.  The host refuses coefficients with which Y could outgrow
-// them.  The small directions are brought up by a, step after step, while B Y is small there: so Y itself is kept in
-// two binary16 planes, the rounded value and the rest (22 bits), for a Y, which is added in binary32.  That costs bytes and no
-// product (gradient of 16 directions plus 3 % noise: error 1.6e-4 with it, 9e-3 without).  A matrix whose norm is small beside eps begins
-// with small singular values in all directions: its planes have a power of two more, step by step, so that they are as full as another's.  Where one product's 11 bits do not do - a binary16
-// result, small matrices - A and B have two planes too and each product is three: hi hi + hi lo + lo hi.
+// Numbers.  The products' operands are binary16 (11 bits; bfloat16's 8 leave an error of 0.01, and 0.07 where a few directions carry the
+// gradient), scaled by powers of two: Y by 2^12, A by 2^13, B by 2^13 or, where it is larger than 7.5, 2^12 or 2^11.  The host refuses
+// coefficients with which Y could outgrow them.  The small directions are brought up by a, step after step, while B Y is small there: so
+// Y itself is kept in two binary16 planes, the rounded value and the rest (22 bits), for a Y, which is added in binary32.  That costs
+// bytes and no product (gradient of 16 directions plus 3 % noise: error 1.6e-4 with it, 9e-3 without).  A matrix whose norm is small
+// beside eps begins with small singular values in all directions: its planes have a power of two more, step by step, so that they are as
+// full as another's.  Where one product's 11 bits do not do - a binary16 result, small matrices - A and B have two planes too and each
+// product is three: hi hi + hi lo + lo hi.
 //
 // The products are one tile kernel, pairs of CTAs as for the vocabulary head: TMA brings the operands through a ring, one
 // thread issues the MMAs, sixteen warps empty the accumulator.  A and B are symmetric: tiles on and below the diagonal are computed, and
